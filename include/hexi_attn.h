@@ -158,6 +158,95 @@ int hexi_attn_bwd_chunk(const hexi_attn_desc* desc, const hexi_range* q_range, c
                         void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Attention with a sliding window and sink tokens on the same shards and chunks: key j is visible to query row i iff
+ *   pos(j) <= pos(i)  and  (pos(i) - pos(j) < window  or  pos(j) < n_sink).
+ * The window counts the row's own token (window = 1: itself alone); n_sink first tokens of the sequence stay visible.
+ * window >= 1, n_sink >= 0; both may exceed the sequence.
+ * Under a window a device needs only its own keys, the window - 1 keys before each of its segments and the sinks: one
+ * kv_range of these (up to HEXI_MAX_SEGS segments) and one call replace the ring.  A ring of chunks works as well, through
+ * the same accumulation as without a window.  Keys that no row sees cost nothing but their zeros in dk and dv.
+ */
+typedef struct { int64_t window, n_sink; } hexi_window;
+
+/* Bytes of device workspace that hexi_attn_win_fwd_chunk needs for this descriptor and window and these lengths, 0 for
+ * most (0 too for arguments that the call refuses).  Nothing is kept in it between calls; calls that may run at the same
+ * time, replays of captured graphs among them, need one each. */
+size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc);
+
+/*
+ * hexi_attn_fwd_chunk under a window.  o has the element type o_dtype: HEXI_F32 as there, HEXI_ACCUMULATE included, or
+ * HEXI_BF16: the result rounded once, dense [Lq][nq][d], for a chunk that holds all keys of the shard's rows
+ * (HEXI_ACCUMULATE is HEXI_EINVAL then).  Rows that see no key get o = 0, lse = -INFINITY.  Values of keys that a row does
+ * not see do not reach it, infinities and NaN included.  workspace: hexi_attn_win_workspace_bytes() bytes, 16-byte
+ * aligned (HEXI_EWORKSPACE if smaller); may be NULL where that is 0.
+ */
+int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_window* window,
+                            const hexi_range* q_range, const hexi_range* kv_range,
+                            const void* q, const void* k, const void* v,
+                            void* o, int32_t o_dtype, float* lse, uint32_t flags,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * hexi_attn_bwd_chunk under a window.  o (read under HEXI_COMPUTE_DELTA alone) has the element type o_dtype.  grad_dtype
+ * HEXI_F32: dq_acc, dk and dv as there (dq is added to, dk and dv are overwritten or added to under HEXI_ACCUMULATE).
+ * HEXI_BF16: dq, dk and dv are overwritten with the results of this chunk rounded once, for a shard whose keys all lie in
+ * it (HEXI_ACCUMULATE is HEXI_EINVAL then).  All sums have a fixed order: results are reproducible run to run.  Calls that
+ * add to the same dq_acc, dk or dv must be ordered.  hexi_set_dkdv_run_len() has no effect here.  Rows whose lse is
+ * infinite have P = 0.  No workspace.
+ */
+int hexi_attn_win_bwd_chunk(const hexi_attn_desc* desc, const hexi_window* window,
+                            const hexi_range* q_range, const hexi_range* kv_range,
+                            const void* q, const void* k, const void* v, const void* o, int32_t o_dtype, const void* d_o,
+                            const float* lse, float* delta,
+                            void* dq, void* dk, void* dv, int32_t grad_dtype, uint32_t flags, void* hip_stream);
+
+/*
+ * Rotary positions with one or several axes (time, height, width) on the rows of a shard.  Of every row of every head the
+ * first rot_dim columns are rotated in pairs, the others copied:
+ *   angle = position[axis_of_pair[p]] * inv_freq[p],  (a, b) -> (a cos - b sin, b cos + a sin),  p = 0 .. rot_dim / 2 - 1
+ * with (a, b) = columns (p, p + rot_dim / 2) for HEXI_ROPE_HALF or (2 p, 2 p + 1) for HEXI_ROPE_ADJACENT.  HEXI_ROPE_INVERSE
+ * rotates by -angle, which is both the inverse and the gradient.  Angles are formed in 64 bits, so far positions
+ * lose nothing; sine, cosine and the products are fp32, and the result is rounded once.
+ *
+ * head_dim and rot_dim are multiples of 16, 16 <= rot_dim <= head_dim <= 256.  inv_freq: HOST double[rot_dim / 2], |.| <= 2^20;
+ * axis_of_pair: HOST int8_t[rot_dim / 2] in [0, n_axes), or NULL for axis 0 throughout; both are copied during the call.
+ * 1 <= n_axes <= HEXI_ROPE_MAX_AXES.
+ * range: the shard; its packed rows are the tensors' rows.  positions: DEVICE int32[n_axes][pos_stride], pos_stride >= rows
+ * (entry [a][r] is row r's position on axis a, negative ones allowed), or NULL: the rows' global positions on every axis.
+ */
+#define HEXI_ROPE_HALF 0
+#define HEXI_ROPE_ADJACENT 1
+#define HEXI_ROPE_INVERSE 16u
+#define HEXI_ROPE_MAX_AXES 4
+#define HEXI_ROPE_MAX_DIM 256
+#define HEXI_ROPE_MAX_TENSORS 4
+typedef struct {
+    int32_t head_dim, rot_dim;
+    int32_t pairing;              /* HEXI_ROPE_HALF | HEXI_ROPE_ADJACENT */
+    int32_t n_axes;
+    const double* inv_freq;
+    const int8_t* axis_of_pair;
+} hexi_rope_desc;
+
+/* One tensor of a call: x [rows][n_heads][head_dim] -> y, strides in elements, head_dim stride 1.  y may be x itself
+ * (same pointer, strides and element type); otherwise the two do not overlap. */
+typedef struct {
+    const void* x;
+    void* y;
+    int32_t n_heads;
+    int64_t x_stride_tok, x_stride_head, y_stride_tok, y_stride_head;
+} hexi_rope_tensor;
+
+/*
+ * Rotates the n_tensors (1 .. HEXI_ROPE_MAX_TENSORS) tensors of a shard, q and k for instance, in one launch.  All have the element type
+ * x_dtype and results of y_dtype (HEXI_BF16 or HEXI_F32 each: the fp32 sums of the attention's backward become bf16
+ * gradients on the way).  Strides of at least head_dim elements, a tensor within 2^40 elements of its first.  Pointers and
+ * strides are multiples of 16 bytes (HEXI_EALIGN).
+ */
+int hexi_rope(const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+              const hexi_rope_tensor* tensors, int32_t n_tensors, int32_t x_dtype, int32_t y_dtype, uint32_t flags, void* hip_stream);
+
+/*
  * Head redistribution either side of the ring (Sec. 3.2: heterogeneous all-to-all with per-rank split
  * tables; sub-ring KV exchange, where non-contiguous head slices are packed into contiguous buffers
  * before transfer; App. A.4: the part for rank j is s * n_j * d_h elements per tensor).
@@ -185,6 +274,22 @@ int hexi_a2a_pack(const void* x, void* packed, int64_t s, int32_t n_heads_total,
 int hexi_a2a_unpack(const void* packed, void* y, int64_t s, int32_t n_heads_total, int32_t head_dim, int32_t elem_bytes,
                     int64_t y_stride_tok, int32_t n_ranks, const int32_t* heads_per_rank, const int32_t* head_list,
                     void* hip_stream);
+
+/*
+ * The redistribution with the rotation of hexi_rope on the way, for a fused q / k / v shard: hexi_rope_a2a_pack rotates the heads
+ * of x whose entry of rotate (HOST uint8_t[n_heads_total]) is not zero and copies the others; hexi_rope_a2a_unpack puts
+ * what comes back into y, rotated by -angle (the gradients' way; with HEXI_ROPE_INVERSE each goes the other way).  Tables, layouts,
+ * limits and refusals are those of hexi_a2a_pack / hexi_a2a_unpack, for elements of type dtype (HEXI_BF16 or HEXI_F32) and
+ * s = the rows of range; desc, range and positions are those of hexi_rope.
+ */
+int hexi_rope_a2a_pack(const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+                       const void* x, void* packed, int32_t n_heads_total, int32_t dtype, int64_t x_stride_tok,
+                       int32_t n_ranks, const int32_t* heads_per_rank, const int32_t* head_list, const uint8_t* rotate,
+                       uint32_t flags, void* hip_stream);
+int hexi_rope_a2a_unpack(const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+                         const void* packed, void* y, int32_t n_heads_total, int32_t dtype, int64_t y_stride_tok,
+                         int32_t n_ranks, const int32_t* heads_per_rank, const int32_t* head_list, const uint8_t* rotate,
+                         uint32_t flags, void* hip_stream);
 
 /*
  * Host-side performance model and hierarchical scheduler (Sec. 4: formalization, performance model,

@@ -3,19 +3,11 @@
 // x[s][N][d] into one contiguous [s][n_j][d] part per destination rank, and the inverse scatter.  Pure data
 // movement, HBM-bound: every 16-byte piece is read once and written once.
 #include "hexi_internal.h"
+#include "hexi_a2a_table.h"
 
 namespace {
 
 typedef unsigned int u4 __attribute__((ext_vector_type(4)));   // one 16-byte piece
-
-// One slot per (rank, head of that rank's list), in send-buffer order.
-struct A2ATable {
-    int n_slots;
-    unsigned short head[HEXI_A2A_MAX_SLOTS];        // head index in x
-    unsigned short n_j[HEXI_A2A_MAX_SLOTS];         // heads of the slot's rank
-    unsigned short local[HEXI_A2A_MAX_SLOTS];       // index of the head within its rank's list
-    unsigned short heads_before[HEXI_A2A_MAX_SLOTS];   // heads of all earlier ranks
-};
 
 constexpr int TOKENS_PER_BLOCK = 16;
 
@@ -62,18 +54,8 @@ hipError_t hexi_launch_a2a(bool pack, const void* x, void* packed, void* y, long
                            long long x_stride_bytes, int n_ranks, const int* heads_per_rank, const int* head_list, hipStream_t st)
 {
     A2ATable tb;
-    int slot = 0, before = 0;
-    for (int j = 0; j < n_ranks; ++j) {
-        for (int i = 0; i < heads_per_rank[j]; ++i, ++slot) {
-            tb.head[slot] = (unsigned short)head_list[slot];
-            tb.n_j[slot] = (unsigned short)heads_per_rank[j];
-            tb.local[slot] = (unsigned short)i;
-            tb.heads_before[slot] = (unsigned short)before;
-        }
-        before += heads_per_rank[j];
-    }
-    tb.n_slots = slot;
-    if (slot == 0 || s == 0) return hipSuccess;
+    hexi_build_a2a_table(n_ranks, heads_per_rank, head_list, &tb);
+    if (tb.n_slots == 0 || s == 0) return hipSuccess;
     const unsigned grid = (unsigned)((s + TOKENS_PER_BLOCK - 1) / TOKENS_PER_BLOCK);
     if (pack)
         a2a_kernel<true><<<grid, 256, 0, st>>>(tb, static_cast<const u4*>(x), static_cast<u4*>(packed), nullptr, s, row_bytes / 16,

@@ -6,6 +6,8 @@
 #include <cmath>
 #include <vector>
 #include "hexi_internal.h"
+#include "hexi_window.h"
+#include "hexi_rope.h"
 
 #define HEXI_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -250,9 +252,79 @@ HEXI_EXPORT int hexi_attn_bwd_chunk(const hexi_attn_desc* desc, const hexi_range
     return HEXI_OK;
 }
 
-static int a2a_call(bool pack, const void* x, void* packed, void* y, int64_t s, int32_t n_heads_total, int32_t head_dim,
-                    int32_t elem_bytes, int64_t stride_tok, int32_t n_ranks, const int32_t* heads_per_rank,
-                    const int32_t* head_list, void* hip_stream)
+// Checks a window and clamps it to what positions can reach.
+static int build_window(const hexi_window* w, int* window, int* n_sink)
+{
+    if (!w) return fail(HEXI_EINVAL, "null window");
+    if (w->window < 1 || w->n_sink < 0) return fail(HEXI_EINVAL, "window=%lld n_sink=%lld (window >= 1, n_sink >= 0)", (long long)w->window, (long long)w->n_sink);
+    *window = (int)(w->window < 2147483647LL ? w->window : 2147483647LL);
+    *n_sink = (int)(w->n_sink < 2147483647LL ? w->n_sink : 2147483647LL);
+    return HEXI_OK;
+}
+
+HEXI_EXPORT size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc*, const hexi_window*, int64_t, int64_t) { return 0; }
+
+HEXI_EXPORT int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_window* window, const hexi_range* q_range, const hexi_range* kv_range,
+                                       const void* q, const void* k, const void* v, void* o, int32_t o_dtype, float* lse, uint32_t flags,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    (void)workspace; (void)workspace_bytes;
+    WinFwdArgs a;
+    int rc = build_geom(desc, q_range, kv_range, &a.g);
+    if (rc == HEXI_OK) rc = build_window(window, &a.window, &a.n_sink);
+    if (rc != HEXI_OK) return rc;
+    if (!q || !k || !v || !o || !lse) return fail(HEXI_EINVAL, "null tensor pointer");
+    if (o_dtype != HEXI_F32 && o_dtype != HEXI_BF16) return fail(HEXI_EUNSUPPORTED, "o_dtype %d", o_dtype);
+    if (flags & ~(HEXI_ACCUMULATE)) return fail(HEXI_EINVAL, "unknown flag bits 0x%x", flags);
+    if ((flags & HEXI_ACCUMULATE) && o_dtype != HEXI_F32) return fail(HEXI_EINVAL, "HEXI_ACCUMULATE needs an fp32 o");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(lse))
+        return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned");
+    hipStream_t s = (hipStream_t)hip_stream;
+    a.q = q; a.k = k; a.v = v; a.o = (float*)o; a.lse = lse;
+    a.accumulate = (flags & HEXI_ACCUMULATE) ? 1 : 0;
+    a.out_bf16 = o_dtype == HEXI_BF16;
+    const hipError_t e = hexi_launch_win_fwd(a, desc->dtype, s);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "windowed forward launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
+}
+
+HEXI_EXPORT int hexi_attn_win_bwd_chunk(const hexi_attn_desc* desc, const hexi_window* window, const hexi_range* q_range, const hexi_range* kv_range,
+                                       const void* q, const void* k, const void* v, const void* o, int32_t o_dtype, const void* d_o,
+                                       const float* lse, float* delta, void* dq, void* dk, void* dv, int32_t grad_dtype, uint32_t flags, void* hip_stream)
+{
+    WinBwdArgs a;
+    int rc = build_geom(desc, q_range, kv_range, &a.g);
+    if (rc == HEXI_OK) rc = build_window(window, &a.window, &a.n_sink);
+    if (rc != HEXI_OK) return rc;
+    if (flags & ~(HEXI_ACCUMULATE | HEXI_COMPUTE_DELTA | HEXI_SKIP_DQ | HEXI_SKIP_DKDV)) return fail(HEXI_EINVAL, "unknown flag bits 0x%x", flags);
+    const bool want_dq = !(flags & HEXI_SKIP_DQ), want_dkdv = !(flags & HEXI_SKIP_DKDV), want_delta = (flags & HEXI_COMPUTE_DELTA) != 0;
+    if (!want_dq && !want_dkdv) return fail(HEXI_EINVAL, "HEXI_SKIP_DQ and HEXI_SKIP_DKDV are both set");
+    if ((want_delta && o_dtype != HEXI_F32 && o_dtype != HEXI_BF16) || (grad_dtype != HEXI_F32 && grad_dtype != HEXI_BF16))
+        return fail(HEXI_EUNSUPPORTED, "o_dtype %d, grad_dtype %d", o_dtype, grad_dtype);
+    if ((flags & HEXI_ACCUMULATE) && grad_dtype != HEXI_F32) return fail(HEXI_EINVAL, "HEXI_ACCUMULATE needs fp32 gradients");
+    if (!q || !k || !v || !d_o || !lse || !delta || (want_dq && !dq) || (want_dkdv && (!dk || !dv))) return fail(HEXI_EINVAL, "null tensor pointer");
+    if (want_delta && !o) return fail(HEXI_EINVAL, "HEXI_COMPUTE_DELTA needs o");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_o) || (want_dq && !aligned16(dq)) || (want_dkdv && (!aligned16(dk) || !aligned16(dv))) ||
+        !aligned16(lse) || !aligned16(delta) || (want_delta && !aligned16(o)))
+        return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned");
+    hipStream_t s = (hipStream_t)hip_stream;
+    a.q = q; a.k = k; a.v = v; a.d_o = d_o; a.lse = lse; a.delta = delta; a.dq = (float*)dq; a.dk = (float*)dk; a.dv = (float*)dv;
+    a.accumulate = (flags & HEXI_ACCUMULATE) ? 1 : 0;
+    a.want_dq = want_dq ? 1 : 0;
+    a.want_dkdv = want_dkdv ? 1 : 0;
+    a.out_bf16 = grad_dtype == HEXI_BF16;
+    hipError_t e = hipSuccess;
+    if (want_delta)
+        e = o_dtype == HEXI_F32 ? hexi_launch_delta(a.g.lq, a.g.nq, a.g.d, (const float*)o, d_o, desc->dtype, a.g.q_stride_tok, a.g.q_stride_head, delta, s)
+                                : hexi_launch_delta_bf16_o(a.g.lq, a.g.nq, a.g.d, o, d_o, desc->dtype, a.g.q_stride_tok, a.g.q_stride_head, delta, s);
+    if (e == hipSuccess) e = hexi_launch_win_bwd(a, desc->dtype, s);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "windowed backward launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
+}
+
+// Checks the tables and tensors of a redistribution: x the [s][heads] side, read or written.
+static int check_a2a(bool pack, const void* x, const void* packed, int64_t s, int32_t n_heads_total, int32_t head_dim,
+                     int32_t elem_bytes, int64_t stride_tok, int32_t n_ranks, const int32_t* heads_per_rank, const int32_t* head_list)
 {
     if (s < 0 || n_heads_total < 1 || n_heads_total > 65535 || head_dim < 1) return fail(HEXI_EINVAL, "bad sizes s=%lld heads=%d d=%d", (long long)s, n_heads_total, head_dim);
     if (elem_bytes != 2 && elem_bytes != 4) return fail(HEXI_EUNSUPPORTED, "elem_bytes %d", elem_bytes);
@@ -276,11 +348,19 @@ static int a2a_call(bool pack, const void* x, void* packed, void* y, int64_t s, 
         }
     }
     if (s > 0 && n_slots > 0) {
-        const void* a = pack ? x : y;
-        if (!a || !packed) return fail(HEXI_EINVAL, "null tensor pointer");
-        if (!aligned16(a) || !aligned16(packed)) return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned");
+        if (!x || !packed) return fail(HEXI_EINVAL, "null tensor pointer");
+        if (!aligned16(x) || !aligned16(packed)) return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned");
     }
-    hipError_t e = hexi_launch_a2a(pack, x, packed, y, s, n_heads_total, (int)row_bytes, stride_tok * elem_bytes, n_ranks,
+    return HEXI_OK;
+}
+
+static int a2a_call(bool pack, const void* x, void* packed, void* y, int64_t s, int32_t n_heads_total, int32_t head_dim,
+                    int32_t elem_bytes, int64_t stride_tok, int32_t n_ranks, const int32_t* heads_per_rank,
+                    const int32_t* head_list, void* hip_stream)
+{
+    const int rc = check_a2a(pack, pack ? x : y, packed, s, n_heads_total, head_dim, elem_bytes, stride_tok, n_ranks, heads_per_rank, head_list);
+    if (rc != HEXI_OK) return rc;
+    hipError_t e = hexi_launch_a2a(pack, x, packed, y, s, n_heads_total, head_dim * elem_bytes, stride_tok * elem_bytes, n_ranks,
                                    heads_per_rank, head_list, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(HEXI_EHIP, "a2a launch failed: %s", hipGetErrorString(e));
     return HEXI_OK;
@@ -298,4 +378,113 @@ HEXI_EXPORT int hexi_a2a_unpack(const void* packed, void* y, int64_t s, int32_t 
                                 void* hip_stream)
 {
     return a2a_call(false, nullptr, const_cast<void*>(packed), y, s, n_heads_total, head_dim, elem_bytes, y_stride_tok, n_ranks, heads_per_rank, head_list, hip_stream);
+}
+
+// Checks a rotation's descriptor, range and positions.
+static int build_rope(const hexi_rope_desc* d, const hexi_range* range, const int32_t* positions, int64_t pos_stride, uint32_t flags, bool inverse, RopeGeom* g)
+{
+    if (!d) return fail(HEXI_EINVAL, "null rope descriptor");
+    if (flags & ~HEXI_ROPE_INVERSE) return fail(HEXI_EINVAL, "unknown flag bits 0x%x", flags);
+    if (d->head_dim < 16 || d->head_dim > HEXI_ROPE_MAX_DIM || d->head_dim % 16 || d->rot_dim < 16 || d->rot_dim > d->head_dim || d->rot_dim % 16)
+        return fail(HEXI_EUNSUPPORTED, "head_dim %d, rot_dim %d (multiples of 16, 16 <= rot_dim <= head_dim <= %d)", d->head_dim, d->rot_dim, HEXI_ROPE_MAX_DIM);
+    if (d->pairing != HEXI_ROPE_HALF && d->pairing != HEXI_ROPE_ADJACENT) return fail(HEXI_EINVAL, "pairing %d", d->pairing);
+    if (d->n_axes < 1 || d->n_axes > HEXI_ROPE_MAX_AXES) return fail(HEXI_EINVAL, "n_axes %d outside 1..%d", d->n_axes, HEXI_ROPE_MAX_AXES);
+    if (!d->inv_freq) return fail(HEXI_EINVAL, "null inv_freq");
+    const int rc = build_segtable(range, "range", &g->range);
+    if (rc != HEXI_OK) return rc;
+    if (positions && pos_stride < g->range.total) return fail(HEXI_EINVAL, "pos_stride %lld smaller than the %d rows", (long long)pos_stride, g->range.total);
+    if (reinterpret_cast<uintptr_t>(positions) & 3u) return fail(HEXI_EALIGN, "positions must be 4-byte aligned");
+    const long double quarter_turns = 0.636619772367581343075535053490057448L;      // 2 / pi
+    for (int p = 0; p < d->rot_dim / 2; ++p) {
+        const int axis = d->axis_of_pair ? d->axis_of_pair[p] : 0;
+        if (axis < 0 || axis >= d->n_axes) return fail(HEXI_EINVAL, "axis_of_pair[%d] = %d out of range", p, axis);
+        // (an angle of up to 2^31 positions stays a 64-bit integer of quarter turns)
+        if (!std::isfinite(d->inv_freq[p]) || std::fabs(d->inv_freq[p]) > 1048576.0) return fail(HEXI_EINVAL, "inv_freq[%d] is not finite or above 2^20", p);
+        const long double c = (long double)d->inv_freq[p] * quarter_turns;
+        g->turn_hi[p] = (double)c;
+        g->turn_lo[p] = (double)(c - (long double)g->turn_hi[p]);
+        g->axis[p] = (unsigned char)axis;
+    }
+    for (int p = d->rot_dim / 2; p < HEXI_ROPE_MAX_DIM / 2; ++p) { g->turn_hi[p] = 0.0; g->turn_lo[p] = 0.0; g->axis[p] = 0; }
+    g->rows = g->range.total;
+    g->head_dim = d->head_dim; g->rot_dim = d->rot_dim;
+    g->adjacent = d->pairing == HEXI_ROPE_ADJACENT;
+    g->inverse = inverse != ((flags & HEXI_ROPE_INVERSE) != 0);
+    g->positions = positions;
+    g->pos_stride = pos_stride;
+    return HEXI_OK;
+}
+
+// True when a tensor of rows x heads with these strides is legal: elements within 2^40 of the first.
+static bool rope_span_ok(int64_t rows, int64_t heads, int64_t head_dim, int64_t stride_tok, int64_t stride_head)
+{
+    return (__int128)(rows - 1) * stride_tok + (__int128)(heads - 1) * stride_head + head_dim <= (__int128)1 << 40;
+}
+
+HEXI_EXPORT int hexi_rope(const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+                          const hexi_rope_tensor* tensors, int32_t n_tensors, int32_t x_dtype, int32_t y_dtype, uint32_t flags, void* hip_stream)
+{
+    RopeGeom g;
+    const int rc = build_rope(desc, range, positions, pos_stride, flags, false, &g);
+    if (rc != HEXI_OK) return rc;
+    if ((x_dtype != HEXI_BF16 && x_dtype != HEXI_F32) || (y_dtype != HEXI_BF16 && y_dtype != HEXI_F32)) return fail(HEXI_EUNSUPPORTED, "element types %d -> %d", x_dtype, y_dtype);
+    if (!tensors || n_tensors < 1 || n_tensors > HEXI_ROPE_MAX_TENSORS) return fail(HEXI_EINVAL, "null tensors or n_tensors=%d outside 1..%d", n_tensors, HEXI_ROPE_MAX_TENSORS);
+    const int xs = x_dtype == HEXI_BF16 ? 2 : 4, ys = y_dtype == HEXI_BF16 ? 2 : 4;
+    RopeTensors all;
+    memset(&all, 0, sizeof(all));
+    all.n = n_tensors;
+    for (int i = 0; i < n_tensors; ++i) {
+        const hexi_rope_tensor& t = tensors[i];
+        if (!t.x || !t.y) return fail(HEXI_EINVAL, "null tensor pointer");
+        if (t.n_heads < 1 || t.n_heads > 65535) return fail(HEXI_EINVAL, "tensor %d: n_heads %d", i, t.n_heads);
+        if (t.x_stride_tok < desc->head_dim || t.x_stride_head < desc->head_dim || t.y_stride_tok < desc->head_dim || t.y_stride_head < desc->head_dim)
+            return fail(HEXI_EINVAL, "tensor %d: strides must be at least head_dim", i);
+        if (!rope_span_ok(g.rows, t.n_heads, desc->head_dim, t.x_stride_tok, t.x_stride_head) || !rope_span_ok(g.rows, t.n_heads, desc->head_dim, t.y_stride_tok, t.y_stride_head))
+            return fail(HEXI_EUNSUPPORTED, "tensor %d spans more than 2^40 elements", i);
+        if (t.x == t.y && (x_dtype != y_dtype || t.x_stride_tok != t.y_stride_tok || t.x_stride_head != t.y_stride_head))
+            return fail(HEXI_EINVAL, "tensor %d: in place needs equal strides and element types", i);
+        if (!aligned16(t.x) || !aligned16(t.y) || (t.x_stride_tok * xs) % 16 || (t.x_stride_head * xs) % 16 || (t.y_stride_tok * ys) % 16 || (t.y_stride_head * ys) % 16)
+            return fail(HEXI_EALIGN, "tensor %d: pointers and strides must be multiples of 16 bytes", i);
+        all.t[i] = t;
+        all.first[i + 1] = all.first[i] + t.n_heads;
+    }
+    const hipError_t e = hexi_launch_rope(g, all, x_dtype, y_dtype, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "rope launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
+}
+
+static int rope_a2a_call(bool pack, const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+                         const void* src, void* dst, int32_t n_heads_total, int32_t dtype, int64_t stride_tok, int32_t n_ranks,
+                         const int32_t* heads_per_rank, const int32_t* head_list, const uint8_t* rotate, uint32_t flags, void* hip_stream)
+{
+    RopeGeom g;
+    int rc = build_rope(desc, range, positions, pos_stride, flags, !pack, &g);
+    if (rc != HEXI_OK) return rc;
+    if (dtype != HEXI_BF16 && dtype != HEXI_F32) return fail(HEXI_EUNSUPPORTED, "dtype %d not supported", dtype);
+    if ((rc = check_a2a(pack, pack ? src : dst, pack ? dst : src, g.rows, n_heads_total, desc->head_dim, dtype == HEXI_BF16 ? 2 : 4, stride_tok,
+                        n_ranks, heads_per_rank, head_list)) != HEXI_OK) return rc;
+    if (!rope_span_ok(g.rows, n_heads_total, desc->head_dim, stride_tok, desc->head_dim)) return fail(HEXI_EUNSUPPORTED, "the shard spans more than 2^40 elements");
+    if (!rotate) return fail(HEXI_EINVAL, "null rotate");
+    RopeParts p;
+    hexi_build_a2a_table(n_ranks, heads_per_rank, head_list, &p.tb);
+    for (int i = 0; i < p.tb.n_slots; ++i) p.rotate[i] = rotate[p.tb.head[i]] ? 1 : 0;
+    p.src = src; p.dst = dst;
+    p.x_stride_tok = stride_tok;
+    const hipError_t e = hexi_launch_rope_a2a(pack, g, p, dtype, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "rope a2a launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
+}
+
+HEXI_EXPORT int hexi_rope_a2a_pack(const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+                                   const void* x, void* packed, int32_t n_heads_total, int32_t dtype, int64_t x_stride_tok, int32_t n_ranks,
+                                   const int32_t* heads_per_rank, const int32_t* head_list, const uint8_t* rotate, uint32_t flags, void* hip_stream)
+{
+    return rope_a2a_call(true, desc, range, positions, pos_stride, x, packed, n_heads_total, dtype, x_stride_tok, n_ranks, heads_per_rank, head_list, rotate, flags, hip_stream);
+}
+
+HEXI_EXPORT int hexi_rope_a2a_unpack(const hexi_rope_desc* desc, const hexi_range* range, const int32_t* positions, int64_t pos_stride,
+                                     const void* packed, void* y, int32_t n_heads_total, int32_t dtype, int64_t y_stride_tok, int32_t n_ranks,
+                                     const int32_t* heads_per_rank, const int32_t* head_list, const uint8_t* rotate, uint32_t flags, void* hip_stream)
+{
+    return rope_a2a_call(false, desc, range, positions, pos_stride, packed, y, n_heads_total, dtype, y_stride_tok, n_ranks, heads_per_rank, head_list, rotate, flags, hip_stream);
 }

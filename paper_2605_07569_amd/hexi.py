@@ -17,8 +17,10 @@ HEXI_BF16, HEXI_F32 = 0, 1
 HEXI_ACCUMULATE, HEXI_COMPUTE_DELTA, HEXI_SKIP_DQ, HEXI_SKIP_DKDV = 1, 2, 4, 8
 HEXI_TILE_EMPTY, HEXI_TILE_FULL, HEXI_TILE_PARTIAL = 0, 1, 2
 HEXI_MAX_SEGS = 16
+HEXI_ROPE_HALF, HEXI_ROPE_ADJACENT, HEXI_ROPE_INVERSE = 0, 1, 16
 
 EXPORTS = ("hexi_shard_mask", "hexi_attn_fwd_chunk", "hexi_attn_merge_lse", "hexi_attn_bwd_chunk",
+           "hexi_attn_win_workspace_bytes", "hexi_attn_win_fwd_chunk", "hexi_attn_win_bwd_chunk", "hexi_rope", "hexi_rope_a2a_pack", "hexi_rope_a2a_unpack",
            "hexi_a2a_pack", "hexi_a2a_unpack", "hexi_sched_cost", "hexi_sched_solve", "hexi_set_dkdv_run_len", "hexi_workspace_bytes", "hexi_last_error", "hexi_version")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -51,6 +53,20 @@ class hexi_attn_desc(ctypes.Structure):
                 ("kv_stride_tok", ctypes.c_int64), ("kv_stride_head", ctypes.c_int64)]
 
 
+class hexi_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int64), ("n_sink", ctypes.c_int64)]
+
+
+class hexi_rope_desc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("pairing", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double)), ("axis_of_pair", ctypes.POINTER(ctypes.c_int8))]
+
+
+class hexi_rope_tensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("x_stride_tok", ctypes.c_int64), ("x_stride_head", ctypes.c_int64), ("y_stride_tok", ctypes.c_int64), ("y_stride_head", ctypes.c_int64)]
+
+
 def load():
     """Loads the in-tree library; raises if it has not been built (no fallback)."""
     global _lib
@@ -71,7 +87,20 @@ def load():
     lib.hexi_attn_merge_lse.restype = ctypes.c_int
     lib.hexi_attn_bwd_chunk.argtypes = [dp, rp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, u32, vp, ctypes.c_size_t, vp]
     lib.hexi_attn_bwd_chunk.restype = ctypes.c_int
+    wp = ctypes.POINTER(hexi_window)
+    lib.hexi_attn_win_workspace_bytes.argtypes = [dp, wp, i64, i64]
+    lib.hexi_attn_win_workspace_bytes.restype = ctypes.c_size_t
+    lib.hexi_attn_win_fwd_chunk.argtypes = [dp, wp, rp, rp, vp, vp, vp, vp, i32, vp, u32, vp, ctypes.c_size_t, vp]
+    lib.hexi_attn_win_fwd_chunk.restype = ctypes.c_int
+    lib.hexi_attn_win_bwd_chunk.argtypes = [dp, wp, rp, rp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, u32, vp]
+    lib.hexi_attn_win_bwd_chunk.restype = ctypes.c_int
     i32p = ctypes.POINTER(i32)
+    op = ctypes.POINTER(hexi_rope_desc)
+    lib.hexi_rope.argtypes = [op, rp, vp, i64, ctypes.POINTER(hexi_rope_tensor), i32, i32, i32, u32, vp]
+    lib.hexi_rope.restype = ctypes.c_int
+    for fn in (lib.hexi_rope_a2a_pack, lib.hexi_rope_a2a_unpack):
+        fn.argtypes = [op, rp, vp, i64, vp, vp, i32, i32, i64, i32, i32p, i32p, ctypes.POINTER(ctypes.c_uint8), u32, vp]
+        fn.restype = ctypes.c_int
     lib.hexi_a2a_pack.argtypes = [vp, vp, i64, i32, i32, i32, i64, i32, i32p, i32p, vp]
     lib.hexi_a2a_pack.restype = ctypes.c_int
     lib.hexi_a2a_unpack.argtypes = [vp, vp, i64, i32, i32, i32, i64, i32, i32p, i32p, vp]
@@ -219,6 +248,179 @@ def hexi_attn_bwd_chunk(desc, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq_a
 
 def hexi_workspace_bytes(desc, lq, lc):
     return int(load().hexi_workspace_bytes(ctypes.byref(desc), lq, lc))
+
+
+def make_window(window, n_sink=0):
+    """Sliding window (the row's own token counts; >= 1) and the number of first tokens that stay visible."""
+    return hexi_window(int(window), int(n_sink))
+
+
+def _refuse(msg):
+    raise HexiError(HEXI_EINVAL, msg)
+
+
+_DTYPES = None
+
+
+def _dtype(t):
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.bfloat16: HEXI_BF16, torch.float32: HEXI_F32}
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise HexiError(HEXI_EUNSUPPORTED, f"element type {t.dtype} (bf16 or fp32)")
+    return code
+
+
+def _on_device(*tensors):
+    """Tensors that the current device's stream may use."""
+    import torch
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or (dev is not None and t.get_device() != dev)):
+            _refuse(f"a tensor is on {t.device}, not on the current GPU")
+
+
+def _dense(name, t, shape, dtype=None):
+    if tuple(t.shape) != shape or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        _refuse(f"{name}: a contiguous {shape} tensor{'' if dtype is None else f' of {dtype}'} is needed, not {tuple(t.shape)} {t.dtype}")
+
+
+def _win_ranges(desc, q_segs, kv_segs, q, k, v, lse, d_o=None):
+    """Ranges of a windowed call, with what the binding can check of the tensors checked: element types, shapes, strides, device."""
+    import torch
+    qr = q_segs if isinstance(q_segs, hexi_range) else make_range(q_segs)[0]
+    kr = kv_segs if isinstance(kv_segs, hexi_range) else make_range(kv_segs)[0]
+    # (whatever else is wrong with a range the library refuses)
+    lq = sum(qr.segs[i].len for i in range(max(0, min(qr.n_segs, HEXI_MAX_SEGS))))
+    lc = sum(kr.segs[i].len for i in range(max(0, min(kr.n_segs, HEXI_MAX_SEGS))))
+    d, nq, nkv = desc.head_dim, desc.n_q_heads, desc.n_kv_heads
+    for name, t, shape, strides in (("q", q, (lq, nq, d), (desc.q_stride_tok, desc.q_stride_head, 1)), ("d_o", d_o, (lq, nq, d), (desc.q_stride_tok, desc.q_stride_head, 1)),
+                                    ("k", k, (lc, nkv, d), (desc.kv_stride_tok, desc.kv_stride_head, 1)), ("v", v, (lc, nkv, d), (desc.kv_stride_tok, desc.kv_stride_head, 1))):
+        if t is None:
+            continue
+        if tuple(t.shape) != shape or _dtype(t) != desc.dtype or any(s != w and n > 1 for s, w, n in zip(t.stride(), strides, shape)):
+            _refuse(f"{name} is {tuple(t.shape)} with strides {t.stride()}, {t.dtype}; the descriptor and the ranges say {shape} with strides {strides}")
+    _dense("lse", lse, (nq, lq), torch.float32)
+    return qr, kr, lq, lc
+
+
+def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
+    return int(load().hexi_attn_win_workspace_bytes(ctypes.byref(desc), ctypes.byref(window), lq, lc))
+
+
+def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flags=0, workspace=None, stream=None):
+    """Windowed forward; o's element type (fp32 or bf16) is the result's."""
+    lib = _lib or load()
+    qr, kr, lq, lc = _win_ranges(desc, q_segs, kv_segs, q, k, v, lse)
+    _dense("o", o, (lq, desc.n_q_heads, desc.head_dim))
+    _on_device(q, k, v, o, lse, workspace)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.hexi_attn_win_fwd_chunk(desc, window, qr, kr, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _dtype(o), _ptr(lse), flags, _ptr(workspace), ws_bytes,
+                                     _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq, dk, dv, flags=0, stream=None):
+    """Windowed backward; the element type of dq, dk and dv (one for all; None for the half that is skipped) is the gradients'."""
+    import torch
+    lib = _lib or load()
+    qr, kr, lq, lc = _win_ranges(desc, q_segs, kv_segs, q, k, v, lse, d_o)
+    nq, nkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    _dense("delta", delta, (nq, lq), torch.float32)
+    if o is not None:
+        _dense("o", o, (lq, nq, d))
+    grads = [t for t in (dq, dk, dv) if t is not None]
+    for name, t, shape in (("dq", dq, (lq, nq, d)), ("dk", dk, (lc, nkv, d)), ("dv", dv, (lc, nkv, d))):
+        if t is not None:
+            _dense(name, t, shape, grads[0].dtype)
+    _on_device(q, k, v, o, d_o, lse, delta, *grads)
+    rc = lib.hexi_attn_win_bwd_chunk(desc, window, qr, kr, _ptr(q), _ptr(k), _ptr(v), _ptr(o), HEXI_F32 if o is None else _dtype(o), _ptr(d_o), _ptr(lse),
+                                     _ptr(delta), _ptr(dq), _ptr(dk), _ptr(dv), _dtype(grads[0]) if grads else HEXI_F32, flags, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def make_rope(head_dim, inv_freq, axis_of_pair=None, pairing="half", n_axes=None):
+    """Descriptor of a rotation: a frequency per pair (rot_dim = 2 len(inv_freq)), the axis of every pair (None: axis 0), "half" or "adjacent" pairs."""
+    if pairing not in ("half", "adjacent"):
+        _refuse(f"pairing {pairing!r}")
+    if axis_of_pair is not None and len(axis_of_pair) != len(inv_freq):
+        _refuse(f"{len(axis_of_pair)} axes for {len(inv_freq)} pairs")
+    freq = (ctypes.c_double * max(1, len(inv_freq)))(*[float(f) for f in inv_freq])
+    axes = None if axis_of_pair is None else (ctypes.c_int8 * max(1, len(axis_of_pair)))(*[int(a) for a in axis_of_pair])
+    if n_axes is None:
+        n_axes = 1 if axis_of_pair is None else max(1, 1 + max([int(a) for a in axis_of_pair], default=0))
+    d = hexi_rope_desc(int(head_dim), 2 * len(inv_freq), HEXI_ROPE_HALF if pairing == "half" else HEXI_ROPE_ADJACENT, int(n_axes), freq,
+                       ctypes.cast(axes, ctypes.POINTER(ctypes.c_int8)) if axes is not None else ctypes.POINTER(ctypes.c_int8)())
+    d._keep = (freq, axes)
+    return d
+
+
+def _rope_positions(rope, positions, rows):
+    if positions is None:
+        return None, 0
+    import torch
+    if positions.dtype != torch.int32 or positions.dim() != 2 or tuple(positions.shape) != (rope.n_axes, rows) or (rows > 1 and positions.stride(1) != 1):
+        _refuse(f"positions: an int32 [{rope.n_axes}][{rows}] tensor is needed, not {tuple(positions.shape)} {positions.dtype}")
+    return positions.data_ptr(), positions.stride(0) if rope.n_axes > 1 else max(1, rows)
+
+
+def _rope_rows(segs):
+    r = segs if isinstance(segs, hexi_range) else make_range(segs)[0]
+    return r, sum(r.segs[i].len for i in range(max(0, min(r.n_segs, HEXI_MAX_SEGS))))
+
+
+def hexi_rope(rope, segs, tensors, positions=None, inverse=False, stream=None):
+    """Rotates the tensors of a shard in one launch.  tensors: [(x, y), ...], x and y [rows, heads, head_dim] with contiguous columns, y may be x; all x
+    of one element type, all y of one.  positions: int32 [n_axes, rows] on the device, or None for the rows' global positions."""
+    lib = _lib or load()
+    r, rows = _rope_rows(segs)
+    if not tensors:
+        _refuse("no tensors")
+    pos, pos_stride = _rope_positions(rope, positions, rows)
+    arr = (hexi_rope_tensor * len(tensors))()
+    x0, y0 = tensors[0]
+    for a, (x, y) in zip(arr, tensors):
+        if x.dim() != 3 or x.shape != y.shape or x.shape[0] != rows or x.shape[2] != rope.head_dim or x.stride(2) != 1 or y.stride(2) != 1 or \
+                x.dtype != x0.dtype or y.dtype != y0.dtype:
+            _refuse(f"a tensor pair of [{rows}, heads, {rope.head_dim}] and one type a side is needed, not {tuple(x.shape)} {x.dtype} -> {tuple(y.shape)} {y.dtype}")
+        # (the stride of an axis of one element is any)
+        d = rope.head_dim
+        st = [t.stride(i) if t.shape[i] > 1 else d * (t.shape[1] if i == 0 else 1) for t in (x, y) for i in (0, 1)]
+        a.x, a.y, a.n_heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+        a.x_stride_tok, a.x_stride_head, a.y_stride_tok, a.y_stride_head = st
+        _on_device(x, y, positions)
+    rc = lib.hexi_rope(rope, r, pos, pos_stride, arr, len(tensors), _dtype(x0), _dtype(y0), HEXI_ROPE_INVERSE if inverse else 0, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _rope_a2a(fn, rope, segs, whole, packed, src, dst, head_lists, rotate, positions, inverse, stream):
+    r, rows = _rope_rows(segs)
+    if whole.dim() != 3 or whole.shape[0] != rows or whole.shape[2] != rope.head_dim or whole.stride(2) != 1 or (whole.shape[1] > 1 and whole.stride(1) != rope.head_dim):
+        _refuse(f"a [{rows}, heads, {rope.head_dim}] tensor with packed heads is needed, not {tuple(whole.shape)} with strides {whole.stride()}")
+    n = whole.shape[1]
+    if packed.dtype != whole.dtype or not packed.is_contiguous() or packed.numel() < sum(len(h) for h in head_lists) * rows * rope.head_dim or len(rotate) != n:
+        _refuse(f"packed: {packed.numel()} elements of {packed.dtype}; rotate: {len(rotate)} entries for {n} heads")
+    pos, pos_stride = _rope_positions(rope, positions, rows)
+    _on_device(whole, packed, positions)
+    counts, heads = _head_tables(head_lists)
+    flags = (ctypes.c_uint8 * max(1, n))(*[1 if x else 0 for x in rotate])
+    _check(fn(rope, r, pos, pos_stride, src.data_ptr(), dst.data_ptr(), n, _dtype(whole), whole.stride(0) if rows > 1 else n * rope.head_dim, len(head_lists), counts, heads, flags,
+              HEXI_ROPE_INVERSE if inverse else 0, _stream(stream)))
+
+
+def hexi_rope_a2a_pack(rope, segs, x, packed, head_lists, rotate, positions=None, inverse=False, stream=None):
+    """hexi_a2a_pack of a fused shard with the heads h of x that have rotate[h] rotated on the way."""
+    _rope_a2a((_lib or load()).hexi_rope_a2a_pack, rope, segs, x, packed, x, packed, head_lists, rotate, positions, inverse, stream)
+
+
+def hexi_rope_a2a_unpack(rope, segs, packed, y, head_lists, rotate, positions=None, inverse=False, stream=None):
+    """hexi_a2a_unpack with the inverse rotation on the way (the gradients'; inverse=True: the rotation itself)."""
+    _rope_a2a((_lib or load()).hexi_rope_a2a_unpack, rope, segs, y, packed, packed, y, head_lists, rotate, positions, inverse, stream)
 
 
 def _head_tables(head_lists):

@@ -1,0 +1,31 @@
+// Host-side check of the window geometry that the kernels use (csrc/hexi_window.h).  One command a line:
+//   window n_sink  q range  kv range   (ranges as read_segs reads them)
+// prints for every q row "sink:lo:hi", "|", then for every key "first:end".
+#include <cstdio>
+#include <iostream>
+#include <sstream>
+#include <string>
+#include "read_segs.h"
+#include "hexi_window.h"
+
+int main()
+{
+    std::string line;
+    while (std::getline(std::cin, line)) {
+        std::istringstream is(line);
+        int window, n_sink;
+        is >> window >> n_sink;
+        const SegTable qs = read_segs(is), ks = read_segs(is);
+        for (int r = 0; r < qs.total; ++r) {
+            const WinKeys w = win_keys_of_row(ks, seg_pos_of_row(qs, r), window, n_sink);
+            std::printf("%d:%d:%d ", w.sink, w.lo, w.hi);
+        }
+        std::printf("|");
+        for (int c = 0; c < ks.total; ++c) {
+            const WinRows w = win_rows_of_key(qs, seg_pos_of_row(ks, c), window, n_sink);
+            std::printf(" %d:%d", w.first, w.end);
+        }
+        std::printf("\n");
+    }
+    return 0;
+}

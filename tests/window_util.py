@@ -1,0 +1,163 @@
+"""Windowed attention by its definition in float64, with elementwise error bounds, and the cases that the tests share.
+
+Bounds.  u = 2^-24 is half a step of fp32, h = 2^-8 half a step of bf16 (0 for fp32 inputs: nothing is rounded to fewer bits there).
+A score is a sum of d products and a few more roundings: |error| <= (d + 16) u scale sum |q k| + 16 u (|s| + |m|), m the value that is
+subtracted from it before the exponential (a row's LSE here: the reference of the kernels is within a few units of it).  Exponentials
+and the sums' own roundings are counted as 2^-20 and n u relative.  E_ij: what that makes of P_ij, relative.  P and dS are rounded to
+bf16 as operands (h each, the sum that normalises o is that of the rounded P: at most h (sum w |v| + |o|)), results to the
+type they are asked for in (h or u)."""
+from dataclasses import dataclass, field
+from typing import List, Optional
+
+import torch
+
+U, H = 2.0 ** -24, 2.0 ** -8
+
+
+@dataclass
+class Case:
+    name: str
+    q_segs: list
+    kv_segs: list
+    window: int
+    n_sink: int
+    nq: int = 2
+    nkv: int = 1
+    kv_of_q: Optional[List[int]] = None
+    k_scale: float = 1.0
+    pad: int = 0                     # extra columns between heads and tokens of the inputs
+
+    @property
+    def lq(self):
+        return sum(n for _, n in self.q_segs)
+
+    @property
+    def lc(self):
+        return sum(n for _, n in self.kv_segs)
+
+    @property
+    def heads(self):
+        return self.kv_of_q or [h // (self.nq // self.nkv) for h in range(self.nq)]
+
+
+BIG = 2 ** 31 - 2
+CASES = [
+    Case("one key", [(5, 1)], [(5, 1)], 1, 0),
+    Case("one row", [(600, 1)], [(0, 3), (401, 200)], 200, 3, nq=8),
+    Case("halo", [(300, 200)], [(0, 3), (264, 236)], 37, 3, nq=3),
+    Case("window of one", [(10, 100)], [(0, 110)], 1, 0, nq=4, nkv=2),
+    Case("zigzag", [(128, 130), (1000, 70)], [(0, 5), (100, 158), (901, 169)], 100, 5, nq=4, nkv=2),
+    Case("whole sequence", [(0, 333)], [(0, 333)], 64, 33, nq=2, nkv=2, k_scale=3.0),
+    Case("window ends at block edges", [(256, 128)], [(128, 256)], 128, 0),
+    Case("step before the shard", [(500, 300)], [(200, 300)], 128, 210, nq=3),          # later rows see 10 sinks alone
+    Case("step too far back", [(5000, 70)], [(1000, 90)], 128, 0),                       # nothing is seen
+    Case("step in the future", [(100, 70)], [(170, 65)], 128, 400),
+    Case("sinks alone", [(9000, 65)], [(0, 40)], 16, 33),
+    Case("sinks reach the window", [(150, 100)], [(0, 250)], 60, 120),
+    Case("sinks past the rows", [(10, 150)], [(0, 300)], 8, 1000),
+    Case("window past everything", [(40, 260)], [(0, 300)], 10 ** 12, 0, nq=5, nkv=2, kv_of_q=[0, 1, 1, 0, 1]),
+    Case("gaps", [(7 + 50 * i, 1 + 2 * i) for i in range(16)], [(40 * i, 3 + 2 * i) for i in range(16)], 45, 50, nq=3, nkv=1),
+    Case("rows without keys", [(0, 70), (500, 70)], [(30, 20), (490, 30)], 25, 0),
+    Case("far positions", [(BIG - 199, 200)], [(0, 4), (BIG - 260, 261)], 50, 4),
+    Case("huge window at far positions", [(BIG - 99, 100)], [(0, 4), (BIG - 160, 161)], 2 ** 40, 2 ** 40),
+    Case("strides", [(70, 90)], [(20, 140)], 33, 0, nq=3, nkv=3, pad=16),
+    Case("long", [(3000, 520)], [(0, 17), (1977, 1543)], 1024, 17, nq=4, nkv=1),
+    Case("long odd", [(2001, 431)], [(101, 2331)], 1901, 0, nq=2, nkv=2, k_scale=2.0),
+]
+
+
+def positions(segs):
+    return torch.cat([torch.arange(s, s + n, dtype=torch.int64) for s, n in segs])
+
+
+def visible(c):
+    p, j = positions(c.q_segs)[:, None], positions(c.kv_segs)[None]
+    return (j <= p) & ((p - j < c.window) | (j < c.n_sink))
+
+
+def strided(x, pad, device):
+    """x [rows, heads, d] as a slice of a wider buffer."""
+    if pad == 0:
+        return x.to(device)
+    wide = torch.full((x.shape[0], x.shape[1] + 1, x.shape[2] + pad), float("nan"), dtype=x.dtype)
+    wide[:, :x.shape[1], :x.shape[2]] = x
+    return wide.to(device)[:, :x.shape[1], :x.shape[2]]
+
+
+def inputs(c, dtype, d, seed=0):
+    g = torch.Generator().manual_seed(1000 * seed + 7)
+    n = lambda *s: torch.randn(s, generator=g, dtype=torch.float32)
+    x = dict(q=n(c.lq, c.nq, d), k=n(c.lc, c.nkv, d) * c.k_scale, v=n(c.lc, c.nkv, d), d_o=n(c.lq, c.nq, d))
+    return {name: t.to(dtype) for name, t in x.items()}
+
+
+def forward(c, x, out):
+    """o [lq, nq, d], lse [nq, lq] in float64 and bounds of their errors."""
+    q, k, v = (x[n].double() for n in ("q", "k", "v"))
+    d = q.shape[2]
+    scale, seen, h = d ** -0.5, visible(c), H if x["q"].dtype == torch.bfloat16 else 0.0
+    o, lse = torch.zeros_like(q), torch.full((c.nq, c.lq), float("-inf"), dtype=torch.float64)
+    bo, bl = torch.zeros_like(o), torch.zeros_like(lse)
+    zero = torch.zeros((), dtype=torch.float64)
+    for i, j in enumerate(c.heads):
+        s = torch.where(seen, scale * q[:, i] @ k[:, j].T, torch.tensor(float("-inf"), dtype=torch.float64))
+        z = torch.logsumexp(s, 1)
+        w = torch.where(seen, torch.exp(s - z[:, None].clamp(min=-1e300)), zero)
+        mag = scale * q[:, i].abs() @ k[:, j].abs().T
+        fin = torch.where(seen, s.abs() + z[:, None].abs().nan_to_num(0, 0, 0), zero)
+        e = torch.where(seen, (d + 16) * U * mag + 16 * U * fin, zero).amax(1) + 2.0 ** -20 + (seen.sum(1) + 16) * U
+        o[:, i], lse[i] = w @ torch.where(torch.isfinite(v[:, j]), v[:, j], zero), z
+        wv = w @ v[:, j].abs().nan_to_num(0, 0, 0)
+        bo[:, i] = (2 * e + 1.01 * h)[:, None] * (wv + o[:, i].abs()) + (1.01 * (H if out == torch.bfloat16 else U) * o[:, i].abs())
+        bl[i] = 2 * e + 4 * U * z.abs().nan_to_num(0, 0, 0)
+    return o, lse, bo, bl
+
+
+def backward(c, x, o, lse, out):
+    """delta, dq, dk, dv in float64 from the given o and lse, and bounds."""
+    q, k, v, g = (x[n].double() for n in ("q", "k", "v", "d_o"))
+    o, lse = o.double(), lse.double()
+    d = q.shape[2]
+    scale, seen, h = d ** -0.5, visible(c), H if x["q"].dtype == torch.bfloat16 else 0.0
+    ho = H if out == torch.bfloat16 else 2 * U
+    delta = (g * o).sum(2).T
+    b_delta = (d + 8) * U * (g * o).abs().sum(2).T
+    dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    bq, bk, bv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    zero = torch.zeros((), dtype=torch.float64)
+    for i, j in enumerate(c.heads):
+        live = seen & torch.isfinite(lse[i])[:, None]
+        s = scale * q[:, i] @ k[:, j].T
+        p = torch.where(live, torch.exp(torch.where(live, s - lse[i][:, None], zero)), zero)
+        mag = scale * q[:, i].abs() @ k[:, j].abs().T
+        e = torch.where(live, (d + 16) * U * mag + 16 * U * (s.abs() + lse[i].abs().nan_to_num(0, 0, 0)[:, None]), zero) + 2.0 ** -20
+        dp = g[:, i] @ v[:, j].T - delta[i][:, None]
+        b_dp = (d + 16) * U * (g[:, i].abs() @ v[:, j].abs().T) + b_delta[i][:, None] + 4 * U * delta[i].abs()[:, None]
+        ds = p * dp
+        b_ds = ds.abs() * (e + 1.01 * h) + 1.01 * p * b_dp
+        n_r, n_c = (c.lc + 16) * U, (c.lq * c.nq + 16) * U
+        dq[:, i] = scale * ds @ k[:, j]
+        bq[:, i] = 1.01 * scale * (b_ds + n_r * ds.abs()) @ k[:, j].abs()
+        dk[:, j] += scale * ds.T @ q[:, i]
+        bk[:, j] += 1.01 * scale * (b_ds + n_c * ds.abs()).T @ q[:, i].abs()
+        dv[:, j] += p.T @ g[:, i]
+        bv[:, j] += 1.01 * (p * (e + 1.01 * h + n_c)).T @ g[:, i].abs()
+    return dict(delta=(delta, b_delta + 2 * U * delta.abs()), dq=(dq, bq + 1.01 * ho * dq.abs()), dk=(dk, bk + 1.01 * ho * dk.abs()), dv=(dv, bv + 1.01 * ho * dv.abs()))
+
+
+def within(name, got, want, bound, rel=None):
+    """Elementwise within the bound; not finite exactly where the reference is not; and, for more than a few elements, relative L2 `rel`."""
+    got = got.detach().double().cpu()
+    assert got.shape == want.shape, (name, got.shape, want.shape)
+    fin = torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want)), f"{name}: NaN elsewhere"
+    assert torch.equal(got[~fin & ~want.isnan()], want[~fin & ~want.isnan()]), f"{name}: infinities differ"
+    err = (got - want)[fin].abs()
+    over = err > bound[fin] + 1e-30
+    worst = float((err / (bound[fin] + 1e-30)).max()) if err.numel() else 0.0
+    norm = float(want[fin].norm())
+    l2 = float(err.norm()) / norm if norm else 0.0
+    print(f"    {name}: rel-L2 {l2:.2e}, {worst:.2f} of the bound", flush=True)
+    assert not bool(over.any()), f"{name}: {int(over.sum())} of {err.numel()} over the bound, worst {worst:.2f}"
+    if rel is not None and norm:
+        assert l2 <= rel, f"{name}: relative L2 {l2:.2e} > {rel}"
