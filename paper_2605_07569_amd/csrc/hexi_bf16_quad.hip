@@ -21,6 +21,7 @@
 //
 // Operand layouts as in hexi_bf16_split.hip; dK and dV are accumulated transposed too (the keys across the lanes).
 #include "hexi_blocks.h"
+#include "hexi_window_plain.h"
 
 namespace {
 
@@ -51,6 +52,57 @@ struct Visible64 {
     }
 };
 
+// The same under a window (WIN): the keys of the lane's two rows (none for padding rows) and the run of blocks of all of them.
+struct VisibleWin {
+    WinKeys mine[2];
+    WinSpan<TB> span;
+    int n_blocks;
+    __device__ __forceinline__ VisibleWin(const WinFwdArgs& a, int row0, int lane, int l32) : VisibleWin(a.g, a.window, a.n_sink, row0, lane, l32) {}
+    __device__ __forceinline__ VisibleWin(const AttnGeom& g, int window, int n_sink, int row0, int lane, int l32)
+        : VisibleWin(of_row(g, window, n_sink, row0 + lane < g.lq ? row0 + lane : g.lq - 1), g, row0 + lane < g.lq, l32) {}
+    __device__ __forceinline__ VisibleWin(const WinKeys& own, const AttnGeom& g, bool exists, int l32) : span(of_lane(own, 0), of_lane(own, 63), g.lc), n_blocks(span.n_blocks)
+    {
+        const WinKeys w = exists ? own : WinKeys{0, 0, 0};
+#pragma unroll
+        for (int r = 0; r < 2; ++r) mine[r] = {__shfl(w.sink, 32 * r + l32, 64), __shfl(w.lo, 32 * r + l32, 64), __shfl(w.hi, 32 * r + l32, 64)};
+    }
+    static __device__ __forceinline__ WinKeys of_row(const AttnGeom& g, int window, int n_sink, int row)
+    {
+        const int p = pos_of_row(g.qs, row), s = rows_le(g.ks, n_sink - 1), lo = p < window ? 0 : rows_le(g.ks, p - window);
+        return s < lo ? WinKeys{s, lo, rows_le(g.ks, p)} : WinKeys{0, 0, rows_le(g.ks, p)};
+    }
+    static __device__ __forceinline__ WinKeys of_lane(const WinKeys& w, int lane)
+    {
+        return {__builtin_amdgcn_readlane(w.sink, lane), __builtin_amdgcn_readlane(w.lo, lane), __builtin_amdgcn_readlane(w.hi, lane)};
+    }
+    // keep(i, whether row block r sees key 8 (i / 4) + 4 hh + i % 4 of the chunk's block b)
+    template <class F> __device__ __forceinline__ void each_key(int r, int b, int hh, F keep) const
+    {
+        const int at = b * TB + 4 * hh, n_sink = mine[r].sink - at, lo = mine[r].lo - at, hi = mine[r].hi - at;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int o = 8 * (i >> 2) + (i & 3);
+            keep(i, o < n_sink || (o >= lo && o < hi));
+        }
+    }
+};
+template <bool WIN> using FwdArgsOf = std::conditional_t<WIN, WinFwdArgs, FwdArgs>;
+template <bool WIN> using BwdArgsOf = std::conditional_t<WIN, WinBwdArgs, BwdArgs>;
+
+// Not 0 (NaN) if some value is not finite.  A key that a row does not see has P = 0 there, and 0 x inf and 0 x NaN are NaN: a windowed unit whose sums are
+// not all finite starts again element by element, where such keys are left out instead of being given no weight.
+template <int NDB> __device__ __forceinline__ float not_finite(const f32x16 (&acc)[2][NDB])
+{
+    float z[2] = {0.f, 0.f};
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) z[r] = fmaf(acc[r][db][i], 0.f, z[r]);
+    return z[0] + z[1];
+}
+
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     const bf16x2 t = {(__bf16)a, (__bf16)b};
@@ -62,8 +114,8 @@ __device__ __forceinline__ float add_rounded(uint32_t p, float sum)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p), ones, sum, false);
 }
 
-template <int D>
-__global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(const FwdArgs a, const QuadRest rest)
+template <int D, bool WIN>
+__global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(const FwdArgsOf<WIN> a, const QuadRest rest)
 {
     using C = QuadCfg<D>;
     const AttnGeom& g = a.g;
@@ -77,9 +129,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     const int l32 = lane & 31, hh = lane >> 5;
 
     // heads of a q tile side by side, the longest (last) q tiles first
-    const int h = blockIdx.x;
-    const int q_tile = rest.tiles - 1 - (int)blockIdx.y;
-    if (!rest.has(h, q_tile)) return;
+    const int h = WIN ? uniform((int)(blockIdx.x % (unsigned)g.nq)) : (int)blockIdx.x;
+    const int q_tile = rest.tiles - 1 - (WIN ? uniform((int)(blockIdx.x / (unsigned)g.nq)) : (int)blockIdx.y);
+    if (!WIN && !rest.has(h, q_tile)) return;
     const int row0 = q_tile * ROWS;
     const int kvh = arg_byte(g.kv_of_q, h);
     const uint16_t* k = static_cast<const uint16_t*>(a.k) + (long long)kvh * g.kv_stride_head;
@@ -93,9 +145,11 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     // their MFMAs.  Q comes by way of the second buffer of wavefront 0.
     const uint32_t lds_q = (uint32_t)(uintptr_t)(&sm.t[0][1][0]);
     fetch_rows<C, ROWS, NW>(static_cast<const uint16_t*>(a.q) + (long long)h * g.q_stride_head, g.q_stride_tok, row0, g.lq, lds_q, sp, lane);
-    if (sp * TB < g.lc) fetch_k(sp, 0);
-    const Visible64 vis(g, row0, lane, l32);
-    const int n_blocks = (vis.n_all + TB - 1) / TB;
+    if (!WIN && sp * TB < g.lc) fetch_k(sp, 0);
+    const std::conditional_t<WIN, VisibleWin, Visible64> vis = [&]() { if constexpr (WIN) return VisibleWin(a, row0, lane, l32); else return Visible64(g, row0, lane, l32); }();
+    auto block = [&](int b) { if constexpr (WIN) return vis.span.block(b); else return b; };      // of the chunk, from the number in this unit's run
+    const int n_blocks = [&]() { if constexpr (WIN) return vis.n_blocks; else return (vis.n_all + TB - 1) / TB; }();
+    if (WIN && sp < n_blocks) fetch_k(block(sp), 0);
     if (n_blocks == 0 && a.accumulate) {                   // merging an empty partial is the identity
         wait_transfers<0>();
         return;
@@ -173,14 +227,22 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     };
 
     auto mask = [&](f32x16 (&s)[2], int b) __attribute__((always_inline)) {
-        if (b < vis.n_full) return;
-        keep_branch();
+        if constexpr (WIN) {
+            const int cb = block(b);
+            if (vis.span.full(cb)) return;
+            keep_branch();
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int n = vis.mine[r] - b * TB - 4 * hh;
+            for (int r = 0; r < 2; ++r) vis.each_key(r, cb, hh, [&](int i, bool seen) __attribute__((always_inline)) { if (!seen) s[r][i] = -INFINITY; });
+        } else {
+            if (b < vis.n_full) return;
+            keep_branch();
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (8 * (i >> 2) + (i & 3) >= n) s[r][i] = -INFINITY;
+            for (int r = 0; r < 2; ++r) {
+                const int n = vis.mine[r] - b * TB - 4 * hh;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + (i & 3) >= n) s[r][i] = -INFINITY;
+            }
         }
     };
     // One block: s its scores, masked and with a reference in m_run; sn receives those of the wavefront's next block.  Its
@@ -193,7 +255,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
         constexpr int N = C::NDB * 2, SLOTS = 2 * C::NKS;  // MFMAs of a row block in the second product, of both in the scores
         constexpr int LEAD = 4, EARLY = 12;                // pairs of probabilities before the first MFMA, before the second product
         const bool next = STEADY || b + NW < n_blocks, next2 = STEADY || b + 2 * NW < n_blocks;
-        const int b2 = b + 2 * NW;
+        const int b2 = block(b + 2 * NW);
         const uint16_t *k2 = k + (long long)(b2 * TB) * g.kv_stride_tok, *v2 = v + (long long)(b2 * TB) * g.kv_stride_tok;
         bf16x8 x[N];
         auto read = [&](int st) __attribute__((always_inline)) {
@@ -264,19 +326,19 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
 
     f32x16 s0[2], s1[2];
     if (sp < n_blocks) {
-        const int n_whole = n_blocks < g.lc / TB ? n_blocks : g.lc / TB;
+        const int n_whole = [&]() { if constexpr (WIN) return vis.span.n_whole; else return n_blocks < g.lc / TB ? n_blocks : g.lc / TB; }();
         if (sp + NW < n_whole) {
-            const uint16_t *v0 = v + (long long)(sp * TB) * g.kv_stride_tok, *k1 = k + (long long)((sp + NW) * TB) * g.kv_stride_tok;
+            const uint16_t *v0 = v + (long long)(block(sp) * TB) * g.kv_stride_tok, *k1 = k + (long long)(block(sp + NW) * TB) * g.kv_stride_tok;
             scores(s0, 0, []() {}, [&](int st) __attribute__((always_inline)) {
                 if (st < C::XFERS) fetch.one(v0, g.kv_stride_tok, lds + C::TILE_BYTES, st);
                 else fetch.one(k1, g.kv_stride_tok, lds + 2 * C::TILE_BYTES, st - C::XFERS);
             });
         } else {
-            fetch_v(sp, 0);
-            if (sp + NW < n_blocks) fetch_k(sp + NW, 1);
+            fetch_v(block(sp), 0);
+            if (sp + NW < n_blocks) fetch_k(block(sp + NW), 1);
             scores(s0, 0, []() {}, [](int) {});
         }
-        if (sp + NW < n_blocks) fetch_v(sp + NW, 1);
+        if (sp + NW < n_blocks) fetch_v(block(sp + NW), 1);
         mask(s0, sp);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -321,6 +383,12 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
         lr_run[r] = sum_across_halves(psr[r][0] + psr[r][1]);
         if (hh == 0) stat[sp][32 * r + l32] = make_float4(m_run[r], l_run[r], lr_run[r], 0.f);
     }
+    if constexpr (WIN) {
+        if (__syncthreads_or(not_finite<C::NDB>(oacc) != 0.f)) {
+            win_plain::fwd_unit<uint16_t, D>(a, h, row0);
+            return;
+        }
+    } else
     __syncthreads();                                       // every wavefront is done with its blocks
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -375,7 +443,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
 #pragma unroll
     for (int j = 0; j < C::OUT_VECS; ++j) {
         const int i = tid + 64 * NW * j, r = i / (D / 4), c = 4 * (i % (D / 4));
-        if (row0 + r < g.lq) *reinterpret_cast<f32x4*>(a.o + ((long long)(row0 + r) * g.nq + h) * D + c) = out[j];
+        if (row0 + r >= g.lq) continue;
+        const long long at = ((long long)(row0 + r) * g.nq + h) * D + c;
+        if constexpr (WIN) win_plain::store4(a.o, at, a.out_bf16, out[j][0], out[j][1], out[j][2], out[j][3]);
+        else *reinterpret_cast<f32x4*>(a.o + at) = out[j];
     }
 }
 
@@ -422,8 +493,8 @@ template <class C> union QuadDqSmem {
     float stage[C::STAGE_FLOATS];
 };
 
-template <int D>
-__device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int q_tile, QuadDqSmem<QuadCfg<D>>& sm)
+template <int D, bool WIN>
+__device__ __forceinline__ void dq_unit(const BwdArgsOf<WIN>& a, const int h, const int q_tile, QuadDqSmem<QuadCfg<D>>& sm)
 {
     using C = QuadCfg<D>;
     const AttnGeom& g = a.g;
@@ -450,13 +521,15 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
     const BlockFetch<C> fetch(lane, g.kv_stride_tok);
     auto fetch_k = [&](int b, int buf) { fetch.issue(k, g.kv_stride_tok, b * TB, g.lc, lds + buf * 2 * C::TILE_BYTES); };
     auto fetch_v = [&](int b, int buf) { fetch.issue(v, g.kv_stride_tok, b * TB, g.lc, lds + buf * 2 * C::TILE_BYTES + C::TILE_BYTES); };
-    const Visible64 vis(g, row0, lane, l32);
-    const int n_blocks = (vis.n_all + TB - 1) / TB;
-    if (n_blocks == 0) {                                   // dq_acc unchanged
+    const std::conditional_t<WIN, VisibleWin, Visible64> vis = [&]() { if constexpr (WIN) return VisibleWin(g, a.window, a.n_sink, row0, lane, l32); else return Visible64(g, row0, lane, l32); }();
+    auto block = [&](int b) { if constexpr (WIN) return vis.span.block(b); else return b; };      // of the chunk, from the number in this unit's run
+    const int n_blocks = [&]() { if constexpr (WIN) return vis.n_blocks; else return (vis.n_all + TB - 1) / TB; }();
+    const bool writes_anyway = [&]() { if constexpr (WIN) return a.out_bf16 != 0; else return false; }();
+    if (n_blocks == 0 && !writes_anyway) {                 // dq_acc unchanged
         wait_transfers<0>();
         return;
     }
-    if (sp < n_blocks) { fetch_v(sp, 0); fetch_k(sp, 0); }
+    if (sp < n_blocks) { fetch_v(block(sp), 0); fetch_k(block(sp), 0); }
     const LaneAddr<C> la(lane, lds);
     const LaneAddr<C> la_q(lane, lds_q);
     const float c_log2 = g.scale * LOG2E;
@@ -493,7 +566,7 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
         }
     reads_done();
     block_barrier();                                          // the second buffers are free
-    if (sp + NW < n_blocks) { fetch_v(sp + NW, 1); fetch_k(sp + NW, 1); }
+    if (sp + NW < n_blocks) { fetch_v(block(sp + NW), 1); fetch_k(block(sp + NW), 1); }
 
     constexpr int N = 2 * C::NDB;                          // MFMAs of a row block in the third product
     static_assert(N == C::NKS, "one transposed read per MFMA");
@@ -510,8 +583,8 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
         constexpr int buf = decltype(bufc)::value;
         constexpr bool STEADY = decltype(steadyc)::value;
         constexpr uint32_t kt = buf * 2 * C::TILE_BYTES, vt = kt + C::TILE_BYTES;
-        const int b2 = b + 2 * NW;
-        const bool next2 = STEADY || b2 < n_blocks;
+        const bool next2 = STEADY || b + 2 * NW < n_blocks;
+        const int b2 = block(b + 2 * NW);
         const uint16_t *k2 = k + (long long)(b2 * TB) * g.kv_stride_tok, *v2 = v + (long long)(b2 * TB) * g.kv_stride_tok;
         constexpr uint32_t kn = (buf ^ 1) * 2 * C::TILE_BYTES;
         f32x16 s[2], dp[2];
@@ -526,12 +599,19 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
             asm volatile("" : "+v"(pw[r][i]), "+v"(s[r][2 * i]), "+v"(s[r][2 * i + 1]));      // stays where it stands
         };
         auto mask = [&](int r) __attribute__((always_inline)) {
-            if (b < vis.n_full) return;
-            keep_branch();
-            const int n = vis.mine[r] - b * TB - 4 * hh;
+            if constexpr (WIN) {
+                const int cb = block(b);
+                if (vis.span.full(cb)) return;
+                keep_branch();
+                vis.each_key(r, cb, hh, [&](int i, bool seen) __attribute__((always_inline)) { if (!seen) s[r][i] = 0.f; });
+            } else {
+                if (b < vis.n_full) return;
+                keep_branch();
+                const int n = vis.mine[r] - b * TB - 4 * hh;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (8 * (i >> 2) + (i & 3) >= n) s[r][i] = 0.f;
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + (i & 3) >= n) s[r][i] = 0.f;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) pw[r][i] = pack2(s[r][2 * i], s[r][2 * i + 1]);
         };
@@ -624,7 +704,7 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
 #pragma unroll
         for (int ks = 0; ks < AHEAD; ++ks) x[ks] = lds_b128(la.row[ks]);
         using Steady = std::true_type; using Last = std::false_type;
-        const int n_whole = n_blocks < g.lc / TB ? n_blocks : g.lc / TB;
+        const int n_whole = [&]() { if constexpr (WIN) return vis.span.n_whole; else return n_blocks < g.lc / TB ? n_blocks : g.lc / TB; }();
         int b = sp;
         for (; b + 3 * NW < n_whole; b += 2 * NW) {        // two blocks at a time: the buffer is a compile-time offset of the reads
             step(IC<0>{}, Steady{}, b);
@@ -640,8 +720,15 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
 #pragma unroll
     for (int j = 0; j < C::OUT_VECS; ++j) {                // (rows past the end read the last one)
         const int i = tid + 64 * NW * j, r = row0 + i / (D / 4), c = 4 * (i % (D / 4));
-        old[j] = *reinterpret_cast<const f32x4*>(a.dq + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
+        if (writes_anyway) old[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        else old[j] = *reinterpret_cast<const f32x4*>(a.dq + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
     }
+    if constexpr (WIN) {
+        if (__syncthreads_or(not_finite<C::NDB>(dq) != 0.f)) {
+            win_plain::dq_unit<uint16_t, D>(a, h, row0);
+            return;
+        }
+    } else
     __syncthreads();
     stage64<C>(sm.stage, dq, sp, l32, hh, g.scale);
     __syncthreads();
@@ -653,7 +740,10 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
 #pragma unroll
     for (int j = 0; j < C::OUT_VECS; ++j) {
         const int i = tid + 64 * NW * j, r = row0 + i / (D / 4), c = 4 * (i % (D / 4));
-        if (r < g.lq) *reinterpret_cast<f32x4*>(a.dq + ((long long)r * g.nq + h) * D + c) = old[j];
+        if (r >= g.lq) continue;
+        const long long at = ((long long)r * g.nq + h) * D + c;
+        if constexpr (WIN) win_plain::store4(a.dq, at, a.out_bf16, old[j][0], old[j][1], old[j][2], old[j][3]);
+        else *reinterpret_cast<f32x4*>(a.dq + at) = old[j];
     }
 }
 
@@ -668,8 +758,8 @@ template <class C> union QuadDkdvSmem {
     float stage[C::STAGE_FLOATS];
 };
 
-template <int D, bool ATOMIC_DKV>
-__device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs, const int run, const int kv_tile, QuadDkdvSmem<QuadCfg<D>>& sm)
+template <int D, bool ATOMIC_DKV, bool WIN>
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, QuadDkdvSmem<QuadCfg<D>>& sm)
 {
     using C = QuadCfg<D>;
     const AttnGeom& g = a.g;
@@ -679,7 +769,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
     const int col0 = kv_tile * ROWS;
     const int n_heads = arg_byte(runs.len, run);
     const int h0 = arg_byte(runs.first, run);
-    const int kvh = arg_byte(g.kv_of_q, h0);
+    const int kvh = WIN ? run : arg_byte(g.kv_of_q, h0);      // (under a window there is a run to every kv head, an empty one where no q head reads it)
     const uint32_t lds_all = (uint32_t)(uintptr_t)(&sm.m.t[0][0][0]);
     const uint32_t lds = lds_all + sp * C::NBUF * 2 * C::TILE_BYTES;
     // the unit's own keys: K in its place, V by way of the second buffer of wavefront 0
@@ -694,7 +784,21 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
     const int row_first = __builtin_amdgcn_readlane(first, 0);
     const int row_full = __builtin_amdgcn_readlane(first_here, 63);
     const int blk0 = row_first / TB;
-    const int n_all = row_first < g.lq ? (g.lq + TB - 1) / TB - blk0 : 0;      // blocks of one head
+    // Under a window the rows that see a key end too.  Ends ascend with the keys, but for sinks, which all later rows see: they come first.
+    int my_end[2] = {g.lq, g.lq}, row_end = g.lq, row_full_end = g.lq;      // no row from row_end on sees any of the keys, rows before row_full_end see all (from row_full on)
+    if constexpr (WIN) {
+        const int key = col0 + lane < g.lc ? col0 + lane : g.lc - 1, p = pos_of_row(g.ks, key);
+        const unsigned last = (unsigned)p + (unsigned)(a.window - 1);
+        const int end = p < a.n_sink || last > 0x7ffffffeu ? g.lq : rows_le(g.qs, (int)last);
+        const int end_here = col0 + lane < g.lc ? end : 0;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) my_end[r] = __shfl(end_here, 32 * r + l32, 64);
+        const int e0 = __builtin_amdgcn_readlane(end, 0), e1 = __builtin_amdgcn_readlane(end, 63);
+        const bool sinks = __builtin_amdgcn_readfirstlane(p) < a.n_sink, all_sinks = __builtin_amdgcn_readlane(p, 63) < a.n_sink;
+        row_end = sinks ? g.lq : e1;
+        row_full_end = all_sinks ? g.lq : sinks ? 0 : e0;      // (a unit of both kinds is masked throughout)
+    }
+    const int n_all = row_first < row_end ? (row_end + TB - 1) / TB - blk0 : 0;      // blocks of one head
 
     const BlockFetch<C> fetch(lane, g.q_stride_tok);
     const uint32_t lds_lse = (uint32_t)(uintptr_t)(&sm.m.lse[sp][0][0]), lds_delta = (uint32_t)(uintptr_t)(&sm.m.delta[sp][0][0]);
@@ -809,13 +913,13 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
             asm volatile("" : "+v"(pw[c][i]), "+v"(dw[c][i]));      // stays where it stands
         };
         auto mask = [&](int c) __attribute__((always_inline)) {     // (a row that sees nothing anywhere, LSE = -inf, is masked in every block)
-            if (cur >= row_full && cur + TB <= g.lq) return;
+            if (cur >= row_full && cur + TB <= (WIN ? row_full_end : g.lq)) return;
             keep_branch();
-            const int lo = my_first[c] > cur ? my_first[c] : cur;
+            const int lo = my_first[c] > cur ? my_first[c] : cur, end = WIN ? my_end[c] : g.lq;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r0 = row + 8 * (i >> 1) + 4 * hh + 2 * (i & 1);
-                const uint32_t keep = (r0 >= lo && r0 < g.lq ? 0xffffu : 0u) | (r0 + 1 >= lo && r0 + 1 < g.lq ? 0xffff0000u : 0u);
+                const uint32_t keep = (r0 >= lo && r0 < end ? 0xffffu : 0u) | (r0 + 1 >= lo && r0 + 1 < end ? 0xffff0000u : 0u);
                 pw[c][i] &= keep;
                 dw[c][i] &= keep;
             }
@@ -937,6 +1041,12 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
 
     acc_settled<C::NDB>(dk);
     acc_settled<C::NDB>(dv);
+    if constexpr (WIN) {
+        if (__syncthreads_or(not_finite<C::NDB>(dk) + not_finite<C::NDB>(dv) != 0.f)) {
+            win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0);
+            return;
+        }
+    }
     auto write_out = [&](float* out, const f32x16 (&acc)[2][C::NDB], float w) {
         __syncthreads();
         stage64<C>(sm.stage, acc, sp, l32, hh, w);
@@ -961,9 +1071,11 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
             for (int j = 0; j < C::OUT_VECS; ++j) {
                 const int i = tid + 64 * NW * j, r = col0 + i / (D / 4), c = 4 * (i % (D / 4));
                 if (r >= g.lc) continue;
-                f32x4* op = reinterpret_cast<f32x4*>(out + ((long long)r * g.nkv + kvh) * D + c);
+                const long long at = ((long long)r * g.nkv + kvh) * D + c;
+                f32x4* op = reinterpret_cast<f32x4*>(out + at);
                 if (a.accumulate) x[j] += *op;
-                *op = x[j];
+                if constexpr (WIN) win_plain::store4(out, at, a.out_bf16, x[j][0], x[j][1], x[j][2], x[j][3]);
+                else *op = x[j];
             }
         }
     };
@@ -973,17 +1085,17 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
 
 // One launch for both halves of a backward step: workgroups [0, n_dkdv) are dK / dV units (the longer ones, first), the
 // others dQ units.  Within each, heads (runs) side by side and the longest tiles first.
-template <int D, bool ATOMIC_DKV>
-__global__ void __launch_bounds__(256, 1) bwd_quad_bf16_kernel(const BwdArgs a, const HeadRuns runs, const unsigned n_dkdv, const int n_q_tiles)
+template <int D, bool ATOMIC_DKV, bool WIN>
+__global__ void __launch_bounds__(256, 1) bwd_quad_bf16_kernel(const BwdArgsOf<WIN> a, const HeadRuns runs, const unsigned n_dkdv, const int n_q_tiles)
 {
     __shared__ __attribute__((aligned(1024))) union { QuadDkdvSmem<QuadCfg<D>> dkdv; QuadDqSmem<QuadCfg<D>> dq; } sm;
     if (blockIdx.x < n_dkdv) {
         const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
-        dkdv_unit<D, ATOMIC_DKV>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
+        dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
     } else {
         const unsigned unit = blockIdx.x - n_dkdv;
         const int tile = uniform((int)(unit / (unsigned)a.g.nq));
-        dq_unit<D>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
+        dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
     }
 }
 
@@ -993,8 +1105,8 @@ hipError_t hexi_launch_fwd_quad_bf16(const FwdArgs& a, QuadRest rest, hipStream_
 {
     if (rest.tiles == 0) rest.tiles = (a.g.lq + ROWS - 1) / ROWS;
     const dim3 grid((unsigned)a.g.nq, (unsigned)rest.tiles);
-    if (a.g.d == 128) fwd_quad_bf16_kernel<128><<<grid, 256, 0, s>>>(a, rest);
-    else if (a.g.d == 64) fwd_quad_bf16_kernel<64><<<grid, 256, 0, s>>>(a, rest);
+    if (a.g.d == 128) fwd_quad_bf16_kernel<128, false><<<grid, 256, 0, s>>>(a, rest);
+    else if (a.g.d == 64) fwd_quad_bf16_kernel<64, false><<<grid, 256, 0, s>>>(a, rest);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }
@@ -1008,11 +1120,33 @@ hipError_t hexi_launch_bwd_quad_bf16(const BwdArgs& a, bool dq, const HeadRuns& 
     const unsigned grid = n_dkdv + (unsigned)n_q_tiles * (unsigned)a.g.nq;
     if (grid == 0) return hipSuccess;
     if (a.g.d == 128) {
-        if (shared) bwd_quad_bf16_kernel<128, true><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
-        else bwd_quad_bf16_kernel<128, false><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        if (shared) bwd_quad_bf16_kernel<128, true, false><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        else bwd_quad_bf16_kernel<128, false, false><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     } else if (a.g.d == 64) {
-        if (shared) bwd_quad_bf16_kernel<64, true><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
-        else bwd_quad_bf16_kernel<64, false><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        if (shared) bwd_quad_bf16_kernel<64, true, false><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        else bwd_quad_bf16_kernel<64, false, false><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     } else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s)
+{
+    QuadRest rest;
+    rest.tiles = (a.g.lq + ROWS - 1) / ROWS;
+    const unsigned grid = (unsigned)a.g.nq * (unsigned)rest.tiles;
+    if (a.g.d == 128) fwd_quad_bf16_kernel<128, true><<<grid, 256, 0, s>>>(a, rest);
+    else fwd_quad_bf16_kernel<64, true><<<grid, 256, 0, s>>>(a, rest);
+    return hipGetLastError();
+}
+
+hipError_t hexi_launch_win_bwd_quad_bf16(const WinBwdArgs& a, hipStream_t s)
+{
+    const int n_q_tiles = a.want_dq ? (a.g.lq + ROWS - 1) / ROWS : 0;
+    HeadRuns runs;
+    hexi_head_run_of_each_kv(a.g.kv_of_q, a.g.nq, a.g.nkv, &runs);
+    const unsigned n_dkdv = a.want_dkdv ? (unsigned)((a.g.lc + ROWS - 1) / ROWS) * (unsigned)a.g.nkv : 0u;
+    const unsigned grid = n_dkdv + (unsigned)n_q_tiles * (unsigned)a.g.nq;
+    if (a.g.d == 128) bwd_quad_bf16_kernel<128, false, true><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+    else bwd_quad_bf16_kernel<64, false, true><<<grid, 256, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     return hipGetLastError();
 }

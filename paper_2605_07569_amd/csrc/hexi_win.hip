@@ -26,6 +26,7 @@ template <class F> void with_type(int dtype, int d, F f)
 
 hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
+    if (dtype == HEXI_BF16) return hexi_launch_win_fwd_quad_bf16(a, s);
     const unsigned grid = (unsigned)((a.g.lq + win_plain::ROWS - 1) / win_plain::ROWS) * (unsigned)a.g.nq;
     with_type(dtype, a.g.d, [&](auto t, auto d) { win_fwd_kernel<decltype(t), decltype(d)::value><<<grid, 256, 0, s>>>(a); });
     return hipGetLastError();
@@ -33,6 +34,7 @@ hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s)
 {
+    if (dtype == HEXI_BF16) return hexi_launch_win_bwd_quad_bf16(a, s);
     const int n_dkdv = a.want_dkdv ? (a.g.lc + win_plain::ROWS - 1) / win_plain::ROWS * a.g.nkv : 0;
     const int n_dq = a.want_dq ? (a.g.lq + win_plain::ROWS - 1) / win_plain::ROWS * a.g.nq : 0;
     with_type(dtype, a.g.d, [&](auto t, auto d) { win_bwd_kernel<decltype(t), decltype(d)::value><<<(unsigned)(n_dkdv + n_dq), 256, 0, s>>>(a, n_dkdv); });

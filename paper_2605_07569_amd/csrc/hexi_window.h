@@ -15,7 +15,8 @@ struct WinBwdArgs : BwdArgs {
     int out_bf16;           // dq, dk, dv are bf16, overwritten
 };
 
-// Keys that a row at position p sees: [0, sink) and [lo, hi), sink <= lo <= hi (sink = lo where the sinks reach the window).
+// Keys that a row at position p sees: [0, sink) and [lo, hi), sink <= lo <= hi.  Where the sinks reach the window they are one run, sink = lo = 0: along
+// a shard these rows come first, and sink, lo and hi never fall.
 struct WinKeys { int sink, lo, hi; };
 __host__ __device__ inline WinKeys win_keys_of_row(const SegTable& ks, int p, int window, int n_sink)
 {
@@ -23,9 +24,33 @@ __host__ __device__ inline WinKeys win_keys_of_row(const SegTable& ks, int p, in
     w.hi = seg_rows_le(ks, p);
     w.lo = p < window ? 0 : seg_rows_le(ks, p - window);
     const int s = seg_rows_le(ks, n_sink - 1);
-    w.sink = s < w.lo ? s : w.lo;                 // (lo <= hi: sinks past the row's own position are not seen)
+    w.sink = s < w.lo ? s : 0;                    // (lo <= hi: sinks past the row's own position are not seen)
+    if (s >= w.lo) w.lo = 0;
     return w;
 }
+
+// What a run of rows sees of the chunk in blocks of B keys, from the keys of its first and last rows: the blocks that hold a key some row sees, numbered
+// 0 .. n_blocks - 1 in order (those of the sinks, then those of the windows), and which of them every row sees in full.
+template <int B> struct WinSpan {
+    int n_sink_blocks, skip;          // block i of the run is block i of the chunk, or i + skip behind the sinks'
+    int n_blocks;
+    int n_whole;                      // blocks of the run before one that the chunk's end cuts
+    int full_sink, full_lo, full_hi;  // keys that every row sees: [0, full_sink) and [full_lo, full_hi)
+    __host__ __device__ WinSpan(const WinKeys& first, const WinKeys& last, int lc)
+    {
+        const int b0 = first.lo / B, b1 = (last.hi + B - 1) / B, s = (last.sink + B - 1) / B;
+        n_sink_blocks = s < b0 ? s : b0;
+        skip = b0 - n_sink_blocks;
+        n_blocks = n_sink_blocks + (b1 > b0 ? b1 - b0 : 0);
+        n_whole = n_blocks - (b1 > b0 && b1 > lc / B ? 1 : 0);
+        full_sink = first.sink;
+        full_lo = last.lo;
+        full_hi = first.hi;
+    }
+    __host__ __device__ int block(int i) const { return i < n_sink_blocks ? i : i + skip; }
+    // whether every row sees all of the chunk's block b
+    __host__ __device__ bool full(int b) const { return (B * b >= full_lo && B * b + B <= full_hi) || B * b + B <= full_sink; }
+};
 
 // Rows that see a key at position p: [first, end).
 struct WinRows { int first, end; };
@@ -38,9 +63,27 @@ __host__ __device__ inline WinRows win_rows_of_key(const SegTable& qs, int p, in
     return w;
 }
 
+// One run of q heads to every kv head, in head order; empty for a kv head that no q head reads.
+inline void hexi_head_run_of_each_kv(const signed char* kv_of_q, int nq, int nkv, HeadRuns* runs)
+{
+    int last[HEXI_MAX_HEADS];
+    runs->n = nkv;
+    for (int kh = 0; kh < nkv; ++kh) { runs->first[kh] = 0; runs->len[kh] = 0; last[kh] = -1; }
+    for (int h = 0; h < nq; ++h) {
+        const int kh = kv_of_q[h];
+        runs->next[h] = -1;
+        if (last[kh] < 0) runs->first[kh] = (signed char)h;
+        else runs->next[last[kh]] = (signed char)h;
+        ++runs->len[kh];
+        last[kh] = h;
+    }
+}
+
 // Launchers.
 hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s);
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s);
+hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_quad.hip
+hipError_t hexi_launch_win_bwd_quad_bf16(const WinBwdArgs& a, hipStream_t s);
 // Delta = rowsum(dO o) of a bf16 o
 hipError_t hexi_launch_delta_bf16_o(long long lq, int nq, int d, const void* o, const void* d_o, int dtype,
                                     long long stride_tok, long long stride_head, float* delta, hipStream_t s);
