@@ -86,8 +86,6 @@ struct VisibleWin {
         }
     }
 };
-template <bool WIN> using FwdArgsOf = std::conditional_t<WIN, WinFwdArgs, FwdArgs>;
-template <bool WIN> using BwdArgsOf = std::conditional_t<WIN, WinBwdArgs, BwdArgs>;
 
 // Not 0 (NaN) if some value is not finite.  A key that a row does not see has P = 0 there, and 0 x inf and 0 x NaN are NaN: a windowed unit whose sums are
 // not all finite starts again element by element, where such keys are left out instead of being given no weight.
@@ -385,7 +383,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     }
     if constexpr (WIN) {
         if (__syncthreads_or(not_finite<C::NDB>(oacc) != 0.f)) {
-            win_plain::fwd_unit<uint16_t, D>(a, h, row0);
+            win_plain::fwd_unit<uint16_t, D>(a, h, row0, ROWS);
             return;
         }
     } else
@@ -725,7 +723,7 @@ __device__ __forceinline__ void dq_unit(const BwdArgsOf<WIN>& a, const int h, co
     }
     if constexpr (WIN) {
         if (__syncthreads_or(not_finite<C::NDB>(dq) != 0.f)) {
-            win_plain::dq_unit<uint16_t, D>(a, h, row0);
+            win_plain::dq_unit<uint16_t, D>(a, h, row0, ROWS);
             return;
         }
     } else
@@ -749,8 +747,11 @@ __device__ __forceinline__ void dq_unit(const BwdArgsOf<WIN>& a, const int h, co
 
 // dK / dV of 64 keys from the q rows of a run of heads: S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS.  V stays in registers, K in
 // LDS at D = 128 (dK and dV take 256 of a wavefront's 512 registers there) and in registers at D = 64.
-template <class C> union QuadDkdvSmem {
-    struct {
+// Rows that see each of the unit's keys under a window (what is masked looks them up: kept in registers they would not fit).
+template <bool WIN> struct KeyRows {};
+template <> struct KeyRows<true> { int2 seen_by[ROWS]; };
+template <class C, bool WIN> union QuadDkdvSmem {
+    struct M : KeyRows<WIN> {
         unsigned char t[NW][C::NBUF][2 * C::TILE_BYTES];   // Q and dO block of each wavefront
         unsigned char k[2 * C::TILE_BYTES];                // the workgroup's K rows
         float lse[NW][C::NBUF][64], delta[NW][C::NBUF][64];      // row scalars of each wavefront's blocks (32 used; a transfer writes 64)
@@ -759,7 +760,7 @@ template <class C> union QuadDkdvSmem {
 };
 
 template <int D, bool ATOMIC_DKV, bool WIN>
-__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, QuadDkdvSmem<QuadCfg<D>>& sm)
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, QuadDkdvSmem<QuadCfg<D>, WIN>& sm)
 {
     using C = QuadCfg<D>;
     const AttnGeom& g = a.g;
@@ -785,14 +786,12 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
     const int row_full = __builtin_amdgcn_readlane(first_here, 63);
     const int blk0 = row_first / TB;
     // Under a window the rows that see a key end too.  Ends ascend with the keys, but for sinks, which all later rows see: they come first.
-    int my_end[2] = {g.lq, g.lq}, row_end = g.lq, row_full_end = g.lq;      // no row from row_end on sees any of the keys, rows before row_full_end see all (from row_full on)
+    int row_end = g.lq, row_full_end = g.lq;      // no row from row_end on sees any of the keys, rows before row_full_end see all (from row_full on)
     if constexpr (WIN) {
         const int key = col0 + lane < g.lc ? col0 + lane : g.lc - 1, p = pos_of_row(g.ks, key);
         const unsigned last = (unsigned)p + (unsigned)(a.window - 1);
         const int end = p < a.n_sink || last > 0x7ffffffeu ? g.lq : rows_le(g.qs, (int)last);
-        const int end_here = col0 + lane < g.lc ? end : 0;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) my_end[r] = __shfl(end_here, 32 * r + l32, 64);
+        if (sp == 0) sm.m.seen_by[lane] = make_int2(first_here, col0 + lane < g.lc ? end : 0);      // (read behind the barriers below)
         const int e0 = __builtin_amdgcn_readlane(end, 0), e1 = __builtin_amdgcn_readlane(end, 63);
         const bool sinks = __builtin_amdgcn_readfirstlane(p) < a.n_sink, all_sinks = __builtin_amdgcn_readlane(p, 63) < a.n_sink;
         row_end = sinks ? g.lq : e1;
@@ -915,11 +914,17 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
         auto mask = [&](int c) __attribute__((always_inline)) {     // (a row that sees nothing anywhere, LSE = -inf, is masked in every block)
             if (cur >= row_full && cur + TB <= (WIN ? row_full_end : g.lq)) return;
             keep_branch();
-            const int lo = my_first[c] > cur ? my_first[c] : cur, end = WIN ? my_end[c] : g.lq;
+            int lo, end = 0;
+            if constexpr (WIN) {
+                const int2 by = sm.m.seen_by[32 * c + l32];
+                lo = by.x > cur ? by.x : cur;
+                end = by.y;
+            } else lo = my_first[c] > cur ? my_first[c] : cur;
+            auto sees = [&](int r) { if constexpr (WIN) return r >= lo && r < end; else return r >= lo && r < g.lq; };
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r0 = row + 8 * (i >> 1) + 4 * hh + 2 * (i & 1);
-                const uint32_t keep = (r0 >= lo && r0 < end ? 0xffffu : 0u) | (r0 + 1 >= lo && r0 + 1 < end ? 0xffff0000u : 0u);
+                const uint32_t keep = (sees(r0) ? 0xffffu : 0u) | (sees(r0 + 1) ? 0xffff0000u : 0u);
                 pw[c][i] &= keep;
                 dw[c][i] &= keep;
             }
@@ -1043,7 +1048,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
     acc_settled<C::NDB>(dv);
     if constexpr (WIN) {
         if (__syncthreads_or(not_finite<C::NDB>(dk) + not_finite<C::NDB>(dv) != 0.f)) {
-            win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0);
+            win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0, ROWS);
             return;
         }
     }
@@ -1088,7 +1093,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
 template <int D, bool ATOMIC_DKV, bool WIN>
 __global__ void __launch_bounds__(256, 1) bwd_quad_bf16_kernel(const BwdArgsOf<WIN> a, const HeadRuns runs, const unsigned n_dkdv, const int n_q_tiles)
 {
-    __shared__ __attribute__((aligned(1024))) union { QuadDkdvSmem<QuadCfg<D>> dkdv; QuadDqSmem<QuadCfg<D>> dq; } sm;
+    __shared__ __attribute__((aligned(1024))) union { QuadDkdvSmem<QuadCfg<D>, WIN> dkdv; QuadDqSmem<QuadCfg<D>> dq; } sm;
     if (blockIdx.x < n_dkdv) {
         const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
         dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);

@@ -40,6 +40,7 @@
 #include "hexi_internal.h"
 #include "hexi_mfma.h"
 #include "hexi_f32_common.h"
+#include "hexi_window_plain.h"
 
 namespace { namespace rows16 {
 
@@ -110,9 +111,14 @@ template <class C> struct TileFetch {
     // rows [row0, row0 + TK) of `src` (its row 0 is packed row 0 of the tensor's head); rows past `total` re-read the last one
     __device__ __forceinline__ void issue(const float* src, long long stride_tok, int row0, int total, uint32_t lds, int wave) const
     {
+        issue(src, stride_tok, row0, total, lds, wave, row0 + C::TK <= total);
+    }
+    // whole: this wavefront's rows of the tile all exist
+    __device__ __forceinline__ void issue(const float* src, long long stride_tok, int row0, int total, uint32_t lds, int wave, bool whole) const
+    {
         const float* base = src + (long long)row0 * stride_tok;
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + wave * C::XFERS * 1024);
-        if (row0 + C::TK <= total) {
+        if (whole) {
 #pragma unroll
             for (int i = 0; i < C::XFERS; ++i) lds_dma16_base(base, off[i], __builtin_amdgcn_readfirstlane(dst + i * 1024));
         } else {
@@ -241,6 +247,23 @@ template <class C> __device__ __forceinline__ void stage_rows(float* stage, cons
                 make_float4(acc[4 * h][r] * w, acc[4 * h + 1][r] * w, acc[4 * h + 2][r] * w, acc[4 * h + 3][r] * w);
 }
 
+// Under a window (WIN) a wavefront's units of streaming are blocks of B rows: its own 16 of a tile, every NW-th block of the unit's run, where the
+// tiles are split; whole tiles where they are shared.  A tile is then where its blocks are (a wavefront's 16 rows lie 16 wave rows into it).
+template <class C> struct WinTiles {
+    static constexpr int B = C::SPLIT ? 16 : C::TK, STEP = C::SPLIT ? C::NW : 1;
+};
+
+// Some sum of a windowed unit is not finite (then it starts again element by element: keys a row does not see have P = 0, and 0 x inf is NaN).
+template <int N> __device__ __forceinline__ float not_finite(const f32x4 (&acc)[N])
+{
+    f32x4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = fmaf(acc[i][e], 0.f, z[e]);
+    return (z[0] + z[1]) + (z[2] + z[3]);
+}
+
 template <class C> struct FwdSmem {
     union {
         struct { unsigned char k[C::NBUF][C::TILE_BYTES], v[C::NBUF][C::TILE_BYTES]; } t;
@@ -249,7 +272,7 @@ template <class C> struct FwdSmem {
     int kpos[2][C::TK];
 };
 
-template <class C> __device__ __forceinline__ void fwd_unit(const FwdArgs& a, const int h, const int q_tile, FwdSmem<C>& sm)
+template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(const FwdArgsOf<WIN>& a, const int h, const int q_tile, FwdSmem<C>& sm)
 {
     constexpr int D = C::D, NW = C::NW, S = C::S, TK = C::TK, NBLK = C::NBLK;
     constexpr bool SPLIT = C::SPLIT, TWO = C::TWO;
@@ -267,10 +290,20 @@ template <class C> __device__ __forceinline__ void fwd_unit(const FwdArgs& a, co
     const int my_row_c = my_row < g.lq ? my_row : g.lq - 1;
     const int my_pos = my_row < g.lq ? seg_pos_of_row(g.qs, my_row) : -1;
     const int last_row = (row0 + C::ROWS < g.lq ? row0 + C::ROWS : g.lq) - 1;
-    const int n_vis = seg_rows_le(g.ks, seg_pos_of_row(g.qs, last_row));      // visible columns form the prefix [0, n_vis)
-    const int n_full = seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TK;    // tiles no row needs a mask for
+    using WT = WinTiles<C>;
+    const WinSpan<WT::B> span = [&]() {
+        if constexpr (WIN)
+            return WinSpan<WT::B>(win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row0), a.window, a.n_sink), win_keys_of_row(g.ks, seg_pos_of_row(g.qs, last_row), a.window, a.n_sink), g.lc);
+        else return WinSpan<WT::B>(WinKeys{0, 0, 0}, WinKeys{0, 0, 0}, 0);
+    }();
+    const int n_vis = WIN ? span.n_blocks : seg_rows_le(g.ks, seg_pos_of_row(g.qs, last_row));      // visible columns form the prefix [0, n_vis)
+    const int n_full = WIN ? 0 : seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TK;    // tiles no row needs a mask for
     if (n_vis == 0 && a.accumulate) return;               // merging an empty partial is the identity
-    const int n_tiles = (n_vis - (SPLIT ? 16 * wave : 0) + TK - 1) / TK;      // of this wavefront: those that hold a visible row
+    const int n_tiles = WIN ? (span.n_blocks - (SPLIT ? wave : 0) + WT::STEP - 1) / WT::STEP
+                            : (n_vis - (SPLIT ? 16 * wave : 0) + TK - 1) / TK;      // of this wavefront: those that hold a visible row
+    auto block = [&](int t) { return span.block(SPLIT ? wave + WT::STEP * t : t); };    // (WIN: of the chunk)
+    auto first_row = [&](int t) { return WIN ? WT::B * block(t) - (SPLIT ? 16 * wave : 0) : t * TK; };
+    auto masked = [&](int t) { return WIN ? !span.full(block(t)) : t >= n_full; };
 
     const float* k = static_cast<const float*>(a.k) + (long long)kvh * g.kv_stride_head;
     const float* v = static_cast<const float*>(a.v) + (long long)kvh * g.kv_stride_head;
@@ -281,11 +314,13 @@ template <class C> __device__ __forceinline__ void fwd_unit(const FwdArgs& a, co
     const uint32_t lds_k = (uint32_t)(uintptr_t)(&sm.t.k[0][0]), lds_v = (uint32_t)(uintptr_t)(&sm.t.v[0][0]);
     const int pos_slot = C::PRIVATE ? (lane < 16 ? 16 * wave + lane : TK) : tid;      // the row whose position this thread looks up
     auto fetch_tile = [&](int t) {
-        const int buf = t & 1;
-        fetch.issue(k, g.kv_stride_tok, t * TK, g.lc, lds_k + (buf % C::NBUF) * C::TILE_BYTES, wave);
-        fetch.issue(v, g.kv_stride_tok, t * TK, g.lc, lds_v + (buf % C::NBUF) * C::TILE_BYTES, wave);
-        if (t >= n_full && pos_slot < TK) kpos[buf][pos_slot] = t * TK + pos_slot < g.lc ? seg_pos_of_row(g.ks, t * TK + pos_slot) : 0x7fffffff;
+        const int buf = t & 1, row = first_row(t);
+        const bool whole = row + (WIN && SPLIT ? 16 * wave + 16 : TK) <= g.lc;
+        fetch.issue(k, g.kv_stride_tok, row, g.lc, lds_k + (buf % C::NBUF) * C::TILE_BYTES, wave, whole);
+        fetch.issue(v, g.kv_stride_tok, row, g.lc, lds_v + (buf % C::NBUF) * C::TILE_BYTES, wave, whole);
+        if (masked(t) && pos_slot < TK) kpos[buf][pos_slot] = row + pos_slot < g.lc ? seg_pos_of_row(g.ks, row + pos_slot) : 0x7fffffff;
     };
+    auto hidden = [&](int kp) { if constexpr (WIN) return kp > my_pos || (my_pos - kp >= a.window && kp >= a.n_sink); else return kp > my_pos; };
 
     f32x4 acc[4 * C::NH];
 #pragma unroll
@@ -314,14 +349,14 @@ template <class C> __device__ __forceinline__ void fwd_unit(const FwdArgs& a, co
 #pragma unroll
         for (int b = 0; b < NBLK; ++b) pv.tile[b] = vt + b * 16 * C::ROW_BYTES;
         pv.first(la);
-        if (t >= n_full) {
+        if (masked(t)) {
 #pragma unroll
             for (int b = 0; b < NBLK; ++b) {
                 const int4 p4 = *reinterpret_cast<const int4*>(&kpos[buf][16 * (sp * NBLK + b) + 4 * grp]);
-                if (p4.x > my_pos) s[b][0] = -INFINITY;
-                if (p4.y > my_pos) s[b][1] = -INFINITY;
-                if (p4.z > my_pos) s[b][2] = -INFINITY;
-                if (p4.w > my_pos) s[b][3] = -INFINITY;
+                if (hidden(p4.x)) s[b][0] = -INFINITY;
+                if (hidden(p4.y)) s[b][1] = -INFINITY;
+                if (hidden(p4.z)) s[b][2] = -INFINITY;
+                if (hidden(p4.w)) s[b][3] = -INFINITY;
             }
         }
         // running maximum of the row over this wavefront's keys, in raw score units
@@ -357,6 +392,9 @@ template <class C> __device__ __forceinline__ void fwd_unit(const FwdArgs& a, co
 
     // Combine the splits and merge with the running (o, lse): weights per (row, split), then a row-contiguous pass.
     l_run = sum_over_groups(l_run);
+    if constexpr (WIN) {
+        if (__syncthreads_or(not_finite(acc) != 0.f)) { win_plain::fwd_unit<float, D>(a, h, row0, C::ROWS); return; }
+    } else
     __syncthreads();              // the tiles are free
     stage_rows<C>(&sm.e.stage[wave * 16 * C::PITCH], acc, grp, l16, 1.0f);
     if (grp == 0) { sm.e.m[wave * 16 + l16] = m_run; sm.e.l[wave * 16 + l16] = l_run; }
@@ -402,9 +440,11 @@ template <class C> __device__ __forceinline__ void fwd_unit(const FwdArgs& a, co
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < S; ++s) x += sm.e.w[s * C::ROWS + r] * *reinterpret_cast<const f32x4*>(&sm.e.stage[(s * C::ROWS + r) * C::PITCH + c]);
-        f32x4* op = reinterpret_cast<f32x4*>(a.o + ((long long)(row0 + r) * g.nq + h) * D + c);
+        const long long at = ((long long)(row0 + r) * g.nq + h) * D + c;
+        f32x4* op = reinterpret_cast<f32x4*>(a.o + at);
         if (a.accumulate) x += sm.e.wa[r] * *op;
-        *op = x;
+        if constexpr (WIN) win_plain::store4(a.o, at, a.out_bf16, x[0], x[1], x[2], x[3]);
+        else *op = x;
     }
 }
 
@@ -417,7 +457,7 @@ template <class C> struct DqSmem {
     int kpos[2][C::TK];
 };
 
-template <class C> __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int q_tile, DqSmem<C>& sm)
+template <class C, bool WIN = false> __device__ __forceinline__ void dq_unit(const BwdArgsOf<WIN>& a, const int h, const int q_tile, DqSmem<C>& sm)
 {
     constexpr int D = C::D, NW = C::NW, S = C::S, TK = C::TK, NBLK = C::NBLK;
     constexpr bool SPLIT = C::SPLIT, TWO = C::TWO;
@@ -434,10 +474,20 @@ template <class C> __device__ __forceinline__ void dq_unit(const BwdArgs& a, con
     const int my_row_c = my_row < g.lq ? my_row : g.lq - 1;
     const int my_pos = my_row < g.lq ? seg_pos_of_row(g.qs, my_row) : -1;
     const int last_row = (row0 + C::ROWS < g.lq ? row0 + C::ROWS : g.lq) - 1;
-    const int n_vis = seg_rows_le(g.ks, seg_pos_of_row(g.qs, last_row));
-    const int n_full = seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TK;
-    if (n_vis == 0) return;                               // dq_acc unchanged
-    const int n_tiles = (n_vis - (SPLIT ? 16 * wave : 0) + TK - 1) / TK;
+    using WT = WinTiles<C>;
+    const WinSpan<WT::B> span = [&]() {
+        if constexpr (WIN)
+            return WinSpan<WT::B>(win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row0), a.window, a.n_sink), win_keys_of_row(g.ks, seg_pos_of_row(g.qs, last_row), a.window, a.n_sink), g.lc);
+        else return WinSpan<WT::B>(WinKeys{0, 0, 0}, WinKeys{0, 0, 0}, 0);
+    }();
+    const bool overwrites = [&]() { if constexpr (WIN) return a.out_bf16 != 0; else return false; }();
+    const int n_vis = WIN ? span.n_blocks : seg_rows_le(g.ks, seg_pos_of_row(g.qs, last_row));
+    const int n_full = WIN ? 0 : seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TK;
+    if (n_vis == 0 && !overwrites) return;                // dq_acc unchanged
+    const int n_tiles = WIN ? (span.n_blocks - (SPLIT ? wave : 0) + WT::STEP - 1) / WT::STEP : (n_vis - (SPLIT ? 16 * wave : 0) + TK - 1) / TK;
+    auto block = [&](int t) { return span.block(SPLIT ? wave + WT::STEP * t : t); };
+    auto first_row = [&](int t) { return WIN ? WT::B * block(t) - (SPLIT ? 16 * wave : 0) : t * TK; };
+    auto masked = [&](int t) { return WIN ? !span.full(block(t)) : t >= n_full; };
 
     const float* k = static_cast<const float*>(a.k) + (long long)kvh * g.kv_stride_head;
     const float* v = static_cast<const float*>(a.v) + (long long)kvh * g.kv_stride_head;
@@ -456,11 +506,13 @@ template <class C> __device__ __forceinline__ void dq_unit(const BwdArgs& a, con
     const uint32_t lds_k = (uint32_t)(uintptr_t)(&sm.t.k[0][0]), lds_v = (uint32_t)(uintptr_t)(&sm.t.v[0][0]);
     const int pos_slot = C::PRIVATE ? (lane < 16 ? 16 * wave + lane : TK) : tid;      // the row whose position this thread looks up
     auto fetch_tile = [&](int t) {
-        const int buf = t & 1;
-        fetch.issue(k, g.kv_stride_tok, t * TK, g.lc, lds_k + (buf % C::NBUF) * C::TILE_BYTES, wave);
-        fetch.issue(v, g.kv_stride_tok, t * TK, g.lc, lds_v + (buf % C::NBUF) * C::TILE_BYTES, wave);
-        if (t >= n_full && pos_slot < TK) kpos[buf][pos_slot] = t * TK + pos_slot < g.lc ? seg_pos_of_row(g.ks, t * TK + pos_slot) : 0x7fffffff;
+        const int buf = t & 1, row = first_row(t);
+        const bool whole = row + (WIN && SPLIT ? 16 * wave + 16 : TK) <= g.lc;
+        fetch.issue(k, g.kv_stride_tok, row, g.lc, lds_k + (buf % C::NBUF) * C::TILE_BYTES, wave, whole);
+        fetch.issue(v, g.kv_stride_tok, row, g.lc, lds_v + (buf % C::NBUF) * C::TILE_BYTES, wave, whole);
+        if (masked(t) && pos_slot < TK) kpos[buf][pos_slot] = row + pos_slot < g.lc ? seg_pos_of_row(g.ks, row + pos_slot) : 0x7fffffff;
     };
+    auto hidden = [&](int kp) { if constexpr (WIN) return kp > my_pos || (my_pos - kp >= a.window && kp >= a.n_sink); else return kp > my_pos; };
 
     f32x4 acc[4 * C::NH];
 #pragma unroll
@@ -482,14 +534,15 @@ template <class C> __device__ __forceinline__ void dq_unit(const BwdArgs& a, con
             ColReads<C, 1> kc;
             kc.tile[0] = kt;
             kc.first(la);
-            int4 p4 = make_int4(-1, -1, -1, -1);
-            if (t >= n_full) p4 = *reinterpret_cast<const int4*>(&kpos[buf][16 * (sp * NBLK + b) + 4 * grp]);
+            const int open = WIN ? my_pos : -1;            // a position that is seen
+            int4 p4 = make_int4(open, open, open, open);
+            if (masked(t)) p4 = *reinterpret_cast<const int4*>(&kpos[buf][16 * (sp * NBLK + b) + 4 * grp]);
             const int pv[4] = {p4.x, p4.y, p4.z, p4.w};
             f32x4 ds;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const float p = prob(sd[0][r], c_hi, c_lo, nl_hi, nl_lo);
-                ds[r] = pv[r] > my_pos ? 0.f : p * (sd[1][r] - delta);
+                ds[r] = hidden(pv[r]) ? 0.f : p * (sd[1][r] - delta);
             }
             f32x4 (*const accs[1])[4 * C::NH] = {&acc};
             const f32x4* const ps[1] = {&ds};
@@ -497,9 +550,25 @@ template <class C> __device__ __forceinline__ void dq_unit(const BwdArgs& a, con
         }
         if (C::NBUF == 1 && t + 1 < n_tiles) { if (TWO) reads_done(); fetch_tile(t + 1); }
     }
+    if constexpr (WIN) {
+        if (__syncthreads_or(not_finite(acc) != 0.f)) { win_plain::dq_unit<float, D>(a, h, row0, C::ROWS); return; }
+    } else
     __syncthreads();
     stage_rows<C>(&sm.stage[wave * 16 * C::PITCH], acc, grp, l16, g.scale);
     __syncthreads();
+    if constexpr (WIN) {
+        if (overwrites) {
+            for (int i = tid; i < C::ROWS * C::PIECES; i += 64 * NW) {
+                const int r = i / C::PIECES, c = 4 * (i % C::PIECES);
+                if (row0 + r >= g.lq) continue;
+                f32x4 x = *reinterpret_cast<const f32x4*>(&sm.stage[r * C::PITCH + c]);
+#pragma unroll
+                for (int s = 1; s < S; ++s) x += *reinterpret_cast<const f32x4*>(&sm.stage[(s * C::ROWS + r) * C::PITCH + c]);
+                win_plain::store4(a.dq, ((long long)(row0 + r) * g.nq + h) * D + c, true, x[0], x[1], x[2], x[3]);
+            }
+            return;
+        }
+    }
     // Added with atomics, consecutive lanes on consecutive floats: chunks of one shard may be in flight on several streams.
     // One addition per element and call, so calls in stream order still have a fixed order.
     for (int i = tid; i < C::ROWS * D; i += 64 * NW) {
@@ -524,7 +593,8 @@ template <class C> struct DkdvSmem {
     __attribute__((aligned(16))) int qpos[2][C::TK];
 };
 
-template <class C> __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const int kvh, const int kv_tile, DkdvSmem<C>& sm, const int h_first, const int h_end, const bool atomic)
+template <class C, bool WIN = false>
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh, const int kv_tile, DkdvSmem<C>& sm, const int h_first, const int h_end, const bool atomic)
 {
     constexpr int D = C::D, NW = C::NW, S = C::S, TM = C::TK, NBLK = C::NBLK;
     constexpr bool SPLIT = C::SPLIT, TWO = C::TWO;
@@ -542,11 +612,27 @@ template <class C> __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, c
     const int my_col_c = my_col < g.lc ? my_col : g.lc - 1;
     const int my_kpos = my_col < g.lc ? seg_pos_of_row(g.ks, my_col) : 0x7fffffff;
     const int last_col = (col0 + C::ROWS < g.lc ? col0 + C::ROWS : g.lc) - 1;
-    const int row_first = seg_rows_le(g.qs, seg_pos_of_row(g.ks, col0) - 1);         // rows before it see nothing of the tile
-    const int row_full = seg_rows_le(g.qs, seg_pos_of_row(g.ks, last_col) - 1);      // rows from it on see all of it
-    const int tile0 = row_first / TM, n_qtiles = (g.lq + TM - 1) / TM;
+    using WT = WinTiles<C>;
+    const WinRowSpan rows = [&]() {
+        if constexpr (WIN) {
+            const int p0 = seg_pos_of_row(g.ks, col0), p1 = seg_pos_of_row(g.ks, last_col);
+            return WinRowSpan(win_rows_of_key(g.qs, p0, a.window, a.n_sink), win_rows_of_key(g.qs, p1, a.window, a.n_sink), p0 < a.n_sink, p1 < a.n_sink, g.lq);
+        } else return WinRowSpan(WinRows{0, 0}, WinRows{0, 0}, false, false, 0);
+    }();
+    const int row_first = WIN ? rows.first : seg_rows_le(g.qs, seg_pos_of_row(g.ks, col0) - 1);         // rows before it see nothing of the tile
+    const int row_full = WIN ? rows.full : seg_rows_le(g.qs, seg_pos_of_row(g.ks, last_col) - 1);      // rows from it on see all of it
+    // tiles of a head: [tile0, n_qtiles) (WIN: blocks of the run of rows, this wavefront's every STEP-th one of all heads' in a row)
+    const int tile0 = WIN ? 0 : row_first / TM, n_qtiles = WIN ? (row_first < rows.end ? (rows.end + WT::B - 1) / WT::B - row_first / WT::B : 0) : (g.lq + TM - 1) / TM;
     const int per_head = n_qtiles - tile0;
     const bool key_ragged = col0 + C::ROWS > g.lc;        // padding keys are masked through their position
+    auto first_row = [&](int t) { return WIN ? WT::B * (row_first / WT::B + t) - (SPLIT ? 16 * wave : 0) : t * TM; };
+    // (the last tile may hold padding rows, whose position is -1)
+    auto masked_tile = [&](int t) {
+        if constexpr (WIN) {
+            const int r = WT::B * (row_first / WT::B + t);
+            return r < row_full || r + WT::B > rows.full_end || key_ragged;
+        } else return t * TM < row_full || key_ragged || t == n_qtiles - 1;
+    };
 
     f32x4 kf[C::NG], vf[C::NG];
     const long long k_off = (long long)my_col_c * g.kv_stride_tok + (long long)kvh * g.kv_stride_head;
@@ -557,38 +643,57 @@ template <class C> __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, c
     const TileFetch<C> fetch(wave, lane, g.q_stride_tok);
     const uint32_t lds_q = (uint32_t)(uintptr_t)(&sm.t.q[0][0]), lds_g = (uint32_t)(uintptr_t)(&sm.t.g[0][0]);
     auto next_head = [&](int h) { for (++h; h < h_end && g.kv_of_q[h] != kvh; ++h) {} return h; };
-    int fetch_h = next_head(h_first - 1), fetch_t = tile0;
+    // the next tile behind (h, t)
+    auto advance = [&](int& h, int& t) {
+        if constexpr (WIN) {
+            t += WT::STEP;
+            while (t >= n_qtiles && h < h_end) { t -= n_qtiles; h = next_head(h); }
+        } else if (++t == n_qtiles) { t = tile0; h = next_head(h); }
+    };
+    auto start = [&](int& h, int& t) {
+        h = next_head(h_first - 1);
+        t = tile0;
+        if constexpr (WIN) {
+            t = SPLIT ? wave : 0;
+            while (t >= n_qtiles && h < h_end) { t -= n_qtiles; h = next_head(h); }
+        }
+    };
+    int fetch_h = h_end, fetch_t = tile0;
+    if (per_head > 0) start(fetch_h, fetch_t);
     const int pos_slot = C::PRIVATE ? (lane < 16 ? 16 * wave + lane : TM) : tid;
     auto fetch_tile = [&](int buf) {
         const long long off = (long long)fetch_h * g.q_stride_head;
-        fetch.issue(static_cast<const float*>(a.q) + off, g.q_stride_tok, fetch_t * TM, g.lq, lds_q + (buf % C::NBUF) * C::TILE_BYTES, wave);
-        fetch.issue(static_cast<const float*>(a.d_o) + off, g.q_stride_tok, fetch_t * TM, g.lq, lds_g + (buf % C::NBUF) * C::TILE_BYTES, wave);
+        const int row0 = first_row(fetch_t);
+        const bool whole = row0 + (WIN && SPLIT ? 16 * wave + 16 : TM) <= g.lq;
+        fetch.issue(static_cast<const float*>(a.q) + off, g.q_stride_tok, row0, g.lq, lds_q + (buf % C::NBUF) * C::TILE_BYTES, wave, whole);
+        fetch.issue(static_cast<const float*>(a.d_o) + off, g.q_stride_tok, row0, g.lq, lds_g + (buf % C::NBUF) * C::TILE_BYTES, wave, whole);
         // The rows' LSE and Delta: a 4-byte-per-lane transfer each, by wavefronts 0 and 1 for the tile, or by every
         // wavefront for its own 16 rows.
         const int lrow = C::PRIVATE ? 16 * wave + (lane & 15) : lane;
-        const int row = fetch_t * TM + lrow < g.lq ? fetch_t * TM + lrow : g.lq - 1;
+        const int row = row0 + lrow < g.lq ? row0 + lrow : g.lq - 1;
         if (C::PRIVATE || wave == 0) lds_dma4(a.lse + (long long)fetch_h * g.lq + row, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)&lse[buf][SET * wave]));
         if (C::PRIVATE || wave == 1) lds_dma4(a.delta + (long long)fetch_h * g.lq + row, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)&delta[buf][SET * wave]));
-        if (pos_slot < TM && (fetch_t * TM < row_full || key_ragged || fetch_t == n_qtiles - 1))
-            qpos[buf][pos_slot] = fetch_t * TM + pos_slot < g.lq ? seg_pos_of_row(g.qs, fetch_t * TM + pos_slot) : -1;
-        if (++fetch_t == n_qtiles) { fetch_t = tile0; fetch_h = next_head(fetch_h); }
+        if (pos_slot < TM && masked_tile(fetch_t))
+            qpos[buf][pos_slot] = row0 + pos_slot < g.lq ? seg_pos_of_row(g.qs, row0 + pos_slot) : -1;
+        advance(fetch_h, fetch_t);
     };
+    auto hidden = [&](int qp) { if constexpr (WIN) return my_kpos > qp || (qp - my_kpos >= a.window && my_kpos >= a.n_sink); else return my_kpos > qp; };
 
     f32x4 dk[4 * C::NH], dv[4 * C::NH];
 #pragma unroll
     for (int i = 0; i < 4 * C::NH; ++i) { dk[i] = f32x4{0.f, 0.f, 0.f, 0.f}; dv[i] = dk[i]; }
     if (per_head > 0) {
-        int buf = 0, t = tile0;
+        int buf = 0, t, h;
+        start(h, t);
         if (fetch_h < h_end) fetch_tile(0);
-        for (int h = next_head(h_first - 1); h < h_end;) {
+        while (h < h_end) {
             tile_landed<C>();
             if (C::NBUF == 2 && fetch_h < h_end) fetch_tile(buf ^ 1);
-            // (the last tile may hold padding rows, whose position is -1)
-            const bool masked = t * TM < row_full || key_ragged || t == n_qtiles - 1;
+            const bool masked = masked_tile(t);
 #pragma unroll
             for (int b = 0; b < NBLK; ++b) {
                 const int blk = sp * NBLK + b;
-                if (SPLIT && (t * TM + 16 * blk >= g.lq || t * TM + 16 * blk + 16 <= row_first)) continue;      // rows that see nothing
+                if (!WIN && SPLIT && (t * TM + 16 * blk >= g.lq || t * TM + 16 * blk + 16 <= row_first)) continue;      // rows that see nothing
                 const unsigned char* qt = &sm.t.q[buf % C::NBUF][blk * 16 * C::ROW_BYTES];
                 const unsigned char* gt = &sm.t.g[buf % C::NBUF][blk * 16 * C::ROW_BYTES];
                 if constexpr (C::CLEAR) {
@@ -615,10 +720,10 @@ template <class C> __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, c
                 }
                 if (masked) {
                     const int4 q4 = *reinterpret_cast<const int4*>(&qpos[buf][16 * blk + 4 * grp]);
-                    if (my_kpos > q4.x) p[0] = 0.f;
-                    if (my_kpos > q4.y) p[1] = 0.f;
-                    if (my_kpos > q4.z) p[2] = 0.f;
-                    if (my_kpos > q4.w) p[3] = 0.f;
+                    if (hidden(q4.x)) p[0] = 0.f;
+                    if (hidden(q4.y)) p[1] = 0.f;
+                    if (hidden(q4.z)) p[2] = 0.f;
+                    if (hidden(q4.w)) p[3] = 0.f;
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) ds[r] = p[r] * (sd[1][r] - dl[r]);
@@ -628,8 +733,11 @@ template <class C> __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, c
             }
             if (C::NBUF == 1 && fetch_h < h_end) { if (TWO) reads_done(); fetch_tile(buf ^ 1); }
             buf ^= 1;
-            if (++t == n_qtiles) { t = tile0; h = next_head(h); }
+            advance(h, t);
         }
+    }
+    if constexpr (WIN) {
+        if (__syncthreads_or(not_finite(dk) + not_finite(dv) != 0.f)) { win_plain::dkdv_unit<float, D>(a, kvh, col0, C::ROWS); return; }
     }
     auto write_out = [&](float* out, const f32x4 (&acc)[4 * C::NH], float w) {
         __syncthreads();
@@ -648,7 +756,8 @@ template <class C> __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, c
                 continue;
             }
             if (a.accumulate) x += *op;
-            *op = x;
+            if constexpr (WIN) win_plain::store4(out, ((long long)(col0 + r) * g.nkv + kvh) * D + c, a.out_bf16, x[0], x[1], x[2], x[3]);
+            else *op = x;
         }
     };
     write_out(a.dv, dv, 1.0f);

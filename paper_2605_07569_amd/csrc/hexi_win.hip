@@ -1,44 +1,70 @@
-// Attention under a sliding window with sink tokens: dispatch, and the kernels that follow the definition.
-#include "hexi_window_plain.h"
+// Attention under a sliding window with sink tokens: the fp32 kernels (units of hexi_f32_units.h on windowed runs of keys and rows), dispatch, and Delta from a
+// bf16 o.  The bf16 kernels are those of hexi_bf16_quad.hip.
+#include "hexi_f32_units.h"
 #include <type_traits>
 
 namespace {
 
-template <class T, int D> __global__ void __launch_bounds__(256) win_fwd_kernel(const WinFwdArgs a)
+template <int D, bool SPLIT, bool TWO> using Cfg = rows16::F32Cfg<D, SPLIT, TWO>;
+
+template <int D, bool SPLIT, bool TWO>
+__global__ void __launch_bounds__((64 * Cfg<D, SPLIT, TWO>::NW), TWO ? 4 : 1) win_fwd_f32_kernel(const WinFwdArgs a)
 {
-    win_plain::fwd_unit<T, D>(a, (int)blockIdx.x % a.g.nq, (int)blockIdx.x / a.g.nq * win_plain::ROWS);
-}
-template <class T, int D> __global__ void __launch_bounds__(256) win_bwd_kernel(const WinBwdArgs a, const int n_dkdv)
-{
-    if ((int)blockIdx.x < n_dkdv) win_plain::dkdv_unit<T, D>(a, (int)blockIdx.x % a.g.nkv, (int)blockIdx.x / a.g.nkv * win_plain::ROWS);
-    else win_plain::dq_unit<T, D>(a, ((int)blockIdx.x - n_dkdv) % a.g.nq, ((int)blockIdx.x - n_dkdv) / a.g.nq * win_plain::ROWS);
+    using C = Cfg<D, SPLIT, TWO>;
+    __shared__ __attribute__((aligned(1024))) rows16::FwdSmem<C> sm;
+    const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)a.g.nq);
+    rows16::fwd_unit<C, true>(a, (int)blockIdx.x - tile * a.g.nq, tile, sm);
 }
 
-// f(element type, head_dim)
-template <class F> void with_type(int dtype, int d, F f)
+// Workgroups [0, n_dkdv) are dK / dV units, the others dQ units.
+template <int D, bool SPLIT, bool TWO>
+__global__ void __launch_bounds__((64 * Cfg<D, SPLIT, TWO>::NW), TWO ? 4 : SPLIT ? 1 : 2) win_bwd_f32_kernel(const WinBwdArgs a, const unsigned n_dkdv)
 {
-    if (dtype == HEXI_F32) { if (d == 128) f(float{}, std::integral_constant<int, 128>{}); else f(float{}, std::integral_constant<int, 64>{}); }
-    else if (d == 128) f(uint16_t{}, std::integral_constant<int, 128>{});
-    else f(uint16_t{}, std::integral_constant<int, 64>{});
+    using C = Cfg<D, SPLIT, TWO>;
+    __shared__ __attribute__((aligned(1024))) union { rows16::DkdvSmem<C> dkdv; rows16::DqSmem<C> dq; } sm;
+    if (blockIdx.x < n_dkdv) {
+        const int tile = __builtin_amdgcn_readfirstlane(blockIdx.x / (unsigned)a.g.nkv);
+        rows16::dkdv_unit<C, true>(a, (int)blockIdx.x - tile * a.g.nkv, tile, sm.dkdv, 0, a.g.nq, false);
+    } else {
+        const unsigned unit = blockIdx.x - n_dkdv;
+        const int tile = __builtin_amdgcn_readfirstlane(unit / (unsigned)a.g.nq);
+        rows16::dq_unit<C, true>(a, (int)unit - tile * a.g.nq, tile, sm.dq);
+    }
+}
+
+// f(configuration)
+template <class F> hipError_t with_cfg(int d, bool split, F f)
+{
+    if (d == 128) { if (split) f(Cfg<128, true, false>{}); else f(Cfg<128, false, false>{}); }
+    else if (split) f(Cfg<64, true, true>{});
+    else f(Cfg<64, false, false>{});
+    return hipGetLastError();
 }
 
 }  // namespace
 
+#include <cstdlib>
+static int env_shape(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 1; }
+
 hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
     if (dtype == HEXI_BF16) return hexi_launch_win_fwd_quad_bf16(a, s);
-    const unsigned grid = (unsigned)((a.g.lq + win_plain::ROWS - 1) / win_plain::ROWS) * (unsigned)a.g.nq;
-    with_type(dtype, a.g.d, [&](auto t, auto d) { win_fwd_kernel<decltype(t), decltype(d)::value><<<grid, 256, 0, s>>>(a); });
-    return hipGetLastError();
+    return with_cfg(a.g.d, env_shape("WFS"), [&](auto cfg) {
+        using C = decltype(cfg);
+        const unsigned grid = (unsigned)((a.g.lq + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nq;
+        win_fwd_f32_kernel<C::D, C::SPLIT, C::TWO><<<grid, 64 * C::NW, 0, s>>>(a);
+    });
 }
 
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s)
 {
     if (dtype == HEXI_BF16) return hexi_launch_win_bwd_quad_bf16(a, s);
-    const int n_dkdv = a.want_dkdv ? (a.g.lc + win_plain::ROWS - 1) / win_plain::ROWS * a.g.nkv : 0;
-    const int n_dq = a.want_dq ? (a.g.lq + win_plain::ROWS - 1) / win_plain::ROWS * a.g.nq : 0;
-    with_type(dtype, a.g.d, [&](auto t, auto d) { win_bwd_kernel<decltype(t), decltype(d)::value><<<(unsigned)(n_dkdv + n_dq), 256, 0, s>>>(a, n_dkdv); });
-    return hipGetLastError();
+    return with_cfg(a.g.d, env_shape("WBS"), [&](auto cfg) {
+        using C = decltype(cfg);
+        const unsigned n_dkdv = a.want_dkdv ? (unsigned)((a.g.lc + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nkv : 0u;
+        const unsigned n_dq = a.want_dq ? (unsigned)((a.g.lq + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nq : 0u;
+        win_bwd_f32_kernel<C::D, C::SPLIT, C::TWO><<<n_dkdv + n_dq, 64 * C::NW, 0, s>>>(a, n_dkdv);
+    });
 }
 
 namespace {
@@ -65,6 +91,14 @@ __global__ void __launch_bounds__(256) delta_bf16_o_kernel(long long lq, int nq,
 #pragma unroll
     for (int off = LANES / 2; off >= 1; off >>= 1) acc += __shfl_xor(acc, off, 64);
     if (valid && c == 0) delta[(long long)h * lq + row] = acc;
+}
+
+// f(element type, head_dim)
+template <class F> void with_type(int dtype, int d, F f)
+{
+    if (dtype == HEXI_F32) { if (d == 128) f(float{}, std::integral_constant<int, 128>{}); else f(float{}, std::integral_constant<int, 64>{}); }
+    else if (d == 128) f(uint16_t{}, std::integral_constant<int, 128>{});
+    else f(uint16_t{}, std::integral_constant<int, 64>{});
 }
 
 }  // namespace

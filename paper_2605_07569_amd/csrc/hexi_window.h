@@ -15,6 +15,12 @@ struct WinBwdArgs : BwdArgs {
     int out_bf16;           // dq, dk, dv are bf16, overwritten
 };
 
+// Argument blocks of kernels that serve both: WIN, under a window.
+template <bool WIN> struct WinOr { using Fwd = FwdArgs; using Bwd = BwdArgs; };
+template <> struct WinOr<true> { using Fwd = WinFwdArgs; using Bwd = WinBwdArgs; };
+template <bool WIN> using FwdArgsOf = typename WinOr<WIN>::Fwd;
+template <bool WIN> using BwdArgsOf = typename WinOr<WIN>::Bwd;
+
 // Keys that a row at position p sees: [0, sink) and [lo, hi), sink <= lo <= hi.  Where the sinks reach the window they are one run, sink = lo = 0: along
 // a shard these rows come first, and sink, lo and hi never fall.
 struct WinKeys { int sink, lo, hi; };
@@ -62,6 +68,19 @@ __host__ __device__ inline WinRows win_rows_of_key(const SegTable& qs, int p, in
     w.end = p < n_sink || last > 0x7ffffffeu ? qs.total : seg_rows_le(qs, (int)last);
     return w;
 }
+
+// What a run of keys is seen by, from its first and last: rows [first, end) see some of them, rows [full, full_end) all.  Ends ascend with the keys but for
+// sinks, which all rows behind them see; they come first.  (A run of both kinds counts as seen in full by no row.)
+struct WinRowSpan {
+    int first, end, full, full_end;
+    __host__ __device__ WinRowSpan(const WinRows& w0, const WinRows& w1, bool first_is_sink, bool last_is_sink, int lq)
+    {
+        first = w0.first;
+        end = first_is_sink ? lq : w1.end;
+        full = w1.first;
+        full_end = last_is_sink ? lq : first_is_sink ? 0 : w0.end;
+    }
+};
 
 // One run of q heads to every kv head, in head order; empty for a kv head that no q head reads.
 inline void hexi_head_run_of_each_kv(const signed char* kv_of_q, int nq, int nkv, HeadRuns* runs)

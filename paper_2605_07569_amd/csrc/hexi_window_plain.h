@@ -1,14 +1,14 @@
 // Windowed attention element by element, as its definition says it.
 //
-// 256 threads own 64 stationary rows (or keys), four neighbouring lanes to a row, D / 4 columns each, and walk the row's own run of the
-// other tensor's rows one by one.  No value of a row that the mask excludes is ever read into a sum, so what is not finite there
+// A workgroup of 64 to 1024 threads takes its stationary rows (or keys) eight neighbouring lanes to a row, D / 8 columns each, which walk the row's own runs
+// of the other tensor's rows one by one.  No value of a row that the mask excludes is ever read into a sum, so what is not finite there
 // stays there.
 #pragma once
 #include "hexi_window.h"
 
 namespace { namespace win_plain {
 
-constexpr int ROWS = 64;
+constexpr int LANES = 8;      // to a row
 
 template <class T> __device__ __forceinline__ void load4(const T* p, float* x)
 {
@@ -43,140 +43,143 @@ template <int N> __device__ __forceinline__ float dot(const float (&a)[N], const
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i & 3] = fmaf(a[i], b[i], s[i & 3]);
     float x = (s[0] + s[1]) + (s[2] + s[3]);
-    x += __shfl_xor(x, 1, 64);                    // the four lanes of a row run the same iterations
-    x += __shfl_xor(x, 2, 64);
+#pragma unroll
+    for (int off = 1; off < LANES; off *= 2) x += __shfl_xor(x, off, 64);      // the lanes of a row run the same iterations
     return x;
 }
 
-// o and lse of rows [row0, row0 + 64) of head h.
-template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdArgs& a, const int h, const int row0)
+// o and lse of rows [row0, row0 + rows) of head h.
+template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdArgs& a, const int h, const int row0, const int rows)
 {
-    constexpr int N = D / 4;
+    constexpr int N = D / LANES;
     const AttnGeom& g = a.g;
-    const int row = row0 + (int)threadIdx.x / 4, col = (int)threadIdx.x % 4 * N;
-    if (row >= g.lq) return;
-    const WinKeys w = win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink);
-    const T* k = static_cast<const T*>(a.k) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
-    const T* v = static_cast<const T*>(a.v) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
-    float q[N], acc[N];
-    load_cols(static_cast<const T*>(a.q) + (long long)row * g.q_stride_tok + (long long)h * g.q_stride_head + col, q);
+    const int col = (int)threadIdx.x % LANES * N, end_row = row0 + rows < g.lq ? row0 + rows : g.lq;
+    for (int row = row0 + (int)threadIdx.x / LANES; row < end_row; row += (int)blockDim.x / LANES) {
+        const WinKeys w = win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink);
+        const T* k = static_cast<const T*>(a.k) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
+        const T* v = static_cast<const T*>(a.v) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
+        float q[N], acc[N];
+        load_cols(static_cast<const T*>(a.q) + (long long)row * g.q_stride_tok + (long long)h * g.q_stride_head + col, q);
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    for (int part = 0; part < 2; ++part)
-        for (int j = part ? w.lo : 0, end = part ? w.hi : w.sink; j < end; ++j) {
-            float x[N];
-            load_cols(k + (long long)j * g.kv_stride_tok, x);
-            const float s = dot(q, x) * g.scale;
-            load_cols(v + (long long)j * g.kv_stride_tok, x);
-            if (s > m) {
-                const float alpha = expf(m - s);   // (m = -inf: 0)
-                m = s;
-                l *= alpha;
+        for (int i = 0; i < N; ++i) acc[i] = 0.f;
+        float m = -INFINITY, l = 0.f;
+        for (int part = 0; part < 2; ++part)
+            for (int j = part ? w.lo : 0, end = part ? w.hi : w.sink; j < end; ++j) {
+                float x[N];
+                load_cols(k + (long long)j * g.kv_stride_tok, x);
+                const float s = dot(q, x) * g.scale;
+                load_cols(v + (long long)j * g.kv_stride_tok, x);
+                if (s > m) {
+                    const float alpha = expf(m - s);   // (m = -inf: 0)
+                    m = s;
+                    l *= alpha;
 #pragma unroll
-                for (int i = 0; i < N; ++i) acc[i] *= alpha;
+                    for (int i = 0; i < N; ++i) acc[i] *= alpha;
+                }
+                // scores of -inf alone so far weigh nothing; a NaN score, or one of +inf, makes the row NaN
+                const float p = s == -INFINITY ? 0.f : expf(s - m);
+                l += p;
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc[i] = fmaf(p, x[i], acc[i]);
             }
-            // scores of -inf alone so far weigh nothing; a NaN score, or one of +inf, makes the row NaN
-            const float p = s == -INFINITY ? 0.f : expf(s - m);
-            l += p;
-#pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] = fmaf(p, x[i], acc[i]);
+        float lse = l == 0.f ? -INFINITY : m + logf(l);
+        float wa = 0.f, wb = l == 0.f ? 0.f : 1.0f / l;
+        float* lp = a.lse + (long long)h * g.lq + row;
+        if (a.accumulate) {
+            const float old = *lp, mm = fmaxf(old, lse);
+            if (mm != -INFINITY) {
+                const float ea = expf(old - mm), eb = expf(lse - mm), r = 1.0f / (ea + eb);
+                wa = ea * r;
+                wb *= eb * r;
+                lse = mm + logf(ea + eb);
+            }
         }
-    float lse = l == 0.f ? -INFINITY : m + logf(l);
-    float wa = 0.f, wb = l == 0.f ? 0.f : 1.0f / l;
-    float* lp = a.lse + (long long)h * g.lq + row;
-    if (a.accumulate) {
-        const float old = *lp, mm = fmaxf(old, lse);
-        if (mm != -INFINITY) {
-            const float ea = expf(old - mm), eb = expf(lse - mm), r = 1.0f / (ea + eb);
-            wa = ea * r;
-            wb *= eb * r;
-            lse = mm + logf(ea + eb);
-        }
-    }
-    __builtin_amdgcn_wave_barrier();              // the four lanes of a row have read the old value
-    if (col == 0) *lp = lse;
-    const long long at = ((long long)row * g.nq + h) * D + col;
+        __builtin_amdgcn_wave_barrier();              // the lanes of a row have read the old value
+        if (col == 0) *lp = lse;
+        const long long at = ((long long)row * g.nq + h) * D + col;
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (a.accumulate) old = *reinterpret_cast<const float4*>(a.o + at + i);
-        store4(a.o, at + i, a.out_bf16, wa * old.x + wb * acc[i], wa * old.y + wb * acc[i + 1], wa * old.z + wb * acc[i + 2], wa * old.w + wb * acc[i + 3]);
+        for (int i = 0; i < N; i += 4) {
+            float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (a.accumulate) old = *reinterpret_cast<const float4*>(a.o + at + i);
+            store4(a.o, at + i, a.out_bf16, wa * old.x + wb * acc[i], wa * old.y + wb * acc[i + 1], wa * old.z + wb * acc[i + 2], wa * old.w + wb * acc[i + 3]);
+        }
     }
 }
 
-// dq of rows [row0, row0 + 64) of head h.
-template <class T, int D> __device__ __forceinline__ void dq_unit(const WinBwdArgs& a, const int h, const int row0)
+// dq of rows [row0, row0 + rows) of head h.
+template <class T, int D> __device__ __forceinline__ void dq_unit(const WinBwdArgs& a, const int h, const int row0, const int rows)
 {
-    constexpr int N = D / 4;
+    constexpr int N = D / LANES;
     const AttnGeom& g = a.g;
-    const int row = row0 + (int)threadIdx.x / 4, col = (int)threadIdx.x % 4 * N;
-    if (row >= g.lq) return;
-    const WinKeys w = win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink);
-    const T* k = static_cast<const T*>(a.k) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
-    const T* v = static_cast<const T*>(a.v) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
-    const long long q_at = (long long)row * g.q_stride_tok + (long long)h * g.q_stride_head + col;
-    float q[N], d_o[N], acc[N];
-    load_cols(static_cast<const T*>(a.q) + q_at, q);
-    load_cols(static_cast<const T*>(a.d_o) + q_at, d_o);
+    const int col = (int)threadIdx.x % LANES * N, end_row = row0 + rows < g.lq ? row0 + rows : g.lq;
+    for (int row = row0 + (int)threadIdx.x / LANES; row < end_row; row += (int)blockDim.x / LANES) {
+        const WinKeys w = win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink);
+        const T* k = static_cast<const T*>(a.k) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
+        const T* v = static_cast<const T*>(a.v) + (long long)g.kv_of_q[h] * g.kv_stride_head + col;
+        const long long q_at = (long long)row * g.q_stride_tok + (long long)h * g.q_stride_head + col;
+        float q[N], d_o[N], acc[N];
+        load_cols(static_cast<const T*>(a.q) + q_at, q);
+        load_cols(static_cast<const T*>(a.d_o) + q_at, d_o);
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.f;
-    const float lse = a.lse[(long long)h * g.lq + row], delta = a.delta[(long long)h * g.lq + row];
-    const bool live = fabsf(lse) != INFINITY;
-    for (int part = 0; part < 2; ++part)
-        for (int j = part ? w.lo : 0, end = !live ? 0 : part ? w.hi : w.sink; j < end; ++j) {
-            float x[N], y[N];
-            load_cols(k + (long long)j * g.kv_stride_tok, x);
-            load_cols(v + (long long)j * g.kv_stride_tok, y);
-            const float ds = expf(dot(q, x) * g.scale - lse) * (dot(d_o, y) - delta);
+        for (int i = 0; i < N; ++i) acc[i] = 0.f;
+        const float lse = a.lse[(long long)h * g.lq + row], delta = a.delta[(long long)h * g.lq + row];
+        const bool live = fabsf(lse) != INFINITY;
+        for (int part = 0; part < 2; ++part)
+            for (int j = part ? w.lo : 0, end = !live ? 0 : part ? w.hi : w.sink; j < end; ++j) {
+                float x[N], y[N];
+                load_cols(k + (long long)j * g.kv_stride_tok, x);
+                load_cols(v + (long long)j * g.kv_stride_tok, y);
+                const float ds = expf(dot(q, x) * g.scale - lse) * (dot(d_o, y) - delta);
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc[i] = fmaf(ds, x[i], acc[i]);
+                for (int i = 0; i < N; ++i) acc[i] = fmaf(ds, x[i], acc[i]);
+            }
+        const long long at = ((long long)row * g.nq + h) * D + col;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (!a.out_bf16) old = *reinterpret_cast<const float4*>(a.dq + at + i);
+            store4(a.dq, at + i, a.out_bf16, fmaf(g.scale, acc[i], old.x), fmaf(g.scale, acc[i + 1], old.y), fmaf(g.scale, acc[i + 2], old.z), fmaf(g.scale, acc[i + 3], old.w));
         }
-    const long long at = ((long long)row * g.nq + h) * D + col;
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!a.out_bf16) old = *reinterpret_cast<const float4*>(a.dq + at + i);
-        store4(a.dq, at + i, a.out_bf16, fmaf(g.scale, acc[i], old.x), fmaf(g.scale, acc[i + 1], old.y), fmaf(g.scale, acc[i + 2], old.z), fmaf(g.scale, acc[i + 3], old.w));
     }
 }
 
-// dk and dv of keys [col0, col0 + 64) of kv head kvh.
-template <class T, int D> __device__ __forceinline__ void dkdv_unit(const WinBwdArgs& a, const int kvh, const int col0)
+// dk and dv of keys [col0, col0 + keys) of kv head kvh.
+template <class T, int D> __device__ __forceinline__ void dkdv_unit(const WinBwdArgs& a, const int kvh, const int col0, const int keys)
 {
-    constexpr int N = D / 4;
+    constexpr int N = D / LANES;
     const AttnGeom& g = a.g;
-    const int key = col0 + (int)threadIdx.x / 4, col = (int)threadIdx.x % 4 * N;
-    if (key >= g.lc) return;
-    const WinRows w = win_rows_of_key(g.qs, seg_pos_of_row(g.ks, key), a.window, a.n_sink);
-    const long long kv_at = (long long)key * g.kv_stride_tok + (long long)kvh * g.kv_stride_head + col;
-    float k[N], v[N], dk[N], dv[N];
-    load_cols(static_cast<const T*>(a.k) + kv_at, k);
-    load_cols(static_cast<const T*>(a.v) + kv_at, v);
+    const int col = (int)threadIdx.x % LANES * N, end_key = col0 + keys < g.lc ? col0 + keys : g.lc;
+    for (int key = col0 + (int)threadIdx.x / LANES; key < end_key; key += (int)blockDim.x / LANES) {
+        const WinRows w = win_rows_of_key(g.qs, seg_pos_of_row(g.ks, key), a.window, a.n_sink);
+        const long long kv_at = (long long)key * g.kv_stride_tok + (long long)kvh * g.kv_stride_head + col;
+        float k[N], v[N], dk[N], dv[N];
+        load_cols(static_cast<const T*>(a.k) + kv_at, k);
+        load_cols(static_cast<const T*>(a.v) + kv_at, v);
 #pragma unroll
-    for (int i = 0; i < N; ++i) { dk[i] = 0.f; dv[i] = 0.f; }
-    for (int h = 0; h < g.nq; ++h) {
-        if (g.kv_of_q[h] != kvh) continue;
-        const T* q = static_cast<const T*>(a.q) + (long long)h * g.q_stride_head + col;
-        const T* d_o = static_cast<const T*>(a.d_o) + (long long)h * g.q_stride_head + col;
-        for (int i = w.first; i < w.end; ++i) {
-            const float lse = a.lse[(long long)h * g.lq + i], delta = a.delta[(long long)h * g.lq + i];
-            if (fabsf(lse) == INFINITY) continue;
-            float x[N], y[N];
-            load_cols(q + (long long)i * g.q_stride_tok, x);
-            load_cols(d_o + (long long)i * g.q_stride_tok, y);
-            const float p = expf(dot(k, x) * g.scale - lse), ds = p * (dot(v, y) - delta);
+        for (int i = 0; i < N; ++i) { dk[i] = 0.f; dv[i] = 0.f; }
+        for (int h = 0; h < g.nq; ++h) {
+            if (g.kv_of_q[h] != kvh) continue;
+            const T* q = static_cast<const T*>(a.q) + (long long)h * g.q_stride_head + col;
+            const T* d_o = static_cast<const T*>(a.d_o) + (long long)h * g.q_stride_head + col;
+            for (int i = w.first; i < w.end; ++i) {
+                const float lse = a.lse[(long long)h * g.lq + i], delta = a.delta[(long long)h * g.lq + i];
+                if (fabsf(lse) == INFINITY) continue;
+                float x[N], y[N];
+                load_cols(q + (long long)i * g.q_stride_tok, x);
+                load_cols(d_o + (long long)i * g.q_stride_tok, y);
+                const float p = expf(dot(k, x) * g.scale - lse), ds = p * (dot(v, y) - delta);
 #pragma unroll
-            for (int c = 0; c < N; ++c) { dv[c] = fmaf(p, y[c], dv[c]); dk[c] = fmaf(ds, x[c], dk[c]); }
+                for (int c = 0; c < N; ++c) { dv[c] = fmaf(p, y[c], dv[c]); dk[c] = fmaf(ds, x[c], dk[c]); }
+            }
         }
-    }
-    const long long at = ((long long)key * g.nkv + kvh) * D + col;
+        const long long at = ((long long)key * g.nkv + kvh) * D + col;
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        float4 ok = make_float4(0.f, 0.f, 0.f, 0.f), ov = ok;
-        if (a.accumulate) { ok = *reinterpret_cast<const float4*>(a.dk + at + i); ov = *reinterpret_cast<const float4*>(a.dv + at + i); }
-        store4(a.dk, at + i, a.out_bf16, fmaf(g.scale, dk[i], ok.x), fmaf(g.scale, dk[i + 1], ok.y), fmaf(g.scale, dk[i + 2], ok.z), fmaf(g.scale, dk[i + 3], ok.w));
-        store4(a.dv, at + i, a.out_bf16, dv[i] + ov.x, dv[i + 1] + ov.y, dv[i + 2] + ov.z, dv[i + 3] + ov.w);
+        for (int i = 0; i < N; i += 4) {
+            float4 ok = make_float4(0.f, 0.f, 0.f, 0.f), ov = ok;
+            if (a.accumulate) { ok = *reinterpret_cast<const float4*>(a.dk + at + i); ov = *reinterpret_cast<const float4*>(a.dv + at + i); }
+            store4(a.dk, at + i, a.out_bf16, fmaf(g.scale, dk[i], ok.x), fmaf(g.scale, dk[i + 1], ok.y), fmaf(g.scale, dk[i + 2], ok.z), fmaf(g.scale, dk[i + 3], ok.w));
+            store4(a.dv, at + i, a.out_bf16, dv[i] + ov.x, dv[i + 1] + ov.y, dv[i + 2] + ov.z, dv[i + 3] + ov.w);
+        }
     }
 }
 
