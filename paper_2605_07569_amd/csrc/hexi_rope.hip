@@ -1,9 +1,8 @@
 // Rotary positions with several axes on a shard's rows, alone (hexi_rope) and on the way into or out of the ragged all-to-all
 // (hexi_rope_a2a_pack / _unpack).  HBM-bound: every element is read once and written once.
 //
-// A thread owns P pairs of columns of one row (one 16-byte piece of x on either side), forms their sines and cosines once, in registers,
-// and walks the heads with them.  A row of a head is head_dim / (2 P) neighbouring threads, so a wavefront reads whole rows of
-// 64 / (head_dim / 2 P) tokens.
+// A workgroup owns a few tokens: it forms their sines and cosines in LDS, then walks their pieces in the order in which they lie in memory.  A piece is P pairs of
+// columns of one head (one 16-byte load of x on either side); head_dim / (2 P) neighbouring threads take a head's row, the next threads the next head.
 //
 // Angle: position times frequency in quarter turns, t = pos (c_hi + c_lo) with c the frequency times 2 / pi as two doubles.  With q = rint(t)
 // the rest r = fma(pos, c_lo, fma(pos, c_hi, -q)) is exact to 2^-53 whatever the position, and |r| <= 1/2 (an eighth of a turn), so fp32 holds it to
@@ -63,23 +62,34 @@ template <int P> struct Piece<uint16_t, P> {
     }
 };
 
+// n / d for n < 2^31: (mulhi(n, mul) + n) >> shift, mul = ceil(2^(32 + shift) / d) - 2^32.
+struct Divisor {
+    unsigned d, mul, shift;
+    explicit Divisor(unsigned x) : d(x), shift(0)
+    {
+        while ((1ull << shift) < x) ++shift;
+        mul = (unsigned)(((1ull << 32) * ((1ull << shift) - x)) / x + 1);
+    }
+    __device__ __forceinline__ unsigned operator()(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
+
 // Where a slot's row lies on either side, and whether its head is rotated.
 template <class X, class Y> struct Where { const X* x; Y* y; bool rotate; };
 struct InTensors {
     RopeTensors t;
-    __device__ __forceinline__ int slots() const { return t.first[t.n]; }
     template <class X, class Y> __device__ __forceinline__ Where<X, Y> at(int slot, int row, const RopeGeom&) const
     {
-        int i = 0;
-        while (slot >= t.first[i + 1]) ++i;
-        const hexi_rope_tensor& a = t.t[i];
-        const int h = slot - t.first[i];
+        hexi_rope_tensor a = t.t[0];
+        int first = 0;
+#pragma unroll
+        for (int i = 1; i < HEXI_ROPE_MAX_TENSORS; ++i)
+            if (i < t.n && slot >= t.first[i]) { a = t.t[i]; first = t.first[i]; }
+        const int h = slot - first;
         return {static_cast<const X*>(a.x) + row * a.x_stride_tok + h * a.x_stride_head, static_cast<Y*>(a.y) + row * a.y_stride_tok + h * a.y_stride_head, true};
     }
 };
 template <bool PACK> struct InParts {
     RopeParts p;
-    __device__ __forceinline__ int slots() const { return p.tb.n_slots; }
     template <class X, class Y> __device__ __forceinline__ Where<X, Y> at(int slot, int row, const RopeGeom& g) const
     {
         const long long whole = row * p.x_stride_tok + (long long)p.tb.head[slot] * g.head_dim;
@@ -88,69 +98,84 @@ template <bool PACK> struct InParts {
     }
 };
 
-// Workgroup (x, y): rows [x rows_per_block, ..), slots [y slots_per_block, ..).
+// Workgroup: tokens [tokens blockIdx.x, + tokens), all slots; by_token divides by the pieces of a token, by_row by those of a head's row.
 template <class X, class Y, class IN, bool ADJACENT>
-__global__ void __launch_bounds__(256) rope_kernel(const RopeGeom g, const IN in, const int rows_per_block, const int slots_per_block)
+__global__ void __launch_bounds__(256) rope_kernel(const RopeGeom g, const IN in, const int tokens, const Divisor by_token, const Divisor by_row)
 {
-    constexpr int P = 16 / sizeof(X);
-    const int units = g.head_dim / (2 * P);                 // threads of a row
-    const int local = (int)threadIdx.x / units, u = (int)threadIdx.x - local * units;
-    const int row = (int)blockIdx.x * rows_per_block + local;
-    if (local >= rows_per_block || row >= g.rows) return;
-    const bool rotated = u < g.rot_dim / (2 * P);           // otherwise 2 P columns that are copied
-    const int col_a = rotated && !ADJACENT ? P * u : 2 * P * u, col_b = rotated && !ADJACENT ? g.rot_dim / 2 + P * u : 2 * P * u + P;
-    float sn[P], cs[P];
-    if (rotated) {
-        const int own = g.positions ? 0 : seg_pos_of_row(g.range, row);
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const int p = P * u + i;
-            const int pos = g.positions ? g.positions[(long long)g.axis[p] * g.pos_stride + row] : own;
-            sincos_turns(pos, g.turn_hi[p], g.turn_lo[p], sn[i], cs[i]);
-            if (g.inverse) sn[i] = -sn[i];
-        }
+    constexpr int P = 16 / sizeof(X), UNROLL = 4;
+    extern __shared__ __attribute__((aligned(16))) float cos_of[];      // [tokens][pairs], and the sines behind them
+    const int t0 = (int)blockIdx.x * tokens, n_tokens = g.rows - t0 < tokens ? g.rows - t0 : tokens;
+    const int pairs = g.rot_dim / 2;
+    float* const sin_of = cos_of + tokens * pairs;
+    for (int i = threadIdx.x; i < n_tokens * pairs; i += 256) {
+        const int tok = i / pairs, p = i - tok * pairs;
+        const int pos = g.positions ? g.positions[(long long)g.axis[p] * g.pos_stride + t0 + tok] : seg_pos_of_row(g.range, t0 + tok);
+        float sn, cs;
+        sincos_turns(pos, g.turn_hi[p], g.turn_lo[p], sn, cs);
+        cos_of[i] = cs;
+        sin_of[i] = g.inverse ? -sn : sn;
     }
-    const int first = (int)blockIdx.y * slots_per_block, end = first + slots_per_block < in.slots() ? first + slots_per_block : in.slots();
-    constexpr int UNROLL = 4;
-    for (int s = first; s < end; s += UNROLL) {
+    __syncthreads();
+    const unsigned total = (unsigned)n_tokens * by_token.d;
+    for (unsigned i0 = threadIdx.x; i0 < total; i0 += 256 * UNROLL) {
         float a[UNROLL][P], b[UNROLL][P];
+        Where<X, Y> w[UNROLL];
+        int trig[UNROLL], col_a[UNROLL], col_b[UNROLL];
 #pragma unroll
-        for (int i = 0; i < UNROLL; ++i)
-            if (s + i < end) {
-                const Where<X, Y> w = in.template at<X, Y>(s + i, row, g);
-                Piece<X, P>::load(w.x + col_a, a[i]);
-                Piece<X, P>::load(w.x + col_b, b[i]);
-            }
+        for (int k = 0; k < UNROLL; ++k) {
+            const unsigned i = i0 + 256 * k;
+            if (i >= total) break;
+            const unsigned tok = by_token(i), piece = i - tok * by_token.d, slot = by_row(piece);
+            const int u = (int)(piece - slot * by_row.d);
+            const bool rotated = u < pairs / P;             // otherwise 2 P columns that are copied
+            col_a[k] = rotated && !ADJACENT ? P * u : 2 * P * u;
+            col_b[k] = rotated && !ADJACENT ? pairs + P * u : 2 * P * u + P;
+            w[k] = in.template at<X, Y>((int)slot, t0 + (int)tok, g);
+            trig[k] = rotated && w[k].rotate ? (int)tok * pairs + P * u : -1;
+            Piece<X, P>::load(w[k].x + col_a[k], a[k]);
+            Piece<X, P>::load(w[k].x + col_b[k], b[k]);
+        }
 #pragma unroll
-        for (int i = 0; i < UNROLL; ++i)
-            if (s + i < end) {
-                const Where<X, Y> w = in.template at<X, Y>(s + i, row, g);
-                if (rotated && w.rotate) {
+        for (int k = 0; k < UNROLL; ++k) {
+            if (i0 + 256 * k >= total) break;
+            if (trig[k] >= 0) {
+                float cs[P], sn[P];
 #pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        // HALF: pair e is (a[e], b[e]); ADJACENT: the 2 P columns of a and b in a row are its pairs
-                        float& x = ADJACENT ? (e < P / 2 ? a[i][(2 * e) % P] : b[i][(2 * e) % P]) : a[i][e];
-                        float& y = ADJACENT ? (e < P / 2 ? a[i][(2 * e + 1) % P] : b[i][(2 * e + 1) % P]) : b[i][e];
-                        const float x0 = x, y0 = y;
-                        x = x0 * cs[e] - y0 * sn[e];
-                        y = y0 * cs[e] + x0 * sn[e];
-                    }
+                for (int e = 0; e < P; e += 4) {
+                    const f32x4 c4 = *reinterpret_cast<const f32x4*>(&cos_of[trig[k] + e]), s4 = *reinterpret_cast<const f32x4*>(&sin_of[trig[k] + e]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) { cs[e + j] = c4[j]; sn[e + j] = s4[j]; }
                 }
-                Piece<Y, P>::store(w.y + col_a, a[i]);
-                Piece<Y, P>::store(w.y + col_b, b[i]);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    // HALF: pair e is (a[e], b[e]); ADJACENT: the 2 P columns of a and b in a row are its pairs
+                    float& x = ADJACENT ? (e < P / 2 ? a[k][(2 * e) % P] : b[k][(2 * e) % P]) : a[k][e];
+                    float& y = ADJACENT ? (e < P / 2 ? a[k][(2 * e + 1) % P] : b[k][(2 * e + 1) % P]) : b[k][e];
+                    const float x0 = x, y0 = y;
+                    x = x0 * cs[e] - y0 * sn[e];
+                    y = y0 * cs[e] + x0 * sn[e];
+                }
             }
+            Piece<Y, P>::store(w[k].y + col_a[k], a[k]);
+            Piece<Y, P>::store(w[k].y + col_b[k], b[k]);
+        }
     }
 }
 
 template <class X, class Y, class IN> hipError_t launch(const RopeGeom& g, const IN& in, int n_slots, hipStream_t s)
 {
     if (n_slots == 0) return hipSuccess;
-    const int rows_per_block = 256 / (g.head_dim / (2 * (16 / (int)sizeof(X))));
-    const unsigned row_blocks = (unsigned)((g.rows + rows_per_block - 1) / rows_per_block);
-    int per = n_slots;
-    const dim3 grid(row_blocks, (unsigned)((n_slots + per - 1) / per));
-    if (g.adjacent) rope_kernel<X, Y, IN, true><<<grid, 256, 0, s>>>(g, in, rows_per_block, per);
-    else rope_kernel<X, Y, IN, false><<<grid, 256, 0, s>>>(g, in, rows_per_block, per);
+    const unsigned row = (unsigned)g.head_dim / (2 * (16 / sizeof(X)));
+    const Divisor by_token(row * (unsigned)n_slots), by_row(row);
+    // Tokens of a workgroup: 2 to 4 pieces a thread, so that many workgroups are under way at different places, unless there are too few rows to go round.
+    // us for 1 / 2 / 4 / 16 tokens: 32768 rows of 40 heads (320 pieces a token) 127 / 111 / 114 / 130; 16384 x 52 heads, packed (416) 83 / 70 / 74 / 80; 8191 x 32
+    // heads from fp32 to bf16 (512) 41 / 43 / 46 / 45.
+    const int most = by_token.d < 640 ? 640 / (int)by_token.d : 1, share = (g.rows + 1023) / 1024;
+    const int tokens = most < share ? most : share;
+    const unsigned grid = (unsigned)((g.rows + tokens - 1) / tokens);
+    const size_t lds = 2 * sizeof(float) * (size_t)(tokens * (g.rot_dim / 2));      // at most 640 pieces of 8 pairs: 40 KB
+    if (g.adjacent) rope_kernel<X, Y, IN, true><<<grid, 256, lds, s>>>(g, in, tokens, by_token, by_row);
+    else rope_kernel<X, Y, IN, false><<<grid, 256, lds, s>>>(g, in, tokens, by_token, by_row);
     return hipGetLastError();
 }
 

@@ -146,7 +146,17 @@ def make_range(segs: Sequence[Tuple[int, int]]):
     arr = (hexi_seg * max(1, len(segs)))(*[(int(s), int(n)) for s, n in segs])
     r = hexi_range(len(segs), arr)
     r._keep = arr
+    r._rows = sum(int(n) for _, n in segs)
     return r, arr
+
+
+def _with_rows(segs):
+    """A range and its rows (whatever is wrong with a range the library says)."""
+    r = segs if isinstance(segs, hexi_range) else make_range(segs)[0]
+    rows = getattr(r, "_rows", None)
+    if rows is None:
+        rows = sum(r.segs[i].len for i in range(max(0, min(r.n_segs, HEXI_MAX_SEGS))))
+    return r, rows
 
 
 def make_desc(dtype, head_dim, n_q_heads, n_kv_heads, softmax_scale, q_strides, kv_strides, kv_of_q=None):
@@ -259,51 +269,49 @@ def _refuse(msg):
     raise HexiError(HEXI_EINVAL, msg)
 
 
-_DTYPES = None
+_DTYPES = {}
 
 
 def _dtype(t):
-    global _DTYPES
-    if _DTYPES is None:
+    if not _DTYPES:
         import torch
-        _DTYPES = {torch.bfloat16: HEXI_BF16, torch.float32: HEXI_F32}
+        _DTYPES.update({torch.bfloat16: HEXI_BF16, torch.float32: HEXI_F32})
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise HexiError(HEXI_EUNSUPPORTED, f"element type {t.dtype} (bf16 or fp32)")
     return code
 
 
-def _on_device(*tensors):
-    """Tensors that the current device's stream may use."""
+def _current_device():
+    """Index of the GPU whose stream the calls use; no tensor is on -2, where none is initialised."""
     import torch
-    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else None
-    for t in tensors:
-        if t is not None and (not t.is_cuda or (dev is not None and t.get_device() != dev)):
-            _refuse(f"a tensor is on {t.device}, not on the current GPU")
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
 
 
-def _dense(name, t, shape, dtype=None):
-    if tuple(t.shape) != shape or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
-        _refuse(f"{name}: a contiguous {shape} tensor{'' if dtype is None else f' of {dtype}'} is needed, not {tuple(t.shape)} {t.dtype}")
+def _fits(name, t, shape, dtype, dev, strides=None):
+    """Refuses a tensor that is not of this shape and element type (a code of the library), on the current GPU, dense or with these strides."""
+    if tuple(t.shape) != shape or _dtype(t) != dtype:
+        _refuse(f"{name}: {shape} elements of type {dtype} are needed, not {tuple(t.shape)} {t.dtype}")
+    if not t.is_contiguous() if strides is None else t.stride() != strides and any(s != w and n > 1 for s, w, n in zip(t.stride(), strides, shape)):
+        _refuse(f"{name}: strides {t.stride()}; {'a contiguous tensor is needed' if strides is None else f'the descriptor says {strides}'}")
+    if t.get_device() != dev:
+        _refuse(f"{name} is on {t.device}, not on the current GPU")
 
 
-def _win_ranges(desc, q_segs, kv_segs, q, k, v, lse, d_o=None):
-    """Ranges of a windowed call, with what the binding can check of the tensors checked: element types, shapes, strides, device."""
-    import torch
-    qr = q_segs if isinstance(q_segs, hexi_range) else make_range(q_segs)[0]
-    kr = kv_segs if isinstance(kv_segs, hexi_range) else make_range(kv_segs)[0]
-    # (whatever else is wrong with a range the library refuses)
-    lq = sum(qr.segs[i].len for i in range(max(0, min(qr.n_segs, HEXI_MAX_SEGS))))
-    lc = sum(kr.segs[i].len for i in range(max(0, min(kr.n_segs, HEXI_MAX_SEGS))))
-    d, nq, nkv = desc.head_dim, desc.n_q_heads, desc.n_kv_heads
-    for name, t, shape, strides in (("q", q, (lq, nq, d), (desc.q_stride_tok, desc.q_stride_head, 1)), ("d_o", d_o, (lq, nq, d), (desc.q_stride_tok, desc.q_stride_head, 1)),
-                                    ("k", k, (lc, nkv, d), (desc.kv_stride_tok, desc.kv_stride_head, 1)), ("v", v, (lc, nkv, d), (desc.kv_stride_tok, desc.kv_stride_head, 1))):
-        if t is None:
-            continue
-        if tuple(t.shape) != shape or _dtype(t) != desc.dtype or any(s != w and n > 1 for s, w, n in zip(t.stride(), strides, shape)):
-            _refuse(f"{name} is {tuple(t.shape)} with strides {t.stride()}, {t.dtype}; the descriptor and the ranges say {shape} with strides {strides}")
-    _dense("lse", lse, (nq, lq), torch.float32)
-    return qr, kr, lq, lc
+def _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o=None):
+    """Ranges, rows, keys and device of a windowed call, its inputs checked."""
+    qr, lq = _with_rows(q_segs)
+    kr, lc = _with_rows(kv_segs)
+    dev, dt, d = _current_device(), desc.dtype, desc.head_dim
+    shape, strides = (lq, desc.n_q_heads, d), (desc.q_stride_tok, desc.q_stride_head, 1)
+    _fits("q", q, shape, dt, dev, strides)
+    if d_o is not None:
+        _fits("d_o", d_o, shape, dt, dev, strides)
+    shape, strides = (lc, desc.n_kv_heads, d), (desc.kv_stride_tok, desc.kv_stride_head, 1)
+    _fits("k", k, shape, dt, dev, strides)
+    _fits("v", v, shape, dt, dev, strides)
+    _fits("lse", lse, (desc.n_q_heads, lq), HEXI_F32, dev)
+    return qr, kr, lq, lc, dev
 
 
 def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
@@ -312,33 +320,37 @@ def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
 
 def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flags=0, workspace=None, stream=None):
     """Windowed forward; o's element type (fp32 or bf16) is the result's."""
-    lib = _lib or load()
-    qr, kr, lq, lc = _win_ranges(desc, q_segs, kv_segs, q, k, v, lse)
-    _dense("o", o, (lq, desc.n_q_heads, desc.head_dim))
-    _on_device(q, k, v, o, lse, workspace)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib.hexi_attn_win_fwd_chunk(desc, window, qr, kr, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _dtype(o), _ptr(lse), flags, _ptr(workspace), ws_bytes,
-                                     _stream(stream))
+    qr, kr, lq, lc, dev = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse)
+    o_type = _dtype(o)
+    _fits("o", o, (lq, desc.n_q_heads, desc.head_dim), o_type, dev)
+    ws_bytes = 0
+    if workspace is not None:
+        if workspace.get_device() != dev:
+            _refuse(f"workspace is on {workspace.device}, not on the current GPU")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    rc = (_lib or load()).hexi_attn_win_fwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), o_type, lse.data_ptr(), flags,
+                                                  _ptr(workspace), ws_bytes, _stream(stream))
     if rc:
         _check(rc)
 
 
 def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq, dk, dv, flags=0, stream=None):
     """Windowed backward; the element type of dq, dk and dv (one for all; None for the half that is skipped) is the gradients'."""
-    import torch
-    lib = _lib or load()
-    qr, kr, lq, lc = _win_ranges(desc, q_segs, kv_segs, q, k, v, lse, d_o)
+    qr, kr, lq, lc, dev = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o)
     nq, nkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
-    _dense("delta", delta, (nq, lq), torch.float32)
+    _fits("delta", delta, (nq, lq), HEXI_F32, dev)
+    o_type = grad = HEXI_F32
     if o is not None:
-        _dense("o", o, (lq, nq, d))
-    grads = [t for t in (dq, dk, dv) if t is not None]
+        o_type = _dtype(o)
+        _fits("o", o, (lq, nq, d), o_type, dev)
+    for t in (dv, dk, dq):
+        if t is not None:
+            grad = _dtype(t)
     for name, t, shape in (("dq", dq, (lq, nq, d)), ("dk", dk, (lc, nkv, d)), ("dv", dv, (lc, nkv, d))):
         if t is not None:
-            _dense(name, t, shape, grads[0].dtype)
-    _on_device(q, k, v, o, d_o, lse, delta, *grads)
-    rc = lib.hexi_attn_win_bwd_chunk(desc, window, qr, kr, _ptr(q), _ptr(k), _ptr(v), _ptr(o), HEXI_F32 if o is None else _dtype(o), _ptr(d_o), _ptr(lse),
-                                     _ptr(delta), _ptr(dq), _ptr(dk), _ptr(dv), _dtype(grads[0]) if grads else HEXI_F32, flags, _stream(stream))
+            _fits(name, t, shape, grad, dev)
+    rc = (_lib or load()).hexi_attn_win_bwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(o), o_type, d_o.data_ptr(), lse.data_ptr(),
+                                                  delta.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), grad, flags, _stream(stream))
     if rc:
         _check(rc)
 
@@ -359,58 +371,62 @@ def make_rope(head_dim, inv_freq, axis_of_pair=None, pairing="half", n_axes=None
     return d
 
 
-def _rope_positions(rope, positions, rows):
+def _rope_positions(rope, positions, rows, dev):
     if positions is None:
         return None, 0
     import torch
-    if positions.dtype != torch.int32 or positions.dim() != 2 or tuple(positions.shape) != (rope.n_axes, rows) or (rows > 1 and positions.stride(1) != 1):
-        _refuse(f"positions: an int32 [{rope.n_axes}][{rows}] tensor is needed, not {tuple(positions.shape)} {positions.dtype}")
-    return positions.data_ptr(), positions.stride(0) if rope.n_axes > 1 else max(1, rows)
-
-
-def _rope_rows(segs):
-    r = segs if isinstance(segs, hexi_range) else make_range(segs)[0]
-    return r, sum(r.segs[i].len for i in range(max(0, min(r.n_segs, HEXI_MAX_SEGS))))
+    n = rope.n_axes
+    if positions.dtype != torch.int32 or tuple(positions.shape) != (n, rows) or (rows > 1 and positions.stride(1) != 1) or (n > 1 and positions.stride(0) < rows):
+        _refuse(f"positions: an int32 [{n}][{rows}] tensor is needed, not {tuple(positions.shape)} {positions.dtype} with strides {positions.stride()}")
+    if positions.get_device() != dev:
+        _refuse(f"positions are on {positions.device}, not on the current GPU")
+    return positions.data_ptr(), positions.stride(0) if n > 1 else rows
 
 
 def hexi_rope(rope, segs, tensors, positions=None, inverse=False, stream=None):
     """Rotates the tensors of a shard in one launch.  tensors: [(x, y), ...], x and y [rows, heads, head_dim] with contiguous columns, y may be x; all x
     of one element type, all y of one.  positions: int32 [n_axes, rows] on the device, or None for the rows' global positions."""
-    lib = _lib or load()
-    r, rows = _rope_rows(segs)
+    r, rows = _with_rows(segs)
     if not tensors:
         _refuse("no tensors")
-    pos, pos_stride = _rope_positions(rope, positions, rows)
+    dev, d = _current_device(), rope.head_dim
+    pos, pos_stride = _rope_positions(rope, positions, rows, dev)
+    x_type, y_type = _dtype(tensors[0][0]), _dtype(tensors[0][1])
     arr = (hexi_rope_tensor * len(tensors))()
-    x0, y0 = tensors[0]
-    for a, (x, y) in zip(arr, tensors):
-        if x.dim() != 3 or x.shape != y.shape or x.shape[0] != rows or x.shape[2] != rope.head_dim or x.stride(2) != 1 or y.stride(2) != 1 or \
-                x.dtype != x0.dtype or y.dtype != y0.dtype:
-            _refuse(f"a tensor pair of [{rows}, heads, {rope.head_dim}] and one type a side is needed, not {tuple(x.shape)} {x.dtype} -> {tuple(y.shape)} {y.dtype}")
-        # (the stride of an axis of one element is any)
-        d = rope.head_dim
-        st = [t.stride(i) if t.shape[i] > 1 else d * (t.shape[1] if i == 0 else 1) for t in (x, y) for i in (0, 1)]
-        a.x, a.y, a.n_heads = x.data_ptr(), y.data_ptr(), x.shape[1]
-        a.x_stride_tok, a.x_stride_head, a.y_stride_tok, a.y_stride_head = st
-        _on_device(x, y, positions)
-    rc = lib.hexi_rope(rope, r, pos, pos_stride, arr, len(tensors), _dtype(x0), _dtype(y0), HEXI_ROPE_INVERSE if inverse else 0, _stream(stream))
+    for i, (x, y) in enumerate(tensors):
+        shape, xs, ys = x.shape, x.stride(), y.stride()
+        if len(shape) != 3 or y.shape != shape or shape[0] != rows or shape[2] != d or xs[2] != 1 or ys[2] != 1 or _dtype(x) != x_type or _dtype(y) != y_type:
+            _refuse(f"a tensor pair of [{rows}, heads, {d}] and one type a side is needed, not {tuple(shape)} {x.dtype} -> {tuple(y.shape)} {y.dtype}")
+        if x.get_device() != dev or y.get_device() != dev:
+            _refuse(f"a tensor is on {x.device} or {y.device}, not on the current GPU")
+        h = shape[1]
+        if rows == 1:         # the stride of an axis of one element is any
+            xs, ys = (h * d, xs[1]), (h * d, ys[1])
+        if h == 1:
+            xs, ys = (xs[0], d), (ys[0], d)
+        arr[i] = (x.data_ptr(), y.data_ptr(), h, xs[0], xs[1], ys[0], ys[1])
+    rc = (_lib or load()).hexi_rope(rope, r, pos, pos_stride, arr, len(tensors), x_type, y_type, HEXI_ROPE_INVERSE if inverse else 0, _stream(stream))
     if rc:
         _check(rc)
 
 
 def _rope_a2a(fn, rope, segs, whole, packed, src, dst, head_lists, rotate, positions, inverse, stream):
-    r, rows = _rope_rows(segs)
-    if whole.dim() != 3 or whole.shape[0] != rows or whole.shape[2] != rope.head_dim or whole.stride(2) != 1 or (whole.shape[1] > 1 and whole.stride(1) != rope.head_dim):
-        _refuse(f"a [{rows}, heads, {rope.head_dim}] tensor with packed heads is needed, not {tuple(whole.shape)} with strides {whole.stride()}")
-    n = whole.shape[1]
-    if packed.dtype != whole.dtype or not packed.is_contiguous() or packed.numel() < sum(len(h) for h in head_lists) * rows * rope.head_dim or len(rotate) != n:
+    r, rows = _with_rows(segs)
+    d, shape, strides = rope.head_dim, whole.shape, whole.stride()
+    if len(shape) != 3 or shape[0] != rows or shape[2] != d or strides[2] != 1 or (shape[1] > 1 and strides[1] != d):
+        _refuse(f"a [{rows}, heads, {d}] tensor with packed heads is needed, not {tuple(shape)} with strides {strides}")
+    n, dev = shape[1], _current_device()
+    if packed.dtype != whole.dtype or not packed.is_contiguous() or packed.numel() < sum(len(h) for h in head_lists) * rows * d or len(rotate) != n:
         _refuse(f"packed: {packed.numel()} elements of {packed.dtype}; rotate: {len(rotate)} entries for {n} heads")
-    pos, pos_stride = _rope_positions(rope, positions, rows)
-    _on_device(whole, packed, positions)
+    if whole.get_device() != dev or packed.get_device() != dev:
+        _refuse(f"a tensor is on {whole.device} or {packed.device}, not on the current GPU")
+    pos, pos_stride = _rope_positions(rope, positions, rows, dev)
     counts, heads = _head_tables(head_lists)
     flags = (ctypes.c_uint8 * max(1, n))(*[1 if x else 0 for x in rotate])
-    _check(fn(rope, r, pos, pos_stride, src.data_ptr(), dst.data_ptr(), n, _dtype(whole), whole.stride(0) if rows > 1 else n * rope.head_dim, len(head_lists), counts, heads, flags,
-              HEXI_ROPE_INVERSE if inverse else 0, _stream(stream)))
+    rc = fn(rope, r, pos, pos_stride, src.data_ptr(), dst.data_ptr(), n, _dtype(whole), strides[0] if rows > 1 else n * d, len(head_lists), counts, heads, flags,
+            HEXI_ROPE_INVERSE if inverse else 0, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def hexi_rope_a2a_pack(rope, segs, x, packed, head_lists, rotate, positions=None, inverse=False, stream=None):
