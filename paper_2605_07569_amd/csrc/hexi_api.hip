@@ -262,13 +262,24 @@ static int build_window(const hexi_window* w, int* window, int* n_sink)
     return HEXI_OK;
 }
 
-HEXI_EXPORT size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc*, const hexi_window*, int64_t, int64_t) { return 0; }
+// Splits of a forward call: by the descriptor, the window and the lengths alone, so that the workspace can be asked for without the ranges.
+static int win_fwd_splits(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
+{
+    if (!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || (d->head_dim != 64 && d->head_dim != 128) ||
+        w->window < 1 || w->n_sink < 0) return 1;
+    return hexi_win_fwd_splits(d->dtype, d->n_q_heads, lq, lc, w->window, w->n_sink);
+}
+
+HEXI_EXPORT size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc)
+{
+    const int n = win_fwd_splits(desc, window, lq, lc);
+    return n > 1 ? hexi_win_fwd_workspace(n, desc->n_q_heads, lq, desc->head_dim) : 0;
+}
 
 HEXI_EXPORT int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_window* window, const hexi_range* q_range, const hexi_range* kv_range,
                                        const void* q, const void* k, const void* v, void* o, int32_t o_dtype, float* lse, uint32_t flags,
                                        void* workspace, size_t workspace_bytes, void* hip_stream)
 {
-    (void)workspace; (void)workspace_bytes;
     WinFwdArgs a;
     int rc = build_geom(desc, q_range, kv_range, &a.g);
     if (rc == HEXI_OK) rc = build_window(window, &a.window, &a.n_sink);
@@ -283,6 +294,15 @@ HEXI_EXPORT int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_w
     a.q = q; a.k = k; a.v = v; a.o = (float*)o; a.lse = lse;
     a.accumulate = (flags & HEXI_ACCUMULATE) ? 1 : 0;
     a.out_bf16 = o_dtype == HEXI_BF16;
+    a.n_splits = win_fwd_splits(desc, window, a.g.lq, a.g.lc);
+    a.part_o = a.part_lse = nullptr;
+    if (a.n_splits > 1) {
+        const size_t need = hexi_win_fwd_workspace(a.n_splits, a.g.nq, a.g.lq, a.g.d);
+        if (!workspace || workspace_bytes < need) return fail(HEXI_EWORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+        if (!aligned16(workspace)) return fail(HEXI_EALIGN, "the workspace must be 16-byte aligned");
+        a.part_o = (float*)workspace;
+        a.part_lse = a.part_o + (size_t)a.n_splits * (size_t)a.g.lq * (size_t)a.g.nq * (size_t)a.g.d;
+    }
     const hipError_t e = hexi_launch_win_fwd(a, desc->dtype, s);
     if (e != hipSuccess) return fail(HEXI_EHIP, "windowed forward launch failed: %s", hipGetErrorString(e));
     return HEXI_OK;

@@ -129,6 +129,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     // heads of a q tile side by side, the longest (last) q tiles first
     const int h = WIN ? uniform((int)(blockIdx.x % (unsigned)g.nq)) : (int)blockIdx.x;
     const int q_tile = rest.tiles - 1 - (WIN ? uniform((int)(blockIdx.x / (unsigned)g.nq)) : (int)blockIdx.y);
+    const int split = WIN ? (int)blockIdx.y : 0;           // (a wavefront takes every fourth block of the split's part of the run)
     if (!WIN && !rest.has(h, q_tile)) return;
     const int row0 = q_tile * ROWS;
     const int kvh = arg_byte(g.kv_of_q, h);
@@ -146,9 +147,12 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     if (!WIN && sp * TB < g.lc) fetch_k(sp, 0);
     const std::conditional_t<WIN, VisibleWin, Visible64> vis = [&]() { if constexpr (WIN) return VisibleWin(a, row0, lane, l32); else return Visible64(g, row0, lane, l32); }();
     auto block = [&](int b) { if constexpr (WIN) return vis.span.block(b); else return b; };      // of the chunk, from the number in this unit's run
-    const int n_blocks = [&]() { if constexpr (WIN) return vis.n_blocks; else return (vis.n_all + TB - 1) / TB; }();
-    if (WIN && sp < n_blocks) fetch_k(block(sp), 0);
-    if (n_blocks == 0 && a.accumulate) {                   // merging an empty partial is the identity
+    const int b_first = [&]() { if constexpr (WIN) return vis.span.split_start(split, a.n_splits); else return 0; }();
+    const int n_blocks = [&]() { if constexpr (WIN) return vis.span.split_start(split + 1, a.n_splits); else return (vis.n_all + TB - 1) / TB; }();
+    const int b_mine = b_first + sp;                       // this wavefront's first block
+    const bool merges = [&]() { if constexpr (WIN) return a.merges(); else return a.accumulate != 0; }();
+    if (WIN && b_mine < n_blocks) fetch_k(block(b_mine), 0);
+    if (n_blocks == b_first && merges) {                   // merging an empty partial is the identity
         wait_transfers<0>();
         return;
     }
@@ -323,21 +327,21 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     };
 
     f32x16 s0[2], s1[2];
-    if (sp < n_blocks) {
-        const int n_whole = [&]() { if constexpr (WIN) return vis.span.n_whole; else return n_blocks < g.lc / TB ? n_blocks : g.lc / TB; }();
-        if (sp + NW < n_whole) {
-            const uint16_t *v0 = v + (long long)(block(sp) * TB) * g.kv_stride_tok, *k1 = k + (long long)(block(sp + NW) * TB) * g.kv_stride_tok;
+    if (b_mine < n_blocks) {
+        const int n_whole = [&]() { if constexpr (WIN) return vis.span.n_whole < n_blocks ? vis.span.n_whole : n_blocks; else return n_blocks < g.lc / TB ? n_blocks : g.lc / TB; }();
+        if (b_mine + NW < n_whole) {
+            const uint16_t *v0 = v + (long long)(block(b_mine) * TB) * g.kv_stride_tok, *k1 = k + (long long)(block(b_mine + NW) * TB) * g.kv_stride_tok;
             scores(s0, 0, []() {}, [&](int st) __attribute__((always_inline)) {
                 if (st < C::XFERS) fetch.one(v0, g.kv_stride_tok, lds + C::TILE_BYTES, st);
                 else fetch.one(k1, g.kv_stride_tok, lds + 2 * C::TILE_BYTES, st - C::XFERS);
             });
         } else {
-            fetch_v(block(sp), 0);
-            if (sp + NW < n_blocks) fetch_k(block(sp + NW), 1);
+            fetch_v(block(b_mine), 0);
+            if (b_mine + NW < n_blocks) fetch_k(block(b_mine + NW), 1);
             scores(s0, 0, []() {}, [](int) {});
         }
-        if (sp + NW < n_blocks) fetch_v(block(sp + NW), 1);
-        mask(s0, sp);
+        if (b_mine + NW < n_blocks) fetch_v(block(b_mine + NW), 1);
+        mask(s0, b_mine);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             m_run[r] = fmaxf(NEG_BIG, block_max(s0[r]) * c_log2);
@@ -345,7 +349,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
         }
         // two blocks at a time: the buffer is a compile-time offset of the reads
         using Steady = std::true_type; using Last = std::false_type;
-        int b = sp;
+        int b = b_mine;
         for (; b + 3 * NW < n_whole; b += 2 * NW) {
             step(IC<0>{}, Steady{}, s0, s1, b);
             step(IC<1>{}, Steady{}, s1, s0, b + NW);
@@ -356,19 +360,20 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
         }
     }
 
-    // Combine the splits: every wavefront weighs its own partial result, merged with the running (o, lse), then one
+    // Combine the wavefronts' parts: each weighs its own partial result, merged with the running (o, lse), then one
     // row-contiguous pass adds them up.
     // The running values are asked for first (rows past the end read the last one).
     wait_transfers<0>();                                   // (a first block that no row sees)
+    float *const o_out = [&]() { if constexpr (WIN) return a.out_o(split); else return a.o; }(), *const lse_out = [&]() { if constexpr (WIN) return a.out_lse(split); else return a.lse; }();
     f32x4 o_old[C::OUT_VECS];
     float lse_old[2] = {-INFINITY, -INFINITY};
-    if (a.accumulate) {
+    if (merges) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) lse_old[r] = a.lse[(long long)h * g.lq + (row0 + 32 * r + l32 < g.lq ? row0 + 32 * r + l32 : g.lq - 1)];
+        for (int r = 0; r < 2; ++r) lse_old[r] = lse_out[(long long)h * g.lq + (row0 + 32 * r + l32 < g.lq ? row0 + 32 * r + l32 : g.lq - 1)];
 #pragma unroll
         for (int j = 0; j < C::OUT_VECS; ++j) {
             const int i = tid + 64 * NW * j, r = row0 + i / (D / 4), c = 4 * (i % (D / 4));
-            o_old[j] = *reinterpret_cast<const f32x4*>(a.o + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
+            o_old[j] = *reinterpret_cast<const f32x4*>(o_out + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
         }
     } else {
 #pragma unroll
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
     }
     if constexpr (WIN) {
         if (__syncthreads_or(not_finite<C::NDB>(oacc) != 0.f)) {
-            win_plain::fwd_unit<uint16_t, D>(a, h, row0, ROWS);
+            win_plain::fwd_unit<uint16_t, D>(a, h, row0, ROWS, win_plain::keys_of_blocks(vis.span, b_first, n_blocks), split);
             return;
         }
     } else
@@ -406,7 +411,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
             lse_new = (m + __log2f(l)) * LN2;
         }
         float wb = inv;
-        if (a.accumulate) {
+        if (merges) {
             const float mm = fmaxf(lse_old[r], lse_new);
             if (mm != -INFINITY) {
                 const float ea = __expf(lse_old[r] - mm), eb = __expf(lse_new - mm);
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
         }
         if (sp == 0 && hh == 0) {
             sm.e.wa[32 * r + l32] = wa;
-            if (row0 + 32 * r + l32 < g.lq) a.lse[(long long)h * g.lq + row0 + 32 * r + l32] = lse_new;
+            if (row0 + 32 * r + l32 < g.lq) lse_out[(long long)h * g.lq + row0 + 32 * r + l32] = lse_new;
         }
         const float w = wb * fast_exp2(m_run[r] - m);
         float* stage = &sm.e.stage[(sp * ROWS + 32 * r) * C::PITCH];
@@ -443,8 +448,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
         const int i = tid + 64 * NW * j, r = i / (D / 4), c = 4 * (i % (D / 4));
         if (row0 + r >= g.lq) continue;
         const long long at = ((long long)(row0 + r) * g.nq + h) * D + c;
-        if constexpr (WIN) win_plain::store4(a.o, at, a.out_bf16, out[j][0], out[j][1], out[j][2], out[j][3]);
-        else *reinterpret_cast<f32x4*>(a.o + at) = out[j];
+        if constexpr (WIN) win_plain::store4(o_out, at, a.rounds(), out[j][0], out[j][1], out[j][2], out[j][3]);
+        else *reinterpret_cast<f32x4*>(o_out + at) = out[j];
     }
 }
 
@@ -1138,7 +1143,7 @@ hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s)
 {
     QuadRest rest;
     rest.tiles = (a.g.lq + ROWS - 1) / ROWS;
-    const unsigned grid = (unsigned)a.g.nq * (unsigned)rest.tiles;
+    const dim3 grid((unsigned)a.g.nq * (unsigned)rest.tiles, (unsigned)a.n_splits);
     if (a.g.d == 128) fwd_quad_bf16_kernel<128, true><<<grid, 256, 0, s>>>(a, rest);
     else fwd_quad_bf16_kernel<64, true><<<grid, 256, 0, s>>>(a, rest);
     return hipGetLastError();

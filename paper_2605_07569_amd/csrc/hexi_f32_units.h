@@ -272,7 +272,7 @@ template <class C> struct FwdSmem {
     int kpos[2][C::TK];
 };
 
-template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(const FwdArgsOf<WIN>& a, const int h, const int q_tile, FwdSmem<C>& sm)
+template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(const FwdArgsOf<WIN>& a, const int h, const int q_tile, FwdSmem<C>& sm, const int key_split = 0)
 {
     constexpr int D = C::D, NW = C::NW, S = C::S, TK = C::TK, NBLK = C::NBLK;
     constexpr bool SPLIT = C::SPLIT, TWO = C::TWO;
@@ -298,10 +298,13 @@ template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(co
     }();
     const int n_vis = WIN ? span.n_blocks : seg_rows_le(g.ks, seg_pos_of_row(g.qs, last_row));      // visible columns form the prefix [0, n_vis)
     const int n_full = WIN ? 0 : seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TK;    // tiles no row needs a mask for
-    if (n_vis == 0 && a.accumulate) return;               // merging an empty partial is the identity
-    const int n_tiles = WIN ? (span.n_blocks - (SPLIT ? wave : 0) + WT::STEP - 1) / WT::STEP
+    const bool merges = [&]() { if constexpr (WIN) return a.merges(); else return a.accumulate != 0; }();
+    if (n_vis == 0 && merges) return;                     // merging an empty partial is the identity
+    const int b_first = [&]() { if constexpr (WIN) return span.split_start(key_split, a.n_splits); else return 0; }();
+    const int b_end = [&]() { if constexpr (WIN) return span.split_start(key_split + 1, a.n_splits); else return 0; }();
+    const int n_tiles = WIN ? (b_end - b_first - (SPLIT ? wave : 0) + WT::STEP - 1) / WT::STEP
                             : (n_vis - (SPLIT ? 16 * wave : 0) + TK - 1) / TK;      // of this wavefront: those that hold a visible row
-    auto block = [&](int t) { return span.block(SPLIT ? wave + WT::STEP * t : t); };    // (WIN: of the chunk)
+    auto block = [&](int t) { return span.block(b_first + (SPLIT ? wave + WT::STEP * t : t)); };    // (WIN: of the chunk)
     auto first_row = [&](int t) { return WIN ? WT::B * block(t) - (SPLIT ? 16 * wave : 0) : t * TK; };
     auto masked = [&](int t) { return WIN ? !span.full(block(t)) : t >= n_full; };
 
@@ -392,8 +395,9 @@ template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(co
 
     // Combine the splits and merge with the running (o, lse): weights per (row, split), then a row-contiguous pass.
     l_run = sum_over_groups(l_run);
+    float *const o_out = [&]() { if constexpr (WIN) return a.out_o(key_split); else return a.o; }(), *const lse_out = [&]() { if constexpr (WIN) return a.out_lse(key_split); else return a.lse; }();
     if constexpr (WIN) {
-        if (__syncthreads_or(not_finite(acc) != 0.f)) { win_plain::fwd_unit<float, D>(a, h, row0, C::ROWS); return; }
+        if (__syncthreads_or(not_finite(acc) != 0.f)) { win_plain::fwd_unit<float, D>(a, h, row0, C::ROWS, win_plain::keys_of_blocks(span, b_first, b_end), key_split); return; }
     } else
     __syncthreads();              // the tiles are free
     stage_rows<C>(&sm.e.stage[wave * 16 * C::PITCH], acc, grp, l16, 1.0f);
@@ -415,8 +419,8 @@ template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(co
         float wb = l > 0.f ? 1.0f / l : 0.f, wa = 0.f, lse_new = lse_part;
         const int row = row0 + tid;
         if (row < g.lq) {
-            float* lp = a.lse + (long long)h * g.lq + row;
-            if (a.accumulate) {
+            float* lp = lse_out + (long long)h * g.lq + row;
+            if (merges) {
                 const float la_old = *lp;
                 const float mm = fmaxf(la_old, lse_part);
                 if (mm == -INFINITY) { wb = 0.f; lse_new = -INFINITY; }
@@ -441,9 +445,9 @@ template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(co
 #pragma unroll
         for (int s = 0; s < S; ++s) x += sm.e.w[s * C::ROWS + r] * *reinterpret_cast<const f32x4*>(&sm.e.stage[(s * C::ROWS + r) * C::PITCH + c]);
         const long long at = ((long long)(row0 + r) * g.nq + h) * D + c;
-        f32x4* op = reinterpret_cast<f32x4*>(a.o + at);
-        if (a.accumulate) x += sm.e.wa[r] * *op;
-        if constexpr (WIN) win_plain::store4(a.o, at, a.out_bf16, x[0], x[1], x[2], x[3]);
+        f32x4* op = reinterpret_cast<f32x4*>(o_out + at);
+        if (merges) x += sm.e.wa[r] * *op;
+        if constexpr (WIN) win_plain::store4(o_out, at, a.rounds(), x[0], x[1], x[2], x[3]);
         else *op = x;
     }
 }

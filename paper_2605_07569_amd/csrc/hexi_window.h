@@ -9,6 +9,15 @@
 struct WinFwdArgs : FwdArgs {
     int window, n_sink;     // both clamped to 2^31 - 1
     int out_bf16;           // o is bf16, overwritten
+    // Splits of a unit's run of blocks, one workgroup each; with more than one their normalised results go to part_o [splits][lq][nq][d] and part_lse
+    // [splits][nq][lq], and a second launch joins them.
+    int n_splits;
+    float *part_o, *part_lse;
+    // where a split writes
+    __device__ float* out_o(int split) const { return n_splits > 1 ? part_o + (long long)split * g.lq * g.nq * g.d : o; }
+    __device__ float* out_lse(int split) const { return n_splits > 1 ? part_lse + (long long)split * g.nq * g.lq : lse; }
+    __device__ bool merges() const { return n_splits == 1 && accumulate; }
+    __device__ bool rounds() const { return n_splits == 1 && out_bf16; }
 };
 struct WinBwdArgs : BwdArgs {
     int window, n_sink;
@@ -54,6 +63,8 @@ template <int B> struct WinSpan {
         full_hi = first.hi;
     }
     __host__ __device__ int block(int i) const { return i < n_sink_blocks ? i : i + skip; }
+    // blocks [i0, i1) of the run of a split
+    __host__ __device__ int split_start(int split, int n_splits) const { return (int)((long long)n_blocks * split / n_splits); }
     // whether every row sees all of the chunk's block b
     __host__ __device__ bool full(int b) const { return (B * b >= full_lo && B * b + B <= full_hi) || B * b + B <= full_sink; }
 };
@@ -81,6 +92,27 @@ struct WinRowSpan {
         full_end = last_is_sink ? lq : first_is_sink ? 0 : w0.end;
     }
 };
+
+// Splits of the units of a forward call with few rows: as many as fill the chip with workgroups, each left with a block for every wavefront at least, if
+// that takes at least eight steps off a unit (a step is 0.8 us, joining the results 5).  One row of 8 heads, window 4096: 34.5 us in one piece, XX in 32.
+inline int hexi_win_fwd_splits(int dtype, int nq, long long lq, long long lc, long long window, long long n_sink)
+{
+    const bool bf16 = dtype == HEXI_BF16;
+    const long long rows = bf16 ? 64 : 16, block = bf16 ? 32 : 16, waves = bf16 ? 4 : 8;
+    const long long units = (lq + rows - 1) / rows * nq;
+    if (units > 128) return 1;
+    long long keys = window < lc ? window + (lq < rows ? lq : rows) : lc;
+    keys += n_sink < lc ? n_sink : lc;
+    if (keys > lc) keys = lc;
+    const long long steps = (keys + block * waves - 1) / (block * waves);
+    long long n = 256 / units;
+    if (n > steps) n = steps;
+    return n > 1 && steps - (steps + n - 1) / n >= 8 ? (int)n : 1;
+}
+inline size_t hexi_win_fwd_workspace(int n_splits, int nq, long long lq, int d)
+{
+    return n_splits > 1 ? (size_t)n_splits * (size_t)lq * (size_t)nq * (size_t)(d + 1) * sizeof(float) : 0;
+}
 
 // One run of q heads to every kv head, in head order; empty for a kv head that no q head reads.
 inline void hexi_head_run_of_each_kv(const signed char* kv_of_q, int nq, int nkv, HeadRuns* runs)

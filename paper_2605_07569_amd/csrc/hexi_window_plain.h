@@ -48,8 +48,8 @@ template <int N> __device__ __forceinline__ float dot(const float (&a)[N], const
     return x;
 }
 
-// o and lse of rows [row0, row0 + rows) of head h.
-template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdArgs& a, const int h, const int row0, const int rows)
+// o and lse of rows [row0, row0 + rows) of head h from the keys in [keys.x, keys.y) and [keys.z, keys.w), those of a split of the unit's run of blocks.
+template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdArgs& a, const int h, const int row0, const int rows, const int4 keys, const int split)
 {
     constexpr int N = D / LANES;
     const AttnGeom& g = a.g;
@@ -63,8 +63,9 @@ template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdA
 #pragma unroll
         for (int i = 0; i < N; ++i) acc[i] = 0.f;
         float m = -INFINITY, l = 0.f;
-        for (int part = 0; part < 2; ++part)
-            for (int j = part ? w.lo : 0, end = part ? w.hi : w.sink; j < end; ++j) {
+        for (int part = 0; part < 4; ++part) {
+            const int p0 = part & 2 ? keys.z : keys.x, p1 = part & 2 ? keys.w : keys.y, k0 = part & 1 ? w.lo : 0, k1 = part & 1 ? w.hi : w.sink;
+            for (int j = k0 > p0 ? k0 : p0, end = k1 < p1 ? k1 : p1; j < end; ++j) {
                 float x[N];
                 load_cols(k + (long long)j * g.kv_stride_tok, x);
                 const float s = dot(q, x) * g.scale;
@@ -82,10 +83,12 @@ template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdA
 #pragma unroll
                 for (int i = 0; i < N; ++i) acc[i] = fmaf(p, x[i], acc[i]);
             }
+        }
         float lse = l == 0.f ? -INFINITY : m + logf(l);
         float wa = 0.f, wb = l == 0.f ? 0.f : 1.0f / l;
-        float* lp = a.lse + (long long)h * g.lq + row;
-        if (a.accumulate) {
+        float* lp = a.out_lse(split) + (long long)h * g.lq + row;
+        float* out = a.out_o(split);
+        if (a.merges()) {
             const float old = *lp, mm = fmaxf(old, lse);
             if (mm != -INFINITY) {
                 const float ea = expf(old - mm), eb = expf(lse - mm), r = 1.0f / (ea + eb);
@@ -100,10 +103,17 @@ template <class T, int D> __device__ __forceinline__ void fwd_unit(const WinFwdA
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
             float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (a.accumulate) old = *reinterpret_cast<const float4*>(a.o + at + i);
-            store4(a.o, at + i, a.out_bf16, wa * old.x + wb * acc[i], wa * old.y + wb * acc[i + 1], wa * old.z + wb * acc[i + 2], wa * old.w + wb * acc[i + 3]);
+            if (a.merges()) old = *reinterpret_cast<const float4*>(out + at + i);
+            store4(out, at + i, a.rounds(), wa * old.x + wb * acc[i], wa * old.y + wb * acc[i + 1], wa * old.z + wb * acc[i + 2], wa * old.w + wb * acc[i + 3]);
         }
     }
+}
+
+// The keys of blocks [i0, i1) of a unit's run, as fwd_unit takes them.
+template <int B> __device__ __forceinline__ int4 keys_of_blocks(const WinSpan<B>& span, int i0, int i1)
+{
+    const int s = span.n_sink_blocks, first = i0 > s ? i0 : s;
+    return make_int4(B * i0, B * (i1 < s ? i1 : s), B * (first + span.skip), i1 > first ? B * (i1 + span.skip) : 0);
 }
 
 // dq of rows [row0, row0 + rows) of head h.

@@ -105,7 +105,22 @@ def _rel_of(pair, rel):
 def test_accumulation_over_chunks_is_the_whole(dtype, d):
     """Keys in three uneven chunks, forward and backward, against one call over all of them."""
     c = Case("chunks", [(150, 180), (700, 90)], [(0, 790)], 140, 9, nq=4, nkv=2)
-    parts = [[(0, 100)], [(100, 333)], [(433, 7), (440, 350)]]
+    _chunks(c, [[(0, 100)], [(100, 333)], [(433, 7), (440, 350)]], dtype, d)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_accumulation_of_split_units(dtype, d):
+    """Few rows, long chunks: the units' runs of keys are split over workgroups, and joined with what is there."""
+    c = Case("split chunks", [(6000, 3)], [(0, 6003)], 5500, 40, nq=3, nkv=1)
+    parts = [[(0, 3100)], [(3100, 2903)]]
+    window = hexi.make_window(c.window, c.n_sink)
+    for part in parts:
+        q, k = torch.empty(c.lq, c.nq, d, dtype=dtype), torch.empty(sum(n for _, n in part), c.nkv, d, dtype=dtype)
+        assert hexi.hexi_attn_win_workspace_bytes(hexi.desc_for(q, k, 1.0), window, c.lq, k.shape[0]) > 0
+    _chunks(c, parts, dtype, d)
+
+
+def _chunks(c, parts, dtype, d):
     x, dev, desc, window = setup(c, dtype, d, 2)
     z = lambda *s: torch.zeros(s, device=DEV)
     o, lse = z(c.lq, c.nq, d), torch.full((c.nq, c.lq), float("-inf"), device=DEV)
@@ -153,7 +168,9 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, d, bad):
     """One bad value of v in a key: rows that see the key have it in that column, no other row or column is touched; one bad key: the rows that see it are
     NaN or as without it (a score of -inf), no other is touched.  Backward: the same for dq, and dk and dv of bad rows of q and dO."""
     c = Case("bad", [(100, 190)], [(0, 5), (61, 229)], 40, 5, nq=2, nkv=1)
-    for where, key, col in (("v", 3, 7), ("v", 90, 50), ("v", 233, 0), ("k", 2, 9), ("k", 120, 33), ("k", 233, 63)):
+    split = Case("bad, split", [(3000, 65)], [(0, 5), (500, 2565)], 2400, 5, nq=2, nkv=1)
+    for c, where, key, col in ((c, "v", 3, 7), (c, "v", 90, 50), (c, "v", 233, 0), (c, "k", 2, 9), (c, "k", 120, 33), (c, "k", 233, 63),
+                               (split, "v", 1, 3), (split, "v", 140, 9), (split, "v", 2540, 63), (split, "k", 150, 4), (split, "k", 2569, 5)):
         print(f"\n  {where}[{key}, {col}] = {bad}", flush=True)
         x = wu.inputs(c, dtype, d, 4)
         clean = {n: t.clone() for n, t in x.items()}
@@ -161,7 +178,7 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, d, bad):
         dev = {n: t.to(DEV) for n, t in x.items()}
         desc, window = hexi.desc_for(dev["q"], dev["k"], d ** -0.5), hexi.make_window(c.window, c.n_sink)
         o, lse = torch.empty(c.lq, c.nq, d, device=DEV), torch.empty(c.nq, c.lq, device=DEV)
-        hexi.hexi_attn_win_fwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], o, lse)
+        hexi.hexi_attn_win_fwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], o, lse, workspace=workspace(desc, window, c))
         sees = wu.visible(c)[:, key]
         ro, rl, bo, bl = wu.forward(c, clean, F32)
         if where == "v":
@@ -170,13 +187,13 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, d, bad):
             wu.within("o", o, ro, bo)
         else:
             o, lse = o.cpu().double(), lse.cpu().double()
-            hit = sees if bad != bad else sees & torch.stack([clean["q"][:, h, col].float() * bad > 0 for h in range(c.nq)]).any(0)
             wu.within("o of the others", o[~sees], ro[~sees], bo[~sees])
             wu.within("lse of the others", lse[:, ~sees], rl[:, ~sees], bl[:, ~sees])
             for h in range(c.nq):
                 hit = sees if bad != bad else sees & (clean["q"][:, h, col].float() * bad > 0)
                 assert o[hit, h].isnan().all() and lse[h, hit].isnan().all()
                 assert torch.isfinite(o[sees & ~hit, h]).all()
+    c = Case("bad", [(100, 190)], [(0, 5), (61, 229)], 40, 5, nq=2, nkv=1)
     ro, rl, _, _ = wu.forward(c, wu.inputs(c, dtype, d, 4), F32)
     for where, at, col in (("v", 90, 50), ("k", 120, 33), ("k", 2, 3), ("q", 77, 5), ("d_o", 130, 11), ("d_o", 0, 1)):
         print(f"\n  backward {where}[{at}, {col}] = {bad}", flush=True)
@@ -184,6 +201,7 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, d, bad):
         ref = wu.backward(c, x, ro.float(), rl.float(), F32)
         x[where][at, 0, col] = bad
         dev = {n: t.to(DEV) for n, t in x.items()}
+        desc, window = hexi.desc_for(dev["q"], dev["k"], d ** -0.5), hexi.make_window(c.window, c.n_sink)
         delta = (ro * wu.inputs(c, dtype, d, 4)["d_o"].double()).sum(2).T.float().contiguous().to(DEV)
         dq, dk, dv = torch.zeros(c.lq, c.nq, d, device=DEV), torch.empty(c.lc, 1, d, device=DEV), torch.empty(c.lc, 1, d, device=DEV)
         hexi.hexi_attn_win_bwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], None, dev["d_o"], rl.float().to(DEV), delta, dq, dk, dv)
