@@ -262,17 +262,16 @@ static int build_window(const hexi_window* w, int* window, int* n_sink)
     return HEXI_OK;
 }
 
-// Splits of a forward call: by the descriptor, the window and the lengths alone, so that the workspace can be asked for without the ranges.
-static int win_fwd_splits(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
+static WinFwdPlan win_fwd_plan(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
 {
-    if (!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || (d->head_dim != 64 && d->head_dim != 128) ||
-        w->window < 1 || w->n_sink < 0) return 1;
-    return hexi_win_fwd_splits(d->dtype, d->n_q_heads, lq, lc, w->window, w->n_sink);
+    if (!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || d->n_kv_heads < 1 ||
+        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || w->window < 1 || w->n_sink < 0) return {0, 1};
+    return hexi_win_fwd_plan(d->dtype, d->n_q_heads, d->n_kv_heads, lq, lc, w->window, w->n_sink);
 }
 
 HEXI_EXPORT size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc)
 {
-    const int n = win_fwd_splits(desc, window, lq, lc);
+    const int n = win_fwd_plan(desc, window, lq, lc).n_splits;
     return n > 1 ? hexi_win_fwd_workspace(n, desc->n_q_heads, lq, desc->head_dim) : 0;
 }
 
@@ -294,7 +293,9 @@ HEXI_EXPORT int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_w
     a.q = q; a.k = k; a.v = v; a.o = (float*)o; a.lse = lse;
     a.accumulate = (flags & HEXI_ACCUMULATE) ? 1 : 0;
     a.out_bf16 = o_dtype == HEXI_BF16;
-    a.n_splits = win_fwd_splits(desc, window, a.g.lq, a.g.lc);
+    const WinFwdPlan plan = win_fwd_plan(desc, window, a.g.lq, a.g.lc);
+    a.few = plan.few;
+    a.n_splits = plan.n_splits;
     a.part_o = a.part_lse = nullptr;
     if (a.n_splits > 1) {
         const size_t need = hexi_win_fwd_workspace(a.n_splits, a.g.nq, a.g.lq, a.g.d);

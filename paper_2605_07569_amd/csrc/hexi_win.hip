@@ -46,41 +46,9 @@ template <class F> hipError_t with_cfg(int d, bool split, F f)
 #include <cstdlib>
 static int env_shape(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 1; }
 
-// The splits' normalised results joined, as hexi_attn_merge_lse joins two: one thread to four columns of a (row, head).
-__global__ void __launch_bounds__(64) win_join_kernel(const WinFwdArgs a)
-{
-    const AttnGeom& g = a.g;
-    const int d4 = g.d / 4, i = (int)(blockIdx.x * 64 + threadIdx.x), rh = i / d4, c = 4 * (i - rh * d4);
-    if (rh >= g.lq * g.nq) return;
-    const int row = rh / g.nq, h = rh - row * g.nq;
-    const long long li = (long long)h * g.lq + row, at = (long long)rh * g.d + c, lse_part = (long long)g.nq * g.lq, o_part = lse_part * g.d;
-    const float old = a.accumulate ? a.lse[li] : -INFINITY;
-    float m = old;
-    for (int s = 0; s < a.n_splits; ++s) m = fmaxf(m, a.part_lse[s * lse_part + li]);
-    float total = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    if (m != -INFINITY) {
-        if (a.accumulate) {
-            total = expf(old - m);
-            o = total * *reinterpret_cast<const f32x4*>(a.o + at);
-        }
-#pragma unroll 8
-        for (int s = 0; s < a.n_splits; ++s) {
-            const float w = expf(a.part_lse[s * lse_part + li] - m);
-            total += w;
-            o += w * *reinterpret_cast<const f32x4*>(a.part_o + s * o_part + at);
-        }
-        o *= 1.0f / total;
-        m += logf(total);
-    }
-    // (the threads of a (row, head) are one wavefront's: all have read the old value)
-    __builtin_amdgcn_wave_barrier();
-    if (c == 0) a.lse[li] = m;
-    win_plain::store4(a.o, at, a.out_bf16, o[0], o[1], o[2], o[3]);
-}
-
 static hipError_t launch_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
+    if (a.few) return hexi_launch_win_few(a, dtype, s);
     if (dtype == HEXI_BF16) return hexi_launch_win_fwd_quad_bf16(a, s);
     return with_cfg(a.g.d, env_shape("WFS"), [&](auto cfg) {
         using C = decltype(cfg);
@@ -92,10 +60,7 @@ static hipError_t launch_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
     const hipError_t e = launch_fwd(a, dtype, s);
-    if (e != hipSuccess || a.n_splits == 1) return e;
-    const unsigned n = (unsigned)((long long)a.g.lq * a.g.nq * (a.g.d / 4));      // (few rows: units <= 128)
-    win_join_kernel<<<(n + 63) / 64, 64, 0, s>>>(a);
-    return hipGetLastError();
+    return e != hipSuccess || a.n_splits == 1 ? e : hexi_launch_win_join(a, s);
 }
 
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s)

@@ -11,6 +11,7 @@ struct WinFwdArgs : FwdArgs {
     int out_bf16;           // o is bf16, overwritten
     // Splits of a unit's run of blocks, one workgroup each; with more than one their normalised results go to part_o [splits][lq][nq][d] and part_lse
     // [splits][nq][lq], and a second launch joins them.
+    int few;                // the units are those of few rows
     int n_splits;
     float *part_o, *part_lse;
     // where a split writes
@@ -51,6 +52,7 @@ template <int B> struct WinSpan {
     int n_blocks;
     int n_whole;                      // blocks of the run before one that the chunk's end cuts
     int full_sink, full_lo, full_hi;  // keys that every row sees: [0, full_sink) and [full_lo, full_hi)
+    WinSpan() = default;
     __host__ __device__ WinSpan(const WinKeys& first, const WinKeys& last, int lc)
     {
         const int b0 = first.lo / B, b1 = (last.hi + B - 1) / B, s = (last.sink + B - 1) / B;
@@ -64,7 +66,12 @@ template <int B> struct WinSpan {
     }
     __host__ __device__ int block(int i) const { return i < n_sink_blocks ? i : i + skip; }
     // blocks [i0, i1) of the run of a split
-    __host__ __device__ int split_start(int split, int n_splits) const { return (int)((long long)n_blocks * split / n_splits); }
+    __host__ __device__ int split_start(int split, int n_splits) const
+    {
+        if (n_splits == 1) return split * n_blocks;
+        const int each = n_blocks / n_splits, rest = n_blocks - each * n_splits;
+        return split * each + (split < rest ? split : rest);
+    }
     // whether every row sees all of the chunk's block b
     __host__ __device__ bool full(int b) const { return (B * b >= full_lo && B * b + B <= full_hi) || B * b + B <= full_sink; }
 };
@@ -93,21 +100,40 @@ struct WinRowSpan {
     }
 };
 
-// Splits of the units of a forward call with few rows: as many as fill the chip with workgroups, each left with a block for every wavefront at least, if
-// that takes at least eight steps off a unit (a step is 0.8 us, joining the results 5).  One row of 8 heads, window 4096: 34.5 us in one piece, XX in 32.
-inline int hexi_win_fwd_splits(int dtype, int nq, long long lq, long long lc, long long window, long long n_sink)
+#define HEXI_WIN_MAX_SPLITS 256
+#define HEXI_WIN_FEW_VECTORS 512
+#define HEXI_WIN_FEW_ROWS 8
+#define HEXI_WIN_FEW_GROUPS 160      // of 16 vectors: 32 whole ones, and one that is not whole for each of 128 heads
+
+// How a forward call is cut, by the descriptor, the window and the lengths alone, so that its workspace can be asked for without the ranges.
+struct WinFwdPlan { int few, n_splits; };
+// Few rows: XX.  Otherwise the units are split as far as fills the chip with workgroups, each left with a block for every wavefront at least, if that takes at
+// least eight steps off a unit (a step is 0.8 us, joining the results 5).
+inline WinFwdPlan hexi_win_fwd_plan(int dtype, int nq, int nkv, long long lq, long long lc, long long window, long long n_sink)
 {
+    auto keys_of = [&](long long rows) {
+        long long keys = window < lc ? window + (lq < rows ? lq : rows) : lc;
+        keys += n_sink < lc ? n_sink : lc;
+        return keys < lc ? keys : lc;
+    };
+    WinFwdPlan plan = {0, 1};
+    if (lq <= HEXI_WIN_FEW_ROWS && lq * nq <= HEXI_WIN_FEW_VECTORS && lq * nq <= 32 * nkv) {
+        const long long groups = nkv * ((lq * nq + 16 * nkv - 1) / (16 * nkv)), blocks = (keys_of(lq) + 63) / 64;
+        long long n = 512 / groups;
+        n = n < blocks ? n : blocks;
+        plan.few = 1;
+        plan.n_splits = n < 1 ? 1 : n < HEXI_WIN_MAX_SPLITS ? (int)n : HEXI_WIN_MAX_SPLITS;
+        return plan;
+    }
     const bool bf16 = dtype == HEXI_BF16;
     const long long rows = bf16 ? 64 : 16, block = bf16 ? 32 : 16, waves = bf16 ? 4 : 8;
     const long long units = (lq + rows - 1) / rows * nq;
-    if (units > 128) return 1;
-    long long keys = window < lc ? window + (lq < rows ? lq : rows) : lc;
-    keys += n_sink < lc ? n_sink : lc;
-    if (keys > lc) keys = lc;
-    const long long steps = (keys + block * waves - 1) / (block * waves);
+    if (units > 128) return plan;
+    const long long steps = (keys_of(rows) + block * waves - 1) / (block * waves);
     long long n = 256 / units;
-    if (n > steps) n = steps;
-    return n > 1 && steps - (steps + n - 1) / n >= 8 ? (int)n : 1;
+    n = n < steps ? n : steps;
+    if (n > 1 && steps - (steps + n - 1) / n >= 8) plan.n_splits = (int)n;
+    return plan;
 }
 inline size_t hexi_win_fwd_workspace(int n_splits, int nq, long long lq, int d)
 {
@@ -133,6 +159,8 @@ inline void hexi_head_run_of_each_kv(const signed char* kv_of_q, int nq, int nkv
 // Launchers.
 hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s);
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s);
+hipError_t hexi_launch_win_few(const WinFwdArgs& a, int dtype, hipStream_t s);      // in hexi_win_few.hip
+hipError_t hexi_launch_win_join(const WinFwdArgs& a, hipStream_t s);
 hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_quad.hip
 hipError_t hexi_launch_win_bwd_quad_bf16(const WinBwdArgs& a, hipStream_t s);
 // Delta = rowsum(dO o) of a bf16 o

@@ -146,17 +146,16 @@ def make_range(segs: Sequence[Tuple[int, int]]):
     arr = (hexi_seg * max(1, len(segs)))(*[(int(s), int(n)) for s, n in segs])
     r = hexi_range(len(segs), arr)
     r._keep = arr
-    r._rows = sum(int(n) for _, n in segs)
     return r, arr
 
 
 def _with_rows(segs):
     """A range and its rows (whatever is wrong with a range the library says)."""
     r = segs if isinstance(segs, hexi_range) else make_range(segs)[0]
-    rows = getattr(r, "_rows", None)
-    if rows is None:
-        rows = sum(r.segs[i].len for i in range(max(0, min(r.n_segs, HEXI_MAX_SEGS))))
-    return r, rows
+    n = r.n_segs
+    if n == 1:
+        return r, r.segs[0].len
+    return r, sum(r.segs[i].len for i in range(max(0, min(n, HEXI_MAX_SEGS))))
 
 
 def make_desc(dtype, head_dim, n_q_heads, n_kv_heads, softmax_scale, q_strides, kv_strides, kv_of_q=None):
@@ -270,12 +269,20 @@ def _refuse(msg):
 
 
 _DTYPES = {}
+_torch = None
+
+
+def _types():
+    """torch, and its element types by the library's codes and the other way round, at the first use."""
+    global _torch
+    import torch
+    _DTYPES.update({torch.bfloat16: HEXI_BF16, torch.float32: HEXI_F32, HEXI_BF16: torch.bfloat16, HEXI_F32: torch.float32})
+    _torch = torch
 
 
 def _dtype(t):
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.bfloat16: HEXI_BF16, torch.float32: HEXI_F32})
+    if _torch is None:
+        _types()
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise HexiError(HEXI_EUNSUPPORTED, f"element type {t.dtype} (bf16 or fp32)")
@@ -284,34 +291,39 @@ def _dtype(t):
 
 def _current_device():
     """Index of the GPU whose stream the calls use; no tensor is on -2, where none is initialised."""
-    import torch
-    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+    if _torch is None:
+        _types()
+    return _torch._C._cuda_getDevice() if _torch.cuda.is_initialized() else -2
 
 
 def _fits(name, t, shape, dtype, dev, strides=None):
     """Refuses a tensor that is not of this shape and element type (a code of the library), on the current GPU, dense or with these strides."""
+    if t.shape == shape and t.dtype is _DTYPES.get(dtype) and t.get_device() == dev and (t.is_contiguous() if strides is None else t.stride() == strides):
+        return
     if tuple(t.shape) != shape or _dtype(t) != dtype:
         _refuse(f"{name}: {shape} elements of type {dtype} are needed, not {tuple(t.shape)} {t.dtype}")
-    if not t.is_contiguous() if strides is None else t.stride() != strides and any(s != w and n > 1 for s, w, n in zip(t.stride(), strides, shape)):
+    if not t.is_contiguous() if strides is None else any(s != w and n > 1 for s, w, n in zip(t.stride(), strides, shape)):
         _refuse(f"{name}: strides {t.stride()}; {'a contiguous tensor is needed' if strides is None else f'the descriptor says {strides}'}")
     if t.get_device() != dev:
         _refuse(f"{name} is on {t.device}, not on the current GPU")
 
 
 def _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o=None):
-    """Ranges, rows, keys and device of a windowed call, its inputs checked."""
+    """Ranges, rows, keys, device and sizes (head_dim, q heads, kv heads) of a windowed call, its inputs checked."""
     qr, lq = _with_rows(q_segs)
     kr, lc = _with_rows(kv_segs)
-    dev, dt, d = _current_device(), desc.dtype, desc.head_dim
-    shape, strides = (lq, desc.n_q_heads, d), (desc.q_stride_tok, desc.q_stride_head, 1)
-    _fits("q", q, shape, dt, dev, strides)
+    dev = _current_device()
+    dt, d, nq, nkv = desc.dtype, desc.head_dim, desc.n_q_heads, desc.n_kv_heads
+    q_strides, kv_strides = (desc.q_stride_tok, desc.q_stride_head, 1), (desc.kv_stride_tok, desc.kv_stride_head, 1)
+    shape = (lq, nq, d)
+    _fits("q", q, shape, dt, dev, q_strides)
     if d_o is not None:
-        _fits("d_o", d_o, shape, dt, dev, strides)
-    shape, strides = (lc, desc.n_kv_heads, d), (desc.kv_stride_tok, desc.kv_stride_head, 1)
-    _fits("k", k, shape, dt, dev, strides)
-    _fits("v", v, shape, dt, dev, strides)
-    _fits("lse", lse, (desc.n_q_heads, lq), HEXI_F32, dev)
-    return qr, kr, lq, lc, dev
+        _fits("d_o", d_o, shape, dt, dev, q_strides)
+    shape = (lc, nkv, d)
+    _fits("k", k, shape, dt, dev, kv_strides)
+    _fits("v", v, shape, dt, dev, kv_strides)
+    _fits("lse", lse, (nq, lq), HEXI_F32, dev)
+    return qr, kr, lq, lc, dev, d, nq, nkv
 
 
 def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
@@ -320,9 +332,9 @@ def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
 
 def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flags=0, workspace=None, stream=None):
     """Windowed forward; o's element type (fp32 or bf16) is the result's."""
-    qr, kr, lq, lc, dev = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse)
+    qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse)
     o_type = _dtype(o)
-    _fits("o", o, (lq, desc.n_q_heads, desc.head_dim), o_type, dev)
+    _fits("o", o, (lq, nq, d), o_type, dev)
     ws_bytes = 0
     if workspace is not None:
         if workspace.get_device() != dev:
@@ -336,8 +348,7 @@ def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flag
 
 def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq, dk, dv, flags=0, stream=None):
     """Windowed backward; the element type of dq, dk and dv (one for all; None for the half that is skipped) is the gradients'."""
-    qr, kr, lq, lc, dev = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o)
-    nq, nkv, d = desc.n_q_heads, desc.n_kv_heads, desc.head_dim
+    qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o)
     _fits("delta", delta, (nq, lq), HEXI_F32, dev)
     o_type = grad = HEXI_F32
     if o is not None:

@@ -111,8 +111,11 @@ def test_accumulation_over_chunks_is_the_whole(dtype, d):
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
 def test_accumulation_of_split_units(dtype, d):
     """Few rows, long chunks: the units' runs of keys are split over workgroups, and joined with what is there."""
-    c = Case("split chunks", [(6000, 3)], [(0, 6003)], 5500, 40, nq=3, nkv=1)
-    parts = [[(0, 3100)], [(3100, 2903)]]
+    for rows in (3, 70):
+        _split_chunks(Case("split chunks", [(6000, rows)], [(0, 6000 + rows)], 5500, 40, nq=3, nkv=1), [[(0, 3100)], [(3100, 2900 + rows)]], dtype, d)
+
+
+def _split_chunks(c, parts, dtype, d):
     window = hexi.make_window(c.window, c.n_sink)
     for part in parts:
         q, k = torch.empty(c.lq, c.nq, d, dtype=dtype), torch.empty(sum(n for _, n in part), c.nkv, d, dtype=dtype)
@@ -168,9 +171,10 @@ def test_what_is_not_finite_stays_with_the_rows_that_see_it(dtype, d, bad):
     """One bad value of v in a key: rows that see the key have it in that column, no other row or column is touched; one bad key: the rows that see it are
     NaN or as without it (a score of -inf), no other is touched.  Backward: the same for dq, and dk and dv of bad rows of q and dO."""
     c = Case("bad", [(100, 190)], [(0, 5), (61, 229)], 40, 5, nq=2, nkv=1)
+    few = Case("bad, few rows", [(3000, 9)], [(0, 5), (500, 2509)], 2400, 5, nq=2, nkv=1)
     split = Case("bad, split", [(3000, 65)], [(0, 5), (500, 2565)], 2400, 5, nq=2, nkv=1)
     for c, where, key, col in ((c, "v", 3, 7), (c, "v", 90, 50), (c, "v", 233, 0), (c, "k", 2, 9), (c, "k", 120, 33), (c, "k", 233, 63),
-                               (split, "v", 1, 3), (split, "v", 140, 9), (split, "v", 2540, 63), (split, "k", 150, 4), (split, "k", 2569, 5)):
+                               (few, "v", 2, 3), (few, "v", 108, 9), (few, "v", 2513, 60), (few, "k", 110, 4), (few, "k", 2513, 5), (split, "v", 1, 3), (split, "v", 140, 9), (split, "v", 2540, 63), (split, "k", 150, 4), (split, "k", 2569, 5)):
         print(f"\n  {where}[{key}, {col}] = {bad}", flush=True)
         x = wu.inputs(c, dtype, d, 4)
         clean = {n: t.clone() for n, t in x.items()}
