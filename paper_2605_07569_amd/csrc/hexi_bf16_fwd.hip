@@ -31,6 +31,7 @@
 #include "hexi_internal.h"
 #include "hexi_shapes.h"
 #include "hexi_mfma.h"
+#include "hexi_window_plain.h"
 
 namespace {
 
@@ -71,8 +72,10 @@ template <int D> struct FwdSmem {
     // 4..7 lie over v[], so every wavefront must be done with the tiles (a workgroup barrier) before any stages.
 };
 
-template <int D>
-__global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const int n_q_tiles, const QShare share, const XcdSplit split)
+// WIN: under a window.  The run of tiles is that of WinSpan, a tile is masked where some row of the group does not see all of it, and as rows come to their first keys
+// at different tiles, masked tiles (and the first that is not) take the online softmax; the others have every row's reference fixed by then.
+template <int D, bool WIN>
+__global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgsOf<WIN> a, const int n_q_tiles, const QShare share, const XcdSplit split)
 {
     using C = FwdCfg<D>;
     constexpr int NKS = C::NKS, NDB = C::NDB, K_ROW_BYTES = C::K_ROW_BYTES, V_ROW_BYTES = C::V_ROW_BYTES;
@@ -117,14 +120,37 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
     // shorter prefix.  n_full_g: tiles this group needs no mask for (the rest are masked by position).
     // NT: tiles the workgroup streams (those of its last rows); n_full_wg: tiles no row needs a mask for.
     int n_full_g = 0;
-    if (grow0 < g.lq) n_full_g = seg_rows_le(g.ks, seg_pos_of_row(g.qs, grow0)) / TN;
+    if (!WIN && grow0 < g.lq) n_full_g = seg_rows_le(g.ks, seg_pos_of_row(g.qs, grow0)) / TN;
     const int wg_last_row = (row0 + WG_ROWS < g.lq ? row0 + WG_ROWS : g.lq) - 1;
-    const int NT = (seg_rows_le(g.ks, seg_pos_of_row(g.qs, wg_last_row)) + TN - 1) / TN;
-    const int n_full_wg = seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TN;
+    // (WIN) the workgroup's run of tiles, what its group's rows see of it, and the run's first tile that all rows of group 0, of group 1, see
+    WinSpan<TN> span, span_g;
+    int first_full[2] = {-1, -1};
+    if constexpr (WIN) {
+        auto keys_of = [&](int row) { return win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink); };
+        auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };      // (the compiler does not see that these are the same in all lanes)
+        span = WinSpan<TN>(keys_of(row0), keys_of(wg_last_row), g.lc);
+        scalar(span.n_sink_blocks); scalar(span.skip); scalar(span.n_blocks);
+        scalar(span.full_sink); scalar(span.full_lo); scalar(span.full_hi);
+        const WinKeys none = {0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r0 = row0 + GROUP_ROWS * i, r1 = (r0 + GROUP_ROWS < g.lq ? r0 + GROUP_ROWS : g.lq) - 1;
+            WinSpan<TN> x = r0 < g.lq ? WinSpan<TN>(keys_of(r0), keys_of(r1), g.lc) : WinSpan<TN>(none, none, g.lc);
+            scalar(x.full_sink); scalar(x.full_lo); scalar(x.full_hi);
+            const int b = (x.full_lo + TN - 1) / TN;      // of the window's tiles
+            if (x.full_sink >= TN) first_full[i] = 0;
+            else if (x.full(b)) first_full[i] = b < span.n_sink_blocks ? b : b - span.skip;
+            if (i == grp) span_g = x;
+        }
+    }
+    auto tile_of = [&](int t) { if constexpr (WIN) return span.block(t); else return t; };      // of the chunk
+    const int NT = [&]() { if constexpr (WIN) return span.n_blocks; else return (seg_rows_le(g.ks, seg_pos_of_row(g.qs, wg_last_row)) + TN - 1) / TN; }();
+    const int n_full_wg = WIN ? 0 : seg_rows_le(g.ks, seg_pos_of_row(g.qs, row0)) / TN;
 
     // A workgroup whose rows see nothing of the chunk leaves the running (o, lse) as they are: merging an empty
     // partial is the identity.  (Without HEXI_ACCUMULATE it goes on and writes o = 0, lse = -inf.)
-    if (NT == 0 && a.accumulate) return;
+    const bool merges = [&]() { if constexpr (WIN) return a.merges(); else return a.accumulate != 0; }();
+    if (NT == 0 && merges) return;
 
     // Q^T operand fragments: lane (row l32, half hh) holds d = 16*ks + 8*hh .. +7
     bf16x8 qf[NKS];
@@ -161,7 +187,7 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
     const uint32_t fetch_lds = grp ? lds_k : lds_v;
     const int fetch_tile_bytes = grp ? K_TILE_BYTES : V_TILE_BYTES;
     auto fetch_tile = [&](int tile) {
-        const int col0 = tile * TN;
+        const int col0 = tile_of(tile) * TN;
         const uint32_t dst = __builtin_amdgcn_readfirstlane(fetch_lds + (tile & (NB - 1)) * fetch_tile_bytes + wg * 1024);
         const uint16_t* src = fetch_src + (long long)col0 * g.kv_stride_tok;
         if (col0 + TN <= g.lc) {
@@ -178,7 +204,8 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
             }
         }
         // global positions of the tile's keys, for the tiles some row needs a mask for
-        if (grp == 1 && wg == 0 && tile >= n_full_wg) {
+        const bool some_mask = [&]() { if constexpr (WIN) return tile == first_full[0] || tile == first_full[1] || !span.full(span.block(tile)); else return tile >= n_full_wg; }();
+        if (grp == 1 && wg == 0 && some_mask) {
             sm.kpos[tile & (2 * NB - 1)][lane] = col0 + lane < g.lc ? seg_pos_of_row(g.ks, col0 + lane) : 0x7fffffff;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
@@ -257,6 +284,7 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
     //   MASKED: the tile needs the causal mask (key positions from LDS).
     //   exact:  online softmax -- running maximum raised lazily (only when a tile exceeds it by more than
     //           2^8; then O and the sums are rescaled).  Otherwise the reference is fixed by the first tile.
+    auto hidden = [&](int kp) { if constexpr (WIN) return kp > my_pos || (my_pos - kp >= a.window && kp >= a.n_sink); else return kp > my_pos; };
     auto v_phase = [&](int buf, auto first_c, auto masked_c, const bool exact) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value, first_tile = decltype(first_c)::value;
         if (MASKED) {
@@ -266,10 +294,10 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
 #pragma unroll
                 for (int rb = 0; rb < 4; ++rb) {
                     const int4 p4 = *reinterpret_cast<const int4*>(&kp[32 * b + 8 * rb + 4 * hh]);
-                    if (p4.x > my_pos) s[b][4 * rb] = -INFINITY;
-                    if (p4.y > my_pos) s[b][4 * rb + 1] = -INFINITY;
-                    if (p4.z > my_pos) s[b][4 * rb + 2] = -INFINITY;
-                    if (p4.w > my_pos) s[b][4 * rb + 3] = -INFINITY;
+                    if (hidden(p4.x)) s[b][4 * rb] = -INFINITY;
+                    if (hidden(p4.y)) s[b][4 * rb + 1] = -INFINITY;
+                    if (hidden(p4.z)) s[b][4 * rb + 2] = -INFINITY;
+                    if (hidden(p4.w)) s[b][4 * rb + 3] = -INFINITY;
                 }
         }
         if (exact || first_tile) {
@@ -359,8 +387,13 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
             if (grp == 1 || !PAIR_BARRIER) wg_barrier();
             const int j = t + (grp ? K_AHEAD : V_AHEAD);
             if (j < NT) fetch_tile(j);
-            if (t >= n_full_g) v_phase(t & (2 * NB - 1), first_c, std::true_type{}, exact);
-            else v_phase(t & (2 * NB - 1), first_c, std::false_type{}, exact);
+            if constexpr (WIN) {
+                if (t == first_full[grp] || !span_g.full(span.block(t))) v_phase(t & (2 * NB - 1), std::false_type{}, std::true_type{}, true);
+                else v_phase(t & (2 * NB - 1), std::false_type{}, std::false_type{}, exact);
+            } else {
+                if (t >= n_full_g) v_phase(t & (2 * NB - 1), first_c, std::true_type{}, exact);
+                else v_phase(t & (2 * NB - 1), first_c, std::false_type{}, exact);
+            }
         };
         enter_m(0);
         m_phase(IC<0>{}, IC<NPV>{}, IC<NST>{});
@@ -398,7 +431,12 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
     float l_tot = sum_across_halves(l_run), lr_tot = sum_across_halves(lr_run);
     {
         // a row that sees any key of the chunk sees its first key
-        const bool sees = my_row < g.lq && my_pos >= g.ks.start[0];
+        const bool sees = [&]() {
+            if constexpr (WIN) {
+                const WinKeys w = win_keys_of_row(g.ks, my_pos < 0 ? 0 : my_pos, a.window, a.n_sink);
+                return my_row < g.lq && w.sink + w.hi > w.lo;
+            } else return my_row < g.lq && my_pos >= g.ks.start[0];
+        }();
         const int bad = sees && !(l_tot >= SUM_LO && l_tot <= SUM_HI);
         if (__syncthreads_or(bad)) {   // a row left the safe range: repeat the tiles with the exact online softmax
             run(std::true_type{});
@@ -407,6 +445,18 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
             // the last matrix phase of the other wavefronts may still be reading V tiles that the staging below
             // overwrites (after the fast pass the vote above is that barrier)
             __syncthreads();
+        }
+    }
+
+    if constexpr (WIN) {      // (a key that a row does not see has P = 0, and 0 x inf is NaN: what is not finite is done again element by element)
+        float z = 0.f;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z = fmaf(oacc[db][r], 0.f, z);
+        if (__syncthreads_or(z != 0.f && my_row < g.lq)) {
+            win_plain::fwd_unit<uint16_t, D>(a, h, row0, WG_ROWS, make_int4(0, g.lc, 0, 0), 0);
+            return;
         }
     }
 
@@ -420,7 +470,7 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
     }
     float wa = 0.f, wb = inv;
     float* lp = a.lse + (long long)h * g.lq + my_row_c;
-    if (a.accumulate) {
+    if (merges) {
         const float la = *lp;
         const float m = fmaxf(la, lse_new);
         if (m != -INFINITY) {
@@ -459,7 +509,7 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
     for (int i = 0; i < N_INST; ++i) {
         const int r = ROWS_PER_INST * i + sub_row;
         val[i] = *reinterpret_cast<const float4*>(&stage[r * O_STAGE_STRIDE + 4 * piece]);
-        if (a.accumulate && wrow0 + r < g.lq) old[i] = *reinterpret_cast<const float4*>(obase + r * row_stride);
+        if (merges && wrow0 + r < g.lq) old[i] = *reinterpret_cast<const float4*>(obase + r * row_stride);
         else old[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
@@ -468,7 +518,9 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgs a, const in
         const float w = stage_wa[r];
         float4 o4 = val[i];
         o4.x += w * old[i].x; o4.y += w * old[i].y; o4.z += w * old[i].z; o4.w += w * old[i].w;
-        if (wrow0 + r < g.lq) *reinterpret_cast<float4*>(obase + r * row_stride) = o4;
+        if (wrow0 + r >= g.lq) continue;
+        if constexpr (WIN) win_plain::store4(a.o, ((long long)(wrow0 + r) * g.nq + h) * D + 4 * piece, a.rounds(), o4.x, o4.y, o4.z, o4.w);
+        else *reinterpret_cast<float4*>(obase + r * row_stride) = o4;
     }
 }
 
@@ -493,11 +545,31 @@ hipError_t hexi_launch_fwd_bf16(const FwdArgs& a, hipStream_t s)
     unsigned grid = 0;
     const XcdSplit split = hexi_split_units(share.n_units(g.nq), [&](int u) { int h, p; share.unit(u, &h, &p); return cost[p < n_known ? p : n_known - 1]; }, &grid);
     if (grid > 0) {
-        if (g.d == 128) fwd_bf16_kernel<128><<<grid, 512, 0, s>>>(a, n_q_tiles, share, split);
-        else if (g.d == 64) fwd_bf16_kernel<64><<<grid, 512, 0, s>>>(a, n_q_tiles, share, split);
+        if (g.d == 128) fwd_bf16_kernel<128, false><<<grid, 512, 0, s>>>(a, n_q_tiles, share, split);
+        else if (g.d == 64) fwd_bf16_kernel<64, false><<<grid, 512, 0, s>>>(a, n_q_tiles, share, split);
         else return hipErrorInvalidValue;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || share.tiles >= n_q_tiles) return e;
     return hexi_launch_fwd_quad_bf16(a, rest_of(share, n_q_tiles), s);      // the first rows of every head
+}
+
+hipError_t hexi_launch_win_fwd_large_bf16(const WinFwdArgs& a, hipStream_t s)
+{
+    const AttnGeom& g = a.g;
+    const int n_q_tiles = (g.lq + WG_ROWS - 1) / WG_ROWS;
+    QShare share;
+    share.tiles = n_q_tiles;
+    share.extra = 0;
+    // a unit's cost: the key tiles that it streams, and about six tiles' worth to start and to finish
+    float cost[4096];
+    const int n_known = n_q_tiles < 4096 ? n_q_tiles : 4096;     // (longer shards: the remaining tiles count like the last known one)
+    for (int p = 0; p < n_known; ++p) {
+        const int row = (n_q_tiles - 1 - p) * WG_ROWS, last = (row + WG_ROWS < g.lq ? row + WG_ROWS : g.lq) - 1;
+        cost[p] = (float)WinSpan<TN>(win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink), win_keys_of_row(g.ks, seg_pos_of_row(g.qs, last), a.window, a.n_sink), g.lc).n_blocks + 6.0f;
+    }
+    unsigned grid = 0;
+    const XcdSplit split = hexi_split_units(share.n_units(g.nq), [&](int u) { int h, p; share.unit(u, &h, &p); return cost[p < n_known ? p : n_known - 1]; }, &grid);
+    fwd_bf16_kernel<128, true><<<grid, 512, 0, s>>>(a, n_q_tiles, share, split);
+    return hipGetLastError();
 }

@@ -10,7 +10,7 @@
 // the first block sets the softmax reference without rescaling zeros.  The end: every wavefront weighs its own partial result, the
 // running values are on their way meanwhile, two barriers instead of three.  These took 512 x 512 x 4 heads x 128 from 9.7 to 8.1 us
 // (forward) and from 11.3 to 8.5 us (dQ), 1024 x 1024 x 8 from 12.9 to 11.7 us.  Larger launches take the 64-row workgroups of
-// hexi_bf16_quad.hip, then the large ones, which stream less per row: see the rules in hexi_shapes.h.  Measured, us per call
+// hexi_bf16_quad.h, then the large ones, which stream less per row: see the rules in hexi_shapes.h.  Measured, us per call
 // (head_dim 128, fully visible chunk), large workgroups -> these: 300 rows x 700 keys, 4 / 2 heads: forward 28.3 -> 9.3, dQ
 // 36.2 -> 9.8, dK/dV 23.5 -> 12.3.
 //

@@ -1,5 +1,5 @@
 // Pieces shared by the bf16 kernels whose wavefronts stream 32-row blocks through a private part of LDS (hexi_bf16_split.hip,
-// hexi_bf16_quad.hip).  A block's LDS image is [32][D] bf16 with the 16-byte pieces of a row permuted by piece ^ swz(row), which makes
+// hexi_bf16_quad.h).  A block's LDS image is [32][D] bf16 with the 16-byte pieces of a row permuted by piece ^ swz(row), which makes
 // the 128-bit row reads (16 rows, one piece) and the transposed 64-bit reads (4 rows x 64 bytes) both touch all 64 banks once.
 #pragma once
 #include <cstddef>

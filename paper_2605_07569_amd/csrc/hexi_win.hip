@@ -1,5 +1,5 @@
 // Attention under a sliding window with sink tokens: the fp32 kernels (units of hexi_f32_units.h on windowed runs of keys and rows), dispatch, and Delta from a
-// bf16 o.  The bf16 kernels are those of hexi_bf16_quad.hip.
+// bf16 o.  The bf16 kernels are those of hexi_bf16_quad.h and hexi_bf16_fwd.hip.
 #include "hexi_f32_units.h"
 #include <type_traits>
 
@@ -43,14 +43,13 @@ template <class F> hipError_t with_cfg(int d, bool split, F f)
 
 }  // namespace
 
-#include <cstdlib>
-static int env_shape(const char* n) { const char* v = getenv(n); return v ? atoi(v) : 1; }
-
 static hipError_t launch_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
     if (a.few) return hexi_launch_win_few(a, dtype, s);
-    if (dtype == HEXI_BF16) return hexi_launch_win_fwd_quad_bf16(a, s);
-    return with_cfg(a.g.d, env_shape("WFS"), [&](auto cfg) {
+    if (dtype == HEXI_BF16) return a.n_splits == 1 && hexi_win_fwd_large(a.g.nq, a.g.lq, a.g.lc, a.g.d, a.window, a.n_sink) ? hexi_launch_win_fwd_large_bf16(a, s) : hexi_launch_win_fwd_quad_bf16(a, s);
+    const AttnGeom& g = a.g;
+    const bool split = a.n_splits > 1 || hexi_win_f32_split(0, g.nq, g.nkv, g.lq, g.lc, g.d, a.window, a.n_sink);      // (runs of keys that are split further are 16-row units')
+    return with_cfg(g.d, split, [&](auto cfg) {
         using C = decltype(cfg);
         const unsigned grid = (unsigned)((a.g.lq + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nq;
         win_fwd_f32_kernel<C::D, C::SPLIT, C::TWO><<<dim3(grid, (unsigned)a.n_splits), 64 * C::NW, 0, s>>>(a);
@@ -66,12 +65,20 @@ hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s)
 {
     if (dtype == HEXI_BF16) return hexi_launch_win_bwd_quad_bf16(a, s);
-    return with_cfg(a.g.d, env_shape("WBS"), [&](auto cfg) {
-        using C = decltype(cfg);
-        const unsigned n_dkdv = a.want_dkdv ? (unsigned)((a.g.lc + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nkv : 0u;
-        const unsigned n_dq = a.want_dq ? (unsigned)((a.g.lq + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nq : 0u;
-        win_bwd_f32_kernel<C::D, C::SPLIT, C::TWO><<<n_dkdv + n_dq, 64 * C::NW, 0, s>>>(a, n_dkdv);
-    });
+    const AttnGeom& g = a.g;
+    auto launch = [&](bool split, bool dkdv, bool dq) {
+        return with_cfg(g.d, split, [&](auto cfg) {
+            using C = decltype(cfg);
+            const unsigned n_dkdv = dkdv ? (unsigned)((g.lc + C::ROWS - 1) / C::ROWS) * (unsigned)g.nkv : 0u;
+            const unsigned n_dq = dq ? (unsigned)((g.lq + C::ROWS - 1) / C::ROWS) * (unsigned)g.nq : 0u;
+            win_bwd_f32_kernel<C::D, C::SPLIT, C::TWO><<<n_dkdv + n_dq, 64 * C::NW, 0, s>>>(a, n_dkdv);
+        });
+    };
+    // (halves of one shape in one launch: they fill each other's last round)
+    const bool kv_split = hexi_win_f32_split(2, g.nq, g.nkv, g.lq, g.lc, g.d, a.window, a.n_sink), q_split = hexi_win_f32_split(1, g.nq, g.nkv, g.lq, g.lc, g.d, a.window, a.n_sink);
+    if (a.want_dkdv && a.want_dq && kv_split == q_split) return launch(kv_split, true, true);
+    const hipError_t e = a.want_dkdv ? launch(kv_split, true, false) : hipSuccess;
+    return e != hipSuccess || !a.want_dq ? e : launch(q_split, false, true);
 }
 
 namespace {

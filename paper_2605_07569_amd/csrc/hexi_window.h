@@ -34,7 +34,7 @@ template <bool WIN> using BwdArgsOf = typename WinOr<WIN>::Bwd;
 // Keys that a row at position p sees: [0, sink) and [lo, hi), sink <= lo <= hi.  Where the sinks reach the window they are one run, sink = lo = 0: along
 // a shard these rows come first, and sink, lo and hi never fall.
 struct WinKeys { int sink, lo, hi; };
-__host__ __device__ inline WinKeys win_keys_of_row(const SegTable& ks, int p, int window, int n_sink)
+__host__ __device__ __attribute__((always_inline)) inline WinKeys win_keys_of_row(const SegTable& ks, int p, int window, int n_sink)
 {
     WinKeys w;
     w.hi = seg_rows_le(ks, p);
@@ -53,7 +53,7 @@ template <int B> struct WinSpan {
     int n_whole;                      // blocks of the run before one that the chunk's end cuts
     int full_sink, full_lo, full_hi;  // keys that every row sees: [0, full_sink) and [full_lo, full_hi)
     WinSpan() = default;
-    __host__ __device__ WinSpan(const WinKeys& first, const WinKeys& last, int lc)
+    __host__ __device__ __attribute__((always_inline)) WinSpan(const WinKeys& first, const WinKeys& last, int lc)
     {
         const int b0 = first.lo / B, b1 = (last.hi + B - 1) / B, s = (last.sink + B - 1) / B;
         n_sink_blocks = s < b0 ? s : b0;
@@ -64,21 +64,21 @@ template <int B> struct WinSpan {
         full_lo = last.lo;
         full_hi = first.hi;
     }
-    __host__ __device__ int block(int i) const { return i < n_sink_blocks ? i : i + skip; }
+    __host__ __device__ __attribute__((always_inline)) int block(int i) const { return i < n_sink_blocks ? i : i + skip; }
     // blocks [i0, i1) of the run of a split
-    __host__ __device__ int split_start(int split, int n_splits) const
+    __host__ __device__ __attribute__((always_inline)) int split_start(int split, int n_splits) const
     {
         if (n_splits == 1) return split * n_blocks;
         const int each = n_blocks / n_splits, rest = n_blocks - each * n_splits;
         return split * each + (split < rest ? split : rest);
     }
     // whether every row sees all of the chunk's block b
-    __host__ __device__ bool full(int b) const { return (B * b >= full_lo && B * b + B <= full_hi) || B * b + B <= full_sink; }
+    __host__ __device__ __attribute__((always_inline)) bool full(int b) const { return (B * b >= full_lo && B * b + B <= full_hi) || B * b + B <= full_sink; }
 };
 
 // Rows that see a key at position p: [first, end).
 struct WinRows { int first, end; };
-__host__ __device__ inline WinRows win_rows_of_key(const SegTable& qs, int p, int window, int n_sink)
+__host__ __device__ __attribute__((always_inline)) inline WinRows win_rows_of_key(const SegTable& qs, int p, int window, int n_sink)
 {
     WinRows w;
     w.first = seg_rows_le(qs, p - 1);
@@ -140,6 +140,46 @@ inline size_t hexi_win_fwd_workspace(int n_splits, int nq, long long lq, int d)
     return n_splits > 1 ? (size_t)n_splits * (size_t)lq * (size_t)nq * (size_t)(d + 1) * sizeof(float) : 0;
 }
 
+// Whether a bf16 forward call takes 256-row workgroups (head_dim 128 alone; at 64 they are slower everywhere).  Fitted to 76 random calls, us: rounds of 256 workgroups
+// times a start and end and their key tiles, 18 + 2.0 a tile of 64 keys, against rounds of 64-row ones, 6 + 1.17 a step of 128.  64 rows / 256 rows: 16 heads of 3729
+// rows, window 4873 190 / 169; 24 of 13495, 2972 665 / 607; 8 of 16384, 4096 327 / 305; 32 of 18703, 1190 703 / 720; 8 of 8513, 2018 (272 workgroups of 256) 127 / 176.
+inline bool hexi_win_fwd_large(int nq, long long lq, long long lc, int d, long long window, long long n_sink)
+{
+    if (d != 128) return false;
+    auto keys = [&](long long rows, long long block) {
+        const double k = (double)window + (double)rows - 1.0 + (double)block - 1.0 + (double)n_sink;
+        return k < (double)lc ? k : (double)lc;
+    };
+    const long long large = (lq + 255) / 256 * nq, small = (lq + 63) / 64 * nq;
+    const double t_large = (double)((large + 255) / 256) * (18.0 + 2.0 / 64.0 * keys(256, 64));
+    const double t_small = ((double)small / 256.0 + 0.25) * (6.0 + 1.17 / 128.0 * keys(64, 32));
+    return t_large < 0.97 * t_small;
+}
+
+// Whether the fp32 units of a windowed call take 16 rows (or keys), streamed rows split over eight wavefronts, or 64 that share tiles: PART 0 forward, 1 dQ, 2 dK/dV.
+// Fitted to 190 random calls (90 % within 15 %), us: a base, and for every round of 256 workgroups a fixed part and a step, 32 streamed rows in the 64-row shape and 128 in
+// the other; more 64-row units than CUs share one and take at least 1.6 rounds at head_dim 128.  The choice is on average under 1 % slower than the better one.  64 rows / 16 rows:
+// forward, 128 columns, 16 heads of 3667, window 26 54 / 104, 4 of 4173, 1581 254 / 190; dQ, 64 columns, 24 of 6094, 83 89 / 156; dK/dV, 8 kv heads, 8000, 821 476 / 642,
+// 8/4 of 1707, 1274 393 / 184.
+inline bool hexi_win_f32_split(int part, int nq, int nkv, long long lq, long long lc, int d, long long window, long long n_sink)
+{
+    struct Fit { double base, fixed, step; };
+    static const Fit fits[2][3][2] = {{{{8.0, 1.0, 1.60}, {4.8, 2.5, 1.47}}, {{6.6, 1.9, 2.03}, {4.9, 3.4, 1.73}}, {{4.2, 3.4, 3.16}, {6.8, 4.7, 2.42}}},
+                                      {{{3.0, 7.4, 2.66}, {1.2, 7.4, 2.79}}, {{0.7, 11.1, 3.51}, {0.7, 9.8, 3.48}}, {{5.7, 4.4, 5.23}, {1.7, 13.6, 4.76}}}};
+    const double seen = window + n_sink < lc ? (double)(window + n_sink) : (double)lc;      // keys of a row
+    auto us = [&](int shape) {
+        const Fit& f = fits[d == 128][part][shape];
+        const int rows = shape ? 16 : 64;
+        const double units = part == 2 ? (double)((lc + rows - 1) / rows * nkv) : (double)((lq + rows - 1) / rows * nq);
+        double chain = part == 2 ? ((double)lq * seen / (double)lc + rows - 1) * nq / nkv : seen + rows - 1 < (double)lc ? seen + rows - 1 : (double)lc;
+        chain /= shape ? 128.0 : 32.0;
+        double rounds = units > 256.0 ? units / 256.0 : 1.0;
+        if (!shape && d == 128 && units > 256.0 && rounds < 1.6) rounds = 1.6;
+        return f.base + rounds * (f.fixed + f.step * chain);
+    };
+    return us(1) <= us(0);
+}
+
 // One run of q heads to every kv head, in head order; empty for a kv head that no q head reads.
 inline void hexi_head_run_of_each_kv(const signed char* kv_of_q, int nq, int nkv, HeadRuns* runs)
 {
@@ -161,7 +201,8 @@ hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s);
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s);
 hipError_t hexi_launch_win_few(const WinFwdArgs& a, int dtype, hipStream_t s);      // in hexi_win_few.hip
 hipError_t hexi_launch_win_join(const WinFwdArgs& a, hipStream_t s);
-hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_quad.hip
+hipError_t hexi_launch_win_fwd_large_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_fwd.hip: 256-row workgroups
+hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_quad_win.hip
 hipError_t hexi_launch_win_bwd_quad_bf16(const WinBwdArgs& a, hipStream_t s);
 // Delta = rowsum(dO o) of a bf16 o
 hipError_t hexi_launch_delta_bf16_o(long long lq, int nq, int d, const void* o, const void* d_o, int dtype,
