@@ -46,9 +46,9 @@ template <class F> hipError_t with_cfg(int d, bool split, F f)
 static hipError_t launch_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
     if (a.few) return hexi_launch_win_few(a, dtype, s);
-    if (dtype == HEXI_BF16) return a.n_splits == 1 && hexi_win_fwd_large(a.g.nq, a.g.lq, a.g.lc, a.g.d, a.window, a.n_sink) ? hexi_launch_win_fwd_large_bf16(a, s) : hexi_launch_win_fwd_quad_bf16(a, s);
+    if (dtype == HEXI_BF16) return a.n_splits == 1 && hexi_win_fwd_large(a.g, a.window, a.n_sink) ? hexi_launch_win_fwd_large_bf16(a, s) : hexi_launch_win_fwd_quad_bf16(a, s);
     const AttnGeom& g = a.g;
-    const bool split = a.n_splits > 1 || hexi_win_f32_split(0, g.nq, g.nkv, g.lq, g.lc, g.d, a.window, a.n_sink);      // (runs of keys that are split further are 16-row units')
+    const bool split = a.n_splits > 1 || hexi_win_f32_split(0, g, a.window, a.n_sink);      // (runs of keys that are split further are 16-row units')
     return with_cfg(g.d, split, [&](auto cfg) {
         using C = decltype(cfg);
         const unsigned grid = (unsigned)((a.g.lq + C::ROWS - 1) / C::ROWS) * (unsigned)a.g.nq;
@@ -75,7 +75,7 @@ hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s)
         });
     };
     // (halves of one shape in one launch: they fill each other's last round)
-    const bool kv_split = hexi_win_f32_split(2, g.nq, g.nkv, g.lq, g.lc, g.d, a.window, a.n_sink), q_split = hexi_win_f32_split(1, g.nq, g.nkv, g.lq, g.lc, g.d, a.window, a.n_sink);
+    const bool kv_split = hexi_win_f32_split(2, g, a.window, a.n_sink), q_split = hexi_win_f32_split(1, g, a.window, a.n_sink);
     if (a.want_dkdv && a.want_dq && kv_split == q_split) return launch(kv_split, true, true);
     const hipError_t e = a.want_dkdv ? launch(kv_split, true, false) : hipSuccess;
     return e != hipSuccess || !a.want_dq ? e : launch(q_split, false, true);

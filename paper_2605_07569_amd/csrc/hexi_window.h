@@ -4,6 +4,7 @@
 // before its own position that are sinks, and those inside its window.  What a key is seen by is one run of rows (a sink: all rows
 // from its own position on; another key: the window - 1 rows' positions behind it).
 #pragma once
+#include <cmath>
 #include "hexi_internal.h"
 
 struct WinFwdArgs : FwdArgs {
@@ -140,19 +141,38 @@ inline size_t hexi_win_fwd_workspace(int n_splits, int nq, long long lq, int d)
     return n_splits > 1 ? (size_t)n_splits * (size_t)lq * (size_t)nq * (size_t)(d + 1) * sizeof(float) : 0;
 }
 
+// What the rows of a shard see of a chunk, and what sees its keys, from 16 of each: the share that sees (is seen by) anything, and the keys (rows) of one that does.
+struct WinLoad { double share, mean; };
+template <class F> inline WinLoad hexi_win_load(int n, F count)
+{
+    int some = 0;
+    double sum = 0.0;
+    for (int i = 0; i < 16; ++i) {
+        const int c = count((int)((long long)n * (2 * i + 1) / 32));
+        some += c > 0;
+        sum += c;
+    }
+    return {some / 16.0, some ? sum / some : 0.0};
+}
+inline WinLoad hexi_win_row_load(const AttnGeom& g, int window, int n_sink)
+{
+    return hexi_win_load(g.lq, [&](int row) { const WinKeys w = win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), window, n_sink); return w.sink + w.hi - w.lo; });
+}
+inline WinLoad hexi_win_key_load(const AttnGeom& g, int window, int n_sink)
+{
+    return hexi_win_load(g.lc, [&](int key) { const WinRows w = win_rows_of_key(g.qs, seg_pos_of_row(g.ks, key), window, n_sink); return w.end > w.first ? w.end - w.first : 0; });
+}
+
 // Whether a bf16 forward call takes 256-row workgroups (head_dim 128 alone; at 64 they are slower everywhere).  Fitted to 76 random calls, us: rounds of 256 workgroups
 // times a start and end and their key tiles, 18 + 2.0 a tile of 64 keys, against rounds of 64-row ones, 6 + 1.17 a step of 128.  64 rows / 256 rows: 16 heads of 3729
 // rows, window 4873 190 / 169; 24 of 13495, 2972 665 / 607; 8 of 16384, 4096 327 / 305; 32 of 18703, 1190 703 / 720; 8 of 8513, 2018 (272 workgroups of 256) 127 / 176.
-inline bool hexi_win_fwd_large(int nq, long long lq, long long lc, int d, long long window, long long n_sink)
+inline bool hexi_win_fwd_large(const AttnGeom& g, int window, int n_sink)
 {
-    if (d != 128) return false;
-    auto keys = [&](long long rows, long long block) {
-        const double k = (double)window + (double)rows - 1.0 + (double)block - 1.0 + (double)n_sink;
-        return k < (double)lc ? k : (double)lc;
-    };
-    const long long large = (lq + 255) / 256 * nq, small = (lq + 63) / 64 * nq;
-    const double t_large = (double)((large + 255) / 256) * (18.0 + 2.0 / 64.0 * keys(256, 64));
-    const double t_small = ((double)small / 256.0 + 0.25) * (6.0 + 1.17 / 128.0 * keys(64, 32));
+    if (g.d != 128) return false;
+    const WinLoad load = hexi_win_row_load(g, window, n_sink);
+    const double large = load.share * ((g.lq + 255) / 256) * g.nq, small = load.share * ((g.lq + 63) / 64) * g.nq;
+    const double t_large = ceil(large / 256.0) * (18.0 + 2.0 / 64.0 * (load.mean + 255 + 63));
+    const double t_small = (small / 256.0 + 0.25) * (6.0 + 1.17 / 128.0 * (load.mean + 63 + 31));
     return t_large < 0.97 * t_small;
 }
 
@@ -161,20 +181,19 @@ inline bool hexi_win_fwd_large(int nq, long long lq, long long lc, int d, long l
 // the other; more 64-row units than CUs share one and take at least 1.6 rounds at head_dim 128.  The choice is on average under 1 % slower than the better one.  64 rows / 16 rows:
 // forward, 128 columns, 16 heads of 3667, window 26 54 / 104, 4 of 4173, 1581 254 / 190; dQ, 64 columns, 24 of 6094, 83 89 / 156; dK/dV, 8 kv heads, 8000, 821 476 / 642,
 // 8/4 of 1707, 1274 393 / 184.
-inline bool hexi_win_f32_split(int part, int nq, int nkv, long long lq, long long lc, int d, long long window, long long n_sink)
+inline bool hexi_win_f32_split(int part, const AttnGeom& g, int window, int n_sink)
 {
     struct Fit { double base, fixed, step; };
     static const Fit fits[2][3][2] = {{{{8.0, 1.0, 1.60}, {4.8, 2.5, 1.47}}, {{6.6, 1.9, 2.03}, {4.9, 3.4, 1.73}}, {{4.2, 3.4, 3.16}, {6.8, 4.7, 2.42}}},
                                       {{{3.0, 7.4, 2.66}, {1.2, 7.4, 2.79}}, {{0.7, 11.1, 3.51}, {0.7, 9.8, 3.48}}, {{5.7, 4.4, 5.23}, {1.7, 13.6, 4.76}}}};
-    const double seen = window + n_sink < lc ? (double)(window + n_sink) : (double)lc;      // keys of a row
+    const WinLoad load = part == 2 ? hexi_win_key_load(g, window, n_sink) : hexi_win_row_load(g, window, n_sink);
     auto us = [&](int shape) {
-        const Fit& f = fits[d == 128][part][shape];
+        const Fit& f = fits[g.d == 128][part][shape];
         const int rows = shape ? 16 : 64;
-        const double units = part == 2 ? (double)((lc + rows - 1) / rows * nkv) : (double)((lq + rows - 1) / rows * nq);
-        double chain = part == 2 ? ((double)lq * seen / (double)lc + rows - 1) * nq / nkv : seen + rows - 1 < (double)lc ? seen + rows - 1 : (double)lc;
-        chain /= shape ? 128.0 : 32.0;
+        const double units = load.share * (part == 2 ? (double)((g.lc + rows - 1) / rows) * g.nkv : (double)((g.lq + rows - 1) / rows) * g.nq);
+        const double chain = (load.mean + rows - 1) * (part == 2 ? (double)g.nq / g.nkv : 1.0) / (shape ? 128.0 : 32.0);
         double rounds = units > 256.0 ? units / 256.0 : 1.0;
-        if (!shape && d == 128 && units > 256.0 && rounds < 1.6) rounds = 1.6;
+        if (!shape && g.d == 128 && units > 256.0 && rounds < 1.6) rounds = 1.6;
         return f.base + rounds * (f.fixed + f.step * chain);
     };
     return us(1) <= us(0);
