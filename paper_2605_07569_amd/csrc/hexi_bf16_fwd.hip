@@ -122,26 +122,24 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgsOf<WIN> a, c
     int n_full_g = 0;
     if (!WIN && grow0 < g.lq) n_full_g = seg_rows_le(g.ks, seg_pos_of_row(g.qs, grow0)) / TN;
     const int wg_last_row = (row0 + WG_ROWS < g.lq ? row0 + WG_ROWS : g.lq) - 1;
-    // (WIN) the workgroup's run of tiles, what its group's rows see of it, and the run's first tile that all rows of group 0, of group 1, see
+    // (WIN) the workgroup's run of tiles, what its group's rows see of it, the run's first tile that all of them see, and the lane's row's keys
     WinSpan<TN> span, span_g;
-    int first_full[2] = {-1, -1};
+    int first_full = -1;
+    WinKeys my_keys = {0, 0, 0};
     if constexpr (WIN) {
         auto keys_of = [&](int row) { return win_keys_of_row(g.ks, seg_pos_of_row(g.qs, row), a.window, a.n_sink); };
         auto scalar = [](int& x) { x = __builtin_amdgcn_readfirstlane(x); };      // (the compiler does not see that these are the same in all lanes)
         span = WinSpan<TN>(keys_of(row0), keys_of(wg_last_row), g.lc);
         scalar(span.n_sink_blocks); scalar(span.skip); scalar(span.n_blocks);
-        scalar(span.full_sink); scalar(span.full_lo); scalar(span.full_hi);
-        const WinKeys none = {0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r0 = row0 + GROUP_ROWS * i, r1 = (r0 + GROUP_ROWS < g.lq ? r0 + GROUP_ROWS : g.lq) - 1;
-            WinSpan<TN> x = r0 < g.lq ? WinSpan<TN>(keys_of(r0), keys_of(r1), g.lc) : WinSpan<TN>(none, none, g.lc);
-            scalar(x.full_sink); scalar(x.full_lo); scalar(x.full_hi);
-            const int b = (x.full_lo + TN - 1) / TN;      // of the window's tiles
-            if (x.full_sink >= TN) first_full[i] = 0;
-            else if (x.full(b)) first_full[i] = b < span.n_sink_blocks ? b : b - span.skip;
-            if (i == grp) span_g = x;
-        }
+        if (grow0 < g.lq) {
+            span_g = WinSpan<TN>(keys_of(grow0), keys_of((grow0 + GROUP_ROWS < g.lq ? grow0 + GROUP_ROWS : g.lq) - 1), g.lc);
+            if (my_pos >= 0) my_keys = win_keys_of_row(g.ks, my_pos, a.window, a.n_sink);
+        } else span_g = WinSpan<TN>(my_keys, my_keys, g.lc);
+        scalar(span_g.full_sink); scalar(span_g.full_lo); scalar(span_g.full_hi);
+        const int b = (span_g.full_lo + TN - 1) / TN;      // of the window's tiles
+        if (span_g.full_sink >= TN) first_full = 0;
+        else if (span_g.full(b)) first_full = b < span.n_sink_blocks ? b : b - span.skip;
+        scalar(first_full);
     }
     auto tile_of = [&](int t) { if constexpr (WIN) return span.block(t); else return t; };      // of the chunk
     const int NT = [&]() { if constexpr (WIN) return span.n_blocks; else return (seg_rows_le(g.ks, seg_pos_of_row(g.qs, wg_last_row)) + TN - 1) / TN; }();
@@ -204,8 +202,7 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgsOf<WIN> a, c
             }
         }
         // global positions of the tile's keys, for the tiles some row needs a mask for
-        const bool some_mask = [&]() { if constexpr (WIN) return tile == first_full[0] || tile == first_full[1] || !span.full(span.block(tile)); else return tile >= n_full_wg; }();
-        if (grp == 1 && wg == 0 && some_mask) {
+        if (!WIN && grp == 1 && wg == 0 && tile >= n_full_wg) {
             sm.kpos[tile & (2 * NB - 1)][lane] = col0 + lane < g.lc ? seg_pos_of_row(g.ks, col0 + lane) : 0x7fffffff;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
@@ -284,20 +281,26 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgsOf<WIN> a, c
     //   MASKED: the tile needs the causal mask (key positions from LDS).
     //   exact:  online softmax -- running maximum raised lazily (only when a tile exceeds it by more than
     //           2^8; then O and the sums are rescaled).  Otherwise the reference is fixed by the first tile.
-    auto hidden = [&](int kp) { if constexpr (WIN) return kp > my_pos || (my_pos - kp >= a.window && kp >= a.n_sink); else return kp > my_pos; };
     auto v_phase = [&](int buf, auto first_c, auto masked_c, const bool exact) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value, first_tile = decltype(first_c)::value;
-        if (MASKED) {
+        if constexpr (MASKED && WIN) {      // (buf: the tile's first key)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const uint32_t seen = win_bits(my_keys, buf + 32 * b) >> (4 * hh);
+                auto one = [&](auto ic) __attribute__((always_inline)) { constexpr int i = decltype(ic)::value; s[b][i] = win_or<8 * (i >> 2) + (i & 3)>(seen, s[b][i], -INFINITY); };
+                for_range<0, 16>(one);
+            }
+        } else if (MASKED) {
             const int* kp = &sm.kpos[buf][0];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int rb = 0; rb < 4; ++rb) {
                     const int4 p4 = *reinterpret_cast<const int4*>(&kp[32 * b + 8 * rb + 4 * hh]);
-                    if (hidden(p4.x)) s[b][4 * rb] = -INFINITY;
-                    if (hidden(p4.y)) s[b][4 * rb + 1] = -INFINITY;
-                    if (hidden(p4.z)) s[b][4 * rb + 2] = -INFINITY;
-                    if (hidden(p4.w)) s[b][4 * rb + 3] = -INFINITY;
+                    if (p4.x > my_pos) s[b][4 * rb] = -INFINITY;
+                    if (p4.y > my_pos) s[b][4 * rb + 1] = -INFINITY;
+                    if (p4.z > my_pos) s[b][4 * rb + 2] = -INFINITY;
+                    if (p4.w > my_pos) s[b][4 * rb + 3] = -INFINITY;
                 }
         }
         if (exact || first_tile) {
@@ -388,8 +391,9 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgsOf<WIN> a, c
             const int j = t + (grp ? K_AHEAD : V_AHEAD);
             if (j < NT) fetch_tile(j);
             if constexpr (WIN) {
-                if (t == first_full[grp] || !span_g.full(span.block(t))) v_phase(t & (2 * NB - 1), std::false_type{}, std::true_type{}, true);
-                else v_phase(t & (2 * NB - 1), std::false_type{}, std::false_type{}, exact);
+                const int b = span.block(t);
+                if (t == first_full || !span_g.full(b)) v_phase(b * TN, std::false_type{}, std::true_type{}, true);
+                else v_phase(b * TN, std::false_type{}, std::false_type{}, exact);
             } else {
                 if (t >= n_full_g) v_phase(t & (2 * NB - 1), first_c, std::true_type{}, exact);
                 else v_phase(t & (2 * NB - 1), first_c, std::false_type{}, exact);
@@ -432,10 +436,7 @@ __global__ void __launch_bounds__(512) fwd_bf16_kernel(const FwdArgsOf<WIN> a, c
     {
         // a row that sees any key of the chunk sees its first key
         const bool sees = [&]() {
-            if constexpr (WIN) {
-                const WinKeys w = win_keys_of_row(g.ks, my_pos < 0 ? 0 : my_pos, a.window, a.n_sink);
-                return my_row < g.lq && w.sink + w.hi > w.lo;
-            } else return my_row < g.lq && my_pos >= g.ks.start[0];
+            if constexpr (WIN) return my_keys.sink + my_keys.hi > my_keys.lo; else return my_row < g.lq && my_pos >= g.ks.start[0];
         }();
         const int bad = sees && !(l_tot >= SUM_LO && l_tot <= SUM_HI);
         if (__syncthreads_or(bad)) {   // a row left the safe range: repeat the tiles with the exact online softmax

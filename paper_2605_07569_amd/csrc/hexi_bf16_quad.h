@@ -76,16 +76,8 @@ struct VisibleWin {
     {
         return {__builtin_amdgcn_readlane(w.sink, lane), __builtin_amdgcn_readlane(w.lo, lane), __builtin_amdgcn_readlane(w.hi, lane)};
     }
-    // keep(i, whether row block r sees key 8 (i / 4) + 4 hh + i % 4 of the chunk's block b)
-    template <class F> __device__ __forceinline__ void each_key(int r, int b, int hh, F keep) const
-    {
-        const int at = b * TB + 4 * hh, n_sink = mine[r].sink - at, lo = mine[r].lo - at, hi = mine[r].hi - at;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int o = 8 * (i >> 2) + (i & 3);
-            keep(i, o < n_sink || (o >= lo && o < hi));
-        }
-    }
+    // bit 8 (i / 4) + i % 4: row block r sees key 8 (i / 4) + 4 hh + i % 4 of the chunk's block b
+    __device__ __forceinline__ uint32_t bits(int r, int b, int hh) const { return win_bits(mine[r], b * TB) >> (4 * hh); }
 };
 
 // Not 0 (NaN) if some value is not finite.  A key that a row does not see has P = 0 there, and 0 x inf and 0 x NaN are NaN: a windowed unit whose sums are
@@ -235,7 +227,11 @@ __global__ void __launch_bounds__(256, D == 64 ? 2 : 1) fwd_quad_bf16_kernel(con
             if (vis.span.full(cb)) return;
             keep_branch();
 #pragma unroll
-            for (int r = 0; r < 2; ++r) vis.each_key(r, cb, hh, [&](int i, bool seen) __attribute__((always_inline)) { if (!seen) s[r][i] = -INFINITY; });
+            for (int r = 0; r < 2; ++r) {
+                const uint32_t seen = vis.bits(r, cb, hh);
+                auto one = [&](auto ic) __attribute__((always_inline)) { constexpr int i = decltype(ic)::value; s[r][i] = win_or<8 * (i >> 2) + (i & 3)>(seen, s[r][i], -INFINITY); };
+                for_range<0, 16>(one);
+            }
         } else {
             if (b < vis.n_full) return;
             keep_branch();
@@ -607,7 +603,9 @@ __device__ __forceinline__ void dq_unit(const BwdArgsOf<WIN>& a, const int h, co
                 const int cb = block(b);
                 if (vis.span.full(cb)) return;
                 keep_branch();
-                vis.each_key(r, cb, hh, [&](int i, bool seen) __attribute__((always_inline)) { if (!seen) s[r][i] = 0.f; });
+                const uint32_t seen = vis.bits(r, cb, hh);
+                auto one = [&](auto ic) __attribute__((always_inline)) { constexpr int i = decltype(ic)::value; s[r][i] = win_or<8 * (i >> 2) + (i & 3)>(seen, s[r][i], 0.f); };
+                for_range<0, 16>(one);
             } else {
                 if (b < vis.n_full) return;
                 keep_branch();
@@ -920,19 +918,25 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
         auto mask = [&](int c) __attribute__((always_inline)) {     // (a row that sees nothing anywhere, LSE = -inf, is masked in every block)
             if (cur >= row_full && cur + TB <= (WIN ? row_full_end : g.lq)) return;
             keep_branch();
-            int lo, end = 0;
             if constexpr (WIN) {
                 const int2 by = sm.m.seen_by[32 * c + l32];
-                lo = by.x > cur ? by.x : cur;
-                end = by.y;
-            } else lo = my_first[c] > cur ? my_first[c] : cur;
-            auto sees = [&](int r) { if constexpr (WIN) return r >= lo && r < end; else return r >= lo && r < g.lq; };
+                const uint32_t seen = win_bits(by.x > cur ? by.x : cur, by.y, row) >> (4 * hh);
+                auto two = [&](auto ic) __attribute__((always_inline)) {
+                    constexpr int i = decltype(ic)::value, o = 8 * (i >> 1) + 2 * (i & 1);
+                    const uint32_t keep = (win_bit<o>(seen) & 0xffffu) | (win_bit<o + 1>(seen) & 0xffff0000u);
+                    pw[c][i] &= keep;
+                    dw[c][i] &= keep;
+                };
+                for_range<0, 8>(two);
+            } else {
+                const int lo = my_first[c] > cur ? my_first[c] : cur;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r0 = row + 8 * (i >> 1) + 4 * hh + 2 * (i & 1);
-                const uint32_t keep = (sees(r0) ? 0xffffu : 0u) | (sees(r0 + 1) ? 0xffff0000u : 0u);
-                pw[c][i] &= keep;
-                dw[c][i] &= keep;
+                for (int i = 0; i < 8; ++i) {
+                    const int r0 = row + 8 * (i >> 1) + 4 * hh + 2 * (i & 1);
+                    const uint32_t keep = (r0 >= lo && r0 < g.lq ? 0xffffu : 0u) | (r0 + 1 >= lo && r0 + 1 < g.lq ? 0xffff0000u : 0u);
+                    pw[c][i] &= keep;
+                    dw[c][i] &= keep;
+                }
             }
         };
         auto frag = [&](const uint32_t (&w)[8], int u) __attribute__((always_inline)) {

@@ -46,6 +46,22 @@ __host__ __device__ __attribute__((always_inline)) inline WinKeys win_keys_of_ro
     return w;
 }
 
+#ifdef __HIP__
+// Bits 0 .. n - 1; n below 0 counts as 0, above 32 as 32.
+__device__ __forceinline__ uint32_t win_low_bits(int n) { return n <= 0 ? 0u : 0xffffffffu >> (n < 32 ? 32 - n : 0); }
+// Bit i: index at + i lies in [lo, hi).
+__device__ __forceinline__ uint32_t win_bits(int lo, int hi, int at) { return win_low_bits(hi - at) & ~win_low_bits(lo - at); }
+__device__ __forceinline__ uint32_t win_bits(const WinKeys& w, int at) { return win_bits(w.lo, w.hi, at) | win_low_bits(w.sink - at); }
+// All ones where bit i of the mask is set, zero where not: two instructions to a masked value (a comparison of positions took six: 1000 clocks of a masked 32-key
+// block of two row blocks, in which a step at head_dim 64 takes 2000).
+template <int I> __device__ __forceinline__ uint32_t win_bit(uint32_t bits) { return (uint32_t)__builtin_amdgcn_sbfe((int)bits, I, 1); }
+template <int I> __device__ __forceinline__ float win_or(uint32_t bits, float x, float other)      // x where bit I is set
+{
+    const uint32_t m = win_bit<I>(bits);
+    return __uint_as_float((__float_as_uint(x) & m) | (__float_as_uint(other) & ~m));
+}
+#endif
+
 // What a run of rows sees of the chunk in blocks of B keys, from the keys of its first and last rows: the blocks that hold a key some row sees, numbered
 // 0 .. n_blocks - 1 in order (those of the sinks, then those of the windows), and which of them every row sees in full.
 template <int B> struct WinSpan {
@@ -170,6 +186,7 @@ inline bool hexi_win_fwd_large(const AttnGeom& g, int window, int n_sink)
 {
     if (g.d != 128) return false;
     const WinLoad load = hexi_win_row_load(g, window, n_sink);
+    if (load.share == 0.0) return false;
     const double large = load.share * ((g.lq + 255) / 256) * g.nq, small = load.share * ((g.lq + 63) / 64) * g.nq;
     const double t_large = ceil(large / 256.0) * (18.0 + 2.0 / 64.0 * (load.mean + 255 + 63));
     const double t_small = (small / 256.0 + 0.25) * (6.0 + 1.17 / 128.0 * (load.mean + 63 + 31));

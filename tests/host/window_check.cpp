@@ -1,6 +1,8 @@
 // Host-side check of the window geometry that the kernels use (csrc/hexi_window.h).  One command a line:
 //   window n_sink  q range  kv range   (ranges as read_segs reads them)
-// prints for every q row "sink:lo:hi", "|", then for every key "first:end".
+// prints for every q row "sink:lo:hi", "|", then for every key "first:end".  Or
+//   large nq nkv head_dim  window n_sink  q range  kv range
+// prints whether a bf16 forward call takes 256-row workgroups.
 #include <cstdio>
 #include <iostream>
 #include <sstream>
@@ -14,6 +16,17 @@ int main()
     while (std::getline(std::cin, line)) {
         std::istringstream is(line);
         int window, n_sink;
+        if (line.rfind("large", 0) == 0) {
+            std::string cmd;
+            AttnGeom g = {};
+            is >> cmd >> g.nq >> g.nkv >> g.d >> window >> n_sink;
+            g.qs = read_segs(is);
+            g.ks = read_segs(is);
+            g.lq = g.qs.total;
+            g.lc = g.ks.total;
+            std::printf("%d\n", (int)hexi_win_fwd_large(g, window, n_sink));
+            continue;
+        }
         is >> window >> n_sink;
         const SegTable qs = read_segs(is), ks = read_segs(is);
         for (int r = 0; r < qs.total; ++r) {

@@ -57,6 +57,59 @@ def test_forward(c, dtype, d):
         untouched(o_flat, l_flat)
 
 
+@pytest.mark.parametrize("c", wu.LARGE, ids=lambda c: c.name)
+def test_forward_in_256_row_workgroups(c):
+    x, dev, desc, window = setup(c, BF16, 128, 11)
+    heads = [0, 1, c.nq // 2, c.nq - 1]
+    sub = Case(c.name, c.q_segs, c.kv_segs, c.window, c.n_sink, len(heads), c.nkv, [h // (c.nq // c.nkv) for h in heads])
+    some = dict(x, q=x["q"][:, heads])
+    for out in (F32, BF16):
+        print(f"\n  {c.name} -> {out}", flush=True)
+        o_flat, o = guarded((c.lq, c.nq, 128), out, float("nan"))
+        l_flat, lse = guarded((c.nq, c.lq), F32, float("nan"))
+        hexi.hexi_attn_win_fwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], o, lse)
+        torch.cuda.synchronize()
+        ro, rl, bo, bl = wu.forward(sub, some, out)
+        wu.within("lse", lse[heads], rl, bl)
+        wu.within("o", o[:, heads], ro, bo, REL[BF16])
+        assert torch.isfinite(o.float()).all() and not lse.isnan().any()
+        untouched(o_flat, l_flat)
+    # merged into a running result
+    old = torch.randn(c.lq, c.nq, 128, generator=torch.Generator().manual_seed(5))
+    o, lse = old.to(DEV), torch.zeros(c.nq, c.lq, device=DEV)
+    hexi.hexi_attn_win_fwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], o, lse, flags=hexi.HEXI_ACCUMULATE)
+    ro, rl, bo, bl = wu.forward(sub, some, F32)
+    total = torch.logaddexp(rl, torch.zeros_like(rl))
+    w = torch.exp(rl - total).T[..., None]
+    old = old[:, heads].double()
+    # (a weight is off by the LSE's error, and the merge rounds a few times more)
+    wu.within("merged lse", lse[heads], total, bl.nan_to_num(0) + 8 * wu.U * (1 + total.abs()))
+    wu.within("merged o", o[:, heads], w * ro + (1 - w) * old, bo + (bl.T[..., None].nan_to_num(0) + 16 * wu.U) * (ro.abs() + old.abs()) + 1e-6)
+    # a value that is not finite
+    bad, at = x["v"].clone(), c.lc // 2
+    bad[at, :, 17] = float("nan")
+    hexi.hexi_attn_win_fwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], bad.to(DEV), o, lse)
+    ro = ro.clone()
+    ro[wu.visible(sub)[:, at], :, 17] = float("nan")
+    wu.within("o", o[:, heads], ro, bo)
+
+
+def test_forward_in_256_row_workgroups_with_drifting_scores():
+    """Scores that rise by far more than 2^60 along a row's keys: the workgroup's second pass with a running maximum."""
+    c = Case("drift", [(600, 512)], [(0, 1112)], 500, 40, nq=128, nkv=1)
+    x = wu.inputs(c, BF16, 128, 12)
+    x["k"] = (x["k"].float() * torch.linspace(0.1, 40, c.lc)[:, None, None]).to(BF16)
+    dev = {n: t.to(DEV) for n, t in x.items()}
+    desc, window = hexi.desc_for(dev["q"], dev["k"], 128 ** -0.5), hexi.make_window(c.window, c.n_sink)
+    o, lse = torch.empty(c.lq, c.nq, 128, device=DEV), torch.empty(c.nq, c.lq, device=DEV)
+    hexi.hexi_attn_win_fwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], o, lse)
+    heads = [0, 100]
+    sub = Case(c.name, c.q_segs, c.kv_segs, c.window, c.n_sink, 2, 1)
+    ro, rl, bo, bl = wu.forward(sub, dict(x, q=x["q"][:, heads]), F32)
+    wu.within("lse", lse[heads], rl, bl)
+    wu.within("o", o[:, heads], ro, bo, REL[BF16])
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("c", CASES, ids=lambda c: c.name)

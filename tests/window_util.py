@@ -68,6 +68,20 @@ CASES = [
     Case("long odd", [(2001, 431)], [(101, 2331)], 1901, 0, nq=2, nkv=2, k_scale=2.0),
 ]
 
+# Steps whose forward takes 256-row workgroups (128 heads of up to 512 rows: 256 of them): windows within a tile and over several, sinks, rows of two places in
+# one workgroup, rows that see nothing, a whole group of rows past the end, chunks whose first keys every row sees
+LARGE = [
+    Case("one", [(900, 511)], [(0, 3), (800, 611)], 1, 3, nq=128, nkv=2),
+    Case("short", [(900, 512)], [(0, 70), (800, 612)], 70, 64, nq=128, nkv=2),
+    Case("pair", [(300, 300), (5000, 201)], [(0, 130), (200, 400), (4600, 601)], 333, 128, nq=128, nkv=1),
+    Case("ring step", [(700, 512)], [(100, 600)], 800, 0, nq=128, nkv=4),
+    Case("odd", [(2000, 449)], [(900, 1549)], 1024, 0, nq=128, nkv=1, k_scale=3.0),
+    Case("rows without keys", [(50, 60), (3000, 452)], [(300, 2500)], 10 ** 6, 0, nq=128, nkv=1),
+    Case("group past the end", [(4000, 1380)], [(1001, 4379)], 3000, 0, nq=42, nkv=1),
+    Case("gap", [(100, 200), (9000, 290)], [(0, 300), (8500, 64), (8600, 690)], 700, 10, nq=128, nkv=128),
+    Case("everything", [(200, 500)], [(0, 640)], 10 ** 9, 0, nq=128, nkv=2),
+]
+
 
 def positions(segs):
     return torch.cat([torch.arange(s, s + n, dtype=torch.int64) for s, n in segs])
