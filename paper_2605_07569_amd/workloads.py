@@ -133,6 +133,27 @@ def contiguous_chunks(w: Workload, n_chunks: int) -> Workload:
     return replace(w, name=w.name + "_contig", chunks=[[(j * lc, lc)] for j in range(n_chunks)])
 
 
+def window_segs(q_segs: List[Seg], window: int, n_sink: int = 0) -> List[Seg]:
+    """The keys that a shard's rows see under a window with sinks: its own segments, the window - 1 keys before each, and the first n_sink."""
+    if not q_segs:
+        return []
+    last = q_segs[-1][0] + q_segs[-1][1]
+    runs = ([(0, min(n_sink, last))] if n_sink > 0 else []) + [(max(0, s - window + 1), s + n) for s, n in q_segs if n > 0]
+    out: List[Seg] = []
+    for lo, hi in runs:
+        if out and lo <= out[-1][0] + out[-1][1]:
+            lo0 = out[-1][0]
+            out[-1] = (lo0, max(hi, lo0 + out[-1][1]) - lo0)
+        else:
+            out.append((lo, hi - lo))
+    return out
+
+
+def windowed(w: Workload, window: int, n_sink: int = 0) -> Workload:
+    """The same shard under a window: one chunk of the keys that its rows see, in place of the ring."""
+    return replace(w, name=w.name + f"_win{window}", chunks=[window_segs(w.q_segs, window, n_sink)])
+
+
 VALUE_BLOCK = 1024     # tokens per independently seeded block of a synthetic tensor
 _M64 = (1 << 64) - 1
 

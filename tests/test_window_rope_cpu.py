@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import window_util as wu
-from paper_2605_07569_amd import hexi
+from paper_2605_07569_amd import hexi, workloads
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 INF = float("inf")
@@ -223,3 +223,15 @@ def test_binding_refuses_what_does_not_fit_before_the_library_is_asked():
     assert refused(P, rope, [(0, 4)], x, flat, [[0, 1]], [1, 1]) == E                            # on the CPU
     assert refused(P, rope, [(0, 4)], x, flat[1:], [[0, 1]], [1, 1]) == E and refused(P, rope, [(0, 4)], x, flat, [[0, 1]], [1]) == E
     assert refused(U, rope, [(0, 4)], flat.bfloat16(), x, [[0, 1]], [1, 1]) == E and refused(U, rope, [(0, 3)], flat, x, [[0, 1]], [1, 1]) == E
+
+
+@pytest.mark.parametrize("q_segs,window,n_sink", [([(0, 5)], 1, 0), ([(7, 3), (12, 1), (30, 4)], 3, 0), ([(7, 3), (12, 1), (30, 4)], 21, 2), ([(7, 3), (30, 4)], 10 ** 12, 0),
+                                                  ([(7, 3), (30, 4)], 5, 10 ** 12), ([(50, 3)], 10, 41), ([(50, 3)], 10, 42), ([(50, 3)], 10, 4), ([], 4, 4)])
+def test_window_segs_are_the_keys_that_rows_see(q_segs, window, n_sink):
+    rows = [p for s, n in q_segs for p in range(s, s + n)]
+    last = max(rows, default=-1)
+    need = {j for p in rows for j in range(p + 1) if p - j < window or j < n_sink}
+    segs = workloads.window_segs(q_segs, window, n_sink)
+    held = [j for s, n in segs for j in range(s, s + n)]
+    assert held == sorted(set(held)) and all(b[0] > a[0] + a[1] for a, b in zip(segs, segs[1:]))
+    assert set(held) == need and (not held or held[-1] == last)
