@@ -6,10 +6,9 @@
 //   a lane then has four keys of ONE vector, so softmax is four values and two exchanges;
 //   O^T[column][vector] = V^T P^T  P as it stands; V by rows, 4 g + e of the block, a piece of neighbouring columns a lane: what the four rows hold of a column is an
 //   operand (bf16: packed by v_perm_b32), so output row l of product c is column PIECE l + c.
-// What bounds it: a call of one row takes a trip to memory, its instructions' way into the cache (a first form without matrix instructions, unrolled to
-// 3100 instructions, took 12 us for any number of keys up to 64 a workgroup; fetching code costs about 25 ns per 64 bytes where every workgroup runs it once), a
-// launch and the join.
-// One row of 8/1 heads, 4100 keys: XX us and XX for the join; 64-row units in 32 splits 10.8, in one piece 34.5.
+// What bounds it: latency.  A call of one row is a launch, a read of its arguments (about half a microsecond), two trips to memory one behind the other, of K and V, and
+// the join of the splits.  One row of 8/1 heads of 128 columns, 4100 keys (2.1 MB: 0.4 us at a copy's rate): 5.0 us and a join of 3.2; 64-row units in 32 splits 10.8 and the
+// join, in one piece 34.5.
 #include "hexi_blocks.h"
 #include "hexi_f32_common.h"
 #include "hexi_window_plain.h"
@@ -18,8 +17,8 @@ namespace {
 
 constexpr int NV = 16, KEYS = 64, NW = 4;
 
-// What the kernel reads of its arguments, side by side and through scalar reads: they lie in host memory, where a first read of a line takes about a microsecond,
-// one behind the other where reads depend on each other, and a vector read of them three to seven.  So what the host can work out it does.
+// What the kernel reads of its arguments, side by side and through scalar reads: a first read of a line takes about half a microsecond, one behind the other where reads
+// depend on each other.  So what the host can work out it does.
 struct FewArgs {
     const void *q, *k, *v;
     float *o, *lse;                   // of split 0; the others' o_split and lse_split further

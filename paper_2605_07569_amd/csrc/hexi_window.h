@@ -124,8 +124,12 @@ struct WinRowSpan {
 
 // How a forward call is cut, by the descriptor, the window and the lengths alone, so that its workspace can be asked for without the ranges.
 struct WinFwdPlan { int few, n_splits; };
-// Few rows: XX.  Otherwise the units are split as far as fills the chip with workgroups, each left with a block for every wavefront at least, if that takes at
-// least eight steps off a unit (a step is 0.8 us, joining the results 5).
+// Few rows whose q heads share kv heads take workgroups of 16 query vectors (hexi_win_few.hip).  us, 64-row units (fp32: 16-row ones) / these, one row, 128 columns, bf16:
+// 8/1 heads, 4097 keys 12.0 / 9.2, 32/8 21.0 / 10.9, 64/8 and 32001 keys 162 / 30, 24/24 18.7 / 18.7, 128/128 and 501 keys 11.8 / 14.8; fp32: 32/8, 4097 keys 29.6 / 18.2, 24/24
+// 25.6 / 28.3.  Two workgroups a CU in all; one split for up to four blocks of keys (fp32: two), where a join takes more than it saves: 8/1 heads, in splits / in one, 100
+// keys 8.2 / 5.9, 255 8.3 / 7.9, 400 8.4 / 10.5; fp32 100 9.7 / 8.5, 190 10.0 / 10.5.
+// Otherwise the units are split as far as fills the chip with workgroups, each left with a block for every wavefront at least, if that takes at
+// least eight steps off a unit (a step is 0.8 us, joining the results 3 to 4).
 inline WinFwdPlan hexi_win_fwd_plan(int dtype, int nq, int nkv, long long lq, long long lc, long long window, long long n_sink)
 {
     auto keys_of = [&](long long rows) {
@@ -134,10 +138,10 @@ inline WinFwdPlan hexi_win_fwd_plan(int dtype, int nq, int nkv, long long lq, lo
         return keys < lc ? keys : lc;
     };
     WinFwdPlan plan = {0, 1};
-    if (lq <= HEXI_WIN_FEW_ROWS && lq * nq <= HEXI_WIN_FEW_VECTORS && lq * nq <= 32 * nkv) {
+    if (lq <= HEXI_WIN_FEW_ROWS && lq * nq <= HEXI_WIN_FEW_VECTORS && lq * nq <= 32 * nkv && nq >= 2 * nkv) {
         const long long groups = nkv * ((lq * nq + 16 * nkv - 1) / (16 * nkv)), blocks = (keys_of(lq) + 63) / 64;
         long long n = 512 / groups;
-        n = n < blocks ? n : blocks;
+        n = blocks <= (dtype == HEXI_BF16 ? 4 : 2) ? 1 : n < blocks ? n : blocks;
         plan.few = 1;
         plan.n_splits = n < 1 ? 1 : n < HEXI_WIN_MAX_SPLITS ? (int)n : HEXI_WIN_MAX_SPLITS;
         return plan;
