@@ -80,8 +80,12 @@ struct VisibleWin {
     __device__ __forceinline__ uint32_t bits(int r, int b, int hh) const { return win_bits(mine[r], b * TB) >> (4 * hh); }
 };
 
-// Not 0 (NaN) if some value is not finite.  A key that a row does not see has P = 0 there, and 0 x inf and 0 x NaN are NaN: a windowed unit whose sums are
-// not all finite starts again element by element, where such keys are left out instead of being given no weight.
+// Not 0 (NaN) if some value is not finite, or z is not.  A key that a row does not see has P = 0 there, and 0 x inf and 0 x NaN are NaN: a windowed unit whose sums
+// are not all finite starts again element by element, where such keys are left out instead of being given no weight.
+__device__ __forceinline__ float not_finite(const f32x4& x, float z)
+{
+    return fmaf(x[0], 0.f, fmaf(x[1], 0.f, fmaf(x[2], 0.f, fmaf(x[3], 0.f, z))));
+}
 template <int NDB> __device__ __forceinline__ float not_finite(const f32x16 (&acc)[2][NDB])
 {
     float z[2] = {0.f, 0.f};
@@ -1057,10 +1061,38 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
     acc_settled<C::NDB>(dk);
     acc_settled<C::NDB>(dv);
     if constexpr (WIN) {
-        if (__syncthreads_or(not_finite<C::NDB>(dk) + not_finite<C::NDB>(dv) != 0.f)) {
+        f32x4 sum[2][C::OUT_VECS];                         // of dV, of dK
+        float z = 0.f;
+        auto gather = [&](int which, const f32x16 (&acc)[2][C::NDB], float w) __attribute__((always_inline)) {
+            __syncthreads();
+            stage64<C>(sm.stage, acc, sp, l32, hh, w);
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < C::OUT_VECS; ++j) {
+                const int i = tid + 64 * NW * j;
+                sum[which][j] = staged_sum<C>(sm.stage, i / (D / 4), 4 * (i % (D / 4)));
+                z = not_finite(sum[which][j], z);
+            }
+        };
+        gather(0, dv, 1.0f);
+        gather(1, dk, g.scale);
+        if (__syncthreads_or(z != 0.f)) {
             win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0, ROWS);
             return;
         }
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int j = 0; j < C::OUT_VECS; ++j) {
+                const int i = tid + 64 * NW * j, r = col0 + i / (D / 4), c = 4 * (i % (D / 4));
+                if (r >= g.lc) continue;
+                float* out = which ? a.dk : a.dv;
+                const long long at = ((long long)r * g.nkv + kvh) * D + c;
+                f32x4 x = sum[which][j];
+                if (a.accumulate) x += *reinterpret_cast<const f32x4*>(out + at);
+                win_plain::store4(out, at, a.out_bf16, x[0], x[1], x[2], x[3]);
+            }
+        return;
     }
     auto write_out = [&](float* out, const f32x16 (&acc)[2][C::NDB], float w) {
         __syncthreads();
@@ -1089,8 +1121,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
                 const long long at = ((long long)r * g.nkv + kvh) * D + c;
                 f32x4* op = reinterpret_cast<f32x4*>(out + at);
                 if (a.accumulate) x[j] += *op;
-                if constexpr (WIN) win_plain::store4(out, at, a.out_bf16, x[j][0], x[j][1], x[j][2], x[j][3]);
-                else *op = x[j];
+                *op = x[j];
             }
         }
     };

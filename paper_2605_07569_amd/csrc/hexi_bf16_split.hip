@@ -17,7 +17,9 @@
 // Operand layouts are those of the large kernels (hexi_mfma.h): scores transposed in the forward and dQ kernels (a lane
 // owns a q row), keys across the lanes in the dK/dV kernel; accumulator registers go straight back in as operands, the
 // other operand through transposed LDS reads.
+#include <type_traits>
 #include "hexi_blocks.h"
+#include "hexi_window_plain.h"
 
 namespace {
 
@@ -76,6 +78,40 @@ struct Visible {
         mine = row0 + l32 < g.lq ? n : 0;
     }
 };
+
+// The same under a window (WIN): the keys of the lane's row (none for padding rows) and the run of blocks of all of them.
+struct VisibleWin {
+    WinKeys mine;
+    WinSpan<TB> span;
+    __device__ __forceinline__ VisibleWin(const WinBwdArgs& a, int row0, int l32)
+    {
+        const AttnGeom& g = a.g;
+        const int p = pos_of_row(g.qs, row0 + l32 < g.lq ? row0 + l32 : g.lq - 1);
+        const int hi = rows_le(g.ks, p), s = rows_le(g.ks, a.n_sink - 1), lo = p < a.window ? 0 : rows_le(g.ks, p - a.window);
+        mine = s < lo ? WinKeys{s, lo, hi} : WinKeys{0, 0, hi};
+        span = WinSpan<TB>(of_lane(0), of_lane(31), g.lc);
+        if (row0 + l32 >= g.lq) mine = WinKeys{0, 0, 0};
+    }
+    __device__ __forceinline__ WinKeys of_lane(int lane) const
+    {
+        return {__builtin_amdgcn_readlane(mine.sink, lane), __builtin_amdgcn_readlane(mine.lo, lane), __builtin_amdgcn_readlane(mine.hi, lane)};
+    }
+};
+
+// Word I of an operand, masked.
+template <int I> __device__ __forceinline__ void and_word(bf16x8& x, uint32_t mask)
+{
+    f32x4 w = __builtin_bit_cast(f32x4, x);
+    w[I] = __uint_as_float(__float_as_uint(w[I]) & mask);
+    x = __builtin_bit_cast(bf16x8, w);
+}
+
+// z, and not 0 (NaN) if some value is not finite.  A key that a row does not see has P = 0 there, and 0 x inf and 0 x NaN are NaN: a windowed unit whose sums are
+// not all finite starts again element by element, where such keys are left out.
+__device__ __forceinline__ float not_finite(const f32x4& x, float z)
+{
+    return fmaf(x[0], 0.f, fmaf(x[1], 0.f, fmaf(x[2], 0.f, fmaf(x[3], 0.f, z))));
+}
 
 // A transposed accumulator (lane = stationary row) as rows of the wavefront's staging area, times w.
 template <class C> __device__ __forceinline__ void stage_transposed(float* stage, const f32x16 (&acc)[C::NDB], int l32, int hh, float w)
@@ -267,8 +303,8 @@ template <class C> union DqSmem {
     float stage[C::STAGE_FLOATS];
 };
 
-template <int D>
-__device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int q_tile, DqSmem<SplitCfg<D>>& sm)
+template <int D, bool WIN>
+__device__ __forceinline__ void dq_unit(const BwdArgsOf<WIN>& a, const int h, const int q_tile, DqSmem<SplitCfg<D>>& sm)
 {
     using C = SplitCfg<D>;
     const AttnGeom& g = a.g;
@@ -289,13 +325,19 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
     const BlockFetch<C> fetch(lane, g.kv_stride_tok);
     auto fetch_k = [&](int b) { fetch.issue(k, g.kv_stride_tok, b * TB, g.lc, lds); };
     auto fetch_v = [&](int b) { fetch.issue(v, g.kv_stride_tok, b * TB, g.lc, lds + C::TILE_BYTES); };
-    const bool asked = sp * TB < g.lc;
-    if (asked) { fetch_v(sp); fetch_k(sp); }
-    const Visible vis(g, row0, l32);
-    const int n_blocks = (vis.n_all + TB - 1) / TB;
-    if (n_blocks == 0) {                                   // dq_acc unchanged
+    bool asked = sp * TB < g.lc;
+    if (!WIN && asked) { fetch_v(sp); fetch_k(sp); }
+    const std::conditional_t<WIN, VisibleWin, Visible> vis = [&]() { if constexpr (WIN) return VisibleWin(a, row0, l32); else return Visible(g, row0, l32); }();
+    auto block = [&](int b) { if constexpr (WIN) return vis.span.block(b); else return b; };      // of the chunk, from the number in this unit's run
+    const int n_blocks = [&]() { if constexpr (WIN) return vis.span.n_blocks; else return (vis.n_all + TB - 1) / TB; }();
+    const bool writes_anyway = [&]() { if constexpr (WIN) return a.out_bf16 != 0; else return false; }();
+    if (n_blocks == 0 && !writes_anyway) {                 // dq_acc unchanged
         wait_transfers<0>();
         return;
+    }
+    if constexpr (WIN) {
+        asked = sp < n_blocks;
+        if (asked) { fetch_v(block(sp)); fetch_k(block(sp)); }
     }
     const LaneAddr<C> la(lane, lds);
     const float c_log2 = g.scale * LOG2E;
@@ -320,7 +362,14 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(s[r], c_log2, neg_l)) * (dp[r] - delta);
-        if (b >= vis.n_full) {
+        if constexpr (WIN) {
+            if (!vis.span.full(b)) {
+                keep_branch();
+                const uint32_t seen = win_bits(vis.mine, b * TB) >> (4 * hh);
+                auto one = [&](auto ic) __attribute__((always_inline)) { constexpr int i = decltype(ic)::value; ds[i] = win_or<8 * (i >> 2) + (i & 3)>(seen, ds[i], 0.f); };
+                for_range<0, 16>(one);
+            }
+        } else if (b >= vis.n_full) {
             keep_branch();
             const int n = vis.mine - b * TB - 4 * hh;
 #pragma unroll
@@ -359,22 +408,43 @@ __device__ __forceinline__ void dq_unit(const BwdArgs& a, const int h, const int
         const f32x16 dp = row_product<C>(la, C::TILE_BYTES, [&](int ks) { return gf[ks]; });
         reads_done();
         wait_transfers<0>();
-        if (more) fetch_v(b + NW);
+        if (more) fetch_v(block(b + NW));
         const f32x16 s = row_product<C>(la, 0, [&](int ks) { return qf[ks]; });
-        accumulate(s, dp, b);
+        accumulate(s, dp, block(b));
         reads_done();
-        if (more) fetch_k(b + NW);
+        if (more) fetch_k(block(b + NW));
     }
     wait_transfers<0>();                                   // (a first block that no row sees)
     f32x4 old[C::OUT_VECS];
 #pragma unroll
     for (int j = 0; j < C::OUT_VECS; ++j) {                // (rows past the end read the last one)
         const int i = tid + 64 * NW * j, r = row0 + i / (D / 4), c = 4 * (i % (D / 4));
-        old[j] = *reinterpret_cast<const f32x4*>(a.dq + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
+        if (writes_anyway) old[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        else old[j] = *reinterpret_cast<const f32x4*>(a.dq + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
     }
     __syncthreads();
     stage_transposed<C>(&sm.stage[sp * TB * C::PITCH], dq, l32, hh, g.scale);
     __syncthreads();
+    if constexpr (WIN) {
+        float z = 0.f;
+#pragma unroll
+        for (int j = 0; j < C::OUT_VECS; ++j) {
+            const int i = tid + 64 * NW * j, r = i / (D / 4);
+            const f32x4 x = staged_sum<C>(sm.stage, r, 4 * (i % (D / 4)));
+            if (row0 + r < g.lq) z = not_finite(x, z);
+            old[j] += x;
+        }
+        if (__syncthreads_or(z != 0.f)) {
+            win_plain::dq_unit<uint16_t, D>(a, h, row0, TB);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < C::OUT_VECS; ++j) {
+            const int i = tid + 64 * NW * j, r = i / (D / 4), c = 4 * (i % (D / 4));
+            if (row0 + r < g.lq) win_plain::store4(a.dq, ((long long)(row0 + r) * g.nq + h) * D + c, a.out_bf16, old[j][0], old[j][1], old[j][2], old[j][3]);
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < C::OUT_VECS; ++j) {
         const int i = tid + 64 * NW * j, r = i / (D / 4), c = 4 * (i % (D / 4));
@@ -394,8 +464,8 @@ template <class C> union DkdvSmem {
     float stage[C::STAGE_FLOATS];
 };
 
-template <int D, bool ATOMIC_DKV>
-__device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs, const int run, const int kv_tile, DkdvSmem<SplitCfg<D>>& sm)
+template <int D, bool ATOMIC_DKV, bool WIN>
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, DkdvSmem<SplitCfg<D>>& sm)
 {
     using C = SplitCfg<D>;
     const AttnGeom& g = a.g;
@@ -404,7 +474,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
     const int l32 = lane & 31, hh = lane >> 5;
     const int col0 = kv_tile * TB;
     const int n_heads = arg_byte(runs.len, run);
-    const int kvh = arg_byte(g.kv_of_q, arg_byte(runs.first, run));
+    const int kvh = WIN ? run : arg_byte(g.kv_of_q, arg_byte(runs.first, run));      // (under a window there is a run to every kv head, an empty one where no q head reads it)
     const int my_col = col0 + l32;
     // the rows that see a key are a suffix of the shard: [my_first, lq); no row before row_first sees any of the keys,
     // all rows from row_full on see all of them
@@ -413,7 +483,19 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
     const int row_first = __builtin_amdgcn_readlane(first, 0);
     const int row_full = col0 + TB <= g.lc ? __builtin_amdgcn_readlane(first, TB - 1) : 0x7fffffff;
     const int blk0 = row_first / TB;
-    const int n_all = row_first < g.lq ? (g.lq + TB - 1) / TB - blk0 : 0;      // blocks of one head
+    // Under a window the rows that see a key end too: of the lane's key at my_end.  Ends ascend with the keys, but for sinks, which all later rows see: they come first.
+    int my_end = 0, row_end = g.lq, row_full_end = g.lq;      // no row from row_end on sees any of the keys, rows before row_full_end see all (from row_full on)
+    if constexpr (WIN) {
+        const int p = pos_of_row(g.ks, my_col < g.lc ? my_col : g.lc - 1);
+        const unsigned last = (unsigned)p + (unsigned)(a.window - 1);
+        const int end = p < a.n_sink || last > 0x7ffffffeu ? g.lq : rows_le(g.qs, (int)last);
+        my_end = my_col < g.lc ? end : 0;
+        const int e0 = __builtin_amdgcn_readlane(end, 0), e1 = __builtin_amdgcn_readlane(end, TB - 1);
+        const bool sinks = __builtin_amdgcn_readfirstlane(p) < a.n_sink, all_sinks = __builtin_amdgcn_readlane(p, TB - 1) < a.n_sink;
+        row_end = sinks ? g.lq : e1;
+        row_full_end = all_sinks ? g.lq : sinks ? 0 : e0;      // (a unit of both kinds is masked throughout)
+    }
+    const int n_all = row_first < row_end ? (row_end + TB - 1) / TB - blk0 : 0;      // blocks of one head
 
     const uint32_t lds_all = (uint32_t)(uintptr_t)(&sm.m.t[0][0]);
     const uint32_t lds = lds_all + wave * 2 * C::TILE_BYTES;
@@ -472,7 +554,9 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
         const f32x16 dp = row_product<C>(la, C::TILE_BYTES, v_frag);
         wait_transfers<0>();
         const f32x16 s = row_product<C>(la, 0, k_frag);
-        const bool masked = row < row_full || row + TB > g.lq;
+        // rows whose LSE is -inf (it is exact about them: P would be infinite) are masked wherever they are
+        const uint32_t dead = WIN ? (uint32_t)__builtin_amdgcn_ballot_w64(sm.m.lse[wave][l32] == -INFINITY) : 0u;
+        const bool masked = row < row_full || row + TB > (WIN ? row_full_end : g.lq) || dead != 0u;
         bf16x8 pf[2], df[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -484,7 +568,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
                 const f32x4 d4 = *reinterpret_cast<const f32x4*>(&sm.m.delta[wave][r0]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[4 * rb + e] = fast_exp2(fmaf(s[8 * u + 4 * rb + e], scale_log2, l4[e] * -LOG2E));
-                if (masked) {      // (a row that sees nothing anywhere, LSE = -inf, is masked in every block)
+                if (!WIN && masked) {      // (a row that sees nothing anywhere, LSE = -inf, is masked in every block)
                     keep_branch();
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -496,6 +580,17 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
             pf[u] = pack_bf16x8(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
             df[u] = pack_bf16x8(ds[0], ds[1], ds[2], ds[3], ds[4], ds[5], ds[6], ds[7]);
         }
+        if (WIN && masked) {
+            keep_branch();
+            const uint32_t seen = (win_bits(my_first, my_end, row) & ~dead) >> (4 * hh);
+            auto two = [&](auto ic) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value, o = 8 * (i >> 1) + 2 * (i & 1);
+                const uint32_t keep = (win_bit<o>(seen) & 0xffffu) | (win_bit<o + 1>(seen) & 0xffff0000u);
+                and_word<(i & 3)>(pf[i >> 2], keep);
+                and_word<(i & 3)>(df[i >> 2], keep);
+            };
+            for_range<0, 8>(two);
+        }
         col_product<C>(dv, la, C::TILE_BYTES, pf);
         reads_done();
         if (more) fetch_g(h, next_row);
@@ -504,6 +599,40 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
         if (more) fetch_q(h, next_row);
     }
 
+    if constexpr (WIN) {
+        f32x4 sum[2][C::OUT_VECS];                         // of dV, of dK
+        float z = 0.f;
+        auto gather = [&](int which, const f32x16 (&acc)[C::NDB], float w) __attribute__((always_inline)) {
+            __syncthreads();
+            stage_transposed<C>(&sm.stage[wave * TB * C::PITCH], acc, l32, hh, w);
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < C::OUT_VECS; ++j) {
+                const int i = tid + 64 * NW * j;
+                sum[which][j] = staged_sum<C>(sm.stage, i / (D / 4), 4 * (i % (D / 4)));
+                z = not_finite(sum[which][j], z);
+            }
+        };
+        gather(0, dv, 1.0f);
+        gather(1, dk, g.scale);
+        if (__syncthreads_or(z != 0.f)) {
+            win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0, TB);
+            return;
+        }
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+#pragma unroll
+            for (int j = 0; j < C::OUT_VECS; ++j) {
+                const int i = tid + 64 * NW * j, r = col0 + i / (D / 4), c = 4 * (i % (D / 4));
+                if (r >= g.lc) continue;
+                float* out = which ? a.dk : a.dv;
+                const long long at = ((long long)r * g.nkv + kvh) * D + c;
+                f32x4 x = sum[which][j];
+                if (a.accumulate) x += *reinterpret_cast<const f32x4*>(out + at);
+                win_plain::store4(out, at, a.out_bf16, x[0], x[1], x[2], x[3]);
+            }
+        return;
+    }
     auto write_out = [&](float* out, const f32x16 (&acc)[C::NDB], float w) {
         __syncthreads();
         stage_transposed<C>(&sm.stage[wave * TB * C::PITCH], acc, l32, hh, w);
@@ -535,17 +664,17 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgs& a, const HeadRuns& runs
 
 // One launch for both halves of a backward step: workgroups [0, n_dkdv) are dK / dV units (the longer ones, first), the
 // others dQ units.  Within each, heads (runs) side by side and the longest tiles first.
-template <int D, bool ATOMIC_DKV>
-__global__ void __launch_bounds__(512) bwd_split_bf16_kernel(const BwdArgs a, const HeadRuns runs, const unsigned n_dkdv, const int n_q_tiles)
+template <int D, bool ATOMIC_DKV, bool WIN>
+__global__ void __launch_bounds__(512) bwd_split_bf16_kernel(const BwdArgsOf<WIN> a, const HeadRuns runs, const unsigned n_dkdv, const int n_q_tiles)
 {
     __shared__ __attribute__((aligned(1024))) union { DkdvSmem<SplitCfg<D>> dkdv; DqSmem<SplitCfg<D>> dq; } sm;
     if (blockIdx.x < n_dkdv) {
         const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
-        dkdv_unit<D, ATOMIC_DKV>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
+        dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
     } else {
         const unsigned unit = blockIdx.x - n_dkdv;
         const int tile = uniform((int)(unit / (unsigned)a.g.nq));
-        dq_unit<D>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
+        dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
     }
 }
 
@@ -571,11 +700,23 @@ hipError_t hexi_launch_bwd_split_bf16(const BwdArgs& a, bool dq, const HeadRuns&
     const unsigned grid = n_dkdv + (unsigned)n_q_tiles * (unsigned)a.g.nq;
     if (grid == 0) return hipSuccess;
     if (a.g.d == 128) {
-        if (shared) bwd_split_bf16_kernel<128, true><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
-        else bwd_split_bf16_kernel<128, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        if (shared) bwd_split_bf16_kernel<128, true, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        else bwd_split_bf16_kernel<128, false, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     } else if (a.g.d == 64) {
-        if (shared) bwd_split_bf16_kernel<64, true><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
-        else bwd_split_bf16_kernel<64, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        if (shared) bwd_split_bf16_kernel<64, true, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+        else bwd_split_bf16_kernel<64, false, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     } else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+hipError_t hexi_launch_win_bwd_split_bf16(const WinBwdArgs& a, hipStream_t s)
+{
+    const int n_q_tiles = a.want_dq ? (a.g.lq + TB - 1) / TB : 0;
+    HeadRuns runs;
+    hexi_head_run_of_each_kv(a.g.kv_of_q, a.g.nq, a.g.nkv, &runs);
+    const unsigned n_dkdv = a.want_dkdv ? (unsigned)((a.g.lc + TB - 1) / TB) * (unsigned)a.g.nkv : 0u;
+    const unsigned grid = n_dkdv + (unsigned)n_q_tiles * (unsigned)a.g.nq;
+    if (a.g.d == 128) bwd_split_bf16_kernel<128, false, true><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
+    else bwd_split_bf16_kernel<64, false, true><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     return hipGetLastError();
 }

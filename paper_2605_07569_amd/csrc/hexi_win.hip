@@ -64,7 +64,8 @@ hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s)
 {
-    if (dtype == HEXI_BF16) return hexi_launch_win_bwd_quad_bf16(a, s);
+    if (dtype == HEXI_BF16)
+        return hexi_win_bwd_split(a.g, a.window, a.n_sink, a.want_dq, a.want_dkdv) ? hexi_launch_win_bwd_split_bf16(a, s) : hexi_launch_win_bwd_quad_bf16(a, s);
     const AttnGeom& g = a.g;
     auto launch = [&](bool split, bool dkdv, bool dq) {
         return with_cfg(g.d, split, [&](auto cfg) {

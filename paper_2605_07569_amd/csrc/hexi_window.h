@@ -197,6 +197,26 @@ inline bool hexi_win_fwd_large(const AttnGeom& g, int window, int n_sink)
     return t_large < 0.97 * t_small;
 }
 
+// Whether a bf16 backward call takes 32-row (32-key) workgroups of eight wavefronts, or 64-row ones of four.  Fitted to 900 random calls (half within 6 %), us: a base, a unit's
+// fixed part and its steps of 256 (128) streamed rows, and the longer of the longest unit and all units' share of 256 CUs with a part of the longest one.  The choice is on
+// average 0.7 % slower than the better one.  64 rows / 32 rows, backward of all three, window 296, 4/4 heads of 241 rows 14.0 / 9.0 (128 columns), 850, 8/2 of 193 22.1 / 13.3, 1469,
+// 12/3 of 1505 85.8 / 82.4, 404, 8/1 of 7646 91 / 108; 64 columns, 163, 8/1 of 1863 27 / 16, 27, 12/3 of 3862 29 / 36.
+inline bool hexi_win_bwd_split(const AttnGeom& g, int window, int n_sink, bool dq, bool dkdv)
+{
+    struct Fit { double base, q_fixed, q_step, k_fixed, k_step, rest; };
+    static const Fit fits[2][2] = {{{1.1, 5.6, 0.75, 6.4, 1.07, 0.33}, {1.3, 3.7, 0.84, 4.7, 1.17, 0.36}}, {{0.3, 8.5, 1.14, 9.4, 1.67, 0.40}, {1.0, 4.8, 1.34, 6.3, 1.92, 0.43}}};
+    const WinLoad keys = hexi_win_row_load(g, window, n_sink), rows = hexi_win_key_load(g, window, n_sink);
+    auto us = [&](int split) {
+        const Fit& f = fits[g.d == 128][split];
+        const int n = split ? 32 : 64, step = split ? 256 : 128;
+        const double q = f.q_fixed + f.q_step * (keys.mean + n + 30) / step, k = f.k_fixed + f.k_step * (rows.mean + n + 30) * g.nq / g.nkv / step;
+        const double sum = (dq ? keys.share * ((g.lq + n - 1) / n) * g.nq * q : 0.0) + (dkdv ? rows.share * ((g.lc + n - 1) / n) * g.nkv * k : 0.0);
+        const double longest = dq && (!dkdv || q > k) ? q : k, even = sum / 256.0 + f.rest * longest;
+        return f.base + (longest > even ? longest : even);
+    };
+    return us(1) < us(0);
+}
+
 // Whether the fp32 units of a windowed call take 16 rows (or keys), streamed rows split over eight wavefronts, or 64 that share tiles: PART 0 forward, 1 dQ, 2 dK/dV.
 // Fitted to 190 random calls (90 % within 15 %), us: a base, and for every round of 256 workgroups a fixed part and a step, 32 streamed rows in the 64-row shape and 128 in
 // the other; more 64-row units than CUs share one and take at least 1.6 rounds at head_dim 128.  The choice is on average under 1 % slower than the better one.  64 rows / 16 rows:
@@ -244,6 +264,7 @@ hipError_t hexi_launch_win_join(const WinFwdArgs& a, hipStream_t s);
 hipError_t hexi_launch_win_fwd_large_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_fwd.hip: 256-row workgroups
 hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_quad_win.hip
 hipError_t hexi_launch_win_bwd_quad_bf16(const WinBwdArgs& a, hipStream_t s);
+hipError_t hexi_launch_win_bwd_split_bf16(const WinBwdArgs& a, hipStream_t s);      // in hexi_bf16_split.hip
 // Delta = rowsum(dO o) of a bf16 o
 hipError_t hexi_launch_delta_bf16_o(long long lq, int nq, int d, const void* o, const void* d_o, int dtype,
                                     long long stride_tok, long long stride_head, float* delta, hipStream_t s);

@@ -154,6 +154,61 @@ def _rel_of(pair, rel):
     return rel if float(bound.norm()) < 0.05 * float(want.norm()) else None
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("c", wu.MANY, ids=lambda c: c.name)
+def test_backward_in_64_row_workgroups(c, d):
+    """All heads at once, two kv heads looked at; rows whose LSE is infinite, and then a value that is not finite in one of each input."""
+    x, dev, desc, window = setup(c, BF16, d, 13)
+    group, kv = c.nq // c.nkv, [0, 33]
+    heads = [h * group + i for h in kv for i in range(group)]
+    sub = Case(c.name, c.q_segs, c.kv_segs, c.window, c.n_sink, len(heads), len(kv))
+    some = dict(q=x["q"][:, heads], k=x["k"][:, kv], v=x["v"][:, kv], d_o=x["d_o"][:, heads])
+    ro, rl, _, _ = wu.forward(sub, some, F32)
+    lse = rl.float()
+    lse[0, c.lq // 2], lse[1, c.lq - 1], lse[2, 3] = float("-inf"), float("inf"), float("-inf")
+    all_o, all_lse = torch.zeros(c.lq, c.nq, d), torch.zeros(c.nq, c.lq)
+    all_lse += 20.0
+    all_o[:, heads], all_lse[heads] = ro.float(), lse
+    seen = wu.visible(c)
+
+    def run(grad, inputs):
+        dq0 = 0.5 if grad == F32 else float("nan")
+        f1, dq = guarded((c.lq, c.nq, d), grad, dq0)
+        f2, dk = guarded((c.lc, c.nkv, d), grad, float("nan"))
+        f3, dv = guarded((c.lc, c.nkv, d), grad, float("nan"))
+        delta = torch.empty(c.nq, c.lq, device=DEV)
+        hexi.hexi_attn_win_bwd_chunk(desc, window, c.q_segs, c.kv_segs, inputs["q"], inputs["k"], inputs["v"], all_o.to(grad).to(DEV), inputs["d_o"], all_lse.to(DEV), delta,
+                                     dq, dk, dv, flags=hexi.HEXI_COMPUTE_DELTA)
+        torch.cuda.synchronize()
+        untouched(f1, f2, f3)
+        return dict(dq=dq[:, heads].float().cpu() - (0.5 if grad == F32 else 0.0), dk=dk[:, kv].cpu(), dv=dv[:, kv].cpu()), dq, dk, dv
+
+    for grad in (F32, BF16):
+        print(f"\n  {c.name}: d={d} -> {grad}", flush=True)
+        ref = wu.backward(sub, some, ro.float().to(grad), lse, grad)
+        got, *whole = run(grad, dev)
+        # (0.5 was added to and taken from dq again: 2^-23)
+        for name in ("dq", "dk", "dv"):
+            wu.within(name, got[name], ref[name][0], ref[name][1] + (2.0 ** -22 if name == "dq" else 0.0), REL[BF16])
+        assert all(torch.isfinite(t.float()).all() for t in whole)
+    ref = wu.backward(sub, some, ro.float(), lse, F32)
+    for where, at, head in (("k", c.lc // 2, 33), ("v", c.lc - 1, 0), ("q", c.lq // 3, 67), ("d_o", c.lq - 2, 0)):
+        bad = x[where].clone()
+        bad[at, head, 5] = float("nan")
+        got, *_ = run(F32, dict(dev, **{where: wu.strided(bad, c.pad, DEV)}))
+        if where in ("k", "v"):
+            rows, keys = seen[:, at], torch.arange(c.lc) == at
+            of_q, of_kv = [h // group == head for h in heads], [h == head for h in kv]
+        else:
+            rows, keys = torch.arange(c.lq) == at, seen[at]
+            of_q, of_kv = [h == head for h in heads], [h == head // group for h in kv]
+        hit = {"dq": rows[:, None] & torch.tensor(of_q), "dk": keys[:, None] & torch.tensor(of_kv)}
+        hit["dv"] = hit["dk"]
+        for name in ("dq", "dk", "dv"):
+            keep = ~hit[name]
+            wu.within(f"{name} of the others", got[name][keep], ref[name][0][keep], ref[name][1][keep] + (2.0 ** -22 if name == "dq" else 0.0))
+
+
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
 def test_accumulation_over_chunks_is_the_whole(dtype, d):
     """Keys in three uneven chunks, forward and backward, against one call over all of them."""

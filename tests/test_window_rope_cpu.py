@@ -61,12 +61,15 @@ def test_window_geometry_is_the_definition(window_binary):
             assert torch.equal(col, want), (c, item)
 
 
-def test_which_forward_steps_take_256_row_workgroups(window_binary):
+def test_which_workgroups_the_steps_take(window_binary):
+    """The GPU tests' steps, that every shape is among them."""
     text = lambda segs: f"{len(segs)} " + " ".join(f"{s} {n}" for s, n in segs)
     ask = lambda cases, d: subprocess.run([window_binary], input="\n".join(f"large {c.nq} {c.nkv} {d} {min(c.window, 2 ** 31 - 1)} {min(c.n_sink, 2 ** 31 - 1)} {text(c.q_segs)} {text(c.kv_segs)}"
                                                                            for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split()
-    assert ask(wu.LARGE, 128) == ["1"] * len(wu.LARGE) and ask(wu.LARGE, 64) == ["0"] * len(wu.LARGE)
-    assert ask(wu.CASES, 128) == ["0"] * len(wu.CASES)
+    assert [x[0] for x in ask(wu.LARGE, 128)] == ["1"] * len(wu.LARGE) and [x[0] for x in ask(wu.LARGE, 64)] == ["0"] * len(wu.LARGE)
+    for d in (64, 128):
+        assert ask(wu.CASES, d) == ["01"] * len(wu.CASES)
+        assert [x[1] for x in ask(wu.MANY, d)] == ["0"] * len(wu.MANY)
 
 
 def _codes(call, good, bad):

@@ -6,7 +6,7 @@ subtracted from it before the exponential (a row's LSE here: the reference of th
 and the sums' own roundings are counted as 2^-20 and n u relative.  E_ij: what that makes of P_ij, relative.  P and dS are rounded to
 bf16 as operands (h each, the sum that normalises o is that of the rounded P: at most h (sum w |v| + |o|)), results to the
 type they are asked for in (h or u)."""
-from dataclasses import dataclass, field
+from dataclasses import dataclass, field, replace
 from typing import List, Optional
 
 import torch
@@ -84,6 +84,9 @@ LARGE = [
     Case("gap", [(100, 200), (9000, 290)], [(0, 300), (8500, 64), (8600, 690)], 700, 10, nq=128, nkv=128),
     Case("everything", [(200, 500)], [(0, 640)], 10 ** 9, 0, nq=128, nkv=2),
 ]
+
+# The same steps with two q heads to a kv head: their backward takes 64-row workgroups, that of CASES 32-row ones.
+MANY = [replace(c, nq=128, nkv=64) for c in LARGE]
 
 
 def positions(segs):
