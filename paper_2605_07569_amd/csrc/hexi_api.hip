@@ -265,8 +265,8 @@ static int build_window(const hexi_window* w, int* window, int* n_sink)
 static WinFwdPlan win_fwd_plan(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
 {
     if (!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || d->n_kv_heads < 1 ||
-        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || w->window < 1 || w->n_sink < 0) return {0, 1};
-    return hexi_win_fwd_plan(d->dtype, d->n_q_heads, d->n_kv_heads, lq, lc, w->window, w->n_sink);
+        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || w->window < 1 || w->n_sink < 0) return {0, 1, 0};
+    return hexi_win_fwd_plan(d->dtype, d->head_dim, d->n_q_heads, d->n_kv_heads, lq, lc, w->window, w->n_sink);
 }
 
 HEXI_EXPORT size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc)
@@ -295,6 +295,7 @@ HEXI_EXPORT int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_w
     a.out_bf16 = o_dtype == HEXI_BF16;
     const WinFwdPlan plan = win_fwd_plan(desc, window, a.g.lq, a.g.lc);
     a.few = plan.few;
+    a.rows32 = plan.rows32;
     a.n_splits = plan.n_splits;
     a.part_o = a.part_lse = nullptr;
     if (a.n_splits > 1) {

@@ -83,7 +83,7 @@ struct Visible {
 struct VisibleWin {
     WinKeys mine;
     WinSpan<TB> span;
-    __device__ __forceinline__ VisibleWin(const WinBwdArgs& a, int row0, int l32)
+    template <class A> __device__ __forceinline__ VisibleWin(const A& a, int row0, int l32)
     {
         const AttnGeom& g = a.g;
         const int p = pos_of_row(g.qs, row0 + l32 < g.lq ? row0 + l32 : g.lq - 1);
@@ -134,8 +134,8 @@ template <class C> __device__ __forceinline__ f32x4 staged_sum(const float* stag
 }
 
 // (at head_dim 64 two workgroups fit a CU if the registers are held to 128)
-template <int D>
-__global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(const FwdArgs a, const int n_q_tiles)
+template <int D, bool WIN>
+__global__ void __launch_bounds__(512, D == 64 && !WIN ? 4 : 2) fwd_split_bf16_kernel(const FwdArgsOf<WIN> a, const int n_q_tiles)
 {
     using C = SplitCfg<D>;
     const AttnGeom& g = a.g;
@@ -149,8 +149,9 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
     const int l32 = lane & 31, hh = lane >> 5;
 
     // heads of a q tile side by side, the longest (last) q tiles first
-    const int h = blockIdx.x;
-    const int row0 = (n_q_tiles - 1 - (int)blockIdx.y) * TB;
+    const int h = WIN ? uniform((int)(blockIdx.x % (unsigned)g.nq)) : (int)blockIdx.x;
+    const int row0 = (n_q_tiles - 1 - (WIN ? uniform((int)(blockIdx.x / (unsigned)g.nq)) : (int)blockIdx.y)) * TB;
+    const int split = WIN ? (int)blockIdx.y : 0;           // (a wavefront takes every eighth block of the split's part of the run)
     const int kvh = arg_byte(g.kv_of_q, h);
     const uint16_t* k = static_cast<const uint16_t*>(a.k) + (long long)kvh * g.kv_stride_head;
     const uint16_t* v = static_cast<const uint16_t*>(a.v) + (long long)kvh * g.kv_stride_head;
@@ -161,13 +162,22 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
     auto fetch_v = [&](int b) { fetch.issue(v, g.kv_stride_tok, b * TB, g.lc, lds + C::TILE_BYTES); };
 
     // the first block is asked for before it is known that some row sees it
-    const bool asked = sp * TB < g.lc;
-    if (asked) { fetch_k(sp); fetch_v(sp); }
-    const Visible vis(g, row0, l32);
-    const int n_blocks = (vis.n_all + TB - 1) / TB;
-    if (n_blocks == 0 && a.accumulate) {                   // merging an empty partial is the identity
+    bool asked = sp * TB < g.lc;
+    if (!WIN && asked) { fetch_k(sp); fetch_v(sp); }
+    const std::conditional_t<WIN, VisibleWin, Visible> vis = [&]() { if constexpr (WIN) return VisibleWin(a, row0, l32); else return Visible(g, row0, l32); }();
+    auto block = [&](int b) { if constexpr (WIN) return vis.span.block(b); else return b; };      // of the chunk, from the number in this unit's run
+    const int b_first = [&]() { if constexpr (WIN) return vis.span.split_start(split, a.n_splits); else return 0; }();
+    const int n_blocks = [&]() { if constexpr (WIN) return vis.span.split_start(split + 1, a.n_splits); else return (vis.n_all + TB - 1) / TB; }();
+    const int b_mine = b_first + sp;                       // this wavefront's first block
+    int merges = a.accumulate;
+    if constexpr (WIN) merges = a.merges();
+    if (n_blocks == b_first && merges) {                   // merging an empty partial is the identity
         wait_transfers<0>();
         return;
+    }
+    if constexpr (WIN) {
+        asked = b_mine < n_blocks;
+        if (asked) { fetch_k(block(b_mine)); fetch_v(block(b_mine)); }
     }
     const LaneAddr<C> la(lane, lds);
     f32x16 oacc[C::NDB];
@@ -181,7 +191,15 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
 
     // probabilities of block b, rounded to bf16 operand slots
     auto softmax = [&](f32x16& s, int b, bf16x8 (&pf)[2]) __attribute__((always_inline)) {
-        if (b >= vis.n_full) {
+        if constexpr (WIN) {
+            const int cb = block(b);
+            if (!vis.span.full(cb)) {
+                keep_branch();
+                const uint32_t seen = win_bits(vis.mine, cb * TB) >> (4 * hh);
+                auto one = [&](auto ic) __attribute__((always_inline)) { constexpr int i = decltype(ic)::value; s[i] = win_or<8 * (i >> 2) + (i & 3)>(seen, s[i], -INFINITY); };
+                for_range<0, 16>(one);
+            }
+        } else if (b >= vis.n_full) {
             keep_branch();
             const int n = vis.mine - b * TB - 4 * hh;
 #pragma unroll
@@ -192,7 +210,7 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
 #pragma unroll
         for (int r = 3; r < 15; r += 2) mx = max3(mx, s[r], s[r + 1]);
         mx = max_across_halves(max2(mx, s[15]));
-        if (b == sp) {                                     // nothing to rescale yet
+        if (b == b_mine) {                                 // nothing to rescale yet
             m_run = fmaxf(NEG_BIG, mx * c_log2);
             thr_raw = (m_run + RESCALE_SLACK) * inv_c_log2;
         } else if (__any(mx > thr_raw)) {                  // running maximum, raised only when a block exceeds it by more than 2^8
@@ -222,32 +240,33 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
     bf16x8 qf[C::NKS];
 #pragma unroll
     for (int ks = 0; ks < C::NKS; ++ks) qf[ks] = lds_b128(la.row[ks] - lds + lds_q);
-    for (int b = sp; b < n_blocks; b += NW) {
+    for (int b = b_mine; b < n_blocks; b += NW) {
         const bool more = b + NW < n_blocks;
         wait_transfers<C::XFERS>();                        // K has landed, V may still be in flight
         f32x16 s = row_product<C>(la, 0, [&](int ks) { return qf[ks]; });
         reads_done();
-        if (more) fetch_k(b + NW);
+        if (more) fetch_k(block(b + NW));
         bf16x8 pf[2];
         softmax(s, b, pf);
         if (more) wait_transfers<C::XFERS>();
         else wait_transfers<0>();
         col_product<C>(oacc, la, C::TILE_BYTES, pf);
         reads_done();
-        if (more) fetch_v(b + NW);
+        if (more) fetch_v(block(b + NW));
     }
 
     // Combine the splits: every wavefront weighs its own partial result, merged with the running (o, lse), then one
     // row-contiguous pass adds them up.  The running values are asked for first (rows past the end read the last one).
     wait_transfers<0>();                                   // (a first block that no row sees)
+    float *const o_out = [&]() { if constexpr (WIN) return a.out_o(split); else return a.o; }(), *const lse_out = [&]() { if constexpr (WIN) return a.out_lse(split); else return a.lse; }();
     f32x4 o_old[C::OUT_VECS];
     float lse_old = -INFINITY;
-    if (a.accumulate) {
-        lse_old = a.lse[(long long)h * g.lq + (row0 + l32 < g.lq ? row0 + l32 : g.lq - 1)];
+    if (merges) {
+        lse_old = lse_out[(long long)h * g.lq + (row0 + l32 < g.lq ? row0 + l32 : g.lq - 1)];
 #pragma unroll
         for (int j = 0; j < C::OUT_VECS; ++j) {
             const int i = tid + 64 * NW * j, r = row0 + i / (D / 4), c = 4 * (i % (D / 4));
-            o_old[j] = *reinterpret_cast<const f32x4*>(a.o + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
+            o_old[j] = *reinterpret_cast<const f32x4*>(o_out + ((long long)(r < g.lq ? r : g.lq - 1) * g.nq + h) * D + c);
         }
     } else {
 #pragma unroll
@@ -273,7 +292,7 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
         lse_new = (m + __log2f(l)) * LN2;
     }
     float wb = inv;
-    if (a.accumulate) {
+    if (merges) {
         const float mm = fmaxf(lse_old, lse_new);
         if (mm != -INFINITY) {
             const float ea = __expf(lse_old - mm), eb = __expf(lse_new - mm);
@@ -285,15 +304,38 @@ __global__ void __launch_bounds__(512, D == 64 ? 4 : 2) fwd_split_bf16_kernel(co
     }
     if (sp == 0 && hh == 0) {
         sm.e.wa[l32] = wa;
-        if (row0 + l32 < g.lq) a.lse[(long long)h * g.lq + row0 + l32] = lse_new;
+        if (!WIN && row0 + l32 < g.lq) lse_out[(long long)h * g.lq + row0 + l32] = lse_new;
     }
     stage_transposed<C>(&sm.e.stage[sp * TB * C::PITCH], oacc, l32, hh, wb * fast_exp2(m_run - m));
     __syncthreads();
+    if constexpr (WIN) {
+        f32x4 sum[C::OUT_VECS];
+        float z = 0.f;
+#pragma unroll
+        for (int j = 0; j < C::OUT_VECS; ++j) {
+            const int i = tid + 64 * NW * j, r = i / (D / 4);
+            sum[j] = staged_sum<C>(sm.e.stage, r, 4 * (i % (D / 4)));
+            if (row0 + r < g.lq) z = not_finite(sum[j], z);
+        }
+        if (__syncthreads_or(z != 0.f)) {
+            win_plain::fwd_unit<uint16_t, D>(a, h, row0, TB, win_plain::keys_of_blocks(vis.span, b_first, n_blocks), split);
+            return;
+        }
+        if (sp == 0 && hh == 0 && row0 + l32 < g.lq) lse_out[(long long)h * g.lq + row0 + l32] = lse_new;
+#pragma unroll
+        for (int j = 0; j < C::OUT_VECS; ++j) {
+            const int i = tid + 64 * NW * j, r = i / (D / 4);
+            if (row0 + r >= g.lq) continue;
+            const f32x4 out = sm.e.wa[r] * o_old[j] + sum[j];
+            win_plain::store4(o_out, ((long long)(row0 + r) * g.nq + h) * D + 4 * (i % (D / 4)), a.rounds(), out[0], out[1], out[2], out[3]);
+        }
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < C::OUT_VECS; ++j) {
         const int i = tid + 64 * NW * j, r = i / (D / 4), c = 4 * (i % (D / 4));
         const f32x4 out = sm.e.wa[r] * o_old[j] + staged_sum<C>(sm.e.stage, r, c);
-        if (row0 + r < g.lq) *reinterpret_cast<f32x4*>(a.o + ((long long)(row0 + r) * g.nq + h) * D + c) = out;
+        if (row0 + r < g.lq) *reinterpret_cast<f32x4*>(o_out + ((long long)(row0 + r) * g.nq + h) * D + c) = out;
     }
 }
 
@@ -684,8 +726,8 @@ hipError_t hexi_launch_fwd_split_bf16(const FwdArgs& a, hipStream_t s)
 {
     const int n_q_tiles = (a.g.lq + TB - 1) / TB;
     const dim3 grid((unsigned)a.g.nq, (unsigned)n_q_tiles);
-    if (a.g.d == 128) fwd_split_bf16_kernel<128><<<grid, 512, 0, s>>>(a, n_q_tiles);
-    else if (a.g.d == 64) fwd_split_bf16_kernel<64><<<grid, 512, 0, s>>>(a, n_q_tiles);
+    if (a.g.d == 128) fwd_split_bf16_kernel<128, false><<<grid, 512, 0, s>>>(a, n_q_tiles);
+    else if (a.g.d == 64) fwd_split_bf16_kernel<64, false><<<grid, 512, 0, s>>>(a, n_q_tiles);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }
@@ -706,6 +748,15 @@ hipError_t hexi_launch_bwd_split_bf16(const BwdArgs& a, bool dq, const HeadRuns&
         if (shared) bwd_split_bf16_kernel<64, true, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
         else bwd_split_bf16_kernel<64, false, false><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     } else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+hipError_t hexi_launch_win_fwd_split_bf16(const WinFwdArgs& a, hipStream_t s)
+{
+    const int n_q_tiles = (a.g.lq + TB - 1) / TB;
+    const dim3 grid((unsigned)a.g.nq * (unsigned)n_q_tiles, (unsigned)a.n_splits);
+    if (a.g.d == 128) fwd_split_bf16_kernel<128, true><<<grid, 512, 0, s>>>(a, n_q_tiles);
+    else fwd_split_bf16_kernel<64, true><<<grid, 512, 0, s>>>(a, n_q_tiles);
     return hipGetLastError();
 }
 

@@ -46,7 +46,10 @@ template <class F> hipError_t with_cfg(int d, bool split, F f)
 static hipError_t launch_fwd(const WinFwdArgs& a, int dtype, hipStream_t s)
 {
     if (a.few) return hexi_launch_win_few(a, dtype, s);
-    if (dtype == HEXI_BF16) return a.n_splits == 1 && hexi_win_fwd_large(a.g, a.window, a.n_sink) ? hexi_launch_win_fwd_large_bf16(a, s) : hexi_launch_win_fwd_quad_bf16(a, s);
+    if (dtype == HEXI_BF16) {
+        if (a.n_splits == 1 && hexi_win_fwd_large(a.g, a.window, a.n_sink)) return hexi_launch_win_fwd_large_bf16(a, s);
+        return (a.n_splits > 1 ? a.rows32 != 0 : hexi_win_fwd_rows32(a.g, a.window, a.n_sink)) ? hexi_launch_win_fwd_split_bf16(a, s) : hexi_launch_win_fwd_quad_bf16(a, s);
+    }
     const AttnGeom& g = a.g;
     const bool split = a.n_splits > 1 || hexi_win_f32_split(0, g, a.window, a.n_sink);      // (runs of keys that are split further are 16-row units')
     return with_cfg(g.d, split, [&](auto cfg) {

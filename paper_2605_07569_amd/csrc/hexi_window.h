@@ -13,6 +13,7 @@ struct WinFwdArgs : FwdArgs {
     // Splits of a unit's run of blocks, one workgroup each; with more than one their normalised results go to part_o [splits][lq][nq][d] and part_lse
     // [splits][nq][lq], and a second launch joins them.
     int few;                // the units are those of few rows
+    int rows32;             // (bf16, with more than one split) the units have 32 rows, not 64
     int n_splits;
     float *part_o, *part_lse;
     // where a split writes
@@ -122,35 +123,56 @@ struct WinRowSpan {
 #define HEXI_WIN_FEW_ROWS 8
 #define HEXI_WIN_FEW_GROUPS 160      // of 16 vectors: 32 whole ones, and one that is not whole for each of 128 heads
 
-// How a forward call is cut, by the descriptor, the window and the lengths alone, so that its workspace can be asked for without the ranges.
-struct WinFwdPlan { int few, n_splits; };
-// Few rows whose q heads share kv heads take workgroups of 16 query vectors (hexi_win_few.hip).  us, 64-row units (fp32: 16-row ones) / these, one row, 128 columns, bf16:
-// 8/1 heads, 4097 keys 12.0 / 9.2, 32/8 21.0 / 10.9, 64/8 and 32001 keys 162 / 30, 24/24 18.7 / 18.7, 128/128 and 501 keys 11.8 / 14.8; fp32: 32/8, 4097 keys 29.6 / 18.2, 24/24
-// 25.6 / 28.3.  Two workgroups a CU in all; one split for up to four blocks of keys (fp32: two), where a join takes more than it saves: 8/1 heads, in splits / in one, 100
-// keys 8.2 / 5.9, 255 8.3 / 7.9, 400 8.4 / 10.5; fp32 100 9.7 / 8.5, 190 10.0 / 10.5.
-// Otherwise the units are split as far as fills the chip with workgroups, each left with a block for every wavefront at least, if that takes at
-// least eight steps off a unit (a step is 0.8 us, joining the results 3 to 4).
-inline WinFwdPlan hexi_win_fwd_plan(int dtype, int nq, int nkv, long long lq, long long lc, long long window, long long n_sink)
+// What a bf16 forward call takes in units of 64 rows (0) or 32 (1), each in n splits, us: a base, a unit's fixed part and its steps of 128 (256) keys, the longer of a unit and
+// all units' share of 256 CUs with a part of one, and the join.  Fitted to 2300 timings of 500 random calls (half within 5 %); the choice by it is on average 1 % slower than
+// the best of them.  64 rows / 32 rows, and in how many splits, 128 columns: 8/1 heads of 775 rows, window 87 10.6 / 6.9, 12/3 of 2158, 3425 75 / 98, 6/2 of 21, 5494 43 / 32, in 8
+// 16.8 / 13.7, in 16 14.5 / 12.1; 64 columns: 16/4 of 278, 4423 28.6 / 21.0, in 4 23.8 / 30.2, 32/8 of 4144, 283 42 / 88.
+inline double hexi_win_fwd_us(int rows32, int d, long long lq, int nq, double share, double keys, int n)
 {
-    auto keys_of = [&](long long rows) {
-        long long keys = window < lc ? window + (lq < rows ? lq : rows) : lc;
-        keys += n_sink < lc ? n_sink : lc;
-        return keys < lc ? keys : lc;
-    };
-    WinFwdPlan plan = {0, 1};
-    if (lq <= HEXI_WIN_FEW_ROWS && lq * nq <= HEXI_WIN_FEW_VECTORS && lq * nq <= 32 * nkv && nq >= 2 * nkv) {
-        const long long groups = nkv * ((lq * nq + 16 * nkv - 1) / (16 * nkv)), blocks = (keys_of(lq) + 63) / 64;
+    struct Fit { double base, fixed, step, rest, join, join_values; };      // join_values: per 10^6 partial results
+    static const Fit fits[2][2] = {{{4.4, 2.1, 0.65, 0.30, 3.3, 3.5}, {1.2, 3.8, 0.94, 0.33, 3.4, 5.0}}, {{0.9, 7.2, 0.90, 0.46, 3.0, 2.6}, {1.0, 4.8, 1.40, 0.38, 3.3, 3.6}}};
+    const Fit& f = fits[d == 128][rows32];
+    const int rows = rows32 ? 32 : 64, step = rows32 ? 256 : 128;
+    const double unit = f.fixed + f.step * (keys + (lq < rows ? lq : rows) + 30) / (step * n), even = share * ((lq + rows - 1) / rows) * nq * n / 256.0 * unit + f.rest * unit;
+    return f.base + (unit > even ? unit : even) + (n > 1 ? f.join + f.join_values * 1e-6 * n * lq * nq * d : 0.0);
+}
+
+// How a forward call is cut, by the descriptor, the window and the lengths alone, so that its workspace can be asked for without the ranges.
+struct WinFwdPlan { int few, n_splits, rows32; };
+// Few rows whose q heads share kv heads take workgroups of 16 query vectors (hexi_win_few.hip), two a CU in all, in one split up to two blocks of 64 keys; but bf16 rows of more
+// than two blocks and at most eight, for which one unit without a join is faster.  us, bf16, 32-row units / these, 128 columns, one row of 8/1 heads, 60 keys 6.0 / 5.1,
+// 250 6.8 / 7.9, 1000 10.1 / 8.7, 4096 10.7 / 9.2; 32/8, 4096 19.3 / 10.9; 64/8, 32000 150 / 30; 8 rows of 8/4, 500 8.2 / 9.5, 4096 10.6 / 11.5; 32/8, 30000 76 / 46; heads of
+// their own, 64-row units / these, one row of 24/24, 4096 18.7 / 18.7, 128/128, 500 11.8 / 14.8.  fp32, 16-row units / these: 32/8, 4096 29.6 / 18.2, 8/1, 400 13.9 / 10.0, 190
+// 9.6 / 10.0, 24/24, 4096 25.6 / 28.3.
+// Otherwise bf16 units are split by hexi_win_fwd_us, where a wavefront is left with a block at least; fp32 ones as far as fills the chip with workgroups, if that takes at least
+// eight steps off a unit (a step is 0.8 us, joining the results 3 to 4).
+inline WinFwdPlan hexi_win_fwd_plan(int dtype, int d, int nq, int nkv, long long lq, long long lc, long long window, long long n_sink)
+{
+    const long long sinks = n_sink < lc ? n_sink : lc, seen = window < lc ? (window + sinks < lc ? window + sinks : lc) : lc;      // keys of a row
+    auto keys_of = [&](long long rows) { return seen + (lq < rows ? lq : rows) < lc ? seen + (lq < rows ? lq : rows) : lc; };
+    WinFwdPlan plan = {0, 1, 0};
+    const long long blocks = (keys_of(lq) + 63) / 64;
+    if (lq <= HEXI_WIN_FEW_ROWS && lq * nq <= HEXI_WIN_FEW_VECTORS && lq * nq <= 32 * nkv && nq >= 2 * nkv && (dtype != HEXI_BF16 || blocks <= 2 || blocks > 8)) {
+        const long long groups = nkv * ((lq * nq + 16 * nkv - 1) / (16 * nkv));
         long long n = 512 / groups;
-        n = blocks <= (dtype == HEXI_BF16 ? 4 : 2) ? 1 : n < blocks ? n : blocks;
+        n = blocks <= 2 ? 1 : n < blocks ? n : blocks;
         plan.few = 1;
         plan.n_splits = n < 1 ? 1 : n < HEXI_WIN_MAX_SPLITS ? (int)n : HEXI_WIN_MAX_SPLITS;
         return plan;
     }
-    const bool bf16 = dtype == HEXI_BF16;
-    const long long rows = bf16 ? 64 : 16, block = bf16 ? 32 : 16, waves = bf16 ? 4 : 8;
-    const long long units = (lq + rows - 1) / rows * nq;
+    if (dtype == HEXI_BF16) {
+        double best = 0.0;
+        for (int r = 0; r < 2; ++r) {
+            const long long rows = r ? 32 : 64, step = r ? 256 : 128, units = (lq + rows - 1) / rows * nq;
+            for (int n = 1; n == 1 || (n <= HEXI_WIN_MAX_SPLITS && units * n <= 512 && step * n < keys_of(rows) + step); n *= 2) {
+                const double us = hexi_win_fwd_us(r, d, lq, nq, 1.0, (double)seen, n);
+                if (best == 0.0 || us < best) { best = us; plan.n_splits = n; plan.rows32 = r; }
+            }
+        }
+        return plan;
+    }
+    const long long units = (lq + 15) / 16 * nq, steps = (keys_of(16) + 127) / 128;
     if (units > 128) return plan;
-    const long long steps = (keys_of(rows) + block * waves - 1) / (block * waves);
     long long n = 256 / units;
     n = n < steps ? n : steps;
     if (n > 1 && steps - (steps + n - 1) / n >= 8) plan.n_splits = (int)n;
@@ -195,6 +217,13 @@ inline bool hexi_win_fwd_large(const AttnGeom& g, int window, int n_sink)
     const double t_large = ceil(large / 256.0) * (18.0 + 2.0 / 64.0 * (load.mean + 255 + 63));
     const double t_small = (small / 256.0 + 0.25) * (6.0 + 1.17 / 128.0 * (load.mean + 63 + 31));
     return t_large < 0.97 * t_small;
+}
+
+// Whether the units of a bf16 forward call that is not split have 32 rows.
+inline bool hexi_win_fwd_rows32(const AttnGeom& g, int window, int n_sink)
+{
+    const WinLoad load = hexi_win_row_load(g, window, n_sink);
+    return hexi_win_fwd_us(1, g.d, g.lq, g.nq, load.share, load.mean, 1) < hexi_win_fwd_us(0, g.d, g.lq, g.nq, load.share, load.mean, 1);
 }
 
 // Whether a bf16 backward call takes 32-row (32-key) workgroups of eight wavefronts, or 64-row ones of four.  Fitted to 900 random calls (half within 6 %), us: a base, a unit's
@@ -263,6 +292,7 @@ hipError_t hexi_launch_win_few(const WinFwdArgs& a, int dtype, hipStream_t s);  
 hipError_t hexi_launch_win_join(const WinFwdArgs& a, hipStream_t s);
 hipError_t hexi_launch_win_fwd_large_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_fwd.hip: 256-row workgroups
 hipError_t hexi_launch_win_fwd_quad_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_quad_win.hip
+hipError_t hexi_launch_win_fwd_split_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_split.hip
 hipError_t hexi_launch_win_bwd_quad_bf16(const WinBwdArgs& a, hipStream_t s);
 hipError_t hexi_launch_win_bwd_split_bf16(const WinBwdArgs& a, hipStream_t s);      // in hexi_bf16_split.hip
 // Delta = rowsum(dO o) of a bf16 o

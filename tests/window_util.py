@@ -64,8 +64,9 @@ CASES = [
     Case("long", [(3000, 520)], [(0, 17), (1977, 1543)], 1024, 17, nq=4, nkv=1),
     Case("one token", [(60000, 1)], [(0, 4), (57000, 3001)], 2990, 4, nq=8),
     Case("one token, heads of their own", [(5000, 1)], [(0, 4), (3000, 2001)], 1990, 4, nq=3, nkv=3),
-    Case("one token, few keys", [(500, 1)], [(0, 4), (300, 201)], 190, 4, nq=4, nkv=2),
-    Case("one token, a block more", [(500, 1)], [(0, 501)], 257, 0, nq=4, nkv=1),
+    Case("one token, a block", [(500, 1)], [(0, 4), (440, 61)], 50, 4, nq=4, nkv=2),
+    Case("one token, a few blocks", [(500, 1)], [(0, 4), (300, 201)], 190, 4, nq=4, nkv=2),
+    Case("two tokens, nine blocks", [(500, 2)], [(0, 502)], 511, 0, nq=4, nkv=1),
     Case("three tokens", [(900, 2), (1200, 1)], [(0, 70), (300, 901)], 700, 60, nq=5, nkv=2, kv_of_q=[1, 0, 1, 1, 1]),
     Case("few rows", [(4000, 70)], [(0, 300), (1500, 2570)], 2500, 100, nq=2, nkv=2),
     Case("long odd", [(2001, 431)], [(101, 2331)], 1901, 0, nq=2, nkv=2, k_scale=2.0),
