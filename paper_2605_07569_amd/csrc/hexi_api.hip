@@ -4,7 +4,6 @@
 #include <cstdlib>
 #include <cstring>
 #include <cmath>
-#include <vector>
 #include "hexi_internal.h"
 #include "hexi_window.h"
 #include "hexi_rope.h"
@@ -361,12 +360,15 @@ static int check_a2a(bool pack, const void* x, const void* packed, int64_t s, in
         if (n_slots > HEXI_A2A_MAX_SLOTS) return fail(HEXI_EUNSUPPORTED, "more than %d listed heads", HEXI_A2A_MAX_SLOTS);
     }
     if (n_slots > 0 && !head_list) return fail(HEXI_EINVAL, "null head_list");
-    std::vector<char> seen(pack ? 0 : n_heads_total, 0);
+    unsigned char seen[65536 / 8];      // a bit to a head
+    if (!pack) memset(seen, 0, (size_t)n_heads_total / 8 + 1);
     for (int i = 0; i < n_slots; ++i) {
         if (head_list[i] < 0 || head_list[i] >= n_heads_total) return fail(HEXI_EINVAL, "head_list[%d] = %d out of range", i, head_list[i]);
         if (!pack) {
-            if (seen[head_list[i]]) return fail(HEXI_EINVAL, "head %d listed twice in an unpack", head_list[i]);
-            seen[head_list[i]] = true;
+            unsigned char& byte = seen[head_list[i] >> 3];
+            const unsigned char bit = (unsigned char)(1u << (head_list[i] & 7));
+            if (byte & bit) return fail(HEXI_EINVAL, "head %d listed twice in an unpack", head_list[i]);
+            byte |= bit;
         }
     }
     if (s > 0 && n_slots > 0) {
