@@ -205,18 +205,19 @@ inline WinLoad hexi_win_key_load(const AttnGeom& g, int window, int n_sink)
     return hexi_win_load(g.lc, [&](int key) { const WinRows w = win_rows_of_key(g.qs, seg_pos_of_row(g.ks, key), window, n_sink); return w.end > w.first ? w.end - w.first : 0; });
 }
 
-// Whether a bf16 forward call takes 256-row workgroups (head_dim 128 alone; at 64 they are slower everywhere).  Fitted to 76 random calls, us: rounds of 256 workgroups
-// times a start and end and their key tiles, 18 + 2.0 a tile of 64 keys, against rounds of 64-row ones, 6 + 1.17 a step of 128.  64 rows / 256 rows: 16 heads of 3729
-// rows, window 4873 190 / 169; 24 of 13495, 2972 665 / 607; 8 of 16384, 4096 327 / 305; 32 of 18703, 1190 703 / 720; 8 of 8513, 2018 (272 workgroups of 256) 127 / 176.
+// Whether a bf16 forward call takes 256-row workgroups (head_dim 128 alone; at 64 they are slower everywhere).  Fitted to 45 random calls (half within 4 %, the choice 1 %
+// slower than the better one), us: rounds of 256 workgroups times a start and end and their key tiles, 17.7 + 1.53 a tile of 64 keys, against rounds of 64-row ones, 6.9 + 0.98 a
+// step of 128.  64 rows / 256 rows: 16 heads of 3729 rows, window 4873 202 / 167; 24 of 13495, 2972 592 / 514; 8 of 16384, 4096 312 / 269; 32 of 18703, 1190 598 / 518; 8 of 8513,
+// 2018 (272 workgroups of 256) 117 / 140; 6 of 11340, 4680 218 / 263.
 inline bool hexi_win_fwd_large(const AttnGeom& g, int window, int n_sink)
 {
     if (g.d != 128) return false;
     const WinLoad load = hexi_win_row_load(g, window, n_sink);
     if (load.share == 0.0) return false;
     const double large = load.share * ((g.lq + 255) / 256) * g.nq, small = load.share * ((g.lq + 63) / 64) * g.nq;
-    const double t_large = ceil(large / 256.0) * (18.0 + 2.0 / 64.0 * (load.mean + 255 + 63));
-    const double t_small = (small / 256.0 + 0.25) * (6.0 + 1.17 / 128.0 * (load.mean + 63 + 31));
-    return t_large < 0.97 * t_small;
+    const double t_large = ceil(large / 256.0) * (17.7 + 1.53 / 64.0 * (load.mean + 255 + 63));
+    const double t_small = (small / 256.0 + 0.41) * (6.9 + 0.98 / 128.0 * (load.mean + 63 + 31));
+    return t_large < t_small;
 }
 
 // Whether the units of a bf16 forward call that is not split have 32 rows.
