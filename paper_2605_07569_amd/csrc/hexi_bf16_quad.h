@@ -18,6 +18,8 @@
 // before -> these, head_dim 128, fully visible chunk: forward 512 rows x 1024 keys, 24 / 8 heads 17.7 -> 15.7, 4096 x 4096 x 24 / 8 x 64
 // 138 -> 130; backward 512 x 1024 x 24 / 8 41 -> 35, 2048 x 2048 x 24 / 8 207 -> 178, 4096 x 4096 x 12 / 3 384 -> 336, 4096 x 4096 x
 // 24 / 8 x 64 445 -> 384.
+// Under a window (WIN) a unit walks the run of blocks that its rows or keys need.  Measured, us: backward of 8192 rows x 24 / 8 heads x 128, window 4096 1400 (dK / dV units 147 each, 133
+// of them steps; dQ units 59 and 50), of 4099 rows x 24 / 8 x 64, window 512 118 (22 and 16, 12 and 7).
 //
 // Operand layouts as in hexi_bf16_split.hip; dK and dV are accumulated transposed too (the keys across the lanes).
 #pragma once

@@ -13,6 +13,9 @@
 // hexi_bf16_quad.h, then the large ones, which stream less per row: see the rules in hexi_shapes.h.  Measured, us per call
 // (head_dim 128, fully visible chunk), large workgroups -> these: 300 rows x 700 keys, 4 / 2 heads: forward 28.3 -> 9.3, dQ
 // 36.2 -> 9.8, dK/dV 23.5 -> 12.3.
+// Under a window (WIN; the rules are in hexi_window.h) the same units walk the run of blocks that their rows or keys need, us per call, 64-row workgroups -> these, 128 columns:
+// forward, 8/1 heads of 775 rows, window 87 10.6 -> 6.9; all of the backward, 4/4 heads of 241 rows, window 296 14.0 -> 9.0.  They vote on the sums as staged: a vote on the
+// accumulators made the compiler spill 53 registers inside the dK/dV loop (1133 rows of 12/3 heads, window 122, dK/dV 19.7 us, 13.6 without them).
 //
 // Operand layouts are those of the large kernels (hexi_mfma.h): scores transposed in the forward and dQ kernels (a lane
 // owns a q row), keys across the lanes in the dK/dV kernel; accumulator registers go straight back in as operands, the
