@@ -168,10 +168,11 @@ int hexi_attn_bwd_chunk(const hexi_attn_desc* desc, const hexi_range* q_range, c
  */
 typedef struct { int64_t window, n_sink; } hexi_window;
 
-/* Bytes of device workspace that hexi_attn_win_fwd_chunk needs for this descriptor and window and these lengths, 0 for
- * most (0 too for arguments that the call refuses).  Nothing is kept in it between calls; calls that may run at the same
- * time, replays of captured graphs among them, need one each. */
+/* Bytes of device workspace that hexi_attn_win_fwd_chunk needs, and that hexi_attn_win_bwd_chunk can use, for this
+ * descriptor and window and these lengths, 0 for most (0 too for arguments that the call refuses).  Nothing is kept in it
+ * between calls; calls that may run at the same time, replays of captured graphs among them, need one each. */
 size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc);
+size_t hexi_attn_win_bwd_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc);
 
 /*
  * hexi_attn_fwd_chunk under a window.  o has the element type o_dtype: HEXI_F32 as there, HEXI_ACCUMULATE included, or
@@ -192,13 +193,18 @@ int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_window* windo
  * HEXI_BF16: dq, dk and dv are overwritten with the results of this chunk rounded once, for a shard whose keys all lie in
  * it (HEXI_ACCUMULATE is HEXI_EINVAL then).  All sums have a fixed order: results are reproducible run to run.  Calls that
  * add to the same dq_acc, dk or dv must be ordered.  hexi_set_dkdv_run_len() has no effect here.  Rows whose lse is
- * infinite have P = 0.  No workspace.
+ * infinite have P = 0.  workspace: hexi_attn_win_bwd_workspace_bytes() bytes of device memory, 16-byte aligned (HEXI_EWORKSPACE
+ * if smaller), or NULL.  With it the rows that see a tile of sinks (all rows behind them do), or of any keys where these
+ * are few, are shared out over workgroups; the order of the sums is then another fixed one.  Without it one workgroup takes
+ * all of them: 16 times the rows, 16 times as long for the sinks.
  */
+
 int hexi_attn_win_bwd_chunk(const hexi_attn_desc* desc, const hexi_window* window,
                             const hexi_range* q_range, const hexi_range* kv_range,
                             const void* q, const void* k, const void* v, const void* o, int32_t o_dtype, const void* d_o,
                             const float* lse, float* delta,
-                            void* dq, void* dk, void* dv, int32_t grad_dtype, uint32_t flags, void* hip_stream);
+                            void* dq, void* dk, void* dv, int32_t grad_dtype, uint32_t flags,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Rotary positions with one or several axes (time, height, width) on the rows of a shard.  Of every row of every head the

@@ -261,10 +261,15 @@ static int build_window(const hexi_window* w, int* window, int* n_sink)
     return HEXI_OK;
 }
 
+static bool win_sizes_fit(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
+{
+    return !(!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || d->n_kv_heads < 1 ||
+        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || w->window < 1 || w->n_sink < 0);
+}
+
 static WinFwdPlan win_fwd_plan(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
 {
-    if (!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || d->n_kv_heads < 1 ||
-        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || w->window < 1 || w->n_sink < 0) return {0, 1, 0};
+    if (!win_sizes_fit(d, w, lq, lc)) return {0, 1, 0};
     return hexi_win_fwd_plan(d->dtype, d->head_dim, d->n_q_heads, d->n_kv_heads, lq, lc, w->window, w->n_sink);
 }
 
@@ -309,9 +314,22 @@ HEXI_EXPORT int hexi_attn_win_fwd_chunk(const hexi_attn_desc* desc, const hexi_w
     return HEXI_OK;
 }
 
+static WinBwdPlan win_bwd_plan(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
+{
+    if (!win_sizes_fit(d, w, lq, lc)) return {1, 1};
+    return hexi_win_bwd_plan(d->dtype, d->n_q_heads, d->n_kv_heads, lq, lc, w->window, w->n_sink);
+}
+
+HEXI_EXPORT size_t hexi_attn_win_bwd_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc)
+{
+    const WinBwdPlan plan = win_bwd_plan(desc, window, lq, lc);
+    return plan.n_sink_parts > 1 || plan.n_parts > 1 ? hexi_win_bwd_workspace(plan, desc->n_kv_heads, desc->head_dim, lc, window->n_sink) : 0;
+}
+
 HEXI_EXPORT int hexi_attn_win_bwd_chunk(const hexi_attn_desc* desc, const hexi_window* window, const hexi_range* q_range, const hexi_range* kv_range,
                                        const void* q, const void* k, const void* v, const void* o, int32_t o_dtype, const void* d_o,
-                                       const float* lse, float* delta, void* dq, void* dk, void* dv, int32_t grad_dtype, uint32_t flags, void* hip_stream)
+                                       const float* lse, float* delta, void* dq, void* dk, void* dv, int32_t grad_dtype, uint32_t flags,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     WinBwdArgs a;
     int rc = build_geom(desc, q_range, kv_range, &a.g);
@@ -334,6 +352,18 @@ HEXI_EXPORT int hexi_attn_win_bwd_chunk(const hexi_attn_desc* desc, const hexi_w
     a.want_dq = want_dq ? 1 : 0;
     a.want_dkdv = want_dkdv ? 1 : 0;
     a.out_bf16 = grad_dtype == HEXI_BF16;
+    a.sink_tiles = 0;
+    a.n_sink_parts = a.n_parts = 1;
+    a.part = nullptr;
+    if (workspace && want_dkdv) {
+        const WinBwdPlan plan = win_bwd_plan(desc, window, a.g.lq, a.g.lc);
+        const size_t need = hexi_win_bwd_workspace(plan, a.g.nkv, a.g.d, a.g.lc, window->n_sink);
+        if (workspace_bytes < need) return fail(HEXI_EWORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+        if (!aligned16(workspace)) return fail(HEXI_EALIGN, "the workspace must be 16-byte aligned");
+        a.n_sink_parts = plan.n_sink_parts;
+        a.n_parts = plan.n_parts;
+        a.part = (float*)workspace;
+    }
     hipError_t e = hipSuccess;
     if (want_delta)
         e = o_dtype == HEXI_F32 ? hexi_launch_delta(a.g.lq, a.g.nq, a.g.d, (const float*)o, d_o, desc->dtype, a.g.q_stride_tok, a.g.q_stride_head, delta, s)

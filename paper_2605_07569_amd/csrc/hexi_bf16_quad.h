@@ -770,7 +770,7 @@ template <class C, bool WIN> union QuadDkdvSmem {
 };
 
 template <int D, bool ATOMIC_DKV, bool WIN>
-__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, QuadDkdvSmem<QuadCfg<D>, WIN>& sm)
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, QuadDkdvSmem<QuadCfg<D>, WIN>& sm, const WinUnit* const unit = nullptr)
 {
     using C = QuadCfg<D>;
     const AttnGeom& g = a.g;
@@ -814,8 +814,20 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
     // The workgroup's sequence of blocks: those of the first head of the run, then the next head's; a wavefront takes every fourth
     // one.  (h, t): the next block to ask for.  The last block of a head is moved back to the last 32 rows (the rows of the block
     // before are masked), so that all blocks are whole unless the shard has fewer rows.
-    const int cnt = n_all * n_heads > sp ? (n_all * n_heads - sp + NW - 1) / NW : 0;
-    int h = h0, t = sp;
+    int first_blk = 0, n_blk = n_all * n_heads;            // of the sequence: this part's
+    if constexpr (WIN) {
+        first_blk = unit->first_of(n_all * n_heads, unit->part);
+        n_blk = unit->first_of(n_all * n_heads, unit->part + 1) - first_blk;
+        n_blk = uniform(n_blk);
+        first_blk = uniform(first_blk);
+        if (n_blk == 0) {
+            wait_transfers<0>();
+            win_plain::no_dkdv<D>(a, *unit, ROWS);
+            return;
+        }
+    }
+    const int cnt = n_blk > sp ? (n_blk - sp + NW - 1) / NW : 0;
+    int h = h0, t = first_blk + sp;
     auto normalise = [&]() { while (t >= n_all) { t -= n_all; h = arg_byte(runs.next, h); } };
     auto start_of = [&](int row) { return row + TB <= g.lq || g.lq < TB ? row : g.lq - TB; };
     const uint32_t scalar_off = 4u * (uint32_t)(l32 < g.lq ? l32 : g.lq - 1);      // (a shard of fewer rows than a block has one block a head)
@@ -1078,6 +1090,14 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
         };
         gather(0, dv, 1.0f);
         gather(1, dk, g.scale);
+        if (unit->n_parts > 1) {
+            float* out = a.part + unit->slot * (2 * ROWS * D);
+#pragma unroll
+            for (int which = 0; which < 2; ++which)
+#pragma unroll
+                for (int j = 0; j < C::OUT_VECS; ++j) *reinterpret_cast<f32x4*>(out + which * ROWS * D + 4 * (tid + 64 * NW * j)) = sum[which][j];
+            return;
+        }
         if (__syncthreads_or(z != 0.f)) {
             win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0, ROWS);
             return;
@@ -1138,12 +1158,18 @@ __global__ void __launch_bounds__(256, 1) bwd_quad_bf16_kernel(const BwdArgsOf<W
 {
     __shared__ __attribute__((aligned(1024))) union { QuadDkdvSmem<QuadCfg<D>, WIN> dkdv; QuadDqSmem<QuadCfg<D>> dq; } sm;
     if (blockIdx.x < n_dkdv) {
-        const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
-        dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
+        if constexpr (WIN) {
+            const WinUnit unit(a, ROWS, (int)blockIdx.x);
+            dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, unit.kvh, unit.tile, sm.dkdv, &unit);
+        } else {
+            const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
+            dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
+        }
     } else {
         const unsigned unit = blockIdx.x - n_dkdv;
         const int tile = uniform((int)(unit / (unsigned)a.g.nq));
-        dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
+        if constexpr (WIN) dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, a.q_tile(tile), sm.dq);
+        else dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
     }
 }
 

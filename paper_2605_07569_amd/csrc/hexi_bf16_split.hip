@@ -510,7 +510,7 @@ template <class C> union DkdvSmem {
 };
 
 template <int D, bool ATOMIC_DKV, bool WIN>
-__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, DkdvSmem<SplitCfg<D>>& sm)
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRuns& runs, const int run, const int kv_tile, DkdvSmem<SplitCfg<D>>& sm, const WinUnit* const unit = nullptr)
 {
     using C = SplitCfg<D>;
     const AttnGeom& g = a.g;
@@ -568,6 +568,20 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
     // the workgroup's sequence of blocks: those of the first head of the run, then the next head's; this wavefront's
     // first one, and a step of NW
     int h = arg_byte(runs.first, run), t = wave, left = n_heads;
+    int to_do = 0;                                         // (WIN) blocks of this part that are left for this wavefront and the ones behind it
+    if constexpr (WIN) {
+        const int first_blk = unit->first_of(n_all * n_heads, unit->part);
+        to_do = unit->first_of(n_all * n_heads, unit->part + 1) - first_blk;
+        to_do = uniform(to_do);
+        if (to_do == 0) {
+            wait_transfers<0>();
+            win_plain::no_dkdv<D>(a, *unit, TB);
+            return;
+        }
+        to_do -= wave;
+        t += first_blk;
+        if (to_do <= 0) left = 0;
+    }
     auto normalise = [&]() { while (left > 0 && t >= n_all) { t -= n_all; h = arg_byte(runs.next, h); --left; } };
     if (n_all == 0) left = 0;
     normalise();
@@ -592,6 +606,10 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
     while (left > 0) {
         const int row = (blk0 + t) * TB;
         t += NW;
+        if constexpr (WIN) {
+            to_do -= NW;
+            if (to_do <= 0) left = 0;
+        }
         normalise();
         const bool more = left > 0;
         const int next_row = (blk0 + t) * TB;
@@ -660,6 +678,14 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const HeadRun
         };
         gather(0, dv, 1.0f);
         gather(1, dk, g.scale);
+        if (unit->n_parts > 1) {
+            float* out = a.part + unit->slot * (2 * TB * D);
+#pragma unroll
+            for (int which = 0; which < 2; ++which)
+#pragma unroll
+                for (int j = 0; j < C::OUT_VECS; ++j) *reinterpret_cast<f32x4*>(out + which * TB * D + 4 * (tid + 64 * NW * j)) = sum[which][j];
+            return;
+        }
         if (__syncthreads_or(z != 0.f)) {
             win_plain::dkdv_unit<uint16_t, D>(a, kvh, col0, TB);
             return;
@@ -714,12 +740,18 @@ __global__ void __launch_bounds__(512) bwd_split_bf16_kernel(const BwdArgsOf<WIN
 {
     __shared__ __attribute__((aligned(1024))) union { DkdvSmem<SplitCfg<D>> dkdv; DqSmem<SplitCfg<D>> dq; } sm;
     if (blockIdx.x < n_dkdv) {
-        const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
-        dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
+        if constexpr (WIN) {
+            const WinUnit unit(a, TB, (int)blockIdx.x);
+            dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, unit.kvh, unit.tile, sm.dkdv, &unit);
+        } else {
+            const int tile = uniform((int)(blockIdx.x / (unsigned)runs.n));
+            dkdv_unit<D, ATOMIC_DKV, WIN>(a, runs, (int)blockIdx.x - tile * runs.n, tile, sm.dkdv);
+        }
     } else {
         const unsigned unit = blockIdx.x - n_dkdv;
         const int tile = uniform((int)(unit / (unsigned)a.g.nq));
-        dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
+        if constexpr (WIN) dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, a.q_tile(tile), sm.dq);
+        else dq_unit<D, WIN>(a, (int)unit - tile * a.g.nq, n_q_tiles - 1 - tile, sm.dq);
     }
 }
 
@@ -763,14 +795,17 @@ hipError_t hexi_launch_win_fwd_split_bf16(const WinFwdArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t hexi_launch_win_bwd_split_bf16(const WinBwdArgs& a, hipStream_t s)
+hipError_t hexi_launch_win_bwd_split_bf16(const WinBwdArgs& whole, hipStream_t s)
 {
-    const int n_q_tiles = a.want_dq ? (a.g.lq + TB - 1) / TB : 0;
+    const WinBwdArgs a = hexi_win_tiles_of(whole, TB);
+    const int n_q_tiles = a.n_q_tiles;
     HeadRuns runs;
     hexi_head_run_of_each_kv(a.g.kv_of_q, a.g.nq, a.g.nkv, &runs);
-    const unsigned n_dkdv = a.want_dkdv ? (unsigned)((a.g.lc + TB - 1) / TB) * (unsigned)a.g.nkv : 0u;
+    const unsigned n_dkdv = a.want_dkdv ? (unsigned)hexi_win_dkdv_units(a, (a.g.lc + TB - 1) / TB) : 0u;
     const unsigned grid = n_dkdv + (unsigned)n_q_tiles * (unsigned)a.g.nq;
+    if (grid == 0) return hipSuccess;
     if (a.g.d == 128) bwd_split_bf16_kernel<128, false, true><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
     else bwd_split_bf16_kernel<64, false, true><<<grid, 512, 0, s>>>(a, runs, n_dkdv, n_q_tiles);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || !a.want_dkdv ? e : hexi_launch_win_parts(a, HEXI_BF16, TB, s);
 }

@@ -598,7 +598,7 @@ template <class C> struct DkdvSmem {
 };
 
 template <class C, bool WIN = false>
-__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh, const int kv_tile, DkdvSmem<C>& sm, const int h_first, const int h_end, const bool atomic)
+__device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh, const int kv_tile, DkdvSmem<C>& sm, const int h_first, const int h_end, const bool atomic, const WinUnit* const unit = nullptr)
 {
     constexpr int D = C::D, NW = C::NW, S = C::S, TM = C::TK, NBLK = C::NBLK;
     constexpr bool SPLIT = C::SPLIT, TWO = C::TWO;
@@ -647,10 +647,20 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
     const TileFetch<C> fetch(wave, lane, g.q_stride_tok);
     const uint32_t lds_q = (uint32_t)(uintptr_t)(&sm.t.q[0][0]), lds_g = (uint32_t)(uintptr_t)(&sm.t.g[0][0]);
     auto next_head = [&](int h) { for (++h; h < h_end && g.kv_of_q[h] != kvh; ++h) {} return h; };
-    // the next tile behind (h, t)
-    auto advance = [&](int& h, int& t) {
+    // (WIN) this part's tiles of the sequence, for this wavefront and the ones behind it
+    int first_tile = 0, n_tiles = 0;
+    if constexpr (WIN) {
+        int heads = 0;
+        for (int h = h_first; h < h_end; ++h) heads += g.kv_of_q[h] == kvh;
+        first_tile = unit->first_of(n_qtiles * heads, unit->part);
+        n_tiles = unit->first_of(n_qtiles * heads, unit->part + 1) - first_tile - (SPLIT ? wave : 0);
+    }
+    // the next tile behind (h, t); left (WIN): tiles from this one on
+    auto advance = [&](int& h, int& t, int& left) {
         if constexpr (WIN) {
             t += WT::STEP;
+            left -= WT::STEP;
+            if (left <= 0) h = h_end;
             while (t >= n_qtiles && h < h_end) { t -= n_qtiles; h = next_head(h); }
         } else if (++t == n_qtiles) { t = tile0; h = next_head(h); }
     };
@@ -658,11 +668,12 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
         h = next_head(h_first - 1);
         t = tile0;
         if constexpr (WIN) {
-            t = SPLIT ? wave : 0;
+            t = first_tile + (SPLIT ? wave : 0);
+            if (n_tiles <= 0) h = h_end;
             while (t >= n_qtiles && h < h_end) { t -= n_qtiles; h = next_head(h); }
         }
     };
-    int fetch_h = h_end, fetch_t = tile0;
+    int fetch_h = h_end, fetch_t = tile0, fetch_left = n_tiles;
     if (per_head > 0) start(fetch_h, fetch_t);
     const int pos_slot = C::PRIVATE ? (lane < 16 ? 16 * wave + lane : TM) : tid;
     auto fetch_tile = [&](int buf) {
@@ -679,7 +690,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
         if (C::PRIVATE || wave == 1) lds_dma4(a.delta + (long long)fetch_h * g.lq + row, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)&delta[buf][SET * wave]));
         if (pos_slot < TM && masked_tile(fetch_t))
             qpos[buf][pos_slot] = row0 + pos_slot < g.lq ? seg_pos_of_row(g.qs, row0 + pos_slot) : -1;
-        advance(fetch_h, fetch_t);
+        advance(fetch_h, fetch_t, fetch_left);
     };
     auto hidden = [&](int qp) { if constexpr (WIN) return my_kpos > qp || (qp - my_kpos >= a.window && my_kpos >= a.n_sink); else return my_kpos > qp; };
 
@@ -687,7 +698,7 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
 #pragma unroll
     for (int i = 0; i < 4 * C::NH; ++i) { dk[i] = f32x4{0.f, 0.f, 0.f, 0.f}; dv[i] = dk[i]; }
     if (per_head > 0) {
-        int buf = 0, t, h;
+        int buf = 0, t, h, left = n_tiles;
         start(h, t);
         if (fetch_h < h_end) fetch_tile(0);
         while (h < h_end) {
@@ -737,13 +748,14 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
             }
             if (C::NBUF == 1 && fetch_h < h_end) { if (TWO) reads_done(); fetch_tile(buf ^ 1); }
             buf ^= 1;
-            advance(h, t);
+            advance(h, t, left);
         }
     }
     if constexpr (WIN) {
-        if (__syncthreads_or(not_finite(dk) + not_finite(dv) != 0.f)) { win_plain::dkdv_unit<float, D>(a, kvh, col0, C::ROWS); return; }
+        if (unit->n_parts == 1 && __syncthreads_or(not_finite(dk) + not_finite(dv) != 0.f)) { win_plain::dkdv_unit<float, D>(a, kvh, col0, C::ROWS); return; }
     }
-    auto write_out = [&](float* out, const f32x4 (&acc)[4 * C::NH], float w) {
+    auto write_out = [&](const int which, const f32x4 (&acc)[4 * C::NH], float w) {
+        float* const out = which ? a.dk : a.dv;
         __syncthreads();
         stage_rows<C>(&sm.stage[wave * 16 * C::PITCH], acc, grp, l16, w);
         __syncthreads();
@@ -753,6 +765,12 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
             f32x4 x = *reinterpret_cast<const f32x4*>(&sm.stage[r * C::PITCH + c]);
 #pragma unroll
             for (int s = 1; s < S; ++s) x += *reinterpret_cast<const f32x4*>(&sm.stage[(s * C::ROWS + r) * C::PITCH + c]);
+            if constexpr (WIN) {
+                if (unit->n_parts > 1) {
+                    *reinterpret_cast<f32x4*>(a.part + (unit->slot * 2 + which) * (C::ROWS * D) + r * D + c) = x;
+                    continue;
+                }
+            }
             f32x4* op = reinterpret_cast<f32x4*>(out + ((long long)(col0 + r) * g.nkv + kvh) * D + c);
             if (atomic) {
 #pragma unroll
@@ -764,8 +782,8 @@ __device__ __forceinline__ void dkdv_unit(const BwdArgsOf<WIN>& a, const int kvh
             else *op = x;
         }
     };
-    write_out(a.dv, dv, 1.0f);
-    write_out(a.dk, dk, g.scale);
+    write_out(0, dv, 1.0f);
+    write_out(1, dk, g.scale);
 }
 
 } }  // namespace rows16

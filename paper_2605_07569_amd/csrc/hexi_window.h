@@ -25,7 +25,46 @@ struct WinFwdArgs : FwdArgs {
 struct WinBwdArgs : BwdArgs {
     int window, n_sink;
     int out_bf16;           // dq, dk, dv are bf16, overwritten
+    // The rows that see a tile of keys in parts, a dK / dV unit each: n_sink_parts for the first sink_tiles tiles, which hold the sinks that all later rows see, n_parts for the
+    // others.  The sums of a tile that has more than one go to part [part][2][keys of a tile][d], dV and dK, and a second launch adds them up.
+    int sink_tiles, n_sink_parts, n_parts;
+    float* part;
+    // the longest units first: tiles of keys (of rows) from the last one on
+    int keys_down, rows_down;
+    int first_q_tile, n_q_tiles;      // tiles of rows that are launched: those that see no key may be left out where dq stays as it is
+    __host__ __device__ int q_tile(int i) const { return first_q_tile + (rows_down ? n_q_tiles - 1 - i : i); }
 };
+inline int hexi_win_dkdv_units(const WinBwdArgs& a, int tiles) { return (a.sink_tiles * a.n_sink_parts + (tiles - a.sink_tiles) * a.n_parts) * a.g.nkv; }
+#ifdef __HIP__
+// A dK / dV unit, by its workgroup: kv heads side by side, then parts, then tiles.
+struct WinUnit {
+    int tile, kvh, part, n_parts;
+    long long slot;         // of its sums, where it is one of several parts
+    __device__ __forceinline__ WinUnit(const WinBwdArgs& a, int keys, int block)      // keys: of a tile
+    {
+        const int sinks = a.sink_tiles * a.n_sink_parts * a.g.nkv;
+        const bool sink = block < sinks;
+        const int b = sink ? block : block - sinks;
+        n_parts = sink ? a.n_sink_parts : a.n_parts;
+        const int ts = __builtin_amdgcn_readfirstlane(b / a.g.nkv);
+        kvh = b - ts * a.g.nkv;
+        const int t = __builtin_amdgcn_readfirstlane(ts / n_parts);
+        part = ts - t * n_parts;
+        const int tiles = __builtin_amdgcn_readfirstlane((a.g.lc + keys - 1) / keys);
+        tile = sink ? t : a.keys_down ? tiles - 1 - t : t + a.sink_tiles;
+        slot = sink ? block : (a.n_sink_parts > 1 ? sinks : 0) + ((long long)(tile - a.sink_tiles) * n_parts + part) * a.g.nkv + kvh;
+    }
+    // first of n blocks of rows that part i takes
+    __device__ __forceinline__ int first_of(int n, int i) const
+    {
+        if (n_parts == 1) return i * n;
+        const int each = __builtin_amdgcn_readfirstlane(n / n_parts), rest = n - each * n_parts;
+        return i * each + (i < rest ? i : rest);
+    }
+};
+#else
+struct WinUnit;
+#endif
 
 // Argument blocks of kernels that serve both: WIN, under a window.
 template <bool WIN> struct WinOr { using Fwd = FwdArgs; using Bwd = BwdArgs; };
@@ -183,18 +222,51 @@ inline size_t hexi_win_fwd_workspace(int n_splits, int nq, long long lq, int d)
     return n_splits > 1 ? (size_t)n_splits * (size_t)lq * (size_t)nq * (size_t)(d + 1) * sizeof(float) : 0;
 }
 
-// What the rows of a shard see of a chunk, and what sees its keys, from 16 of each: the share that sees (is seen by) anything, and the keys (rows) of one that does.
-struct WinLoad { double share, mean; };
+// Parts of the rows of a tile of sinks and of another one in the backward, by the descriptor, the window and the lengths alone.  A part is left with `least` rows of all heads, and a
+// tile is cut if that takes as many off its chain: 1024 rows of bf16 or 384 of fp32 are about 8 us, the join 4.  Sinks, which all later rows see, are cut to the other tiles' length or
+// to 0.7 of what a CU has of all units (a unit's start and end counted as `least` rows, dQ's rows as 0.6), whichever is more; other tiles, where they are fewer than half the CUs, to what
+// a CU has of them.  us, in one / in parts: bf16, 3/1 heads of 1269 rows, window 121, a sink 36 / 20; fp32, 6/3 of 498, 37, four sinks 53 / 33, 2/1 of 3798, 432, 128 sinks 266 / 104, 4/1
+// of 2766 and the step in front of them, 1086, a sink 537 / 100.
+struct WinBwdPlan { int n_sink_parts, n_parts; };
+inline WinBwdPlan hexi_win_bwd_plan(int dtype, int nq, int nkv, long long lq, long long lc, long long window, long long n_sink)
+{
+    const long long least = dtype == HEXI_BF16 ? 1024 : 384, sinks = n_sink < lc ? n_sink : lc;
+    const long long all = lq * nq / nkv, chain = (window < lq ? window : lq) * nq / nkv;      // rows of all heads that a sink's tile walks, another's
+    auto parts_of = [&](long long rows, long long target, long long keys) {
+        const long long units = (keys + 31) / 32 * nkv;
+        target = target > least ? target : least;
+        if (rows - target < least || units > 256) return 1;
+        const long long n = (rows + target - 1) / target, most = 512 / units;
+        return (int)(n < most ? n : most);
+    };
+    WinBwdPlan plan = {1, 1};
+    const long long units = (lc + 31) / 32 * nkv;
+    const double keys = (double)(window < lc ? window : lc) + sinks;
+    const double even = 0.7 * (units * (double)(chain + least) + 0.6 * ((lq + 31) / 32 * nq) * ((keys < lc ? keys : lc) + least)) / 256.0;
+    if (units <= 128) plan.n_parts = parts_of(chain, chain * units / 256, lc);
+    if (sinks > 0) plan.n_sink_parts = parts_of(all, chain / plan.n_parts > even ? chain / plan.n_parts : (long long)even, sinks);
+    return plan;
+}
+inline size_t hexi_win_bwd_workspace(const WinBwdPlan& plan, int nkv, int d, long long lc, long long n_sink)
+{
+    const long long sinks = n_sink < lc ? n_sink : lc;
+    const long long keys = (plan.n_sink_parts > 1 ? plan.n_sink_parts * (sinks + 63) : 0) + (plan.n_parts > 1 ? plan.n_parts * (lc + 63) : 0);
+    return (size_t)keys * (size_t)nkv * (size_t)d * 2 * sizeof(float);
+}
+
+// What the rows of a shard see of a chunk, and what sees its keys, from 16 of each: the share that sees (is seen by) anything, and the keys (rows) of one that does, on average and at most.
+struct WinLoad { double share, mean, most; };
 template <class F> inline WinLoad hexi_win_load(int n, F count)
 {
-    int some = 0;
+    int some = 0, most = 0;
     double sum = 0.0;
     for (int i = 0; i < 16; ++i) {
         const int c = count((int)((long long)n * (2 * i + 1) / 32));
         some += c > 0;
+        most = c > most ? c : most;
         sum += c;
     }
-    return {some / 16.0, some ? sum / some : 0.0};
+    return {some / 16.0, some ? sum / some : 0.0, (double)most};
 }
 inline WinLoad hexi_win_row_load(const AttnGeom& g, int window, int n_sink)
 {
@@ -241,7 +313,8 @@ inline bool hexi_win_bwd_split(const AttnGeom& g, int window, int n_sink, bool d
         const int n = split ? 32 : 64, step = split ? 256 : 128;
         const double q = f.q_fixed + f.q_step * (keys.mean + n + 30) / step, k = f.k_fixed + f.k_step * (rows.mean + n + 30) * g.nq / g.nkv / step;
         const double sum = (dq ? keys.share * ((g.lq + n - 1) / n) * g.nq * q : 0.0) + (dkdv ? rows.share * ((g.lc + n - 1) / n) * g.nkv * k : 0.0);
-        const double longest = dq && (!dkdv || q > k) ? q : k, even = sum / 256.0 + f.rest * longest;
+        const double q_most = f.q_fixed + f.q_step * (keys.most + n + 30) / step, k_most = f.k_fixed + f.k_step * (rows.most + n + 30) * g.nq / g.nkv / step;
+        const double longest = dq && (!dkdv || q_most > k_most) ? q_most : k_most, even = sum / 256.0 + f.rest * (dq && (!dkdv || q > k) ? q : k);
         return f.base + (longest > even ? longest : even);
     };
     return us(1) < us(0);
@@ -265,7 +338,8 @@ inline bool hexi_win_f32_split(int part, const AttnGeom& g, int window, int n_si
         const double chain = (load.mean + rows - 1) * (part == 2 ? (double)g.nq / g.nkv : 1.0) / (shape ? 128.0 : 32.0);
         double rounds = units > 256.0 ? units / 256.0 : 1.0;
         if (!shape && g.d == 128 && units > 256.0 && rounds < 1.6) rounds = 1.6;
-        return f.base + rounds * (f.fixed + f.step * chain);
+        const double longest = f.fixed + f.step * (load.most + rows - 1) * (part == 2 ? (double)g.nq / g.nkv : 1.0) / (shape ? 128.0 : 32.0), even = rounds * (f.fixed + f.step * chain);
+        return f.base + (longest > even ? longest : even);
     };
     return us(1) <= us(0);
 }
@@ -289,6 +363,8 @@ inline void hexi_head_run_of_each_kv(const signed char* kv_of_q, int nq, int nkv
 // Launchers.
 hipError_t hexi_launch_win_fwd(const WinFwdArgs& a, int dtype, hipStream_t s);
 hipError_t hexi_launch_win_bwd(const WinBwdArgs& a, int dtype, hipStream_t s);
+WinBwdArgs hexi_win_tiles_of(const WinBwdArgs& a, int keys);      // in hexi_win.hip: the arguments for tiles of so many keys, and the parts of such tiles added up
+hipError_t hexi_launch_win_parts(const WinBwdArgs& a, int dtype, int keys, hipStream_t s);
 hipError_t hexi_launch_win_few(const WinFwdArgs& a, int dtype, hipStream_t s);      // in hexi_win_few.hip
 hipError_t hexi_launch_win_join(const WinFwdArgs& a, hipStream_t s);
 hipError_t hexi_launch_win_fwd_large_bf16(const WinFwdArgs& a, hipStream_t s);      // in hexi_bf16_fwd.hip: 256-row workgroups

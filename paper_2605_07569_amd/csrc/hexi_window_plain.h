@@ -193,4 +193,15 @@ template <class T, int D> __device__ __forceinline__ void dkdv_unit(const WinBwd
     }
 }
 
+// dk and dv of keys that no row of the unit's part sees: zeros, to its slot or, unless they would be added, to the outputs.
+template <int D> __device__ __forceinline__ void no_dkdv(const WinBwdArgs& a, const WinUnit& unit, const int keys)
+{
+    for (int i = (int)threadIdx.x; i < keys * (D / 4); i += (int)blockDim.x)
+        for (int which = 0; which < 2; ++which) {
+            const int key = unit.tile * keys + i / (D / 4);
+            if (unit.n_parts > 1) store4(a.part, (unit.slot * 2 + which) * (keys * D) + 4 * i, false, 0.f, 0.f, 0.f, 0.f);
+            else if (!a.accumulate && key < a.g.lc) store4(which ? a.dk : a.dv, ((long long)key * a.g.nkv + unit.kvh) * D + 4 * (i % (D / 4)), a.out_bf16, 0.f, 0.f, 0.f, 0.f);
+        }
+}
+
 } }  // namespace win_plain

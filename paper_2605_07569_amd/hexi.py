@@ -20,7 +20,7 @@ HEXI_MAX_SEGS = 16
 HEXI_ROPE_HALF, HEXI_ROPE_ADJACENT, HEXI_ROPE_INVERSE = 0, 1, 16
 
 EXPORTS = ("hexi_shard_mask", "hexi_attn_fwd_chunk", "hexi_attn_merge_lse", "hexi_attn_bwd_chunk",
-           "hexi_attn_win_workspace_bytes", "hexi_attn_win_fwd_chunk", "hexi_attn_win_bwd_chunk", "hexi_rope", "hexi_rope_a2a_pack", "hexi_rope_a2a_unpack",
+           "hexi_attn_win_workspace_bytes", "hexi_attn_win_fwd_chunk", "hexi_attn_win_bwd_workspace_bytes", "hexi_attn_win_bwd_chunk", "hexi_rope", "hexi_rope_a2a_pack", "hexi_rope_a2a_unpack",
            "hexi_a2a_pack", "hexi_a2a_unpack", "hexi_sched_cost", "hexi_sched_solve", "hexi_set_dkdv_run_len", "hexi_workspace_bytes", "hexi_last_error", "hexi_version")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -92,7 +92,9 @@ def load():
     lib.hexi_attn_win_workspace_bytes.restype = ctypes.c_size_t
     lib.hexi_attn_win_fwd_chunk.argtypes = [dp, wp, rp, rp, vp, vp, vp, vp, i32, vp, u32, vp, ctypes.c_size_t, vp]
     lib.hexi_attn_win_fwd_chunk.restype = ctypes.c_int
-    lib.hexi_attn_win_bwd_chunk.argtypes = [dp, wp, rp, rp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, u32, vp]
+    lib.hexi_attn_win_bwd_chunk.argtypes = [dp, wp, rp, rp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, i32, u32, vp, ctypes.c_size_t, vp]
+    lib.hexi_attn_win_bwd_workspace_bytes.argtypes = [dp, wp, i64, i64]
+    lib.hexi_attn_win_bwd_workspace_bytes.restype = ctypes.c_size_t
     lib.hexi_attn_win_bwd_chunk.restype = ctypes.c_int
     i32p = ctypes.POINTER(i32)
     op = ctypes.POINTER(hexi_rope_desc)
@@ -330,6 +332,10 @@ def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
     return int(load().hexi_attn_win_workspace_bytes(ctypes.byref(desc), ctypes.byref(window), lq, lc))
 
 
+def hexi_attn_win_bwd_workspace_bytes(desc, window, lq, lc):
+    return int(load().hexi_attn_win_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(window), lq, lc))
+
+
 def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flags=0, workspace=None, stream=None):
     """Windowed forward; o's element type (fp32 or bf16) is the result's."""
     qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse)
@@ -346,8 +352,9 @@ def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flag
         _check(rc)
 
 
-def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq, dk, dv, flags=0, stream=None):
-    """Windowed backward; the element type of dq, dk and dv (one for all; None for the half that is skipped) is the gradients'."""
+def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq, dk, dv, flags=0, workspace=None, stream=None):
+    """Windowed backward; the element type of dq, dk and dv (one for all; None for the half that is skipped) is the gradients'.  workspace: a tensor of at least
+    hexi_attn_win_bwd_workspace_bytes; None takes one from torch for the call where one is of use (on the current stream: none, and a slower call, on a stream given by hand)."""
     qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o)
     _fits("delta", delta, (nq, lq), HEXI_F32, dev)
     o_type = grad = HEXI_F32
@@ -360,8 +367,17 @@ def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse,
     for name, t, shape in (("dq", dq, (lq, nq, d)), ("dk", dk, (lc, nkv, d)), ("dv", dv, (lc, nkv, d))):
         if t is not None:
             _fits(name, t, shape, grad, dev)
-    rc = (_lib or load()).hexi_attn_win_bwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(o), o_type, d_o.data_ptr(), lse.data_ptr(),
-                                                  delta.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), grad, flags, _stream(stream))
+    lib, ws_bytes = _lib or load(), 0
+    if workspace is not None:
+        if workspace.get_device() != dev:
+            _refuse(f"workspace is on {workspace.device}, not on the current GPU")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    elif stream is None and not flags & HEXI_SKIP_DKDV:
+        ws_bytes = lib.hexi_attn_win_bwd_workspace_bytes(desc, window, lq, lc)
+        if ws_bytes:
+            workspace = _torch.empty(ws_bytes, dtype=_torch.uint8, device=q.device)
+    rc = lib.hexi_attn_win_bwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(o), o_type, d_o.data_ptr(), lse.data_ptr(),
+                                     delta.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), grad, flags, _ptr(workspace), ws_bytes, _stream(stream))
     if rc:
         _check(rc)
 

@@ -2,7 +2,8 @@
 //   window n_sink  q range  kv range   (ranges as read_segs reads them)
 // prints for every q row "sink:lo:hi", "|", then for every key "first:end".  Or
 //   large nq nkv head_dim  window n_sink  q range  kv range
-// prints whether a bf16 forward call takes 256-row workgroups, and whether a backward call of everything takes 32-row ones.
+// prints whether a bf16 forward call takes 256-row workgroups, whether a backward call of everything takes 32-row ones, ":" and into how many parts that
+// divides the rows of a tile of sinks, ":" and of another one.
 #include <cstdio>
 #include <iostream>
 #include <sstream>
@@ -24,7 +25,8 @@ int main()
             g.ks = read_segs(is);
             g.lq = g.qs.total;
             g.lc = g.ks.total;
-            std::printf("%d%d\n", (int)hexi_win_fwd_large(g, window, n_sink), (int)hexi_win_bwd_split(g, window, n_sink, true, true));
+            const WinBwdPlan plan = hexi_win_bwd_plan(HEXI_BF16, g.nq, g.nkv, g.lq, g.lc, window, n_sink);
+            std::printf("%d%d:%d:%d\n", (int)hexi_win_fwd_large(g, window, n_sink), (int)hexi_win_bwd_split(g, window, n_sink, true, true), plan.n_sink_parts, plan.n_parts);
             continue;
         }
         is >> window >> n_sink;

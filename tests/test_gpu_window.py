@@ -155,11 +155,68 @@ def _rel_of(pair, rel):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("c", wu.MANY, ids=lambda c: c.name)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("c", wu.PARTS, ids=lambda c: c.name)
+def test_backward_in_parts(c, dtype, d):
+    """With the workspace that a call takes by itself, with one given, and with none; a value that is not finite; the sums added to what is there."""
+    x, dev, desc, window = setup(c, dtype, d, 15)
+    ro, rl, _, _ = wu.forward(c, x, F32)
+    lse, o = rl.float(), ro.float()
+    need = hexi.hexi_attn_win_bwd_workspace_bytes(desc, window, c.lq, c.lc)
+    assert need > 0
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device=DEV)
+    delta = torch.empty(c.nq, c.lq, device=DEV)
+    lib, (qr, kr) = hexi.load(), (hexi.make_range(c.q_segs)[0], hexi.make_range(c.kv_segs)[0])
+
+    def run(grad, inputs=dev, how=None, fill=float("nan"), flags=0):
+        f1, dq = guarded((c.lq, c.nq, d), grad, 0.0)
+        f2, dk = guarded((c.lc, c.nkv, d), grad, fill)
+        f3, dv = guarded((c.lc, c.nkv, d), grad, fill)
+        flags |= hexi.HEXI_COMPUTE_DELTA
+        if how == "none":
+            code = hexi.HEXI_BF16 if grad == BF16 else hexi.HEXI_F32
+            assert lib.hexi_attn_win_bwd_chunk(desc, window, qr, kr, *(inputs[n].data_ptr() for n in ("q", "k", "v")), o_dev.data_ptr(), hexi.HEXI_F32, inputs["d_o"].data_ptr(),
+                                               lse_dev.data_ptr(), delta.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), code, flags, None, 0,
+                                               torch.cuda.current_stream().cuda_stream) == hexi.HEXI_OK
+        else:
+            hexi.hexi_attn_win_bwd_chunk(desc, window, qr, kr, inputs["q"], inputs["k"], inputs["v"], o_dev, inputs["d_o"], lse_dev, delta, dq, dk, dv, flags=flags,
+                                         workspace=ws[:need] if how == "given" else None)
+        torch.cuda.synchronize()
+        untouched(f1, f2, f3)
+        assert torch.all(ws[need:] == 255)
+        return dict(dq=dq, dk=dk, dv=dv)
+
+    o_dev, lse_dev = o.to(DEV), lse.to(DEV)
+    for grad in (F32, BF16):
+        print(f"\n  {c.name}: {dtype} d={d} -> {grad}", flush=True)
+        ref = wu.backward(c, x, o, lse, grad)
+        rel = max(REL[dtype], 0 if grad == F32 else REL[BF16])
+        got = run(grad)
+        again, none = run(grad, how="given"), run(grad, how="none")
+        for name in got:
+            wu.within(name, got[name], *ref[name], rel)
+            wu.within(name + " without a workspace", none[name], *ref[name], rel)
+            assert torch.equal(got[name], again[name])
+    ref = wu.backward(c, x, o, lse, F32)
+    got = run(F32, fill=0.25, flags=hexi.HEXI_ACCUMULATE)
+    for name in ("dk", "dv"):
+        wu.within("added " + name, got[name] - 0.25, ref[name][0], ref[name][1] + 2.0 ** -23 + 2 * wu.U * ref[name][0].abs())
+    seen = wu.visible(c)
+    for where, at in (("q", c.lq // 2), ("d_o", c.lq - 1), ("k", 1)):
+        bad = x[where].clone()
+        bad[at, 0, 5] = float("inf")
+        got = run(F32, dict(dev, **{where: wu.strided(bad, c.pad, DEV)}))
+        rows, keys = (seen[:, at], torch.arange(c.lc) == at) if where == "k" else (torch.arange(c.lq) == at, seen[at])
+        for name, hit in (("dq", rows), ("dk", keys), ("dv", keys)):
+            wu.within(name + " of the others", got[name].cpu()[~hit], ref[name][0][~hit], ref[name][1][~hit])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("c", wu.MANY + [wu.MANY_PARTS], ids=lambda c: c.name)
 def test_backward_in_64_row_workgroups(c, d):
     """All heads at once, two kv heads looked at; rows whose LSE is infinite, and then a value that is not finite in one of each input."""
     x, dev, desc, window = setup(c, BF16, d, 13)
-    group, kv = c.nq // c.nkv, [0, 33]
+    group, kv = c.nq // c.nkv, [0, min(33, c.nkv - 1)]
     heads = [h * group + i for h in kv for i in range(group)]
     sub = Case(c.name, c.q_segs, c.kv_segs, c.window, c.n_sink, len(heads), len(kv))
     some = dict(q=x["q"][:, heads], k=x["k"][:, kv], v=x["v"][:, kv], d_o=x["d_o"][:, heads])
@@ -192,7 +249,7 @@ def test_backward_in_64_row_workgroups(c, d):
             wu.within(name, got[name], ref[name][0], ref[name][1] + (2.0 ** -22 if name == "dq" else 0.0), REL[BF16])
         assert all(torch.isfinite(t.float()).all() for t in whole)
     ref = wu.backward(sub, some, ro.float(), lse, F32)
-    for where, at, head in (("k", c.lc // 2, 33), ("v", c.lc - 1, 0), ("q", c.lq // 3, 67), ("d_o", c.lq - 2, 0)):
+    for where, at, head in (("k", c.lc // 2, kv[-1]), ("v", c.lc - 1, 0), ("q", c.lq // 3, heads[-1]), ("d_o", c.lq - 2, 0)):
         bad = x[where].clone()
         bad[at, head, 5] = float("nan")
         got, *_ = run(F32, dict(dev, **{where: wu.strided(bad, c.pad, DEV)}))

@@ -68,8 +68,12 @@ def test_which_workgroups_the_steps_take(window_binary):
                                                                            for c in cases) + "\n", capture_output=True, text=True, check=True).stdout.split()
     assert [x[0] for x in ask(wu.LARGE, 128)] == ["1"] * len(wu.LARGE) and [x[0] for x in ask(wu.LARGE, 64)] == ["0"] * len(wu.LARGE)
     for d in (64, 128):
-        assert ask(wu.CASES, d) == ["01"] * len(wu.CASES)
+        assert [x[:2] for x in ask(wu.CASES, d)] == ["01"] * len(wu.CASES)
         assert [x[1] for x in ask(wu.MANY, d)] == ["0"] * len(wu.MANY)
+        assert [[p != "1" for p in x.split(":")[1:]] for x in ask(wu.PARTS, d)] == [[True, False], [True, False], [False, True], [True, True], [True, False], [True, True], [True, False]]
+        assert [x[1] for x in ask(wu.PARTS, d)] == ["1"] * len(wu.PARTS)
+        many = ask([wu.MANY_PARTS], d)[0]
+        assert many[1] == "0" and int(many.split(":")[1]) > 1
 
 
 def _codes(call, good, bad):
@@ -120,7 +124,7 @@ def test_windowed_backward_refusals():
 
     def call(q=16, k=16, v=16, o=16, d_o=16, lse=16, delta=16, dq=16, dk=16, dv=16, o_dtype=hexi.HEXI_F32, grad=hexi.HEXI_BF16, flags=hexi.HEXI_COMPUTE_DELTA, **kw):
         desc, win, qr, kr = _common(**kw)
-        return lib.hexi_attn_win_bwd_chunk(ctypes.byref(desc), win, ctypes.byref(qr), ctypes.byref(kr), q, k, v, o, o_dtype, d_o, lse, delta, dq, dk, dv, grad, flags, None)
+        return lib.hexi_attn_win_bwd_chunk(ctypes.byref(desc), win, ctypes.byref(qr), ctypes.byref(kr), q, k, v, o, o_dtype, d_o, lse, delta, dq, dk, dv, grad, flags, None, 0, None)
 
     good = dict(DESC, q_segs=[(4, 4)], kv_segs=[(0, 8)], window=3, n_sink=1, no_window=False)
     names = ("q", "k", "v", "o", "d_o", "lse", "delta", "dq", "dk", "dv")
@@ -128,6 +132,15 @@ def test_windowed_backward_refusals():
            [(hexi.HEXI_EUNSUPPORTED, dict(o_dtype=2)), (hexi.HEXI_EUNSUPPORTED, dict(grad=3)), (hexi.HEXI_EINVAL, dict(flags=32)), (hexi.HEXI_EINVAL, dict(flags=hexi.HEXI_ACCUMULATE)),
             (hexi.HEXI_EINVAL, dict(flags=hexi.HEXI_SKIP_DQ | hexi.HEXI_SKIP_DKDV)), (hexi.HEXI_EINVAL, dict(flags=hexi.HEXI_SKIP_DQ, dk=None)),
             (hexi.HEXI_EINVAL, dict(flags=hexi.HEXI_SKIP_DKDV, dq=None))])
+    # many rows behind sinks are of use in parts; the workspace is asked for by the lengths alone, and may be left out
+    desc, win = hexi.make_desc(hexi.HEXI_BF16, 128, 8, 1, 0.1, (1024, 128), (128, 128)), hexi.make_window(1024, 4)
+    size = hexi.hexi_attn_win_bwd_workspace_bytes
+    need = size(desc, win, 16384, 17408)
+    assert need > 0 and size(desc, win, 512, 17408) == 0 and size(desc, hexi.make_window(1024), 16384, 17408) == 0
+    assert size(desc, hexi.make_window(0, 4), 16384, 17408) == 0 and size(desc, win, 0, 17408) == 0 and lib.hexi_attn_win_bwd_workspace_bytes(None, None, 5, 5) == 0
+    qr, kr = hexi.make_range([(1024, 16384)])[0], hexi.make_range([(0, 17408)])[0]
+    for ws, n, code in ((16, need - 1, hexi.HEXI_EWORKSPACE), (24, need, hexi.HEXI_EALIGN)):
+        assert lib.hexi_attn_win_bwd_chunk(desc, win, qr, kr, 16, 16, 16, 16, hexi.HEXI_BF16, 16, 16, 16, 16, 16, 16, hexi.HEXI_BF16, 0, ws, n, None) == code
 
 
 def test_rope_refusals():

@@ -89,6 +89,19 @@ LARGE = [
 # The same steps with two q heads to a kv head: their backward takes 64-row workgroups, that of CASES 32-row ones.
 MANY = [replace(c, nq=128, nkv=64) for c in LARGE]
 
+# Steps whose dK / dV units walk their rows in parts: the sinks', all, both; keys behind the sinks in their tile, sinks that only some of the chunk's rows see, sinks elsewhere, a
+# step in the future of most of them.
+PARTS = [
+    Case("sinks", [(100, 3000)], [(0, 3100)], 50, 20, nq=2, nkv=1),
+    Case("sinks of two tiles", [(40, 2100), (9000, 901)], [(0, 70), (8700, 1201)], 300, 67, nq=6, nkv=2, kv_of_q=[0, 1, 1, 0, 1, 1]),
+    Case("all", [(300, 2501)], [(0, 601)], 10 ** 6, 0, nq=8, nkv=1),
+    Case("all and sinks", [(0, 3333)], [(0, 400)], 700, 33, nq=8, nkv=1, k_scale=2.0),
+    Case("sinks elsewhere", [(5000, 3000)], [(4900, 700)], 101, 16, nq=2, nkv=1),
+    Case("mostly in the future", [(0, 3001)], [(2800, 500)], 2500, 3000, nq=4, nkv=1),
+    Case("strides", [(1000, 2222)], [(3, 5), (700, 2522)], 222, 7, nq=3, nkv=1, pad=16),
+]
+MANY_PARTS = Case("many heads", [(500, 1333)], [(0, 40), (460, 1373)], 40, 30, nq=64, nkv=8)
+
 
 def positions(segs):
     return torch.cat([torch.arange(s, s + n, dtype=torch.int64) for s, n in segs])
