@@ -223,20 +223,20 @@ inline size_t hexi_win_fwd_workspace(int n_splits, int nq, long long lq, int d)
 }
 
 // Parts of the rows of a tile of sinks and of another one in the backward, by the descriptor, the window and the lengths alone.  A part is left with `least` rows of all heads, and a
-// tile is cut if that takes as many off its chain: 1024 rows of bf16 or 384 of fp32 are about 8 us, the join 4.  Sinks, which all later rows see, are cut to the other tiles' length or
+// tile is cut if that takes as many off its chain: 1024 rows of bf16 or 256 of fp32 are about 8 us, the join 4.  Sinks, which all later rows see, are cut to the other tiles' length or
 // to 0.7 of what a CU has of all units (a unit's start and end counted as `least` rows, dQ's rows as 0.6), whichever is more; other tiles, where they are fewer than half the CUs, to what
 // a CU has of them.  us, in one / in parts: bf16, 3/1 heads of 1269 rows, window 121, a sink 36 / 20; fp32, 6/3 of 498, 37, four sinks 53 / 33, 2/1 of 3798, 432, 128 sinks 266 / 104, 4/1
 // of 2766 and the step in front of them, 1086, a sink 537 / 100.
 struct WinBwdPlan { int n_sink_parts, n_parts; };
 inline WinBwdPlan hexi_win_bwd_plan(int dtype, int nq, int nkv, long long lq, long long lc, long long window, long long n_sink)
 {
-    const long long least = dtype == HEXI_BF16 ? 1024 : 384, sinks = n_sink < lc ? n_sink : lc;
+    const long long least = dtype == HEXI_BF16 ? 1024 : 256, sinks = n_sink < lc ? n_sink : lc;
     const long long all = lq * nq / nkv, chain = (window < lq ? window : lq) * nq / nkv;      // rows of all heads that a sink's tile walks, another's
     auto parts_of = [&](long long rows, long long target, long long keys) {
         const long long units = (keys + 31) / 32 * nkv;
         target = target > least ? target : least;
         if (rows - target < least || units > 256) return 1;
-        const long long n = (rows + target - 1) / target, most = 512 / units;
+        const long long n = (rows + target - 1) / target, most = units > 16 ? 512 / units : 32;
         return (int)(n < most ? n : most);
     };
     WinBwdPlan plan = {1, 1};

@@ -489,3 +489,53 @@ def test_streams_graphs_and_repeats(dtype):
     step(eager)
     torch.cuda.synchronize()
     assert all(torch.equal(got[n], eager[n]) for n in got) and not torch.equal(got["o"], want["o"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_parts_on_streams_and_in_graphs(dtype):
+    """A backward that takes a workspace by itself: on two streams at once, captured and replayed among eager calls, on a stream given by hand (without one)."""
+    c, d = wu.PARTS[0], 64
+    x, dev, desc, window = setup(c, dtype, d, 17)
+    ro, rl, _, _ = wu.forward(c, x, F32)
+    o, lse = ro.float().to(DEV), rl.float().to(DEV)
+    ref = wu.backward(c, x, ro.float(), rl.float(), dtype)
+    assert hexi.hexi_attn_win_bwd_workspace_bytes(desc, window, c.lq, c.lc) > 0
+
+    def buffers():
+        e = lambda *s, t=dtype: torch.zeros(s, dtype=t, device=DEV)
+        return dict(delta=e(c.nq, c.lq, t=F32), dq=e(c.lq, c.nq, d), dk=e(c.lc, c.nkv, d), dv=e(c.lc, c.nkv, d))
+
+    def run(b, **kw):
+        b["dq"].zero_()
+        hexi.hexi_attn_win_bwd_chunk(desc, window, c.q_segs, c.kv_segs, dev["q"], dev["k"], dev["v"], o, dev["d_o"], lse, b["delta"], b["dq"], b["dk"], b["dv"],
+                                     flags=hexi.HEXI_COMPUTE_DELTA, **kw)
+
+    want = buffers()
+    run(want)
+    torch.cuda.synchronize()
+    same = lambda b: all(torch.equal(b[n], want[n]) for n in want)
+    two, streams = [buffers(), buffers()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for b, stream in zip(two, streams):
+            with torch.cuda.stream(stream):
+                run(b)
+    torch.cuda.synchronize()
+    assert same(two[0]) and same(two[1])
+    captured, eager = buffers(), buffers()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(captured)
+    for _ in range(4):
+        captured["dk"].fill_(float("nan"))
+        captured["dv"].fill_(float("nan"))
+        graph.replay()
+        run(eager)
+        torch.cuda.synchronize()
+        assert same(captured) and same(eager)
+    b = buffers()
+    torch.cuda.synchronize()
+    run(b, stream=torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for name in ("dq", "dk", "dv"):
+        wu.within(name, b[name], *ref[name], max(REL[dtype], 0 if dtype == F32 else REL[BF16]))
