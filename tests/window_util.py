@@ -102,6 +102,30 @@ PARTS = [
 ]
 MANY_PARTS = Case("many heads", [(500, 1333)], [(0, 40), (460, 1373)], 40, 30, nq=64, nkv=8)
 
+# Steps whose forward takes 64-row units, whole, in bf16 and fp32 at both head_dims
+FORWARD_64 = [
+    Case("mid-size", [(500, 333)], [(0, 9), (380, 453)], 121, 9, nq=64, nkv=16),
+    Case("ring step", [(700, 300)], [(500, 230)], 150, 0, nq=96, nkv=8),                  # later rows see nothing
+    Case("rows without keys", [(50, 60), (3000, 271)], [(300, 2500), (2890, 201)], 70, 0, nq=128, nkv=4),
+    Case("gaps", [(7 + 50 * i, 11 + 2 * i) for i in range(16)], [(40 * i, 9 + 2 * i) for i in range(16)], 95, 50, nq=64, nkv=8, kv_of_q=[(5 * h + h // 7) % 8 for h in range(64)]),
+    Case("strides", [(2000, 257)], [(1901, 356)], 101, 0, nq=60, nkv=12, k_scale=2.0, pad=16),
+    Case("sinks of the step", [(9000, 259)], [(0, 130)], 64, 100, nq=64, nkv=64),
+    Case("everything", [(40, 250)], [(0, 290)], 10 ** 9, 0, nq=96, nkv=32),
+]
+# and, in bf16, in splits of their keys
+FORWARD_64_SPLITS = [
+    Case("long window", [(8000, 40)], [(0, 8040)], 7001, 0, nq=32, nkv=8),
+    Case("long window, sinks", [(8000, 60)], [(0, 70), (1000, 7060)], 7001, 67, nq=16, nkv=2, kv_of_q=[1, 0, 0, 1] * 4),
+]
+# Steps whose fp32 backward takes 64-row dQ and 64-key dK / dV units, whole and in parts (a name says which)
+BACKWARD_64 = [
+    Case("whole", [(40, 700)], [(0, 820)], 20, 0, nq=32, nkv=32),
+    Case("whole, ring step", [(900, 1111)], [(300, 720)], 150, 0, nq=64, nkv=64),
+    Case("whole, strides", [(900, 877)], [(0, 7), (889, 888)], 11, 5, nq=24, nkv=24, pad=16),
+    Case("parts", [(500, 1133)], [(0, 5), (480, 1153)], 21, 3, nq=16, nkv=16),
+    Case("parts, heads", [(900, 1377)], [(0, 40), (880, 1397)], 20, 37, nq=32, nkv=16, kv_of_q=[(5 * h + h // 7) % 16 for h in range(32)]),
+]
+
 
 def positions(segs):
     return torch.cat([torch.arange(s, s + n, dtype=torch.int64) for s, n in segs])
