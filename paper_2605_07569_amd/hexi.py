@@ -354,7 +354,8 @@ def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flag
 
 def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse, delta, dq, dk, dv, flags=0, workspace=None, stream=None):
     """Windowed backward; the element type of dq, dk and dv (one for all; None for the half that is skipped) is the gradients'.  workspace: a tensor of at least
-    hexi_attn_win_bwd_workspace_bytes; None takes one from torch for the call where one is of use (on the current stream: none, and a slower call, on a stream given by hand)."""
+    hexi_attn_win_bwd_workspace_bytes; None takes one from torch for the call where one is of use (none, and a slower call whose sums have another order, on a stream given by
+    hand that is being captured by other means than torch.cuda.graph)."""
     qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o)
     _fits("delta", delta, (nq, lq), HEXI_F32, dev)
     o_type = grad = HEXI_F32
@@ -372,14 +373,29 @@ def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse,
         if workspace.get_device() != dev:
             _refuse(f"workspace is on {workspace.device}, not on the current GPU")
         ws_bytes = workspace.numel() * workspace.element_size()
-    elif stream is None and not flags & HEXI_SKIP_DKDV:
+    elif not flags & HEXI_SKIP_DKDV:
         ws_bytes = lib.hexi_attn_win_bwd_workspace_bytes(desc, window, lq, lc)
-        if ws_bytes:
+        if ws_bytes and stream is None:
             workspace = _torch.empty(ws_bytes, dtype=_torch.uint8, device=q.device)
-    rc = lib.hexi_attn_win_bwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(o), o_type, d_o.data_ptr(), lse.data_ptr(),
-                                     delta.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), grad, flags, _ptr(workspace), ws_bytes, _stream(stream))
+    space, handle = _ptr(workspace), _stream(stream)
+    taken = _take(lib, ws_bytes, dev, handle) if ws_bytes and space is None else None
+    try:
+        rc = lib.hexi_attn_win_bwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(o), o_type, d_o.data_ptr(), lse.data_ptr(),
+                                         delta.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), grad, flags, taken if space is None else space, ws_bytes, handle)
+    finally:
+        if taken is not None:
+            _torch.cuda.caching_allocator_delete(taken)
     if rc:
         _check(rc)
+
+
+def _take(lib, n, dev, handle):
+    """n bytes from torch's allocator that belong to the stream of this handle: given back, they serve what follows on it.  None on a stream that is being captured while
+    torch's current one is not: torch does not know of that graph, and would hand the bytes out again while it lives."""
+    status = ctypes.c_int(0)
+    if (lib.hipStreamIsCapturing(ctypes.c_void_p(handle), ctypes.byref(status)) != 0 or status.value != 0) and not _torch.cuda.is_current_stream_capturing():
+        return None
+    return _torch.cuda.caching_allocator_alloc(n, dev, handle)
 
 
 def make_rope(head_dim, inv_freq, axis_of_pair=None, pairing="half", n_axes=None):
