@@ -29,5 +29,18 @@ struct RopeParts {
     long long x_stride_tok;           // of the [rows][heads] side, elements
 };
 
+// Tokens of a workgroup of 256 threads, and workgroups, for so many 16-byte pieces a token (n_slots heads' rows): 2 or 3 pieces a thread, so that many workgroups are under way at
+// different places, unless there are too few rows to go round; and more where the launch would have 2^32 threads.
+// us for 1 / 2 / 4 / 16 tokens: 32768 rows of 40 heads (320 pieces a token) 127 / 111 / 114 / 130; 16384 x 54 heads, packed (432) 83 / 70 / 74 / 80; 8191 x 32
+// heads from fp32 to bf16 (512) 41 / 43 / 46 / 45.
+struct RopeShape { int tokens; unsigned grid; };
+inline RopeShape hexi_rope_shape(int rows, unsigned pieces)
+{
+    const long long n = rows, most = pieces < 896 ? 896 / pieces : 1, share = (n + 1023) / 1024, least = (n + (1 << 24) - 2) / ((1 << 24) - 1);
+    long long tokens = most < share ? most : share;
+    tokens = tokens > least ? tokens : least;
+    return {(int)tokens, (unsigned)((n + tokens - 1) / tokens)};
+}
+
 hipError_t hexi_launch_rope(const RopeGeom& g, const RopeTensors& t, int x_dtype, int y_dtype, hipStream_t s);
 hipError_t hexi_launch_rope_a2a(bool pack, const RopeGeom& g, const RopeParts& p, int dtype, hipStream_t s);

@@ -167,13 +167,11 @@ template <class X, class Y, class IN> hipError_t launch(const RopeGeom& g, const
     if (n_slots == 0) return hipSuccess;
     const unsigned row = (unsigned)g.head_dim / (2 * (16 / sizeof(X)));
     const Divisor by_token(row * (unsigned)n_slots), by_row(row);
-    // Tokens of a workgroup: 2 or 3 pieces a thread, so that many workgroups are under way at different places, unless there are too few rows to go round.
-    // us for 1 / 2 / 4 / 16 tokens: 32768 rows of 40 heads (320 pieces a token) 127 / 111 / 114 / 130; 16384 x 54 heads, packed (432) 83 / 70 / 74 / 80; 8191 x 32
-    // heads from fp32 to bf16 (512) 41 / 43 / 46 / 45.
-    const int most = by_token.d < 896 ? 896 / (int)by_token.d : 1, share = (g.rows + 1023) / 1024;
-    const int tokens = most < share ? most : share;
-    const unsigned grid = (unsigned)((g.rows + tokens - 1) / tokens);
-    const size_t lds = 2 * sizeof(float) * (size_t)(tokens * (g.rot_dim / 2));      // at most 896 pieces of 8 pairs: 56 KB
+    const RopeShape shape = hexi_rope_shape(g.rows, by_token.d);
+    const int tokens = shape.tokens;
+    const unsigned grid = shape.grid;
+    const size_t lds = 2 * sizeof(float) * (size_t)tokens * (size_t)(g.rot_dim / 2);      // 896 pieces of 8 pairs: 56 KB
+    if (lds > 65536) return hipErrorInvalidConfiguration;      // (2^30 rows of more than 400 bytes: more than there is memory for)
     if (g.adjacent) rope_kernel<X, Y, IN, true><<<grid, 256, lds, s>>>(g, in, tokens, by_token, by_row);
     else rope_kernel<X, Y, IN, false><<<grid, 256, lds, s>>>(g, in, tokens, by_token, by_row);
     return hipGetLastError();

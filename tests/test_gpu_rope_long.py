@@ -100,3 +100,24 @@ def test_rope_pack_and_unpack(rows, n, d, rot, adjacent, axes, pad, dtype):
     listed[order[n - 1]] = False
     close(yd[:, listed], w[:, listed], b[:, listed], dtype)
     assert torch.all(yd[:, ~listed] == 77.0) and torch.all(y_wide[:, n * d:] == 77.0)
+
+
+def test_rope_on_as_many_rows_as_a_range_can_have():
+    """2^31 - 1 rows of one head of 16 columns, in place (64 GiB): the first and last rows, and those around the ends of workgroups in the middle."""
+    rows, d = 2 ** 31 - 1, 16
+    if torch.cuda.mem_get_info()[0] < 80 * 2 ** 30:
+        pytest.skip("needs 80 GiB of free device memory")
+    freq, axis = freqs(d, 1)
+    at = torch.tensor([0, 1, 895, 896, 2 ** 30 - 1, 2 ** 30, 1198372 * 896 - 1, 1198372 * 896, rows - 1024, rows - 2, rows - 1])
+    x = torch.randn(len(at), 1, d, generator=torch.Generator().manual_seed(2)).to(BF16)
+    big = torch.zeros(rows, 1, d, dtype=BF16, device=DEV)
+    for i, r in enumerate(at.tolist()):
+        big[r] = x[i].to(DEV)
+    hexi.hexi_rope(hexi.make_rope(d, freq, axis), [(0, rows)], [(big, big)])
+    torch.cuda.synchronize()
+    got = torch.stack([big[r] for r in at.tolist()])
+    close(got, *turned(x.double(), at[None], freq, axis, False, False), BF16)
+    beside = torch.stack([big[r] for r in (2, 894, 2 ** 30 + 1, rows - 3)])
+    assert torch.all(beside == 0)
+    del big
+    torch.cuda.empty_cache()
