@@ -411,8 +411,8 @@ template <class C, bool WIN = false> __device__ __forceinline__ void fwd_unit(co
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const float ms = sm.e.m[s * C::ROWS + tid];
-            const float x = ms - m;
-            e[s] = ms == -INFINITY ? 0.f : fast_exp2(fmaf(x, c_hi, x * c_lo));
+            const float x = ms - m;           // (-inf too where the two are finite and far apart: 0, whatever the sign of c_lo)
+            e[s] = ms == -INFINITY ? 0.f : fast_exp2(fmaf(x, c_hi, x == -INFINITY ? 0.f : x * c_lo));
             l += e[s] * sm.e.l[s * C::ROWS + tid];
         }
         const float lse_part = l > 0.f ? fmaf(m, g.scale, logf(l)) : -INFINITY;

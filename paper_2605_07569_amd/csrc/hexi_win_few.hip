@@ -225,7 +225,8 @@ __global__ void __launch_bounds__(64 * NW) win_few_kernel(const FewArgs f, const
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float x = stat[0][w][i] - mm, e = stat[0][w][i] == -INFINITY ? 0.f : fast_exp2(fmaf(x, c_hi, x * c_lo));
+            // (x is -inf too where the two are finite and far apart: 0, whatever the sign of c_lo)
+            const float x = stat[0][w][i] - mm, e = stat[0][w][i] == -INFINITY ? 0.f : fast_exp2(fmaf(x, c_hi, x == -INFINITY ? 0.f : x * c_lo));
             total += e * stat[1][w][i];
             used += e * stat[2][w][i];
             o += e * *reinterpret_cast<const f32x4*>(&acc_of[w][i][c]);
