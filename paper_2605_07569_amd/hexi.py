@@ -328,6 +328,15 @@ def _win_inputs(desc, q_segs, kv_segs, q, k, v, lse, d_o=None):
     return qr, kr, lq, lc, dev, d, nq, nkv
 
 
+def _bytes_of(workspace, dev):
+    """Bytes of a workspace from its first element on."""
+    if workspace.get_device() != dev:
+        _refuse(f"workspace is on {workspace.device}, not on the current GPU")
+    if not workspace.is_contiguous():
+        _refuse(f"workspace: strides {workspace.stride()}; a contiguous tensor is needed")
+    return workspace.numel() * workspace.element_size()
+
+
 def hexi_attn_win_workspace_bytes(desc, window, lq, lc):
     return int(load().hexi_attn_win_workspace_bytes(ctypes.byref(desc), ctypes.byref(window), lq, lc))
 
@@ -341,11 +350,7 @@ def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flag
     qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse)
     o_type = _dtype(o)
     _fits("o", o, (lq, nq, d), o_type, dev)
-    ws_bytes = 0
-    if workspace is not None:
-        if workspace.get_device() != dev:
-            _refuse(f"workspace is on {workspace.device}, not on the current GPU")
-        ws_bytes = workspace.numel() * workspace.element_size()
+    ws_bytes = 0 if workspace is None else _bytes_of(workspace, dev)
     rc = (_lib or load()).hexi_attn_win_fwd_chunk(desc, window, qr, kr, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), o_type, lse.data_ptr(), flags,
                                                   _ptr(workspace), ws_bytes, _stream(stream))
     if rc:
@@ -370,9 +375,7 @@ def hexi_attn_win_bwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, d_o, lse,
             _fits(name, t, shape, grad, dev)
     lib, ws_bytes = _lib or load(), 0
     if workspace is not None:
-        if workspace.get_device() != dev:
-            _refuse(f"workspace is on {workspace.device}, not on the current GPU")
-        ws_bytes = workspace.numel() * workspace.element_size()
+        ws_bytes = _bytes_of(workspace, dev)
     elif not flags & HEXI_SKIP_DKDV:
         ws_bytes = lib.hexi_attn_win_bwd_workspace_bytes(desc, window, lq, lc)
         if ws_bytes and stream is None:
