@@ -235,7 +235,8 @@ typedef struct {
 } hexi_rope_desc;
 
 /* One tensor of a call: x [rows][n_heads][head_dim] -> y, strides in elements, head_dim stride 1.  y may be x itself
- * (same pointer, strides and element type); otherwise the two do not overlap. */
+ * (same pointer, strides and element type); otherwise the two do not overlap, nor does y overlap another tensor's x or y
+ * (HEXI_EINVAL where they start at the same address). */
 typedef struct {
     const void* x;
     void* y;

@@ -499,6 +499,8 @@ HEXI_EXPORT int hexi_rope(const hexi_rope_desc* desc, const hexi_range* range, c
             return fail(HEXI_EINVAL, "tensor %d: in place needs equal strides and element types", i);
         if (!aligned16(t.x) || !aligned16(t.y) || (t.x_stride_tok * xs) % 16 || (t.x_stride_head * xs) % 16 || (t.y_stride_tok * ys) % 16 || (t.y_stride_head * ys) % 16)
             return fail(HEXI_EALIGN, "tensor %d: pointers and strides must be multiples of 16 bytes", i);
+        for (int j = 0; j < i; ++j)
+            if (t.y == tensors[j].y || t.y == tensors[j].x || t.x == tensors[j].y) return fail(HEXI_EINVAL, "tensor %d is written where tensor %d is read or written", t.x == tensors[j].y ? j : i, t.x == tensors[j].y ? i : j);
         all.t[i] = t;
         all.first[i + 1] = all.first[i] + t.n_heads;
     }
