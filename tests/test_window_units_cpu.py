@@ -22,10 +22,12 @@ def units(tmp_path_factory):
                            os.path.join(ROOT, "tests", "host", "window_shapes_check.cpp"), "-o", exe])
     text = lambda segs: f"{len(segs)} " + " ".join(f"{s} {n}" for s, n in segs)
 
-    def ask(cases, dtype, d):
+    def ask(cases, dtype, d, plain=False):
         lines = [f"{dtype} {c.nq} {c.nkv} {d} {min(c.window, 2 ** 31 - 1)} {min(c.n_sink, 2 ** 31 - 1)} {text(c.q_segs)} {text(c.kv_segs)}" for c in cases]
         out = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True, check=True).stdout.splitlines()
         assert len(out) == len(cases)
+        if plain:      # the forward's rows of a unit and number of splits
+            return [tuple(map(int, line.split()[0][3:].split(":"))) for line in out]
         split = lambda word, name: (int(word[len(name):].split(":")[0]), word.split(":")[1] != "1")
         return [(split(f, "fwd"), int(q[2:]), split(k, "dkdv")) for f, q, k in (line.split() for line in out)]
 
