@@ -29,10 +29,10 @@ struct RopeParts {
     long long x_stride_tok;           // of the [rows][heads] side, elements
 };
 
-// Tokens of a workgroup of 256 threads, and workgroups, for so many 16-byte pieces a token (n_slots heads' rows): 2 or 3 pieces a thread, so that many workgroups are under way at
+// Tokens of a workgroup of 256 threads, and workgroups, for so many pieces (two loads of 16 bytes) a token: 2 or 3 pieces a thread, so that many workgroups are under way at
 // different places, unless there are too few rows to go round; and more where the launch would have 2^32 threads.
-// us for 1 / 2 / 4 / 16 tokens: 32768 rows of 40 heads (320 pieces a token) 127 / 111 / 114 / 130; 16384 x 54 heads, packed (432) 83 / 70 / 74 / 80; 8191 x 32
-// heads from fp32 to bf16 (512) 41 / 43 / 46 / 45.
+// us for 1 / 2 / 4 / 16 tokens, 128 columns: 32768 rows of 40 heads (320 pieces a token) 119 / 107 / 112 / 127; 16384 rows of 40 heads packed into 48 slots (384) 79 / 67 / 70 / 78;
+// 8191 rows of 32 heads from fp32 to bf16 (512) 38.5 / 40.8 / 43.6 / 43.1.
 struct RopeShape { int tokens; unsigned grid; };
 inline RopeShape hexi_rope_shape(int rows, unsigned pieces)
 {

@@ -171,7 +171,7 @@ template <class X, class Y, class IN> hipError_t launch(const RopeGeom& g, const
     const int tokens = shape.tokens;
     const unsigned grid = shape.grid;
     const size_t lds = 2 * sizeof(float) * (size_t)tokens * (size_t)(g.rot_dim / 2);      // 896 pieces of 8 pairs: 56 KB
-    if (lds > 65536) return hipErrorInvalidConfiguration;      // (2^30 rows of more than 400 bytes: more than there is memory for)
+    if (lds > 65536) return hipErrorInvalidConfiguration;      // (only where the rows are more bytes than there is memory for)
     if (g.adjacent) rope_kernel<X, Y, IN, true><<<grid, 256, lds, s>>>(g, in, tokens, by_token, by_row);
     else rope_kernel<X, Y, IN, false><<<grid, 256, lds, s>>>(g, in, tokens, by_token, by_row);
     return hipGetLastError();

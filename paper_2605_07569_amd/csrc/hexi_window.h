@@ -321,7 +321,7 @@ inline bool hexi_win_bwd_split(const AttnGeom& g, int window, int n_sink, bool d
 }
 
 // Whether the fp32 units of a windowed call take 16 rows (or keys), streamed rows split over eight wavefronts, or 64 that share tiles: PART 0 forward, 1 dQ, 2 dK/dV.
-// Fitted to 190 random calls (90 % within 15 %), us: a base, and for every round of 256 workgroups a fixed part and a step, 32 streamed rows in the 64-row shape and 128 in
+// Fitted to 189 random calls (90 % within 15 %), us: a base, and for every round of 256 workgroups a fixed part and a step, 32 streamed rows in the 64-row shape and 128 in
 // the other; more 64-row units than CUs share one and take at least 1.6 rounds at head_dim 128.  The choice is on average under 1 % slower than the better one.  64 rows / 16 rows:
 // forward, 128 columns, 16 heads of 3667, window 26 54 / 104, 4 of 4173, 1581 254 / 190; dQ, 64 columns, 24 of 6094, 83 89 / 156; dK/dV, 8 kv heads, 8000, 821 476 / 642,
 // 8/4 of 1707, 1274 393 / 184.
