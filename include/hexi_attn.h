@@ -169,7 +169,7 @@ int hexi_attn_bwd_chunk(const hexi_attn_desc* desc, const hexi_range* q_range, c
 typedef struct { int64_t window, n_sink; } hexi_window;
 
 /* Bytes of device workspace that hexi_attn_win_fwd_chunk needs, and that hexi_attn_win_bwd_chunk can use, for this
- * descriptor and window and these lengths, 0 for most (0 too for arguments that the call refuses).  Nothing is kept in it
+ * descriptor and window and these lengths, 0 for most (0 too for an element type, heads, a window or lengths that the calls refuse).  Nothing is kept in it
  * between calls; calls that may run at the same time, replays of captured graphs among them, need one each. */
 size_t hexi_attn_win_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc);
 size_t hexi_attn_win_bwd_workspace_bytes(const hexi_attn_desc* desc, const hexi_window* window, int64_t lq, int64_t lc);

@@ -264,7 +264,7 @@ static int build_window(const hexi_window* w, int* window, int* n_sink)
 static bool win_sizes_fit(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)
 {
     return !(!d || !w || lq < 1 || lc < 1 || lq > 2147483647LL || lc > 2147483647LL || d->n_q_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || d->n_kv_heads < 1 ||
-        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || w->window < 1 || w->n_sink < 0);
+        d->n_kv_heads > d->n_q_heads || (d->head_dim != 64 && d->head_dim != 128) || (d->dtype != HEXI_BF16 && d->dtype != HEXI_F32) || w->window < 1 || w->n_sink < 0);
 }
 
 static WinFwdPlan win_fwd_plan(const hexi_attn_desc* d, const hexi_window* w, int64_t lq, int64_t lc)

@@ -346,7 +346,7 @@ def hexi_attn_win_bwd_workspace_bytes(desc, window, lq, lc):
 
 
 def hexi_attn_win_fwd_chunk(desc, window, q_segs, kv_segs, q, k, v, o, lse, flags=0, workspace=None, stream=None):
-    """Windowed forward; o's element type (fp32 or bf16) is the result's."""
+    """Windowed forward; o's element type (fp32 or bf16) is the result's.  workspace: a tensor of at least hexi_attn_win_workspace_bytes, where that is not 0."""
     qr, kr, lq, lc, dev, d, nq, nkv = _win_inputs(desc, q_segs, kv_segs, q, k, v, lse)
     o_type = _dtype(o)
     _fits("o", o, (lq, nq, d), o_type, dev)
