@@ -299,6 +299,79 @@ int hexi_rope_a2a_unpack(const hexi_rope_desc* desc, const hexi_range* range, co
                          uint32_t flags, void* hip_stream);
 
 /*
+ * Paged key / value caches: a request's keys and values lie on pages of `page` tokens, its row of a block table says which.  What the
+ * lengths are only the device needs to know, so a step (plan, rotate, write, attend) can be captured once and replayed while they
+ * change.  All int32 arrays here are DEVICE arrays; nothing that they hold, whatever it is, makes a call read or write outside its
+ * tensors.
+ */
+#define HEXI_PAGED_MAX_PAGE 1024            /* tokens */
+#define HEXI_PAGED_MAX_REQUESTS 8192
+#define HEXI_PAGED_MAX_TOKENS (1 << 30)     /* of a request (columns * page), and rows of a call */
+
+/*
+ * The plan of a step: pages for the requests' lengths, and the place of every new row.  Request r keeps `cached[r]` tokens of what it
+ * has in the cache (0 with no new ones: it has ended; fewer than before: the last ones are dropped) and adds added[r]; negative
+ * counts are 0.
+ *   table     [n_requests][columns]: page ids; the first held[r] entries of a row are the request's.  Updated, as is held [n_requests].
+ *   free_list [n_pages]: ids of the pages that no request holds, *n_free of them.  Updated.
+ * First every request returns the pages it no longer fills, from request 0 on and from its first such page on, to the list's end.
+ * Then requests take what they lack, in the same order, from the list's end.  A request gets all that it lacks or nothing: nothing
+ * where what it and the requests before it lack is more than the list holds, where it lacks more than its table row has room
+ * for, or where its new rows end behind n_rows; it can then be asked for again in another step.
+ *   row_start [n_requests + 1]: first new row of every request, rows in the order of the requests; the last entry is their number.
+ *   kv_len    [n_requests]: cached[r] + added[r]; cached[r] (no more than its pages hold) where it got nothing.
+ *   pos, slot [n_rows]: position of every new row in its request (cached[r] + i; hexi_rope takes these) and its place in the
+ *             cache, page id * page + token, -1 where its request got nothing.  Rows behind the last request's get 0 and -1.
+ * Numbers of rows and positions above 2^31 - 1 are given as 2^31 - 1.
+ * 16 <= page <= HEXI_PAGED_MAX_PAGE, a multiple of 16; n_pages * page < 2^31; columns * page <= HEXI_PAGED_MAX_TOKENS.
+ * pos and slot may be NULL where n_rows is 0.  A page belongs to one request.
+ */
+int hexi_paged_plan(int32_t page, int32_t n_pages, int32_t n_requests, const int32_t* cached, const int32_t* added,
+                    int32_t* table, int32_t columns, int32_t* held, int32_t* free_list, int32_t* n_free,
+                    int32_t* row_start, int32_t* kv_len, int64_t n_rows, int32_t* pos, int32_t* slot, void* hip_stream);
+
+/* A cache of keys, and one of values of the same layout: element (page id, head, token of the page, column) at
+ * id * stride_page + head * stride_head + token * stride_tok + column.  Strides in elements, multiples of 16 bytes. */
+typedef struct {
+    int32_t dtype;                /* HEXI_BF16 | HEXI_F32 */
+    int32_t head_dim;             /* 64 or 128 */
+    int32_t n_kv_heads;
+    int32_t page, n_pages;
+    int64_t stride_page, stride_head, stride_tok;      /* stride_tok <= HEXI_MAX_TOKEN_STRIDE */
+} hexi_paged_cache;
+
+/*
+ * Writes keys and values of new tokens, k and v [n_rows][n_kv_heads][head_dim] with the strides given, into their slots.  Rows with a
+ * slot that the cache does not have (-1 for instance) are left out.  x_dtype: the element type of k and v, that of the cache, or
+ * HEXI_F32 for a bf16 cache (rounded to nearest even).  Slots are distinct: of two rows with the same slot either may remain, in parts.
+ */
+int hexi_paged_write(const hexi_paged_cache* cache, const int32_t* slot, int64_t n_rows, const void* k, const void* v, int32_t x_dtype,
+                     int64_t x_stride_tok, int64_t x_stride_head, void* k_cache, void* v_cache, void* hip_stream);
+
+/*
+ * Attention of new tokens over a paged cache that holds their own keys already: of request r the rows row_start[r] ..
+ * row_start[r + 1] - 1 of q, over its first kv_len[r] cached keys, forward, from single tokens to whole prompts.  Row i of it stands at
+ * position q_start[r] + i, key j at kv_start[r] + j; it sees key j iff the key's position is not behind its own and, with a window (NULL: none),
+ * iff that of hexi_window says so.  kv_start NULL: 0.  q_start NULL: its rows are the last of its keys.  (Both
+ * are for contexts that are spread over devices, each with the cache of a part: partial results, joined by hexi_attn_merge_lse.)
+ * desc: that of the ring step; its kv strides are not used.  q: [n_rows][n_q_heads][head_dim] with its strides.  table, columns: as in
+ * hexi_paged_plan; an entry that is no page of the cache holds no keys.
+ * o: [n_rows][n_q_heads][head_dim], dense, of o_dtype (HEXI_BF16: rounded once); lse: fp32 [n_q_heads][n_rows], or NULL.  Rows that see no key get
+ * o = 0, lse = -INFINITY; rows in front of the first request's and behind the last one's are left as they are.  Values of keys that a row does not
+ * see do not reach it, infinities and NaN included.  Results are reproducible run to run.
+ * max_rows: no request has more rows than this (further ones are left as they are); 0 where that is not known.
+ * workspace: hexi_paged_attn_workspace_bytes() bytes of device memory, 16-byte aligned.  Nothing is kept in it between calls; calls that may run at
+ * the same time, replays of captured graphs among them, need one each.  0 there: arguments that the call refuses, or no rows.
+ */
+size_t hexi_paged_attn_workspace_bytes(const hexi_attn_desc* desc, const hexi_paged_cache* cache, int32_t n_requests, int32_t columns,
+                                       int64_t n_rows, int64_t max_rows);
+int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cache* cache, const hexi_window* window,
+                    int32_t n_requests, const int32_t* table, int32_t columns, const int32_t* row_start, const int32_t* kv_len,
+                    const int32_t* q_start, const int32_t* kv_start, int64_t n_rows, int64_t max_rows,
+                    const void* q, const void* k_cache, const void* v_cache, void* o, int32_t o_dtype, float* lse,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Host-side performance model and hierarchical scheduler (Sec. 4: formalization, performance model,
  * scheduler; App. A: cost and memory model; App. B: the scheduler's algorithm).  No GPU is touched.
  * All pointers are HOST pointers; inputs are read during the call only.

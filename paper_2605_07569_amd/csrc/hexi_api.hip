@@ -7,6 +7,7 @@
 #include "hexi_internal.h"
 #include "hexi_window.h"
 #include "hexi_rope.h"
+#include "hexi_paged.h"
 
 #define HEXI_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -116,7 +117,8 @@ HEXI_EXPORT int hexi_shard_mask(const hexi_range* q_range, const hexi_range* kv_
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-static int build_geom(const hexi_attn_desc* d, const hexi_range* q_range, const hexi_range* kv_range, AttnGeom* g)
+// Element type, columns, head counts and scale of a descriptor.
+static int check_desc(const hexi_attn_desc* d)
 {
     if (!d) return fail(HEXI_EINVAL, "null descriptor");
     if (d->dtype != HEXI_BF16 && d->dtype != HEXI_F32) return fail(HEXI_EUNSUPPORTED, "dtype %d not supported", d->dtype);
@@ -124,7 +126,29 @@ static int build_geom(const hexi_attn_desc* d, const hexi_range* q_range, const 
     if (d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_q_heads > HEXI_MAX_HEADS || d->n_kv_heads > d->n_q_heads)
         return fail(HEXI_EINVAL, "head counts nq=%d nkv=%d invalid (1 <= nkv <= nq <= %d)", d->n_q_heads, d->n_kv_heads, HEXI_MAX_HEADS);
     if (!(d->softmax_scale > 0.f) || !std::isfinite(d->softmax_scale)) return fail(HEXI_EINVAL, "softmax_scale must be positive and finite");
-    int rc;
+    return HEXI_OK;
+}
+
+// The kv head of every q head.
+static int build_kv_of_q(const hexi_attn_desc* d, signed char* kv_of_q)
+{
+    if (d->kv_of_q) {
+        for (int h = 0; h < d->n_q_heads; ++h) {
+            if (d->kv_of_q[h] < 0 || d->kv_of_q[h] >= d->n_kv_heads) return fail(HEXI_EINVAL, "kv_of_q[%d]=%d out of range", h, d->kv_of_q[h]);
+            kv_of_q[h] = (signed char)d->kv_of_q[h];
+        }
+    } else {
+        if (d->n_q_heads % d->n_kv_heads) return fail(HEXI_EINVAL, "kv_of_q is NULL but n_q_heads %% n_kv_heads != 0");
+        const int grp = d->n_q_heads / d->n_kv_heads;
+        for (int h = 0; h < d->n_q_heads; ++h) kv_of_q[h] = (signed char)(h / grp);
+    }
+    return HEXI_OK;
+}
+
+static int build_geom(const hexi_attn_desc* d, const hexi_range* q_range, const hexi_range* kv_range, AttnGeom* g)
+{
+    int rc = check_desc(d);
+    if (rc != HEXI_OK) return rc;
     if ((rc = build_segtable(q_range, "q_range", &g->qs)) != HEXI_OK) return rc;
     if ((rc = build_segtable(kv_range, "kv_range", &g->ks)) != HEXI_OK) return rc;
     g->lq = g->qs.total; g->lc = g->ks.total;
@@ -141,17 +165,7 @@ static int build_geom(const hexi_attn_desc* d, const hexi_range* q_range, const 
     const int esz = d->dtype == HEXI_BF16 ? 2 : 4;
     if ((d->q_stride_tok * esz) % 16 || (d->q_stride_head * esz) % 16 || (d->kv_stride_tok * esz) % 16 || (d->kv_stride_head * esz) % 16)
         return fail(HEXI_EALIGN, "token and head strides must be multiples of 16 bytes");
-    if (d->kv_of_q) {
-        for (int h = 0; h < d->n_q_heads; ++h) {
-            if (d->kv_of_q[h] < 0 || d->kv_of_q[h] >= d->n_kv_heads) return fail(HEXI_EINVAL, "kv_of_q[%d]=%d out of range", h, d->kv_of_q[h]);
-            g->kv_of_q[h] = (signed char)d->kv_of_q[h];
-        }
-    } else {
-        if (d->n_q_heads % d->n_kv_heads) return fail(HEXI_EINVAL, "kv_of_q is NULL but n_q_heads %% n_kv_heads != 0");
-        const int grp = d->n_q_heads / d->n_kv_heads;
-        for (int h = 0; h < d->n_q_heads; ++h) g->kv_of_q[h] = (signed char)(h / grp);
-    }
-    return HEXI_OK;
+    return build_kv_of_q(d, g->kv_of_q);
 }
 
 // True when no key of the chunk is visible to any row of the shard.
@@ -543,4 +557,153 @@ HEXI_EXPORT int hexi_rope_a2a_unpack(const hexi_rope_desc* desc, const hexi_rang
                                      const int32_t* heads_per_rank, const int32_t* head_list, const uint8_t* rotate, uint32_t flags, void* hip_stream)
 {
     return rope_a2a_call(false, desc, range, positions, pos_stride, packed, y, n_heads_total, dtype, y_stride_tok, n_ranks, heads_per_rank, head_list, rotate, flags, hip_stream);
+}
+
+// Checks a paged cache.
+static int check_paged_cache(const hexi_paged_cache* c)
+{
+    if (!c) return fail(HEXI_EINVAL, "null cache descriptor");
+    if (c->dtype != HEXI_BF16 && c->dtype != HEXI_F32) return fail(HEXI_EUNSUPPORTED, "dtype %d not supported", c->dtype);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(HEXI_EUNSUPPORTED, "head_dim %d not supported (64 or 128)", c->head_dim);
+    if (c->n_kv_heads < 1 || c->n_kv_heads > HEXI_MAX_HEADS) return fail(HEXI_EINVAL, "n_kv_heads %d outside 1..%d", c->n_kv_heads, HEXI_MAX_HEADS);
+    if (c->page < 16 || c->page % 16 || c->page > HEXI_PAGED_MAX_PAGE) return fail(HEXI_EUNSUPPORTED, "page of %d tokens (a multiple of 16, 16..%d)", c->page, HEXI_PAGED_MAX_PAGE);
+    if (c->n_pages < 1) return fail(HEXI_EINVAL, "n_pages %d", c->n_pages);
+    if ((int64_t)c->n_pages * c->page > 2147483647LL) return fail(HEXI_EUNSUPPORTED, "%d pages of %d tokens: more than 2^31-1 tokens", c->n_pages, c->page);
+    if (c->stride_page < c->head_dim || c->stride_head < c->head_dim || c->stride_tok < c->head_dim) return fail(HEXI_EINVAL, "strides must be at least head_dim");
+    if (c->stride_tok > HEXI_MAX_TOKEN_STRIDE) return fail(HEXI_EUNSUPPORTED, "token stride above %d elements", HEXI_MAX_TOKEN_STRIDE);
+    const __int128 last = (__int128)(c->n_pages - 1) * c->stride_page + (__int128)(c->n_kv_heads - 1) * c->stride_head + (__int128)(c->page - 1) * c->stride_tok;
+    if (last + c->head_dim > (__int128)1 << 40) return fail(HEXI_EUNSUPPORTED, "the cache spans more than 2^40 elements");
+    const int esz = c->dtype == HEXI_BF16 ? 2 : 4;
+    if ((c->stride_page * esz) % 16 || (c->stride_head * esz) % 16 || (c->stride_tok * esz) % 16) return fail(HEXI_EALIGN, "strides must be multiples of 16 bytes");
+    return HEXI_OK;
+}
+
+// Requests and the columns of their table.
+static int check_paged_requests(int32_t n_requests, int32_t columns, int32_t page)
+{
+    if (n_requests < 1 || n_requests > HEXI_PAGED_MAX_REQUESTS) return fail(HEXI_EINVAL, "n_requests %d outside 1..%d", n_requests, HEXI_PAGED_MAX_REQUESTS);
+    if (columns < 1) return fail(HEXI_EINVAL, "table of %d columns", columns);
+    if ((int64_t)columns * page > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EUNSUPPORTED, "a table of %d columns of %d tokens: more than 2^30 tokens a request", columns, page);
+    return HEXI_OK;
+}
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+HEXI_EXPORT int hexi_paged_plan(int32_t page, int32_t n_pages, int32_t n_requests, const int32_t* cached, const int32_t* added,
+                                int32_t* table, int32_t columns, int32_t* held, int32_t* free_list, int32_t* n_free,
+                                int32_t* row_start, int32_t* kv_len, int64_t n_rows, int32_t* pos, int32_t* slot, void* hip_stream)
+{
+    if (page < 16 || page % 16 || page > HEXI_PAGED_MAX_PAGE) return fail(HEXI_EUNSUPPORTED, "page of %d tokens (a multiple of 16, 16..%d)", page, HEXI_PAGED_MAX_PAGE);
+    if (n_pages < 1) return fail(HEXI_EINVAL, "n_pages %d", n_pages);
+    if ((int64_t)n_pages * page > 2147483647LL) return fail(HEXI_EUNSUPPORTED, "%d pages of %d tokens: more than 2^31-1 tokens", n_pages, page);
+    const int rc = check_paged_requests(n_requests, columns, page);
+    if (rc != HEXI_OK) return rc;
+    if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EINVAL, "n_rows %lld outside 0..2^30", (long long)n_rows);
+    if (!cached || !added || !table || !held || !free_list || !n_free || !row_start || !kv_len || (n_rows > 0 && (!pos || !slot))) return fail(HEXI_EINVAL, "null pointer");
+    for (const void* p : {(const void*)cached, (const void*)added, (const void*)table, (const void*)held, (const void*)free_list, (const void*)n_free, (const void*)row_start,
+                          (const void*)kv_len, (const void*)pos, (const void*)slot})
+        if (!aligned4(p)) return fail(HEXI_EALIGN, "pointers must be 4-byte aligned");
+    const PagedPlanArgs a = {cached, added, table, held, free_list, n_free, row_start, kv_len, pos, slot, n_requests, columns, n_pages, (int)n_rows, Divisor((unsigned)page)};
+    const hipError_t e = hexi_launch_paged_plan(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "paged plan launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
+}
+
+HEXI_EXPORT int hexi_paged_write(const hexi_paged_cache* cache, const int32_t* slot, int64_t n_rows, const void* k, const void* v, int32_t x_dtype,
+                                 int64_t x_stride_tok, int64_t x_stride_head, void* k_cache, void* v_cache, void* hip_stream)
+{
+    const int rc = check_paged_cache(cache);
+    if (rc != HEXI_OK) return rc;
+    if (x_dtype != cache->dtype && !(x_dtype == HEXI_F32 && cache->dtype == HEXI_BF16)) return fail(HEXI_EUNSUPPORTED, "element types %d -> %d", x_dtype, cache->dtype);
+    if (n_rows < 0) return fail(HEXI_EINVAL, "n_rows %lld", (long long)n_rows);
+    if ((__int128)n_rows * cache->n_kv_heads * (cache->head_dim / 8) > 2147483647) return fail(HEXI_EUNSUPPORTED, "n_rows * n_kv_heads * head_dim / 8 exceeds 2^31-1");
+    if (x_stride_tok < cache->head_dim || x_stride_head < cache->head_dim) return fail(HEXI_EINVAL, "strides must be at least head_dim");
+    if (!rope_span_ok(n_rows, cache->n_kv_heads, cache->head_dim, x_stride_tok, x_stride_head)) return fail(HEXI_EUNSUPPORTED, "the rows span more than 2^40 elements");
+    const int esz = x_dtype == HEXI_BF16 ? 2 : 4;
+    if ((x_stride_tok * esz) % 16 || (x_stride_head * esz) % 16) return fail(HEXI_EALIGN, "token and head strides must be multiples of 16 bytes");
+    if (!k_cache || !v_cache || (n_rows > 0 && (!slot || !k || !v))) return fail(HEXI_EINVAL, "null tensor pointer");
+    if (k_cache == v_cache || k == k_cache || v == v_cache || k == v_cache || v == k_cache) return fail(HEXI_EINVAL, "a cache is written where another tensor is read or written");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(slot)) return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned, slots 4-byte aligned");
+    const unsigned pieces = (unsigned)cache->head_dim / 8;
+    const PagedWriteArgs a = {slot, {k, v}, {k_cache, v_cache}, n_rows, (long long)cache->n_pages * cache->page, x_stride_tok, x_stride_head, cache->stride_page, cache->stride_head,
+                              cache->stride_tok, cache->n_kv_heads, cache->head_dim, Divisor((unsigned)cache->page), Divisor((unsigned)cache->n_kv_heads * pieces), Divisor(pieces)};
+    const hipError_t e = hexi_launch_paged_write(a, x_dtype, cache->dtype, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "paged write launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
+}
+
+// Checks what a call of paged attention and its workspace's size depend on, and settles how it is launched.
+static int paged_attn_shape(const hexi_attn_desc* desc, const hexi_paged_cache* cache, int32_t n_requests, int32_t columns, int64_t n_rows, int64_t max_rows,
+                            PagedGeom* g, PagedShape* shape)
+{
+    int rc = check_desc(desc);
+    if (rc == HEXI_OK) rc = check_paged_cache(cache);
+    if (rc == HEXI_OK) rc = check_paged_requests(n_requests, columns, cache->page);
+    if (rc != HEXI_OK) return rc;
+    if (desc->dtype != cache->dtype || desc->head_dim != cache->head_dim || desc->n_kv_heads != cache->n_kv_heads)
+        return fail(HEXI_EINVAL, "descriptor of type %d, %d columns, %d kv heads; cache of type %d, %d columns, %d heads", desc->dtype, desc->head_dim, desc->n_kv_heads, cache->dtype,
+                    cache->head_dim, cache->n_kv_heads);
+    if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS / desc->n_q_heads) return fail(HEXI_EINVAL, "n_rows %lld: 0 <= n_rows * n_q_heads <= 2^30", (long long)n_rows);
+    if (max_rows < 0) return fail(HEXI_EINVAL, "max_rows %lld", (long long)max_rows);
+    if (max_rows == 0 || max_rows > n_rows) max_rows = n_rows;
+    signed char kv_of_q[HEXI_MAX_HEADS];
+    if ((rc = build_kv_of_q(desc, kv_of_q)) != HEXI_OK) return rc;
+    hexi_paged_runs(kv_of_q, desc->n_q_heads, desc->n_kv_heads, g);
+    g->columns = columns; g->n_requests = n_requests; g->n_rows = (int)n_rows; g->max_rows = (int)max_rows;
+    *shape = hexi_paged_shape(desc->dtype, desc->head_dim, g->n_runs, g->most, n_requests, n_rows, max_rows, (int64_t)columns * cache->page);
+    return HEXI_OK;
+}
+
+HEXI_EXPORT size_t hexi_paged_attn_workspace_bytes(const hexi_attn_desc* desc, const hexi_paged_cache* cache, int32_t n_requests, int32_t columns, int64_t n_rows, int64_t max_rows)
+{
+    PagedGeom g;
+    PagedShape shape;
+    if (paged_attn_shape(desc, cache, n_requests, columns, n_rows, max_rows, &g, &shape) != HEXI_OK || n_rows == 0) return 0;
+    return hexi_paged_workspace(shape, desc->head_dim);
+}
+
+HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cache* cache, const hexi_window* window,
+                                int32_t n_requests, const int32_t* table, int32_t columns, const int32_t* row_start, const int32_t* kv_len,
+                                const int32_t* q_start, const int32_t* kv_start, int64_t n_rows, int64_t max_rows,
+                                const void* q, const void* k_cache, const void* v_cache, void* o, int32_t o_dtype, float* lse,
+                                void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    PagedArgs a;
+    PagedShape shape;
+    PagedGeom& g = a.g;
+    int rc = paged_attn_shape(desc, cache, n_requests, columns, n_rows, max_rows, &g, &shape);
+    g.window = 0x7fffffff;
+    g.n_sink = 0;
+    if (rc == HEXI_OK && window) rc = build_window(window, &g.window, &g.n_sink);
+    if (rc != HEXI_OK) return rc;
+    if (desc->q_stride_head < desc->head_dim || desc->q_stride_tok < desc->head_dim) return fail(HEXI_EINVAL, "strides must be at least head_dim");
+    if (desc->q_stride_tok > HEXI_MAX_TOKEN_STRIDE) return fail(HEXI_EUNSUPPORTED, "token stride above %d elements", HEXI_MAX_TOKEN_STRIDE);
+    const int esz = desc->dtype == HEXI_BF16 ? 2 : 4;
+    if ((desc->q_stride_tok * esz) % 16 || (desc->q_stride_head * esz) % 16) return fail(HEXI_EALIGN, "token and head strides must be multiples of 16 bytes");
+    if (o_dtype != HEXI_F32 && o_dtype != HEXI_BF16) return fail(HEXI_EUNSUPPORTED, "o_dtype %d", o_dtype);
+    if (n_rows == 0) return HEXI_OK;
+    if (!table || !row_start || !kv_len || !q || !k_cache || !v_cache || !o) return fail(HEXI_EINVAL, "null pointer");
+    if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) || !aligned4(lse) || !aligned4(table) || !aligned4(row_start) || !aligned4(kv_len) ||
+        !aligned4(q_start) || !aligned4(kv_start))
+        return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned, lse and the requests' arrays 4-byte aligned");
+    const size_t need = hexi_paged_workspace(shape, desc->head_dim);
+    if (!workspace || workspace_bytes < need) return fail(HEXI_EWORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned16(workspace)) return fail(HEXI_EALIGN, "the workspace must be 16-byte aligned");
+    g.table = table; g.row_start = row_start; g.kv_len = kv_len; g.q_start = q_start; g.kv_start = kv_start;
+    g.stride_page = cache->stride_page; g.stride_head = cache->stride_head; g.stride_tok = cache->stride_tok;
+    g.q_stride_tok = desc->q_stride_tok; g.q_stride_head = desc->q_stride_head;
+    g.n_pages = cache->n_pages;
+    g.by_page = Divisor((unsigned)cache->page);
+    g.scale = desc->softmax_scale;
+    a.q = q; a.k = k_cache; a.v = v_cache; a.o = o; a.lse = lse;
+    a.out_bf16 = o_dtype == HEXI_BF16;
+    a.n_ranges = shape.ranges;
+    a.min_blocks = shape.min_blocks;
+    a.n_active = (int*)workspace;
+    a.tiles = (PagedTile*)((char*)workspace + 256);
+    a.part_o = (float*)(a.tiles + shape.ranges);
+    a.part_lse = a.part_o + (size_t)2 * (size_t)shape.ranges * (size_t)shape.vectors * (size_t)desc->head_dim;
+    const hipError_t e = hexi_launch_paged_attn(a, shape, desc->dtype, desc->head_dim, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return fail(HEXI_EHIP, "paged attention launch failed: %s", hipGetErrorString(e));
+    return HEXI_OK;
 }

@@ -7,6 +7,7 @@
 // Angle: position times frequency in quarter turns, t = pos (c_hi + c_lo) with c the frequency times 2 / pi as two doubles.  With q = rint(t)
 // the rest r = fma(pos, c_lo, fma(pos, c_hi, -q)) is exact to 2^-53 whatever the position, and |r| <= 1/2 (an eighth of a turn), so fp32 holds it to
 // 2^-26: 2.4e-8 rad.  sin and cos of x = r pi / 2 from their power series up to x^9 and x^10 (the next terms are below 2e-9), swapped and negated by q mod 4.
+#include "hexi_divisor.h"
 #include "hexi_rope.h"
 #include "hexi_mfma.h"
 
@@ -60,17 +61,6 @@ template <int P> struct Piece<uint16_t, P> {
         if constexpr (P == 8) __builtin_nontemporal_store(u4{w[0], w[1], w[2], w[3]}, reinterpret_cast<u4*>(p));
         else __builtin_nontemporal_store(u2{w[0], w[1]}, reinterpret_cast<u2*>(p));
     }
-};
-
-// n / d for n < 2^31: (mulhi(n, mul) + n) >> shift, mul = ceil(2^(32 + shift) / d) - 2^32.
-struct Divisor {
-    unsigned d, mul, shift;
-    explicit Divisor(unsigned x) : d(x), shift(0)
-    {
-        while ((1ull << shift) < x) ++shift;
-        mul = (unsigned)(((1ull << 32) * ((1ull << shift) - x)) / x + 1);
-    }
-    __device__ __forceinline__ unsigned operator()(unsigned n) const { return (__umulhi(n, mul) + n) >> shift; }
 };
 
 // Where a slot's row lies on either side, and whether its head is rotated.

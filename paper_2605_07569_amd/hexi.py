@@ -21,6 +21,7 @@ HEXI_ROPE_HALF, HEXI_ROPE_ADJACENT, HEXI_ROPE_INVERSE = 0, 1, 16
 
 EXPORTS = ("hexi_shard_mask", "hexi_attn_fwd_chunk", "hexi_attn_merge_lse", "hexi_attn_bwd_chunk",
            "hexi_attn_win_workspace_bytes", "hexi_attn_win_fwd_chunk", "hexi_attn_win_bwd_workspace_bytes", "hexi_attn_win_bwd_chunk", "hexi_rope", "hexi_rope_a2a_pack", "hexi_rope_a2a_unpack",
+           "hexi_paged_plan", "hexi_paged_write", "hexi_paged_attn_workspace_bytes", "hexi_paged_attn",
            "hexi_a2a_pack", "hexi_a2a_unpack", "hexi_sched_cost", "hexi_sched_solve", "hexi_set_dkdv_run_len", "hexi_workspace_bytes", "hexi_last_error", "hexi_version")
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -67,6 +68,11 @@ class hexi_rope_tensor(ctypes.Structure):
                 ("x_stride_tok", ctypes.c_int64), ("x_stride_head", ctypes.c_int64), ("y_stride_tok", ctypes.c_int64), ("y_stride_head", ctypes.c_int64)]
 
 
+class hexi_paged_cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("page", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("stride_page", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64)]
+
+
 def load():
     """Loads the in-tree library; raises if it has not been built (no fallback)."""
     global _lib
@@ -103,6 +109,15 @@ def load():
     for fn in (lib.hexi_rope_a2a_pack, lib.hexi_rope_a2a_unpack):
         fn.argtypes = [op, rp, vp, i64, vp, vp, i32, i32, i64, i32, i32p, i32p, ctypes.POINTER(ctypes.c_uint8), u32, vp]
         fn.restype = ctypes.c_int
+    cp = ctypes.POINTER(hexi_paged_cache)
+    lib.hexi_paged_plan.argtypes = [i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, vp, vp, vp]
+    lib.hexi_paged_plan.restype = ctypes.c_int
+    lib.hexi_paged_write.argtypes = [cp, vp, i64, vp, vp, i32, i64, i64, vp, vp, vp]
+    lib.hexi_paged_write.restype = ctypes.c_int
+    lib.hexi_paged_attn_workspace_bytes.argtypes = [dp, cp, i32, i32, i64, i64]
+    lib.hexi_paged_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.hexi_paged_attn.argtypes = [dp, cp, wp, i32, vp, i32, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.hexi_paged_attn.restype = ctypes.c_int
     lib.hexi_a2a_pack.argtypes = [vp, vp, i64, i32, i32, i32, i64, i32, i32p, i32p, vp]
     lib.hexi_a2a_pack.restype = ctypes.c_int
     lib.hexi_a2a_unpack.argtypes = [vp, vp, i64, i32, i32, i32, i64, i32, i32p, i32p, vp]
@@ -452,6 +467,124 @@ def hexi_rope(rope, segs, tensors, positions=None, inverse=False, stream=None):
             xs, ys = (xs[0], d), (ys[0], d)
         arr[i] = (x.data_ptr(), y.data_ptr(), h, xs[0], xs[1], ys[0], ys[1])
     rc = (_lib or load()).hexi_rope(rope, r, pos, pos_stride, arr, len(tensors), x_type, y_type, HEXI_ROPE_INVERSE if inverse else 0, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def make_paged_cache(cache):
+    """Descriptor of a paged cache from its tensor of keys (or values), [pages, kv heads, tokens of a page, head_dim] with contiguous columns; of one that is laid out token by
+    token the view whose axes 1 and 2 are swapped."""
+    if cache.dim() != 4 or cache.stride(3) != 1:
+        _refuse(f"a cache of [pages, heads, tokens, columns] with contiguous columns is needed, not {tuple(cache.shape)} with strides {cache.stride()}")
+    n_pages, heads, page, d = cache.shape
+    s = cache.stride()
+    return hexi_paged_cache(_dtype(cache), d, heads, page, n_pages, s[0] if n_pages > 1 else heads * page * d, s[1] if heads > 1 else d, s[2])
+
+
+def paged_desc_for(q, cache, softmax_scale, kv_of_q=None):
+    """Descriptor of an attention call for q [rows, q heads, head_dim] over a paged cache (make_paged_cache has its shape)."""
+    if q.dim() != 3 or q.stride(2) != 1 or cache.dim() != 4:
+        _refuse(f"q of [rows, heads, columns] with contiguous columns and a cache of four axes are needed, not {tuple(q.shape)} with strides {q.stride()}, {tuple(cache.shape)}")
+    if kv_of_q is not None and len(kv_of_q) != q.shape[1]:
+        _refuse(f"kv_of_q: {len(kv_of_q)} entries for {q.shape[1]} heads")
+    return make_desc(_dtype(q), q.shape[2], q.shape[1], cache.shape[1], softmax_scale, _q_strides(q), (cache.shape[3], cache.shape[3]), kv_of_q)
+
+
+def _q_strides(q):
+    """Token and head stride; of an axis of one element any will do."""
+    n, h, d = q.shape
+    return (q.stride(0) if n > 1 else h * d, q.stride(1) if h > 1 else d)
+
+
+def _ints(name, t, shape, dev):
+    if _torch is None:
+        _types()
+    if t.dtype is not _torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
+        _refuse(f"{name}: a contiguous int32 tensor of {tuple(shape)} on the current GPU is needed, not {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+    return t.data_ptr()
+
+
+def hexi_paged_plan(page, cached, added, table, held, free_list, n_free, row_start, kv_len, pos, slot, stream=None):
+    """Pages for the requests' lengths and the places of their new rows; all int32 tensors on the device: cached, added, held, kv_len [requests], table [requests, columns],
+    free_list [pages], n_free [1], row_start [requests + 1], pos, slot [rows]."""
+    dev, n, rows = _current_device(), cached.shape, slot.shape
+    if len(n) != 1 or len(table.shape) != 2 or len(rows) != 1 or len(free_list.shape) != 1:
+        _refuse(f"cached {tuple(n)}, table {tuple(table.shape)}, free_list {tuple(free_list.shape)}, slot {tuple(rows)}: one, two, one and one axes are needed")
+    r, columns = n[0], table.shape[1]
+    rc = (_lib or load()).hexi_paged_plan(page, free_list.shape[0], r, _ints("cached", cached, n, dev), _ints("added", added, n, dev), _ints("table", table, (r, columns), dev), columns,
+                                          _ints("held", held, n, dev), _ints("free_list", free_list, free_list.shape, dev), _ints("n_free", n_free, (1,), dev),
+                                          _ints("row_start", row_start, (r + 1,), dev), _ints("kv_len", kv_len, n, dev), rows[0], _ints("pos", pos, rows, dev),
+                                          _ints("slot", slot, rows, dev), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _cache_fits(name, t, c, dev):
+    s = t.stride()
+    if t.shape != (c.n_pages, c.n_kv_heads, c.page, c.head_dim) or _dtype(t) != c.dtype or s[3] != 1 or s[2] != c.stride_tok or (s[1] != c.stride_head and c.n_kv_heads > 1) or (
+            s[0] != c.stride_page and c.n_pages > 1):
+        _refuse(f"{name}: {tuple(t.shape)} {t.dtype} with strides {s}; the descriptor says otherwise")
+    if t.get_device() != dev:
+        _refuse(f"{name} is on {t.device}, not on the current GPU")
+    return t.data_ptr()
+
+
+def hexi_paged_write(cache, slot, k, v, k_cache, v_cache, stream=None):
+    """Writes k and v [rows, kv heads, head_dim] (one type, one pair of strides) into their slots (int32 [rows]; -1: left out).  cache: that of make_paged_cache."""
+    dev, shape = _current_device(), k.shape
+    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or v.shape != shape or v.dtype is not k.dtype or k.stride(2) != 1 or v.stride(2) != 1:
+        _refuse(f"k, v: [rows, {cache.n_kv_heads}, {cache.head_dim}] of one type with contiguous columns are needed, not {tuple(shape)} {k.dtype}, {tuple(v.shape)} {v.dtype}")
+    tok, head = _q_strides(k)
+    if _q_strides(v) != (tok, head):
+        _refuse(f"k and v differ in their strides: {k.stride()}, {v.stride()}")
+    if k.get_device() != dev or v.get_device() != dev:
+        _refuse(f"k or v is on {k.device} or {v.device}, not on the current GPU")
+    rc = (_lib or load()).hexi_paged_write(cache, _ints("slot", slot, (shape[0],), dev), shape[0], k.data_ptr(), v.data_ptr(), _dtype(k), tok, head,
+                                           _cache_fits("k_cache", k_cache, cache, dev), _cache_fits("v_cache", v_cache, cache, dev), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def hexi_paged_attn_workspace_bytes(desc, cache, n_requests, columns, n_rows, max_rows=0):
+    return int((_lib or load()).hexi_paged_attn_workspace_bytes(desc, cache, n_requests, columns, n_rows, max_rows))
+
+
+def hexi_paged_attn(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, o, lse=None, max_rows=0, window=None, q_start=None, kv_start=None, workspace=None, stream=None):
+    """Attention of the requests' new rows, q [rows, q heads, head_dim], over their cached keys.  table [requests, columns], row_start [requests + 1], kv_len, q_start, kv_start
+    [requests]: int32 on the device; o's element type (fp32 or bf16) is the result's.  max_rows: no request has more rows (0: not known).  workspace: a tensor of at least
+    hexi_paged_attn_workspace_bytes, not shared with a call that may run at the same time; None takes one from torch for the call."""
+    dev = _current_device()
+    if len(table.shape) != 2 or len(kv_len.shape) != 1 or len(q.shape) != 3:
+        _refuse(f"table {tuple(table.shape)}, kv_len {tuple(kv_len.shape)}, q {tuple(q.shape)}: two, one and three axes are needed")
+    (r, columns), shape = table.shape, (q.shape[0], desc.n_q_heads, desc.head_dim)
+    if q.shape != shape or _dtype(q) != desc.dtype or q.stride(2) != 1 or any(
+            n > 1 and x != y for n, x, y in zip(shape, q.stride(), (desc.q_stride_tok, desc.q_stride_head))):
+        _refuse(f"q: [rows, {shape[1]}, {shape[2]}] of type {desc.dtype} with the descriptor's strides is needed, not {tuple(q.shape)} {q.dtype} with strides {q.stride()}")
+    if q.get_device() != dev:
+        _refuse(f"q is on {q.device}, not on the current GPU")
+    o_type = _dtype(o)
+    _fits("o", o, shape, o_type, dev)
+    if lse is not None:
+        _fits("lse", lse, (shape[1], shape[0]), HEXI_F32, dev)
+    lib, handle = _lib or load(), _stream(stream)
+    taken = None
+    if workspace is not None:
+        space, ws_bytes = workspace.data_ptr(), _bytes_of(workspace, dev)
+    else:
+        ws_bytes = lib.hexi_paged_attn_workspace_bytes(desc, cache, r, columns, shape[0], max_rows)
+        if stream is None:
+            workspace = _torch.empty(ws_bytes, dtype=_torch.uint8, device=q.device)
+            space = workspace.data_ptr()
+        else:
+            space = taken = _take(lib, ws_bytes, dev, handle) if ws_bytes else None
+    try:
+        rc = lib.hexi_paged_attn(desc, cache, window, r, _ints("table", table, (r, columns), dev), columns, _ints("row_start", row_start, (r + 1,), dev),
+                                 _ints("kv_len", kv_len, (r,), dev), None if q_start is None else _ints("q_start", q_start, (r,), dev),
+                                 None if kv_start is None else _ints("kv_start", kv_start, (r,), dev), shape[0], max_rows, q.data_ptr(),
+                                 _cache_fits("k_cache", k_cache, cache, dev), _cache_fits("v_cache", v_cache, cache, dev), o.data_ptr(), o_type, _ptr(lse), space, ws_bytes, handle)
+    finally:
+        if taken is not None:
+            _torch.cuda.caching_allocator_delete(taken)
     if rc:
         _check(rc)
 

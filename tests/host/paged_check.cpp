@@ -1,0 +1,64 @@
+// Host-side check of the paged caches' geometry (csrc/hexi_paged.h).  Lines on stdin:
+//   request page columns n_rows max_rows window n_sink row_start row_end kv_len has_q_start q_start kv_start   -> row0 rows kv, then sink:lo:hi of every row (of the first 40 and the last)
+//   place page columns n_pages key entry ...                                                     -> page id and row of a key
+//   ask page columns cached added held                                                           -> cached added want held keep
+//   runs nq nkv kv_of_q ...                                                                      -> "kvh:head,head" of every run, and the most heads of one
+#include <cstdio>
+#include <cstring>
+#include <vector>
+#include "hexi_paged.h"
+
+int main()
+{
+    char what[16];
+    while (std::scanf("%15s", what) == 1) {
+        PagedGeom g = {};
+        int page;
+        if (!std::strcmp(what, "request")) {
+            int row_start[2], kv_len, has_q, q_start, kv_start;
+            if (std::scanf("%d %d %d %d %d %d %d %d %d %d %d %d", &page, &g.columns, &g.n_rows, &g.max_rows, &g.window, &g.n_sink, row_start, row_start + 1, &kv_len, &has_q, &q_start, &kv_start) != 12) return 1;
+            g.by_page = Divisor((unsigned)page);
+            g.row_start = row_start;
+            g.kv_len = &kv_len;
+            g.q_start = has_q ? &q_start : nullptr;
+            g.kv_start = &kv_start;
+            const PagedRequest q = paged_request(g, 0);
+            std::printf("%d %d %d", q.row0, q.rows, q.kv);
+            for (int i = 0; i < q.rows; i = i < 39 || i == q.rows - 1 ? i + 1 : q.rows - 1) {
+                const WinKeys w = paged_keys_of_row(g, q, i);
+                std::printf(" %d:%d:%d", w.sink, w.lo, w.hi);
+            }
+            std::printf("\n");
+        } else if (!std::strcmp(what, "place")) {
+            int key;
+            if (std::scanf("%d %d %d %d", &page, &g.columns, &g.n_pages, &key) != 4) return 1;
+            std::vector<int> row((size_t)g.columns);
+            for (int& x : row)
+                if (std::scanf("%d", &x) != 1) return 1;
+            g.by_page = Divisor((unsigned)page);
+            const PagedPlace p = paged_place(g, row.data(), key);
+            std::printf("%d %d\n", p.id, p.row);
+        } else if (!std::strcmp(what, "ask")) {
+            int cached, added, held;
+            if (std::scanf("%d %d %d %d %d", &page, &g.columns, &cached, &added, &held) != 5) return 1;
+            const PagedAsk a = paged_ask(cached, added, held, page, g.columns);
+            std::printf("%lld %lld %lld %d %d\n", a.cached, a.added, a.want, a.held, a.keep);
+        } else {
+            int nq, nkv;
+            signed char kv_of_q[HEXI_MAX_HEADS];
+            if (std::scanf("%d %d", &nq, &nkv) != 2) return 1;
+            for (int h = 0; h < nq; ++h) {
+                int x;
+                if (std::scanf("%d", &x) != 1) return 1;
+                kv_of_q[h] = (signed char)x;
+            }
+            hexi_paged_runs(kv_of_q, nq, nkv, &g);
+            for (int i = 0; i < g.n_runs; ++i) {
+                std::printf("%d:", g.kvh[i]);
+                for (int x = g.first[i]; x < g.first[i + 1]; ++x) std::printf("%d%s", g.head[x], x + 1 < g.first[i + 1] ? "," : " ");
+            }
+            std::printf("%d\n", g.most);
+        }
+    }
+    return 0;
+}

@@ -1,0 +1,238 @@
+"""Paged caches by their definition: attention in float64 with elementwise error bounds, the rules of a plan one request at a time, and the cases that the tests share.
+
+Bounds.  u = 2^-24 is half a step of fp32, h = 2^-8 half a step of bf16 (0 for fp32 inputs: nothing is rounded to fewer bits there).  A score is a sum of d products and a few more
+roundings: |error| <= (d + 16) u scale sum |q k| + 16 u (|s| + |m|), m the value that is subtracted from it before the exponential (the row's LSE here; the kernels' reference is
+within a few units of it).  Exponentials and the sums' own roundings are counted as 2^-20 and n u relative.  E_j: what that makes of P_j, relative.  P is rounded to bf16
+as an operand (the sum that normalises o is that of the rounded P: at most h (sum P |v| + |o|)), results to the type they are asked for in (h or u)."""
+import random
+from dataclasses import dataclass
+from typing import List, Optional, Tuple
+
+import torch
+
+from paper_2605_07569_amd import hexi
+
+U, H = 2.0 ** -24, 2.0 ** -8
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@dataclass
+class Case:
+    name: str
+    lens: List[Tuple[int, int]]              # (keys in the cache, new rows) of every request
+    nq: int = 2
+    nkv: int = 1
+    page: int = 16
+    kv_of_q: Optional[List[int]] = None
+    window: int = 0
+    n_sink: int = 0
+    layout: str = "heads"
+    k_scale: float = 1.0
+    q_start: Optional[List[int]] = None
+    kv_start: Optional[List[int]] = None
+    first: int = 0                           # rows in front of the first request's
+    behind: int = 0                          # and behind the last one's
+    pad: int = 0                             # extra columns between heads and tokens of q
+
+    @property
+    def heads(self):
+        return self.kv_of_q or [h // (self.nq // self.nkv) for h in range(self.nq)]
+
+    @property
+    def rows(self):
+        return self.first + sum(n for _, n in self.lens) + self.behind
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+class Setup:
+    """Inputs of a case on the device.  Cache rows that hold no token of a request are NaN."""
+
+    def __init__(self, c, dtype, d, seed=1, spare=3, columns=0):
+        self.c, self.dtype, self.d = c, dtype, d
+        g = torch.Generator().manual_seed(seed)
+        counts = [-(-kv // c.page) for kv, _ in c.lens]
+        n_pages = sum(counts) + spare
+        order = torch.randperm(n_pages, generator=g).tolist()
+        self.table = torch.full((len(c.lens), max(max(counts), columns, 1)), -7, dtype=torch.int32)      # (an entry that no key is on: no page of the cache)
+        self.k = [torch.randn(kv, c.nkv, d, generator=g).mul(c.k_scale).to(dtype) for kv, _ in c.lens]
+        self.v = [torch.randn(kv, c.nkv, d, generator=g).to(dtype) for kv, _ in c.lens]
+        nan = float("nan")
+        shape = (n_pages, c.nkv, c.page, d) if c.layout == "heads" else (n_pages, c.page, c.nkv, d)
+        kc, vc = torch.full(shape, nan, dtype=dtype), torch.full(shape, nan, dtype=dtype)
+        if c.layout == "tokens":
+            kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
+        for r, n in enumerate(counts):
+            for i in range(n):
+                id_ = order.pop()
+                self.table[r, i] = id_
+                m = min(c.page, c.lens[r][0] - i * c.page)
+                kc[id_, :, :m] = self.k[r][i * c.page:i * c.page + m].transpose(0, 1)
+                vc[id_, :, :m] = self.v[r][i * c.page:i * c.page + m].transpose(0, 1)
+        to = lambda t: t.to(DEV) if c.layout == "heads" else t.transpose(1, 2).contiguous().to(DEV).transpose(1, 2)
+        self.k_cache, self.v_cache = to(kc), to(vc)
+        wide = torch.randn(c.rows, c.nq, d + c.pad, generator=g).to(dtype)
+        self.q = wide.to(DEV)[:, :, :d]
+        self.table = self.table.to(DEV)
+        starts = [c.first]
+        for _, n in c.lens:
+            starts.append(starts[-1] + n)
+        self.starts = starts
+        self.row_start, self.kv_len = ints(starts), ints([kv for kv, _ in c.lens])
+        self.q_start = None if c.q_start is None else ints(c.q_start)
+        self.kv_start = None if c.kv_start is None else ints(c.kv_start)
+        self.cache = hexi.make_paged_cache(self.k_cache)
+        self.scale = d ** -0.5
+        self.desc = hexi.paged_desc_for(self.q, self.k_cache, self.scale, c.kv_of_q)
+        self.window = hexi.make_window(c.window, c.n_sink) if c.window else None
+
+    def workspace(self, max_rows=0):
+        n = hexi.hexi_paged_attn_workspace_bytes(self.desc, self.cache, len(self.c.lens), self.table.shape[1], self.c.rows, max_rows)
+        return torch.full((n,), 255, dtype=torch.uint8, device=DEV)      # (NaN, and no number of pieces)
+
+    def out(self, out=None):
+        return (torch.full((self.c.rows, self.c.nq, self.d), 7.0, dtype=out or self.dtype, device=DEV), torch.full((self.c.nq, self.c.rows), 7.0, device=DEV))
+
+    def run(self, out=None, max_rows=0, bufs=None, **kw):
+        o, lse = bufs or self.out(out)
+        kw.setdefault("workspace", self.workspace(max_rows))
+        hexi.hexi_paged_attn(self.desc, self.cache, self.table, self.row_start, self.kv_len, self.q, self.k_cache, self.v_cache, o, lse, max_rows=max_rows, window=self.window,
+                             q_start=self.q_start, kv_start=self.kv_start, **kw)
+        return o, lse
+
+    def request(self, r):
+        """Rows, q [rows, nq, d], k, v, mask of a request, on the device in float64."""
+        c = self.c
+        kv, n = c.lens[r]
+        kv_start = c.kv_start[r] if c.kv_start else 0
+        q_start = c.q_start[r] if c.q_start else kv_start + kv - n
+        p, j = torch.arange(n, device=DEV)[:, None] + q_start, torch.arange(kv, device=DEV)[None, :] + kv_start
+        seen = j <= p
+        if c.window:
+            seen &= (p - j < c.window) | (j < c.n_sink)
+        return slice(self.starts[r], self.starts[r + 1]), self.q[self.starts[r]:self.starts[r + 1]].double(), self.k[r].double().to(DEV), self.v[r].double().to(DEV), seen
+
+    def reference(self, out=None):
+        """o, lse and bounds on their errors; 7 in rows that are no request's."""
+        c, d = self.c, self.d
+        h_in, h_out = H if self.dtype == BF16 else 0.0, H if (out or self.dtype) == BF16 else U
+        f64 = dict(dtype=torch.float64, device=DEV)
+        o, bo = torch.full((c.rows, c.nq, d), 7.0, **f64), torch.zeros((c.rows, c.nq, d), **f64)
+        lse, bl = torch.full((c.nq, c.rows), 7.0, **f64), torch.zeros((c.nq, c.rows), **f64)
+        for r in range(len(c.lens)):
+            rows, q, k, v, seen = self.request(r)
+            n = k.shape[0]
+            for h in range(c.nq):
+                kh, vh = k[:, c.heads[h]], v[:, c.heads[h]]
+                s = (q[:, h] @ kh.T) * self.scale
+                size = (q[:, h].abs() @ kh.abs().T) * self.scale
+                s = torch.where(seen, s, torch.full_like(s, float("-inf")))
+                z = torch.logsumexp(s, 1) if n else torch.full((s.shape[0],), float("-inf"), **f64)
+                m = torch.where(z.isinf(), torch.zeros_like(z), z)
+                p = torch.where(seen, torch.exp(s - m[:, None]), torch.zeros_like(s))
+                e = (d + 16) * U * size + 16 * U * (s.abs().nan_to_num(posinf=0.0) + m.abs()[:, None]) + 2.0 ** -20 + n * U
+                e = torch.where(seen, e, torch.zeros_like(e))
+                o[rows, h] = p @ vh
+                lse[h, rows] = z
+                weight = p @ vh.abs()
+                worst = (p * e).sum(1) if n else torch.zeros_like(z)
+                bo[rows, h] = (p * e) @ vh.abs() + (worst[:, None] + h_in) * (weight + o[rows, h].abs()) * 1.02 + h_out * o[rows, h].abs() * 1.02 + 1e-37
+                bl[h, rows] = worst * 1.02 + 4 * U * m.abs() + 2.0 ** -20
+        return o, lse, bo, bl
+
+
+# relative L2 that results may be off by: the flat bounds of the library's outputs, those of bf16 inputs whatever type they are returned in (weights rounded to 2^-8, evenly spread: 2^-8 / sqrt(3) = 2.3e-3 of them)
+REL = {BF16: 5e-3, F32: 1e-5}
+
+
+def within(name, got, want, bound, rel=None):
+    got, want = got.double(), want.to(got.device)
+    assert torch.equal(got.isinf(), want.isinf()) and not got.isnan().any(), name
+    fin = ~want.isinf()
+    assert torch.equal(got[~fin], want[~fin]), name
+    worst = float(((got - want)[fin].abs() / bound.to(got.device)[fin].clamp(min=1e-30)).max()) if fin.any() else 0.0
+    l2 = float((got - want)[fin].norm() / want[fin].norm().clamp(min=1e-30)) if fin.any() else 0.0
+    print(f"\n    {name}: {worst:.3f} of the bound, rel-L2 {l2:.2e}", end="", flush=True)
+    assert worst <= 1.0, (name, worst)
+    assert rel is None or l2 <= rel, (name, l2)
+
+
+def check(s, out=None, max_rows=0, **kw):
+    got = s.run(out, max_rows, **kw)
+    torch.cuda.synchronize()
+    o, lse, bo, bl = s.reference(out)
+    c = s.c
+    for rows in (slice(0, c.first), slice(c.rows - c.behind, c.rows)):      # left as they were
+        assert (got[0][rows] == 7).all() and (got[1][:, rows] == 7).all()
+    mine = slice(c.first, c.rows - c.behind)
+    within("o", got[0][mine], o[mine], bo[mine], REL[BF16 if BF16 in (s.dtype, out) else F32])
+    within("lse", got[1][:, mine], lse[:, mine], bl[:, mine])
+    return got
+
+
+FAR = 2 ** 31 - 5
+CASES = [
+    Case("one token, its own key", [(1, 1)]),
+    Case("one token", [(2900, 1)], nq=8),
+    Case("lengths around pages and blocks", [(n, 1) for n in (1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257)], nq=3, nkv=3),
+    Case("no keys, no rows", [(0, 1), (5, 0), (0, 0), (40, 3), (0, 2), (7, 7)], nq=4, nkv=2, first=2, behind=5),
+    Case("more rows than keys", [(3, 10), (1, 2), (100, 130)], nq=3),                         # the first rows see nothing
+    Case("prompts", [(70, 70), (1, 1), (200, 200), (33, 33)], nq=6, nkv=2, page=48, layout="tokens"),
+    Case("chunks", [(400, 37), (1000, 5), (64, 64), (530, 130)], nq=4, nkv=4, page=32, pad=8),
+    Case("cut head map", [(300, 3), (65, 1), (17, 9)], nq=7, nkv=3, kv_of_q=[0, 0, 1, 1, 1, 2, 2], page=64),
+    Case("heads in any order, one unread", [(150, 2), (90, 20)], nq=5, nkv=4, kv_of_q=[3, 0, 3, 0, 3], page=80, layout="tokens"),
+    Case("window", [(1000, 1), (37, 4), (600, 300)], nq=4, nkv=2, window=100),
+    Case("window with sinks", [(2000, 6), (50, 50), (900, 1)], nq=8, nkv=2, window=200, n_sink=5, page=32),
+    Case("window of one", [(200, 7), (3, 1)], window=1),
+    Case("sinks past the rows", [(100, 40)], window=3, n_sink=10 ** 12, nq=2, nkv=2),
+    Case("window past everything", [(130, 70)], window=10 ** 12, n_sink=0, nq=3),
+    Case("part of a context", [(500, 3), (64, 2), (10, 1)], nq=4, nkv=2, q_start=[5000, 64, 3], kv_start=[1000, 0, 7], behind=1),       # the last sees nothing
+    Case("part of a context, window", [(500, 30), (500, 2), (70, 9)], nq=4, nkv=2, window=300, n_sink=1010, q_start=[1600, 9000, FAR], kv_start=[1000, 1005, FAR - 60], page=64),
+    Case("wide scores", [(700, 5), (300, 1)], nq=2, k_scale=40.0),
+    Case("large pages", [(1500, 3), (1024, 1), (1025, 2)], nq=16, nkv=2, page=1024),
+    Case("many heads of one", [(333, 3)], nq=128, nkv=1),
+    Case("every head its own", [(90, 2)], nq=128, nkv=128),
+]
+
+
+class Pool:
+    """The rules of a plan, one request, page and row at a time: pages handed out and taken back."""
+
+    def __init__(self, page, n_pages, n_requests, columns, seed=1):
+        self.page, self.columns, self.n = page, columns, n_requests
+        free = list(range(n_pages))
+        random.Random(seed).shuffle(free)
+        self.free, self.n_free = free, n_pages
+        self.held, self.table = [0] * n_requests, [[-1] * columns for _ in range(n_requests)]
+
+    def step(self, cached, added, n_rows):
+        page, pages = self.page, lambda n: -(-n // self.page)
+        cached, added = [max(x, 0) for x in cached], [max(x, 0) for x in added]
+        want = [pages(a + b) for a, b in zip(cached, added)]
+        for r in range(self.n):
+            keep = min(self.held[r], want[r])
+            for i in range(keep, self.held[r]):
+                self.free[self.n_free] = self.table[r][i]
+                self.n_free += 1
+            self.held[r] = keep
+        budget, asked, rows = self.n_free, 0, 0
+        row_start, kv_len, pos, slot = [0], [], [], []
+        for r in range(self.n):
+            need = want[r] - self.held[r]
+            asked += need
+            rows += added[r]
+            granted = asked <= budget and want[r] <= self.columns and rows <= n_rows
+            if granted:
+                for _ in range(need):
+                    self.n_free -= 1
+                    self.table[r][self.held[r]] = self.free[self.n_free]
+                    self.held[r] += 1
+            row_start.append(min(rows, 2 ** 31 - 1))
+            kv_len.append(cached[r] + added[r] if granted else min(cached[r], self.held[r] * page))
+            for i in range(cached[r], cached[r] + min(added[r], n_rows - len(pos))):
+                pos.append(min(i, 2 ** 31 - 1))
+                slot.append(self.table[r][i // page] * page + i % page if granted else -1)
+        return row_start, kv_len, pos + [0] * (n_rows - len(pos)), slot + [-1] * (n_rows - len(slot))

@@ -1,0 +1,257 @@
+"""Paged caches on the GPU: attention against its definition in float64, writes against torch's copies, plans against their rules."""
+import random
+
+import pytest
+import torch
+
+import paged_util as pu
+from paged_util import BF16, DEV, F32, Case, Setup, check, ints
+from paper_2605_07569_amd import hexi
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)], ids=str)
+@pytest.mark.parametrize("c", pu.CASES, ids=lambda c: c.name)
+def test_attention_parity(c, dtype, d):
+    check(Setup(c, dtype, d))
+
+
+@pytest.mark.parametrize("c", [pu.CASES[i] for i in (3, 6, 10)], ids=lambda c: c.name)
+def test_results_in_fp32_of_bf16_inputs_and_without_lse(c):
+    s = Setup(c, BF16, 128)
+    o, lse = check(s, F32)
+    assert torch.equal(s.run(F32, bufs=(torch.full_like(o, 7.0), None))[0], o)
+    check(Setup(c, F32, 64), BF16)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)], ids=str)
+def test_long_contexts_that_many_workgroups_share(dtype, d):
+    check(Setup(Case("long", [(40001, 1), (1, 1), (9000, 3)], nq=8, nkv=2, page=64), dtype, d))
+    check(Setup(Case("batch", [(1 + 397 * i % 3000, 1 + i % 2) for i in range(70)], nq=6, nkv=2), dtype, d, columns=300))
+    check(Setup(Case("chunk", [(5000, 300), (640, 1)], nq=4, nkv=2, page=64), dtype, d))
+
+
+def test_how_many_rows_a_request_has_may_be_said():
+    c = Case("verify", [(500, 3), (64, 1), (33, 4), (200, 2)], nq=4, nkv=1)
+    s = Setup(c, BF16, 128)
+    for most in (4, 5, 10, 1000):
+        check(s, max_rows=most)
+    # further rows are left as they are, and the others stand where they stood
+    o, lse = s.run(max_rows=2)
+    want, wl = s.run()
+    torch.cuda.synchronize()
+    for r, (_, n) in enumerate(c.lens):
+        a, m = s.starts[r], min(n, 2)
+        assert (o[a + m:s.starts[r + 1]] == 7).all() and (lse[:, a + m:s.starts[r + 1]] == 7).all()
+        assert (o[a:a + m].float() - want[a:a + m].float()).abs().max() < 0.02 and (lse[:, a:a + m] - wl[:, a:a + m]).abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+def test_what_a_row_does_not_see_does_not_reach_it(dtype):
+    """Infinities and NaN in keys behind a row, behind a window and on pages of others (Setup has NaN wherever no token lies)."""
+    c = Case("masked", [(300, 40), (500, 2)], nq=4, nkv=2, page=32, window=90, n_sink=3)
+    s = Setup(c, dtype, 128)
+    want = s.run()
+    torch.cuda.synchronize()
+    spoiled = Setup(c, dtype, 128)
+
+    def spoil(r, key, value):
+        id_ = int(spoiled.table[r, key // c.page])
+        spoiled.k_cache[id_, :, key % c.page] = value
+        spoiled.v_cache[id_, :, key % c.page] = value
+    # request 0's rows stand at 260 .. 299: keys 3 .. 170 are seen by none, key 299 by the last alone; request 1's at 498, 499: keys 3 .. 408
+    for key in (3, 60, 169, 170):
+        spoil(0, key, NAN if key % 2 else INF)
+    for key in (3, 100, 407, 408):
+        spoil(1, key, -INF if key % 2 else NAN)
+    got = spoiled.run()
+    torch.cuda.synchronize()
+    o, lse, bo, bl = s.reference()
+    pu.within("o", got[0], o, bo)
+    pu.within("lse", got[1], lse, bl)
+    spoil(0, 299, NAN)
+    spoil(1, 499, INF)
+    got = spoiled.run()
+    torch.cuda.synchronize()
+    alone = [39, 41]                 # the last row of either request
+    rest = [i for i in range(42) if i not in alone]
+    pu.within("o", got[0][rest], o[rest], bo[rest])
+    pu.within("lse", got[1][:, rest], lse[:, rest], bl[:, rest])
+    assert got[0][alone].isnan().all() and want[0][alone].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+def test_entries_that_are_no_page_hold_no_keys(dtype):
+    """A table whose entries are anything: the keys on pages that the cache does not have are not seen."""
+    c = Case("bad pages", [(200, 2), (500, 1), (100, 30), (64, 3)], nq=4, nkv=2, page=32)
+    s = Setup(c, dtype, 64)
+    s.k_cache.nan_to_num_(0.0)
+    s.v_cache.nan_to_num_(0.0)
+    bad = {0: [1, 6], 1: [0, 7, 15], 2: [3], 3: [0, 1]}       # request 3 has no key left
+    n_pages = s.k_cache.shape[0]
+    for r, columns in bad.items():
+        for i, col in enumerate(columns):
+            s.table[r, col] = [-1, n_pages, 2 ** 31 - 1, -2 ** 31][i % 4]
+    request = s.request
+
+    def without(r):
+        rows, q, k, v, seen = request(r)
+        for col in bad[r]:
+            seen[:, col * c.page:(col + 1) * c.page] = False
+        return rows, q, k, v, seen
+    s.request = without
+    o, lse = check(s)
+    assert (o[s.starts[3]:] == 0).all() and (lse[:, s.starts[3]:] == -INF).all()
+
+
+def test_lengths_that_are_anything_stay_inside_the_tensors():
+    """Row starts and lengths out of range are taken as the nearest that are not; nothing outside the named rows is written (the arithmetic runs on the CPU too: test_paged_cpu.py)."""
+    c = Case("wild", [(100, 3), (60, 2), (40, 1)], nq=4, nkv=2, page=16, behind=3)
+    s = Setup(c, BF16, 64)
+    s.table.clamp_(min=0)
+    s.k_cache.nan_to_num_(0.0)
+    s.v_cache.nan_to_num_(0.0)
+    for starts, lens in (([-5, 3, 2 ** 31 - 1, 2 ** 31 - 1], [2 ** 31 - 1, -3, 40]), ([4, 2, 2, 3], [100, 60, 40]), ([-2 ** 31, -1, 0, 0], [1, 1, 1])):
+        s.row_start, s.kv_len = ints(starts), ints(lens)
+        o, lse = s.run()
+        torch.cuda.synchronize()
+        clip = [min(max(x, 0), c.rows) for x in starts]
+        mine = torch.zeros(c.rows, dtype=torch.bool)
+        for a, b in zip(clip, clip[1:]):
+            mine[a:b] = True
+        assert o.isfinite().all() and (o[~mine.to(DEV)] == 7).all() and not (o[mine.to(DEV)] == 7).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+def test_results_are_reproducible(dtype):
+    s = Setup(Case("again", [(7000, 1), (20, 20), (900, 5), (1, 1)], nq=8, nkv=2, page=32), dtype, 128)
+    want = s.run()
+    for _ in range(5):
+        got = s.run()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_cache_of_more_than_2_31_elements():
+    """Pages on either side of element 2^31 and 2^32."""
+    page, nkv, d = 64, 8, 128
+    n_pages = (2 ** 32 + 2 ** 27) // (page * nkv * d)
+    k, v = (torch.zeros(n_pages, nkv, page, d, dtype=BF16, device=DEV) for _ in range(2))
+    c = Case("far", [(200, 3), (64, 1)], nq=16, nkv=nkv, page=page)
+    s = Setup(c, BF16, d, spare=0)
+    at = [2 ** 31 // (page * nkv * d) - 1, 2 ** 31 // (page * nkv * d), n_pages - 1, 2 ** 32 // (page * nkv * d), 5]
+    ids = s.table.flatten().tolist()
+    for old, new in zip([i for i in ids if i >= 0], at):
+        k[new], v[new] = s.k_cache[old], s.v_cache[old]
+        s.table[s.table == old] = new + 10 ** 8
+    s.table[s.table >= 10 ** 8] -= 10 ** 8
+    s.k_cache, s.v_cache, s.cache = k, v, hexi.make_paged_cache(k)
+    check(s)
+    # and writes into it
+    slots = ints([p * page + 7 for p in at])
+    new = torch.randn(5, nkv, d, device=DEV).to(BF16)
+    hexi.hexi_paged_write(s.cache, slots, new, -new, k, v)
+    torch.cuda.synchronize()
+    for i, p in enumerate(at):
+        assert torch.equal(k[p, :, 7], new[i]) and torch.equal(v[p, :, 7], -new[i])
+
+
+# ---- writes ----
+
+@pytest.mark.parametrize("layout", ["heads", "tokens"])
+@pytest.mark.parametrize("x_dtype,dtype", [(BF16, BF16), (F32, F32), (F32, BF16)], ids=str)
+@pytest.mark.parametrize("rows,nkv,d,page", [(1, 1, 64, 16), (5, 3, 128, 48), (1000, 2, 64, 1024), (4099, 8, 128, 32)])
+def test_writes_are_exact(rows, nkv, d, page, x_dtype, dtype, layout):
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    n_pages = -(-rows // page) + 4
+    shape = (n_pages, nkv, page, d) if layout == "heads" else (n_pages, page, nkv, d)
+    k, v = (torch.randn(shape, generator=g, device=DEV).to(dtype) for _ in range(2))
+    if layout == "tokens":
+        k, v = k.transpose(1, 2), v.transpose(1, 2)
+    slot = torch.randperm(n_pages * page, generator=g, device=DEV)[:rows].to(torch.int32)
+    if rows > 4:      # rows of no slot
+        slot[1], slot[2], slot[rows - 1] = -1, n_pages * page, -2 ** 31
+        slot[3] = 2 ** 31 - 1
+    x = torch.randn(rows, 2 + 2 * nkv, d, generator=g, device=DEV).to(x_dtype)      # fused q, k and v
+    x[0, 2, 0], x[0, 2, 1], x[0, 2, 2] = INF, NAN, 2.0 ** -133 if x_dtype == F32 else 0.0
+    new_k, new_v = x[:, 2:2 + nkv], x[:, 2 + nkv:]
+    want_k, want_v = k.clone(), v.clone()
+    for i in torch.nonzero((slot >= 0) & (slot < n_pages * page)).flatten().tolist():
+        p, t = divmod(int(slot[i]), page)
+        want_k[p, :, t], want_v[p, :, t] = new_k[i].to(dtype), new_v[i].to(dtype)
+    hexi.hexi_paged_write(hexi.make_paged_cache(k), slot, new_k, new_v, k, v)
+    torch.cuda.synchronize()
+    as_bits = lambda t: t.nan_to_num(nan=12345.0)
+    assert torch.equal(as_bits(k), as_bits(want_k)) and torch.equal(as_bits(v), as_bits(want_v)) and k.isnan().sum() == want_k.isnan().sum()
+
+
+# ---- plans ----
+
+class Planner:
+    """A pool of pages on the device beside its rules on the host."""
+
+    def __init__(self, page, n_pages, n, columns, seed=1):
+        self.pool = pu.Pool(page, n_pages, n, columns, seed)
+        self.table, self.held, self.free, self.n_free = ints(self.pool.table), ints(self.pool.held), ints(self.pool.free), ints([n_pages])
+        self.row_start, self.kv_len = torch.full((n + 1,), -9, dtype=torch.int32, device=DEV), torch.full((n,), -9, dtype=torch.int32, device=DEV)
+
+    def step(self, cached, added, n_rows):
+        pos, slot = (torch.full((n_rows,), -9, dtype=torch.int32, device=DEV) for _ in range(2))
+        hexi.hexi_paged_plan(self.pool.page, ints(cached), ints(added), self.table, self.held, self.free, self.n_free, self.row_start, self.kv_len, pos, slot)
+        want = self.pool.step(cached, added, n_rows)
+        torch.cuda.synchronize()
+        assert [self.row_start.tolist(), self.kv_len.tolist(), pos.tolist(), slot.tolist()] == [list(x) for x in want]
+        assert self.held.tolist() == self.pool.held and self.n_free.tolist() == [self.pool.n_free]
+        assert self.free.tolist() == self.pool.free and self.table.tolist() == self.pool.table
+        return want
+
+
+@pytest.mark.parametrize("n,page,columns,pages,seed", [(1, 16, 1, 1, 1), (1, 16, 900, 1000, 2), (7, 48, 9, 30, 3), (64, 16, 40, 1500, 4), (700, 32, 12, 5000, 5), (1025, 16, 6, 4000, 6), (2049, 64, 4, 8000, 7)])
+def test_plans_over_many_steps(n, page, columns, pages, seed):
+    """Requests come, grow, lose tokens, end and are refused; the free list is empty at times."""
+    rng = random.Random(seed)
+    p = Planner(page, pages, n, columns, seed)
+    cached = [0] * n
+    for step in range(8):
+        added = [rng.choice([0, 1, 1, 1, rng.randint(0, columns * page // 3 + 2)]) for _ in range(n)]
+        for r in range(n):
+            x = rng.random()
+            if x < 0.1:
+                cached[r] = added[r] = 0
+            elif x < 0.2:
+                cached[r] = rng.randint(0, cached[r])
+            elif x < 0.23:
+                added[r] = columns * page + 1            # more than its row of the table holds
+        n_rows = max(0, sum(added) + rng.choice([0, 0, 3, 2500, -rng.randint(1, 5)]))
+        row_start, kv_len, _, _ = p.step(cached, added, n_rows)
+        cached = list(kv_len)
+
+
+def test_plans_of_counts_that_are_anything():
+    big = 2 ** 31 - 1
+    p = Planner(16, 40, 6, 8)
+    p.step([0, 0, 0, 0, 0, 0], [20, 1, 0, 128, 5, 33], 187)
+    p.step([20, -3, -2 ** 31, 128, 5, 33], [-1, big, 4, 0, -2 ** 31, big], 10)
+    p.step([big, 0, 0, 128, big, 0], [big, 0, 1, 1, 0, 0], 5000)
+    p.step([0] * 6, [0] * 6, 0)
+    assert p.pool.n_free == 40
+
+
+def test_held_and_free_counts_out_of_range():
+    """Counts that no plan leaves behind are taken as the nearest that can be, and nothing is written outside the arrays."""
+    n, columns, pages = 3, 4, 10
+    guard = lambda m: torch.full((m + 64,), 77, dtype=torch.int32, device=DEV)
+    for held, n_free in (([99, -5, 4], 50), ([0, 0, 0], -7), ([2 ** 31 - 1, 1, 2], 9)):
+        whole = {k: guard(m) for k, m in dict(table=n * columns, held=n, free=pages, n_free=1, row_start=n + 1, kv_len=n, pos=9, slot=9).items()}
+        a = {k: t[32:-32] for k, t in whole.items()}
+        a["table"].fill_(3)
+        a["free"].copy_(ints(range(pages)))
+        a["held"].copy_(ints(held))
+        a["n_free"].fill_(n_free)
+        hexi.hexi_paged_plan(16, ints([5, 16, 0]), ints([1, 1, 3]), a["table"].view(n, columns), a["held"], a["free"], a["n_free"], a["row_start"], a["kv_len"], a["pos"], a["slot"])
+        torch.cuda.synchronize()
+        assert all((t[:32] == 77).all() and (t[-32:] == 77).all() for t in whole.values())
+        assert 0 <= int(a["n_free"]) <= pages and ((a["held"] >= 0) & (a["held"] <= columns)).all()
+        assert ((a["slot"] >= -1) & (a["slot"] < 16 * pages)).all()

@@ -1,0 +1,197 @@
+"""Paged caches without a GPU: what the kernels work out from lengths, tables and slots, whatever these hold (under UBSan), and every refusal of the entry points, before anything is launched."""
+import ctypes
+import os
+import random
+import subprocess
+
+import pytest
+import torch
+
+from paper_2605_07569_amd import hexi
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+E, S, A, W = hexi.HEXI_EINVAL, hexi.HEXI_EUNSUPPORTED, hexi.HEXI_EALIGN, hexi.HEXI_EWORKSPACE
+LOW, TOP = -2 ** 31, 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    hipcc = "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("hipcc not available")
+    exe = str(tmp_path_factory.mktemp("paged") / "paged_check")
+    subprocess.check_call([hipcc, "-O1", "-std=c++17", "-x", "c++", "-D__HIP_PLATFORM_AMD__", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=all", "-I", "/opt/rocm/include",
+                           "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2605_07569_amd", "csrc"), os.path.join(ROOT, "tests", "host", "paged_check.cpp"), "-o", exe])
+
+    def run(lines):
+        out = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True)
+        assert out.returncode == 0, out.stderr
+        return out.stdout.strip("\n").split("\n")
+    return run
+
+
+def _clamp(x, lo, hi):
+    return min(max(x, lo), hi)
+
+
+def test_rows_and_keys_of_requests_are_the_definition_and_stay_in_range(ask):
+    rng = random.Random(3)
+    wild = lambda: rng.choice([LOW, LOW + 1, -1, 0, 1, TOP - 1, TOP, rng.randint(LOW, TOP)])
+    asked = []
+    for i in range(600):
+        page, columns, n_rows = rng.choice([16, 48, 64, 1024]), rng.randint(1, 30), rng.randint(1, 300)
+        a = rng.randint(0, n_rows)
+        case = [page, columns, n_rows, rng.choice([1, 3, n_rows]), rng.choice([1, 2, 17, 64, 5000, TOP]), rng.choice([0, 1, 5, 64, 300, TOP]), a, rng.randint(a, n_rows),
+                rng.randint(0, columns * page), rng.randint(0, 1), rng.randint(0, 4000), rng.choice([0, 0, rng.randint(0, 4000)])]
+        if i % 3 == 0:      # lengths and positions that are anything
+            for j in (6, 7, 8, 10, 11):
+                if rng.random() < 0.5:
+                    case[j] = wild()
+        asked.append(case)
+    for case, line in zip(asked, ask(["request " + " ".join(map(str, c)) for c in asked])):
+        page, columns, n_rows, max_rows, window, n_sink, start, end, kv_len, has_q, q_start, kv_start = case
+        row0, rows, kv = map(int, line.split()[:3])
+        assert 0 <= row0 <= row0 + rows <= n_rows and rows <= max_rows and 0 <= kv <= columns * page, (case, line)
+        own = _clamp(end, 0, n_rows) - _clamp(start, 0, _clamp(end, 0, n_rows))
+        assert rows == min(own, max_rows) and kv == _clamp(kv_len, 0, columns * page)
+        index = [i for i in range(rows) if i < 40 or i == rows - 1]
+        assert len(line.split()) == 3 + len(index)
+        for i, item in zip(index, line.split()[3:]):
+            sink, lo, hi = map(int, item.split(":"))
+            assert 0 <= sink <= lo <= hi <= kv, (case, item)
+            p = q_start + i - kv_start if has_q else kv - own + i      # relative to key 0
+            seen = {j for j in range(kv) if j <= p and (p - j < window or j + kv_start < n_sink)}
+            assert seen == set(range(sink)) | set(range(lo, hi)), (case, i, item)
+
+
+def test_places_of_keys_in_any_table(ask):
+    rng = random.Random(4)
+    asked = []
+    for _ in range(300):
+        page, columns, n_pages = rng.choice([16, 48, 80, 64, 1024]), rng.randint(1, 9), rng.randint(1, 50)
+        row = [rng.choice([rng.randint(0, n_pages - 1), rng.randint(0, n_pages - 1), -1, n_pages, LOW, TOP]) for _ in range(columns)]
+        asked.append((page, columns, n_pages, rng.choice([rng.randint(0, columns * page - 1), columns * page, columns * page + 63, 2 ** 30 + 63]), row))
+    for (page, columns, n_pages, key, row), line in zip(asked, ask([f"place {p} {c} {n} {k} " + " ".join(map(str, r)) for p, c, n, k, r in asked])):
+        entry = row[key // page] if key // page < columns else -1
+        assert list(map(int, line.split())) == [entry if 0 <= entry < n_pages else -1, key % page]
+
+
+def test_what_a_request_asks_for(ask):
+    rng = random.Random(5)
+    numbers = lambda: rng.choice([LOW, -1, 0, 1, 15, 16, 17, rng.randint(0, 5000), TOP])
+    asked = [(rng.choice([16, 48, 1024]), rng.randint(1, 400), numbers(), numbers(), numbers()) for _ in range(300)]
+    for (page, columns, cached, added, held), line in zip(asked, ask(["ask " + " ".join(map(str, a)) for a in asked])):
+        want = -(-(max(cached, 0) + max(added, 0)) // page)
+        held = _clamp(held, 0, columns)
+        assert list(map(int, line.split())) == [max(cached, 0), max(added, 0), want, held, min(want, held)]
+
+
+def test_head_runs(ask):
+    for nq, nkv, heads in ((8, 1, [0] * 8), (4, 2, [0, 0, 1, 1]), (7, 3, [0, 0, 1, 1, 1, 2, 2]), (5, 4, [3, 0, 3, 0, 3]), (128, 128, list(range(128))), (128, 1, [0] * 128)):
+        runs = [f"{k}:" + ",".join(str(h) for h in range(nq) if heads[h] == k) for k in range(nkv) if k in heads]
+        assert ask([f"runs {nq} {nkv} " + " ".join(map(str, heads))])[0].split() == runs + [str(max(heads.count(k) for k in heads))]
+
+
+def _codes(call, bad):
+    for code, changes in bad:
+        assert call(**changes) == code, (changes, hexi.hexi_last_error())
+        assert hexi.hexi_last_error()
+
+
+def _cache(dtype=0, d=128, heads=2, page=16, n_pages=10, strides=None):
+    return hexi.hexi_paged_cache(dtype, d, heads, page, n_pages, *(strides or (heads * page * d, page * d, d)))
+
+
+BAD_CACHES = [(S, dict(dtype=2)), (S, dict(d=96)), (E, dict(heads=0)), (E, dict(heads=129)), (S, dict(page=8)), (S, dict(page=24)), (S, dict(page=0)), (S, dict(page=-16)), (S, dict(page=1040)),
+              (E, dict(n_pages=0)), (S, dict(n_pages=2 ** 27)), (E, dict(strides=(4096, 2048, 64))), (E, dict(strides=(64, 2048, 128))), (E, dict(strides=(4096, 0, 128))),
+              (S, dict(strides=(2 ** 40, 2048, 128))), (S, dict(strides=(2 ** 30, 2048, 2 ** 22 + 8))), (A, dict(strides=(4097, 2048, 128))), (A, dict(strides=(4096, 2049, 128))),
+              (A, dict(strides=(4096, 2048, 132)))]
+
+
+def test_plan_refusals():
+    lib = hexi.load()
+    names = ("cached", "added", "table", "held", "free_list", "n_free", "row_start", "kv_len", "pos", "slot")
+
+    def call(page=16, n_pages=10, n=4, columns=5, n_rows=6, **kw):
+        p = {k: kw.get(k, 16) for k in names}
+        return lib.hexi_paged_plan(page, n_pages, n, p["cached"], p["added"], p["table"], columns, p["held"], p["free_list"], p["n_free"], p["row_start"], p["kv_len"], n_rows, p["pos"],
+                                   p["slot"], None)
+
+    _codes(call, [(S, dict(page=0)), (S, dict(page=-16)), (S, dict(page=20)), (S, dict(page=1040)), (E, dict(n_pages=0)), (S, dict(n_pages=2 ** 27)), (E, dict(n=0)), (E, dict(n=8193)),
+                  (E, dict(columns=0)), (S, dict(columns=2 ** 26 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 30 + 1))] + [(E, {k: None}) for k in names] + [(A, {k: 18}) for k in names])
+
+
+def test_write_refusals():
+    lib = hexi.load()
+
+    def call(slot=16, n_rows=3, k=32, v=48, x_dtype=0, tok=256, head=128, kc=64, vc=80, no_cache=False, **cache):
+        c = _cache(**cache)
+        return lib.hexi_paged_write(None if no_cache else ctypes.byref(c), slot, n_rows, k, v, x_dtype, tok, head, kc, vc, None)
+
+    _codes(call, BAD_CACHES + [(E, dict(no_cache=True)), (S, dict(x_dtype=2)), (S, dict(dtype=1)), (E, dict(n_rows=-1)), (S, dict(n_rows=2 ** 26)), (E, dict(tok=64)), (E, dict(head=64)),
+                               (S, dict(tok=2 ** 40)), (A, dict(tok=260)), (A, dict(head=132))] + [(E, {n: None}) for n in ("slot", "k", "v", "kc", "vc")] +
+           [(A, {n: 24}) for n in ("k", "v", "kc", "vc")] + [(A, dict(slot=18)), (E, dict(kc=80)), (E, dict(kc=32)), (E, dict(vc=48)), (E, dict(vc=32)), (E, dict(kc=48))])
+    assert call(n_rows=0, slot=None, k=None, v=None) == hexi.HEXI_OK
+
+
+def test_attention_refusals():
+    lib = hexi.load()
+    size = lib.hexi_paged_attn_workspace_bytes
+
+    def descs(dtype=0, d=128, heads=2, nq=8, scale=0.1, qs=(1024, 128), kv_of_q=None, desc=None, **cache):
+        a = dict(dtype=dtype, d=d, nq=nq, nkv=heads)
+        a.update(desc or {})
+        return hexi.make_desc(a["dtype"], a["d"], a["nq"], a["nkv"], scale, qs, (a["d"], a["d"]), kv_of_q), _cache(dtype=dtype, d=d, heads=heads, **cache)
+
+    def call(n=4, columns=5, n_rows=6, max_rows=0, window=None, table=16, row_start=16, kv_len=16, q_start=None, kv_start=None, q=16, k=16, v=16, o=16, o_dtype=0, lse=16, space=16, short=0,
+             no_desc=False, no_cache=False, **kw):
+        desc, cache = descs(**kw)
+        need = size(ctypes.byref(desc), ctypes.byref(cache), n, columns, n_rows, max_rows)
+        return lib.hexi_paged_attn(None if no_desc else ctypes.byref(desc), None if no_cache else ctypes.byref(cache), None if window is None else ctypes.byref(hexi.make_window(*window)), n, table,
+                                   columns, row_start, kv_len, q_start, kv_start, n_rows, max_rows, q, k, v, o, o_dtype, lse, space, need - short, None)
+
+    _codes(call, [(c, k) for c, k in BAD_CACHES if "d" not in k and k.get("heads") != 129 and "dtype" not in k] +
+           [(E, dict(no_desc=True)), (E, dict(no_cache=True)), (S, dict(d=96)), (S, dict(dtype=2)), (E, dict(nq=129)), (E, dict(nq=7)), (E, dict(scale=float("inf"))), (E, dict(scale=0.0)),
+            (E, dict(kv_of_q=[0] * 7 + [2])), (E, dict(desc=dict(dtype=1))), (E, dict(desc=dict(d=64), qs=(1024, 128))), (E, dict(desc=dict(nkv=4))), (E, dict(n=0)), (E, dict(n=8193)), (E, dict(columns=0)),
+            (S, dict(columns=2 ** 26 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 28)), (E, dict(max_rows=-1)), (E, dict(window=(0, 0))), (E, dict(window=(1, -1))), (E, dict(qs=(64, 128))),
+            (E, dict(qs=(1024, 64))), (S, dict(qs=(2 ** 22 + 8, 128))), (A, dict(qs=(1028, 128))), (A, dict(qs=(1024, 132))), (S, dict(o_dtype=2))] +
+           [(E, {p: None}) for p in ("table", "row_start", "kv_len", "q", "k", "v", "o")] + [(A, {p: 24}) for p in ("q", "k", "v", "o", "space")] +
+           [(A, {p: 18}) for p in ("lse", "table", "row_start", "kv_len", "q_start", "kv_start")] + [(W, dict(space=None)), (W, dict(short=1))])
+    assert call(n_rows=0, table=None, q=None, o=None, space=None) == hexi.HEXI_OK
+    desc, cache = descs()
+    assert size(ctypes.byref(desc), ctypes.byref(cache), 4, 5, 0, 0) == 0 and size(None, None, 4, 5, 6, 0) == 0 and size(ctypes.byref(desc), ctypes.byref(cache), 0, 5, 6, 0) == 0
+    assert size(ctypes.byref(desc), ctypes.byref(cache), 4, 5, 6, 0) > 0
+
+
+def test_binding_refuses_what_does_not_fit_before_the_library_is_asked():
+    """Shapes, element types, strides and devices that the C ABI cannot see."""
+    i32, bf16 = torch.int32, torch.bfloat16
+    z = lambda *s, t=i32: torch.zeros(s, dtype=t)
+
+    def refused(f, *args, **kw):
+        with pytest.raises(hexi.HexiError) as e:
+            f(*args, **kw)
+        return e.value.code
+
+    plan = dict(cached=z(3), added=z(3), table=z(3, 5), held=z(3), free_list=z(9), n_free=z(1), row_start=z(4), kv_len=z(3), pos=z(6), slot=z(6))
+    for change in ({}, dict(cached=z(3, 1)), dict(added=z(4)), dict(table=z(15)), dict(table=z(3, 6)[:, :5]), dict(held=z(2)), dict(free_list=z(3, 3)), dict(n_free=z(2)), dict(row_start=z(3)),
+                   dict(kv_len=z(3, t=torch.int64)), dict(pos=z(5)), dict(slot=z(12)[::2])):      # ({}: on the CPU)
+        assert refused(hexi.hexi_paged_plan, 16, **{**plan, **change}) == E
+    kc = z(10, 2, 16, 128, t=bf16)
+    cache = hexi.make_paged_cache(kc)
+    assert (cache.stride_page, cache.stride_head, cache.stride_tok) == (4096, 2048, 128)
+    tokens = hexi.make_paged_cache(z(10, 16, 2, 128, t=bf16).transpose(1, 2))
+    assert (tokens.page, tokens.n_kv_heads, tokens.stride_page, tokens.stride_head, tokens.stride_tok) == (16, 2, 4096, 128, 256)
+    assert refused(hexi.make_paged_cache, kc[0]) == E and refused(hexi.make_paged_cache, kc[..., ::2]) == E and refused(hexi.make_paged_cache, kc.half()) == S
+    new = z(6, 2, 128, t=bf16)
+    write = dict(slot=z(6), k=new, v=new, k_cache=kc, v_cache=kc.clone())
+    for change in ({}, dict(k=new[:, :1], v=new[:, :1]), dict(v=new[:5]), dict(v=new.float()), dict(v=z(6, 4, 128, t=bf16)[:, ::2]), dict(slot=z(5)), dict(k=new[..., :64], v=new[..., :64]), dict(k_cache=kc[:9]),
+                   dict(v_cache=z(10, 16, 2, 128, t=bf16).transpose(1, 2))):
+        assert refused(hexi.hexi_paged_write, cache, **{**write, **change}) == E
+    q = z(6, 8, 128, t=bf16)
+    desc = hexi.paged_desc_for(q, kc, 0.1)
+    assert refused(hexi.paged_desc_for, q[0], kc, 0.1) == E and refused(hexi.paged_desc_for, q, kc, 0.1, [0] * 7) == E
+    attn = dict(table=z(3, 5), row_start=z(4), kv_len=z(3), q=q, k_cache=kc, v_cache=kc, o=q.clone(), lse=z(8, 6, t=torch.float32), workspace=z(1 << 20, t=torch.uint8))
+    for change in ({}, dict(table=z(15)), dict(kv_len=z(3, 1)), dict(row_start=z(3)), dict(q=q[:, :7]), dict(q=q.float()), dict(q=z(6, 16, 128, t=bf16)[:, ::2]), dict(o=q[:5]), dict(lse=z(6, 8, t=torch.float32)),
+                   dict(q_start=z(2)), dict(kv_start=z(3, t=torch.int64)), dict(k_cache=kc[:9]), dict(workspace=z(1 << 20, t=torch.uint8)[::2])):
+        assert refused(hexi.hexi_paged_attn, desc, cache, **{**attn, **change}) == E
