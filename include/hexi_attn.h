@@ -306,7 +306,7 @@ int hexi_rope_a2a_unpack(const hexi_rope_desc* desc, const hexi_range* range, co
  */
 #define HEXI_PAGED_MAX_PAGE 1024            /* tokens */
 #define HEXI_PAGED_MAX_REQUESTS 8192
-#define HEXI_PAGED_MAX_TOKENS (1 << 30)     /* of a request (columns * page), and rows of a call */
+#define HEXI_PAGED_MAX_TOKENS (1 << 28)     /* of a request (columns * page), and rows (attention: rows * q heads) of a call */
 
 /*
  * The plan of a step: pages for the requests' lengths, and the place of every new row.  Request r keeps `cached[r]` tokens of what it

@@ -583,7 +583,7 @@ static int check_paged_requests(int32_t n_requests, int32_t columns, int32_t pag
 {
     if (n_requests < 1 || n_requests > HEXI_PAGED_MAX_REQUESTS) return fail(HEXI_EINVAL, "n_requests %d outside 1..%d", n_requests, HEXI_PAGED_MAX_REQUESTS);
     if (columns < 1) return fail(HEXI_EINVAL, "table of %d columns", columns);
-    if ((int64_t)columns * page > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EUNSUPPORTED, "a table of %d columns of %d tokens: more than 2^30 tokens a request", columns, page);
+    if ((int64_t)columns * page > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EUNSUPPORTED, "a table of %d columns of %d tokens: more than 2^28 tokens a request", columns, page);
     return HEXI_OK;
 }
 
@@ -598,7 +598,7 @@ HEXI_EXPORT int hexi_paged_plan(int32_t page, int32_t n_pages, int32_t n_request
     if ((int64_t)n_pages * page > 2147483647LL) return fail(HEXI_EUNSUPPORTED, "%d pages of %d tokens: more than 2^31-1 tokens", n_pages, page);
     const int rc = check_paged_requests(n_requests, columns, page);
     if (rc != HEXI_OK) return rc;
-    if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EINVAL, "n_rows %lld outside 0..2^30", (long long)n_rows);
+    if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EINVAL, "n_rows %lld outside 0..2^28", (long long)n_rows);
     if (!cached || !added || !table || !held || !free_list || !n_free || !row_start || !kv_len || (n_rows > 0 && (!pos || !slot))) return fail(HEXI_EINVAL, "null pointer");
     for (const void* p : {(const void*)cached, (const void*)added, (const void*)table, (const void*)held, (const void*)free_list, (const void*)n_free, (const void*)row_start,
                           (const void*)kv_len, (const void*)pos, (const void*)slot})
@@ -643,14 +643,14 @@ static int paged_attn_shape(const hexi_attn_desc* desc, const hexi_paged_cache* 
     if (desc->dtype != cache->dtype || desc->head_dim != cache->head_dim || desc->n_kv_heads != cache->n_kv_heads)
         return fail(HEXI_EINVAL, "descriptor of type %d, %d columns, %d kv heads; cache of type %d, %d columns, %d heads", desc->dtype, desc->head_dim, desc->n_kv_heads, cache->dtype,
                     cache->head_dim, cache->n_kv_heads);
-    if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS / desc->n_q_heads) return fail(HEXI_EINVAL, "n_rows %lld: 0 <= n_rows * n_q_heads <= 2^30", (long long)n_rows);
+    if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS / desc->n_q_heads) return fail(HEXI_EINVAL, "n_rows %lld: 0 <= n_rows * n_q_heads <= 2^28", (long long)n_rows);
     if (max_rows < 0) return fail(HEXI_EINVAL, "max_rows %lld", (long long)max_rows);
     if (max_rows == 0 || max_rows > n_rows) max_rows = n_rows;
     signed char kv_of_q[HEXI_MAX_HEADS];
     if ((rc = build_kv_of_q(desc, kv_of_q)) != HEXI_OK) return rc;
     hexi_paged_runs(kv_of_q, desc->n_q_heads, desc->n_kv_heads, g);
     g->columns = columns; g->n_requests = n_requests; g->n_rows = (int)n_rows; g->max_rows = (int)max_rows;
-    *shape = hexi_paged_shape(desc->dtype, desc->head_dim, g->n_runs, g->most, n_requests, n_rows, max_rows, (int64_t)columns * cache->page);
+    *shape = hexi_paged_shape(desc->dtype, g->n_runs, g->most, n_requests, n_rows, max_rows, (int64_t)columns * cache->page);
     return HEXI_OK;
 }
 
@@ -659,7 +659,7 @@ HEXI_EXPORT size_t hexi_paged_attn_workspace_bytes(const hexi_attn_desc* desc, c
     PagedGeom g;
     PagedShape shape;
     if (paged_attn_shape(desc, cache, n_requests, columns, n_rows, max_rows, &g, &shape) != HEXI_OK || n_rows == 0) return 0;
-    return hexi_paged_workspace(shape, desc->head_dim);
+    return hexi_paged_workspace(shape, 0, desc->head_dim) + hexi_paged_workspace(shape, 1, desc->head_dim);
 }
 
 HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cache* cache, const hexi_window* window,
@@ -686,7 +686,7 @@ HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cac
     if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) || !aligned4(lse) || !aligned4(table) || !aligned4(row_start) || !aligned4(kv_len) ||
         !aligned4(q_start) || !aligned4(kv_start))
         return fail(HEXI_EALIGN, "tensor base pointers must be 16-byte aligned, lse and the requests' arrays 4-byte aligned");
-    const size_t need = hexi_paged_workspace(shape, desc->head_dim);
+    const size_t few_bytes = hexi_paged_workspace(shape, 0, desc->head_dim), need = few_bytes + hexi_paged_workspace(shape, 1, desc->head_dim);
     if (!workspace || workspace_bytes < need) return fail(HEXI_EWORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(workspace)) return fail(HEXI_EALIGN, "the workspace must be 16-byte aligned");
     g.table = table; g.row_start = row_start; g.kv_len = kv_len; g.q_start = q_start; g.kv_start = kv_start;
@@ -697,13 +697,14 @@ HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cac
     g.scale = desc->softmax_scale;
     a.q = q; a.k = k_cache; a.v = v_cache; a.o = o; a.lse = lse;
     a.out_bf16 = o_dtype == HEXI_BF16;
-    a.n_ranges = shape.ranges;
-    a.min_blocks = shape.min_blocks;
-    a.n_active = (int*)workspace;
-    a.tiles = (PagedTile*)((char*)workspace + 256);
-    a.part_o = (float*)(a.tiles + shape.ranges);
-    a.part_lse = a.part_o + (size_t)2 * (size_t)shape.ranges * (size_t)shape.vectors * (size_t)desc->head_dim;
-    const hipError_t e = hexi_launch_paged_attn(a, shape, desc->dtype, desc->head_dim, (hipStream_t)hip_stream);
+    PagedArgs large = a;
+    hexi_paged_place(shape, 0, desc->head_dim, (char*)workspace, &a);
+    hexi_paged_place(shape, 1, desc->head_dim, (char*)workspace + few_bytes, &large);
+    hipStream_t s = (hipStream_t)hip_stream;
+    hipError_t e = hipSuccess;
+    if (shape.ranges[1]) e = hexi_launch_paged_large(large, desc->head_dim, s);
+    if (e == hipSuccess && shape.ranges[0]) e = hexi_launch_paged_few(a, desc->dtype, desc->head_dim, s);
+    if (e == hipSuccess && shape.splits) e = hexi_launch_paged_join(a, large, desc->head_dim, s);
     if (e != hipSuccess) return fail(HEXI_EHIP, "paged attention launch failed: %s", hipGetErrorString(e));
     return HEXI_OK;
 }

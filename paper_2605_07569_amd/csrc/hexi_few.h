@@ -77,7 +77,20 @@ template <int D> struct Ops<uint16_t, D> {
         const bf16x4 b = {(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
 #pragma unroll
         for (int e = 0; e < 4; ++e) l += (float)b[e];
-        const s16x4 pb = __builtin_bit_cast(s16x4, b);
+        products(acc, __builtin_bit_cast(s16x4, b));
+    }
+    // with weights of 16 bits, the rounded ones and what rounding left of them
+    __device__ __forceinline__ void sums_fine(f32x4 (&acc)[NC], const f32x4& p, float& l) const
+    {
+        const bf16x4 b = {(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
+        const bf16x4 rest = {(__bf16)(p[0] - (float)b[0]), (__bf16)(p[1] - (float)b[1]), (__bf16)(p[2] - (float)b[2]), (__bf16)(p[3] - (float)b[3])};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l += (float)b[e] + (float)rest[e];
+        products(acc, __builtin_bit_cast(s16x4, b));
+        products(acc, __builtin_bit_cast(s16x4, rest));
+    }
+    __device__ __forceinline__ void products(f32x4 (&acc)[NC], const s16x4& pb) const
+    {
 #pragma unroll
         for (int i = 0; i < PIECE / 2; ++i) {      // columns 2 i (low halves) and 2 i + 1 (high ones) of the four rows
             const uint2 lo = {__builtin_amdgcn_perm(v[1][i], v[0][i], 0x05040100), __builtin_amdgcn_perm(v[3][i], v[2][i], 0x05040100)};

@@ -16,7 +16,9 @@ struct PagedGeom {
     Divisor by_page;
     int window, n_sink;               // window: 2^31 - 1 without one
     int nq, n_runs, most;             // most: heads of the run that has most
+    int regular;                      // run i: kv head i, heads i most .. i most + most - 1
     float scale;
+    double per_block;                 // 1 / (64 most)
     // The q heads sorted by the kv head that they read: run i, heads head[first[i]] .. head[first[i + 1] - 1], reads kv head kvh[i].
     unsigned char kvh[HEXI_MAX_HEADS], head[HEXI_MAX_HEADS], first[HEXI_MAX_HEADS + 1];
 };
@@ -37,6 +39,9 @@ inline void hexi_paged_runs(const signed char* kv_of_q, int nq, int nkv, PagedGe
     }
     g->first[n] = (unsigned char)at;
     g->n_runs = n;
+    g->per_block = 1.0 / (64.0 * g->most);
+    g->regular = n * g->most == nq;
+    for (int i = 0; i < nq; ++i) g->regular = g->regular && g->head[i] == i && (i >= n || g->kvh[i] == i);
 }
 
 __host__ __device__ __attribute__((always_inline)) inline int paged_clamp(long long x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : (int)x; }
@@ -108,49 +113,119 @@ struct PagedWriteArgs {
     Divisor by_page, by_row, by_head;      // pieces of a row, of a head
 };
 
-// Attention.  The work is the tiles of all requests (query vectors of one head run, row by row) times the 64-key blocks that the request's rows see, one behind the other; every
-// workgroup takes an equal range of it.  A range that ends inside a tile leaves a partial result: part_o [2 ranges][vectors][d], normalised, and part_lse; piece 2 w + 1 is that of a tile
-// which range w starts, 2 w that of one which it goes on with.  tiles[w]: the tile that range w starts and does not end, for the joining launch.
+// Attention.
+//
+// The query vectors of a request and a head run (row by row, a row's heads side by side) are cut into tiles; a tile costs about the 64-key blocks that its last row sees and a start.
+// All tiles of all requests lie one behind the other (request, run, tile), and every workgroup takes an equal range of their summed costs: contexts of all lengths fill the chip evenly,
+// and neighbouring ranges, which are dealt to one XCD, share keys.  A range that ends inside a tile leaves a partial result of it: part_o [2 ranges][vectors][d], normalised, and part_lse; piece
+// 2 w + 1 is that of a tile which range w starts, 2 w that of one which it goes on with, and tiles[w] tells the joining launch of the tile that range w starts and does not end.
 struct PagedTile { int pieces, run, row0, rows, v0, pad[3]; };      // pieces: 0 where there is no such tile; v0: first vector
+
+// Costs of a request's tiles, in blocks; before(t): of the first t tiles of a run, by the closed form of its sums, so that no table is needed.
+// Of tile t the last row sees keys up to at + (t + 1) vectors / most, and a window leaves out what the first one no longer sees.
+struct PagedCost {
+    long long up, low, top;           // most x (keys up to the last row's own, of tile 0), most x (keys in front of its first row's window), most x kv
+    double per_block;                 // 1 / (64 most)
+    int shift, start;                 // vectors of a tile: 2^shift; of every tile
+    int up0, up1, low0, low1;         // tiles in front of those that see a key, and of those that see them all; of those with keys in front of the window, and with all there
+    __host__ __device__ __attribute__((always_inline)) PagedCost(const PagedGeom& g, const PagedRequest& q, int shift_, int start_, int tiles)
+    {
+        shift = shift_;
+        per_block = g.per_block;
+        start = start_ + (q.sinks + 63) / 64;
+        top = (long long)g.most * q.kv;
+        up = g.most * q.at + (1 << shift);
+        low = g.most * (q.at + 1 - g.window);
+        up0 = first_over(up, 0, tiles); up1 = first_over(up, top, tiles);
+        low0 = first_over(low, 0, tiles); low1 = first_over(low, top, tiles);
+    }
+    // first t with a + t 2^shift > x, no more than `tiles`
+    __host__ __device__ __attribute__((always_inline)) int first_over(long long a, long long x, int tiles) const
+    {
+        if (a > x) return 0;
+        const long long t = ((x - a) >> shift) + 1;
+        return t < tiles ? (int)t : tiles;
+    }
+    // sum over i < t of a + i 2^shift, cut off at 0 and at top
+    __host__ __device__ __attribute__((always_inline)) long long sum(long long a, int t0, int t1, int t) const
+    {
+        const long long n = t < t0 ? 0 : (t < t1 ? t : t1) - t0;
+        return n * (a + ((long long)t0 << shift)) + ((n * (n - 1) / 2) << shift) + (t > t1 ? (long long)(t - t1) * top : 0);
+    }
+    // (rounded to a double, divided and rounded down: it never falls, and is the same wherever it is worked out)
+    __host__ __device__ __attribute__((always_inline)) long long before(int t) const { return (long long)((double)(sum(up, up0, up1, t) - sum(low, low0, low1, t)) * per_block) + (long long)t * start; }
+    // the tile that cost x lies in
+    __host__ __device__ __attribute__((always_inline)) int tile_of(long long x, int tiles) const
+    {
+        int lo = 0, hi = tiles;
+        while (hi - lo > 1) {
+            const int mid = lo + (hi - lo) / 2;
+            if (before(mid) <= x) lo = mid; else hi = mid;
+        }
+        return lo;
+    }
+};
+
+// Tiles of one head run of a request that a kernel takes: those with up to `few` vectors are one kernel's, the others another's.
+struct PagedShare { int shift, few, takes_few, takes_many, start, min_cost; };      // 2^shift vectors to a tile; limit; which of them; cost of a tile's start; the least of a range
+__host__ __device__ __attribute__((always_inline)) inline int paged_tiles(const PagedGeom& g, const PagedShare& s, const PagedRequest& q)
+{
+    const long long n = (long long)q.rows * g.most;
+    return n == 0 || !(n <= s.few ? s.takes_few : s.takes_many) ? 0 : (int)((n + (1 << s.shift) - 1) >> s.shift);
+}
+
 struct PagedArgs {
     PagedGeom g;
+    PagedShare share;
     const void *q, *k, *v;
     void* o;
     float* lse;               // may be null
     int out_bf16;
-    int n_ranges, min_blocks; // a range has at least so many blocks
+    int n_ranges;
     int* n_active;            // ranges that there is work for
     PagedTile* tiles;
     float *part_o, *part_lse;
 };
 
-// How a call is launched.
+// How a call is launched: by the kernel for few vectors to a key, by the one for many, or by both, each with the requests that it is for.
 struct PagedShape {
-    int vectors;              // of a tile: 16 or 32
-    int ranges;               // workgroups, a multiple of 8
-    int min_blocks;
-    bool splits;              // a tile can be cut: a second launch joins
+    PagedShare share[2];
+    int ranges[2];            // workgroups, multiples of 8; 0: the kernel is not launched
+    bool splits;              // a tile can be cut: a further launch joins
 };
-inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
+inline PagedShape hexi_paged_shape(int dtype, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
 {
     PagedShape s;
-    const long long most_vectors = max_rows * most;
-    s.vectors = most_vectors > 16 ? 32 : 16;
-    s.min_blocks = 2;
-    const long long blocks = (max_keys + 63) / 64 + 1, tiles = n_runs * ((n_rows * most + s.vectors - 1) / s.vectors + (n_requests < n_rows ? n_requests : n_rows));
-    const int full = 512;
-    long long n = tiles > full ? full : tiles * blocks / s.min_blocks + 1;
-    n = n > full ? full : n;
-    s.ranges = (int)((n + 7) / 8 * 8);
-    s.splits = blocks > s.min_blocks;
-    (void)d;
+    const bool large = dtype == HEXI_BF16 && max_rows * most > 32;
+    const bool few = !large || n_requests > 1;
+    s.share[0] = PagedShare{max_rows * most > 16 ? 5 : 4, 32, 1, !large, 1, 2};
+    s.share[1] = PagedShare{8, 32, !few, 1, 4, 12};
+    const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
+    for (int i = 0; i < 2; ++i) {
+        const long long tiles = n_runs * ((n_rows * most >> s.share[i].shift) + most_requests), full = i == 0 ? 512 : 256;
+        long long n = tiles > full ? full : tiles * (blocks + s.share[i].start) / s.share[i].min_cost + 1;
+        n = n > full ? full : n;
+        s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;
+    }
+    s.splits = blocks > 2;
     return s;
 }
-inline size_t hexi_paged_workspace(const PagedShape& s, int d)
+inline size_t hexi_paged_workspace(const PagedShape& s, int i, int d)      // of one kernel
 {
-    return 256 + (size_t)s.ranges * sizeof(PagedTile) + (size_t)2 * (size_t)s.ranges * (size_t)s.vectors * (size_t)(d + 1) * 4;
+    return s.ranges[i] == 0 ? 0 : 256 + (size_t)s.ranges[i] * sizeof(PagedTile) + (size_t)2 * (size_t)s.ranges[i] * ((size_t)(d + 1) * 4 << s.share[i].shift);
+}
+inline void hexi_paged_place(const PagedShape& s, int i, int d, char* workspace, PagedArgs* a)
+{
+    a->share = s.share[i];
+    a->n_ranges = s.ranges[i];
+    a->n_active = (int*)workspace;
+    a->tiles = (PagedTile*)(workspace + 256);
+    a->part_o = (float*)(a->tiles + s.ranges[i]);
+    a->part_lse = a->part_o + (size_t)2 * (size_t)s.ranges[i] * ((size_t)d << s.share[i].shift);
 }
 
 hipError_t hexi_launch_paged_plan(const PagedPlanArgs& a, hipStream_t s);
 hipError_t hexi_launch_paged_write(const PagedWriteArgs& a, int x_dtype, int y_dtype, hipStream_t s);
-hipError_t hexi_launch_paged_attn(const PagedArgs& a, const PagedShape& shape, int dtype, int d, hipStream_t s);
+hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, hipStream_t s);
+hipError_t hexi_launch_paged_large(const PagedArgs& a, int d, hipStream_t s);
+hipError_t hexi_launch_paged_join(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s);

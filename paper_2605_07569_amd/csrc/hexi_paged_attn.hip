@@ -1,203 +1,52 @@
-// Attention of new tokens over a paged cache: 16 or 32 query vectors to a tile, and the join of tiles that several workgroups share.
+// Attention of new tokens over a paged cache: tiles of 16 or 32 query vectors, and the join of tiles that several workgroups share.
 //
-// The query vectors of a request and a kv head are its rows' q heads that read it, row by row.  A workgroup's four wavefronts split every 64-key block of a tile, 16 keys each, which lie on
-// one page; operands come straight from memory, the next block's while this one is multiplied (hexi_few.h has the products).  Every wavefront keeps a softmax of its own; LDS joins the four at a tile's end.
+// A workgroup's four wavefronts split every 64-key block of a tile, 16 keys each, which lie on one page; operands come straight from memory, the next block's while this one is multiplied
+// (hexi_few.h has the products).  Every wavefront keeps a softmax of its own; LDS joins the four at a tile's end.
+// P as an operand: bf16 where results are bf16 (FINE off: a weight is off by at most 2^-8 of itself, less than the result's own rounding in all), two bf16 values where they are fp32 (2^-16: partial
+// results of a context on several devices); the sum that normalises is that of the weights as they are multiplied.
 // What bounds it: few vectors a key, so the reads of K and V.
 #include "hexi_few.h"
-#include "hexi_paged.h"
-#include "hexi_window_plain.h"
+#include "hexi_paged_tiles.h"
 
 namespace {
 
-constexpr int KEYS = 64, NW = 4;
+constexpr int NW = 4;
 
-// A tile of a request.
-struct Tile {
-    PagedRequest q;
-    WinSpan<KEYS> span;       // of all rows of the request
-    int r, run, count, v0, vectors;      // count: heads of the run; vectors: of the tile, 0 or less: none
-};
-
-// ---- element by element ----
-// A tile's vectors, eight lanes each, walk the keys of blocks [b0, b1) of the request's run that they see, one by one: what a vector does not see is not read into it.
-template <class T, int D> __device__ __forceinline__ void plain_tile(const PagedArgs& a, const Tile& t, const int b0, const int b1, float* part_o, float* part_lse)
-{
-    constexpr int N = D / win_plain::LANES;
-    const PagedGeom& g = a.g;
-    const int col = (int)threadIdx.x % win_plain::LANES * N;
-    const int* table = g.table + (long long)t.r * g.columns;
-    for (int i = (int)threadIdx.x / win_plain::LANES; i < t.vectors; i += (int)blockDim.x / win_plain::LANES) {
-        const int row = (t.v0 + i) / t.count, h = g.head[g.first[t.run] + (t.v0 + i) - row * t.count];
-        const WinKeys w = paged_keys_of_row(g, t.q, row);
-        const long long head = (long long)g.kvh[t.run] * g.stride_head + col;
-        float q[N], acc[N];
-        win_plain::load_cols(static_cast<const T*>(a.q) + (long long)(t.q.row0 + row) * g.q_stride_tok + (long long)h * g.q_stride_head + col, q);
-#pragma unroll
-        for (int c = 0; c < N; ++c) acc[c] = 0.f;
-        float m = -INFINITY, l = 0.f;
-        for (int b = b0; b < b1; ++b) {
-            const int k0 = KEYS * t.span.block(b);
-            for (int j = k0; j < k0 + KEYS && j < w.hi; ++j) {
-                if (j >= w.sink && j < w.lo) continue;
-                const PagedPlace p = paged_place(g, table, j);
-                if (p.id < 0) continue;
-                const long long at = (long long)p.id * g.stride_page + (long long)p.row * g.stride_tok + head;
-                float x[N];
-                win_plain::load_cols(static_cast<const T*>(a.k) + at, x);
-                const float s = win_plain::dot(q, x) * g.scale;
-                win_plain::load_cols(static_cast<const T*>(a.v) + at, x);
-                if (s > m) {
-                    const float alpha = expf(m - s);   // (m = -inf: 0)
-                    m = s;
-                    l *= alpha;
-#pragma unroll
-                    for (int c = 0; c < N; ++c) acc[c] *= alpha;
-                }
-                const float p_j = s == -INFINITY ? 0.f : expf(s - m);
-                l += p_j;
-#pragma unroll
-                for (int c = 0; c < N; ++c) acc[c] = fmaf(p_j, x[c], acc[c]);
-            }
-        }
-        const float lse = l == 0.f ? -INFINITY : m + logf(l), r = l == 0.f ? 0.f : 1.0f / l;
-        if (part_o) {
-            if (col == 0) part_lse[i] = lse;
-#pragma unroll
-            for (int c = 0; c < N; c += 4) win_plain::store4(part_o, i * D + col + c, false, r * acc[c], r * acc[c + 1], r * acc[c + 2], r * acc[c + 3]);
-        } else {
-            if (col == 0 && a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
-            const long long at = ((long long)(t.q.row0 + row) * g.nq + h) * D + col;
-#pragma unroll
-            for (int c = 0; c < N; c += 4) win_plain::store4(a.o, at + c, a.out_bf16, r * acc[c], r * acc[c + 1], r * acc[c + 2], r * acc[c + 3]);
-        }
-    }
-}
-
-// ---- work ----
-
-struct Work { PagedRequest q; WinSpan<KEYS> span; int tiles, blocks; };     // of one head run
-template <int NV> __device__ __forceinline__ Work work_of(const PagedGeom& g, int r)
-{
-    Work w;
-    w.q = paged_request(g, r);
-    w.tiles = w.blocks = 0;
-    if (w.q.rows > 0) {
-        w.span = WinSpan<KEYS>(paged_keys_of_row(g, w.q, 0), paged_keys_of_row(g, w.q, w.q.rows - 1), w.q.kv);
-        w.tiles = (w.q.rows * g.most + NV - 1) / NV;
-        w.blocks = w.span.n_blocks > 0 ? w.span.n_blocks : 1;      // (a tile that sees nothing is written too)
-    }
-    return w;
-}
-
-template <class T, int D, int NG>
-__global__ void __launch_bounds__(64 * NW) paged_few_kernel(const PagedArgs a)
+template <class T, int D, int NG, bool FINE>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 4 && D * NG == 256 ? 1 : 2) paged_few_kernel(const PagedArgs a)
 {
     using O = Ops<T, D>;
     constexpr int NV = 16 * NG;
     __shared__ __attribute__((aligned(16))) float acc_of[NW][NV][D + 4];
     __shared__ float stat[3][NW][NV];             // reference, sum of P, sum of P as it was multiplied
-    __shared__ long long of_wave[NW], found[2];
+    __shared__ typename PagedWalk<64 * NW>::Shared shared;
     const PagedGeom& g = a.g;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = lane >> 4, l16 = lane & 15;
-
-    // The ranges: sums over the requests, a few to a thread.
-    const int each = (g.n_requests + 64 * NW - 1) / (64 * NW), r0 = tid * each < g.n_requests ? tid * each : g.n_requests, r1 = r0 + each < g.n_requests ? r0 + each : g.n_requests;
-    long long mine = 0;
-    for (int r = r0; r < r1; ++r) {
-        const Work w = work_of<NV>(g, r);
-        mine += (long long)w.tiles * w.blocks * g.n_runs;
-    }
-    long long before = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const long long y = __shfl_up(before, off, 64);
-        if (lane >= off) before += y;
-    }
-    if (lane == 63) of_wave[wave] = before;
-    __syncthreads();
-    before -= mine;
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        if (w < wave) before += of_wave[w];
-        total += of_wave[w];
-    }
-    long long range = (total + a.n_ranges - 1) / a.n_ranges;
-    range = range < a.min_blocks ? a.min_blocks : range;
-    const int active = (int)((total + range - 1) / range), per_xcd = (active + 7) / 8;
-    if (blockIdx.x == 0 && tid == 0) *a.n_active = active;
-    const int slot = (int)blockIdx.x >> 3, me = ((int)blockIdx.x & 7) * per_xcd + slot;
-    if (slot >= per_xcd || me >= active) return;
-    const long long start = me * range, end = start + range < total ? start + range : total;
-    if (start >= before && start < before + mine) {
-        long long at = before;
-        for (int r = r0; r < r1; ++r) {
-            const Work w = work_of<NV>(g, r);
-            const long long n = (long long)w.tiles * w.blocks * g.n_runs;
-            if (start < at + n) { found[0] = r; found[1] = at; break; }
-            at += n;
-        }
-    }
-    __syncthreads();
-    int r = __builtin_amdgcn_readfirstlane((int)found[0]);
-    long long first = found[1];                   // work in front of request r
+    PagedWalk<64 * NW> walk(a, shared);
+    if (!walk.any) return;
     const float c_hi = g.scale * LOG2E_HI, c_lo = fmaf(g.scale, LOG2E_HI, -c_hi) + g.scale * LOG2E_LO;
     PagedTile open = {0, 0, 0, 0, 0, {0, 0, 0}};
-    bool alone = true;                            // no wavefront is behind in a tile's end
-
-    for (long long at = start; at < end;) {
-        Work w = work_of<NV>(g, r);
-        const long long n = (long long)w.tiles * w.blocks * g.n_runs;
-        if (at >= first + n) { first += n; ++r; continue; }
-        // the tile that `at` lies in, and which of its blocks are this range's
-        Tile t;
-        const long long in = (at - first) / w.blocks;
-        const int b0 = __builtin_amdgcn_readfirstlane((int)(at - first - in * w.blocks));
-        const long long tile_at = at - b0, tile_end = tile_at + w.blocks;
-        const int b1 = __builtin_amdgcn_readfirstlane((int)((tile_end < end ? tile_end : end) - tile_at));
-        const bool starts = b0 == 0, ends = b1 == w.blocks;
-        at = tile_at + b1;
-        t.r = r;
-        t.q = w.q;
-        t.span = w.span;
-        t.run = __builtin_amdgcn_readfirstlane((int)(in / w.tiles));
-        t.count = g.first[t.run + 1] - g.first[t.run];
-        t.v0 = __builtin_amdgcn_readfirstlane((int)(in - (long long)t.run * w.tiles)) * NV;
-        t.vectors = w.q.rows * t.count - t.v0;
-        if (t.vectors > NV) t.vectors = NV;
-        if (t.vectors <= 0) continue;
-        const bool part = !(starts && ends);
-        if (starts && part) open = {(int)((tile_end - 1) / range) - me + 1, t.run, t.q.row0, t.q.rows, t.v0, {0, 0, 0}};
-        const long long piece = 2 * (long long)me + (starts ? 1 : 0);
-        float* const part_o = part ? a.part_o + piece * NV * D : nullptr;
-        float* const part_lse = part ? a.part_lse + piece * NV : nullptr;
-
-        // what the tile's own rows see: keys [0, last], and blocks of the run in front of and behind which there is nothing
-        const int row_a = t.v0 / t.count, row_b = (t.v0 + t.vectors - 1) / t.count;
-        const WinKeys keys_a = paged_keys_of_row(g, t.q, row_a), keys_b = paged_keys_of_row(g, t.q, row_b);
-        const int last = __builtin_amdgcn_readfirstlane(keys_b.hi > keys_b.sink ? keys_b.hi : keys_b.sink) - 1;      // -1: nothing
-        int lane_row[NG], lane_head[NG];
+    Tile t;
+    for (bool again = false; walk.next(t, open); again = true) {
+        // the lane's vectors; of one that is none the first one's row again, which sees no key
         WinKeys keys[NG];
         decltype(O::k) q[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-            const int v = 16 * i + l16 < t.vectors ? t.v0 + 16 * i + l16 : t.v0;      // (of no vector: the first one again)
-            lane_row[i] = v / t.count;
-            lane_head[i] = g.head[g.first[t.run] + v - lane_row[i] * t.count];
-            keys[i] = paged_keys_of_row(g, t.q, lane_row[i]);
-            O::row(q[i], static_cast<const T*>(a.q) + (long long)(t.q.row0 + lane_row[i]) * g.q_stride_tok + (long long)lane_head[i] * g.q_stride_head, grp);
-            if (16 * i + l16 >= t.vectors) keys[i] = WinKeys{0, 0, 0};
+            const bool real = 16 * i + l16 < t.vectors;
+            const int v = real ? 16 * i + l16 : 0, row = t.row_of(v);
+            keys[i] = paged_keys_of_row(g, t.q, row);
+            O::row(q[i], static_cast<const T*>(a.q) + (long long)(t.q.row0 + row) * g.q_stride_tok + (long long)t.head_of(g, v, row) * g.q_stride_head, grp);
+            if (!real) keys[i] = WinKeys{0, 0, 0};
         }
-        (void)keys_a;
-
-        const int* table = g.table + (long long)r * g.columns;
-        const long long head = (long long)g.kvh[t.run] * g.stride_head;
-        int ids = -1, page_rows = 0;              // lane i: page and row of this wavefront's first key in block `listed` + i
-        int listed = 0;
+        const int* table = g.table + (long long)t.r * g.columns;
+        const long long head = (long long)t.kv_head(g) * g.stride_head;
+        const int last = t.last;
+        int ids = -1, page_rows = 0, listed = 0;  // lane i: page and row of this wavefront's first key in block `listed` + i
         auto list = [&](int b) {
             listed = b;
-            const int key = KEYS * t.span.block(b + lane) + 16 * wave;
+            const int key = PAGED_KEYS * t.span.block(b + lane) + 16 * wave;
             const PagedPlace p = paged_place(g, table, key < last ? key : last & ~15);
             ids = p.id;
             page_rows = p.row;
@@ -205,7 +54,7 @@ __global__ void __launch_bounds__(64 * NW) paged_few_kernel(const PagedArgs a)
         struct Block { O ops; int key; bool seen; };
         auto load = [&](Block& x, int b) {
             if (b - listed >= 64) list(b);
-            const int key = KEYS * t.span.block(b) + 16 * wave;
+            const int key = PAGED_KEYS * t.span.block(b) + 16 * wave;
             const int id = __builtin_amdgcn_readlane(ids, b - listed), row = __builtin_amdgcn_readlane(page_rows, b - listed);
             x.key = key;
             x.seen = id >= 0;
@@ -250,28 +99,28 @@ __global__ void __launch_bounds__(64 * NW) paged_few_kernel(const PagedArgs a)
                 }
 #pragma unroll
                 for (int c = 0; c < O::NC; ++c) acc[i][c] *= alpha;
-                x.ops.sums(acc[i], s, l_used[i]);
+                if constexpr (FINE) x.ops.sums_fine(acc[i], s, l_used[i]);
+                else x.ops.sums(acc[i], s, l_used[i]);
             }
         };
-        if (last >= 0) {
+        if (t.b0 < t.b1) {
             Block x, y;
-            int b = b0;
+            int b = t.b0;
             list(b);
             load(x, b);
-            for (; b + 1 < b1; b += 2) {
+            for (; b + 1 < t.b1; b += 2) {
                 load(y, b + 1);
                 __builtin_amdgcn_sched_barrier(0);
                 use(x);
-                if (b + 2 < b1) load(x, b + 2);
+                if (b + 2 < t.b1) load(x, b + 2);
                 __builtin_amdgcn_sched_barrier(0);
                 use(y);
             }
-            if (b < b1) use(x);
+            if (b < t.b1) use(x);
         }
 
         // the four wavefronts' results joined
-        if (!alone) __syncthreads();              // the last tile's have been read
-        alone = false;
+        if (again) __syncthreads();               // the last tile's have been read
         float z = 0.f;
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
@@ -288,9 +137,11 @@ __global__ void __launch_bounds__(64 * NW) paged_few_kernel(const PagedArgs a)
         }
         // (a key that a vector does not see has P = 0, and 0 x inf is NaN: what is not finite is done again element by element)
         if (__syncthreads_or(z != 0.f)) {
-            plain_tile<T, D>(a, t, b0, b1, part_o, part_lse);
+            plain_tile<T, D>(t);
             continue;
         }
+        const PagedArgs& a = paged_args();
+        const PagedGeom& g = a.g;
         for (int p = tid; p < NV * D / 4; p += 64 * NW) {       // four columns of a vector
             const int i = p / (D / 4), c = 4 * (p % (D / 4));
             if (i >= t.vectors) break;
@@ -308,32 +159,67 @@ __global__ void __launch_bounds__(64 * NW) paged_few_kernel(const PagedArgs a)
             }
             const float lse = sum == 0.f ? -INFINITY : fmaf(mm, g.scale, logf(sum));
             o *= used == 0.f ? 0.f : 1.0f / used;
-            if (part) {
-                if (c == 0) part_lse[i] = lse;
-                win_plain::store4(part_o, i * D + c, false, o[0], o[1], o[2], o[3]);
+            if (t.piece >= 0) {
+                const long long at = t.piece * NV + i;
+                if (c == 0) a.part_lse[at] = lse;
+                win_plain::store4(a.part_o, at * D + c, false, o[0], o[1], o[2], o[3]);
             } else {
-                const int row = (t.v0 + i) / t.count, h = g.head[g.first[t.run] + t.v0 + i - row * t.count];
+                const int row = t.row_of(i), h = t.head_of(g, i, row);
                 if (c == 0 && a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
-                win_plain::store4(a.o, ((long long)(t.q.row0 + row) * g.nq + h) * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
+                win_plain::store4(a.o, paged_out(a, t, row, h) * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
             }
         }
     }
-    if (tid == 0) a.tiles[me] = open;
+    if (tid == 0) paged_args().tiles[walk.me] = open;
 }
 
-// The pieces of a tile joined, as hexi_attn_merge_lse joins two.  Workgroup (w, y): the tile that range w starts and does not end, every gridDim.y-th vector of it.
-template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs a, const int nv)
+// The pieces of a tile joined, as hexi_attn_merge_lse joins two.  Workgroup (w, y): the tile that range w starts and does not end.  Of few pieces a thread takes four columns of a
+// vector and reads them all; of many a workgroup takes a vector at a time, eight or sixteen threads to its columns.
+template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const PagedArgs few, const PagedArgs large, const int n_few)
 {
-    constexpr int D4 = D / 4, G = 256 / D4, MAX = 1024;
+    constexpr int D4 = D / 4, G = 256 / D4, MAX = 512, FEW = 8;
     __shared__ float weight[MAX], reduced[4];
     __shared__ __attribute__((aligned(16))) float sum[G][D];
-    const PagedGeom& g = a.g;
-    const int w = (int)blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool second = (int)blockIdx.x >= n_few;
+    const PagedArgs& a = second ? large : few;
+    const PagedGeom& g = few.g;
+    const int w = (int)blockIdx.x - (second ? n_few : 0), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int active = *a.n_active;
     const PagedTile t = a.tiles[w];
     if (w >= active || t.pieces == 0) return;
-    const int count = g.first[t.run + 1] - g.first[t.run], left = t.rows * count - t.v0, vectors = left < nv ? left : nv;
+    const int nv = 1 << a.share.shift, count = g.regular ? g.most : g.first[t.run + 1] - g.first[t.run], left = t.rows * count - t.v0, vectors = left < nv ? left : nv;
     auto piece_of = [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); };
+    auto put = [&](int i, int c, const f32x4& o, float m, float total) {
+        const float r = total == 0.f ? 0.f : 1.0f / total;
+        const int row = (int)((unsigned)(t.v0 + i) / (unsigned)count), k = t.v0 + i - row * count, h = g.regular ? t.run * count + k : g.head[g.first[t.run] + k];
+        if (c == 0 && a.lse) a.lse[(long long)h * g.n_rows + t.row0 + row] = total == 0.f ? -INFINITY : m + logf(total);
+        win_plain::store4(a.o, ((long long)(t.row0 + row) * g.nq + h) * D + c, a.out_bf16, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
+    };
+    if (t.pieces <= FEW) {
+        for (int p = (int)blockIdx.y * 256 + tid; p < vectors * D4; p += (int)gridDim.y * 256) {
+            const int i = p / D4, c = 4 * (p % D4);
+            float l[FEW], m = -INFINITY, total = 0.f;
+            f32x4 x[FEW], o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < FEW; ++k) {
+                const long long at = (long long)piece_of(k < t.pieces ? k : 0) * nv + i;
+                l[k] = k < t.pieces ? a.part_lse[at] : -INFINITY;
+                x[k] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + c);
+            }
+#pragma unroll
+            for (int k = 0; k < FEW; ++k) m = fmaxf(m, l[k]);
+            if (m == -INFINITY) m = 0.f;          // no weight at all, or NaN alone
+#pragma unroll
+            for (int k = 0; k < FEW; ++k) {
+                if (k >= t.pieces) break;
+                const float e = expf(l[k] - m);
+                total += e;
+                o += e * x[k];
+            }
+            put(i, c, o, m, total);
+        }
+        return;
+    }
     for (int i = blockIdx.y; i < vectors; i += gridDim.y) {
         float m = -INFINITY;
         for (int p = tid; p < t.pieces; p += 256) {
@@ -346,42 +232,60 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
         if (lane == 0) reduced[wave] = m;
         __syncthreads();
         m = fmaxf(fmaxf(reduced[0], reduced[1]), fmaxf(reduced[2], reduced[3]));
-        if (m == -INFINITY) m = 0.f;              // no weight at all, or NaN alone
+        if (m == -INFINITY) m = 0.f;
         float total = 0.f;
-        for (int p = 0; p < t.pieces; ++p) total += expf(weight[p] - m);
+        for (int p = tid; p < t.pieces; p += 256) {
+            const float e = expf(weight[p] - m);
+            weight[p] = e;
+            total += e;
+        }
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) total += __shfl_xor(total, off, 64);
+        __syncthreads();                          // the maxima have been read
+        if (lane == 0) reduced[wave] = total;
+        __syncthreads();
+        total = (reduced[0] + reduced[1]) + (reduced[2] + reduced[3]);
         const int c = 4 * (tid % D4), p0 = tid / D4;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int p = p0; p < t.pieces; p += G) o += expf(weight[p] - m) * *reinterpret_cast<const f32x4*>(a.part_o + ((long long)piece_of(p) * nv + i) * D + c);
+#pragma unroll 16
+        for (int p = p0; p < t.pieces; p += G) o += weight[p] * *reinterpret_cast<const f32x4*>(a.part_o + ((long long)piece_of(p) * nv + i) * D + c);
         *reinterpret_cast<f32x4*>(&sum[p0][c]) = o;
         __syncthreads();
         if (tid < D4) {
             o = *reinterpret_cast<const f32x4*>(&sum[0][c]);
 #pragma unroll
             for (int x = 1; x < G; ++x) o += *reinterpret_cast<const f32x4*>(&sum[x][c]);
-            o *= total == 0.f ? 0.f : 1.0f / total;
-            const int row = (t.v0 + i) / count, h = g.head[g.first[t.run] + t.v0 + i - row * count];
-            if (tid == 0 && a.lse) a.lse[(long long)h * g.n_rows + t.row0 + row] = total == 0.f ? -INFINITY : m + logf(total);
-            win_plain::store4(a.o, ((long long)(t.row0 + row) * g.nq + h) * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
+            put(i, c, o, m, total);
         }
         __syncthreads();
     }
 }
 
-template <class T, int D> void launch_few(const PagedArgs& a, const PagedShape& shape, hipStream_t s)
+template <class T, int D, bool FINE> void launch_few(const PagedArgs& a, hipStream_t s)
 {
-    if (shape.vectors == 16) paged_few_kernel<T, D, 1><<<a.n_ranges, 64 * NW, 0, s>>>(a);
-    else paged_few_kernel<T, D, 2><<<a.n_ranges, 64 * NW, 0, s>>>(a);
-    if (shape.splits) paged_join_kernel<D><<<dim3((unsigned)a.n_ranges, 4u), 256, 0, s>>>(a, shape.vectors);
+    if (a.share.shift == 4) paged_few_kernel<T, D, 1, FINE><<<a.n_ranges, 64 * NW, 0, s>>>(a);
+    else paged_few_kernel<T, D, 2, FINE><<<a.n_ranges, 64 * NW, 0, s>>>(a);
 }
 
 }  // namespace
 
-hipError_t hexi_launch_paged_attn(const PagedArgs& a, const PagedShape& shape, int dtype, int d, hipStream_t s)
+hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, hipStream_t s)
 {
     if (dtype == HEXI_F32) {
-        if (d == 128) launch_few<float, 128>(a, shape, s); else launch_few<float, 64>(a, shape, s);
-    } else if (d == 128) launch_few<uint16_t, 128>(a, shape, s);
-    else launch_few<uint16_t, 64>(a, shape, s);
+        if (d == 128) launch_few<float, 128, false>(a, s); else launch_few<float, 64, false>(a, s);
+    } else if (a.out_bf16) {
+        if (d == 128) launch_few<uint16_t, 128, false>(a, s); else launch_few<uint16_t, 64, false>(a, s);
+    } else if (d == 128) launch_few<uint16_t, 128, true>(a, s);
+    else launch_few<uint16_t, 64, true>(a, s);
+    return hipGetLastError();
+}
+
+hipError_t hexi_launch_paged_join(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s)
+{
+    // few tiles that may have many pieces: a workgroup to a vector; many tiles: they have few pieces
+    const long long tiles = few.g.n_runs * (((long long)few.g.n_rows * few.g.most >> 4) + few.g.n_requests);
+    const dim3 grid((unsigned)(few.n_ranges + large.n_ranges), tiles <= 32 ? 16u : tiles <= 256 ? 4u : 2u);
+    if (d == 128) paged_join_kernel<128><<<grid, 256, 0, s>>>(few, large, few.n_ranges);
+    else paged_join_kernel<64><<<grid, 256, 0, s>>>(few, large, few.n_ranges);
     return hipGetLastError();
 }

@@ -1,0 +1,379 @@
+// Attention of many new tokens over a paged cache: bf16 tiles of 256 query vectors, eight wavefronts of 32 each, one workgroup to a CU.
+//
+// The schedule is that of the ring step's 256-row kernel: two groups of four wavefronts, one to each SIMD, alternate between a matrix phase (O^T += V^T P^T of block t - 1, S^T = K Q^T of
+// block t) and a vector phase (softmax of block t, requests of later blocks), one phase apart, so that a SIMD has one wavefront that feeds the matrix pipe and one that does the rest.
+// Group 1 requests K four blocks ahead, group 0 V two.
+//
+// What pages change is how a 64-key block comes to LDS.  A transfer (1 KB: 64 lanes x 16 bytes, back to back) takes its address from a scalar base, the page's, so all its rows have to lie on one page:
+// 4 whole rows (8 at 64 columns), and each wavefront takes the 16 rows of one page by itself.  Rows are not padded then but transfers are, by 16 bytes, and inside one
+// the 16-byte pieces of a row are exchanged by their high bits (`flip`), so that both the 128-bit row reads of K and the transposed 64-bit reads of V^T touch all 64 banks once: of 16 rows
+// of K the same piece lies in four (two) places by flip, moved on by a piece a transfer; four rows of V side by side lie in different quarters by flip.
+#include "hexi_mfma.h"
+#include "hexi_paged_tiles.h"
+
+namespace {
+
+constexpr int TN = PAGED_KEYS, NB = 4, GROUP = 128, WG = 256;      // keys of a block, buffers of either tensor, vectors of a group, of a tile
+constexpr int K_AHEAD = 4, V_AHEAD = 2;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float NEG_BIG = -1.0e30f;        // finite stand-in for "no key seen yet"
+constexpr float RESCALE_SLACK = 8.0f;
+constexpr float SUM_LO = 8.6736174e-19f, SUM_HI = 1.1529215e18f;      // 2^-60, 2^60
+
+template <int D> struct Cfg {
+    static constexpr int NKS = D / 16, NDB = D / 32;               // 16-wide steps over the columns, 32-column blocks of the output
+    static constexpr int ROW = 2 * D, ROWS = 1024 / ROW;           // bytes of a row; rows of a transfer
+    static constexpr int XFER = 1024 + 16, XFERS = TN / ROWS, PER_WAVE = XFERS / 4;
+    static constexpr int TILE = XFERS * XFER;
+    // which of its four places the aligned run of pieces (4 of 16 at 128 columns, 2 of 8 at 64) with number `a` takes in row r of a transfer: a ^ flip(r)
+    static constexpr __host__ __device__ int flip(int r) { return D == 128 ? r & 3 : ((r >> 1) & 1) * 2 + ((r >> 2) & 1); }
+    static constexpr int RUN = D / 32;                             // pieces of a run
+    static constexpr int PITCH = D + 4;                            // floats of a staged output row
+};
+
+template <int D> struct Smem {
+    struct Tiles { unsigned char k[NB][Cfg<D>::TILE], v[NB][Cfg<D>::TILE]; };
+    union { Tiles tiles; float stage[8][32 * Cfg<D>::PITCH + 32]; };
+};
+
+template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_kernel(const PagedArgs a)
+{
+    using C = Cfg<D>;
+    constexpr int NKS = C::NKS, NDB = C::NDB;
+    constexpr bool PAIR_BARRIER = D == 128;     // one workgroup barrier per pair of phases instead of one per phase
+    __shared__ __attribute__((aligned(1024))) Smem<D> sm;
+    __shared__ typename PagedWalk<512>::Shared shared;
+    const PagedGeom& g = a.g;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = wave >> 2, wg = wave & 3;
+    const int l32 = lane & 31, hh = lane >> 5, grp2 = (lane >> 4) & 1, j16 = lane & 15, jj = j16 >> 2;
+
+    // Lane parts of the LDS byte addresses; buffer, key block and step are compile-time offsets of the reads.
+    //   K (ks, 32-key half b) of buffer B: k_addr[run of the piece] + B TILE + b (32 / ROWS) XFER + 16 x (piece's place in its run)
+    //   V^T (16-key step u, 32-column block db, `second` 8 keys) of buffer B: v_addr[db] + B TILE + (16 u + 8 second) / ROWS x XFER
+    // A transposed read hands lane i of a 16-lane group the elements [row0 + e][col0 + i], e = 0..3, where lane j supplies the address of [row0 + j / 4][col0 + 4 (j % 4)].
+    const uint32_t lds_k = (uint32_t)(uintptr_t)(&sm.tiles.k[0][0]), lds_v = (uint32_t)(uintptr_t)(&sm.tiles.v[0][0]);
+    constexpr int K_RUNS = 2 * NKS / C::RUN;      // 4
+    uint32_t k_addr[K_RUNS], v_addr[NDB];
+#pragma unroll
+    for (int i = 0; i < K_RUNS; ++i)
+        k_addr[i] = lds_k + l32 / C::ROWS * C::XFER + l32 % C::ROWS * C::ROW + (i ^ C::flip(l32 % C::ROWS)) * (16 * C::RUN) + 16 * hh;
+    const int vr = (4 * hh + jj) % C::ROWS;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+        const int piece = 4 * db + 2 * grp2 + ((j16 & 3) >> 1);
+        v_addr[db] = lds_v + (4 * hh + jj) / C::ROWS * C::XFER + vr * C::ROW + ((piece / C::RUN) ^ C::flip(vr)) * (16 * C::RUN) + piece % C::RUN * 16 + 8 * (j16 & 1);
+    }
+    // what the lane fetches of a transfer: a row and a piece of it
+    const int fetch_row = lane / (C::ROW / 16), fetch_pos = lane % (C::ROW / 16);
+    const int fetch_piece = ((fetch_pos / C::RUN) ^ C::flip(fetch_row)) * C::RUN + fetch_pos % C::RUN;
+    const uint32_t fetch_off = 2u * (uint32_t)(fetch_row * (int)g.stride_tok + 8 * fetch_piece);
+    const uint32_t fetch_lds = (grp ? lds_k : lds_v) + (uint32_t)(wg * C::PER_WAVE * C::XFER);
+    const float c_log2 = g.scale * LOG2E, inv_c_log2 = 1.0f / c_log2;
+
+    PagedWalk<512> walk(a, shared);
+    if (!walk.any) return;
+    PagedTile open = {0, 0, 0, 0, 0, {0, 0, 0}};
+    Tile t;
+    while (walk.next(t, open)) {
+        const int NT = t.b1 - t.b0, last = t.last;
+        const int my_vector = GROUP * grp + 32 * wg + l32;
+        const bool real = my_vector < t.vectors;
+        const int my_row = t.row_of(real ? my_vector : 0), my_head = t.head_of(g, real ? my_vector : 0, my_row);
+        WinKeys my_keys = {0, 0, 0};
+        if (real) my_keys = paged_keys_of_row(g, t.q, my_row);
+        // what the group's rows see of the blocks, and the range's first block that all of them see
+        WinSpan<TN> span_g(WinKeys{0, 0, 0}, WinKeys{0, 0, 0}, 0);
+        if (GROUP * grp < t.vectors)
+            span_g = WinSpan<TN>(paged_keys_of_row(g, t.q, t.row_of(GROUP * grp)), paged_keys_of_row(g, t.q, t.row_of((GROUP * (grp + 1) < t.vectors ? GROUP * (grp + 1) : t.vectors) - 1)), t.q.kv);
+        span_g.full_sink = paged_uniform(span_g.full_sink); span_g.full_lo = paged_uniform(span_g.full_lo); span_g.full_hi = paged_uniform(span_g.full_hi);
+        const int n_sink_blocks = paged_uniform(t.span.n_sink_blocks), skip = paged_uniform(t.span.skip), b0 = t.b0;
+        auto block_of = [&](int i) { const int b = b0 + i; return b < n_sink_blocks ? b : b + skip; };
+        int first_full = -1;
+        if (NT > 0) {
+            const int b = (span_g.full_lo + TN - 1) / TN, i = (b < n_sink_blocks ? b : b - skip) - b0;
+            if (span_g.full(block_of(0))) first_full = 0;
+            else if (i >= 0 && i < NT && span_g.full(b)) first_full = i;
+        }
+
+        // Q^T operand fragments: lane (vector l32, half hh) holds columns 16 ks + 8 hh .. + 7
+        bf16x8 qf[NKS];
+        {
+            const uint16_t* qp = static_cast<const uint16_t*>(a.q) + (long long)(t.q.row0 + my_row) * g.q_stride_tok + (long long)my_head * g.q_stride_head + 8 * hh;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) pin(qf[ks]);
+        }
+
+        // A wavefront's 16 rows of a block: their page, looked up 64 blocks at a time, a block to a lane.
+        const int* table = g.table + (long long)t.r * g.columns;
+        const char* fetch_src = static_cast<const char*>(grp ? a.k : a.v) + 2 * (long long)t.kv_head(g) * g.stride_head;
+        int ids = -1, page_rows = 0, listed = 0;
+        bool bad = false;                         // a page that the cache does not have
+        auto list = [&](int i) {
+            listed = i;
+            const int key = TN * block_of(i + lane) + 16 * wg;
+            const PagedPlace p = paged_place(g, table, key < last ? key : last & ~15);
+            bad |= p.id < 0 && i + lane < NT;
+            ids = p.id < 0 ? 0 : p.id;
+            page_rows = p.row;
+            asm volatile("" : "+v"(ids), "+v"(page_rows));
+        };
+        auto fetch_tile = [&](int i) {
+            if (i - listed >= 64) list(i);
+            const int key = TN * block_of(i) + 16 * wg;
+            const int id = __builtin_amdgcn_readlane(ids, i - listed), row = __builtin_amdgcn_readlane(page_rows, i - listed);
+            const char* src = fetch_src + 2 * ((long long)id * g.stride_page + (long long)row * g.stride_tok);
+            const uint32_t dst = fetch_lds + (uint32_t)((i & (NB - 1)) * C::TILE);
+            if (key + 15 <= last) {
+#pragma unroll
+                for (int x = 0; x < C::PER_WAVE; ++x)
+                    lds_dma16_base(src + 2 * (long long)(x * C::ROWS) * g.stride_tok, fetch_off, __builtin_amdgcn_readfirstlane(dst + x * C::XFER));
+            } else {   // keys past the last one that is seen: that one again
+                const int most = last - (key < last ? key : last & ~15);
+#pragma unroll
+                for (int x = 0; x < C::PER_WAVE; ++x) {
+                    const int r = x * C::ROWS + fetch_row;
+                    lds_dma16_base(src, 2u * (uint32_t)((r < most ? r : most) * (int)g.stride_tok + 8 * fetch_piece), __builtin_amdgcn_readfirstlane(dst + x * C::XFER));
+                }
+            }
+        };
+
+        f32x16 oacc[NDB];
+        f32x16 s[2];
+        bf16x8 pf[4], rest[FINE ? 4 : 1];         // FINE: P as two bf16 values
+        float m_run, l_run, lr_run, thr_raw;
+
+        // Matrix phase on buffers (B + NB - 1) % NB (V of block t - 1) and B (K of block t).  Steps 0 .. NPV - 1: O^T += V^T P^T, four 16-key steps x NDB 32-column blocks; steps NPV ..
+        // NST - 1: S^T for two 32-key halves.  [FIRST, LAST) selects the steps; operand fragments are requested PF steps ahead.
+        constexpr int NPV = 4 * NDB, NST = NPV + 2 * NKS;
+        auto m_phase = [&](auto bc, auto first_c, auto last_c) __attribute__((always_inline)) {
+            constexpr int B = decltype(bc)::value, FIRST = decltype(first_c)::value, LAST = decltype(last_c)::value;
+            constexpr int PF = 4, NS = PF + 1;
+            constexpr int KOFF = B * C::TILE, VOFF = (B + NB - 1) % NB * C::TILE;
+            s16x4 ta[NS], tb[NS];
+            bf16x8 kb[NS];
+            auto issue = [&](auto stc) __attribute__((always_inline)) {
+                constexpr int st = decltype(stc)::value, slot = (st - FIRST) % NS;
+                if constexpr (st < NPV) {
+                    constexpr int u = st / NDB, db = st % NDB;
+                    lds_issue_tr16<VOFF + 16 * u / C::ROWS * C::XFER>(ta[slot], v_addr[db]);
+                    lds_issue_tr16<VOFF + (16 * u + 8) / C::ROWS * C::XFER>(tb[slot], v_addr[db]);
+                } else {
+                    constexpr int b = (st - NPV) & 1, ks = (st - NPV) >> 1, run = 2 * ks / C::RUN, in_run = 2 * ks % C::RUN;
+                    lds_issue_b128<KOFF + 32 * b / C::ROWS * C::XFER + 16 * in_run>(kb[slot], k_addr[run]);
+                }
+            };
+            auto step = [&](auto stc) __attribute__((always_inline)) {
+                constexpr int st = decltype(stc)::value, slot = (st - FIRST) % NS;
+                if constexpr (st + PF < LAST) issue(IC<st + PF>{});
+                // LDS reads younger than this step's fragment: those of the next PF steps that exist
+                constexpr int hi = st + PF < LAST ? st + PF : LAST - 1;
+                constexpr int n_tr = (hi < NPV ? hi : NPV - 1) - (st < NPV ? st : NPV - 1);
+                constexpr int younger = 2 * n_tr + ((hi - st) - n_tr);
+                if constexpr (st < NPV) {
+                    lds_wait<younger>(ta[slot], tb[slot]);
+                    oacc[st % NDB] = mfma32(join_halves(ta[slot], tb[slot]), pf[st / NDB], oacc[st % NDB]);
+                    if constexpr (FINE) oacc[st % NDB] = mfma32(join_halves(ta[slot], tb[slot]), rest[st / NDB], oacc[st % NDB]);
+                } else {
+                    constexpr int b = (st - NPV) & 1, ks = (st - NPV) >> 1;
+                    lds_wait<younger>(kb[slot]);
+                    const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    s[b] = mfma32(kb[slot], qf[ks], ks == 0 ? zero : s[b]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            __builtin_amdgcn_sched_barrier(0);
+            for_range<FIRST, (FIRST + PF < LAST ? FIRST + PF : LAST)>(issue);
+            for_range<FIRST, LAST>(step);
+        };
+
+        // Vector phase: softmax numerators of the block whose scores sit in s[], rounded to bf16 operand slots.  Two running sums: of the exact values (for the LSE) and of the rounded ones (they
+        // normalise O).  MASKED: some row of the group does not see all of the block, or none has a reference yet.  exact: the reference is the running maximum, raised where a
+        // block exceeds it by more than 2^8; otherwise it stays what it is.
+        auto v_phase = [&](int key0, auto masked_c, const bool exact) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(masked_c)::value;
+            if constexpr (MASKED) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t seen = win_bits(my_keys, key0 + 32 * b) >> (4 * hh);
+                    auto one = [&](auto ic) __attribute__((always_inline)) { constexpr int i = decltype(ic)::value; s[b][i] = win_or<8 * (i >> 2) + (i & 3)>(seen, s[b][i], -INFINITY); };
+                    for_range<0, 16>(one);
+                }
+            }
+            if (exact) {
+                float mx = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+                for (int r = 3; r < 15; r += 2) mx = max3(mx, s[0][r], s[0][r + 1]);
+                mx = max3(mx, s[0][15], s[1][0]);
+#pragma unroll
+                for (int r = 1; r < 15; r += 2) mx = max3(mx, s[1][r], s[1][r + 1]);
+                mx = max_across_halves(max2(mx, s[1][15]));
+                if (__any(mx > thr_raw)) {        // mx is the raw score; thr_raw = (m_run + slack) / c
+                    const float m_new = fmaxf(m_run, mx * c_log2), alpha = fast_exp2(m_run - m_new);
+                    l_run *= alpha;
+                    lr_run *= alpha;
+#pragma unroll
+                    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+                    m_run = m_new;
+                    thr_raw = (m_run + RESCALE_SLACK) * inv_c_log2;
+                }
+            }
+            float ps[4] = {0.f, 0.f, 0.f, 0.f}, psr[4] = {0.f, 0.f, 0.f, 0.f};
+            const float neg_m = -m_run;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int b = u >> 1, x = (u & 1) * 8;
+                float p[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { p[e] = fast_exp2(fmaf(s[b][x + e], c_log2, neg_m)); ps[e & 3] += p[e]; }
+                pf[u] = pack_bf16x8_sum4(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], psr);
+                if constexpr (FINE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) p[e] -= (float)pf[u][e];
+                    rest[u] = pack_bf16x8_sum4(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], psr);
+                }
+            }
+            l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+            lr_run += (psr[0] + psr[1]) + (psr[2] + psr[3]);
+            // (nothing of the vector phase may drift into the matrix phase)
+            asm volatile("" : "+v"(l_run), "+v"(lr_run), "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]));
+            if constexpr (FINE) asm volatile("" : "+v"(rest[0]), "+v"(rest[1]), "+v"(rest[2]), "+v"(rest[3]));
+        };
+
+        // One pass over the blocks: M(0) V(0) M(1) V(1) ... M(NT), the barriers as in the ring step's kernel.
+        auto run = [&](auto exact_c) __attribute__((always_inline)) {
+            constexpr bool exact = decltype(exact_c)::value;
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+            m_run = NEG_BIG; l_run = 0.f; lr_run = 0.f;
+            thr_raw = NEG_BIG;   // any finite score exceeds it: the first one that is seen always sets the maximum
+            if (NT == 0) return;
+            list(0);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // from here on transfers alone are counted
+            {
+                const int n_pre = grp ? K_AHEAD : V_AHEAD;
+                for (int j = 0; j < n_pre && j < NT; ++j) fetch_tile(j);
+            }
+            if (grp == 1) {   // K(0) complete before anyone's M(0)
+                wait_tiles_in_flight_n<C::PER_WAVE>((NT < K_AHEAD ? NT : K_AHEAD) - 1);
+                wg_barrier();
+            }
+            // before M(t): group 0 has requested V up to min(t + 1, NT - 1) and needs V(t - 1) complete
+            auto enter_m = [&](int i) __attribute__((always_inline)) {
+                if (grp == 0) wait_tiles_in_flight_n<C::PER_WAVE>(NT - i < 2 ? NT - i : 2);
+                if (grp == 0 || !PAIR_BARRIER) wg_barrier();
+            };
+            // before V(t): group 1 has requested K up to min(t + 3, NT - 1) and needs K(t + 1) complete
+            auto vector_part = [&](int i) __attribute__((always_inline)) {
+                if (grp == 1 && i + 1 < NT) wait_tiles_in_flight_n<C::PER_WAVE>(NT - 2 - i < 2 ? NT - 2 - i : 2);
+                if (grp == 1 || !PAIR_BARRIER) wg_barrier();
+                const int j = i + (grp ? K_AHEAD : V_AHEAD);
+                if (j < NT) fetch_tile(j);
+                const int b = block_of(i);
+                if (i == first_full || !span_g.full(b)) v_phase(b * TN, std::true_type{}, true);
+                else v_phase(b * TN, std::false_type{}, exact);
+            };
+            enter_m(0);
+            m_phase(IC<0>{}, IC<NPV>{}, IC<NST>{});
+            vector_part(0);
+            // blocks 1 .. NT - 1: four at a time in a straight line, so that the buffer is a compile-time constant and no accumulator passes through a merge of control flow
+            int i = 1;
+            for (; i + 3 < NT; i += 4) {
+                enter_m(i);     m_phase(IC<1>{}, IC<0>{}, IC<NST>{}); vector_part(i);
+                enter_m(i + 1); m_phase(IC<2>{}, IC<0>{}, IC<NST>{}); vector_part(i + 1);
+                enter_m(i + 2); m_phase(IC<3>{}, IC<0>{}, IC<NST>{}); vector_part(i + 2);
+                enter_m(i + 3); m_phase(IC<0>{}, IC<0>{}, IC<NST>{}); vector_part(i + 3);
+            }
+            for (; i < NT; ++i) {
+                enter_m(i);
+                switch (i & 3) {
+                    case 0: m_phase(IC<0>{}, IC<0>{}, IC<NST>{}); break;
+                    case 1: m_phase(IC<1>{}, IC<0>{}, IC<NST>{}); break;
+                    case 2: m_phase(IC<2>{}, IC<0>{}, IC<NST>{}); break;
+                    default: m_phase(IC<3>{}, IC<0>{}, IC<NST>{}); break;
+                }
+                vector_part(i);
+            }
+            enter_m(NT);
+            switch (NT & 3) {
+                case 0: m_phase(IC<0>{}, IC<0>{}, IC<NPV>{}); break;
+                case 1: m_phase(IC<1>{}, IC<0>{}, IC<NPV>{}); break;
+                case 2: m_phase(IC<2>{}, IC<0>{}, IC<NPV>{}); break;
+                default: m_phase(IC<3>{}, IC<0>{}, IC<NPV>{}); break;
+            }
+            if (!PAIR_BARRIER && grp == 0) wg_barrier();
+        };
+
+        run(std::false_type{});
+        float l_tot = sum_across_halves(l_run), lr_tot = sum_across_halves(lr_run);
+        {
+            // a row that sees a key of these blocks has a sum (its reference's block adds 1): has that stayed in the range where nothing over- or underflows?
+            const int off = real && l_tot != 0.f && !(l_tot >= SUM_LO && l_tot <= SUM_HI);
+            if (__syncthreads_or(off)) {          // otherwise once more with the running maximum
+                run(std::true_type{});
+                l_tot = sum_across_halves(l_run);
+                lr_tot = sum_across_halves(lr_run);
+            }
+        }
+        float z = 0.f;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z = fmaf(oacc[db][r], 0.f, z);
+        // (a key that a row does not see has P = 0, and 0 x inf is NaN: what is not finite is done again element by element, and so is what has keys on pages that the cache does not have)
+        if (__syncthreads_or((z != 0.f && real) || bad)) {
+            plain_tile<uint16_t, D>(t);
+            continue;
+        }
+
+        // Rows of O go through LDS (a region of every wavefront's own) so that global accesses are row-contiguous.
+        const float inv = l_tot > 0.f && lr_tot > 0.f ? 1.0f / lr_tot : 0.f, lse = l_tot > 0.f ? (m_run + __log2f(l_tot)) * LN2 : -INFINITY;
+        float* stage = sm.stage[wave];
+        const PagedArgs& a = paged_args();
+        const PagedGeom& g = a.g;
+        int* stage_at = reinterpret_cast<int*>(stage + 32 * C::PITCH);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<float4*>(&stage[l32 * C::PITCH + 32 * db + 8 * b + 4 * hh]) =
+                    make_float4(oacc[db][4 * b] * inv, oacc[db][4 * b + 1] * inv, oacc[db][4 * b + 2] * inv, oacc[db][4 * b + 3] * inv);
+        if (hh == 0) {
+            stage_at[l32] = real ? t.piece >= 0 ? my_vector : (int)paged_out(a, t, my_row, my_head) : -1;
+            if (real && t.piece >= 0) a.part_lse[t.piece * WG + my_vector] = lse;
+            else if (real && a.lse) a.lse[(long long)my_head * g.n_rows + t.q.row0 + my_row] = lse;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        constexpr int LANES = D / 4, ROWS = 64 / LANES;
+        const int sub_row = lane / LANES, col = 4 * (lane % LANES);
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS; ++i) {
+            const int r = ROWS * i + sub_row, at = stage_at[r];
+            const float4 x = *reinterpret_cast<const float4*>(&stage[r * C::PITCH + col]);
+            if (at < 0) continue;
+            if (t.piece >= 0) win_plain::store4(a.part_o, (t.piece * WG + at) * D + col, false, x.x, x.y, x.z, x.w);
+            else win_plain::store4(a.o, (long long)at * D + col, a.out_bf16, x.x, x.y, x.z, x.w);
+        }
+        __syncthreads();                          // the next tile's transfers write where these rows were staged
+    }
+    if (tid == 0) paged_args().tiles[walk.me] = open;
+}
+
+}  // namespace
+
+hipError_t hexi_launch_paged_large(const PagedArgs& a, int d, hipStream_t s)
+{
+    if (d == 128) {
+        if (a.out_bf16) paged_large_kernel<128, false><<<a.n_ranges, 512, 0, s>>>(a); else paged_large_kernel<128, true><<<a.n_ranges, 512, 0, s>>>(a);
+    } else if (a.out_bf16) paged_large_kernel<64, false><<<a.n_ranges, 512, 0, s>>>(a);
+    else paged_large_kernel<64, true><<<a.n_ranges, 512, 0, s>>>(a);
+    return hipGetLastError();
+}

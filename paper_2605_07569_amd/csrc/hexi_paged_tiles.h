@@ -1,0 +1,216 @@
+// Tiles of paged attention: how a workgroup walks its range of them, and a tile element by element (hexi_paged.h has the layout of the work).
+#pragma once
+#include "hexi_paged.h"
+#include "hexi_window_plain.h"
+
+namespace {
+
+constexpr int PAGED_KEYS = 64;      // of a block
+
+__device__ __forceinline__ int paged_uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long paged_uniform(long long x)
+{
+    return (long long)(((unsigned long long)(unsigned)paged_uniform((int)(x >> 32)) << 32) | (unsigned)paged_uniform((int)x));
+}
+
+__device__ __forceinline__ PagedRequest paged_uniform(const PagedRequest& q)
+{
+    return PagedRequest{paged_uniform(q.row0), paged_uniform(q.rows), paged_uniform(q.kv), paged_uniform(q.sinks), paged_uniform(q.at)};
+}
+__device__ __forceinline__ WinKeys paged_uniform(const WinKeys& w) { return WinKeys{paged_uniform(w.sink), paged_uniform(w.lo), paged_uniform(w.hi)}; }
+
+// The launch's arguments, read again here: what is worked out from them once a tile does not keep scalar registers through its loop.  (They are the kernel's first ones.)
+__device__ __forceinline__ const PagedArgs& paged_args()
+{
+    typedef const __attribute__((address_space(4))) PagedArgs* Ptr;
+    Ptr p = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const PagedArgs*)p;
+}
+
+struct Tile {
+    PagedRequest q;
+    WinSpan<PAGED_KEYS> span;           // blocks that its rows see
+    int r, run, count, v0, vectors;     // count: heads of the run; vectors: how many it has, none where 0
+    int b0, b1;                         // blocks of the span that are this range's
+    int last;                           // no row sees a key behind this one; -1: none is seen, and there are no blocks
+    long long piece;                    // of the partial results; -1: the tile is this range's alone
+    __device__ __forceinline__ int row_of(int v) const { return (int)((unsigned)(v0 + v) / (unsigned)count); }
+    __device__ __forceinline__ int head_of(const PagedGeom& g, int v, int row) const
+    {
+        const int i = v0 + v - row * count;
+        return g.regular ? run * count + i : g.head[g.first[run] + i];
+    }
+    __device__ __forceinline__ int kv_head(const PagedGeom& g) const { return g.regular ? run : g.kvh[run]; }
+};
+
+// The ranges of a launch, by a workgroup of NT threads: the sums over the requests, a few to a thread, give every workgroup its own.
+template <int NT> struct PagedWalk {
+    struct Shared { long long of_wave[NT / 64], first; PagedRequest q; int r; };
+    long long at, end, first, range;    // costs; first: in front of request r
+    int r, me;
+    PagedRequest q;
+    bool any;
+    __device__ __forceinline__ PagedWalk(const PagedArgs& a, Shared& sh)
+    {
+        const PagedGeom& g = a.g;
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int each = (g.n_requests + NT - 1) / NT, r0 = tid * each < g.n_requests ? tid * each : g.n_requests, r1 = r0 + each < g.n_requests ? r0 + each : g.n_requests;
+        auto cost_of = [&](const PagedRequest& x) {
+            const int tiles = paged_tiles(g, a.share, x);
+            return tiles == 0 ? 0LL : PagedCost(g, x, a.share.shift, a.share.start, tiles).before(tiles) * g.n_runs;
+        };
+        PagedRequest x = {0, 0, 0, 0, 0};
+        long long mine = 0;
+        for (int i = r0; i < r1; ++i) {
+            x = paged_request(g, i);
+            mine += cost_of(x);
+        }
+        long long before = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const long long y = __shfl_up(before, off, 64);
+            if (lane >= off) before += y;
+        }
+        if (lane == 63) sh.of_wave[wave] = before;
+        __syncthreads();
+        before -= mine;
+        long long total = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) {
+            if (w < wave) before += sh.of_wave[w];
+            total += sh.of_wave[w];
+        }
+        range = (total + a.n_ranges - 1) / a.n_ranges;
+        range = paged_uniform(range < a.share.min_cost ? (long long)a.share.min_cost : range);
+        const int active = paged_uniform((int)((total + range - 1) / range)), per_xcd = (active + 7) / 8, slot = (int)blockIdx.x >> 3;
+        if (blockIdx.x == 0 && tid == 0) *a.n_active = active;
+        me = ((int)blockIdx.x & 7) * per_xcd + slot;
+        any = slot < per_xcd && me < active;
+        if (!any) return;
+        at = me * range;
+        end = paged_uniform(at + range < total ? at + range : total);
+        if (at >= before && at < before + mine) {
+            long long front = before;
+            int i = r0;
+            if (r1 - r0 > 1)
+                for (;; ++i) {
+                    x = paged_request(g, i);
+                    const long long n = cost_of(x);
+                    if (at < front + n) break;
+                    front += n;
+                }
+            sh.first = front; sh.r = i; sh.q = x;
+        }
+        __syncthreads();
+        first = paged_uniform(sh.first);
+        r = paged_uniform(sh.r);
+        q = paged_uniform(sh.q);
+    }
+    // The next tile of the range that has vectors, and the part of it that is the range's; open: the tile that the range starts and does not end.
+    __device__ __forceinline__ bool next(Tile& t, PagedTile& open)
+    {
+        const PagedArgs& a = paged_args();
+        const PagedGeom& g = a.g;
+        while (at < end) {
+            const int tiles = paged_uniform(paged_tiles(g, a.share, q));
+            if (tiles > 0) {
+                const PagedCost cost(g, q, a.share.shift, a.share.start, tiles);
+                const long long of_run = paged_uniform(cost.before(tiles)), in = at - first;
+                if (in < of_run * g.n_runs) {
+                    int run = g.n_runs == 1 ? 0 : (int)((double)in / (double)of_run);
+                    if (run * of_run > in) --run;
+                    if ((run + 1) * of_run <= in) ++run;
+                    run = paged_uniform(run);
+                    const int tile = paged_uniform(cost.tile_of(in - run * of_run, tiles));
+                    const long long c0 = paged_uniform(cost.before(tile)), size = paged_uniform(cost.before(tile + 1)) - c0, tile_at = first + run * of_run + c0;
+                    const long long x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
+                    at = tile_at + x1;
+                    t.q = q;
+                    t.r = r;
+                    t.run = run;
+                    t.count = g.regular ? g.most : g.first[run + 1] - g.first[run];
+                    t.v0 = tile << a.share.shift;
+                    const int left = q.rows * t.count - t.v0;
+                    t.vectors = paged_uniform(left < 1 << a.share.shift ? left : 1 << a.share.shift);
+                    if (t.vectors <= 0) continue;
+                    const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(t.vectors - 1)));
+                    t.span = WinSpan<PAGED_KEYS>(k0, k1, q.kv);
+                    t.last = k1.hi - 1;
+                    const int blocks = paged_uniform(t.span.n_blocks);
+                    auto block_at = [&](long long x) { return x == size ? blocks : (int)((double)(x * blocks) / (double)size); };      // (exact: below 2^48)
+                    t.b0 = paged_uniform(block_at(x0));
+                    t.b1 = paged_uniform(block_at(x1));
+                    const bool starts = x0 == 0, ends = x1 == size;
+                    t.piece = starts && ends ? -1 : 2 * (long long)me + (starts ? 1 : 0);
+                    if (starts && !ends) open = PagedTile{(int)((tile_at + size - 1) / range) - me + 1, t.run, q.row0, q.rows, t.v0, {0, 0, 0}};
+                    return true;
+                }
+                first += of_run * g.n_runs;
+            }
+            q = paged_uniform(paged_request(g, ++r));
+        }
+        return false;
+    }
+};
+
+// Where the lane's vector of a tile goes.
+__device__ __forceinline__ long long paged_out(const PagedArgs& a, const Tile& t, int row, int h) { return (long long)(t.q.row0 + row) * a.g.nq + h; }
+
+// A tile's vectors, eight lanes each, walk the keys of the range's blocks that they see, one by one: what a vector does not see is not read into it.
+template <class T, int D> __device__ __forceinline__ void plain_tile(const Tile& t)
+{
+    constexpr int N = D / win_plain::LANES;
+    const PagedArgs& a = paged_args();
+    const PagedGeom& g = a.g;
+    const int col = (int)threadIdx.x % win_plain::LANES * N;
+    const int* table = g.table + (long long)t.r * g.columns;
+    const long long head = (long long)t.kv_head(g) * g.stride_head + col;
+    for (int i = (int)threadIdx.x / win_plain::LANES; i < t.vectors; i += (int)blockDim.x / win_plain::LANES) {
+        const int row = t.row_of(i), h = t.head_of(g, i, row);
+        const WinKeys w = paged_keys_of_row(g, t.q, row);
+        float q[N], acc[N];
+        win_plain::load_cols(static_cast<const T*>(a.q) + (long long)(t.q.row0 + row) * g.q_stride_tok + (long long)h * g.q_stride_head + col, q);
+#pragma unroll
+        for (int c = 0; c < N; ++c) acc[c] = 0.f;
+        float m = -INFINITY, l = 0.f;
+        for (int b = t.b0; b < t.b1; ++b) {
+            const int k0 = PAGED_KEYS * t.span.block(b);
+            for (int j = k0; j < k0 + PAGED_KEYS && j < w.hi; ++j) {
+                if (j >= w.sink && j < w.lo) continue;
+                const PagedPlace p = paged_place(g, table, j);
+                if (p.id < 0) continue;
+                const long long at = (long long)p.id * g.stride_page + (long long)p.row * g.stride_tok + head;
+                float x[N];
+                win_plain::load_cols(static_cast<const T*>(a.k) + at, x);
+                const float s = win_plain::dot(q, x) * g.scale;
+                win_plain::load_cols(static_cast<const T*>(a.v) + at, x);
+                if (s > m) {
+                    const float alpha = expf(m - s);   // (m = -inf: 0)
+                    m = s;
+                    l *= alpha;
+#pragma unroll
+                    for (int c = 0; c < N; ++c) acc[c] *= alpha;
+                }
+                const float p_j = s == -INFINITY ? 0.f : expf(s - m);
+                l += p_j;
+#pragma unroll
+                for (int c = 0; c < N; ++c) acc[c] = fmaf(p_j, x[c], acc[c]);
+            }
+        }
+        const float lse = l == 0.f ? -INFINITY : m + logf(l), r = l == 0.f ? 0.f : 1.0f / l;
+        if (t.piece >= 0) {
+            const long long at = (t.piece << a.share.shift) + i;
+            if (col == 0) a.part_lse[at] = lse;
+#pragma unroll
+            for (int c = 0; c < N; c += 4) win_plain::store4(a.part_o, at * D + col + c, false, r * acc[c], r * acc[c + 1], r * acc[c + 2], r * acc[c + 3]);
+        } else {
+            if (col == 0 && a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
+            const long long at = paged_out(a, t, row, h) * D + col;
+#pragma unroll
+            for (int c = 0; c < N; c += 4) win_plain::store4(a.o, at + c, a.out_bf16, r * acc[c], r * acc[c + 1], r * acc[c + 2], r * acc[c + 3]);
+        }
+    }
+}
+
+}  // namespace

@@ -118,7 +118,7 @@ def test_plan_refusals():
                                    p["slot"], None)
 
     _codes(call, [(S, dict(page=0)), (S, dict(page=-16)), (S, dict(page=20)), (S, dict(page=1040)), (E, dict(n_pages=0)), (S, dict(n_pages=2 ** 27)), (E, dict(n=0)), (E, dict(n=8193)),
-                  (E, dict(columns=0)), (S, dict(columns=2 ** 26 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 30 + 1))] + [(E, {k: None}) for k in names] + [(A, {k: 18}) for k in names])
+                  (E, dict(columns=0)), (S, dict(columns=2 ** 24 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 28 + 1))] + [(E, {k: None}) for k in names] + [(A, {k: 18}) for k in names])
 
 
 def test_write_refusals():
@@ -153,7 +153,7 @@ def test_attention_refusals():
     _codes(call, [(c, k) for c, k in BAD_CACHES if "d" not in k and k.get("heads") != 129 and "dtype" not in k] +
            [(E, dict(no_desc=True)), (E, dict(no_cache=True)), (S, dict(d=96)), (S, dict(dtype=2)), (E, dict(nq=129)), (E, dict(nq=7)), (E, dict(scale=float("inf"))), (E, dict(scale=0.0)),
             (E, dict(kv_of_q=[0] * 7 + [2])), (E, dict(desc=dict(dtype=1))), (E, dict(desc=dict(d=64), qs=(1024, 128))), (E, dict(desc=dict(nkv=4))), (E, dict(n=0)), (E, dict(n=8193)), (E, dict(columns=0)),
-            (S, dict(columns=2 ** 26 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 28)), (E, dict(max_rows=-1)), (E, dict(window=(0, 0))), (E, dict(window=(1, -1))), (E, dict(qs=(64, 128))),
+            (S, dict(columns=2 ** 24 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 28)), (E, dict(max_rows=-1)), (E, dict(window=(0, 0))), (E, dict(window=(1, -1))), (E, dict(qs=(64, 128))),
             (E, dict(qs=(1024, 64))), (S, dict(qs=(2 ** 22 + 8, 128))), (A, dict(qs=(1028, 128))), (A, dict(qs=(1024, 132))), (S, dict(o_dtype=2))] +
            [(E, {p: None}) for p in ("table", "row_start", "kv_len", "q", "k", "v", "o")] + [(A, {p: 24}) for p in ("q", "k", "v", "o", "space")] +
            [(A, {p: 18}) for p in ("lse", "table", "row_start", "kv_len", "q_start", "kv_start")] + [(W, dict(space=None)), (W, dict(short=1))])
