@@ -650,7 +650,7 @@ static int paged_attn_shape(const hexi_attn_desc* desc, const hexi_paged_cache* 
     if ((rc = build_kv_of_q(desc, kv_of_q)) != HEXI_OK) return rc;
     hexi_paged_runs(kv_of_q, desc->n_q_heads, desc->n_kv_heads, g);
     g->columns = columns; g->n_requests = n_requests; g->n_rows = (int)n_rows; g->max_rows = (int)max_rows;
-    *shape = hexi_paged_shape(desc->dtype, g->n_runs, g->most, n_requests, n_rows, max_rows, (int64_t)columns * cache->page);
+    *shape = hexi_paged_shape(desc->dtype, desc->head_dim, g->n_runs, g->most, n_requests, n_rows, max_rows, (int64_t)columns * cache->page);
     return HEXI_OK;
 }
 

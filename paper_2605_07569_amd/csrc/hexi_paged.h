@@ -187,22 +187,25 @@ struct PagedArgs {
     float *part_o, *part_lse;
 };
 
+// Blocks of a wavefront's ring in the kernel for few vectors, 16 rows of K and V each: two, or four where rows are short, so that two workgroups fit a CU (one of fp32 with 128 columns).
+constexpr int paged_ring(size_t bytes, int d) { return (int)bytes * d <= 128 ? 4 : 2; }
+
 // How a call is launched: by the kernel for few vectors to a key, by the one for many, or by both, each with the requests that it is for.
 struct PagedShape {
     PagedShare share[2];
     int ranges[2];            // workgroups, multiples of 8; 0: the kernel is not launched
     bool splits;              // a tile can be cut: a further launch joins
 };
-inline PagedShape hexi_paged_shape(int dtype, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
+inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
 {
     PagedShape s;
     const bool large = dtype == HEXI_BF16 && max_rows * most > 32;
     const bool few = !large || n_requests > 1;
-    s.share[0] = PagedShare{max_rows * most > 16 ? 5 : 4, 32, 1, !large, 1, 2};
-    s.share[1] = PagedShare{8, 32, !few, 1, 4, 12};
+    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 1, 2};
+    s.share[1] = PagedShare{8, 16, !few, 1, 4, 12};
     const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
     for (int i = 0; i < 2; ++i) {
-        const long long tiles = n_runs * ((n_rows * most >> s.share[i].shift) + most_requests), full = i == 0 ? 512 : 256;
+        const long long tiles = n_runs * ((n_rows * most >> s.share[i].shift) + most_requests), full = i == 1 || (dtype == HEXI_F32 && d == 128) ? 256 : 512;
         long long n = tiles > full ? full : tiles * (blocks + s.share[i].start) / s.share[i].min_cost + 1;
         n = n > full ? full : n;
         s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;

@@ -44,27 +44,40 @@ struct Tile {
     __device__ __forceinline__ int kv_head(const PagedGeom& g) const { return g.regular ? run : g.kvh[run]; }
 };
 
+// floor(x / y) of numbers below 2^52: exact.
+__device__ __forceinline__ long long paged_ratio(long long x, long long y)
+{
+    long long q = (long long)((double)x / (double)y);
+    q -= q * y > x;
+    return q + ((q + 1) * y <= x);
+}
+
 // The ranges of a launch, by a workgroup of NT threads: the sums over the requests, a few to a thread, give every workgroup its own.
 template <int NT> struct PagedWalk {
-    struct Shared { long long of_wave[NT / 64], first; PagedRequest q; int r; };
+    struct Shared { long long of_wave[NT / 64], first, of_run; PagedRequest q; int r, tiles; };
     long long at, end, first, range;    // costs; first: in front of request r
-    int r, me;
+    long long of_run;                   // of a run of it
+    int r, me, tiles;                   // tiles of a run of it
     PagedRequest q;
     bool any;
+    static __device__ __forceinline__ long long cost_of(const PagedArgs& a, const PagedRequest& x, int tiles)
+    {
+        return tiles == 0 ? 0LL : PagedCost(a.g, x, a.share.shift, a.share.start, tiles).before(tiles);
+    }
     __device__ __forceinline__ PagedWalk(const PagedArgs& a, Shared& sh)
     {
         const PagedGeom& g = a.g;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (g.n_requests + NT - 1) / NT, r0 = tid * each < g.n_requests ? tid * each : g.n_requests, r1 = r0 + each < g.n_requests ? r0 + each : g.n_requests;
-        auto cost_of = [&](const PagedRequest& x) {
-            const int tiles = paged_tiles(g, a.share, x);
-            return tiles == 0 ? 0LL : PagedCost(g, x, a.share.shift, a.share.start, tiles).before(tiles) * g.n_runs;
-        };
         PagedRequest x = {0, 0, 0, 0, 0};
-        long long mine = 0;
+        long long mine = 0, run = 0;
+        int n = 0;
+#pragma unroll 1
         for (int i = r0; i < r1; ++i) {
             x = paged_request(g, i);
-            mine += cost_of(x);
+            n = paged_tiles(g, a.share, x);
+            run = cost_of(a, x, n);
+            mine += run * g.n_runs;
         }
         long long before = mine;
 #pragma unroll
@@ -81,30 +94,34 @@ template <int NT> struct PagedWalk {
             if (w < wave) before += sh.of_wave[w];
             total += sh.of_wave[w];
         }
-        range = (total + a.n_ranges - 1) / a.n_ranges;
+        total = paged_uniform(total);
+        range = paged_ratio(total + a.n_ranges - 1, a.n_ranges);
         range = paged_uniform(range < a.share.min_cost ? (long long)a.share.min_cost : range);
-        const int active = paged_uniform((int)((total + range - 1) / range)), per_xcd = (active + 7) / 8, slot = (int)blockIdx.x >> 3;
+        const int active = paged_uniform((int)paged_ratio(total + range - 1, range)), per_xcd = (active + 7) / 8, slot = (int)blockIdx.x >> 3;
         if (blockIdx.x == 0 && tid == 0) *a.n_active = active;
         me = ((int)blockIdx.x & 7) * per_xcd + slot;
         any = slot < per_xcd && me < active;
         if (!any) return;
         at = me * range;
-        end = paged_uniform(at + range < total ? at + range : total);
+        end = at + range < total ? at + range : total;
         if (at >= before && at < before + mine) {
-            long long front = before;
             int i = r0;
-            if (r1 - r0 > 1)
+            if (each > 1)
+#pragma unroll 1
                 for (;; ++i) {
                     x = paged_request(g, i);
-                    const long long n = cost_of(x);
-                    if (at < front + n) break;
-                    front += n;
+                    n = paged_tiles(g, a.share, x);
+                    run = cost_of(a, x, n);
+                    if (at < before + run * g.n_runs) break;
+                    before += run * g.n_runs;
                 }
-            sh.first = front; sh.r = i; sh.q = x;
+            sh.first = before; sh.of_run = run; sh.r = i; sh.tiles = n; sh.q = x;
         }
         __syncthreads();
         first = paged_uniform(sh.first);
+        of_run = paged_uniform(sh.of_run);
         r = paged_uniform(sh.r);
+        tiles = paged_uniform(sh.tiles);
         q = paged_uniform(sh.q);
     }
     // The next tile of the range that has vectors, and the part of it that is the range's; open: the tile that the range starts and does not end.
@@ -113,42 +130,44 @@ template <int NT> struct PagedWalk {
         const PagedArgs& a = paged_args();
         const PagedGeom& g = a.g;
         while (at < end) {
-            const int tiles = paged_uniform(paged_tiles(g, a.share, q));
-            if (tiles > 0) {
-                const PagedCost cost(g, q, a.share.shift, a.share.start, tiles);
-                const long long of_run = paged_uniform(cost.before(tiles)), in = at - first;
-                if (in < of_run * g.n_runs) {
-                    int run = g.n_runs == 1 ? 0 : (int)((double)in / (double)of_run);
-                    if (run * of_run > in) --run;
-                    if ((run + 1) * of_run <= in) ++run;
-                    run = paged_uniform(run);
-                    const int tile = paged_uniform(cost.tile_of(in - run * of_run, tiles));
-                    const long long c0 = paged_uniform(cost.before(tile)), size = paged_uniform(cost.before(tile + 1)) - c0, tile_at = first + run * of_run + c0;
-                    const long long x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
-                    at = tile_at + x1;
-                    t.q = q;
-                    t.r = r;
-                    t.run = run;
-                    t.count = g.regular ? g.most : g.first[run + 1] - g.first[run];
-                    t.v0 = tile << a.share.shift;
-                    const int left = q.rows * t.count - t.v0;
-                    t.vectors = paged_uniform(left < 1 << a.share.shift ? left : 1 << a.share.shift);
-                    if (t.vectors <= 0) continue;
-                    const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(t.vectors - 1)));
-                    t.span = WinSpan<PAGED_KEYS>(k0, k1, q.kv);
-                    t.last = k1.hi - 1;
-                    const int blocks = paged_uniform(t.span.n_blocks);
-                    auto block_at = [&](long long x) { return x == size ? blocks : (int)((double)(x * blocks) / (double)size); };      // (exact: below 2^48)
-                    t.b0 = paged_uniform(block_at(x0));
-                    t.b1 = paged_uniform(block_at(x1));
-                    const bool starts = x0 == 0, ends = x1 == size;
-                    t.piece = starts && ends ? -1 : 2 * (long long)me + (starts ? 1 : 0);
-                    if (starts && !ends) open = PagedTile{(int)((tile_at + size - 1) / range) - me + 1, t.run, q.row0, q.rows, t.v0, {0, 0, 0}};
-                    return true;
-                }
+            const long long in = at - first;
+            if (in >= of_run * g.n_runs) {
                 first += of_run * g.n_runs;
+                q = paged_uniform(paged_request(g, ++r));
+                tiles = paged_uniform(paged_tiles(g, a.share, q));
+                of_run = paged_uniform(cost_of(a, q, tiles));
+                continue;
             }
-            q = paged_uniform(paged_request(g, ++r));
+            const int run = g.n_runs == 1 ? 0 : paged_uniform((int)paged_ratio(in, of_run));
+            int tile = 0;
+            long long c0 = 0, size = of_run;
+            if (tiles > 1) {
+                const PagedCost cost(g, q, a.share.shift, a.share.start, tiles);
+                tile = paged_uniform(cost.tile_of(in - run * of_run, tiles));
+                c0 = paged_uniform(cost.before(tile));
+                size = paged_uniform(cost.before(tile + 1)) - c0;
+            }
+            const long long tile_at = first + run * of_run + c0, x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
+            at = tile_at + x1;
+            t.q = q;
+            t.r = r;
+            t.run = run;
+            t.count = g.regular ? g.most : g.first[run + 1] - g.first[run];
+            t.v0 = tile << a.share.shift;
+            const int left = q.rows * t.count - t.v0;
+            t.vectors = left < 1 << a.share.shift ? left : 1 << a.share.shift;
+            if (t.vectors <= 0) continue;
+            const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(t.vectors - 1)));
+            t.span = WinSpan<PAGED_KEYS>(k0, k1, q.kv);
+            t.last = k1.hi - 1;
+            const int blocks = t.span.n_blocks;
+            const bool starts = x0 == 0, ends = x1 == size;
+            auto block_at = [&](long long x) { return paged_uniform((int)((double)(x * blocks) / (double)size)); };      // (exact: below 2^48)
+            t.b0 = starts ? 0 : block_at(x0);
+            t.b1 = ends ? blocks : block_at(x1);
+            t.piece = starts && ends ? -1 : 2 * (long long)me + (starts ? 1 : 0);
+            if (starts && !ends) open = PagedTile{(int)paged_uniform((int)paged_ratio(tile_at + size - 1, range)) - me + 1, t.run, q.row0, q.rows, t.v0, {0, 0, 0}};
+            return true;
         }
         return false;
     }

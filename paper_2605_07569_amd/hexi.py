@@ -286,13 +286,14 @@ def _refuse(msg):
 
 
 _DTYPES = {}
-_torch = None
+_torch = _int32 = None
 
 
 def _types():
     """torch, and its element types by the library's codes and the other way round, at the first use."""
-    global _torch
+    global _torch, _int32
     import torch
+    _int32 = torch.int32
     _DTYPES.update({torch.bfloat16: HEXI_BF16, torch.float32: HEXI_F32, HEXI_BF16: torch.bfloat16, HEXI_F32: torch.float32})
     _torch = torch
 
@@ -496,51 +497,57 @@ def _q_strides(q):
     return (q.stride(0) if n > 1 else h * d, q.stride(1) if h > 1 else d)
 
 
-def _ints(name, t, shape, dev):
-    if _torch is None:
-        _types()
-    if t.dtype is not _torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
-        _refuse(f"{name}: a contiguous int32 tensor of {tuple(shape)} on the current GPU is needed, not {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
-    return t.data_ptr()
+def _ints(dev, *named):
+    """Addresses of int32 tensors, (name, tensor, elements) each: contiguous ones of so many elements on the current GPU."""
+    out = []
+    for name, t, n in named:
+        if t.dtype is not _int32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+            _refuse(f"{name}: a contiguous int32 tensor of {n} elements on the current GPU is needed, not {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
+        out.append(t.data_ptr())
+    return out
 
 
 def hexi_paged_plan(page, cached, added, table, held, free_list, n_free, row_start, kv_len, pos, slot, stream=None):
     """Pages for the requests' lengths and the places of their new rows; all int32 tensors on the device: cached, added, held, kv_len [requests], table [requests, columns],
     free_list [pages], n_free [1], row_start [requests + 1], pos, slot [rows]."""
-    dev, n, rows = _current_device(), cached.shape, slot.shape
-    if len(n) != 1 or len(table.shape) != 2 or len(rows) != 1 or len(free_list.shape) != 1:
-        _refuse(f"cached {tuple(n)}, table {tuple(table.shape)}, free_list {tuple(free_list.shape)}, slot {tuple(rows)}: one, two, one and one axes are needed")
-    r, columns = n[0], table.shape[1]
-    rc = (_lib or load()).hexi_paged_plan(page, free_list.shape[0], r, _ints("cached", cached, n, dev), _ints("added", added, n, dev), _ints("table", table, (r, columns), dev), columns,
-                                          _ints("held", held, n, dev), _ints("free_list", free_list, free_list.shape, dev), _ints("n_free", n_free, (1,), dev),
-                                          _ints("row_start", row_start, (r + 1,), dev), _ints("kv_len", kv_len, n, dev), rows[0], _ints("pos", pos, rows, dev),
-                                          _ints("slot", slot, rows, dev), _stream(stream))
+    dev, shape = _current_device(), table.shape
+    if len(shape) != 2:
+        _refuse(f"table {tuple(shape)}: two axes are needed")
+    r, columns = shape
+    pages, rows = free_list.numel(), slot.numel()
+    a = _ints(dev, ("cached", cached, r), ("added", added, r), ("table", table, r * columns), ("held", held, r), ("free_list", free_list, pages), ("n_free", n_free, 1),
+              ("row_start", row_start, r + 1), ("kv_len", kv_len, r), ("pos", pos, rows), ("slot", slot, rows))
+    rc = (_lib or load()).hexi_paged_plan(page, pages, r, a[0], a[1], a[2], columns, a[3], a[4], a[5], a[6], a[7], rows, a[8], a[9], _stream(stream))
     if rc:
         _check(rc)
 
 
-def _cache_fits(name, t, c, dev):
-    s = t.stride()
-    if t.shape != (c.n_pages, c.n_kv_heads, c.page, c.head_dim) or _dtype(t) != c.dtype or s[3] != 1 or s[2] != c.stride_tok or (s[1] != c.stride_head and c.n_kv_heads > 1) or (
-            s[0] != c.stride_page and c.n_pages > 1):
-        _refuse(f"{name}: {tuple(t.shape)} {t.dtype} with strides {s}; the descriptor says otherwise")
-    if t.get_device() != dev:
-        _refuse(f"{name} is on {t.device}, not on the current GPU")
-    return t.data_ptr()
+def _caches(c, dev, k, v):
+    """Addresses of the caches of keys and values that a descriptor describes."""
+    heads, n_pages = c.n_kv_heads, c.n_pages
+    shape, strides, dtype = (n_pages, heads, c.page, c.head_dim), (c.stride_page, c.stride_head, c.stride_tok, 1), _DTYPES.get(c.dtype)
+    for name, t in (("k_cache", k), ("v_cache", v)):
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or t.stride() != strides:
+            if t.dtype is not dtype or t.shape != shape or any(n > 1 and x != y for n, x, y in zip(shape, t.stride(), strides)):
+                _refuse(f"{name}: {tuple(t.shape)} {t.dtype} with strides {t.stride()}; the descriptor says {shape} {dtype} with {strides}")
+            if t.get_device() != dev:
+                _refuse(f"{name} is on {t.device}, not on the current GPU")
+    return k.data_ptr(), v.data_ptr()
 
 
 def hexi_paged_write(cache, slot, k, v, k_cache, v_cache, stream=None):
     """Writes k and v [rows, kv heads, head_dim] (one type, one pair of strides) into their slots (int32 [rows]; -1: left out).  cache: that of make_paged_cache."""
-    dev, shape = _current_device(), k.shape
-    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or v.shape != shape or v.dtype is not k.dtype or k.stride(2) != 1 or v.stride(2) != 1:
+    dev, shape, strides = _current_device(), k.shape, k.stride()
+    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or v.shape != shape or v.dtype is not k.dtype or strides[2] != 1 or v.stride(2) != 1:
         _refuse(f"k, v: [rows, {cache.n_kv_heads}, {cache.head_dim}] of one type with contiguous columns are needed, not {tuple(shape)} {k.dtype}, {tuple(v.shape)} {v.dtype}")
-    tok, head = _q_strides(k)
-    if _q_strides(v) != (tok, head):
-        _refuse(f"k and v differ in their strides: {k.stride()}, {v.stride()}")
+    rows = shape[0]
+    tok, head = strides[:2] if rows > 1 and shape[1] > 1 else _q_strides(k)
+    if v.stride() != strides and _q_strides(v) != (tok, head):
+        _refuse(f"k and v differ in their strides: {strides}, {v.stride()}")
     if k.get_device() != dev or v.get_device() != dev:
         _refuse(f"k or v is on {k.device} or {v.device}, not on the current GPU")
-    rc = (_lib or load()).hexi_paged_write(cache, _ints("slot", slot, (shape[0],), dev), shape[0], k.data_ptr(), v.data_ptr(), _dtype(k), tok, head,
-                                           _cache_fits("k_cache", k_cache, cache, dev), _cache_fits("v_cache", v_cache, cache, dev), _stream(stream))
+    kc, vc = _caches(cache, dev, k_cache, v_cache)
+    rc = (_lib or load()).hexi_paged_write(cache, _ints(dev, ("slot", slot, rows))[0], rows, k.data_ptr(), v.data_ptr(), _dtype(k), tok, head, kc, vc, _stream(stream))
     if rc:
         _check(rc)
 
@@ -553,35 +560,37 @@ def hexi_paged_attn(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, 
     """Attention of the requests' new rows, q [rows, q heads, head_dim], over their cached keys.  table [requests, columns], row_start [requests + 1], kv_len, q_start, kv_start
     [requests]: int32 on the device; o's element type (fp32 or bf16) is the result's.  max_rows: no request has more rows (0: not known).  workspace: a tensor of at least
     hexi_paged_attn_workspace_bytes, not shared with a call that may run at the same time; None takes one from torch for the call."""
-    dev = _current_device()
-    if len(table.shape) != 2 or len(kv_len.shape) != 1 or len(q.shape) != 3:
-        _refuse(f"table {tuple(table.shape)}, kv_len {tuple(kv_len.shape)}, q {tuple(q.shape)}: two, one and three axes are needed")
-    (r, columns), shape = table.shape, (q.shape[0], desc.n_q_heads, desc.head_dim)
-    if q.shape != shape or _dtype(q) != desc.dtype or q.stride(2) != 1 or any(
-            n > 1 and x != y for n, x, y in zip(shape, q.stride(), (desc.q_stride_tok, desc.q_stride_head))):
-        _refuse(f"q: [rows, {shape[1]}, {shape[2]}] of type {desc.dtype} with the descriptor's strides is needed, not {tuple(q.shape)} {q.dtype} with strides {q.stride()}")
+    dev, shape, columns = _current_device(), q.shape, table.shape
+    rows, nq, d = desc_shape = (shape[0] if shape else 0, desc.n_q_heads, desc.head_dim)
+    strides = q.stride()
+    if shape != desc_shape or _dtype(q) != desc.dtype or strides != (desc.q_stride_tok, desc.q_stride_head, 1) and any(
+            n > 1 and x != y for n, x, y in zip(shape, strides, (desc.q_stride_tok, desc.q_stride_head, 1))):
+        _refuse(f"q: [rows, {nq}, {d}] of type {desc.dtype} with the descriptor's strides is needed, not {tuple(shape)} {q.dtype} with strides {strides}")
     if q.get_device() != dev:
         _refuse(f"q is on {q.device}, not on the current GPU")
+    if len(columns) != 2:
+        _refuse(f"table {tuple(columns)}: two axes are needed")
+    r, columns = columns
     o_type = _dtype(o)
-    _fits("o", o, shape, o_type, dev)
+    _fits("o", o, desc_shape, o_type, dev)
     if lse is not None:
-        _fits("lse", lse, (shape[1], shape[0]), HEXI_F32, dev)
+        _fits("lse", lse, (nq, rows), HEXI_F32, dev)
+    kc, vc = _caches(cache, dev, k_cache, v_cache)
+    a = _ints(dev, ("table", table, r * columns), ("row_start", row_start, r + 1), ("kv_len", kv_len, r))
+    qs, ks = (None if t is None else _ints(dev, (name, t, r))[0] for name, t in (("q_start", q_start), ("kv_start", kv_start))) if q_start is not None or kv_start is not None else (None, None)
     lib, handle = _lib or load(), _stream(stream)
     taken = None
     if workspace is not None:
         space, ws_bytes = workspace.data_ptr(), _bytes_of(workspace, dev)
     else:
-        ws_bytes = lib.hexi_paged_attn_workspace_bytes(desc, cache, r, columns, shape[0], max_rows)
+        ws_bytes = lib.hexi_paged_attn_workspace_bytes(desc, cache, r, columns, rows, max_rows)
         if stream is None:
             workspace = _torch.empty(ws_bytes, dtype=_torch.uint8, device=q.device)
             space = workspace.data_ptr()
         else:
             space = taken = _take(lib, ws_bytes, dev, handle) if ws_bytes else None
     try:
-        rc = lib.hexi_paged_attn(desc, cache, window, r, _ints("table", table, (r, columns), dev), columns, _ints("row_start", row_start, (r + 1,), dev),
-                                 _ints("kv_len", kv_len, (r,), dev), None if q_start is None else _ints("q_start", q_start, (r,), dev),
-                                 None if kv_start is None else _ints("kv_start", kv_start, (r,), dev), shape[0], max_rows, q.data_ptr(),
-                                 _cache_fits("k_cache", k_cache, cache, dev), _cache_fits("v_cache", v_cache, cache, dev), o.data_ptr(), o_type, _ptr(lse), space, ws_bytes, handle)
+        rc = lib.hexi_paged_attn(desc, cache, window, r, a[0], columns, a[1], a[2], qs, ks, rows, max_rows, q.data_ptr(), kc, vc, o.data_ptr(), o_type, _ptr(lse), space, ws_bytes, handle)
     finally:
         if taken is not None:
             _torch.cuda.caching_allocator_delete(taken)
