@@ -121,18 +121,20 @@ struct PagedWriteArgs {
 // 2 w + 1 is that of a tile which range w starts, 2 w that of one which it goes on with, and tiles[w] tells the joining launch of the tile that range w starts and does not end.
 struct PagedTile { int pieces, run, row0, rows, v0, pad[3]; };      // pieces: 0 where there is no such tile; v0: first vector
 
-// Costs of a request's tiles, in blocks; before(t): of the first t tiles of a run, by the closed form of its sums, so that no table is needed.
-// Of tile t the last row sees keys up to at + (t + 1) vectors / most, and a window leaves out what the first one no longer sees.
+// Costs of a request's tiles, in units of 2^coarse blocks; before(t): of the first t tiles of a run, by the closed form of its sums, so that no table is needed.
+// Of tile t the last row sees keys up to at + (t + 1) vectors / most, and a window leaves out what the first one no longer sees.  The host sees to it that all costs of a launch together stay
+// below 2^31.
+struct PagedShare { int shift, few, takes_few, takes_many, start, min_cost, coarse; };      // 2^shift vectors to a tile; limit of few vectors, and which requests are the kernel's; cost of a tile's start; the least of a range
 struct PagedCost {
     long long up, low, top;           // most x (keys up to the last row's own, of tile 0), most x (keys in front of its first row's window), most x kv
-    double per_block;                 // 1 / (64 most)
+    double per_unit;                  // 1 / (64 most 2^coarse)
     int shift, start;                 // vectors of a tile: 2^shift; of every tile
     int up0, up1, low0, low1;         // tiles in front of those that see a key, and of those that see them all; of those with keys in front of the window, and with all there
-    __host__ __device__ __attribute__((always_inline)) PagedCost(const PagedGeom& g, const PagedRequest& q, int shift_, int start_, int tiles)
+    __host__ __device__ __attribute__((always_inline)) PagedCost(const PagedGeom& g, const PagedShare& s, const PagedRequest& q, int tiles)
     {
-        shift = shift_;
-        per_block = g.per_block;
-        start = start_ + (q.sinks + 63) / 64;
+        shift = s.shift;
+        per_unit = g.per_block / (double)(1 << s.coarse);
+        start = s.start;
         top = (long long)g.most * q.kv;
         up = g.most * q.at + (1 << shift);
         low = g.most * (q.at + 1 - g.window);
@@ -153,9 +155,9 @@ struct PagedCost {
         return n * (a + ((long long)t0 << shift)) + ((n * (n - 1) / 2) << shift) + (t > t1 ? (long long)(t - t1) * top : 0);
     }
     // (rounded to a double, divided and rounded down: it never falls, and is the same wherever it is worked out)
-    __host__ __device__ __attribute__((always_inline)) long long before(int t) const { return (long long)((double)(sum(up, up0, up1, t) - sum(low, low0, low1, t)) * per_block) + (long long)t * start; }
+    __host__ __device__ __attribute__((always_inline)) int before(int t) const { return (int)((double)(sum(up, up0, up1, t) - sum(low, low0, low1, t)) * per_unit) + t * start; }
     // the tile that cost x lies in
-    __host__ __device__ __attribute__((always_inline)) int tile_of(long long x, int tiles) const
+    __host__ __device__ __attribute__((always_inline)) int tile_of(int x, int tiles) const
     {
         int lo = 0, hi = tiles;
         while (hi - lo > 1) {
@@ -166,12 +168,18 @@ struct PagedCost {
     }
 };
 
-// Tiles of one head run of a request that a kernel takes: those with up to `few` vectors are one kernel's, the others another's.
-struct PagedShare { int shift, few, takes_few, takes_many, start, min_cost; };      // 2^shift vectors to a tile; limit; which of them; cost of a tile's start; the least of a range
+// Tiles of one head run of a request that are a kernel's, and the run's cost.
 __host__ __device__ __attribute__((always_inline)) inline int paged_tiles(const PagedGeom& g, const PagedShare& s, const PagedRequest& q)
 {
-    const long long n = (long long)q.rows * g.most;
-    return n == 0 || !(n <= s.few ? s.takes_few : s.takes_many) ? 0 : (int)((n + (1 << s.shift) - 1) >> s.shift);
+    const int n = q.rows * g.most;      // at most 2^28
+    return n == 0 || !(n <= s.few ? s.takes_few : s.takes_many) ? 0 : (n + (1 << s.shift) - 1) >> s.shift;
+}
+__host__ __device__ __attribute__((always_inline)) inline int paged_cost(const PagedGeom& g, const PagedShare& s, const PagedRequest& q, int tiles)
+{
+    if (tiles == 0) return 0;
+    if (tiles > 1) return PagedCost(g, s, q, tiles).before(tiles);
+    const WinKeys w = paged_keys_of_row(g, q, q.rows - 1);
+    return ((w.sink + w.hi - w.lo) >> (6 + s.coarse)) + s.start;
 }
 
 struct PagedArgs {
@@ -201,12 +209,14 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
     PagedShape s;
     const bool large = dtype == HEXI_BF16 && max_rows * most > 32;
     const bool few = !large || n_requests > 1;
-    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 1, 2};
-    s.share[1] = PagedShare{8, 16, !few, 1, 4, 12};
+    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 1, 2, 0};
+    s.share[1] = PagedShare{8, 16, !few, 1, 4, 6, 0};
     const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
     for (int i = 0; i < 2; ++i) {
-        const long long tiles = n_runs * ((n_rows * most >> s.share[i].shift) + most_requests), full = i == 1 || (dtype == HEXI_F32 && d == 128) ? 256 : 512;
-        long long n = tiles > full ? full : tiles * (blocks + s.share[i].start) / s.share[i].min_cost + 1;
+        PagedShare& h = s.share[i];
+        const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests), full = i == 1 || (dtype == HEXI_F32 && d == 128) ? 256 : 512;      // (below 2^31: rows x heads are at most 2^28)
+        while ((double)tiles * (double)((blocks >> h.coarse) + 1 + h.start) > 1e9) ++h.coarse;
+        long long n = tiles > full ? full : tiles * (blocks + h.start) / h.min_cost + 1;
         n = n > full ? full : n;
         s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;
     }

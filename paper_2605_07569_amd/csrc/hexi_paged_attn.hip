@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
         fetch_off[x] = (uint32_t)(fetch_row * (int)g.stride_tok * (int)sizeof(T)) + 16u * (uint32_t)(fetch_place ^ R::swz(x * R::PER_XFER + fetch_row));
     PagedTile open = {0, 0, 0, 0, 0, {0, 0, 0}};
     Tile t;
-    while (walk.next(t, open)) {
+    while (walk.next(a, t, open)) {
         // the lane's vectors; of one that is none the first one again
         WinKeys keys[NG];
         typename O::Q q[NG][O::NQ];
@@ -278,8 +278,6 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
             plain_tile<T, D>(t);
             continue;
         }
-        const PagedArgs& a = paged_args();
-        const PagedGeom& g = a.g;
         for (int p = tid; p < NV * D / 4; p += 64 * NW) {       // four columns of a vector
             const int i = p / (D / 4), c = 4 * (p % (D / 4));
             if (i >= t.vectors) break;
@@ -317,7 +315,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
 struct PagedJoin { PagedArgs a[2]; int n_few; };
 template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const PagedJoin)
 {
-    constexpr int D4 = D / 4, G = 256 / D4, MAX = 512, FEW = 16;
+    constexpr int D4 = D / 4, G = 256 / D4, MAX = 1024, FEW = 16;      // MAX: ranges, and so pieces
     __shared__ float weight[MAX], reduced[4];
     __shared__ __attribute__((aligned(16))) float sum[G][D];
     __shared__ int found, opened[4];
@@ -328,22 +326,23 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
     const PagedArgs& a = both.a[second];
     const PagedGeom& g = a.g;
     const int x = (int)blockIdx.x - (second ? n_few : 0), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    static_assert(MAX == 2 * 256, "two ranges to a thread");
-    const int2 of = make_int2(2 * tid < a.n_ranges ? a.tiles[2 * tid].pieces : 0, 2 * tid + 1 < a.n_ranges ? a.tiles[2 * tid + 1].pieces : 0);
-    const int active = *a.n_active, cut0 = 2 * tid < active && of.x > 0, cut1 = 2 * tid + 1 < active && of.y > 0;
-    int before = cut0 + cut1;
+    const int each = (a.n_ranges + 255) / 256;    // at most four
+    unsigned cut = 0;                             // bit i: range each tid + i starts a tile that it does not end
 #pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const int y = __shfl_up(before, off, 64);
-        if (lane >= off) before += y;
-    }
+    for (int i = 0; i < MAX / 256; ++i)
+        if (i < each && each * tid + i < a.n_ranges && a.tiles[each * tid + i].pieces > 0) cut |= 1u << i;
+    const int here = *a.n_active - each * tid;    // (behind the last range there is none: what lies there is not a tile)
+    cut &= here <= 0 ? 0u : here < each ? (1u << here) - 1 : 15u;
+    int before = paged_sum_to(__popc(cut));
     if (lane == 63) opened[wave] = before;
     if (tid == 0) found = -1;
     __syncthreads();
     for (int i = 0; i < wave; ++i) before += opened[i];
-    before -= cut0 + cut1;
-    if (cut0 && before == x) found = 2 * tid;
-    else if (cut1 && before + cut0 == x) found = 2 * tid + 1;
+    before -= __popc(cut);
+    if (x >= before && x < before + __popc(cut)) {
+        for (int i = before; i < x; ++i) cut &= cut - 1;
+        found = each * tid + __ffs(cut) - 1;
+    }
     __syncthreads();
     const int w = found;
     if (w < 0) return;

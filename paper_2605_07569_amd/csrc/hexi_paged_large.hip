@@ -75,7 +75,7 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
     if (!walk.any) return;
     PagedTile open = {0, 0, 0, 0, 0, {0, 0, 0}};
     Tile t;
-    while (walk.next(t, open)) {
+    while (walk.next(paged_args(), t, open)) {
         const int NT = t.b1 - t.b0, last = t.last;
         const int my_vector = GROUP * grp + 32 * wg + l32;
         const bool real = my_vector < t.vectors;
@@ -148,21 +148,21 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
         // Matrix phase on buffers (B + NB - 1) % NB (V of block t - 1) and B (K of block t).  Steps 0 .. NPV - 1: O^T += V^T P^T, four 16-key steps x NDB 32-column blocks; steps NPV ..
         // NST - 1: S^T for two 32-key halves.  [FIRST, LAST) selects the steps; operand fragments are requested PF steps ahead.
         constexpr int NPV = 4 * NDB, NST = NPV + 2 * NKS;
-        auto m_phase = [&](auto bc, auto first_c, auto last_c) __attribute__((always_inline)) {
-            constexpr int B = decltype(bc)::value, FIRST = decltype(first_c)::value, LAST = decltype(last_c)::value;
+        auto m_phase = [&](auto bc, auto first_c, auto last_c, const uint32_t (&k_at)[K_RUNS], const uint32_t (&v_at)[NDB]) __attribute__((always_inline)) {
+            constexpr int B = decltype(bc)::value, FIRST = decltype(first_c)::value, LAST = decltype(last_c)::value;      // B -1: the addresses are those of the buffers
             constexpr int PF = 4, NS = PF + 1;
-            constexpr int KOFF = B * C::TILE, VOFF = (B + NB - 1) % NB * C::TILE;
+            constexpr int KOFF = B < 0 ? 0 : B * C::TILE, VOFF = B < 0 ? 0 : (B + NB - 1) % NB * C::TILE;
             s16x4 ta[NS], tb[NS];
             bf16x8 kb[NS];
             auto issue = [&](auto stc) __attribute__((always_inline)) {
                 constexpr int st = decltype(stc)::value, slot = (st - FIRST) % NS;
                 if constexpr (st < NPV) {
                     constexpr int u = st / NDB, db = st % NDB;
-                    lds_issue_tr16<VOFF + 16 * u / C::ROWS * C::XFER>(ta[slot], v_addr[db]);
-                    lds_issue_tr16<VOFF + (16 * u + 8) / C::ROWS * C::XFER>(tb[slot], v_addr[db]);
+                    lds_issue_tr16<VOFF + 16 * u / C::ROWS * C::XFER>(ta[slot], v_at[db]);
+                    lds_issue_tr16<VOFF + (16 * u + 8) / C::ROWS * C::XFER>(tb[slot], v_at[db]);
                 } else {
                     constexpr int b = (st - NPV) & 1, ks = (st - NPV) >> 1, run = 2 * ks / C::RUN, in_run = 2 * ks % C::RUN;
-                    lds_issue_b128<KOFF + 32 * b / C::ROWS * C::XFER + 16 * in_run>(kb[slot], k_addr[run]);
+                    lds_issue_b128<KOFF + 32 * b / C::ROWS * C::XFER + 16 * in_run>(kb[slot], k_at[run]);
                 }
             };
             auto step = [&](auto stc) __attribute__((always_inline)) {
@@ -276,37 +276,39 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
                 const int j = i + (grp ? K_AHEAD : V_AHEAD);
                 if (j < NT) fetch_tile(j);
                 const int b = block_of(i);
-                if (i == first_full || !span_g.full(b)) v_phase(b * TN, std::true_type{}, true);
-                else v_phase(b * TN, std::false_type{}, exact);
+                if (exact || i == first_full || !span_g.full(b)) v_phase(b * TN, std::true_type{}, true);
+                else v_phase(b * TN, std::false_type{}, false);
             };
             enter_m(0);
-            m_phase(IC<0>{}, IC<NPV>{}, IC<NST>{});
+            m_phase(IC<0>{}, IC<NPV>{}, IC<NST>{}, k_addr, v_addr);
             vector_part(0);
-            // blocks 1 .. NT - 1: four at a time in a straight line, so that the buffer is a compile-time constant and no accumulator passes through a merge of control flow
+            // blocks 1 .. NT - 1: four at a time in a straight line, so that the buffer is a compile-time constant and no accumulator passes through a merge of control flow; the rest by addresses that are
+            // worked out (a copy of the phases for every remainder made the kernel twice as long, and a tile of a few blocks waits for its instructions)
             int i = 1;
             for (; i + 3 < NT; i += 4) {
-                enter_m(i);     m_phase(IC<1>{}, IC<0>{}, IC<NST>{}); vector_part(i);
-                enter_m(i + 1); m_phase(IC<2>{}, IC<0>{}, IC<NST>{}); vector_part(i + 1);
-                enter_m(i + 2); m_phase(IC<3>{}, IC<0>{}, IC<NST>{}); vector_part(i + 2);
-                enter_m(i + 3); m_phase(IC<0>{}, IC<0>{}, IC<NST>{}); vector_part(i + 3);
+                enter_m(i);     m_phase(IC<1>{}, IC<0>{}, IC<NST>{}, k_addr, v_addr); vector_part(i);
+                enter_m(i + 1); m_phase(IC<2>{}, IC<0>{}, IC<NST>{}, k_addr, v_addr); vector_part(i + 1);
+                enter_m(i + 2); m_phase(IC<3>{}, IC<0>{}, IC<NST>{}, k_addr, v_addr); vector_part(i + 2);
+                enter_m(i + 3); m_phase(IC<0>{}, IC<0>{}, IC<NST>{}, k_addr, v_addr); vector_part(i + 3);
             }
+            uint32_t k_at[K_RUNS], v_at[NDB];
+            auto buffers = [&](int i) __attribute__((always_inline)) {
+                const uint32_t of_k = (uint32_t)((i & (NB - 1)) * C::TILE), of_v = (uint32_t)(((i - 1) & (NB - 1)) * C::TILE);
+#pragma unroll
+                for (int x = 0; x < K_RUNS; ++x) k_at[x] = k_addr[x] + of_k;
+#pragma unroll
+                for (int x = 0; x < NDB; ++x) v_at[x] = v_addr[x] + of_v;
+            };
+#pragma unroll 1
             for (; i < NT; ++i) {
                 enter_m(i);
-                switch (i & 3) {
-                    case 0: m_phase(IC<0>{}, IC<0>{}, IC<NST>{}); break;
-                    case 1: m_phase(IC<1>{}, IC<0>{}, IC<NST>{}); break;
-                    case 2: m_phase(IC<2>{}, IC<0>{}, IC<NST>{}); break;
-                    default: m_phase(IC<3>{}, IC<0>{}, IC<NST>{}); break;
-                }
+                buffers(i);
+                m_phase(IC<-1>{}, IC<0>{}, IC<NST>{}, k_at, v_at);
                 vector_part(i);
             }
             enter_m(NT);
-            switch (NT & 3) {
-                case 0: m_phase(IC<0>{}, IC<0>{}, IC<NPV>{}); break;
-                case 1: m_phase(IC<1>{}, IC<0>{}, IC<NPV>{}); break;
-                case 2: m_phase(IC<2>{}, IC<0>{}, IC<NPV>{}); break;
-                default: m_phase(IC<3>{}, IC<0>{}, IC<NPV>{}); break;
-            }
+            buffers(NT);
+            m_phase(IC<-1>{}, IC<0>{}, IC<NPV>{}, k_at, v_at);
             if (!PAIR_BARRIER && grp == 0) wg_barrier();
         };
 

@@ -44,110 +44,111 @@ struct Tile {
     __device__ __forceinline__ int kv_head(const PagedGeom& g) const { return g.regular ? run : g.kvh[run]; }
 };
 
-// floor(x / y) of numbers below 2^52: exact.
-__device__ __forceinline__ long long paged_ratio(long long x, long long y)
+// Inclusive sum over a wavefront's lanes.
+__device__ __forceinline__ int paged_sum_to(int x)
 {
-    long long q = (long long)((double)x / (double)y);
-    q -= q * y > x;
-    return q + ((q + 1) * y <= x);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // from one, two, four, eight lanes below in the row of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the last lane of rows 0 and 2 to the rows behind them
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // lane 31 to the upper half
+    return x;
 }
 
-// The ranges of a launch, by a workgroup of NT threads: the sums over the requests, a few to a thread, give every workgroup its own.
+// The ranges of a launch, by a workgroup of NT threads: the sums over the requests, a few to a thread, give every workgroup its own.  (Costs are 32-bit numbers and one request, or one tile, has short ways:
+// a step of single tokens waits for this.)
 template <int NT> struct PagedWalk {
-    struct Shared { long long of_wave[NT / 64], first, of_run; PagedRequest q; int r, tiles; };
-    long long at, end, first, range;    // costs; first: in front of request r
-    long long of_run;                   // of a run of it
+    struct Shared { int of_wave[NT / 64], first, of_run, r, tiles; PagedRequest q; };
+    int at, end, first, range;          // costs; first: in front of request r
+    int of_run;                         // of a run of it
     int r, me, tiles;                   // tiles of a run of it
     PagedRequest q;
     bool any;
-    static __device__ __forceinline__ long long cost_of(const PagedArgs& a, const PagedRequest& x, int tiles)
-    {
-        return tiles == 0 ? 0LL : PagedCost(a.g, x, a.share.shift, a.share.start, tiles).before(tiles);
-    }
     __device__ __forceinline__ PagedWalk(const PagedArgs& a, Shared& sh)
     {
         const PagedGeom& g = a.g;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (g.n_requests + NT - 1) / NT, r0 = tid * each < g.n_requests ? tid * each : g.n_requests, r1 = r0 + each < g.n_requests ? r0 + each : g.n_requests;
         PagedRequest x = {0, 0, 0, 0, 0};
-        long long mine = 0, run = 0;
-        int n = 0;
-#pragma unroll 1
-        for (int i = r0; i < r1; ++i) {
+        int mine = 0, run = 0, n = 0, before = 0, total = 0;
+        auto look = [&](int i) {
             x = paged_request(g, i);
             n = paged_tiles(g, a.share, x);
-            run = cost_of(a, x, n);
-            mine += run * g.n_runs;
-        }
-        long long before = mine;
+            run = paged_cost(g, a.share, x, n);
+        };
+        if (g.n_requests == 1) {
+            look(0);
+            total = run * g.n_runs;
+        } else {
+#pragma unroll 1
+            for (int i = r0; i < r1; ++i) {
+                look(i);
+                mine += run * g.n_runs;
+            }
+            before = paged_sum_to(mine);
+            if (lane == 63) sh.of_wave[wave] = before;
+            __syncthreads();
+            before -= mine;
 #pragma unroll
-        for (int off = 1; off < 64; off *= 2) {
-            const long long y = __shfl_up(before, off, 64);
-            if (lane >= off) before += y;
-        }
-        if (lane == 63) sh.of_wave[wave] = before;
-        __syncthreads();
-        before -= mine;
-        long long total = 0;
-#pragma unroll
-        for (int w = 0; w < NT / 64; ++w) {
-            if (w < wave) before += sh.of_wave[w];
-            total += sh.of_wave[w];
+            for (int w = 0; w < NT / 64; ++w) {
+                if (w < wave) before += sh.of_wave[w];
+                total += sh.of_wave[w];
+            }
         }
         total = paged_uniform(total);
-        range = paged_ratio(total + a.n_ranges - 1, a.n_ranges);
-        range = paged_uniform(range < a.share.min_cost ? (long long)a.share.min_cost : range);
-        const int active = paged_uniform((int)paged_ratio(total + range - 1, range)), per_xcd = (active + 7) / 8, slot = (int)blockIdx.x >> 3;
+        range = (int)((unsigned)(total + a.n_ranges - 1) / (unsigned)a.n_ranges);
+        range = paged_uniform(range < a.share.min_cost ? a.share.min_cost : range);
+        const int active = paged_uniform((int)((unsigned)(total + range - 1) / (unsigned)range)), per_xcd = (active + 7) / 8, slot = (int)blockIdx.x >> 3;
         if (blockIdx.x == 0 && tid == 0) *a.n_active = active;
         me = ((int)blockIdx.x & 7) * per_xcd + slot;
         any = slot < per_xcd && me < active;
         if (!any) return;
         at = me * range;
         end = at + range < total ? at + range : total;
-        if (at >= before && at < before + mine) {
-            int i = r0;
-            if (each > 1)
+        int i = r0;
+        if (g.n_requests > 1) {
+            if (at >= before && at < before + mine) {
+                if (each > 1)
 #pragma unroll 1
-                for (;; ++i) {
-                    x = paged_request(g, i);
-                    n = paged_tiles(g, a.share, x);
-                    run = cost_of(a, x, n);
-                    if (at < before + run * g.n_runs) break;
-                    before += run * g.n_runs;
-                }
-            sh.first = before; sh.of_run = run; sh.r = i; sh.tiles = n; sh.q = x;
-        }
-        __syncthreads();
-        first = paged_uniform(sh.first);
-        of_run = paged_uniform(sh.of_run);
-        r = paged_uniform(sh.r);
-        tiles = paged_uniform(sh.tiles);
-        q = paged_uniform(sh.q);
+                    for (;; ++i) {
+                        look(i);
+                        if (at < before + run * g.n_runs) break;
+                        before += run * g.n_runs;
+                    }
+                sh.first = before; sh.of_run = run; sh.r = i; sh.tiles = n; sh.q = x;
+            }
+            __syncthreads();
+            before = sh.first; run = sh.of_run; i = sh.r; n = sh.tiles; x = sh.q;
+        } else i = 0;
+        first = paged_uniform(before);
+        of_run = paged_uniform(run);
+        r = paged_uniform(i);
+        tiles = paged_uniform(n);
+        q = paged_uniform(x);
     }
     // The next tile of the range that has vectors, and the part of it that is the range's; open: the tile that the range starts and does not end.
-    __device__ __forceinline__ bool next(Tile& t, PagedTile& open)
+    __device__ __forceinline__ bool next(const PagedArgs& a, Tile& t, PagedTile& open)
     {
-        const PagedArgs& a = paged_args();
         const PagedGeom& g = a.g;
         while (at < end) {
-            const long long in = at - first;
+            const int in = at - first;
             if (in >= of_run * g.n_runs) {
                 first += of_run * g.n_runs;
                 q = paged_uniform(paged_request(g, ++r));
                 tiles = paged_uniform(paged_tiles(g, a.share, q));
-                of_run = paged_uniform(cost_of(a, q, tiles));
+                of_run = paged_uniform(paged_cost(g, a.share, q, tiles));
                 continue;
             }
-            const int run = g.n_runs == 1 ? 0 : paged_uniform((int)paged_ratio(in, of_run));
-            int tile = 0;
-            long long c0 = 0, size = of_run;
+            const int run = g.n_runs == 1 ? 0 : paged_uniform((int)((unsigned)in / (unsigned)of_run));
+            int tile = 0, c0 = 0, size = of_run;
             if (tiles > 1) {
-                const PagedCost cost(g, q, a.share.shift, a.share.start, tiles);
+                const PagedCost cost(g, a.share, q, tiles);
                 tile = paged_uniform(cost.tile_of(in - run * of_run, tiles));
                 c0 = paged_uniform(cost.before(tile));
                 size = paged_uniform(cost.before(tile + 1)) - c0;
             }
-            const long long tile_at = first + run * of_run + c0, x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
+            const int tile_at = first + run * of_run + c0, x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
             at = tile_at + x1;
             t.q = q;
             t.r = r;
@@ -162,11 +163,11 @@ template <int NT> struct PagedWalk {
             t.last = k1.hi - 1;
             const int blocks = t.span.n_blocks;
             const bool starts = x0 == 0, ends = x1 == size;
-            auto block_at = [&](long long x) { return paged_uniform((int)((double)(x * blocks) / (double)size)); };      // (exact: below 2^48)
+            auto block_at = [&](int x) { return paged_uniform((int)((double)x * (double)blocks / (double)size)); };
             t.b0 = starts ? 0 : block_at(x0);
             t.b1 = ends ? blocks : block_at(x1);
-            t.piece = starts && ends ? -1 : 2 * (long long)me + (starts ? 1 : 0);
-            if (starts && !ends) open = PagedTile{(int)paged_uniform((int)paged_ratio(tile_at + size - 1, range)) - me + 1, t.run, q.row0, q.rows, t.v0, {0, 0, 0}};
+            t.piece = starts && ends ? -1 : 2LL * me + (starts ? 1 : 0);
+            if (starts && !ends) open = PagedTile{paged_uniform((int)((unsigned)(tile_at + size - 1) / (unsigned)range)) - me + 1, t.run, q.row0, q.rows, t.v0, {0, 0, 0}};
             return true;
         }
         return false;
