@@ -357,7 +357,8 @@ int hexi_paged_write(const hexi_paged_cache* cache, const int32_t* slot, int64_t
  * desc: that of the ring step; its kv strides are not used.  q: [n_rows][n_q_heads][head_dim] with its strides.  table, columns: as in
  * hexi_paged_plan; an entry that is no page of the cache holds no keys.
  * o: [n_rows][n_q_heads][head_dim], dense, of o_dtype (HEXI_BF16: rounded once); lse: fp32 [n_q_heads][n_rows], or NULL.  Rows that see no key get
- * o = 0, lse = -INFINITY; rows in front of the first request's and behind the last one's are left as they are.  Values of keys that a row does not
+ * o = 0, lse = -INFINITY; rows in front of the first request's and behind the last one's are left as they are, and all of them where
+ * row_start does not ascend from 0 or more to n_rows or less.  Lengths out of range count as the nearest that are not.  Values of keys that a row does not
  * see do not reach it, infinities and NaN included.  Results are reproducible run to run.
  * max_rows: no request has more rows than this (further ones are left as they are); 0 where that is not known.
  * workspace: hexi_paged_attn_workspace_bytes() bytes of device memory, 16-byte aligned.  Nothing is kept in it between calls; calls that may run at

@@ -118,8 +118,9 @@ struct PagedWriteArgs {
 // The query vectors of a request and a head run (row by row, a row's heads side by side) are cut into tiles; a tile costs about the 64-key blocks that its last row sees and a start.
 // All tiles of all requests lie one behind the other (request, run, tile), and every workgroup takes an equal range of their summed costs: contexts of all lengths fill the chip evenly,
 // and neighbouring ranges, which are dealt to one XCD, share keys.  A range that ends inside a tile leaves a partial result of it: part_o [2 ranges][vectors][d], normalised, and part_lse; piece
-// 2 w + 1 is that of a tile which range w starts, 2 w that of one which it goes on with, and tiles[w] tells the joining launch of the tile that range w starts and does not end.
-struct PagedTile { int pieces, run, row0, rows, v0, pad[3]; };      // pieces: 0 where there is no such tile; v0: first vector
+// 2 w + 1 is that of a tile which range w starts, 2 w that of one which it goes on with.  The range that starts a tile leaves word of it for the joining launch, in an entry for every tile, or, where
+// there may be more tiles than ranges, for every range (which starts one at most that it does not end).
+struct PagedTile { int pieces, run, row0, rows, v0, range, pad[2]; };      // pieces: 0 where the tile is not cut; v0: first vector; range: that starts it
 
 // Costs of a request's tiles, in units of 2^coarse blocks; before(t): of the first t tiles of a run, by the closed form of its sums, so that no table is needed.
 // Of tile t the last row sees keys up to at + (t + 1) vectors / most, and a window leaves out what the first one no longer sees.  The host sees to it that all costs of a launch together stay
@@ -190,8 +191,9 @@ struct PagedArgs {
     float* lse;               // may be null
     int out_bf16;
     int n_ranges;
-    int* n_active;            // ranges that there is work for
-    PagedTile* tiles;
+    int n_entries, by_tile;   // entries there is room for; whether they are the tiles'
+    int* n_used;              // entries that are written
+    PagedTile* entries;
     float *part_o, *part_lse;
 };
 
@@ -202,6 +204,7 @@ constexpr int paged_ring(size_t bytes, int d) { return (int)bytes * d <= 128 ? 4
 struct PagedShape {
     PagedShare share[2];
     int ranges[2];            // workgroups, multiples of 8; 0: the kernel is not launched
+    int entries[2];           // tiles there may be, no more than ranges
     bool splits;              // a tile can be cut: a further launch joins
 };
 inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
@@ -219,6 +222,7 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
         long long n = tiles > full ? full : tiles * (blocks + h.start) / h.min_cost + 1;
         n = n > full ? full : n;
         s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;
+        s.entries[i] = (int)(tiles < s.ranges[i] ? tiles : s.ranges[i]);
     }
     s.splits = blocks > 2;
     return s;
@@ -231,9 +235,11 @@ inline void hexi_paged_place(const PagedShape& s, int i, int d, char* workspace,
 {
     a->share = s.share[i];
     a->n_ranges = s.ranges[i];
-    a->n_active = (int*)workspace;
-    a->tiles = (PagedTile*)(workspace + 256);
-    a->part_o = (float*)(a->tiles + s.ranges[i]);
+    a->n_entries = s.entries[i];
+    a->by_tile = s.entries[i] < s.ranges[i];
+    a->n_used = (int*)workspace;
+    a->entries = (PagedTile*)(workspace + 256);
+    a->part_o = (float*)(a->entries + s.ranges[i]);
     a->part_lse = a->part_o + (size_t)2 * (size_t)s.ranges[i] * ((size_t)d << s.share[i].shift);
 }
 

@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
     using R = Rows<T, D>;
     constexpr int NV = 16 * NG;
     constexpr int AHEAD = paged_ring(sizeof(T), D);      // blocks of a ring
-    struct Ends { float acc[NW][NV][D + 4], stat[3][NW][NV]; };      // stat: reference, sum of P, sum of P as it was multiplied
+    struct Ends { float acc[NW][NV][D + 4], stat[3][NW][NV]; int out[NV]; };      // stat: reference, sum of P, sum of P as it was multiplied
     struct Ring { unsigned char k[AHEAD][R::TILE], v[AHEAD][R::TILE]; };
     __shared__ __attribute__((aligned(1024))) union { Ring ring[NW]; Ends ends; } sm;
     __shared__ typename PagedWalk<64 * NW>::Shared shared;
@@ -155,9 +155,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
 #pragma unroll
     for (int x = 0; x < R::XFERS; ++x)
         fetch_off[x] = (uint32_t)(fetch_row * (int)g.stride_tok * (int)sizeof(T)) + 16u * (uint32_t)(fetch_place ^ R::swz(x * R::PER_XFER + fetch_row));
-    PagedTile open = {0, 0, 0, 0, 0, {0, 0, 0}};
     Tile t;
-    while (walk.next(a, t, open)) {
+    while (walk.next(a, t)) {
         // the lane's vectors; of one that is none the first one again
         WinKeys keys[NG];
         typename O::Q q[NG][O::NQ];
@@ -278,75 +277,63 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
             plain_tile<T, D>(t);
             continue;
         }
-        for (int p = tid; p < NV * D / 4; p += 64 * NW) {       // four columns of a vector
-            const int i = p / (D / 4), c = 4 * (p % (D / 4));
-            if (i >= t.vectors) break;
-            float mm = -INFINITY, sum = 0.f, used = 0.f;
+        if (tid < NV) {                           // a vector's LSE, and what the wavefronts' sums of V are multiplied by
+            float mm = -INFINITY, sum = 0.f, used = 0.f, e[NW];
 #pragma unroll
-            for (int x = 0; x < NW; ++x) mm = fmaxf(mm, sm.ends.stat[0][x][i]);
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+            for (int x = 0; x < NW; ++x) mm = fmaxf(mm, sm.ends.stat[0][x][tid]);
 #pragma unroll
             for (int x = 0; x < NW; ++x) {
                 // (d is -inf too where the two are finite and far apart: 0, whatever the sign of c_lo)
-                const float r = sm.ends.stat[0][x][i], d = r - mm, e = r == -INFINITY ? 0.f : fast_exp2(fmaf(d, c_hi, d == -INFINITY ? 0.f : d * c_lo));
-                sum += e * sm.ends.stat[1][x][i];
-                used += e * sm.ends.stat[2][x][i];
-                o += e * *reinterpret_cast<const f32x4*>(&sm.ends.acc[x][i][c]);
+                const float r = sm.ends.stat[0][x][tid], d = r - mm;
+                e[x] = r == -INFINITY ? 0.f : fast_exp2(fmaf(d, c_hi, d == -INFINITY ? 0.f : d * c_lo));
+                sum += e[x] * sm.ends.stat[1][x][tid];
+                used += e[x] * sm.ends.stat[2][x][tid];
             }
-            const float lse = sum == 0.f ? -INFINITY : fmaf(mm, g.scale, logf(sum));
-            o *= used == 0.f ? 0.f : 1.0f / used;
-            if (t.piece >= 0) {
-                const long long at = t.piece * NV + i;
-                if (c == 0) a.part_lse[at] = lse;
-                win_plain::store4(a.part_o, at * D + c, false, o[0], o[1], o[2], o[3]);
-            } else {
-                const int row = t.row_of(i), h = t.head_of(g, i, row);
-                if (c == 0 && a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
-                win_plain::store4(a.o, paged_out(a, t, row, h) * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
+            const float lse = sum == 0.f ? -INFINITY : fmaf(mm, g.scale, logf(sum)), r = used == 0.f ? 0.f : 1.0f / used;
+#pragma unroll
+            for (int x = 0; x < NW; ++x) sm.ends.stat[0][x][tid] = e[x] * r;
+            int at = -1;
+            if (tid < t.vectors) {
+                const int row = t.row_of(tid), h = t.head_of(g, tid, row);
+                at = (int)paged_out(a, t, row, h);
+                if (t.piece >= 0) a.part_lse[(long long)t.piece * NV + tid] = lse;
+                else if (a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
             }
+            sm.ends.out[tid] = at;
+        }
+        __syncthreads();
+        for (int p = tid; p < t.vectors * (D / 4); p += 64 * NW) {       // four columns of a vector
+            const int i = p / (D / 4), c = 4 * (p % (D / 4));
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < NW; ++x) o += sm.ends.stat[0][x][i] * *reinterpret_cast<const f32x4*>(&sm.ends.acc[x][i][c]);
+            if (t.piece >= 0) win_plain::store4(a.part_o, ((long long)t.piece * NV + i) * D + c, false, o[0], o[1], o[2], o[3]);
+            else win_plain::store4(a.o, (long long)sm.ends.out[i] * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
         }
         __syncthreads();                          // the rings are written again
     }
-    if (tid == 0) paged_args().tiles[walk.me] = open;
+    walk.done(a);
 }
 
-// The pieces of a tile joined, as hexi_attn_merge_lse joins two.  Workgroup (x, y): the x-th tile that is cut.  Of a few pieces a thread takes four columns of a vector and reads them
-// all; of many a workgroup takes a vector at a time, 16 or 32 threads to its columns and the pieces dealt to the groups of these.
-struct PagedJoin { PagedArgs a[2]; int n_few; };
+// The pieces of a tile joined, as hexi_attn_merge_lse joins two; `ways` workgroups to an entry.  Of a few pieces a thread takes four columns of a vector and reads them all; of many a workgroup takes
+// half the columns of a vector at a time, 8 or 16 threads to them and the pieces dealt to the groups of these.
+struct PagedJoin { PagedArgs a[2]; int ways[2]; };
 template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const PagedJoin)
 {
-    constexpr int D4 = D / 4, G = 256 / D4, MAX = 1024, FEW = 16;      // MAX: ranges, and so pieces
+    constexpr int D4 = D / 4, H4 = D4 / 2, G = 256 / H4, MAX = 512, FEW = 16;      // MAX: ranges, and so pieces
     __shared__ float weight[MAX], reduced[4];
-    __shared__ __attribute__((aligned(16))) float sum[G][D];
-    __shared__ int found, opened[4];
+    __shared__ __attribute__((aligned(16))) float sum[G][D / 2];
     typedef const __attribute__((address_space(4))) PagedJoin* Ptr;
     const PagedJoin& both = *(const PagedJoin*)(Ptr)__builtin_amdgcn_kernarg_segment_ptr();      // (indexed where it lies)
-    const int n_few = both.n_few;
+    const int n_few = both.a[0].n_entries * both.ways[0];
     const bool second = (int)blockIdx.x >= n_few;
     const PagedArgs& a = both.a[second];
     const PagedGeom& g = a.g;
-    const int x = (int)blockIdx.x - (second ? n_few : 0), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (a.n_ranges + 255) / 256;    // at most four
-    unsigned cut = 0;                             // bit i: range each tid + i starts a tile that it does not end
-#pragma unroll
-    for (int i = 0; i < MAX / 256; ++i)
-        if (i < each && each * tid + i < a.n_ranges && a.tiles[each * tid + i].pieces > 0) cut |= 1u << i;
-    const int here = *a.n_active - each * tid;    // (behind the last range there is none: what lies there is not a tile)
-    cut &= here <= 0 ? 0u : here < each ? (1u << here) - 1 : 15u;
-    int before = paged_sum_to(__popc(cut));
-    if (lane == 63) opened[wave] = before;
-    if (tid == 0) found = -1;
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) before += opened[i];
-    before -= __popc(cut);
-    if (x >= before && x < before + __popc(cut)) {
-        for (int i = before; i < x; ++i) cut &= cut - 1;
-        found = each * tid + __ffs(cut) - 1;
-    }
-    __syncthreads();
-    const int w = found;
-    if (w < 0) return;
-    const PagedTile t = a.tiles[w];
+    const int ways = both.ways[second], block = (int)blockIdx.x - (second ? n_few : 0), x = block / ways, way = block - x * ways;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const PagedTile t = a.entries[x];
+    if (x >= *a.n_used || t.pieces == 0) return;
+    const int w = t.range;
     const int nv = 1 << a.share.shift, count = g.regular ? g.most : g.first[t.run + 1] - g.first[t.run], left = t.rows * count - t.v0, vectors = left < nv ? left : nv;
     auto piece_of = [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); };
     auto put = [&](int i, int c, const f32x4& o, float m, float total) {
@@ -356,7 +343,7 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
         win_plain::store4(a.o, ((long long)(t.row0 + row) * g.nq + h) * D + c, a.out_bf16, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
     };
     if (t.pieces <= FEW) {
-        for (int p = (int)blockIdx.y * 256 + tid; p < vectors * D4; p += (int)gridDim.y * 256) {
+        for (int p = way * 256 + tid; p < vectors * D4; p += ways * 256) {
             const int i = p / D4, c = 4 * (p % D4);
             float m = -INFINITY, total = 0.f;
             f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -374,7 +361,8 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
         }
         return;
     }
-    for (int i = blockIdx.y; i < vectors; i += gridDim.y) {
+    for (int part = way; part < 2 * vectors; part += ways) {
+        const int i = part >> 1, c = (part & 1) * (D / 2) + 4 * (tid % H4), p0 = tid / H4;
         float m = -INFINITY;
         for (int p = tid; p < t.pieces; p += 256) {
             const float l = a.part_lse[(long long)piece_of(p) * nv + i];
@@ -399,16 +387,15 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
         if (lane == 0) reduced[wave] = total;
         __syncthreads();
         total = (reduced[0] + reduced[1]) + (reduced[2] + reduced[3]);
-        const int c = 4 * (tid % D4), p0 = tid / D4;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 16
         for (int p = p0; p < t.pieces; p += G) o += weight[p] * *reinterpret_cast<const f32x4*>(a.part_o + ((long long)piece_of(p) * nv + i) * D + c);
-        *reinterpret_cast<f32x4*>(&sum[p0][c]) = o;
+        *reinterpret_cast<f32x4*>(&sum[p0][4 * (tid % H4)]) = o;
         __syncthreads();
-        if (tid < D4) {
-            o = *reinterpret_cast<const f32x4*>(&sum[0][c]);
+        if (tid < H4) {
+            o = *reinterpret_cast<const f32x4*>(&sum[0][4 * tid]);
 #pragma unroll
-            for (int k = 1; k < G; ++k) o += *reinterpret_cast<const f32x4*>(&sum[k][c]);
+            for (int k = 1; k < G; ++k) o += *reinterpret_cast<const f32x4*>(&sum[k][4 * tid]);
             put(i, c, o, m, total);
         }
         __syncthreads();
@@ -436,14 +423,14 @@ hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, hipStream
 
 hipError_t hexi_launch_paged_join(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s)
 {
-    // as many cut tiles as there may be; of few, which may have many pieces, a workgroup to a vector
-    auto cut = [](const PagedArgs& a) {
-        const long long tiles = a.g.n_runs * (((long long)a.g.n_rows * a.g.most >> a.share.shift) + (a.g.n_requests < a.g.n_rows ? a.g.n_requests : a.g.n_rows));
-        return (unsigned)(tiles < a.n_ranges ? tiles : a.n_ranges);
+    // about as many workgroups as the chip holds at once, most of them for the large tiles; few tiles may have many pieces
+    auto ways = [](const PagedArgs& a) {
+        const int n = a.n_entries > 0 ? (a.share.shift == 8 ? 2048 : 1024) / a.n_entries : 1;
+        return n > 32 ? 32 : n < 1 ? 1 : n;
     };
-    const unsigned n_few = cut(few), n_large = cut(large);
-    const dim3 grid(n_few + n_large, n_few + n_large <= 64 ? 16u : n_large ? 8u : 2u);
-    if (d == 128) paged_join_kernel<128><<<grid, 256, 0, s>>>(PagedJoin{{few, large}, (int)n_few});
-    else paged_join_kernel<64><<<grid, 256, 0, s>>>(PagedJoin{{few, large}, (int)n_few});
+    const PagedJoin both = {{few, large}, {ways(few), ways(large)}};
+    const unsigned grid = (unsigned)(few.n_entries * both.ways[0] + large.n_entries * both.ways[1]);
+    if (d == 128) paged_join_kernel<128><<<grid, 256, 0, s>>>(both);
+    else paged_join_kernel<64><<<grid, 256, 0, s>>>(both);
     return hipGetLastError();
 }

@@ -73,9 +73,8 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
 
     PagedWalk<512> walk(a, shared);
     if (!walk.any) return;
-    PagedTile open = {0, 0, 0, 0, 0, {0, 0, 0}};
     Tile t;
-    while (walk.next(paged_args(), t, open)) {
+    while (walk.next(paged_args(), t)) {
         const int NT = t.b1 - t.b0, last = t.last;
         const int my_vector = GROUP * grp + 32 * wg + l32;
         const bool real = my_vector < t.vectors;
@@ -348,7 +347,7 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
                     make_float4(oacc[db][4 * b] * inv, oacc[db][4 * b + 1] * inv, oacc[db][4 * b + 2] * inv, oacc[db][4 * b + 3] * inv);
         if (hh == 0) {
             stage_at[l32] = real ? t.piece >= 0 ? my_vector : (int)paged_out(a, t, my_row, my_head) : -1;
-            if (real && t.piece >= 0) a.part_lse[t.piece * WG + my_vector] = lse;
+            if (real && t.piece >= 0) a.part_lse[(long long)t.piece * WG + my_vector] = lse;
             else if (real && a.lse) a.lse[(long long)my_head * g.n_rows + t.q.row0 + my_row] = lse;
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -361,12 +360,12 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
             const int r = ROWS * i + sub_row, at = stage_at[r];
             const float4 x = *reinterpret_cast<const float4*>(&stage[r * C::PITCH + col]);
             if (at < 0) continue;
-            if (t.piece >= 0) win_plain::store4(a.part_o, (t.piece * WG + at) * D + col, false, x.x, x.y, x.z, x.w);
+            if (t.piece >= 0) win_plain::store4(a.part_o, ((long long)t.piece * WG + at) * D + col, false, x.x, x.y, x.z, x.w);
             else win_plain::store4(a.o, (long long)at * D + col, a.out_bf16, x.x, x.y, x.z, x.w);
         }
         __syncthreads();                          // the next tile's transfers write where these rows were staged
     }
-    if (tid == 0) paged_args().tiles[walk.me] = open;
+    walk.done(paged_args());
 }
 
 }  // namespace

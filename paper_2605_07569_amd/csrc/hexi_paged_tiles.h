@@ -34,7 +34,7 @@ struct Tile {
     int r, run, count, v0, vectors;     // count: heads of the run; vectors: how many it has, none where 0
     int b0, b1;                         // blocks of the span that are this range's
     int last;                           // no row sees a key behind this one; -1: none is seen, and there are no blocks
-    long long piece;                    // of the partial results; -1: the tile is this range's alone
+    int piece;                          // of the partial results; -1: the tile is this range's alone
     __device__ __forceinline__ int row_of(int v) const { return (int)((unsigned)(v0 + v) / (unsigned)count); }
     __device__ __forceinline__ int head_of(const PagedGeom& g, int v, int row) const
     {
@@ -59,11 +59,13 @@ __device__ __forceinline__ int paged_sum_to(int x)
 // The ranges of a launch, by a workgroup of NT threads: the sums over the requests, a few to a thread, give every workgroup its own.  (Costs are 32-bit numbers and one request, or one tile, has short ways:
 // a step of single tokens waits for this.)
 template <int NT> struct PagedWalk {
-    struct Shared { int of_wave[NT / 64], first, of_run, r, tiles; PagedRequest q; };
+    struct Shared { int of_wave[NT / 64], tiles_of_wave[NT / 64], first, of_run, r, tiles, number; PagedRequest q; };
     int at, end, first, range;          // costs; first: in front of request r
     int of_run;                         // of a run of it
     int r, me, tiles;                   // tiles of a run of it
+    int number;                         // tiles in front of it
     PagedRequest q;
+    PagedTile open;                     // the tile that the range starts and does not end
     bool any;
     __device__ __forceinline__ PagedWalk(const PagedArgs& a, Shared& sh)
     {
@@ -71,36 +73,47 @@ template <int NT> struct PagedWalk {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (g.n_requests + NT - 1) / NT, r0 = tid * each < g.n_requests ? tid * each : g.n_requests, r1 = r0 + each < g.n_requests ? r0 + each : g.n_requests;
         PagedRequest x = {0, 0, 0, 0, 0};
-        int mine = 0, run = 0, n = 0, before = 0, total = 0;
+        int mine = 0, mine_tiles = 0, run = 0, n = 0, before = 0, total = 0, before_tiles = 0, all_tiles = 0;
+        bool bad = false;                   // row starts that do not ascend within the rows: nothing is computed (and all sums below are of rows that there are)
         auto look = [&](int i) {
             x = paged_request(g, i);
+            bad |= g.row_start[i] != x.row0 || g.row_start[i + 1] < x.row0 || g.row_start[i + 1] > g.n_rows;
             n = paged_tiles(g, a.share, x);
             run = paged_cost(g, a.share, x, n);
         };
         if (g.n_requests == 1) {
             look(0);
-            total = run * g.n_runs;
+            total = bad ? 0 : run * g.n_runs;
+            all_tiles = bad ? 0 : n * g.n_runs;
         } else {
 #pragma unroll 1
             for (int i = r0; i < r1; ++i) {
                 look(i);
                 mine += run * g.n_runs;
+                mine_tiles += n * g.n_runs;
             }
             before = paged_sum_to(mine);
-            if (lane == 63) sh.of_wave[wave] = before;
+            before_tiles = paged_sum_to(mine_tiles);
+            const bool any_bad = __any(bad);
+            if (lane == 63) { sh.of_wave[wave] = before; sh.tiles_of_wave[wave] = any_bad ? -1 : before_tiles; }
             __syncthreads();
             before -= mine;
+            before_tiles -= mine_tiles;
+            bad = false;
 #pragma unroll
             for (int w = 0; w < NT / 64; ++w) {
-                if (w < wave) before += sh.of_wave[w];
+                if (w < wave) { before += sh.of_wave[w]; before_tiles += sh.tiles_of_wave[w]; }
                 total += sh.of_wave[w];
+                all_tiles += sh.tiles_of_wave[w];
+                bad |= sh.tiles_of_wave[w] < 0;
             }
+            if (bad) total = all_tiles = 0;
         }
         total = paged_uniform(total);
         range = (int)((unsigned)(total + a.n_ranges - 1) / (unsigned)a.n_ranges);
         range = paged_uniform(range < a.share.min_cost ? a.share.min_cost : range);
         const int active = paged_uniform((int)((unsigned)(total + range - 1) / (unsigned)range)), per_xcd = (active + 7) / 8, slot = (int)blockIdx.x >> 3;
-        if (blockIdx.x == 0 && tid == 0) *a.n_active = active;
+        if (blockIdx.x == 0 && tid == 0) *a.n_used = a.by_tile ? all_tiles : active;
         me = ((int)blockIdx.x & 7) * per_xcd + slot;
         any = slot < per_xcd && me < active;
         if (!any) return;
@@ -115,26 +128,30 @@ template <int NT> struct PagedWalk {
                         look(i);
                         if (at < before + run * g.n_runs) break;
                         before += run * g.n_runs;
+                        before_tiles += n * g.n_runs;
                     }
-                sh.first = before; sh.of_run = run; sh.r = i; sh.tiles = n; sh.q = x;
+                sh.first = before; sh.of_run = run; sh.r = i; sh.tiles = n; sh.number = before_tiles; sh.q = x;
             }
             __syncthreads();
-            before = sh.first; run = sh.of_run; i = sh.r; n = sh.tiles; x = sh.q;
+            before = sh.first; run = sh.of_run; i = sh.r; n = sh.tiles; before_tiles = sh.number; x = sh.q;
         } else i = 0;
         first = paged_uniform(before);
         of_run = paged_uniform(run);
         r = paged_uniform(i);
         tiles = paged_uniform(n);
+        number = paged_uniform(before_tiles);
         q = paged_uniform(x);
+        open.pieces = 0;
     }
-    // The next tile of the range that has vectors, and the part of it that is the range's; open: the tile that the range starts and does not end.
-    __device__ __forceinline__ bool next(const PagedArgs& a, Tile& t, PagedTile& open)
+    // The next tile of the range that has vectors, and the part of it that is the range's.
+    __device__ __forceinline__ bool next(const PagedArgs& a, Tile& t)
     {
         const PagedGeom& g = a.g;
         while (at < end) {
             const int in = at - first;
             if (in >= of_run * g.n_runs) {
                 first += of_run * g.n_runs;
+                number += tiles * g.n_runs;
                 q = paged_uniform(paged_request(g, ++r));
                 tiles = paged_uniform(paged_tiles(g, a.share, q));
                 of_run = paged_uniform(paged_cost(g, a.share, q, tiles));
@@ -157,20 +174,28 @@ template <int NT> struct PagedWalk {
             t.v0 = tile << a.share.shift;
             const int left = q.rows * t.count - t.v0;
             t.vectors = left < 1 << a.share.shift ? left : 1 << a.share.shift;
+            const bool starts = x0 == 0, ends = x1 == size;
+            if (starts) {
+                open = PagedTile{ends || t.vectors <= 0 ? 0 : paged_uniform((int)((unsigned)(tile_at + size - 1) / (unsigned)range)) - me + 1, t.run, q.row0, q.rows, t.v0, me, {0, 0}};
+                if (a.by_tile && threadIdx.x == 0) a.entries[number + run * tiles + tile] = open;
+            }
             if (t.vectors <= 0) continue;
             const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(t.vectors - 1)));
             t.span = WinSpan<PAGED_KEYS>(k0, k1, q.kv);
             t.last = k1.hi - 1;
             const int blocks = t.span.n_blocks;
-            const bool starts = x0 == 0, ends = x1 == size;
             auto block_at = [&](int x) { return paged_uniform((int)((double)x * (double)blocks / (double)size)); };
             t.b0 = starts ? 0 : block_at(x0);
             t.b1 = ends ? blocks : block_at(x1);
-            t.piece = starts && ends ? -1 : 2LL * me + (starts ? 1 : 0);
-            if (starts && !ends) open = PagedTile{paged_uniform((int)((unsigned)(tile_at + size - 1) / (unsigned)range)) - me + 1, t.run, q.row0, q.rows, t.v0, {0, 0, 0}};
+            t.piece = starts && ends ? -1 : 2 * me + (starts ? 1 : 0);
             return true;
         }
         return false;
+    }
+    // Behind the last tile.
+    __device__ __forceinline__ void done(const PagedArgs& a) const
+    {
+        if (!a.by_tile && threadIdx.x == 0) a.entries[me] = open;
     }
 };
 
@@ -220,7 +245,7 @@ template <class T, int D> __device__ __forceinline__ void plain_tile(const Tile&
         }
         const float lse = l == 0.f ? -INFINITY : m + logf(l), r = l == 0.f ? 0.f : 1.0f / l;
         if (t.piece >= 0) {
-            const long long at = (t.piece << a.share.shift) + i;
+            const long long at = ((long long)t.piece << a.share.shift) + i;
             if (col == 0) a.part_lse[at] = lse;
 #pragma unroll
             for (int c = 0; c < N; c += 4) win_plain::store4(a.part_o, at * D + col + c, false, r * acc[c], r * acc[c + 1], r * acc[c + 2], r * acc[c + 3]);

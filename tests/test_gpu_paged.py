@@ -106,22 +106,25 @@ def test_entries_that_are_no_page_hold_no_keys(dtype):
     assert (o[s.starts[3]:] == 0).all() and (lse[:, s.starts[3]:] == -INF).all()
 
 
-def test_lengths_that_are_anything_stay_inside_the_tensors():
-    """Row starts and lengths out of range are taken as the nearest that are not; nothing outside the named rows is written (the arithmetic runs on the CPU too: test_paged_cpu.py)."""
-    c = Case("wild", [(100, 3), (60, 2), (40, 1)], nq=4, nkv=2, page=16, behind=3)
+@pytest.mark.parametrize("rows", [3, 40])      # both kernels
+def test_lengths_that_are_anything_stay_inside_the_tensors(rows):
+    """Lengths out of range are taken as the nearest that are not, row starts that do not ascend within the rows leave everything as it was (the arithmetic runs on the CPU too: test_paged_cpu.py)."""
+    c = Case("wild", [(100, rows), (60, 2), (40, 1)], nq=4, nkv=2, page=16, behind=3)
     s = Setup(c, BF16, 64)
     s.table.clamp_(min=0)
     s.k_cache.nan_to_num_(0.0)
     s.v_cache.nan_to_num_(0.0)
-    for starts, lens in (([-5, 3, 2 ** 31 - 1, 2 ** 31 - 1], [2 ** 31 - 1, -3, 40]), ([4, 2, 2, 3], [100, 60, 40]), ([-2 ** 31, -1, 0, 0], [1, 1, 1])):
-        s.row_start, s.kv_len = ints(starts), ints(lens)
+    big, n = 2 ** 31 - 1, c.rows
+    for starts in ([-5, 3, 4, 4], [4, 2, 2, 3], [-big - 1, -1, 0, 0], [0, 3, big, big], [0, n, 0, n], [0, 1, n + 1, n + 2], [big, big, big, big]):
+        s.row_start = ints(starts)
         o, lse = s.run()
         torch.cuda.synchronize()
-        clip = [min(max(x, 0), c.rows) for x in starts]
-        mine = torch.zeros(c.rows, dtype=torch.bool)
-        for a, b in zip(clip, clip[1:]):
-            mine[a:b] = True
-        assert o.isfinite().all() and (o[~mine.to(DEV)] == 7).all() and not (o[mine.to(DEV)] == 7).any()
+        assert (o == 7).all() and (lse == 7).all(), starts
+    for lens in ([big, -3, 40], [-big - 1, 0, big], [100, 60, 40]):
+        s.row_start, s.kv_len = ints([1, 1 + rows, 1 + rows, n]), ints(lens)
+        o, lse = s.run()
+        torch.cuda.synchronize()
+        assert o.isfinite().all() and (o[:1] == 7).all() and not (o[1:] == 7).any() and not (lse[:, 1:] == 7).any(), lens
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
