@@ -6,8 +6,8 @@
 //
 // What pages change is how a 64-key block comes to LDS.  A transfer (1 KB: 64 lanes x 16 bytes, back to back) takes its address from a scalar base, the page's, so all its rows have to lie on one page:
 // 4 whole rows (8 at 64 columns), and each wavefront takes the 16 rows of one page by itself.  Rows are not padded then but transfers are, by 16 bytes, and inside one
-// the 16-byte pieces of a row are exchanged by their high bits (`flip`), so that both the 128-bit row reads of K and the transposed 64-bit reads of V^T touch all 64 banks once: of 16 rows
-// of K the same piece lies in four (two) places by flip, moved on by a piece a transfer; four rows of V side by side lie in different quarters by flip.
+// the 16-byte pieces of a row are exchanged by their high bits (`flip`), so that both the 128-bit row reads of K and the transposed 64-bit reads of V^T touch all 64 banks once (a 128-bit read is
+// served 16 lanes at a time, 0-3, 12-15, 20-23, 24-27 and so on, a transposed one 32 neighbouring lanes).
 #include "hexi_mfma.h"
 #include "hexi_paged_tiles.h"
 
@@ -26,7 +26,7 @@ template <int D> struct Cfg {
     static constexpr int XFER = 1024 + 16, XFERS = TN / ROWS, PER_WAVE = XFERS / 4;
     static constexpr int TILE = XFERS * XFER;
     // which of its four places the aligned run of pieces (4 of 16 at 128 columns, 2 of 8 at 64) with number `a` takes in row r of a transfer: a ^ flip(r)
-    static constexpr __host__ __device__ int flip(int r) { return D == 128 ? r & 3 : ((r >> 1) & 1) * 2 + ((r >> 2) & 1); }
+    static constexpr __host__ __device__ int flip(int r) { return D == 128 ? r & 3 : r & 2; }
     static constexpr int RUN = D / 32;                             // pieces of a run
     static constexpr int PITCH = D + 4;                            // floats of a staged output row
 };
