@@ -8,30 +8,47 @@ namespace {
 //
 // Sums over the requests in front (pages that go back, pages that are asked for, rows) say where everything goes, so one workgroup forms them, a few requests to a thread,
 // and the flat lists of pages and rows are then shared out over all threads, each of which finds its request by halving.
-// What bounds it: latency, of the reads that follow each other (lengths, then pages, then the free list) and of the barriers between them.
+// What bounds it: latency, of the reads that follow each other (lengths, then pages, then the free list) and of the barriers between them; so three sums are formed at once, by lane shifts, and
+// lengths are read once where a thread has one request.
 
 constexpr int PT = 1024;      // threads
 
-// Exclusive sum over the workgroup, and the total.
-__device__ __forceinline__ long long sum_before(long long x, long long* of_wave, long long* total)
+// Numbers that are no counts of anything may add up to more than 32 bits: sums stay at 2^32 - 1 then, which is above all that they are compared with.
+__device__ __forceinline__ unsigned sat(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ unsigned from_below(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false); }
+
+// Sums over the threads in front, and over all.
+template <int N> struct Sums { unsigned before[N], all[N]; };
+template <int N> __device__ __forceinline__ Sums<N> sums_before(const unsigned (&x)[N], unsigned (*of_wave)[PT / 64])
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    long long s = x;
+    static_assert(PT / 64 == 16, "a wave's total to a lane of a row");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Sums<N> r;
 #pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const long long y = __shfl_up(s, off, 64);
-        if (lane >= off) s += y;
+    for (int i = 0; i < N; ++i) {
+        unsigned s = x[i];
+        s = sat(s, from_below<0x111>(s));         // one, two, four, eight lanes below in the row of 16
+        s = sat(s, from_below<0x112>(s));
+        s = sat(s, from_below<0x114>(s));
+        s = sat(s, from_below<0x118>(s));
+        s = sat(s, from_below<0x142, 0xa>(s));    // the last lane of rows 0 and 2 to the rows behind them
+        s = sat(s, from_below<0x143, 0xc>(s));    // lane 31 to the upper half
+        if (lane == 63) of_wave[i][wave] = s;
+        r.before[i] = from_below<0x138>(s);       // the lane below
     }
-    if (lane == 63) of_wave[wave] = s;
     __syncthreads();
-    long long before = 0, all = 0;
-    for (int w = 0; w < PT / 64; ++w) {
-        if (w < wave) before += of_wave[w];
-        all += of_wave[w];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        unsigned s = of_wave[i][lane & 15];
+        s = sat(s, from_below<0x111>(s));
+        s = sat(s, from_below<0x112>(s));
+        s = sat(s, from_below<0x114>(s));
+        s = sat(s, from_below<0x118>(s));
+        r.all[i] = (unsigned)__builtin_amdgcn_readlane((int)s, 15);
+        if (wave > 0) r.before[i] = sat(r.before[i], (unsigned)__builtin_amdgcn_readlane((int)s, wave - 1));
     }
     __syncthreads();
-    *total = all;
-    return before + s - x;
+    return r;
 }
 
 // Last r in [0, n) with first[r] <= i (first[0] = 0, ascending).
@@ -63,79 +80,87 @@ __device__ __forceinline__ void place_row(const PagedPlanArgs& a, const int* fir
     a.slot[t] = slot;
 }
 
+__device__ __forceinline__ int to_int(unsigned x) { return x < 0x7fffffffu ? (int)x : 0x7fffffff; }
+__device__ __forceinline__ unsigned to_sum(long long x) { return x < 0xffffffffLL ? (unsigned)x : 0xffffffffu; }
+
 __global__ void __launch_bounds__(PT) paged_plan_kernel(const PagedPlanArgs a, const int rows_here)
 {
     extern __shared__ int first[];      // [n_requests]
-    __shared__ long long of_wave[PT / 64];
+    __shared__ unsigned of_wave[3][PT / 64];
     const int tid = threadIdx.x, n = a.n_requests, page = (int)a.by_page.d;
     const int each = (n + PT - 1) / PT, r0 = tid * each < n ? tid * each : n, r1 = r0 + each < n ? r0 + each : n;
-    auto ask = [&](int r) { return paged_ask(a.cached[r], a.added[r], a.held[r], page, a.columns); };
     const int had = paged_clamp(a.n_free[0], 0, a.n_pages);
-    // pages that go back
-    long long mine[2] = {0, 0}, total_back, total, rows;
+    PagedAsk only = {0, 0, 0, 0, 0};
+    auto look = [&](int r) { return paged_ask(a.cached[r], a.added[r], a.held[r], page, a.columns); };
+    if (r0 < r1) only = look(r0);
+    auto ask = [&](int r) { return each == 1 ? only : look(r); };      // (of the thread's own requests)
+    // pages that go back, pages that are asked for, rows
+    unsigned mine[3] = {0, 0, 0};
     for (int r = r0; r < r1; ++r) {
         const PagedAsk q = ask(r);
-        mine[0] += q.held - q.keep;
-        mine[1] += q.want - q.keep;
+        mine[0] = sat(mine[0], (unsigned)(q.held - q.keep));
+        mine[1] = sat(mine[1], to_sum(q.want - q.keep));
+        mine[2] = sat(mine[2], (unsigned)q.added);
     }
-    long long before = sum_before(mine[0], of_wave, &total_back);
-    const int n_back = paged_clamp(total_back, 0, a.n_pages - had);
-    if (total_back > 0) {
+    Sums<3> sums = sums_before(mine, of_wave);
+    const int n_back = paged_clamp(sums.all[0], 0, a.n_pages - had), top = had + n_back;
+    if (n_back > 0) {
+        unsigned before = sums.before[0];
         for (int r = r0; r < r1; ++r) {
             const PagedAsk q = ask(r);
-            first[r] = paged_clamp(before, 0, 0x7fffffff);
-            before += q.held - q.keep;
+            first[r] = to_int(before);
+            before = sat(before, (unsigned)(q.held - q.keep));
         }
         __syncthreads();
         for (int i = tid; i < n_back; i += PT) {
             const int r = owner_of(first, n, i);
-            a.free_list[had + i] = a.table[(long long)r * a.columns + ask(r).keep + (i - first[r])];
+            a.free_list[had + i] = a.table[(long long)r * a.columns + look(r).keep + (i - first[r])];
         }
         __syncthreads();
     }
-    // pages that are asked for: to the requests whose needs, and those in front of them, the list can meet
-    const int top = had + n_back;
-    long long asked = sum_before(mine[1], of_wave, &total), added = 0, got = 0;
-    for (int r = r0; r < r1; ++r) added += a.added[r] > 0 ? a.added[r] : 0;
-    long long row = sum_before(added, of_wave, &rows);
-    {
-        long long need_to = asked, row_to = row;
-        for (int r = r0; r < r1; ++r) {
-            const PagedAsk q = ask(r);
-            need_to += q.want - q.keep;
-            row_to += q.added;
-            const bool granted = need_to <= top && q.want <= a.columns && row_to <= a.n_rows;
-            got += granted ? q.want - q.keep : 0;
-        }
-    }
-    long long given, at = sum_before(got, of_wave, &given);
+    // to the requests whose needs, and those in front of them, the list can meet
+    unsigned asked = sums.before[1], row = sums.before[2];
+    auto granted = [&](const PagedAsk& q) {       // (and moves on to the next request)
+        asked = sat(asked, to_sum(q.want - q.keep));
+        row = sat(row, (unsigned)q.added);
+        return asked <= (unsigned)top && q.want <= a.columns && row <= (unsigned)a.n_rows;
+    };
+    unsigned got[1] = {0};
     for (int r = r0; r < r1; ++r) {
         const PagedAsk q = ask(r);
-        asked += q.want - q.keep;
-        const long long row_to = row + q.added;
-        const bool granted = asked <= top && q.want <= a.columns && row_to <= a.n_rows;
-        first[r] = (int)at;           // at most `top`
-        at += granted ? q.want - q.keep : 0;
-        a.row_start[r] = paged_clamp(row, 0, 0x7fffffff);
+        if (granted(q)) got[0] += (unsigned)(q.want - q.keep);      // at most `top` in all
+    }
+    const Sums<1> given = sums_before(got, of_wave);
+    unsigned at = given.before[0];
+    asked = sums.before[1];
+    row = sums.before[2];
+    for (int r = r0; r < r1; ++r) {
+        const PagedAsk q = ask(r);
+        first[r] = (int)at;
+        a.row_start[r] = to_int(row);
+        const bool gets = granted(q);
+        if (gets) at += (unsigned)(q.want - q.keep);
         const long long kept = (long long)q.keep * page;
-        a.kv_len[r] = paged_clamp(granted ? q.cached + q.added : q.cached < kept ? q.cached : kept, 0, 0x7fffffff);
-        a.held[r] = granted ? (int)q.want : q.keep;
-        row = row_to;
+        a.kv_len[r] = paged_clamp(gets ? q.cached + q.added : q.cached < kept ? q.cached : kept, 0, 0x7fffffff);
+        a.held[r] = gets ? (int)q.want : q.keep;
     }
+    const int total = (int)given.all[0];
     if (tid == 0) {
-        a.row_start[n] = paged_clamp(rows, 0, 0x7fffffff);
-        a.n_free[0] = top - (int)given;
+        a.row_start[n] = to_int(sums.all[2]);
+        a.n_free[0] = top - total;
     }
-    __syncthreads();
-    for (int j = tid; j < (int)given; j += PT) {
-        const int r = owner_of(first, n, j), end = r + 1 < n ? first[r + 1] : (int)given;
-        a.table[(long long)r * a.columns + a.held[r] - (end - j)] = a.free_list[top - 1 - j];
+    if (total > 0) {
+        __syncthreads();
+        for (int j = tid; j < total; j += PT) {
+            const int r = owner_of(first, n, j), end = r + 1 < n ? first[r + 1] : total;
+            a.table[(long long)r * a.columns + a.held[r] - (end - j)] = a.free_list[top - 1 - j];
+        }
     }
     if (!rows_here) return;
     __syncthreads();
     for (int r = tid; r < n; r += PT) first[r] = a.row_start[r];
     __syncthreads();
-    for (int t = tid; t < a.n_rows; t += PT) place_row(a, first, paged_clamp(rows, 0, 0x7fffffff), t);
+    for (int t = tid; t < a.n_rows; t += PT) place_row(a, first, to_int(sums.all[2]), t);
 }
 
 // Positions and slots of many rows: as the plan's last part, by the whole chip.
@@ -150,29 +175,61 @@ __global__ void __launch_bounds__(256) paged_rows_kernel(const PagedPlanArgs a)
 
 // ---- writes ----
 //
-// A thread takes pieces of eight columns of a row; neighbouring threads neighbouring pieces, heads and rows.  What bounds it: HBM.
-template <class X, class Y> __global__ void __launch_bounds__(256) paged_write_kernel(const PagedWriteArgs a, const unsigned pieces)
+// A thread takes pieces of eight columns of a row, K and V, neighbouring threads neighbouring pieces, heads and rows; where there are many, four pieces each, all on the way at once.  Many rows
+// are more than the caches hold: loads and stores past them.  What bounds it: HBM, and the launch for a step's few rows.
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+template <int U> __device__ __forceinline__ u4 read(const u4* p) { return U > 1 ? __builtin_nontemporal_load(p) : *p; }
+template <int U> __device__ __forceinline__ void write(const u4& x, u4* p)
 {
-    const unsigned step = gridDim.x * 256;
-    for (unsigned i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += step) {
+    if constexpr (U > 1) __builtin_nontemporal_store(x, p);
+    else *p = x;
+}
+
+template <class X, class Y, int U> __global__ void __launch_bounds__(256) paged_write_kernel(const PagedWriteArgs a, const unsigned pieces)
+{
+    constexpr int NX = sizeof(X) / 2, NY = sizeof(Y) / 2;      // 16-byte words of a piece
+    const unsigned first = blockIdx.x * (256u * U) + threadIdx.x;
+    long long from[U], to[U];
+    u4 x[U][2][NX];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned i = first + 256u * u;
+        to[u] = -1;
+        if (i >= pieces) continue;
         const unsigned row = a.by_row(i), in_row = i - row * a.by_row.d, h = a.by_head(in_row);
         const int c = 8 * (int)(in_row - h * a.by_head.d), slot = a.slot[row];
+        from[u] = row * a.x_stride_tok + h * a.x_stride_head + c;
         if (slot < 0 || slot >= a.n_slots) continue;
         const unsigned p = a.by_page((unsigned)slot);
-        const long long from = row * a.x_stride_tok + h * a.x_stride_head + c, to = p * a.stride_page + h * a.stride_head + (slot - p * a.by_page.d) * a.stride_tok + c;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const X* x = static_cast<const X*>(a.x[t]) + from;
-            Y* y = static_cast<Y*>(a.y[t]) + to;
-            if constexpr (sizeof(X) == sizeof(Y)) {
-#pragma unroll
-                for (int e = 0; e < (int)sizeof(X) / 2; ++e) reinterpret_cast<uint4*>(y)[e] = reinterpret_cast<const uint4*>(x)[e];
-            } else {
-                const float4 lo = reinterpret_cast<const float4*>(x)[0], hi = reinterpret_cast<const float4*>(x)[1];
-                *reinterpret_cast<bf16x8*>(y) = pack_bf16x8(lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w);
-            }
-        }
+        to[u] = p * a.stride_page + h * a.stride_head + (slot - p * a.by_page.d) * a.stride_tok + c;
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (to[u] >= 0)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < NX; ++e) x[u][t][e] = read<U>(reinterpret_cast<const u4*>(static_cast<const X*>(a.x[t]) + from[u]) + e);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (to[u] >= 0)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                u4* const y = reinterpret_cast<u4*>(static_cast<Y*>(a.y[t]) + to[u]);
+                if constexpr (NX == NY) {
+#pragma unroll
+                    for (int e = 0; e < NX; ++e) write<U>(x[u][t][e], y + e);
+                } else {
+                    const f32x4 lo = __builtin_bit_cast(f32x4, x[u][t][0]), hi = __builtin_bit_cast(f32x4, x[u][t][1]);
+                    write<U>(__builtin_bit_cast(u4, pack_bf16x8(lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3])), y);
+                }
+            }
+}
+
+template <class X, class Y> void launch_write(const PagedWriteArgs& a, unsigned pieces, hipStream_t s)
+{
+    if (pieces <= 1u << 17) paged_write_kernel<X, Y, 1><<<(pieces + 255) / 256, 256, 0, s>>>(a, pieces);      // two workgroups a CU
+    else paged_write_kernel<X, Y, 4><<<(pieces + 1023) / 1024, 256, 0, s>>>(a, pieces);
 }
 
 }  // namespace
@@ -193,9 +250,8 @@ hipError_t hexi_launch_paged_write(const PagedWriteArgs& a, int x_dtype, int y_d
 {
     const unsigned pieces = (unsigned)(a.n_rows * a.n_heads * (a.d / 8));      // below 2^31
     if (pieces == 0) return hipSuccess;
-    const unsigned all = (pieces + 255) / 256, grid = all < 4096u ? all : 4096u;
-    if (y_dtype == HEXI_F32) paged_write_kernel<float, float><<<grid, 256, 0, s>>>(a, pieces);
-    else if (x_dtype == HEXI_F32) paged_write_kernel<float, uint16_t><<<grid, 256, 0, s>>>(a, pieces);
-    else paged_write_kernel<uint16_t, uint16_t><<<grid, 256, 0, s>>>(a, pieces);
+    if (y_dtype == HEXI_F32) launch_write<float, float>(a, pieces, s);
+    else if (x_dtype == HEXI_F32) launch_write<float, uint16_t>(a, pieces, s);
+    else launch_write<uint16_t, uint16_t>(a, pieces, s);
     return hipGetLastError();
 }

@@ -472,6 +472,16 @@ def hexi_rope(rope, segs, tensors, positions=None, inverse=False, stream=None):
         _check(rc)
 
 
+def _device_and_stream(stream):
+    """_current_device() and _stream() at once."""
+    if _torch is None:
+        _types()
+    if not _torch.cuda.is_initialized():
+        return -2, 0
+    dev = _torch._C._cuda_getDevice()
+    return dev, _torch._C._cuda_getCurrentRawStream(dev) if stream is None else int(stream)
+
+
 def make_paged_cache(cache):
     """Descriptor of a paged cache from its tensor of keys (or values), [pages, kv heads, tokens of a page, head_dim] with contiguous columns; of one that is laid out token by
     token the view whose axes 1 and 2 are swapped."""
@@ -510,14 +520,27 @@ def _ints(dev, *named):
 def hexi_paged_plan(page, cached, added, table, held, free_list, n_free, row_start, kv_len, pos, slot, stream=None):
     """Pages for the requests' lengths and the places of their new rows; all int32 tensors on the device: cached, added, held, kv_len [requests], table [requests, columns],
     free_list [pages], n_free [1], row_start [requests + 1], pos, slot [rows]."""
-    dev, shape = _current_device(), table.shape
+    (dev, handle), shape = _device_and_stream(stream), table.shape
     if len(shape) != 2:
         _refuse(f"table {tuple(shape)}: two axes are needed")
     r, columns = shape
     pages, rows = free_list.numel(), slot.numel()
-    a = _ints(dev, ("cached", cached, r), ("added", added, r), ("table", table, r * columns), ("held", held, r), ("free_list", free_list, pages), ("n_free", n_free, 1),
+    i32 = _int32
+    # (written out: a loop over the ten costs as much as the checks)
+    if (cached.dtype is not i32 or cached.numel() != r or cached.get_device() != dev or not cached.is_contiguous()
+            or added.dtype is not i32 or added.numel() != r or added.get_device() != dev or not added.is_contiguous()
+            or table.dtype is not i32 or table.get_device() != dev or not table.is_contiguous()
+            or held.dtype is not i32 or held.numel() != r or held.get_device() != dev or not held.is_contiguous()
+            or free_list.dtype is not i32 or free_list.get_device() != dev or not free_list.is_contiguous()
+            or n_free.dtype is not i32 or n_free.numel() != 1 or n_free.get_device() != dev
+            or row_start.dtype is not i32 or row_start.numel() != r + 1 or row_start.get_device() != dev or not row_start.is_contiguous()
+            or kv_len.dtype is not i32 or kv_len.numel() != r or kv_len.get_device() != dev or not kv_len.is_contiguous()
+            or pos.dtype is not i32 or pos.numel() != rows or pos.get_device() != dev or not pos.is_contiguous()
+            or slot.dtype is not i32 or slot.get_device() != dev or not slot.is_contiguous()):
+        _ints(dev, ("cached", cached, r), ("added", added, r), ("table", table, r * columns), ("held", held, r), ("free_list", free_list, pages), ("n_free", n_free, 1),
               ("row_start", row_start, r + 1), ("kv_len", kv_len, r), ("pos", pos, rows), ("slot", slot, rows))
-    rc = (_lib or load()).hexi_paged_plan(page, pages, r, a[0], a[1], a[2], columns, a[3], a[4], a[5], a[6], a[7], rows, a[8], a[9], _stream(stream))
+    rc = (_lib or load()).hexi_paged_plan(page, pages, r, cached.data_ptr(), added.data_ptr(), table.data_ptr(), columns, held.data_ptr(), free_list.data_ptr(), n_free.data_ptr(),
+                                          row_start.data_ptr(), kv_len.data_ptr(), rows, pos.data_ptr(), slot.data_ptr(), handle)
     if rc:
         _check(rc)
 
@@ -537,17 +560,19 @@ def _caches(c, dev, k, v):
 
 def hexi_paged_write(cache, slot, k, v, k_cache, v_cache, stream=None):
     """Writes k and v [rows, kv heads, head_dim] (one type, one pair of strides) into their slots (int32 [rows]; -1: left out).  cache: that of make_paged_cache."""
-    dev, shape, strides = _current_device(), k.shape, k.stride()
-    if len(shape) != 3 or shape[1] != cache.n_kv_heads or shape[2] != cache.head_dim or v.shape != shape or v.dtype is not k.dtype or strides[2] != 1 or v.stride(2) != 1:
-        _refuse(f"k, v: [rows, {cache.n_kv_heads}, {cache.head_dim}] of one type with contiguous columns are needed, not {tuple(shape)} {k.dtype}, {tuple(v.shape)} {v.dtype}")
+    (dev, handle), shape, strides, heads, d = _device_and_stream(stream), k.shape, k.stride(), cache.n_kv_heads, cache.head_dim
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d or v.shape != shape or v.dtype is not k.dtype or strides[2] != 1 or v.stride(2) != 1:
+        _refuse(f"k, v: [rows, {heads}, {d}] of one type with contiguous columns are needed, not {tuple(shape)} {k.dtype}, {tuple(v.shape)} {v.dtype}")
     rows = shape[0]
-    tok, head = strides[:2] if rows > 1 and shape[1] > 1 else _q_strides(k)
+    tok, head = strides[:2] if rows > 1 and heads > 1 else _q_strides(k)
     if v.stride() != strides and _q_strides(v) != (tok, head):
         _refuse(f"k and v differ in their strides: {strides}, {v.stride()}")
     if k.get_device() != dev or v.get_device() != dev:
         _refuse(f"k or v is on {k.device} or {v.device}, not on the current GPU")
     kc, vc = _caches(cache, dev, k_cache, v_cache)
-    rc = (_lib or load()).hexi_paged_write(cache, _ints(dev, ("slot", slot, rows))[0], rows, k.data_ptr(), v.data_ptr(), _dtype(k), tok, head, kc, vc, _stream(stream))
+    if slot.dtype is not _int32 or slot.numel() != rows or slot.get_device() != dev or not slot.is_contiguous():
+        _ints(dev, ("slot", slot, rows))
+    rc = (_lib or load()).hexi_paged_write(cache, slot.data_ptr(), rows, k.data_ptr(), v.data_ptr(), _dtype(k), tok, head, kc, vc, handle)
     if rc:
         _check(rc)
 
@@ -560,7 +585,7 @@ def hexi_paged_attn(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, 
     """Attention of the requests' new rows, q [rows, q heads, head_dim], over their cached keys.  table [requests, columns], row_start [requests + 1], kv_len, q_start, kv_start
     [requests]: int32 on the device; o's element type (fp32 or bf16) is the result's.  max_rows: no request has more rows (0: not known).  workspace: a tensor of at least
     hexi_paged_attn_workspace_bytes, not shared with a call that may run at the same time; None takes one from torch for the call."""
-    dev, shape, columns = _current_device(), q.shape, table.shape
+    (dev, handle), shape, columns = _device_and_stream(stream), q.shape, table.shape
     rows, nq, d = desc_shape = (shape[0] if shape else 0, desc.n_q_heads, desc.head_dim)
     strides = q.stride()
     if shape != desc_shape or _dtype(q) != desc.dtype or strides != (desc.q_stride_tok, desc.q_stride_head, 1) and any(
@@ -578,8 +603,7 @@ def hexi_paged_attn(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, 
     kc, vc = _caches(cache, dev, k_cache, v_cache)
     a = _ints(dev, ("table", table, r * columns), ("row_start", row_start, r + 1), ("kv_len", kv_len, r))
     qs, ks = (None if t is None else _ints(dev, (name, t, r))[0] for name, t in (("q_start", q_start), ("kv_start", kv_start))) if q_start is not None or kv_start is not None else (None, None)
-    lib, handle = _lib or load(), _stream(stream)
-    taken = None
+    lib, taken = _lib or load(), None
     if workspace is not None:
         space, ws_bytes = workspace.data_ptr(), _bytes_of(workspace, dev)
     else:
