@@ -1,0 +1,40 @@
+"""Serving steps over a paged cache on one GPU: plan, rotation, writes and attention of one layer, as a program runs them.
+
+PagedRun owns the buffers and the sequence of the library's calls; all arithmetic is in the library's kernels.  What changes from step to step (lengths, new rows) lies in device
+tensors, so `step` can be captured once and replayed.
+"""
+import torch
+
+from . import hexi
+
+
+class PagedRun:
+    """One layer's share on one device: `requests` slots for requests, a cache of `n_pages` pages, up to `rows` new rows a step.
+
+    A step reads cached, added (int32 [requests]: tokens that stay, new ones) and the first rows of q [rows, nq, d], k, v [rows, nkv, d]; q and k are rotated in place where `rope` is given.  It
+    leaves o and lse of the rows, kv_len (below cached + added where a request got no pages) and the state of the pages."""
+
+    def __init__(self, requests, rows, n_pages, page, columns, nq, nkv, head_dim, dtype=torch.bfloat16, max_rows=0, rope=None, window=None, kv_of_q=None, device="cuda:0"):
+        self.page, self.rope, self.window, self.max_rows = page, rope, window, max_rows
+        ints = dict(dtype=torch.int32, device=device)
+        self.cached, self.added, self.held, self.kv_len = (torch.zeros(requests, **ints) for _ in range(4))
+        self.table, self.row_start = torch.zeros(requests, columns, **ints), torch.zeros(requests + 1, **ints)
+        self.free, self.n_free = torch.arange(n_pages, **ints), torch.full((1,), n_pages, **ints)
+        self.pos, self.slot = torch.zeros(rows, **ints), torch.zeros(rows, **ints)
+        self.q = torch.zeros(rows, nq, head_dim, dtype=dtype, device=device)
+        self.k, self.v = (torch.zeros(rows, nkv, head_dim, dtype=dtype, device=device) for _ in range(2))
+        self.k_cache, self.v_cache = (torch.zeros(n_pages, nkv, page, head_dim, dtype=dtype, device=device) for _ in range(2))
+        self.o, self.lse = torch.zeros_like(self.q), torch.zeros(nq, rows, device=device)
+        self.rows = hexi.make_range([(0, rows)])[0]
+        self.cache = hexi.make_paged_cache(self.k_cache)
+        self.desc = hexi.paged_desc_for(self.q, self.k_cache, head_dim ** -0.5, kv_of_q)
+        n = hexi.hexi_paged_attn_workspace_bytes(self.desc, self.cache, requests, columns, rows, max_rows)
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+
+    def step(self, stream=None):
+        hexi.hexi_paged_plan(self.page, self.cached, self.added, self.table, self.held, self.free, self.n_free, self.row_start, self.kv_len, self.pos, self.slot, stream=stream)
+        if self.rope is not None:
+            hexi.hexi_rope(self.rope, self.rows, [(self.q, self.q), (self.k, self.k)], positions=self.pos.view(1, -1), stream=stream)
+        hexi.hexi_paged_write(self.cache, self.slot, self.k, self.v, self.k_cache, self.v_cache, stream=stream)
+        hexi.hexi_paged_attn(self.desc, self.cache, self.table, self.row_start, self.kv_len, self.q, self.k_cache, self.v_cache, self.o, self.lse, max_rows=self.max_rows, window=self.window,
+                             workspace=self.workspace, stream=stream)

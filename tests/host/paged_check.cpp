@@ -2,6 +2,7 @@
 //   request page columns n_rows max_rows window n_sink row_start row_end kv_len has_q_start q_start kv_start   -> row0 rows kv, then sink:lo:hi of every row (of the first 40 and the last)
 //   place page columns n_pages key entry ...                                                     -> page id and row of a key
 //   ask page columns cached added held                                                           -> cached added want held keep
+//   cost most shift start coarse at rows kv window -> tiles, then before(t) of t = 0 .. tiles (of at most 200), and the tiles that these costs lie in
 //   runs nq nkv kv_of_q ...                                                                      -> "kvh:head,head" of every run, and the most heads of one
 #include <cstdio>
 #include <cstring>
@@ -43,6 +44,17 @@ int main()
             if (std::scanf("%d %d %d %d %d", &page, &g.columns, &cached, &added, &held) != 5) return 1;
             const PagedAsk a = paged_ask(cached, added, held, page, g.columns);
             std::printf("%lld %lld %lld %d %d\n", a.cached, a.added, a.want, a.held, a.keep);
+        } else if (!std::strcmp(what, "cost")) {
+            PagedShare sh = {0, 0, 1, 1, 0, 1, 0};
+            PagedRequest q = {0, 0, 0, 0, 0};
+            if (std::scanf("%d %d %d %d %lld %d %d %d", &g.most, &sh.shift, &sh.start, &sh.coarse, &q.at, &q.rows, &q.kv, &g.window) != 8) return 1;
+            g.per_block = 1.0 / (64.0 * g.most);
+            const int tiles = paged_tiles(g, sh, q);
+            const PagedCost c(g, sh, q, tiles);
+            std::printf("%d", tiles);
+            for (int t = 0; t <= tiles && t <= 200; ++t) std::printf(" %d", c.before(t));
+            for (int t = 0; t < tiles && t < 200; ++t) std::printf(" %d %d", c.tile_of(c.before(t), tiles), c.tile_of(c.before(t + 1) - 1, tiles));
+            std::printf("\n");
         } else {
             int nq, nkv;
             signed char kv_of_q[HEXI_MAX_HEADS];

@@ -1,0 +1,210 @@
+"""Plan, rotation, writes and paged attention run together, as a serving program runs them: steps of prompts and tokens, captured and replayed, on several streams, over several devices' parts of a context."""
+import ctypes
+import random
+
+import pytest
+import torch
+
+import paged_util as pu
+from paged_util import BF16, DEV, F32, Case, Setup, ints
+from paper_2605_07569_amd import hexi
+from paper_2605_07569_amd.paged import PagedRun
+from test_gpu_rope import freqs, turned
+
+pytestmark = pytest.mark.gpu
+
+
+class Program:
+    """Requests that come, grow, lose speculated tokens, wait for pages and end; what every step should give, from the tokens' own keys and values."""
+
+    def __init__(self, dtype, d, requests=5, rows=300, n_pages=60, page=16, columns=40, nq=6, nkv=2, seed=1, window=None, max_rows=0):
+        self.freq, self.axis = freqs(d, 1)
+        self.nq, self.nkv, self.d, self.dtype, self.window, self.rows = nq, nkv, d, dtype, window, rows
+        self.run = PagedRun(requests, rows, n_pages, page, columns, nq, nkv, d, dtype, max_rows=max_rows, rope=hexi.make_rope(d, self.freq, self.axis, n_axes=1),
+                            window=hexi.make_window(*window) if window else None)
+        for t in (self.run.k_cache, self.run.v_cache):
+            t.fill_(float("nan"))          # (what no token has been written to)
+        self.pool = pu.Pool(page, n_pages, requests, columns)
+        self.run.free.copy_(ints(self.pool.free))
+        self.keys = [torch.zeros(0, nkv, d) for _ in range(requests)]      # rotated keys and values of every request's tokens, as the cache holds them
+        self.values = [torch.zeros(0, nkv, d) for _ in range(requests)]
+        self.gen = torch.Generator().manual_seed(seed)
+
+    def inputs(self, cached, added):
+        """New rows into the run's buffers."""
+        total = sum(added)
+        assert total <= self.rows
+        self.cached_now, self.added_now = cached, added
+        self.new = [torch.randn(total, h, self.d, generator=self.gen).to(self.dtype) for h in (self.nq, self.nkv, self.nkv)]
+        for t, x in zip((self.run.q, self.run.k, self.run.v), self.new):
+            t[:total].copy_(x)
+        self.run.cached.copy_(ints(cached))
+        self.run.added.copy_(ints(added))
+
+    def check(self, rel=None):
+        """The step's results against the definition; returns the lengths after it."""
+        run, cached, added = self.run, self.cached_now, self.added_now
+        torch.cuda.synchronize()
+        row_start, kv_len, pos, slot = self.pool.step(cached, added, self.rows)
+        assert [run.row_start.tolist(), run.kv_len.tolist(), run.pos.tolist(), run.slot.tolist()] == [row_start, kv_len, pos, slot]
+        assert run.held.tolist() == self.pool.held and int(run.n_free) == self.pool.n_free
+        total = sum(added)
+        q, _ = turned(self.new[0].double(), torch.tensor([pos[:total]]), self.freq, self.axis, False, False) if total else (self.new[0].double(), None)
+        k, _ = turned(self.new[1].double(), torch.tensor([pos[:total]]), self.freq, self.axis, False, False) if total else (self.new[1].double(), None)
+        errs, norms = 0.0, 0.0
+        for r, (a, b) in enumerate(zip(row_start, row_start[1:])):
+            self.keys[r], self.values[r] = self.keys[r][:cached[r]], self.values[r][:cached[r]]
+            if kv_len[r] < cached[r] + added[r]:
+                continue                  # no pages: the request is asked for again
+            self.keys[r] = torch.cat([self.keys[r].double(), k[a:b]])
+            self.values[r] = torch.cat([self.values[r].double(), self.new[2][a:b].double()])
+            if a == b:
+                continue
+            p, j = torch.arange(cached[r], cached[r] + added[r])[:, None], torch.arange(kv_len[r])[None]
+            seen = j <= p
+            if self.window:
+                seen &= (p - j < self.window[0]) | (j < self.window[1])
+            for h in range(self.nq):
+                g = h // (self.nq // self.nkv)
+                s = (q[a:b, h] @ self.keys[r][:, g].T * self.d ** -0.5).masked_fill(~seen, float("-inf"))
+                want = torch.softmax(s, 1) @ self.values[r][:, g]
+                errs += float((run.o[a:b, h].double().cpu() - want).pow(2).sum())
+                norms += float(want.pow(2).sum())
+                assert (run.lse[h, a:b].double().cpu() - torch.logsumexp(s, 1)).abs().max() < (0.05 if self.dtype == BF16 else 1e-4)
+        # rotated q and k are rounded once (bf16: 2^-8 / sqrt(12) of each element's rms at worst, both of them in a score of about 1: 2e-3 of P), then as for attention alone (under 5e-3)
+        if norms:
+            assert (errs / norms) ** 0.5 <= (rel or (7e-3 if self.dtype == BF16 else 1e-5))
+        return kv_len
+
+
+def _lengths(rng, cached, rows, columns_tokens):
+    """A step's lengths: tokens for most, prompts for those that have ended, some tokens dropped."""
+    cached, added, left = list(cached), [], rows
+    for r in range(len(cached)):
+        x = rng.random()
+        n = 1
+        if cached[r] == 0:
+            n = rng.randint(1, 130)
+        elif x < 0.1:
+            cached[r], n = 0, 0
+        elif x < 0.2:
+            cached[r], n = max(1, cached[r] - rng.randint(0, 20)), rng.randint(1, 6)
+        elif x < 0.3:
+            n = 0
+        n = min(n, left, columns_tokens - cached[r])
+        added.append(n)
+        left -= n
+    return cached, added
+
+
+@pytest.mark.parametrize("dtype,d,kw", [(BF16, 128, {}), (F32, 64, dict(nq=4, nkv=4)), (BF16, 64, dict(window=(50, 3), page=32, n_pages=30, columns=20)),
+                                        (BF16, 128, dict(n_pages=20, requests=9, nq=16, nkv=2))], ids=str)      # (the last: often too few pages)
+def test_steps_of_a_serving_program(dtype, d, kw):
+    p = Program(dtype, d, **kw)
+    rng, cached = random.Random(7), [0] * len(p.keys)
+    denied = 0
+    for _ in range(10):
+        lengths = _lengths(rng, cached, p.rows, p.pool.columns * p.pool.page)
+        p.inputs(*lengths)
+        p.run.step()
+        cached = p.check()
+        denied += sum(a > 0 and k < c + a for c, a, k in zip(*lengths, cached))
+    assert (denied > 0) == (kw.get("n_pages") == 20)
+
+
+def test_steps_captured_once_and_replayed():
+    """The graph of a step with room for 40 rows, replayed while lengths change, between eager steps of another program."""
+    p, other = Program(BF16, 128, requests=7, rows=40), Program(F32, 64, requests=3, rows=200, seed=3)
+    rng, cached, theirs = random.Random(9), [0] * 7, [0] * 3
+    p.inputs([0] * 7, [0] * 7)
+    p.run.step()
+    p.check()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.run.step()
+    for _ in range(8):
+        lengths = _lengths(rng, cached, 40, 600)
+        p.inputs(*lengths)
+        graph.replay()
+        cached = p.check()
+        other.inputs(*_lengths(rng, theirs, 200, 600))
+        other.run.step()
+        theirs = other.check()
+
+
+def test_two_graphs_and_an_eager_step_at_once_on_streams_of_their_own():
+    programs = [Program(BF16, 64, rows=60, seed=s, requests=4) for s in range(3)]
+    streams, graphs = [torch.cuda.Stream() for _ in range(3)], []
+    for p in programs[:2]:
+        p.inputs([0] * 4, [0] * 4)
+        p.run.step()
+        p.check()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            p.run.step()
+        graphs.append(g)
+    rng, cached = random.Random(3), [[0] * 4 for _ in range(3)]
+    for _ in range(5):
+        for i, p in enumerate(programs):
+            p.inputs(*_lengths(rng, cached[i], 60, 600))
+        torch.cuda.synchronize()
+        for i, (p, s) in enumerate(zip(programs, streams)):
+            if i < 2:
+                with torch.cuda.stream(s):
+                    graphs[i].replay()
+            else:
+                p.run.step(stream=s.cuda_stream)
+        torch.cuda.synchronize()
+        cached = [p.check() for p in programs]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+@pytest.mark.parametrize("rows", [1, 70])
+def test_a_context_spread_over_devices(dtype, rows):
+    """Each device attends to its part of the keys; joined through their LSE the parts are the whole."""
+    total, cuts, nq, nkv, d = 1000, [0, 300, 640, 1000], 4, 2, 64
+    g = torch.Generator().manual_seed(5)
+    q = torch.randn(rows, nq, d, generator=g).to(dtype).to(DEV)
+    k, v = (torch.randn(total, nkv, d, generator=g).to(dtype) for _ in range(2))
+    o, lse = torch.zeros(rows, nq, d, device=DEV), torch.full((nq, rows), float("-inf"), device=DEV)
+    for a, b in zip(cuts, cuts[1:]):
+        s = Setup(Case("part", [(b - a, rows)], nq=nq, nkv=nkv, q_start=[total - rows], kv_start=[a], window=500, n_sink=7), dtype, d)
+        for i in range(b - a):
+            page, row = int(s.table[0, i // 16]), i % 16
+            s.k_cache[page, :, row], s.v_cache[page, :, row] = k[a + i].to(DEV), v[a + i].to(DEV)
+        s.q = q
+        part = s.run(F32)
+        hexi.hexi_attn_merge_lse(o, lse, *part)
+    torch.cuda.synchronize()
+    p, j = torch.arange(rows)[:, None] + total - rows, torch.arange(total)[None]
+    seen = (j <= p) & ((p - j < 500) | (j < 7))
+    for h in range(nq):
+        sc = (q[:, h].double().cpu() @ k[:, h // 2].double().T * d ** -0.5).masked_fill(~seen, float("-inf"))
+        want = torch.softmax(sc, 1) @ v[:, h // 2].double()
+        # fp32 results of bf16 inputs have weights of 16 bits: 2^-16 of them at most, spread evenly
+        assert (o[:, h].double().cpu() - want).norm() / want.norm() < 1e-5
+        assert (lse[h].double().cpu() - torch.logsumexp(sc, 1)).abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
+def test_workspaces_that_are_not_given(dtype):
+    """Taken from torch for the call, on its current stream and on one given by hand; a capture that torch does not know of is refused."""
+    s = Setup(Case("ws", [(3000, 1), (40, 40)], nq=4, nkv=2), dtype, 64)
+    want = s.run()
+    torch.cuda.synchronize()
+    side, bufs = torch.cuda.Stream(), [s.out() for _ in range(3)]
+    torch.cuda.synchronize()
+    s.run(bufs=bufs[0], workspace=None)
+    s.run(bufs=bufs[1], workspace=None, stream=side.cuda_stream)
+    with torch.cuda.stream(side):
+        s.run(bufs=bufs[2], workspace=None)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for buf in bufs for a, b in zip(buf, want))
+    lib, graph, handle = hexi.load(), ctypes.c_void_p(), ctypes.c_void_p(side.cuda_stream)
+    assert lib.hipStreamBeginCapture(handle, 1) == 0
+    with pytest.raises(hexi.HexiError) as e:
+        s.run(bufs=bufs[0], workspace=None, stream=side.cuda_stream)
+    assert lib.hipStreamEndCapture(handle, ctypes.byref(graph)) == 0
+    assert e.value.code == hexi.HEXI_EWORKSPACE and lib.hipGraphDestroy(graph) == 0

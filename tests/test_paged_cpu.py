@@ -92,6 +92,30 @@ def test_head_runs(ask):
         assert ask([f"runs {nq} {nkv} " + " ".join(map(str, heads))])[0].split() == runs + [str(max(heads.count(k) for k in heads))]
 
 
+def test_costs_of_tiles_are_sums_and_lead_back_to_their_tiles(ask):
+    rng = random.Random(6)
+    asked = []
+    for _ in range(300):
+        most, shift = rng.choice([1, 3, 5, 8, 128]), rng.choice([4, 5, 8])
+        kv, rows = rng.choice([0, 1, 63, 64, 65, rng.randint(0, 5000), 2 ** 28]), rng.choice([1, 2, rng.randint(1, 3000)])
+        at = rng.choice([kv - rows, kv - rows, rng.randint(-2 * rows, 6000), -2 ** 31, 2 ** 32 - 1])
+        start, coarse = rng.randint(1, 6), rng.choice([0, 0, 1, 5])
+        while (rows * most // 2 ** shift + 1) * ((kv // 64 + 2 >> coarse) + 1 + start) > 1e9:      # (as a launch chooses it)
+            coarse += 1
+        asked.append((most, shift, start, coarse, at, rows, kv, rng.choice([TOP, TOP, 1, 17, 64, 500])))
+    for (most, shift, start, coarse, at, rows, kv, window), line in zip(asked, ask(["cost " + " ".join(map(str, a)) for a in asked])):
+        tiles, *x = map(int, line.split())
+        assert tiles == -(-rows * most // 2 ** shift)
+        n = min(tiles, 200)
+        before, back = x[:n + 1], x[n + 1:]
+        seen = [_clamp(most * at + (t + 1) * 2 ** shift, 0, most * kv) - _clamp(most * (at + 1 - window) + t * 2 ** shift, 0, most * kv) for t in range(n)]
+        for t in range(n + 1):
+            want = sum(seen[:t]) / (64 * most * 2 ** coarse) + t * start
+            assert want - 1.001 <= before[t] <= want + 0.001, (most, shift, at, rows, kv, window, t)
+        assert all(b - a >= start for a, b in zip(before, before[1:]))
+        assert back == [t for t in range(n) for _ in range(2)]
+
+
 def _codes(call, bad):
     for code, changes in bad:
         assert call(**changes) == code, (changes, hexi.hexi_last_error())
