@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_f
     struct Ring { unsigned char k[AHEAD][R::TILE], v[AHEAD][R::TILE]; };
     __shared__ __attribute__((aligned(1024))) union { Ring ring[NW]; Ends ends; } sm;
     __shared__ typename PagedWalk<64 * NW>::Shared shared;
+    paged_touch();
     const PagedGeom& g = a.g;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = lane >> 4, l16 = lane & 15;

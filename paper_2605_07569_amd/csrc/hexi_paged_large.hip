@@ -43,6 +43,7 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
     constexpr bool PAIR_BARRIER = D == 128;     // one workgroup barrier per pair of phases instead of one per phase
     __shared__ __attribute__((aligned(1024))) Smem<D> sm;
     __shared__ typename PagedWalk<512>::Shared shared;
+    paged_touch();
     const PagedGeom& g = a.g;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = wave >> 2, wg = wave & 3;

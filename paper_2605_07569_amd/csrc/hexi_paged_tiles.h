@@ -28,6 +28,15 @@ __device__ __forceinline__ const PagedArgs& paged_args()
     return *(const PagedArgs*)p;
 }
 
+// Asks for all of the arguments' lines at once, before the first of them is waited for.  (Read one behind the other they cost 0.7 us more: 107.0 us against 106.3 for a verifying batch, 32.4 against 31.7 for a small one of fp32.)
+__device__ __forceinline__ void paged_touch()
+{
+    typedef const __attribute__((address_space(4))) int* Ptr;
+    const Ptr p = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    static_assert(sizeof(PagedArgs) > 10 * 64 && sizeof(PagedArgs) <= 11 * 64, "eleven lines");
+    asm volatile("" ::"s"(p[0]), "s"(p[16]), "s"(p[32]), "s"(p[48]), "s"(p[64]), "s"(p[80]), "s"(p[96]), "s"(p[112]), "s"(p[128]), "s"(p[144]), "s"(p[160]));
+}
+
 struct Tile {
     PagedRequest q;
     WinSpan<PAGED_KEYS> span;           // blocks that its rows see
