@@ -200,23 +200,27 @@ struct PagedArgs {
 // Blocks of a wavefront's ring in the kernel for few vectors, 16 rows of K and V each: two, or four where rows are short, so that two workgroups fit a CU (one of fp32 with 128 columns).
 constexpr int paged_ring(size_t bytes, int d) { return (int)bytes * d <= 128 ? 4 : 2; }
 
-// How a call is launched: by the kernel for few vectors to a key, by the one for many, or by both, each with the requests that it is for.
+// How a call is launched: by the kernel for few vectors to a key, by the one for many, or by both, each with the requests that it is for; a further launch joins the tiles that are cut (whether any is, the costs say, which the host does not know).
 struct PagedShape {
     PagedShare share[2];
     int ranges[2];            // workgroups, multiples of 8; 0: the kernel is not launched
     int entries[2];           // tiles there may be, no more than ranges
-    bool splits;              // a tile can be cut: a further launch joins
 };
 inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
 {
     PagedShape s;
-    const bool large = dtype == HEXI_BF16 && max_rows * most > 32;
+    // Large tiles have a long way in and out, and launch beside them what is for few vectors; they read keys once for 256 vectors where others read them for 32.  (8 requests of up to 4K keys, 32 / 8 heads
+    // x 128: up to 64 vectors each 57.7 us large, 37.6 not, up to 128 53.9 and 43.3; 24 of 16K 241 and 252, 270 and 362.  64 columns: 128 vectors 43.4 and 33.3, 202 and 177; 256 vectors 45.9 and 44.7, 216 and 290.)
+    const bool large = dtype == HEXI_BF16 && max_rows * most > (d == 64 ? 128 : 64);
     const bool few = !large || n_requests > 1;
-    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 1, 2, 0};
+    // A tile's start costs about what four blocks do (64 requests of 1K, one token each: 50.0 us with 1, 42.9 with 4, 44.7 with 8).  Ranges of few vectors may be as short as there are workgroups for them (one request
+    // of 2K: 11.5 us, 13.5 with two blocks at least); shorter large ones than six gain nothing (512 tokens over 4K: 68.9 us with 3, 6 and 12, 72.0 with 24).
+    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 4, 1, 0};
     s.share[1] = PagedShare{8, 16, !few, 1, 4, 6, 0};
     const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
     for (int i = 0; i < 2; ++i) {
         PagedShare& h = s.share[i];
+        // as many workgroups as run at once: one to a CU where the LDS is full, else two (24 requests of 16K, 128 columns: decoding 164 us with 256, 162 with 512, verifying 163 and 166; 64 columns: 96 and 92, 115 and 96)
         const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests), full = i == 1 || (dtype == HEXI_F32 && d == 128) ? 256 : 512;      // (below 2^31: rows x heads are at most 2^28)
         while ((double)tiles * (double)((blocks >> h.coarse) + 1 + h.start) > 1e9) ++h.coarse;
         long long n = tiles > full ? full : tiles * (blocks + h.start) / h.min_cost + 1;
@@ -224,7 +228,6 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
         s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;
         s.entries[i] = (int)(tiles < s.ranges[i] ? tiles : s.ranges[i]);
     }
-    s.splits = blocks > 2;
     return s;
 }
 inline size_t hexi_paged_workspace(const PagedShape& s, int i, int d)      // of one kernel

@@ -9,7 +9,8 @@ namespace {
 // Sums over the requests in front (pages that go back, pages that are asked for, rows) say where everything goes, so one workgroup forms them, a few requests to a thread,
 // and the flat lists of pages and rows are then shared out over all threads, each of which finds its request by halving.
 // What bounds it: latency, of the reads that follow each other (lengths, then pages, then the free list) and of the barriers between them; so three sums are formed at once, by lane shifts, and
-// lengths are read once where a thread has one request.
+// lengths are read once where a thread has one request.  A step of 64 requests takes 3.1 us.  Positions and slots of up to 2048 rows are its own last part, of more a launch over the whole chip
+// (256 requests: 2K rows 5.7 us, 6.8 as a second launch; 4K rows 7.1 and 6.8; 16K rows 15.1 and 6.9).
 
 constexpr int PT = 1024;      // threads
 
@@ -175,8 +176,9 @@ __global__ void __launch_bounds__(256) paged_rows_kernel(const PagedPlanArgs a)
 
 // ---- writes ----
 //
-// A thread takes pieces of eight columns of a row, K and V, neighbouring threads neighbouring pieces, heads and rows; where there are many, four pieces each, all on the way at once.  Many rows
-// are more than the caches hold: loads and stores past them.  What bounds it: HBM, and the launch for a step's few rows.
+// A thread takes pieces of eight columns of a row, K and V, neighbouring threads neighbouring pieces, heads and rows.  What bounds it: HBM, and the launch for a step's few rows.  Many rows of
+// bf16 are more than the L2 caches hold: loads and stores past them, four pieces to a thread, all on the way at once (8 heads x 128: 16K rows 26.4 us, 5.1 TB/s, against 29.4 with one piece; 4K rows 7.5 and 7.8,
+// 2K rows 6.0 and 4.7).  To fp32 caches it does not pay (16K rows 57.7 and 57.4 us, 4.7 TB/s; 4K 16.3 and 14.7).
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 template <int U> __device__ __forceinline__ u4 read(const u4* p) { return U > 1 ? __builtin_nontemporal_load(p) : *p; }
 template <int U> __device__ __forceinline__ void write(const u4& x, u4* p)
@@ -228,8 +230,12 @@ template <class X, class Y, int U> __global__ void __launch_bounds__(256) paged_
 
 template <class X, class Y> void launch_write(const PagedWriteArgs& a, unsigned pieces, hipStream_t s)
 {
-    if (pieces <= 1u << 17) paged_write_kernel<X, Y, 1><<<(pieces + 255) / 256, 256, 0, s>>>(a, pieces);      // two workgroups a CU
-    else paged_write_kernel<X, Y, 4><<<(pieces + 1023) / 1024, 256, 0, s>>>(a, pieces);
+    if constexpr (sizeof(Y) == 2)
+        if (pieces > 1u << 18) {
+            paged_write_kernel<X, Y, 4><<<(pieces + 1023) / 1024, 256, 0, s>>>(a, pieces);
+            return;
+        }
+    paged_write_kernel<X, Y, 1><<<(pieces + 255) / 256, 256, 0, s>>>(a, pieces);
 }
 
 }  // namespace

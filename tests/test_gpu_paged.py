@@ -33,6 +33,14 @@ def test_long_contexts_that_many_workgroups_share(dtype, d):
     check(Setup(Case("chunk", [(5000, 300), (640, 1)], nq=4, nkv=2, page=64), dtype, d))
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 128)], ids=str)
+@pytest.mark.parametrize("n", [600, 1700])
+def test_many_contexts_of_one_block(n, dtype, d):
+    """More requests than workgroups, no table longer than a block of keys: tiles are cut where the ranges end all the same."""
+    check(Setup(Case("short", [(64, 1 + i % 2) for i in range(n)]), dtype, d))
+    check(Setup(Case("short prompts", [(1 + i % 63, 1 + i % 63) for i in range(n // 10)], nq=4, nkv=2), dtype, d))
+
+
 def test_how_many_rows_a_request_has_may_be_said():
     c = Case("verify", [(500, 3), (64, 1), (33, 4), (200, 2)], nq=4, nkv=1)
     s = Setup(c, BF16, 128)
