@@ -209,8 +209,9 @@ struct PagedShape {
 inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
 {
     PagedShape s;
-    // Large tiles have a long way in and out, and launch beside them what is for few vectors; they read keys once for 256 vectors where others read them for 32.  (8 requests of up to 4K keys, 32 / 8 heads
-    // x 128: up to 64 vectors each 57.7 us large, 37.6 not, up to 128 53.9 and 43.3; 24 of 16K 241 and 252, 270 and 362.  64 columns: 128 vectors 43.4 and 33.3, 202 and 177; 256 vectors 45.9 and 44.7, 216 and 290.)
+    // Large tiles have a long way in and out; they read keys once for 256 vectors where others read them for 32.  (8 requests of up to 4K keys, 32 / 8 heads x 128, up to 64 vectors each: 53.6 us large,
+    // 36.7 not, up to 128 51.3 and 41.4; 24 of 16K 219 and 243, 249 and 348.  64 columns: up to 128 vectors 44.1 and 33.6, 188 and 174; up to 256 43.8 and 43.3, 201 and 292.)  Beside them requests of 16 vectors or
+    // fewer are the other kernel's (a limit of 32 or 64 gains nothing: the last pair 201, 206, 197; up to 64 vectors over 16K 219, 220, 326).
     const bool large = dtype == HEXI_BF16 && max_rows * most > (d == 64 ? 128 : 64);
     const bool few = !large || n_requests > 1;
     // A tile's start costs about what four blocks do (64 requests of 1K, one token each: 50.0 us with 1, 42.9 with 4, 44.7 with 8).  Ranges of few vectors may be as short as there are workgroups for them (one request
@@ -220,8 +221,8 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
     const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
     for (int i = 0; i < 2; ++i) {
         PagedShare& h = s.share[i];
-        // as many workgroups as run at once: one to a CU where the LDS is full, else two (24 requests of 16K, 128 columns: decoding 164 us with 256, 162 with 512, verifying 163 and 166; 64 columns: 96 and 92, 115 and 96)
-        const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests), full = i == 1 || (dtype == HEXI_F32 && d == 128) ? 256 : 512;      // (below 2^31: rows x heads are at most 2^28)
+        // as many workgroups as run at once: one to a CU where it takes the LDS, else two (24 requests of 16K, 128 columns: decoding 164 us with 256, 162 with 512, verifying 163 and 166; 64 columns: 96 and 92, 115 and 96)
+        const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests), full = large || (dtype == HEXI_F32 && d == 128) ? 256 : 512;      // (below 2^31: rows x heads are at most 2^28)
         while ((double)tiles * (double)((blocks >> h.coarse) + 1 + h.start) > 1e9) ++h.coarse;
         long long n = tiles > full ? full : tiles * (blocks + h.start) / h.min_cost + 1;
         n = n > full ? full : n;
@@ -249,5 +250,5 @@ inline void hexi_paged_place(const PagedShape& s, int i, int d, char* workspace,
 hipError_t hexi_launch_paged_plan(const PagedPlanArgs& a, hipStream_t s);
 hipError_t hexi_launch_paged_write(const PagedWriteArgs& a, int x_dtype, int y_dtype, hipStream_t s);
 hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, hipStream_t s);
-hipError_t hexi_launch_paged_large(const PagedArgs& a, int d, hipStream_t s);
+hipError_t hexi_launch_paged_large(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s);      // and few, where it has ranges
 hipError_t hexi_launch_paged_join(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s);

@@ -1,0 +1,327 @@
+// Attention of new tokens over a paged cache: tiles of 16 or 32 query vectors.
+//
+// Four wavefronts split every 64-key block of a tile, 16 keys each, which lie on one page.  Each streams its own keys through a private ring in LDS, by transfers that it
+// counts itself (nothing is held in registers on the way, and the loop has no barrier), and keeps a softmax of its own; LDS joins the four at a tile's end.
+//   S^T[key][vector] = K Q^T        lane (g, l) = (lane / 16, lane % 16) has keys 4 g + e of ONE vector, l;
+//   O^T[column][vector] = V^T P^T   P as it stands is the operand; V^T by transposed reads (bf16), or row pieces whose columns are dealt to the products (fp32).
+// P as an operand: bf16 where results are bf16 (FINE off: a weight is off by at most 2^-8 of itself, less than the result's own rounding in all), two bf16 values where they are fp32
+// (2^-16: partial results of a context on several devices); the sum that normalises is that of the weights as they are multiplied.
+// What bounds it: few vectors a key, so the reads of K and V.
+#pragma once
+#include "hexi_f32_common.h"
+#include "hexi_paged_tiles.h"
+
+namespace {
+
+constexpr float SLACK = 8.f;      // in units of log2: weights of up to 2^8
+
+// 16 rows of K or V in LDS: rows back to back, 16-byte piece c of row r at place c ^ swz(r).  A 128-bit read is served 16 lanes at a time, 0-3, 12-15, 20-23, 24-27 and so on (measured: with
+// 16 neighbouring lanes in mind a quarter of the LDS cycles were conflicts), a transposed 64-bit one 32 neighbouring lanes; either then touches all 64 banks once.
+template <class T, int D> struct Rows {
+    static constexpr int BYTES = D * (int)sizeof(T), PIECES = BYTES / 16, TILE = 16 * BYTES, XFERS = TILE / 1024, PER_XFER = 16 / XFERS;
+    static __host__ __device__ constexpr int swz(int r)
+    {
+        return sizeof(T) == 4 ? (r & 3) ^ (r >> 2 & 1) * 12 ^ (r >> 3 & 1) * 4 : PIECES == 16 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
+    }
+    static __device__ __forceinline__ const unsigned char* piece(const unsigned char* tile, int r, int c) { return tile + r * BYTES + ((c ^ swz(r)) << 4); }
+};
+
+// The products of a wavefront's 16 keys with 16 vectors.
+template <class T, int D> struct Ops;
+template <int D> struct Ops<uint16_t, D> {
+    using R = Rows<uint16_t, D>;
+    static constexpr int NQ = D / 32, NC = D / 16;
+    typedef bf16x8 Q;
+    // columns 32 i + 8 g .. + 7 of a vector
+    static __device__ __forceinline__ void vector(Q (&x)[NQ], const uint16_t* p, int g)
+    {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) x[i] = *reinterpret_cast<const bf16x8*>(p + 32 * i + 8 * g);
+    }
+    template <int NG> static __device__ __forceinline__ void scores(f32x4 (&s)[NG], const unsigned char* k, const Q (&q)[NG][NQ], int g, int l)
+    {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(R::piece(k, l, 4 * i + g));
+#pragma unroll
+            for (int n = 0; n < NG; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[n][i], s[n], 0, 0, 0);
+        }
+    }
+    // acc[n][c] += ...; used: sums of P as it is multiplied
+    template <int NG, bool FINE> static __device__ __forceinline__ void sums(f32x4 (&acc)[NG][NC], float (&used)[NG], const unsigned char* v, const f32x4 (&p)[NG], int g, int l)
+    {
+        bf16x4 b[NG], rest[NG];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            b[n] = bf16x4{(__bf16)p[n][0], (__bf16)p[n][1], (__bf16)p[n][2], (__bf16)p[n][3]};
+            used[n] += ((float)b[n][0] + (float)b[n][1]) + ((float)b[n][2] + (float)b[n][3]);
+            if constexpr (FINE) {
+                rest[n] = bf16x4{(__bf16)(p[n][0] - (float)b[n][0]), (__bf16)(p[n][1] - (float)b[n][1]), (__bf16)(p[n][2] - (float)b[n][2]), (__bf16)(p[n][3] - (float)b[n][3])};
+                used[n] += ((float)rest[n][0] + (float)rest[n][1]) + ((float)rest[n][2] + (float)rest[n][3]);
+            }
+        }
+        const int row = 4 * g + (l >> 2);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const s16x4 x = lds_read_tr16(reinterpret_cast<const uint16_t*>(R::piece(v, row, 2 * c + (l >> 1 & 1)) + 8 * (l & 1)));
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                acc[n][c] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(s16x4, b[n]), acc[n][c], 0, 0, 0);
+                if constexpr (FINE) acc[n][c] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(s16x4, rest[n]), acc[n][c], 0, 0, 0);
+            }
+        }
+    }
+    // column of row r of product c (r = 4 g + register)
+    static __device__ __forceinline__ int column(int c, int r) { return 16 * c + r; }
+};
+template <int D> struct Ops<float, D> {
+    using R = Rows<float, D>;
+    static constexpr int NQ = D / 16, NC = D / 16;
+    typedef f32x4 Q;
+    // columns 16 i + 4 g .. + 3 of a vector
+    static __device__ __forceinline__ void vector(Q (&x)[NQ], const float* p, int g)
+    {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) x[i] = *reinterpret_cast<const f32x4*>(p + 16 * i + 4 * g);
+    }
+    template <int NG> static __device__ __forceinline__ void scores(f32x4 (&s)[NG], const unsigned char* k, const Q (&q)[NG][NQ], int g, int l)
+    {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(R::piece(k, l, 4 * i + g));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int n = 0; n < NG; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], q[n][i][e], s[n], 0, 0, 0);
+        }
+    }
+    template <int NG, bool> static __device__ __forceinline__ void sums(f32x4 (&acc)[NG][NC], float (&used)[NG], const unsigned char* v, const f32x4 (&p)[NG], int g, int l)
+    {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) used[n] += (p[n][0] + p[n][1]) + (p[n][2] + p[n][3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(R::piece(v, 4 * g + e, 16 * i + l));
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int n = 0; n < NG; ++n) acc[n][4 * i + c] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[c], p[n][e], acc[n][4 * i + c], 0, 0, 0);
+            }
+    }
+    static __device__ __forceinline__ int column(int c, int r) { return 64 * (c / 4) + 4 * r + c % 4; }
+};
+
+// over lanes l, l + 16, l + 32, l + 48
+__device__ __forceinline__ float max_over_groups(float x)
+{
+    const unsigned i = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+    return max_across_halves(max2(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_over_groups(float x)
+{
+    const unsigned i = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+    return sum_across_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <int N> __device__ __forceinline__ void wait_transfers() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// LDS of a workgroup of NW wavefronts.
+template <class T, int D, int NG, int NW> struct FewShared {
+    static constexpr int NV = 16 * NG, AHEAD = paged_ring(sizeof(T), D);      // vectors, blocks of a ring
+    struct Ends { float acc[NW][NV][D + 4], stat[3][NW][NV]; int out[NV]; };      // stat: reference, sum of P, sum of P as it was multiplied
+    struct Ring { unsigned char k[AHEAD][Rows<T, D>::TILE], v[AHEAD][Rows<T, D>::TILE]; };
+    union { Ring ring[NW]; Ends ends; };
+};
+
+// The workgroup's range of the tiles; `a` is the kernel's argument with number WHICH.  NW wavefronts have NW / 4 blocks at a time.
+template <class T, int D, int NG, bool FINE, int NW, int WHICH>
+__device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, NG, NW>& sm, typename PagedWalk<64 * NW>::Shared& shared)
+{
+    using O = Ops<T, D>;
+    using R = Rows<T, D>;
+    using Ring = typename FewShared<T, D, NG, NW>::Ring;
+    constexpr int NV = 16 * NG, AHEAD = FewShared<T, D, NG, NW>::AHEAD, NB = NW / 4;
+    const PagedGeom& g = a.g;
+    const int tid = NB > 1 ? paged_thread() : (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = lane >> 4, l16 = lane & 15, sub = NB > 1 ? wave & 3 : wave;      // sub: which 16 keys of a block
+    PagedWalk<64 * NW> walk(a, shared);
+    if (!walk.any) return;
+    const float c_hi = g.scale * LOG2E_HI, c_lo = fmaf(g.scale, LOG2E_HI, -c_hi) + g.scale * LOG2E_LO, slack = SLACK / c_hi;
+    Ring& ring = sm.ring[wave];
+    const uint32_t lds_k = (uint32_t)(uintptr_t)&ring.k[0][0], lds_v = (uint32_t)(uintptr_t)&ring.v[0][0];
+    // what the lane fetches: a row of every transfer and a piece of it
+    const int fetch_row = lane / R::PIECES, fetch_place = lane % R::PIECES;
+    uint32_t fetch_off[R::XFERS];
+#pragma unroll
+    for (int x = 0; x < R::XFERS; ++x)
+        fetch_off[x] = (uint32_t)(fetch_row * (int)g.stride_tok * (int)sizeof(T)) + 16u * (uint32_t)(fetch_place ^ R::swz(x * R::PER_XFER + fetch_row));
+    Tile t;
+    while (walk.next(a, t)) {
+        // the lane's vectors; of one that is none the first one again
+        WinKeys keys[NG];
+        typename O::Q q[NG][O::NQ];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            const int v = 16 * i + l16 < t.vectors ? 16 * i + l16 : 0, row = t.row_of(v);
+            keys[i] = paged_keys_of_row(g, t.q, row);
+            O::vector(q[i], static_cast<const T*>(a.q) + (long long)(t.q.row0 + row) * g.q_stride_tok + (long long)t.head_of(g, v, row) * g.q_stride_head, grp);
+        }
+        const int* table = g.table + (long long)t.r * g.columns;
+        const long long head = (long long)t.kv_head(g) * g.stride_head;
+        const char *k_head = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + head), *v_head = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + head);
+        const int last = t.last, b0 = t.b0 + (NB > 1 ? wave / 4 : 0), b1 = t.b1;      // every NB-th block from b0 on
+        int ids = -1, page_rows = 0, listed = 0;  // lane i: page and row of this wavefront's first key in block `listed` + NB i
+        bool bad = false;                         // a page that the cache does not have
+        auto list = [&](int b) {
+            listed = b;
+            const int key = PAGED_KEYS * t.span.block(b + NB * lane) + 16 * sub;
+            const PagedPlace p = paged_place(g, table, key < last ? key : last & ~15);
+            bad |= p.id < 0 && b + NB * lane < b1;
+            ids = p.id < 0 ? 0 : p.id;
+            page_rows = p.row;
+            asm volatile("" : "+v"(ids), "+v"(page_rows));      // (waited for here, before any transfer is counted)
+        };
+        // requests 16 rows of K or V of block b
+        auto fetch = [&](const char* src, uint32_t lds, int b) {
+            const int key = PAGED_KEYS * t.span.block(b) + 16 * sub;
+            const int id = __builtin_amdgcn_readlane(ids, (b - listed) / NB), row = __builtin_amdgcn_readlane(page_rows, (b - listed) / NB);
+            const char* from = src + (long long)sizeof(T) * ((long long)id * g.stride_page + (long long)row * g.stride_tok);
+            if (key + 15 <= last) {
+#pragma unroll
+                for (int x = 0; x < R::XFERS; ++x)
+                    lds_dma16_base(from + (long long)sizeof(T) * (x * R::PER_XFER) * g.stride_tok, fetch_off[x], __builtin_amdgcn_readfirstlane(lds + 1024 * x));
+            } else {      // keys past the last one that is seen: that one again
+                const int most = last - (key < last ? key : last & ~15);
+#pragma unroll
+                for (int x = 0; x < R::XFERS; ++x) {
+                    const int r = x * R::PER_XFER + fetch_row;
+                    lds_dma16_base(from, (uint32_t)((r < most ? r : most) * (int)g.stride_tok * (int)sizeof(T)) + 16u * (uint32_t)(fetch_place ^ R::swz(r)), __builtin_amdgcn_readfirstlane(lds + 1024 * x));
+                }
+            }
+        };
+        // The reference m of a vector is the largest score so far, or up to SLACK units of log2 less: sums are scaled again where a score exceeds it by more.
+        float m[NG], over[NG], l[NG], l_used[NG];
+        f32x4 acc[NG][O::NC];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            m[i] = over[i] = -INFINITY; l[i] = l_used[i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < O::NC; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        auto weights = [&](f32x4& s, int i, bool whole, uint32_t seen) __attribute__((always_inline)) {      // seen: bit e: register e's key is seen
+            if (!whole) { s[0] = win_or<0>(seen, s[0], -INFINITY); s[1] = win_or<1>(seen, s[1], -INFINITY); s[2] = win_or<2>(seen, s[2], -INFINITY); s[3] = win_or<3>(seen, s[3], -INFINITY); }
+            const float mx = max2(max3(s[0], s[1], s[2]), s[3]);
+            if (__any(mx > over[i])) {
+                const float top = fmaxf(m[i], max_over_groups(mx)), y = m[i] - top, alpha = m[i] == -INFINITY ? 0.f : fast_exp2(fmaf(y, c_hi, y * c_lo));
+                m[i] = top;
+                over[i] = top + slack;
+                l[i] *= alpha;
+                l_used[i] *= alpha;
+#pragma unroll
+                for (int c = 0; c < O::NC; ++c) acc[i][c] *= alpha;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d = s[e] - m[i];      // (-inf less -inf, or -inf times c_lo, makes NaN: of keys that are not seen, whose weight is 0 whatever comes out, or of infinite scores)
+                s[e] = fast_exp2(fmaf(d, c_hi, d * c_lo));
+            }
+            if (!whole) { s[0] = win_or<0>(seen, s[0], 0.f); s[1] = win_or<1>(seen, s[1], 0.f); s[2] = win_or<2>(seen, s[2], 0.f); s[3] = win_or<3>(seen, s[3], 0.f); }
+            l[i] += (s[0] + s[1]) + (s[2] + s[3]);
+        };
+        if (b0 < b1) {
+            list(b0);
+            wait_transfers<0>();                  // (stores of the tile in front: from here on transfers alone are counted)
+            for (int i = 0; i < AHEAD && b0 + NB * i < b1; ++i) {
+                fetch(k_head, lds_k + i * R::TILE, b0 + NB * i);
+                fetch(v_head, lds_v + i * R::TILE, b0 + NB * i);
+            }
+            int at = 0;                           // place in the ring
+            for (int b = b0; b < b1; b += NB) {
+                const int next = b + NB * AHEAD;
+                const bool more = next < b1;
+                if (more && next - listed >= 64 * NB) list(next);
+                const unsigned char *k = ring.k[0] + at * R::TILE, *v = ring.v[0] + at * R::TILE;
+                // behind K of this block: V of it and both of AHEAD - 1 further ones; and then, behind V, these and K of another one
+                if (more) wait_transfers<(2 * AHEAD - 1) * R::XFERS>(); else wait_transfers<0>();
+                const int block = t.span.block(b);
+                f32x4 s[NG];
+                O::template scores<NG>(s, k, q, grp, l16);
+                if (more) { reads_done(); fetch(k_head, lds_k + at * R::TILE, next); }
+                const bool whole = t.span.full(block);
+#pragma unroll
+                for (int i = 0; i < NG; ++i) weights(s[i], i, whole, whole ? 15u : win_bits(keys[i], PAGED_KEYS * block + 16 * sub + 4 * grp));
+                if (more) wait_transfers<(2 * AHEAD - 1) * R::XFERS>();
+                O::template sums<NG, FINE>(acc, l_used, v, s, grp, l16);
+                if (more) { reads_done(); fetch(v_head, lds_v + at * R::TILE, next); }
+                at = at + 1 == AHEAD ? 0 : at + 1;
+            }
+        }
+
+        // the wavefronts' results joined
+        __syncthreads();                          // all rings are free
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+            l[i] = sum_over_groups(l[i]);
+            l_used[i] = sum_over_groups(l_used[i]);
+            if (grp == 0) { sm.ends.stat[0][wave][16 * i + l16] = m[i]; sm.ends.stat[1][wave][16 * i + l16] = l[i]; sm.ends.stat[2][wave][16 * i + l16] = l_used[i]; }
+#pragma unroll
+            for (int c = 0; c < O::NC; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    z = fmaf(acc[i][c][e], 0.f, z);
+                    sm.ends.acc[wave][16 * i + l16][O::column(c, 4 * grp + e)] = acc[i][c][e];
+                }
+        }
+        // (a key that a vector does not see has P = 0, and 0 x inf is NaN: what is not finite is done again element by element, and so is what has keys on pages that the cache does not have)
+        if (__syncthreads_or(z != 0.f || bad)) {
+            plain_tile<T, D, WHICH>(t);
+            continue;
+        }
+        if (tid < NV) {                           // a vector's LSE, and what the wavefronts' sums of V are multiplied by
+            float mm = -INFINITY, sum = 0.f, used = 0.f, e[NW];
+#pragma unroll
+            for (int x = 0; x < NW; ++x) mm = fmaxf(mm, sm.ends.stat[0][x][tid]);
+#pragma unroll
+            for (int x = 0; x < NW; ++x) {
+                // (d is -inf too where the two are finite and far apart: 0, whatever the sign of c_lo)
+                const float r = sm.ends.stat[0][x][tid], d = r - mm;
+                e[x] = r == -INFINITY ? 0.f : fast_exp2(fmaf(d, c_hi, d == -INFINITY ? 0.f : d * c_lo));
+                sum += e[x] * sm.ends.stat[1][x][tid];
+                used += e[x] * sm.ends.stat[2][x][tid];
+            }
+            const float lse = sum == 0.f ? -INFINITY : fmaf(mm, g.scale, logf(sum)), r = used == 0.f ? 0.f : 1.0f / used;
+#pragma unroll
+            for (int x = 0; x < NW; ++x) sm.ends.stat[0][x][tid] = e[x] * r;
+            int at = -1;
+            if (tid < t.vectors) {
+                const int row = t.row_of(tid), h = t.head_of(g, tid, row);
+                at = (int)paged_out(a, t, row, h);
+                if (t.piece >= 0) a.part_lse[(long long)t.piece * NV + tid] = lse;
+                else if (a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
+            }
+            sm.ends.out[tid] = at;
+        }
+        __syncthreads();
+        for (int p = tid; p < t.vectors * (D / 4); p += 64 * NW) {       // four columns of a vector
+            const int i = p / (D / 4), c = 4 * (p % (D / 4));
+            f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < NW; ++x) o += sm.ends.stat[0][x][i] * *reinterpret_cast<const f32x4*>(&sm.ends.acc[x][i][c]);
+            if (t.piece >= 0) win_plain::store4(a.part_o, ((long long)t.piece * NV + i) * D + c, false, o[0], o[1], o[2], o[3]);
+            else win_plain::store4(a.o, (long long)sm.ends.out[i] * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
+        }
+        __syncthreads();                          // the rings are written again
+    }
+    walk.done(a);
+}
+
+}  // namespace

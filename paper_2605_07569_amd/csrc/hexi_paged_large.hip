@@ -9,7 +9,7 @@
 // the 16-byte pieces of a row are exchanged by their high bits (`flip`), so that both the 128-bit row reads of K and the transposed 64-bit reads of V^T touch all 64 banks once (a 128-bit read is
 // served 16 lanes at a time, 0-3, 12-15, 20-23, 24-27 and so on, a transposed one 32 neighbouring lanes).
 #include "hexi_mfma.h"
-#include "hexi_paged_tiles.h"
+#include "hexi_paged_few.h"
 
 namespace {
 
@@ -36,16 +36,14 @@ template <int D> struct Smem {
     union { Tiles tiles; float stage[8][32 * Cfg<D>::PITCH + 32]; };
 };
 
-template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_kernel(const PagedArgs a)
+// The workgroup's range of the large tiles.
+template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const PagedArgs& a, Smem<D>& sm, typename PagedWalk<512>::Shared& shared)
 {
     using C = Cfg<D>;
     constexpr int NKS = C::NKS, NDB = C::NDB;
     constexpr bool PAIR_BARRIER = D == 128;     // one workgroup barrier per pair of phases instead of one per phase
-    __shared__ __attribute__((aligned(1024))) Smem<D> sm;
-    __shared__ typename PagedWalk<512>::Shared shared;
-    paged_touch();
     const PagedGeom& g = a.g;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = paged_thread(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = wave >> 2, wg = wave & 3;
     const int l32 = lane & 31, hh = lane >> 5, grp2 = (lane >> 4) & 1, j16 = lane & 15, jj = j16 >> 2;
 
@@ -75,7 +73,7 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
     PagedWalk<512> walk(a, shared);
     if (!walk.any) return;
     Tile t;
-    while (walk.next(paged_args(), t)) {
+    while (walk.next(paged_args<1>(), t)) {
         const int NT = t.b1 - t.b0, last = t.last;
         const int my_vector = GROUP * grp + 32 * wg + l32;
         const bool real = my_vector < t.vectors;
@@ -330,14 +328,14 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
             for (int r = 0; r < 16; ++r) z = fmaf(oacc[db][r], 0.f, z);
         // (a key that a row does not see has P = 0, and 0 x inf is NaN: what is not finite is done again element by element, and so is what has keys on pages that the cache does not have)
         if (__syncthreads_or((z != 0.f && real) || bad)) {
-            plain_tile<uint16_t, D>(t);
+            plain_tile<uint16_t, D, 1>(t);
             continue;
         }
 
         // Rows of O go through LDS (a region of every wavefront's own) so that global accesses are row-contiguous.
         const float inv = l_tot > 0.f && lr_tot > 0.f ? 1.0f / lr_tot : 0.f, lse = l_tot > 0.f ? (m_run + __log2f(l_tot)) * LN2 : -INFINITY;
         float* stage = sm.stage[wave];
-        const PagedArgs& a = paged_args();
+        const PagedArgs& a = paged_args<1>();
         const PagedGeom& g = a.g;
         int* stage_at = reinterpret_cast<int*>(stage + 32 * C::PITCH);
 #pragma unroll
@@ -366,16 +364,49 @@ template <int D, bool FINE> __global__ void __launch_bounds__(512) paged_large_k
         }
         __syncthreads();                          // the next tile's transfers write where these rows were staged
     }
-    walk.done(paged_args());
+    walk.done(paged_args<1>());
+}
+
+// BOTH: with the tiles of few vectors (argument 0) as well.  Every workgroup has a range of either, and neighbouring ones take them in opposite order: those of few vectors wait for memory, the large ones for
+// the matrix and vector units, so they run side by side all through the launch (1400 prompt rows and 21 tokens over up to 9K keys, 24 / 8 heads: 227 us in two launches, 189 in one, 64 columns 150 and 133).
+struct PagedBoth { PagedArgs a[2]; };
+template <int D, bool FINE, bool BOTH> __global__ void __launch_bounds__(512) paged_large_kernel(const PagedBoth)
+{
+    if constexpr (!BOTH) {
+        __shared__ __attribute__((aligned(1024))) Smem<D> sm;
+        __shared__ typename PagedWalk<512>::Shared shared;
+        paged_touch<1>();
+        large_ranges<D, FINE>(paged_args<1>(), sm, shared);
+    } else {
+        __shared__ __attribute__((aligned(1024))) union { Smem<D> large; FewShared<uint16_t, D, 1, 8> few; } sm;
+        __shared__ typename PagedWalk<512>::Shared shared;
+        paged_touch<0>();
+        paged_touch<1>();
+        const int first = (int)blockIdx.x >> 3 & 1;
+#pragma unroll 1
+        for (int i = 0; i < 2; ++i) {
+            if (i == first) large_ranges<D, FINE>(paged_args<1>(), sm.large, shared);
+            else few_ranges<uint16_t, D, 1, FINE, 8, 0>(paged_args<0>(), sm.few, shared);
+            __syncthreads();                      // LDS is free
+        }
+    }
+}
+
+template <int D, bool FINE> void launch_large(const PagedBoth& both, hipStream_t s)
+{
+    const int few = both.a[0].n_ranges, large = both.a[1].n_ranges;
+    if (few > 0) paged_large_kernel<D, FINE, true><<<few > large ? few : large, 512, 0, s>>>(both);
+    else paged_large_kernel<D, FINE, false><<<large, 512, 0, s>>>(both);
 }
 
 }  // namespace
 
-hipError_t hexi_launch_paged_large(const PagedArgs& a, int d, hipStream_t s)
+hipError_t hexi_launch_paged_large(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s)
 {
+    const PagedBoth both = {{few, large}};
     if (d == 128) {
-        if (a.out_bf16) paged_large_kernel<128, false><<<a.n_ranges, 512, 0, s>>>(a); else paged_large_kernel<128, true><<<a.n_ranges, 512, 0, s>>>(a);
-    } else if (a.out_bf16) paged_large_kernel<64, false><<<a.n_ranges, 512, 0, s>>>(a);
-    else paged_large_kernel<64, true><<<a.n_ranges, 512, 0, s>>>(a);
+        if (large.out_bf16) launch_large<128, false>(both, s); else launch_large<128, true>(both, s);
+    } else if (large.out_bf16) launch_large<64, false>(both, s);
+    else launch_large<64, true>(both, s);
     return hipGetLastError();
 }

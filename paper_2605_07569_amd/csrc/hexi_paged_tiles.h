@@ -19,22 +19,30 @@ __device__ __forceinline__ PagedRequest paged_uniform(const PagedRequest& q)
 }
 __device__ __forceinline__ WinKeys paged_uniform(const WinKeys& w) { return WinKeys{paged_uniform(w.sink), paged_uniform(w.lo), paged_uniform(w.hi)}; }
 
-// The launch's arguments, read again here: what is worked out from them once a tile does not keep scalar registers through its loop.  (They are the kernel's first ones.)
-__device__ __forceinline__ const PagedArgs& paged_args()
+// The launch's arguments with number WHICH, read again here: what is worked out from them once a tile does not keep scalar registers through its loop.  (They are the kernel's first ones.)
+template <int WHICH> __device__ __forceinline__ const PagedArgs& paged_args()
 {
     typedef const __attribute__((address_space(4))) PagedArgs* Ptr;
-    Ptr p = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    Ptr p = (Ptr)__builtin_amdgcn_kernarg_segment_ptr() + WHICH;
     asm volatile("" : "+s"(p));
     return *(const PagedArgs*)p;
 }
 
 // Asks for all of the arguments' lines at once, before the first of them is waited for.  (Read one behind the other they cost 0.7 us more: 107.0 us against 106.3 for a verifying batch, 32.4 against 31.7 for a small one of fp32.)
-__device__ __forceinline__ void paged_touch()
+template <int WHICH> __device__ __forceinline__ void paged_touch()
 {
     typedef const __attribute__((address_space(4))) int* Ptr;
-    const Ptr p = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    const Ptr p = (Ptr)((const __attribute__((address_space(4))) PagedArgs*)__builtin_amdgcn_kernarg_segment_ptr() + WHICH);
     static_assert(sizeof(PagedArgs) > 10 * 64 && sizeof(PagedArgs) <= 11 * 64, "eleven lines");
     asm volatile("" ::"s"(p[0]), "s"(p[16]), "s"(p[32]), "s"(p[48]), "s"(p[64]), "s"(p[80]), "s"(p[96]), "s"(p[112]), "s"(p[128]), "s"(p[144]), "s"(p[160]));
+}
+
+// The thread's number, such that what follows from it is worked out behind this point and no earlier (where one kernel does several things one behind the other).
+__device__ __forceinline__ int paged_thread()
+{
+    int x = (int)threadIdx.x;
+    asm volatile("" : "+v"(x));
+    return x;
 }
 
 struct Tile {
@@ -212,10 +220,10 @@ template <int NT> struct PagedWalk {
 __device__ __forceinline__ long long paged_out(const PagedArgs& a, const Tile& t, int row, int h) { return (long long)(t.q.row0 + row) * a.g.nq + h; }
 
 // A tile's vectors, eight lanes each, walk the keys of the range's blocks that they see, one by one: what a vector does not see is not read into it.
-template <class T, int D> __device__ __forceinline__ void plain_tile(const Tile& t)
+template <class T, int D, int WHICH> __device__ __forceinline__ void plain_tile(const Tile& t)
 {
     constexpr int N = D / win_plain::LANES;
-    const PagedArgs& a = paged_args();
+    const PagedArgs& a = paged_args<WHICH>();
     const PagedGeom& g = a.g;
     const int col = (int)threadIdx.x % win_plain::LANES * N;
     const int* table = g.table + (long long)t.r * g.columns;

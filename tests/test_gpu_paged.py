@@ -41,6 +41,33 @@ def test_many_contexts_of_one_block(n, dtype, d):
     check(Setup(Case("short prompts", [(1 + i % 63, 1 + i % 63) for i in range(n // 10)], nq=4, nkv=2), dtype, d))
 
 
+@pytest.mark.parametrize("dtype,d,chunk", [(BF16, 128, 0), (BF16, 64, 0), (F32, 64, 0), (BF16, 128, 200), (BF16, 64, 200)], ids=str)
+def test_requests_on_the_same_pages(dtype, d, chunk):
+    """A prefix that 64 requests share, 66 thousand keys each: ranges of many hundred blocks of one request; with `chunk` a request of as many rows among them."""
+    kv, page, n = 66001, 64, 64
+    alone = Setup(Case("token", [(kv, 1)], nq=2, nkv=2, page=page), dtype, d)
+    many = Setup(Case("chunk", [(kv, chunk)], nq=2, nkv=2, page=page), dtype, d)
+    assert torch.equal(alone.table, many.table) and torch.equal(alone.k[0], many.k[0]) and torch.equal(alone.v[0], many.v[0])
+    q = torch.randn(n, 2, d, generator=torch.Generator().manual_seed(5)).to(dtype).to(DEV)
+    rows = torch.cat([q[:40], many.q, q[40:]])
+    lens = [1] * 40 + ([chunk] if chunk else []) + [1] * 24
+    starts = [sum(lens[:r]) for r in range(len(lens) + 1)]
+    s = Setup(Case("all", [(1, n) for n in lens], nq=2, nkv=2, page=page), dtype, d)
+    s.table, s.row_start, s.kv_len, s.q, s.k_cache, s.v_cache = alone.table.repeat(len(lens), 1), ints(starts), ints([kv] * len(lens)), rows, alone.k_cache, alone.v_cache
+    s.cache, s.desc = hexi.make_paged_cache(s.k_cache), hexi.paged_desc_for(s.q, s.k_cache, s.scale, None)
+    o, lse = s.run()
+    torch.cuda.synchronize()
+    rel = pu.REL[dtype]
+    for r, m in enumerate(lens):
+        if m == 1 and r % 8 not in (0, 7):
+            continue
+        x = alone if m == 1 else many
+        x.q = rows[starts[r]:starts[r + 1]]
+        want, wl, bo, bl = x.reference()
+        pu.within("o", o[starts[r]:starts[r + 1]], want, bo, rel)
+        pu.within("lse", lse[:, starts[r]:starts[r + 1]], wl, bl)
+
+
 def test_how_many_rows_a_request_has_may_be_said():
     c = Case("verify", [(500, 3), (64, 1), (33, 4), (200, 2)], nq=4, nkv=1)
     s = Setup(c, BF16, 128)
