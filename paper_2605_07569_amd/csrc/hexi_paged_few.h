@@ -4,8 +4,8 @@
 // counts itself (nothing is held in registers on the way, and the loop has no barrier), and keeps a softmax of its own; LDS joins the four at a tile's end.
 //   S^T[key][vector] = K Q^T        lane (g, l) = (lane / 16, lane % 16) has keys 4 g + e of ONE vector, l;
 //   O^T[column][vector] = V^T P^T   P as it stands is the operand; V^T by transposed reads (bf16), or row pieces whose columns are dealt to the products (fp32).
-// P as an operand: bf16 where results are bf16 (FINE off: a weight is off by at most 2^-8 of itself, less than the result's own rounding in all), two bf16 values where they are fp32
-// (2^-16: partial results of a context on several devices); the sum that normalises is that of the weights as they are multiplied.
+// P as an operand: bf16 where results are bf16 (FINE off: a weight is off by at most 2^-8 of itself, less than the result's own rounding in all), three bf16 values where they are fp32
+// (2^-24: partial results of a context on several devices; with two they were off by 1.7e-6, relative L2, where fp32 sums are by 5e-7); the sum that normalises is that of the weights as they are multiplied.
 // What bounds it: few vectors a key, so the reads of K and V.
 #pragma once
 #include "hexi_f32_common.h"
@@ -52,25 +52,29 @@ template <int D> struct Ops<uint16_t, D> {
     // acc[n][c] += ...; used: sums of P as it is multiplied
     template <int NG, bool FINE> static __device__ __forceinline__ void sums(f32x4 (&acc)[NG][NC], float (&used)[NG], const unsigned char* v, const f32x4 (&p)[NG], int g, int l)
     {
-        bf16x4 b[NG], rest[NG];
+        bf16x4 b[NG][FINE ? 3 : 1];
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
-            b[n] = bf16x4{(__bf16)p[n][0], (__bf16)p[n][1], (__bf16)p[n][2], (__bf16)p[n][3]};
-            used[n] += ((float)b[n][0] + (float)b[n][1]) + ((float)b[n][2] + (float)b[n][3]);
-            if constexpr (FINE) {
-                rest[n] = bf16x4{(__bf16)(p[n][0] - (float)b[n][0]), (__bf16)(p[n][1] - (float)b[n][1]), (__bf16)(p[n][2] - (float)b[n][2]), (__bf16)(p[n][3] - (float)b[n][3])};
-                used[n] += ((float)rest[n][0] + (float)rest[n][1]) + ((float)rest[n][2] + (float)rest[n][3]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float x = p[n][e];
+                b[n][0][e] = (__bf16)x;
+                if constexpr (FINE) {
+                    b[n][1][e] = (__bf16)(x -= (float)b[n][0][e]);
+                    b[n][2][e] = (__bf16)(x - (float)b[n][1][e]);
+                }
             }
+            if constexpr (FINE) used[n] += (p[n][0] + p[n][1]) + (p[n][2] + p[n][3]);
+            else used[n] += ((float)b[n][0][0] + (float)b[n][0][1]) + ((float)b[n][0][2] + (float)b[n][0][3]);
         }
         const int row = 4 * g + (l >> 2);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const s16x4 x = lds_read_tr16(reinterpret_cast<const uint16_t*>(R::piece(v, row, 2 * c + (l >> 1 & 1)) + 8 * (l & 1)));
 #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                acc[n][c] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(s16x4, b[n]), acc[n][c], 0, 0, 0);
-                if constexpr (FINE) acc[n][c] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(s16x4, rest[n]), acc[n][c], 0, 0, 0);
-            }
+            for (int n = 0; n < NG; ++n)
+#pragma unroll
+                for (int i = 0; i < (FINE ? 3 : 1); ++i) acc[n][c] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, __builtin_bit_cast(s16x4, b[n][i]), acc[n][c], 0, 0, 0);
         }
     }
     // column of row r of product c (r = 4 g + register)

@@ -140,7 +140,7 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
 
         f32x16 oacc[NDB];
         f32x16 s[2];
-        bf16x8 pf[4], rest[FINE ? 4 : 1];         // FINE: P as two bf16 values
+        bf16x8 pf[FINE ? 1 : 4];                  // (FINE: P as three bf16 values, from s as they are multiplied)
         float m_run, l_run, lr_run, thr_raw;
 
         // Matrix phase on buffers (B + NB - 1) % NB (V of block t - 1) and B (K of block t).  Steps 0 .. NPV - 1: O^T += V^T P^T, four 16-key steps x NDB 32-column blocks; steps NPV ..
@@ -151,7 +151,7 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
             constexpr int PF = 4, NS = PF + 1;
             constexpr int KOFF = B < 0 ? 0 : B * C::TILE, VOFF = B < 0 ? 0 : (B + NB - 1) % NB * C::TILE;
             s16x4 ta[NS], tb[NS];
-            bf16x8 kb[NS];
+            bf16x8 kb[NS], fine[3];
             auto issue = [&](auto stc) __attribute__((always_inline)) {
                 constexpr int st = decltype(stc)::value, slot = (st - FIRST) % NS;
                 if constexpr (st < NPV) {
@@ -172,8 +172,20 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
                 constexpr int younger = 2 * n_tr + ((hi - st) - n_tr);
                 if constexpr (st < NPV) {
                     lds_wait<younger>(ta[slot], tb[slot]);
-                    oacc[st % NDB] = mfma32(join_halves(ta[slot], tb[slot]), pf[st / NDB], oacc[st % NDB]);
-                    if constexpr (FINE) oacc[st % NDB] = mfma32(join_halves(ta[slot], tb[slot]), rest[st / NDB], oacc[st % NDB]);
+                    constexpr int u = st / NDB, db = st % NDB;
+                    if constexpr (!FINE) oacc[db] = mfma32(join_halves(ta[slot], tb[slot]), pf[u], oacc[db]);
+                    else {
+                        if constexpr (db == 0)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const float p = s[u >> 1][8 * (u & 1) + e];
+                                fine[0][e] = (__bf16)p;
+                                fine[1][e] = (__bf16)(p - (float)fine[0][e]);
+                                fine[2][e] = (__bf16)(p - (float)fine[0][e] - (float)fine[1][e]);
+                            }
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) oacc[db] = mfma32(join_halves(ta[slot], tb[slot]), fine[i], oacc[db]);
+                    }
                 } else {
                     constexpr int b = (st - NPV) & 1, ks = (st - NPV) >> 1;
                     lds_wait<younger>(kb[slot]);
@@ -187,8 +199,8 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
             for_range<FIRST, LAST>(step);
         };
 
-        // Vector phase: softmax numerators of the block whose scores sit in s[], rounded to bf16 operand slots.  Two running sums: of the exact values (for the LSE) and of the rounded ones (they
-        // normalise O).  MASKED: some row of the group does not see all of the block, or none has a reference yet.  exact: the reference is the running maximum, raised where a
+        // Vector phase: softmax numerators of the block whose scores sit in s[], rounded to bf16 operand slots (FINE: left in s).  Two running sums: of the exact values (for the LSE) and of the rounded
+        // ones (they normalise O).  MASKED: some row of the group does not see all of the block, or none has a reference yet.  exact: the reference is the running maximum, raised where a
         // block exceeds it by more than 2^8; otherwise it stays what it is.
         auto v_phase = [&](int key0, auto masked_c, const bool exact) __attribute__((always_inline)) {
             constexpr bool MASKED = decltype(masked_c)::value;
@@ -228,18 +240,16 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
                 float p[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) { p[e] = fast_exp2(fmaf(s[b][x + e], c_log2, neg_m)); ps[e & 3] += p[e]; }
-                pf[u] = pack_bf16x8_sum4(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], psr);
-                if constexpr (FINE) {
+                if constexpr (!FINE) pf[u] = pack_bf16x8_sum4(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], psr);
+                else
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] -= (float)pf[u][e];
-                    rest[u] = pack_bf16x8_sum4(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], psr);
-                }
+                    for (int e = 0; e < 8; ++e) s[b][x + e] = p[e];
             }
             l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
-            lr_run += (psr[0] + psr[1]) + (psr[2] + psr[3]);
+            lr_run += FINE ? (ps[0] + ps[1]) + (ps[2] + ps[3]) : (psr[0] + psr[1]) + (psr[2] + psr[3]);
             // (nothing of the vector phase may drift into the matrix phase)
-            asm volatile("" : "+v"(l_run), "+v"(lr_run), "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]));
-            if constexpr (FINE) asm volatile("" : "+v"(rest[0]), "+v"(rest[1]), "+v"(rest[2]), "+v"(rest[3]));
+            if constexpr (FINE) asm volatile("" : "+v"(l_run), "+v"(lr_run), "+v"(s[0]), "+v"(s[1]));
+            else asm volatile("" : "+v"(l_run), "+v"(lr_run), "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]));
         };
 
         // One pass over the blocks: M(0) V(0) M(1) V(1) ... M(NT), the barriers as in the ring step's kernel.

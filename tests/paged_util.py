@@ -3,7 +3,8 @@
 Bounds.  u = 2^-24 is half a step of fp32, h = 2^-8 half a step of bf16 (0 for fp32 inputs: nothing is rounded to fewer bits there).  A score is a sum of d products and a few more
 roundings: |error| <= (d + 16) u scale sum |q k| + 16 u (|s| + |m|), m the value that is subtracted from it before the exponential (the row's LSE here; the kernels' reference is
 within a few units of it).  Exponentials and the sums' own roundings are counted as 2^-20 and n u relative.  E_j: what that makes of P_j, relative.  P is rounded to bf16
-as an operand (the sum that normalises o is that of the rounded P: at most h (sum P |v| + |o|)), results to the type they are asked for in (h or u)."""
+as an operand where results are bf16, to 2^-24 where they are fp32 (the sum that normalises o is that of the rounded P: at most h (sum P |v| + |o|), or u), results to the type
+they are asked for in (h or u)."""
 import random
 from dataclasses import dataclass
 from typing import List, Optional, Tuple
@@ -118,7 +119,7 @@ class Setup:
     def reference(self, out=None):
         """o, lse and bounds on their errors; 7 in rows that are no request's."""
         c, d = self.c, self.d
-        h_in, h_out = H if self.dtype == BF16 else 0.0, H if (out or self.dtype) == BF16 else U
+        h_in, h_out = (0.0 if self.dtype == F32 else H if (out or BF16) == BF16 else U), H if (out or self.dtype) == BF16 else U
         f64 = dict(dtype=torch.float64, device=DEV)
         o, bo = torch.full((c.rows, c.nq, d), 7.0, **f64), torch.zeros((c.rows, c.nq, d), **f64)
         lse, bl = torch.full((c.nq, c.rows), 7.0, **f64), torch.zeros((c.nq, c.rows), **f64)
@@ -144,7 +145,7 @@ class Setup:
         return o, lse, bo, bl
 
 
-# relative L2 that results may be off by: the flat bounds of the library's outputs, those of bf16 inputs whatever type they are returned in (weights rounded to 2^-8, evenly spread: 2^-8 / sqrt(3) = 2.3e-3 of them)
+# relative L2 that results may be off by, by the type they are returned in: the flat bounds of the library's outputs (bf16 weights and results, roundings evenly spread: 2^-8 / sqrt(3) = 2.3e-3 each at most)
 REL = {BF16: 5e-3, F32: 1e-5}
 
 
@@ -168,7 +169,7 @@ def check(s, out=None, max_rows=0, **kw):
     for rows in (slice(0, c.first), slice(c.rows - c.behind, c.rows)):      # left as they were
         assert (got[0][rows] == 7).all() and (got[1][:, rows] == 7).all()
     mine = slice(c.first, c.rows - c.behind)
-    within("o", got[0][mine], o[mine], bo[mine], REL[BF16 if BF16 in (s.dtype, out) else F32])
+    within("o", got[0][mine], o[mine], bo[mine], REL[out or s.dtype])
     within("lse", got[1][:, mine], lse[:, mine], bl[:, mine])
     return got
 

@@ -18,12 +18,13 @@ def test_attention_parity(c, dtype, d):
     check(Setup(c, dtype, d))
 
 
-@pytest.mark.parametrize("c", [pu.CASES[i] for i in (3, 6, 10)], ids=lambda c: c.name)
-def test_results_in_fp32_of_bf16_inputs_and_without_lse(c):
-    s = Setup(c, BF16, 128)
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("c", [pu.CASES[i] for i in (3, 6, 10, 16)] + [Case("a chunk alone", [(700, 141)], nq=2, page=32), Case("rows of a few", [(900, 5), (31, 4)], nq=4)], ids=lambda c: c.name)
+def test_results_in_fp32_of_bf16_inputs_and_without_lse(c, d):
+    s = Setup(c, BF16, d)
     o, lse = check(s, F32)
     assert torch.equal(s.run(F32, bufs=(torch.full_like(o, 7.0), None))[0], o)
-    check(Setup(c, F32, 64), BF16)
+    check(Setup(c, F32, d), BF16)
 
 
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)], ids=str)
