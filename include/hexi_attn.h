@@ -324,7 +324,8 @@ int hexi_rope_a2a_unpack(const hexi_rope_desc* desc, const hexi_range* range, co
  *             cache, page id * page + token, -1 where its request got nothing.  Rows behind the last request's get 0 and -1.
  * Numbers of rows and positions above 2^31 - 1 are given as 2^31 - 1.
  * 16 <= page <= HEXI_PAGED_MAX_PAGE, a multiple of 16; n_pages * page < 2^31; columns * page <= HEXI_PAGED_MAX_TOKENS.
- * pos and slot may be NULL where n_rows is 0.  A page belongs to one request.
+ * pos and slot may be NULL where n_rows is 0.  A page belongs to one request.  What is written overlaps no other array (kv_len is not the next
+ * step's cached, for instance).
  */
 int hexi_paged_plan(int32_t page, int32_t n_pages, int32_t n_requests, const int32_t* cached, const int32_t* added,
                     int32_t* table, int32_t columns, int32_t* held, int32_t* free_list, int32_t* n_free,
@@ -356,7 +357,7 @@ int hexi_paged_write(const hexi_paged_cache* cache, const int32_t* slot, int64_t
  * are for contexts that are spread over devices, each with the cache of a part: partial results, joined by hexi_attn_merge_lse.)
  * desc: that of the ring step; its kv strides are not used.  q: [n_rows][n_q_heads][head_dim] with its strides.  table, columns: as in
  * hexi_paged_plan; an entry that is no page of the cache holds no keys.
- * o: [n_rows][n_q_heads][head_dim], dense, of o_dtype (HEXI_BF16: rounded once); lse: fp32 [n_q_heads][n_rows], or NULL.  Rows that see no key get
+ * o: [n_rows][n_q_heads][head_dim], dense, of o_dtype (HEXI_BF16: rounded once), not over q or the caches; lse: fp32 [n_q_heads][n_rows], or NULL.  Rows that see no key get
  * o = 0, lse = -INFINITY; rows in front of the first request's and behind the last one's are left as they are, and all of them where
  * row_start does not ascend from 0 or more to n_rows or less.  Lengths out of range count as the nearest that are not.  Values of keys that a row does not
  * see do not reach it, infinities and NaN included.  Results are reproducible run to run.

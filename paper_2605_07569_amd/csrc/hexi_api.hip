@@ -600,9 +600,12 @@ HEXI_EXPORT int hexi_paged_plan(int32_t page, int32_t n_pages, int32_t n_request
     if (rc != HEXI_OK) return rc;
     if (n_rows < 0 || n_rows > HEXI_PAGED_MAX_TOKENS) return fail(HEXI_EINVAL, "n_rows %lld outside 0..2^28", (long long)n_rows);
     if (!cached || !added || !table || !held || !free_list || !n_free || !row_start || !kv_len || (n_rows > 0 && (!pos || !slot))) return fail(HEXI_EINVAL, "null pointer");
-    for (const void* p : {(const void*)cached, (const void*)added, (const void*)table, (const void*)held, (const void*)free_list, (const void*)n_free, (const void*)row_start,
-                          (const void*)kv_len, (const void*)pos, (const void*)slot})
+    const void* const all[] = {cached, added, table, held, free_list, n_free, row_start, kv_len, pos, slot};
+    for (const void* p : all)
         if (!aligned4(p)) return fail(HEXI_EALIGN, "pointers must be 4-byte aligned");
+    for (int i = 2; i < 10; ++i)      // (from the third on they are written)
+        for (int j = 0; j < i; ++j)
+            if (all[i] && all[i] == all[j]) return fail(HEXI_EINVAL, "an array that is written is given twice");
     const PagedPlanArgs a = {cached, added, table, held, free_list, n_free, row_start, kv_len, pos, slot, n_requests, columns, n_pages, (int)n_rows, Divisor((unsigned)page)};
     const hipError_t e = hexi_launch_paged_plan(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return fail(HEXI_EHIP, "paged plan launch failed: %s", hipGetErrorString(e));
@@ -689,6 +692,7 @@ HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cac
     const size_t few_bytes = hexi_paged_workspace(shape, 0, desc->head_dim), need = few_bytes + hexi_paged_workspace(shape, 1, desc->head_dim);
     if (!workspace || workspace_bytes < need) return fail(HEXI_EWORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
     if (!aligned16(workspace)) return fail(HEXI_EALIGN, "the workspace must be 16-byte aligned");
+    if (o == q || o == k_cache || o == v_cache || o == (void*)lse || workspace == o || workspace == (void*)lse) return fail(HEXI_EINVAL, "a tensor that is written is given twice");
     g.table = table; g.row_start = row_start; g.kv_len = kv_len; g.q_start = q_start; g.kv_start = kv_start;
     g.stride_page = cache->stride_page; g.stride_head = cache->stride_head; g.stride_tok = cache->stride_tok;
     g.q_stride_tok = desc->q_stride_tok; g.q_stride_head = desc->q_stride_head;

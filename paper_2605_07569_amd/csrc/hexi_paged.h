@@ -124,7 +124,7 @@ struct PagedTile { int pieces, run, row0, rows, v0, range, pad[2]; };      // pi
 
 // Costs of a request's tiles, in units of 2^coarse blocks; before(t): of the first t tiles of a run, by the closed form of its sums, so that no table is needed.
 // Of tile t the last row sees keys up to at + (t + 1) vectors / most, and a window leaves out what the first one no longer sees.  The host sees to it that all costs of a launch together stay
-// below 2^31.
+// below 1.2e9.
 struct PagedShare { int shift, few, takes_few, takes_many, start, min_cost, coarse; };      // 2^shift vectors to a tile; limit of few vectors, and which requests are the kernel's; cost of a tile's start; the least of a range
 struct PagedCost {
     long long up, low, top;           // most x (keys up to the last row's own, of tile 0), most x (keys in front of its first row's window), most x kv
@@ -223,7 +223,9 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
         PagedShare& h = s.share[i];
         // as many workgroups as run at once: one to a CU where it takes the LDS, else two (24 requests of 16K, 128 columns: decoding 164 us with 256, 162 with 512, verifying 163 and 166; 64 columns: 96 and 92, 115 and 96)
         const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests), full = large || (dtype == HEXI_F32 && d == 128) ? 256 : 512;      // (below 2^31: rows x heads are at most 2^28)
-        while ((double)tiles * (double)((blocks >> h.coarse) + 1 + h.start) > 1e9) ++h.coarse;
+        auto most_cost = [&] { return (double)tiles * (double)((blocks >> h.coarse) + 1 + h.start); };
+        while (most_cost() > 1e9 && blocks >> h.coarse > 0) ++h.coarse;
+        if (most_cost() > 1e9) h.start = 1;      // (no more than 5.5e8 tiles: 64 runs, 65 heads in one of them, 2^21 rows)
         long long n = tiles > full ? full : tiles * (blocks + h.start) / h.min_cost + 1;
         n = n > full ? full : n;
         s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;

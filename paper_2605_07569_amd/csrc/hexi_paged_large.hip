@@ -7,7 +7,8 @@
 // What pages change is how a 64-key block comes to LDS.  A transfer (1 KB: 64 lanes x 16 bytes, back to back) takes its address from a scalar base, the page's, so all its rows have to lie on one page:
 // 4 whole rows (8 at 64 columns), and each wavefront takes the 16 rows of one page by itself.  Rows are not padded then but transfers are, by 16 bytes, and inside one
 // the 16-byte pieces of a row are exchanged by their high bits (`flip`), so that both the 128-bit row reads of K and the transposed 64-bit reads of V^T touch all 64 banks once (a 128-bit read is
-// served 16 lanes at a time, 0-3, 12-15, 20-23, 24-27 and so on, a transposed one 32 neighbouring lanes).
+// served 16 lanes at a time, 0-3, 12-15, 20-23, 24-27 and so on, a transposed one 32 neighbouring lanes; laid out for 16 neighbouring lanes a quarter of the LDS cycles and more were conflicts).
+// What bounds it: at 128 columns the chip's power, 2048 tokens over 32K keys, 24 / 8 heads, 728 us with the join, 1130 TFLOP/s, what the library's product reaches; at 64 columns vector issue (500 to 520 us, 800 TFLOP/s).
 #include "hexi_mfma.h"
 #include "hexi_paged_few.h"
 

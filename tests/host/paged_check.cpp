@@ -3,6 +3,7 @@
 //   place page columns n_pages key entry ...                                                     -> page id and row of a key
 //   ask page columns cached added held                                                           -> cached added want held keep
 //   cost most shift start coarse at rows kv window -> tiles, then before(t) of t = 0 .. tiles (of at most 200), and the tiles that these costs lie in
+//   shape dtype d n_runs most n_requests n_rows max_rows max_keys                                -> of both kernels: ranges entries shift start min_cost coarse
 //   runs nq nkv kv_of_q ...                                                                      -> "kvh:head,head" of every run, and the most heads of one
 #include <cstdio>
 #include <cstring>
@@ -55,6 +56,13 @@ int main()
             for (int t = 0; t <= tiles && t <= 200; ++t) std::printf(" %d", c.before(t));
             for (int t = 0; t < tiles && t < 200; ++t) std::printf(" %d %d", c.tile_of(c.before(t), tiles), c.tile_of(c.before(t + 1) - 1, tiles));
             std::printf("\n");
+        } else if (!std::strcmp(what, "shape")) {
+            int dtype, d, n_runs, most;
+            long long n_requests, n_rows, max_rows, max_keys;
+            if (std::scanf("%d %d %d %d %lld %lld %lld %lld", &dtype, &d, &n_runs, &most, &n_requests, &n_rows, &max_rows, &max_keys) != 8) return 1;
+            const PagedShape s = hexi_paged_shape(dtype, d, n_runs, most, n_requests, n_rows, max_rows, max_keys);
+            for (int i = 0; i < 2; ++i)
+                std::printf("%d %d %d %d %d %d%s", s.ranges[i], s.entries[i], s.share[i].shift, s.share[i].start, s.share[i].min_cost, s.share[i].coarse, i ? "\n" : " ");
         } else {
             int nq, nkv;
             signed char kv_of_q[HEXI_MAX_HEADS];

@@ -116,6 +116,30 @@ def test_costs_of_tiles_are_sums_and_lead_back_to_their_tiles(ask):
         assert back == [t for t in range(n) for _ in range(2)]
 
 
+def test_launches_of_any_size_keep_their_costs_in_32_bits(ask):
+    rng = random.Random(7)
+    asked = []
+    for _ in range(400):
+        nq = rng.choice([1, 8, 24, 128])
+        n_runs = rng.randint(1, nq)
+        most = rng.choice([-(-nq // n_runs), nq - n_runs + 1])      # even heads, or all but one of each in one run
+        n_rows = min(2 ** 28 // nq, rng.choice([1, 7, 2048, 2 ** 21, 2 ** 28]))
+        asked.append((rng.choice([0, 1]), rng.choice([64, 128]), n_runs, most, rng.choice([1, 2, 300, 8192]), n_rows, rng.choice([1, n_rows]), 16 * rng.choice([1, 4, 5, 2000, 2 ** 24])))
+    asked.append((0, 128, 64, 65, 8192, 2 ** 21, 1, 2 ** 28))
+    for case, line in zip(asked, ask(["shape " + " ".join(map(str, c)) for c in asked])):
+        _, _, n_runs, most, n_requests, n_rows, _, max_keys = case
+        x, used = list(map(int, line.split())), 0
+        for ranges, entries, shift, start, min_cost, coarse in (x[:6], x[6:]):
+            if ranges == 0:
+                continue
+            used += 1
+            tiles = n_runs * ((n_rows * most >> shift) + min(n_requests, n_rows))
+            assert ranges % 8 == 0 and 8 <= ranges <= 512 and entries == min(tiles, ranges) and start >= 1 and min_cost >= 1, case
+            total = tiles * (((-(-max_keys // 64) + 1) >> coarse) + 1 + start)
+            assert total + max(min_cost, -(-total // ranges)) < 2 ** 31, (case, line)
+        assert used, case
+
+
 def _codes(call, bad):
     for code, changes in bad:
         assert call(**changes) == code, (changes, hexi.hexi_last_error())
@@ -143,6 +167,8 @@ def test_plan_refusals():
 
     _codes(call, [(S, dict(page=0)), (S, dict(page=-16)), (S, dict(page=20)), (S, dict(page=1040)), (E, dict(n_pages=0)), (S, dict(n_pages=2 ** 27)), (E, dict(n=0)), (E, dict(n=8193)),
                   (E, dict(columns=0)), (S, dict(columns=2 ** 24 + 1)), (E, dict(n_rows=-1)), (E, dict(n_rows=2 ** 28 + 1))] + [(E, {k: None}) for k in names] + [(A, {k: 18}) for k in names])
+    apart = {k: 16 + 4 * i for i, k in enumerate(names)}
+    _codes(call, [(E, dict(apart, **{k: apart[m]})) for k in names[2:] for m in names if m != k])
 
 
 def test_write_refusals():
@@ -181,6 +207,8 @@ def test_attention_refusals():
             (E, dict(qs=(1024, 64))), (S, dict(qs=(2 ** 22 + 8, 128))), (A, dict(qs=(1028, 128))), (A, dict(qs=(1024, 132))), (S, dict(o_dtype=2))] +
            [(E, {p: None}) for p in ("table", "row_start", "kv_len", "q", "k", "v", "o")] + [(A, {p: 24}) for p in ("q", "k", "v", "o", "space")] +
            [(A, {p: 18}) for p in ("lse", "table", "row_start", "kv_len", "q_start", "kv_start")] + [(W, dict(space=None)), (W, dict(short=1))])
+    apart = dict(q=32, k=48, v=64, o=80, lse=96, space=112)
+    _codes(call, [(E, dict(apart, **{k: apart[m]})) for k, m in ("oq", "ok", "ov", ("o", "lse"), ("space", "o"), ("space", "lse"))])
     assert call(n_rows=0, table=None, q=None, o=None, space=None) == hexi.HEXI_OK
     desc, cache = descs()
     assert size(ctypes.byref(desc), ctypes.byref(cache), 4, 5, 0, 0) == 0 and size(None, None, 4, 5, 6, 0) == 0 and size(ctypes.byref(desc), ctypes.byref(cache), 0, 5, 6, 0) == 0
