@@ -707,7 +707,7 @@ HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cac
     hipStream_t s = (hipStream_t)hip_stream;
     hipError_t e = hipSuccess;
     if (shape.ranges[1]) e = hexi_launch_paged_large(a, large, desc->head_dim, s);
-    else e = hexi_launch_paged_few(a, desc->dtype, desc->head_dim, s);
+    else e = hexi_launch_paged_few(a, desc->dtype, desc->head_dim, shape.waves, s);
     if (e == hipSuccess) e = hexi_launch_paged_join(a, large, desc->head_dim, s);
     if (e != hipSuccess) return fail(HEXI_EHIP, "paged attention launch failed: %s", hipGetErrorString(e));
     return HEXI_OK;

@@ -205,6 +205,7 @@ struct PagedShape {
     PagedShare share[2];
     int ranges[2];            // workgroups, multiples of 8; 0: the kernel is not launched
     int entries[2];           // tiles there may be, no more than ranges
+    int waves;                // wavefronts of a workgroup for few vectors, where it is launched alone: 4, two workgroups to a CU, or 8, one
 };
 inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long long n_requests, long long n_rows, long long max_rows, long long max_keys)
 {
@@ -221,8 +222,12 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
     const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
     for (int i = 0; i < 2; ++i) {
         PagedShare& h = s.share[i];
-        // as many workgroups as run at once: one to a CU where it takes the LDS, else two (24 requests of 16K, 128 columns: decoding 164 us with 256, 162 with 512, verifying 163 and 166; 64 columns: 96 and 92, 115 and 96)
-        const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests), full = large || (dtype == HEXI_F32 && d == 128) ? 256 : 512;      // (below 2^31: rows x heads are at most 2^28)
+        const long long tiles = n_runs * ((n_rows * most >> h.shift) + most_requests);      // (below 2^31: rows x heads are at most 2^28)
+        // Eight wavefronts join less often and have half as many ranges, a longer way in and out and no neighbour to hide it: for long ranges of wide rows.  (128 columns, 64 requests of up to 8K, four / eight: decoding
+        // 213 / 202 us, 24 of 16K 159 / 156, verifying 170 / 163; 64 of 1K 45.4 / 47.5, one of 300 10.9 / 11.5.  64 columns: 126 / 128, 104 / 104, 94 / 99.)
+        if (i == 0) s.waves = dtype == HEXI_BF16 && d == 128 && tiles * blocks >= 64 * 256 ? 8 : 4;
+        // as many workgroups as run at once: one to a CU where it takes the LDS, else two (24 requests of 16K, four wavefronts, 128 columns: decoding 164 us with 256, 162 with 512; 64 columns: 96 and 92, verifying 115 and 96)
+        const long long full = large || s.waves == 8 || (dtype == HEXI_F32 && d == 128) ? 256 : 512;
         auto most_cost = [&] { return (double)tiles * (double)((blocks >> h.coarse) + 1 + h.start); };
         while (most_cost() > 1e9 && blocks >> h.coarse > 0) ++h.coarse;
         if (most_cost() > 1e9) h.start = 1;      // (no more than 5.5e8 tiles: 64 runs, 65 heads in one of them, 2^21 rows)
@@ -251,6 +256,6 @@ inline void hexi_paged_place(const PagedShape& s, int i, int d, char* workspace,
 
 hipError_t hexi_launch_paged_plan(const PagedPlanArgs& a, hipStream_t s);
 hipError_t hexi_launch_paged_write(const PagedWriteArgs& a, int x_dtype, int y_dtype, hipStream_t s);
-hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, hipStream_t s);
+hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, int waves, hipStream_t s);
 hipError_t hexi_launch_paged_large(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s);      // and few, where it has ranges
 hipError_t hexi_launch_paged_join(const PagedArgs& few, const PagedArgs& large, int d, hipStream_t s);

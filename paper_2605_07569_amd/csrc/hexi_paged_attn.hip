@@ -3,12 +3,12 @@
 
 namespace {
 
-template <class T, int D, int NG, bool FINE> __global__ void __launch_bounds__(256, sizeof(T) * D == 512 ? 1 : 2) paged_few_kernel(const PagedArgs a)
+template <class T, int D, int NG, bool FINE, int NW> __global__ void __launch_bounds__(64 * NW, sizeof(T) * D == 512 ? 1 : 2) paged_few_kernel(const PagedArgs a)
 {
-    __shared__ __attribute__((aligned(1024))) FewShared<T, D, NG, 4> sm;
-    __shared__ typename PagedWalk<256>::Shared shared;
+    __shared__ __attribute__((aligned(1024))) FewShared<T, D, NG, NW> sm;
+    __shared__ typename PagedWalk<64 * NW>::Shared shared;
     paged_touch<0>();
-    few_ranges<T, D, NG, FINE, 4, 0>(a, sm, shared);
+    few_ranges<T, D, NG, FINE, NW, 0>(a, sm, shared);
 }
 
 // The pieces of a tile joined, as hexi_attn_merge_lse joins two; `ways` workgroups to an entry.  Of a few pieces a thread takes four columns of a vector and reads them all; of many a workgroup takes
@@ -98,22 +98,24 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
     }
 }
 
-template <class T, int D, bool FINE> void launch_few(const PagedArgs& a, hipStream_t s)
+template <class T, int D, bool FINE, int NW> void launch_few(const PagedArgs& a, hipStream_t s)
 {
-    if (a.share.shift == 4) paged_few_kernel<T, D, 1, FINE><<<a.n_ranges, 256, 0, s>>>(a);
-    else paged_few_kernel<T, D, 2, FINE><<<a.n_ranges, 256, 0, s>>>(a);
+    if (a.share.shift == 4) paged_few_kernel<T, D, 1, FINE, NW><<<a.n_ranges, 64 * NW, 0, s>>>(a);
+    else paged_few_kernel<T, D, 2, FINE, NW><<<a.n_ranges, 64 * NW, 0, s>>>(a);
 }
 
 }  // namespace
 
-hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, hipStream_t s)
+hipError_t hexi_launch_paged_few(const PagedArgs& a, int dtype, int d, int waves, hipStream_t s)
 {
     if (dtype == HEXI_F32) {
-        if (d == 128) launch_few<float, 128, false>(a, s); else launch_few<float, 64, false>(a, s);
-    } else if (a.out_bf16) {
-        if (d == 128) launch_few<uint16_t, 128, false>(a, s); else launch_few<uint16_t, 64, false>(a, s);
-    } else if (d == 128) launch_few<uint16_t, 128, true>(a, s);
-    else launch_few<uint16_t, 64, true>(a, s);
+        if (d == 128) launch_few<float, 128, false, 4>(a, s); else launch_few<float, 64, false, 4>(a, s);
+    } else if (d == 64) {
+        if (a.out_bf16) launch_few<uint16_t, 64, false, 4>(a, s); else launch_few<uint16_t, 64, true, 4>(a, s);
+    } else if (waves == 8) {
+        if (a.out_bf16) launch_few<uint16_t, 128, false, 8>(a, s); else launch_few<uint16_t, 128, true, 8>(a, s);
+    } else if (a.out_bf16) launch_few<uint16_t, 128, false, 4>(a, s);
+    else launch_few<uint16_t, 128, true, 4>(a, s);
     return hipGetLastError();
 }
 
