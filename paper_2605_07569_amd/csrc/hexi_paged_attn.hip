@@ -16,7 +16,7 @@ template <class T, int D, int NG, bool FINE, int NW> __global__ void __launch_bo
 struct PagedJoin { PagedArgs a[2]; int ways[2]; };
 template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const PagedJoin)
 {
-    constexpr int D4 = D / 4, H4 = D4 / 2, G = 256 / H4, MAX = 512, FEW = 16;      // MAX: ranges, and so pieces
+    constexpr int D4 = D / 4, H4 = D4 / 2, G = 256 / H4, MAX = 512, FEW = 16, AT_ONCE = 4;      // MAX: ranges, and so pieces
     __shared__ float weight[MAX], reduced[4];
     __shared__ __attribute__((aligned(16))) float sum[G][D / 2];
     typedef const __attribute__((address_space(4))) PagedJoin* Ptr;
@@ -39,19 +39,39 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
         win_plain::store4(a.o, ((long long)(t.row0 + row) * g.nq + h) * D + c, a.out_bf16, o[0] * r, o[1] * r, o[2] * r, o[3] * r);
     };
     if (t.pieces <= FEW) {
+#pragma unroll 1
         for (int p = way * 256 + tid; p < vectors * D4; p += ways * 256) {
             const int i = p / D4, c = 4 * (p % D4);
             float m = -INFINITY, total = 0.f;
             f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-            for (int k = 0; k < t.pieces; ++k) m = fmaxf(m, a.part_lse[(long long)piece_of(k) * nv + i]);
-            if (m == -INFINITY) m = 0.f;          // no weight at all, or NaN alone
-#pragma unroll 4
-            for (int k = 0; k < t.pieces; ++k) {
-                const long long at = (long long)piece_of(k) * nv + i;
-                const float e = expf(a.part_lse[at] - m);
-                total += e;
-                o += e * *reinterpret_cast<const f32x4*>(a.part_o + at * D + c);
+            // (weights and values are asked for together: 64 requests of 1K 43.2 us, with a loop for the weights in front 44.1; 48 of 12K 209.9 and 211.2)
+#pragma unroll 1
+            for (int k = 0; k < t.pieces; k += AT_ONCE) {
+                float l[AT_ONCE];
+                f32x4 x[AT_ONCE];
+#pragma unroll
+                for (int e = 0; e < AT_ONCE; ++e) {
+                    const long long at = (long long)piece_of(k + e < t.pieces ? k + e : k) * nv + i;
+                    l[e] = a.part_lse[at];
+                    x[e] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + c);
+                }
+                float top = m;
+#pragma unroll
+                for (int e = 0; e < AT_ONCE; ++e) {
+                    if (k + e >= t.pieces) l[e] = -INFINITY;
+                    top = fmaxf(top, l[e]);
+                }
+                if (top == -INFINITY) top = 0.f;  // no weight at all, or NaN alone
+                const float old = k == 0 ? 0.f : expf(m - top);
+                total *= old;
+                o *= old;
+#pragma unroll
+                for (int e = 0; e < AT_ONCE; ++e) {
+                    const float w = expf(l[e] - top);
+                    total += w;
+                    o += w * x[e];
+                }
+                m = total == 0.f ? -INFINITY : top;
             }
             put(i, c, o, m, total);
         }
