@@ -68,6 +68,16 @@ def test_requests_on_the_same_pages(dtype, d, chunk, out):
         pu.within("lse", lse[:, starts[r]:starts[r + 1]], wl, bl)
 
 
+@pytest.mark.parametrize("dtype,rows", [(BF16, 1), (BF16, 150), (F32, 3)], ids=str)
+def test_as_many_requests_as_a_call_takes(dtype, rows):
+    """8192 requests, most of them without new rows; one of `rows` rows."""
+    lens = [((7 * i) % 90, 1 if i % 61 == 0 or i == 8191 else 0) for i in range(8192)]
+    lens[5003] = (200, rows)
+    s = Setup(Case("most", lens, nq=2), dtype, 64)
+    check(s, max_rows=rows)
+    check(s)
+
+
 def test_how_many_rows_a_request_has_may_be_said():
     c = Case("verify", [(500, 3), (64, 1), (33, 4), (200, 2)], nq=4, nkv=1)
     s = Setup(c, BF16, 128)
@@ -246,7 +256,7 @@ class Planner:
         return want
 
 
-@pytest.mark.parametrize("n,page,columns,pages,seed", [(1, 16, 1, 1, 1), (1, 16, 900, 1000, 2), (7, 48, 9, 30, 3), (64, 16, 40, 1500, 4), (700, 32, 12, 5000, 5), (1025, 16, 6, 4000, 6), (2049, 64, 4, 8000, 7)])
+@pytest.mark.parametrize("n,page,columns,pages,seed", [(1, 16, 1, 1, 1), (1, 16, 900, 1000, 2), (7, 48, 9, 30, 3), (64, 16, 40, 1500, 4), (700, 32, 12, 5000, 5), (1025, 16, 6, 4000, 6), (2049, 64, 4, 8000, 7), (8192, 16, 2, 9000, 8)])
 def test_plans_over_many_steps(n, page, columns, pages, seed):
     """Requests come, grow, lose tokens, end and are refused; the free list is empty at times."""
     rng = random.Random(seed)
