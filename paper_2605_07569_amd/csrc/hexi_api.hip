@@ -698,7 +698,7 @@ HEXI_EXPORT int hexi_paged_attn(const hexi_attn_desc* desc, const hexi_paged_cac
     g.q_stride_tok = desc->q_stride_tok; g.q_stride_head = desc->q_stride_head;
     g.n_pages = cache->n_pages;
     g.by_page = Divisor((unsigned)cache->page);
-    g.scale = desc->softmax_scale;
+    hexi_paged_scale(desc->softmax_scale, &a);
     a.q = q; a.k = k_cache; a.v = v_cache; a.o = o; a.lse = lse;
     a.out_bf16 = o_dtype == HEXI_BF16;
     PagedArgs large = a;

@@ -18,7 +18,7 @@ struct PagedGeom {
     int nq, n_runs, most;             // most: heads of the run that has most
     int regular;                      // run i: kv head i, heads i most .. i most + most - 1
     float scale;
-    double per_block;                 // 1 / (64 most)
+    Divisor by_most;
     // The q heads sorted by the kv head that they read: run i, heads head[first[i]] .. head[first[i + 1] - 1], reads kv head kvh[i].
     unsigned char kvh[HEXI_MAX_HEADS], head[HEXI_MAX_HEADS], first[HEXI_MAX_HEADS + 1];
 };
@@ -39,7 +39,7 @@ inline void hexi_paged_runs(const signed char* kv_of_q, int nq, int nkv, PagedGe
     }
     g->first[n] = (unsigned char)at;
     g->n_runs = n;
-    g->per_block = 1.0 / (64.0 * g->most);
+    g->by_most = Divisor((unsigned)g->most);
     g->regular = n * g->most == nq;
     for (int i = 0; i < nq; ++i) g->regular = g->regular && g->head[i] == i && (i >= n || g->kvh[i] == i);
 }
@@ -125,16 +125,16 @@ struct PagedTile { int pieces, run, row0, rows, v0, range, pad[2]; };      // pi
 // Costs of a request's tiles, in units of 2^coarse blocks; before(t): of the first t tiles of a run, by the closed form of its sums, so that no table is needed.
 // Of tile t the last row sees keys up to at + (t + 1) vectors / most, and a window leaves out what the first one no longer sees.  The host sees to it that all costs of a launch together stay
 // below 1.2e9.
-struct PagedShare { int shift, few, takes_few, takes_many, start, min_cost, coarse; };      // 2^shift vectors to a tile; limit of few vectors, and which requests are the kernel's; cost of a tile's start; the least of a range
+struct PagedShare { int shift, few, takes_few, takes_many, start, min_cost, coarse; double per_unit; };      // 2^shift vectors to a tile; limit of few vectors, and which requests are the kernel's; cost of a tile's start; the least of a range; 1 / (64 most 2^coarse)
 struct PagedCost {
     long long up, low, top;           // most x (keys up to the last row's own, of tile 0), most x (keys in front of its first row's window), most x kv
-    double per_unit;                  // 1 / (64 most 2^coarse)
+    double per_unit;
     int shift, start;                 // vectors of a tile: 2^shift; of every tile
     int up0, up1, low0, low1;         // tiles in front of those that see a key, and of those that see them all; of those with keys in front of the window, and with all there
     __host__ __device__ __attribute__((always_inline)) PagedCost(const PagedGeom& g, const PagedShare& s, const PagedRequest& q, int tiles)
     {
         shift = s.shift;
-        per_unit = g.per_block / (double)(1 << s.coarse);
+        per_unit = s.per_unit;
         start = s.start;
         top = (long long)g.most * q.kv;
         up = g.most * q.at + (1 << shift);
@@ -190,6 +190,7 @@ struct PagedArgs {
     void* o;
     float* lse;               // may be null
     int out_bf16;
+    float c_hi, c_lo, inv_c;  // scale x log2(e) as two floats, and the first one's inverse
     int n_ranges;
     int n_entries, by_tile;   // entries there is room for; whether they are the tiles'
     int* n_used;              // entries that are written
@@ -217,8 +218,8 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
     const bool few = !large || n_requests > 1;
     // A tile's start costs about what four blocks do (64 requests of 1K, one token each: 50.0 us with 1, 42.9 with 4, 44.7 with 8).  Ranges of few vectors may be as short as there are workgroups for them (one request
     // of 2K: 11.5 us, 13.5 with two blocks at least); shorter large ones than six gain nothing (512 tokens over 4K: 68.9 us with 3, 6 and 12, 72.0 with 24).
-    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 4, 1, 0};
-    s.share[1] = PagedShare{8, 16, !few, 1, 4, 6, 0};
+    s.share[0] = PagedShare{max_rows * most > 16 && !large ? 5 : 4, 16, 1, !large, 4, 1, 0, 0.0};
+    s.share[1] = PagedShare{8, 16, !few, 1, 4, 6, 0, 0.0};
     const long long blocks = (max_keys + 63) / 64 + 1, most_requests = n_requests < n_rows ? n_requests : n_rows;
     for (int i = 0; i < 2; ++i) {
         PagedShare& h = s.share[i];
@@ -231,12 +232,20 @@ inline PagedShape hexi_paged_shape(int dtype, int d, int n_runs, int most, long 
         auto most_cost = [&] { return (double)tiles * (double)((blocks >> h.coarse) + 1 + h.start); };
         while (most_cost() > 1e9 && blocks >> h.coarse > 0) ++h.coarse;
         if (most_cost() > 1e9) h.start = 1;      // (no more than 5.5e8 tiles: 64 runs, 65 heads in one of them, 2^21 rows)
+        h.per_unit = 1.0 / (64.0 * most * (double)(1 << h.coarse));
         long long n = tiles > full ? full : tiles * (blocks + h.start) / h.min_cost + 1;
         n = n > full ? full : n;
         s.ranges[i] = (i == 0 ? few : large) ? (int)((n + 7) / 8 * 8) : 0;
         s.entries[i] = (int)(tiles < s.ranges[i] ? tiles : s.ranges[i]);
     }
     return s;
+}
+inline void hexi_paged_scale(float scale, PagedArgs* a)
+{
+    a->g.scale = scale;
+    a->c_hi = scale * 1.4426950408889634f;
+    a->c_lo = (float)(scale * 1.4426950408889634 - (double)a->c_hi);
+    a->inv_c = 1.0f / a->c_hi;
 }
 inline size_t hexi_paged_workspace(const PagedShape& s, int i, int d)      // of one kernel
 {

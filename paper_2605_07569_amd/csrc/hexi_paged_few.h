@@ -159,7 +159,7 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
     const int grp = lane >> 4, l16 = lane & 15, sub = NB > 1 ? wave & 3 : wave;      // sub: which 16 keys of a block
     PagedWalk<64 * NW> walk(a, shared);
     if (!walk.any) return;
-    const float c_hi = g.scale * LOG2E_HI, c_lo = fmaf(g.scale, LOG2E_HI, -c_hi) + g.scale * LOG2E_LO, slack = SLACK / c_hi;
+    const float c_hi = a.c_hi, c_lo = a.c_lo, slack = SLACK * a.inv_c;
     Ring& ring = sm.ring[wave];
     const uint32_t lds_k = (uint32_t)(uintptr_t)&ring.k[0][0], lds_v = (uint32_t)(uintptr_t)&ring.v[0][0];
     // what the lane fetches: a row of every transfer and a piece of it
@@ -169,13 +169,15 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
     for (int x = 0; x < R::XFERS; ++x)
         fetch_off[x] = (uint32_t)(fetch_row * (int)g.stride_tok * (int)sizeof(T)) + 16u * (uint32_t)(fetch_place ^ R::swz(x * R::PER_XFER + fetch_row));
     Tile t;
-    while (walk.next(a, t)) {
+    while (walk.next(paged_args<WHICH>(), t)) {
+        const PagedArgs& a = paged_args<WHICH>();
+        const PagedGeom& g = a.g;
         // the lane's vectors; of one that is none the first one again
         WinKeys keys[NG];
         typename O::Q q[NG][O::NQ];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-            const int v = 16 * i + l16 < t.vectors ? 16 * i + l16 : 0, row = t.row_of(v);
+            const int v = 16 * i + l16 < t.vectors ? 16 * i + l16 : 0, row = t.row_of(g, v);
             keys[i] = paged_keys_of_row(g, t.q, row);
             O::vector(q[i], static_cast<const T*>(a.q) + (long long)(t.q.row0 + row) * g.q_stride_tok + (long long)t.head_of(g, v, row) * g.q_stride_head, grp);
         }
@@ -308,7 +310,7 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
             for (int x = 0; x < NW; ++x) sm.ends.stat[0][x][tid] = e[x] * r;
             int at = -1;
             if (tid < t.vectors) {
-                const int row = t.row_of(tid), h = t.head_of(g, tid, row);
+                const int row = t.row_of(g, tid), h = t.head_of(g, tid, row);
                 at = (int)paged_out(a, t, row, h);
                 if (t.piece >= 0) a.part_lse[(long long)t.piece * NV + tid] = lse;
                 else if (a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
@@ -326,7 +328,7 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
         }
         __syncthreads();                          // the rings are written again
     }
-    walk.done(a);
+    walk.done(paged_args<WHICH>());
 }
 
 }  // namespace

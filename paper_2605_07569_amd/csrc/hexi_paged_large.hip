@@ -16,7 +16,7 @@ namespace {
 
 constexpr int TN = PAGED_KEYS, NB = 4, GROUP = 128, WG = 256;      // keys of a block, buffers of either tensor, vectors of a group, of a tile
 constexpr int K_AHEAD = 4, V_AHEAD = 2;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_BIG = -1.0e30f;        // finite stand-in for "no key seen yet"
 constexpr float RESCALE_SLACK = 8.0f;
 constexpr float SUM_LO = 8.6736174e-19f, SUM_HI = 1.1529215e18f;      // 2^-60, 2^60
@@ -69,7 +69,7 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
     const int fetch_piece = ((fetch_pos / C::RUN) ^ C::flip(fetch_row)) * C::RUN + fetch_pos % C::RUN;
     const uint32_t fetch_off = 2u * (uint32_t)(fetch_row * (int)g.stride_tok + 8 * fetch_piece);
     const uint32_t fetch_lds = (grp ? lds_k : lds_v) + (uint32_t)(wg * C::PER_WAVE * C::XFER);
-    const float c_log2 = g.scale * LOG2E, inv_c_log2 = 1.0f / c_log2;
+    const float c_log2 = a.c_hi, inv_c_log2 = a.inv_c;
 
     PagedWalk<512> walk(a, shared);
     if (!walk.any) return;
@@ -78,13 +78,13 @@ template <int D, bool FINE> __device__ __forceinline__ void large_ranges(const P
         const int NT = t.b1 - t.b0, last = t.last;
         const int my_vector = GROUP * grp + 32 * wg + l32;
         const bool real = my_vector < t.vectors;
-        const int my_row = t.row_of(real ? my_vector : 0), my_head = t.head_of(g, real ? my_vector : 0, my_row);
+        const int my_row = t.row_of(g, real ? my_vector : 0), my_head = t.head_of(g, real ? my_vector : 0, my_row);
         WinKeys my_keys = {0, 0, 0};
         if (real) my_keys = paged_keys_of_row(g, t.q, my_row);
         // what the group's rows see of the blocks, and the range's first block that all of them see
         WinSpan<TN> span_g(WinKeys{0, 0, 0}, WinKeys{0, 0, 0}, 0);
         if (GROUP * grp < t.vectors)
-            span_g = WinSpan<TN>(paged_keys_of_row(g, t.q, t.row_of(GROUP * grp)), paged_keys_of_row(g, t.q, t.row_of((GROUP * (grp + 1) < t.vectors ? GROUP * (grp + 1) : t.vectors) - 1)), t.q.kv);
+            span_g = WinSpan<TN>(paged_keys_of_row(g, t.q, t.row_of(g, GROUP * grp)), paged_keys_of_row(g, t.q, t.row_of(g, (GROUP * (grp + 1) < t.vectors ? GROUP * (grp + 1) : t.vectors) - 1)), t.q.kv);
         span_g.full_sink = paged_uniform(span_g.full_sink); span_g.full_lo = paged_uniform(span_g.full_lo); span_g.full_hi = paged_uniform(span_g.full_hi);
         const int n_sink_blocks = paged_uniform(t.span.n_sink_blocks), skip = paged_uniform(t.span.skip), b0 = t.b0;
         auto block_of = [&](int i) { const int b = b0 + i; return b < n_sink_blocks ? b : b + skip; };

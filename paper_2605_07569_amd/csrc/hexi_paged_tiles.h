@@ -52,7 +52,7 @@ struct Tile {
     int b0, b1;                         // blocks of the span that are this range's
     int last;                           // no row sees a key behind this one; -1: none is seen, and there are no blocks
     int piece;                          // of the partial results; -1: the tile is this range's alone
-    __device__ __forceinline__ int row_of(int v) const { return (int)((unsigned)(v0 + v) / (unsigned)count); }
+    __device__ __forceinline__ int row_of(const PagedGeom& g, int v) const { return (int)(g.regular ? g.by_most((unsigned)(v0 + v)) : (unsigned)(v0 + v) / (unsigned)count); }
     __device__ __forceinline__ int head_of(const PagedGeom& g, int v, int row) const
     {
         const int i = v0 + v - row * count;
@@ -197,11 +197,13 @@ template <int NT> struct PagedWalk {
                 if (a.by_tile && threadIdx.x == 0) a.entries[number + run * tiles + tile] = open;
             }
             if (t.vectors <= 0) continue;
-            const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(t.vectors - 1)));
+            const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(g, 0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(g, t.vectors - 1)));
             t.span = WinSpan<PAGED_KEYS>(k0, k1, q.kv);
             t.last = k1.hi - 1;
             const int blocks = t.span.n_blocks;
-            auto block_at = [&](int x) { return paged_uniform((int)((double)x * (double)blocks / (double)size)); };
+            // (of two ranges that meet in a tile the one's end and the other's start: the same number by the same steps, and never falling)
+            const float per = (float)blocks * __builtin_amdgcn_rcpf((float)size);
+            auto block_at = [&](int x) { const int b = (int)((float)x * per); return paged_uniform(b < blocks ? b : blocks); };
             t.b0 = starts ? 0 : block_at(x0);
             t.b1 = ends ? blocks : block_at(x1);
             t.piece = starts && ends ? -1 : 2 * me + (starts ? 1 : 0);
@@ -229,7 +231,7 @@ template <class T, int D, int WHICH> __device__ __forceinline__ void plain_tile(
     const int* table = g.table + (long long)t.r * g.columns;
     const long long head = (long long)t.kv_head(g) * g.stride_head + col;
     for (int i = (int)threadIdx.x / win_plain::LANES; i < t.vectors; i += (int)blockDim.x / win_plain::LANES) {
-        const int row = t.row_of(i), h = t.head_of(g, i, row);
+        const int row = t.row_of(g, i), h = t.head_of(g, i, row);
         const WinKeys w = paged_keys_of_row(g, t.q, row);
         float q[N], acc[N];
         win_plain::load_cols(static_cast<const T*>(a.q) + (long long)(t.q.row0 + row) * g.q_stride_tok + (long long)h * g.q_stride_head + col, q);

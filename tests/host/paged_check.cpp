@@ -46,10 +46,10 @@ int main()
             const PagedAsk a = paged_ask(cached, added, held, page, g.columns);
             std::printf("%lld %lld %lld %d %d\n", a.cached, a.added, a.want, a.held, a.keep);
         } else if (!std::strcmp(what, "cost")) {
-            PagedShare sh = {0, 0, 1, 1, 0, 1, 0};
+            PagedShare sh = {0, 0, 1, 1, 0, 1, 0, 0.0};
             PagedRequest q = {0, 0, 0, 0, 0};
             if (std::scanf("%d %d %d %d %lld %d %d %d", &g.most, &sh.shift, &sh.start, &sh.coarse, &q.at, &q.rows, &q.kv, &g.window) != 8) return 1;
-            g.per_block = 1.0 / (64.0 * g.most);
+            sh.per_unit = 1.0 / (64.0 * g.most * (double)(1 << sh.coarse));
             const int tiles = paged_tiles(g, sh, q);
             const PagedCost c(g, sh, q, tiles);
             std::printf("%d", tiles);
