@@ -488,8 +488,13 @@ def make_paged_cache(cache):
     if cache.dim() != 4 or cache.stride(3) != 1:
         _refuse(f"a cache of [pages, heads, tokens, columns] with contiguous columns is needed, not {tuple(cache.shape)} with strides {cache.stride()}")
     n_pages, heads, page, d = cache.shape
-    s = cache.stride()
-    return hexi_paged_cache(_dtype(cache), d, heads, page, n_pages, s[0] if n_pages > 1 else heads * page * d, s[1] if heads > 1 else d, s[2])
+    s, dtype = cache.stride(), _dtype(cache)
+    return hexi_paged_cache(dtype, d, heads, page, n_pages, s[0] if n_pages > 1 else _any_stride(s[0], dtype, d, heads * page * d), s[1] if heads > 1 else _any_stride(s[1], dtype, d, d), s[2])
+
+
+def _any_stride(s, dtype, d, other):
+    """The stride of an axis of one element as it is where the library takes it, else another one."""
+    return s if d <= s <= 1 << 22 and s % (8 if dtype == HEXI_BF16 else 4) == 0 else other
 
 
 def paged_desc_for(q, cache, softmax_scale, kv_of_q=None):
@@ -498,11 +503,13 @@ def paged_desc_for(q, cache, softmax_scale, kv_of_q=None):
         _refuse(f"q of [rows, heads, columns] with contiguous columns and a cache of four axes are needed, not {tuple(q.shape)} with strides {q.stride()}, {tuple(cache.shape)}")
     if kv_of_q is not None and len(kv_of_q) != q.shape[1]:
         _refuse(f"kv_of_q: {len(kv_of_q)} entries for {q.shape[1]} heads")
-    return make_desc(_dtype(q), q.shape[2], q.shape[1], cache.shape[1], softmax_scale, _q_strides(q), (cache.shape[3], cache.shape[3]), kv_of_q)
+    dtype, (n, h, d), s = _dtype(q), q.shape, q.stride()
+    s = (s[0] if n > 1 else _any_stride(s[0], dtype, d, h * d), s[1] if h > 1 else _any_stride(s[1], dtype, d, d))
+    return make_desc(dtype, d, h, cache.shape[1], softmax_scale, s, (cache.shape[3], cache.shape[3]), kv_of_q)
 
 
 def _q_strides(q):
-    """Token and head stride; of an axis of one element any will do."""
+    """Token and head stride; of an axis of one element that of a dense tensor."""
     n, h, d = q.shape
     return (q.stride(0) if n > 1 else h * d, q.stride(1) if h > 1 else d)
 
@@ -549,6 +556,9 @@ def _caches(c, dev, k, v):
     """Addresses of the caches of keys and values that a descriptor describes."""
     heads, n_pages = c.n_kv_heads, c.n_pages
     shape, strides, dtype = (n_pages, heads, c.page, c.head_dim), (c.stride_page, c.stride_head, c.stride_tok, 1), _DTYPES.get(c.dtype)
+    if (k.dtype is dtype and k.shape == shape and k.get_device() == dev and k.stride() == strides
+            and v.dtype is dtype and v.shape == shape and v.get_device() == dev and v.stride() == strides):
+        return k.data_ptr(), v.data_ptr()
     for name, t in (("k_cache", k), ("v_cache", v)):
         if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or t.stride() != strides:
             if t.dtype is not dtype or t.shape != shape or any(n > 1 and x != y for n, x, y in zip(shape, t.stride(), strides)):
@@ -581,27 +591,40 @@ def hexi_paged_attn_workspace_bytes(desc, cache, n_requests, columns, n_rows, ma
     return int((_lib or load()).hexi_paged_attn_workspace_bytes(desc, cache, n_requests, columns, n_rows, max_rows))
 
 
+def _paged_attn_fits(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, o, dev):
+    """The tensors of hexi_paged_attn one by one."""
+    shape, strides, size = q.shape, q.stride(), table.shape
+    want = (shape[0] if shape else 0, desc.n_q_heads, desc.head_dim)
+    if shape != want or _dtype(q) != desc.dtype or strides != (desc.q_stride_tok, desc.q_stride_head, 1) and any(
+            n > 1 and x != y for n, x, y in zip(shape, strides, (desc.q_stride_tok, desc.q_stride_head, 1))):
+        _refuse(f"q: [rows, {desc.n_q_heads}, {desc.head_dim}] of type {desc.dtype} with the descriptor's strides is needed, not {tuple(shape)} {q.dtype} with strides {strides}")
+    if q.get_device() != dev:
+        _refuse(f"q is on {q.device}, not on the current GPU")
+    if len(size) != 2:
+        _refuse(f"table {tuple(size)}: two axes are needed")
+    _fits("o", o, want, _dtype(o), dev)
+    _caches(cache, dev, k_cache, v_cache)
+    _ints(dev, ("table", table, size[0] * size[1]), ("row_start", row_start, size[0] + 1), ("kv_len", kv_len, size[0]))
+
+
 def hexi_paged_attn(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, o, lse=None, max_rows=0, window=None, q_start=None, kv_start=None, workspace=None, stream=None):
     """Attention of the requests' new rows, q [rows, q heads, head_dim], over their cached keys.  table [requests, columns], row_start [requests + 1], kv_len, q_start, kv_start
     [requests]: int32 on the device; o's element type (fp32 or bf16) is the result's.  max_rows: no request has more rows (0: not known).  workspace: a tensor of at least
     hexi_paged_attn_workspace_bytes, not shared with a call that may run at the same time; None takes one from torch for the call."""
-    (dev, handle), shape, columns = _device_and_stream(stream), q.shape, table.shape
-    rows, nq, d = desc_shape = (shape[0] if shape else 0, desc.n_q_heads, desc.head_dim)
-    strides = q.stride()
-    if shape != desc_shape or _dtype(q) != desc.dtype or strides != (desc.q_stride_tok, desc.q_stride_head, 1) and any(
-            n > 1 and x != y for n, x, y in zip(shape, strides, (desc.q_stride_tok, desc.q_stride_head, 1))):
-        _refuse(f"q: [rows, {nq}, {d}] of type {desc.dtype} with the descriptor's strides is needed, not {tuple(shape)} {q.dtype} with strides {strides}")
-    if q.get_device() != dev:
-        _refuse(f"q is on {q.device}, not on the current GPU")
-    if len(columns) != 2:
-        _refuse(f"table {tuple(columns)}: two axes are needed")
-    r, columns = columns
-    o_type = _dtype(o)
-    _fits("o", o, desc_shape, o_type, dev)
+    (dev, handle), shape, size, i32, dtype, o_dtype, nq = _device_and_stream(stream), q.shape, table.shape, _int32, q.dtype, o.dtype, desc.n_q_heads
+    pages, strides = (cache.n_pages, cache.n_kv_heads, cache.page, cache.head_dim), (cache.stride_page, cache.stride_head, cache.stride_tok, 1)
+    # (written out, as in hexi_paged_plan; what is refused, or unusual and right, is looked at piece by piece)
+    if (len(shape) != 3 or len(size) != 2 or shape[1] != nq or shape[2] != desc.head_dim or _DTYPES.get(dtype) != desc.dtype or cache.dtype != desc.dtype or o_dtype not in _DTYPES
+            or q.stride() != (desc.q_stride_tok, desc.q_stride_head, 1) or q.get_device() != dev or o.shape != shape or o.get_device() != dev or not o.is_contiguous()
+            or k_cache.dtype is not dtype or k_cache.shape != pages or k_cache.stride() != strides or k_cache.get_device() != dev
+            or v_cache.dtype is not dtype or v_cache.shape != pages or v_cache.stride() != strides or v_cache.get_device() != dev
+            or table.dtype is not i32 or table.get_device() != dev or not table.is_contiguous()
+            or row_start.dtype is not i32 or row_start.numel() != size[0] + 1 or row_start.get_device() != dev or not row_start.is_contiguous()
+            or kv_len.dtype is not i32 or kv_len.numel() != size[0] or kv_len.get_device() != dev or not kv_len.is_contiguous()):
+        _paged_attn_fits(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, o, dev)
+    rows, (r, columns) = shape[0], size
     if lse is not None:
         _fits("lse", lse, (nq, rows), HEXI_F32, dev)
-    kc, vc = _caches(cache, dev, k_cache, v_cache)
-    a = _ints(dev, ("table", table, r * columns), ("row_start", row_start, r + 1), ("kv_len", kv_len, r))
     qs, ks = (None if t is None else _ints(dev, (name, t, r))[0] for name, t in (("q_start", q_start), ("kv_start", kv_start))) if q_start is not None or kv_start is not None else (None, None)
     lib, taken = _lib or load(), None
     if workspace is not None:
@@ -614,7 +637,8 @@ def hexi_paged_attn(desc, cache, table, row_start, kv_len, q, k_cache, v_cache, 
         else:
             space = taken = _take(lib, ws_bytes, dev, handle) if ws_bytes else None
     try:
-        rc = lib.hexi_paged_attn(desc, cache, window, r, a[0], columns, a[1], a[2], qs, ks, rows, max_rows, q.data_ptr(), kc, vc, o.data_ptr(), o_type, _ptr(lse), space, ws_bytes, handle)
+        rc = lib.hexi_paged_attn(desc, cache, window, r, table.data_ptr(), columns, row_start.data_ptr(), kv_len.data_ptr(), qs, ks, rows, max_rows, q.data_ptr(), k_cache.data_ptr(),
+                                 v_cache.data_ptr(), o.data_ptr(), _DTYPES[o_dtype], _ptr(lse), space, ws_bytes, handle)
     finally:
         if taken is not None:
             _torch.cuda.caching_allocator_delete(taken)

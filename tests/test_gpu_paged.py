@@ -235,6 +235,24 @@ def test_writes_are_exact(rows, nkv, d, page, x_dtype, dtype, layout):
     assert torch.equal(as_bits(k), as_bits(want_k)) and torch.equal(as_bits(v), as_bits(want_v)) and k.isnan().sum() == want_k.isnan().sum()
 
 
+def test_rows_heads_and_pages_of_one_whatever_their_strides():
+    k, v = (torch.randn(1, 1, 64, 128, device=DEV).to(BF16) for _ in range(2))
+    wide = torch.randn(7, 9, 128, device=DEV).to(BF16)
+    new_k, new_v = wide[3:4, 2:3].clone(), wide[3:4, 5:6]                # dense, and out of a fused row
+    cache = hexi.make_paged_cache(k)
+    hexi.hexi_paged_write(cache, ints([6]), new_k, new_v, k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(k[0, 0, 6], wide[3, 2]) and torch.equal(v[0, 0, 6], wide[3, 5])
+    desc = hexi.paged_desc_for(wide[3:4, 7:8], k, 0.1)
+    out = [torch.zeros(1, 1, 128, dtype=BF16, device=DEV) for _ in range(2)]
+    as_pages = lambda t: t.as_strided((1, 1, 64, 128), (3, 5, 128, 1))      # of axes of one element the strides say nothing
+    for o, q, kc, vc in ((out[0], wide[3:4, 7:8], k, v), (out[1], wide[3:4, 7:8].clone(), as_pages(k), as_pages(v))):
+        hexi.hexi_paged_attn(desc, cache, ints([[0]]), ints([0, 1]), ints([7]), q, kc, vc, o)
+    torch.cuda.synchronize()
+    w = torch.softmax(0.1 * (k[0, 0, :7].double() @ wide[3, 7].double()), 0) @ v[0, 0, :7].double()
+    assert torch.equal(out[0], out[1]) and (out[0][0, 0].double() - w).norm() <= 5e-3 * w.norm()
+
+
 # ---- plans ----
 
 class Planner:

@@ -235,6 +235,14 @@ def test_binding_refuses_what_does_not_fit_before_the_library_is_asked():
     tokens = hexi.make_paged_cache(z(10, 16, 2, 128, t=bf16).transpose(1, 2))
     assert (tokens.page, tokens.n_kv_heads, tokens.stride_page, tokens.stride_head, tokens.stride_tok) == (16, 2, 4096, 128, 256)
     assert refused(hexi.make_paged_cache, kc[0]) == E and refused(hexi.make_paged_cache, kc[..., ::2]) == E and refused(hexi.make_paged_cache, kc.half()) == S
+    # axes of one element: their strides as they are, where the library takes them
+    one = hexi.make_paged_cache(z(10, 2, 16, 128, t=bf16)[:1, :1])
+    assert (one.stride_page, one.stride_head, one.stride_tok) == (4096, 2048, 128)
+    assert hexi.make_paged_cache(z(10, 16, 4, 128, t=bf16).transpose(1, 2)[:, :1]).stride_head == 128 and hexi.make_paged_cache(z(3, 2, 16, 64, t=bf16).as_strided((3, 1, 16, 64), (2048, 4, 64, 1))).stride_head == 64
+    for q, strides in ((z(6, 8, 128, t=bf16)[:1], (1024, 128)), (z(6, 12, 128, t=bf16)[2:3, 4:], (1536, 128)), (z(1, 8, 128, t=bf16).as_strided((1, 8, 128), (12, 128, 1)), (1024, 128)),
+                       (z(5, 8, 128, t=bf16)[:, 3:4], (1024, 128)), (z(4, 128, t=bf16).as_strided((4, 1, 128), (128, 3, 1)), (128, 128))):
+        desc = hexi.paged_desc_for(q, z(10, q.shape[1], 16, 128, t=bf16), 0.1)
+        assert (desc.q_stride_tok, desc.q_stride_head) == strides
     new = z(6, 2, 128, t=bf16)
     write = dict(slot=z(6), k=new, v=new, k_cache=kc, v_cache=kc.clone())
     for change in ({}, dict(k=new[:, :1], v=new[:, :1]), dict(v=new[:5]), dict(v=new.float()), dict(v=z(6, 4, 128, t=bf16)[:, ::2]), dict(slot=z(5)), dict(k=new[..., :64], v=new[..., :64]), dict(k_cache=kc[:9]),
