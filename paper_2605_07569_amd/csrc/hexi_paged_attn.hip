@@ -12,13 +12,14 @@ template <class T, int D, int NG, bool FINE, int NW> __global__ void __launch_bo
 }
 
 // The pieces of a tile joined, as hexi_attn_merge_lse joins two; `ways` workgroups to an entry.  Of a few pieces a thread takes four columns of a vector and reads them all; of many a workgroup takes
-// half the columns of a vector at a time, 8 or 16 threads to them and the pieces dealt to the groups of these.
+// half the columns of a vector at a time, 8 or 16 threads to them and the pieces dealt to the groups of these.  What bounds it: a launch and waits that
+// follow each other (entry, weights and values): a token over 2900 keys in 46 pieces, with the kernel in front, 10.7 us in a graph, 11.2 where values are asked for behind the weights.
 struct PagedJoin { PagedArgs a[2]; int ways[2]; };
 template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const PagedJoin)
 {
-    constexpr int D4 = D / 4, H4 = D4 / 2, G = 256 / H4, MAX = 512, FEW = 16, AT_ONCE = 4;      // MAX: ranges, and so pieces
+    constexpr int D4 = D / 4, H4 = D4 / 2, G = 256 / H4, MAX = 512, FEW = 16, AT_ONCE = 4, EARLY = 8;      // MAX: ranges, and so pieces
     __shared__ float weight[MAX], reduced[4];
-    __shared__ __attribute__((aligned(16))) float sum[G][D / 2];
+    __shared__ __attribute__((aligned(16))) float sum[4][D / 2];
     typedef const __attribute__((address_space(4))) PagedJoin* Ptr;
     const PagedJoin& both = *(const PagedJoin*)(Ptr)__builtin_amdgcn_kernarg_segment_ptr();      // (indexed where it lies)
     const int n_few = both.a[0].n_entries * both.ways[0];
@@ -69,7 +70,7 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
                 for (int e = 0; e < AT_ONCE; ++e) {
                     const float w = expf(l[e] - top);
                     total += w;
-                    o += w * x[e];
+                    if (k + e < t.pieces) o += w * x[e];      // (0 x inf is NaN)
                 }
                 m = total == 0.f ? -INFINITY : top;
             }
@@ -79,6 +80,11 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
     }
     for (int part = way; part < 2 * vectors; part += ways) {
         const int i = part >> 1, c = (part & 1) * (D / 2) + 4 * (tid % H4), p0 = tid / H4;
+        auto value = [&](int p) { return *reinterpret_cast<const f32x4*>(a.part_o + ((long long)piece_of(p) * nv + i) * D + c); };
+        f32x4 x[EARLY];                           // the group's first pieces, on the way while the weights are formed
+#pragma unroll
+        for (int u = 0; u < EARLY; ++u)
+            if (G * u < t.pieces) x[u] = value(p0 + G * u < t.pieces ? p0 + G * u : 0);
         float m = -INFINITY;
         for (int p = tid; p < t.pieces; p += 256) {
             const float l = a.part_lse[(long long)piece_of(p) * nv + i];
@@ -104,14 +110,20 @@ template <int D> __global__ void __launch_bounds__(256) paged_join_kernel(const 
         __syncthreads();
         total = (reduced[0] + reduced[1]) + (reduced[2] + reduced[3]);
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 16
-        for (int p = p0; p < t.pieces; p += G) o += weight[p] * *reinterpret_cast<const f32x4*>(a.part_o + ((long long)piece_of(p) * nv + i) * D + c);
-        *reinterpret_cast<f32x4*>(&sum[p0][4 * (tid % H4)]) = o;
+#pragma unroll
+        for (int u = 0; u < EARLY; ++u)
+            if (p0 + G * u < t.pieces) o += weight[p0 + G * u] * x[u];
+#pragma unroll 4
+        for (int p = p0 + G * EARLY; p < t.pieces; p += G) o += weight[p] * value(p);
+#pragma unroll
+        for (int off = H4; off < 64; off *= 2)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
+        if (lane < H4) *reinterpret_cast<f32x4*>(&sum[wave][4 * lane]) = o;
         __syncthreads();
         if (tid < H4) {
-            o = *reinterpret_cast<const f32x4*>(&sum[0][4 * tid]);
-#pragma unroll
-            for (int k = 1; k < G; ++k) o += *reinterpret_cast<const f32x4*>(&sum[k][4 * tid]);
+            o = (*reinterpret_cast<const f32x4*>(&sum[0][4 * tid]) + *reinterpret_cast<const f32x4*>(&sum[1][4 * tid])) +
+                (*reinterpret_cast<const f32x4*>(&sum[2][4 * tid]) + *reinterpret_cast<const f32x4*>(&sum[3][4 * tid]));
             put(i, c, o, m, total);
         }
         __syncthreads();

@@ -127,6 +127,23 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype):
     assert got[0][alone].isnan().all() and want[0][alone].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)], ids=str)
+@pytest.mark.parametrize("n,rows", [(1, 1), (40, 1), (3, 70)])
+def test_infinite_values_that_are_seen_stay_infinite(dtype, d, n, rows):
+    """In tiles of one part and of few and many, in the first one and further back."""
+    s = Setup(Case("inf", [(3000 + r, rows) for r in range(n)], nq=2, nkv=1, page=64), dtype, d)
+    want, _ = s.run()
+    for r in range(n):
+        for key, column in ((5, 3), (1700, 4), (2900 - rows, 7)):
+            s.v_cache[s.table[r, key // 64], 0, key % 64, column] = INF if column != 4 else -INF
+    for out in (dtype, F32):
+        o, lse = s.run(out)
+        torch.cuda.synchronize()
+        assert (o[..., [3, 7]] == INF).all() and (o[..., 4] == -INF).all()
+        rest = [c for c in range(d) if c not in (3, 4, 7)]
+        assert (o[..., rest].double() - want[..., rest].double()).norm() <= 1e-2 * want[..., rest].double().norm() and lse.isfinite().all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=str)
 def test_entries_that_are_no_page_hold_no_keys(dtype):
     """A table whose entries are anything: the keys on pages that the cache does not have are not seen."""
