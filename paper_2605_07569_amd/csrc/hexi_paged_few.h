@@ -141,7 +141,7 @@ template <int N> __device__ __forceinline__ void wait_transfers() { asm volatile
 // LDS of a workgroup of NW wavefronts.
 template <class T, int D, int NG, int NW> struct FewShared {
     static constexpr int NV = 16 * NG, AHEAD = paged_ring(sizeof(T), D);      // vectors, blocks of a ring
-    struct Ends { float acc[NW][NV][D + 4], stat[3][NW][NV]; int out[NV]; };      // stat: reference, sum of P, sum of P as it was multiplied
+    struct Ends { float acc[NW][NV][D + 4], stat[3][NW][NV]; int again[NW]; };      // stat: reference, sum of P, sum of P as it was multiplied
     struct Ring { unsigned char k[AHEAD][Rows<T, D>::TILE], v[AHEAD][Rows<T, D>::TILE]; };
     union { Ring ring[NW]; Ends ends; };
 };
@@ -289,42 +289,42 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
                 }
         }
         // (a key that a vector does not see has P = 0, and 0 x inf is NaN: what is not finite is done again element by element, and so is what has keys on pages that the cache does not have)
-        if (__syncthreads_or(z != 0.f || bad)) {
-            plain_tile<T, D, WHICH>(t);
-            continue;
-        }
-        if (tid < NV) {                           // a vector's LSE, and what the wavefronts' sums of V are multiplied by
+        const bool mine = __any(z != 0.f || bad);
+        if (lane == 0) sm.ends.again[wave] = mine;
+        __syncthreads();
+        bool again = false;
+#pragma unroll
+        for (int x = 0; x < NW; ++x) again |= sm.ends.again[x] != 0;
+        constexpr int EACH = 64 * NW / NV;        // threads to a vector
+        const int i = tid / EACH;
+        if (again) plain_tile<T, D, WHICH>(t);
+        else if (i < t.vectors) {
             float mm = -INFINITY, sum = 0.f, used = 0.f, e[NW];
 #pragma unroll
-            for (int x = 0; x < NW; ++x) mm = fmaxf(mm, sm.ends.stat[0][x][tid]);
+            for (int x = 0; x < NW; ++x) mm = fmaxf(mm, sm.ends.stat[0][x][i]);
 #pragma unroll
             for (int x = 0; x < NW; ++x) {
                 // (d is -inf too where the two are finite and far apart: 0, whatever the sign of c_lo)
-                const float r = sm.ends.stat[0][x][tid], d = r - mm;
+                const float r = sm.ends.stat[0][x][i], d = r - mm;
                 e[x] = r == -INFINITY ? 0.f : fast_exp2(fmaf(d, c_hi, d == -INFINITY ? 0.f : d * c_lo));
-                sum += e[x] * sm.ends.stat[1][x][tid];
-                used += e[x] * sm.ends.stat[2][x][tid];
+                sum += e[x] * sm.ends.stat[1][x][i];
+                used += e[x] * sm.ends.stat[2][x][i];
             }
-            const float lse = sum == 0.f ? -INFINITY : fmaf(mm, g.scale, logf(sum)), r = used == 0.f ? 0.f : 1.0f / used;
+            const float r = used == 0.f ? 0.f : 1.0f / used;
+            const int row = t.row_of(g, i), h = t.head_of(g, i, row);
 #pragma unroll
-            for (int x = 0; x < NW; ++x) sm.ends.stat[0][x][tid] = e[x] * r;
-            int at = -1;
-            if (tid < t.vectors) {
-                const int row = t.row_of(g, tid), h = t.head_of(g, tid, row);
-                at = (int)paged_out(a, t, row, h);
-                if (t.piece >= 0) a.part_lse[(long long)t.piece * NV + tid] = lse;
-                else if (a.lse) a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
+            for (int c = 4 * (tid % EACH); c < D; c += 4 * EACH) {
+                f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < NW; ++x) o += e[x] * r * *reinterpret_cast<const f32x4*>(&sm.ends.acc[x][i][c]);
+                if (t.piece >= 0) win_plain::store4(a.part_o, ((long long)t.piece * NV + i) * D + c, false, o[0], o[1], o[2], o[3]);
+                else win_plain::store4(a.o, paged_out(a, t, row, h) * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
             }
-            sm.ends.out[tid] = at;
-        }
-        __syncthreads();
-        for (int p = tid; p < t.vectors * (D / 4); p += 64 * NW) {       // four columns of a vector
-            const int i = p / (D / 4), c = 4 * (p % (D / 4));
-            f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < NW; ++x) o += sm.ends.stat[0][x][i] * *reinterpret_cast<const f32x4*>(&sm.ends.acc[x][i][c]);
-            if (t.piece >= 0) win_plain::store4(a.part_o, ((long long)t.piece * NV + i) * D + c, false, o[0], o[1], o[2], o[3]);
-            else win_plain::store4(a.o, (long long)sm.ends.out[i] * D + c, a.out_bf16, o[0], o[1], o[2], o[3]);
+            if (tid % EACH == 0 && (t.piece >= 0 || a.lse)) {
+                const float lse = sum == 0.f ? -INFINITY : fmaf(mm, g.scale, logf(sum));
+                if (t.piece >= 0) a.part_lse[(long long)t.piece * NV + i] = lse;
+                else a.lse[(long long)h * g.n_rows + t.q.row0 + row] = lse;
+            }
         }
         __syncthreads();                          // the rings are written again
     }

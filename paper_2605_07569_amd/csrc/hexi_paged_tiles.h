@@ -80,6 +80,7 @@ template <int NT> struct PagedWalk {
     int at, end, first, range;          // costs; first: in front of request r
     int of_run;                         // of a run of it
     int r, me, tiles;                   // tiles of a run of it
+    int run, tile, tile_at;             // the tile that the range goes on with, and the cost in front of it
     int number;                         // tiles in front of it
     PagedRequest q;
     PagedTile open;                     // the tile that the range starts and does not end
@@ -90,23 +91,23 @@ template <int NT> struct PagedWalk {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (g.n_requests + NT - 1) / NT, r0 = tid * each < g.n_requests ? tid * each : g.n_requests, r1 = r0 + each < g.n_requests ? r0 + each : g.n_requests;
         PagedRequest x = {0, 0, 0, 0, 0};
-        int mine = 0, mine_tiles = 0, run = 0, n = 0, before = 0, total = 0, before_tiles = 0, all_tiles = 0;
+        int mine = 0, mine_tiles = 0, run_cost = 0, n = 0, before = 0, total = 0, before_tiles = 0, all_tiles = 0;
         bool bad = false;                   // row starts that do not ascend within the rows: nothing is computed (and all sums below are of rows that there are)
         auto look = [&](int i) {
             x = paged_request(g, i);
             bad |= g.row_start[i] != x.row0 || g.row_start[i + 1] < x.row0 || g.row_start[i + 1] > g.n_rows;
             n = paged_tiles(g, a.share, x);
-            run = paged_cost(g, a.share, x, n);
+            run_cost = paged_cost(g, a.share, x, n);
         };
         if (g.n_requests == 1) {
             look(0);
-            total = bad ? 0 : run * g.n_runs;
+            total = bad ? 0 : run_cost * g.n_runs;
             all_tiles = bad ? 0 : n * g.n_runs;
         } else {
 #pragma unroll 1
             for (int i = r0; i < r1; ++i) {
                 look(i);
-                mine += run * g.n_runs;
+                mine += run_cost * g.n_runs;
                 mine_tiles += n * g.n_runs;
             }
             before = paged_sum_to(mine);
@@ -143,46 +144,43 @@ template <int NT> struct PagedWalk {
 #pragma unroll 1
                     for (;; ++i) {
                         look(i);
-                        if (at < before + run * g.n_runs) break;
-                        before += run * g.n_runs;
+                        if (at < before + run_cost * g.n_runs) break;
+                        before += run_cost * g.n_runs;
                         before_tiles += n * g.n_runs;
                     }
-                sh.first = before; sh.of_run = run; sh.r = i; sh.tiles = n; sh.number = before_tiles; sh.q = x;
+                sh.first = before; sh.of_run = run_cost; sh.r = i; sh.tiles = n; sh.number = before_tiles; sh.q = x;
             }
             __syncthreads();
-            before = sh.first; run = sh.of_run; i = sh.r; n = sh.tiles; before_tiles = sh.number; x = sh.q;
+            before = sh.first; run_cost = sh.of_run; i = sh.r; n = sh.tiles; before_tiles = sh.number; x = sh.q;
         } else i = 0;
         first = paged_uniform(before);
-        of_run = paged_uniform(run);
+        of_run = paged_uniform(run_cost);
         r = paged_uniform(i);
         tiles = paged_uniform(n);
         number = paged_uniform(before_tiles);
         q = paged_uniform(x);
         open.pieces = 0;
+        const int in = at - first;
+        run = g.n_runs == 1 ? 0 : paged_uniform((int)((unsigned)in / (unsigned)of_run));
+        tile = 0;
+        tile_at = first + run * of_run;
+        if (tiles > 1) {
+            const PagedCost cost(g, a.share, q, tiles);
+            tile = paged_uniform(cost.tile_of(in - run * of_run, tiles));
+            tile_at += paged_uniform(cost.before(tile));
+        }
     }
     // The next tile of the range that has vectors, and the part of it that is the range's.
     __device__ __forceinline__ bool next(const PagedArgs& a, Tile& t)
     {
         const PagedGeom& g = a.g;
         while (at < end) {
-            const int in = at - first;
-            if (in >= of_run * g.n_runs) {
-                first += of_run * g.n_runs;
-                number += tiles * g.n_runs;
-                q = paged_uniform(paged_request(g, ++r));
-                tiles = paged_uniform(paged_tiles(g, a.share, q));
-                of_run = paged_uniform(paged_cost(g, a.share, q, tiles));
-                continue;
-            }
-            const int run = g.n_runs == 1 ? 0 : paged_uniform((int)((unsigned)in / (unsigned)of_run));
-            int tile = 0, c0 = 0, size = of_run;
+            int size = of_run;
             if (tiles > 1) {
                 const PagedCost cost(g, a.share, q, tiles);
-                tile = paged_uniform(cost.tile_of(in - run * of_run, tiles));
-                c0 = paged_uniform(cost.before(tile));
-                size = paged_uniform(cost.before(tile + 1)) - c0;
+                size = paged_uniform(cost.before(tile + 1)) - paged_uniform(cost.before(tile));
             }
-            const int tile_at = first + run * of_run + c0, x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
+            const int x0 = at - tile_at, x1 = (end < tile_at + size ? end : tile_at + size) - tile_at;
             at = tile_at + x1;
             t.q = q;
             t.r = r;
@@ -196,9 +194,28 @@ template <int NT> struct PagedWalk {
                 open = PagedTile{ends || t.vectors <= 0 ? 0 : paged_uniform((int)((unsigned)(tile_at + size - 1) / (unsigned)range)) - me + 1, t.run, q.row0, q.rows, t.v0, me, {0, 0}};
                 if (a.by_tile && threadIdx.x == 0) a.entries[number + run * tiles + tile] = open;
             }
+            if (ends) {                                    // on to the next one
+                tile_at = at;
+                if (++tile == tiles) {
+                    tile = 0;
+                    if (++run == g.n_runs) {
+                        run = 0;
+                        if (at < end)
+                            do {
+                                number += tiles * g.n_runs;
+                                q = paged_uniform(paged_request(g, ++r));
+                                tiles = paged_uniform(paged_tiles(g, a.share, q));
+                            } while (tiles == 0);
+                        of_run = paged_uniform(paged_cost(g, a.share, q, tiles));
+                    }
+                }
+            }
             if (t.vectors <= 0) continue;
-            const WinKeys k0 = paged_uniform(paged_keys_of_row(g, q, t.row_of(g, 0))), k1 = paged_uniform(paged_keys_of_row(g, q, t.row_of(g, t.vectors - 1)));
-            t.span = WinSpan<PAGED_KEYS>(k0, k1, q.kv);
+            const int row0 = t.row_of(g, 0), row1 = t.row_of(g, t.vectors - 1);
+            const WinKeys k0 = paged_uniform(paged_keys_of_row(g, t.q, row0));
+            WinKeys k1 = k0;
+            if (row1 != row0) k1 = paged_uniform(paged_keys_of_row(g, t.q, row1));
+            t.span = WinSpan<PAGED_KEYS>(k0, k1, t.q.kv);
             t.last = k1.hi - 1;
             const int blocks = t.span.n_blocks;
             // (of two ranges that meet in a tile the one's end and the other's start: the same number by the same steps, and never falling)
