@@ -6,7 +6,7 @@
 //   O^T[column][vector] = V^T P^T   P as it stands is the operand; V^T by transposed reads (bf16), or row pieces whose columns are dealt to the products (fp32).
 // P as an operand: bf16 where results are bf16 (FINE off: a weight is off by at most 2^-8 of itself, less than the result's own rounding in all), three bf16 values where they are fp32
 // (2^-24: partial results of a context on several devices; with two they were off by 1.7e-6, relative L2, where fp32 sums are by 5e-7); the sum that normalises is that of the weights as they are multiplied.
-// What bounds it: few vectors a key, so the reads of K and V: 48 tokens, 24 / 8 heads x 128, over up to 12K keys 194 us alone, 5.6 TB/s; one token over 2900 keys 6.8 us, waits that follow each other.  (Keys held
+// What bounds it: few vectors a key, so the reads of K and V: 48 tokens, 24 / 8 heads x 128, over up to 12K keys 192 us alone, 5.7 TB/s; one token over 2900 keys 6.7 us, waits that follow each other.  (Keys held
 // in registers on the way, with waits by the compiler: a verifying batch 116 us, through the ring 108.)
 #pragma once
 #include "hexi_f32_common.h"
@@ -272,7 +272,7 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
             }
         }
 
-        // the wavefronts' results joined
+        // the wavefronts' results joined: one vote and three barriers in all, every thread forms the weights of its own vector (256 tokens over up to 300 keys 69.7 us; with weights formed by one thread a vector, for all, 74.4)
         __syncthreads();                          // all rings are free
         float z = 0.f;
 #pragma unroll
