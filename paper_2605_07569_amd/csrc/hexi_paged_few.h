@@ -272,7 +272,7 @@ __device__ __forceinline__ void few_ranges(const PagedArgs& a, FewShared<T, D, N
             }
         }
 
-        // the wavefronts' results joined: one vote and three barriers in all, every thread forms the weights of its own vector (256 tokens over up to 300 keys 69.7 us; with weights formed by one thread a vector, for all, 74.4)
+        // the wavefronts' results joined: one vote and three barriers in all, every thread forms the weights of its own vector (256 tokens over up to 300 keys 69.7 us; formed by one thread a vector for all, and with a search for the next tile, 74.4)
         __syncthreads();                          // all rings are free
         float z = 0.f;
 #pragma unroll

@@ -77,8 +77,8 @@ __device__ __forceinline__ int paged_sum_to(int x)
 // a step of single tokens waits for this.)
 template <int NT> struct PagedWalk {
     struct Shared { int of_wave[NT / 64], tiles_of_wave[NT / 64], first, of_run, r, tiles, number; PagedRequest q; };
-    int at, end, first, range;          // costs; first: in front of request r
-    int of_run;                         // of a run of it
+    int at, end, range;                 // costs
+    int of_run;                         // of a run of request r
     int r, me, tiles;                   // tiles of a run of it
     int run, tile, tile_at;             // the tile that the range goes on with, and the cost in front of it
     int number;                         // tiles in front of it
@@ -153,7 +153,7 @@ template <int NT> struct PagedWalk {
             __syncthreads();
             before = sh.first; run_cost = sh.of_run; i = sh.r; n = sh.tiles; before_tiles = sh.number; x = sh.q;
         } else i = 0;
-        first = paged_uniform(before);
+        const int first = paged_uniform(before);      // cost in front of the request
         of_run = paged_uniform(run_cost);
         r = paged_uniform(i);
         tiles = paged_uniform(n);
